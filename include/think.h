@@ -321,6 +321,120 @@ thinK_status thinK_device_error(thinK_cache* c, int32_t* out_code);
 
 thinK_status thinK_destroy(thinK_cache* c);
 
+/* ---------------------------------------------------------------------------------------------------------
+ * Paged key-value cache: the unpruned side of a serving process.  (The paper has no counterpart; its App. C.1
+ * runs ThinK next to a quantised cache.)  Sequences whose keys are not (or not yet) thinned live in a pool of
+ * pages; their lengths and page tables are DEVICE arrays, so a captured graph serves any batch.  A prompt that
+ * is to be thinned is read back (thinK_paged_read) into the tensors thinK_prefill takes.
+ *
+ * A page holds 64 tokens of every layer and key head.  The pool is [L][num_pages][N_kv] blocks; a block is
+ *     64 key rows | 64 value rows | scales of the 64 key rows | scales of the 64 value rows
+ * and a row is the D channels of one token in order (no swizzle, no padding):
+ *   THINK_PAGE_PLAIN  the elements themselves (cfg.dtype), no scales.
+ *   THINK_PAGE_E4M3   one e4m3 byte per channel, one scale byte per row: byte e stands for 2^(e - 127).  Written
+ *                     rows use the smallest power of two >= 2^-126 under which the row's largest magnitude is at
+ *                     most 448; codes are x / scale rounded to nearest even.  bf16 caches only.
+ *   THINK_PAGE_INT4   4 bits per channel (the even channel of a pair in the low half of the byte), code = n + 8,
+ *                     one bf16 scale per 32 channels, channel groups in order: s = amax / 7 rounded to bf16,
+ *                     n = x / s rounded to nearest even and limited to [-7, 7]; s = 0 gives n = 0.  bf16 caches only.
+ * A row (E4M3) or a group of 32 channels (INT4) that holds a NaN or an infinity is stored so that all of it reads
+ * back as NaN, and sets bit 8 of the device error word.
+ *
+ * Sequence b of a call owns row b of the page table: its token t lies in page table[b * table_stride + t / 64],
+ * slot t % 64.  Only the entries that a call needs are read, and what lies in a page outside of the tokens a call
+ * names is never looked at (it may hold NaN) nor changed.  The host cannot see table, lengths and positions: an
+ * entry outside [0, num_pages), a position outside [0, 64 * max_pages), a length above 64 * max_pages or a row
+ * count above max_rows sets bit 16 of the error word; the tokens concerned are left out (not written, not read,
+ * no weight in the softmax), and lengths and counts are cut to the limit.  Negative lengths and counts mean zero.
+ *
+ * A handle is constant after creation apart from its error word: calls that write different pages, or only read,
+ * may run at the same time on any streams of its device, except that attention calls need a scratch buffer each
+ * (see thinK_paged_decode_attn).  Calls enqueue on `stream`, which must belong to the device that was current
+ * when the handle was created; that device must be current in every call. */
+typedef enum { THINK_PAGE_PLAIN = 0, THINK_PAGE_E4M3 = 1, THINK_PAGE_INT4 = 2 } thinK_page_format;
+
+typedef struct {
+  int32_t L;             /* layers held by the pool */
+  int32_t N_q, N_kv;     /* N_q % N_kv == 0, group size N_q / N_kv from 1 to 8 */
+  int32_t D;             /* head dimension: 64 or 128 */
+  int32_t num_pages;     /* pages of the pool */
+  int32_t max_batch;     /* sequences a call may name, at most 4096 */
+  int32_t dtype;         /* thinK_dtype of rows, queries and outputs */
+  int32_t page_format;   /* thinK_page_format */
+  double softmax_scale;  /* factor on q.k; 0 means 1/sqrt(D) */
+} thinK_paged_config;
+
+typedef struct {
+  size_t pages;          /* bytes of the pool: L * num_pages * N_kv * block */
+  size_t workspace;      /* bytes of the workspace, and of a scratch buffer */
+  size_t block;          /* bytes of one (layer, page, key head) block */
+} thinK_paged_sizes;
+
+/* Page table of a call (device memory, int32 [B][table_stride], the first max_pages entries of a row usable). */
+typedef struct {
+  const int32_t* table;
+  int64_t table_stride;  /* in entries, >= max_pages */
+  int32_t max_pages;
+  int32_t B;             /* sequences of this call, 1 <= B <= max_batch */
+} thinK_page_table;
+
+typedef struct thinK_paged thinK_paged; /* opaque, host side */
+
+thinK_status thinK_paged_bytes(const thinK_paged_config* cfg, thinK_paged_sizes* out);
+
+/* Builds the host-side handle; zeroes the counters in `workspace` (synchronously) and leaves `pages` alone.  `sizes`
+ * (host) states the bytes allocated for the two buffers (256-byte aligned), THINK_ERR_CAPACITY if too few.  The
+ * buffers stay valid until thinK_paged_destroy. */
+thinK_status thinK_paged_create(const thinK_paged_config* cfg, const thinK_paged_sizes* sizes, void* pages,
+                                void* workspace, thinK_paged** out);
+
+/* Parts of a block, for thinK_paged_offset. */
+typedef enum { THINK_PART_K = 0, THINK_PART_V = 1, THINK_PART_K_SCALE = 2, THINK_PART_V_SCALE = 3 } thinK_page_part;
+
+/* Byte offset in the pool of a token's row (or of its scales) in the given part, for programs that move pages
+ * themselves; -1 if anything is out of range or the format has no such part. */
+int64_t thinK_paged_offset(const thinK_paged_config* cfg, int32_t layer, int32_t page, int32_t head, int32_t slot,
+                           int32_t part);
+
+/* Writes rows to their pages, quantising them.  k, v: [B, max_rows, nlayers, N_kv, D] views; layer index i of the
+ * views is layer layer0 + i of the pool.  Row s < rows[b] of entry b becomes token pos[b] + s.
+ *   pos, rows: device int32 [B]; NULL means 0 for all, max_rows for all.
+ * One-token appends (max_rows = 1, pos = the lengths so far) and whole prompts use the same call.  Rows at and
+ * behind rows[b] are not read.  No two rows of a call may go to the same slot of the same page (what that slot
+ * holds afterwards is unspecified). */
+thinK_status thinK_paged_write(thinK_paged* p, thinK_tensor5 k, thinK_tensor5 v, thinK_page_table table,
+                               const int32_t* pos, const int32_t* rows, int32_t max_rows, int32_t layer0,
+                               int32_t nlayers, void* stream);
+
+/* Reads rows back: the reverse of thinK_paged_write, same arguments; k and v are written.  Values are the stored
+ * ones rounded to cfg.dtype (E4M3: exact; INT4: n * s to nearest even).  Rows at and behind rows[b] of the views, and
+ * rows whose page is out of range, are left as they were. */
+thinK_status thinK_paged_read(thinK_paged* p, thinK_tensor5 k, thinK_tensor5 v, thinK_page_table table,
+                              const int32_t* pos, const int32_t* rows, int32_t max_rows, int32_t layer0,
+                              int32_t nlayers, void* stream);
+
+/* Attention of one new token per sequence over its first seq_len[b] tokens (append the token's own key and value
+ * first): out = softmax(softmax_scale * q K^T) V for every query head, head h of the queries reading key head
+ * h / (N_q / N_kv).
+ *   q, out: dense [B, nlayers, N_q, D] in cfg.dtype, not overlapping.
+ *   lse:    fp32 [B, nlayers, N_q], the natural logarithm of the softmax's sum (for joining with attention over
+ *           other tokens), or NULL.
+ *   seq_len: device int32 [B].  A sequence without tokens gets out = 0 and lse = -infinity.
+ *   scratch: NULL for the handle's own workspace, or a device buffer of scratch_bytes >= thinK_paged_sizes.workspace,
+ *           256-byte aligned, that was filled with zeros once before its first use (a call leaves it ready for the
+ *           next).  Calls that may run at the same time - on two streams, or as two captured graphs - need a scratch
+ *           buffer each.
+ * Logits, softmax sums and outputs are accumulated in fp32.  Results do not depend on timing: partial results are
+ * joined in token order. */
+thinK_status thinK_paged_decode_attn(thinK_paged* p, const void* q, void* out, float* lse, thinK_page_table table,
+                                     const int32_t* seq_len, void* scratch, size_t scratch_bytes, int32_t layer0,
+                                     int32_t nlayers, void* stream);
+
+/* The handle's error word (bits 8 and 16 above), read with a synchronous copy. */
+thinK_status thinK_paged_device_error(thinK_paged* p, int32_t* out_code);
+
+thinK_status thinK_paged_destroy(thinK_paged* p);
+
 #ifdef __cplusplus
 }
 #endif

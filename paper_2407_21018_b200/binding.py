@@ -29,6 +29,10 @@ SCORE_QUERY_DRIVEN, SCORE_KEY_L2, SCORE_KEY_L1 = 0, 1, 2
 VALUE_SCORE_AUTO, VALUE_SCORE_MMA_SYNC = 0, 1
 ERR_BIT_TOKEN_RANGE, ERR_BIT_WAIT_TIMEOUT, ERR_BIT_SMEM_ALIGN, ERR_BIT_NON_FINITE = 1, 2, 4, 8
 TILE_TOKENS = 64
+PAGE_PLAIN, PAGE_E4M3, PAGE_INT4 = 0, 1, 2
+PART_K, PART_V, PART_K_SCALE, PART_V_SCALE = range(4)
+ERR_BIT_PAGE = 16
+PAGE_TOKENS = 64
 
 
 class Config(C.Structure):
@@ -47,6 +51,19 @@ class Sizes(C.Structure):
     _fields_ = [("k_thin", C.c_size_t), ("tail_k", C.c_size_t), ("tail_v", C.c_size_t), ("idx", C.c_size_t),
                 ("scores", C.c_size_t), ("workspace", C.c_size_t), ("model_think_bytes", C.c_size_t),
                 ("model_dense_bytes", C.c_size_t), ("v_thin", C.c_size_t), ("perm_v", C.c_size_t)]
+
+
+class PagedConfig(C.Structure):
+    _fields_ = [("L", C.c_int32), ("N_q", C.c_int32), ("N_kv", C.c_int32), ("D", C.c_int32), ("num_pages", C.c_int32),
+                ("max_batch", C.c_int32), ("dtype", C.c_int32), ("page_format", C.c_int32), ("softmax_scale", C.c_double)]
+
+
+class PagedSizes(C.Structure):
+    _fields_ = [("pages", C.c_size_t), ("workspace", C.c_size_t), ("block", C.c_size_t)]
+
+
+class PageTable(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("table_stride", C.c_int64), ("max_pages", C.c_int32), ("B", C.c_int32)]
 
 
 EXPORTS = {
@@ -74,6 +91,18 @@ EXPORTS = {
     "thinK_tail_len": (C.c_int32, [C.c_void_p, C.c_int32]),
     "thinK_device_error": (C.c_int, [C.c_void_p, C.POINTER(C.c_int32)]),
     "thinK_destroy": (C.c_int, [C.c_void_p]),
+    "thinK_paged_bytes": (C.c_int, [C.POINTER(PagedConfig), C.POINTER(PagedSizes)]),
+    "thinK_paged_create": (C.c_int, [C.POINTER(PagedConfig), C.POINTER(PagedSizes), C.c_void_p, C.c_void_p,
+                                     C.POINTER(C.c_void_p)]),
+    "thinK_paged_offset": (C.c_int64, [C.POINTER(PagedConfig)] + [C.c_int32] * 5),
+    "thinK_paged_write": (C.c_int, [C.c_void_p, Tensor5, Tensor5, PageTable, C.c_void_p, C.c_void_p, C.c_int32,
+                                    C.c_int32, C.c_int32, C.c_void_p]),
+    "thinK_paged_read": (C.c_int, [C.c_void_p, Tensor5, Tensor5, PageTable, C.c_void_p, C.c_void_p, C.c_int32,
+                                   C.c_int32, C.c_int32, C.c_void_p]),
+    "thinK_paged_decode_attn": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, PageTable, C.c_void_p,
+                                          C.c_void_p, C.c_size_t, C.c_int32, C.c_int32, C.c_void_p]),
+    "thinK_paged_device_error": (C.c_int, [C.c_void_p, C.POINTER(C.c_int32)]),
+    "thinK_paged_destroy": (C.c_int, [C.c_void_p]),
 }
 for _name, (_res, _args) in EXPORTS.items():
     _fn = getattr(lib, _name)
@@ -291,6 +320,161 @@ class ThinKCache:
     def close(self):
         if getattr(self, "handle", None):
             lib.thinK_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+# ---------------------------------------------------------------------------
+# Paged key-value cache
+# ---------------------------------------------------------------------------
+def make_paged_config(L, N_q, N_kv, D, num_pages, max_batch, dtype, page_format=PAGE_PLAIN, softmax_scale=0.0):
+    return PagedConfig(L, N_q, N_kv, D, num_pages, max_batch, dtype if isinstance(dtype, int) else _dtype_code(dtype),
+                       page_format, float(softmax_scale))
+
+
+def paged_bytes(cfg: PagedConfig) -> PagedSizes:
+    out = PagedSizes()
+    _check(lib.thinK_paged_bytes(C.byref(cfg), C.byref(out)), "thinK_paged_bytes")
+    return out
+
+
+def paged_offset(cfg: PagedConfig, layer: int, page: int, head: int, slot: int, part: int) -> int:
+    """Byte offset in the pool of a token's row or scales (part: PART_K, ...), -1 if out of range."""
+    return int(lib.thinK_paged_offset(C.byref(cfg), layer, page, head, slot, part))
+
+
+class PagedKVCache:
+    """Pool of 64-token pages with device-side page tables and lengths: write, read back, one-token attention.
+
+    Tables are int32 [B, max_pages] (rows may be strided), lengths, positions and row counts int32 [B], all on the
+    cache's device.  `pages`: an existing pool (uint8, cfg's size) to work on; by default one is allocated."""
+
+    def __init__(self, cfg: PagedConfig, device="cuda", pages: Optional[torch.Tensor] = None):
+        self.cfg = cfg
+        self.handle = None
+        self.sizes = paged_bytes(cfg)
+        device = torch.device(device) if pages is None else pages.device
+        if device.type != "cuda":
+            raise ThinKError(ERR_INVALID_ARG, "PagedKVCache: device")
+        self.device = torch.device("cuda", torch.cuda.current_device() if device.index is None else device.index)
+        self.torch_dtype = torch.bfloat16 if cfg.dtype == BF16 else torch.float32
+        if pages is None:
+            pages = torch.empty(int(self.sizes.pages), dtype=torch.uint8, device=self.device)
+        elif pages.dtype != torch.uint8 or not pages.is_contiguous():
+            raise ThinKError(ERR_INVALID_ARG, "PagedKVCache: pages")
+        self.pages = pages
+        self.workspace = torch.empty(int(self.sizes.workspace), dtype=torch.uint8, device=self.device)
+        have = PagedSizes(pages.numel(), self.workspace.numel(), 0)
+        h = C.c_void_p()
+        with torch.cuda.device(self.device):
+            # the library zeroes the counters outside of torch's streams: wait for what last used this memory
+            torch.cuda.current_stream().synchronize()
+            _check(lib.thinK_paged_create(C.byref(cfg), C.byref(have), pages.data_ptr(), self.workspace.data_ptr(),
+                                          C.byref(h)), "thinK_paged_create")
+        self.handle = h
+
+    def new_scratch(self) -> torch.Tensor:
+        """A scratch buffer for attention calls that may run at the same time as others of this cache."""
+        return torch.zeros(int(self.sizes.workspace), dtype=torch.uint8, device=self.device)
+
+    # -- argument marshalling -------------------------------------------
+    def _table(self, table: torch.Tensor, B: int, where: str) -> PageTable:
+        if (table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] < B or table.device != self.device
+                or (table.shape[1] > 1 and table.stride(1) != 1)):
+            raise ThinKError(ERR_INVALID_ARG, where + ": page table")
+        return PageTable(table.data_ptr(), max(table.stride(0), table.shape[1]) if B == 1 else table.stride(0),
+                         table.shape[1], B)
+
+    def _vector(self, x: Optional[torch.Tensor], B: int, where: str):
+        if x is None:
+            return None
+        if (x.dtype != torch.int32 or x.dim() != 1 or x.shape[0] < B or x.device != self.device
+                or (B > 1 and x.stride(0) != 1)):
+            raise ThinKError(ERR_INVALID_ARG, where)
+        return x.data_ptr()
+
+    def _layers(self, layer0: int, nlayers: Optional[int]) -> int:
+        return self.cfg.L - layer0 if nlayers is None else nlayers
+
+    def _on(self, call, stream, where: str):
+        """Runs call(stream pointer) with the cache's device current."""
+        if torch.cuda.current_device() == self.device.index:
+            s = torch.cuda.current_stream() if stream is None else stream
+            _check(call(s.cuda_stream), where)
+            return
+        with torch.cuda.device(self.device):
+            s = torch.cuda.current_stream() if stream is None else stream
+            _check(call(s.cuda_stream), where)
+
+    def _rows(self, fn, where, k, v, table, pos, rows, layer0, nlayers, stream):
+        n = self._layers(layer0, nlayers)
+        want = (n, self.cfg.N_kv, self.cfg.D)
+        for x in (k, v):
+            if (x.dim() != 5 or tuple(x.shape[2:]) != want or x.shape[:2] != k.shape[:2] or x.dtype != self.torch_dtype
+                    or x.device != self.device or x.stride(4) != 1):
+                raise ThinKError(ERR_INVALID_ARG, where + ": rows")
+        B, max_rows = k.shape[0], k.shape[1]
+        t = self._table(table, B, where)
+        pp, rp = self._vector(pos, B, where + ": pos"), self._vector(rows, B, where + ": rows")
+        k5, v5 = tensor5(k), tensor5(v)
+        self._on(lambda s: fn(self.handle, k5, v5, t, pp, rp, max_rows, layer0, n, s), stream, where)
+
+    # -- the calls ------------------------------------------------------
+    def write(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, pos: Optional[torch.Tensor] = None,
+              rows: Optional[torch.Tensor] = None, layer0=0, nlayers=None, stream=None):
+        """Row s < rows[b] of k[b], v[b] ([B, S, nlayers, N_kv, D]) becomes token pos[b] + s of sequence b."""
+        self._rows(lib.thinK_paged_write, "thinK_paged_write", k, v, table, pos, rows, layer0, nlayers, stream)
+
+    def read(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, pos: Optional[torch.Tensor] = None,
+             rows: Optional[torch.Tensor] = None, layer0=0, nlayers=None, stream=None):
+        """The reverse of write: fills row s < rows[b] of k[b], v[b] with token pos[b] + s of sequence b."""
+        self._rows(lib.thinK_paged_read, "thinK_paged_read", k, v, table, pos, rows, layer0, nlayers, stream)
+
+    def decode_attn(self, q: torch.Tensor, table: torch.Tensor, seq_lens: torch.Tensor,
+                    out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, return_lse: bool = False,
+                    scratch: Optional[torch.Tensor] = None, layer0=0, nlayers=None, stream=None):
+        """Attention of one token per sequence, q [B, nlayers, N_q, D], over its first seq_lens[b] tokens.  Returns
+        out, or (out, lse) when lse (fp32 [B, nlayers, N_q]) is given or asked for."""
+        where = "thinK_paged_decode_attn"
+        n = self._layers(layer0, nlayers)
+        if (q.dim() != 4 or tuple(q.shape[1:]) != (n, self.cfg.N_q, self.cfg.D) or q.dtype != self.torch_dtype
+                or q.device != self.device or not q.is_contiguous()):
+            raise ThinKError(ERR_INVALID_ARG, where + ": q")
+        if out is None:
+            out = torch.empty_like(q)
+        elif out.shape != q.shape or out.dtype != q.dtype or out.device != q.device or not out.is_contiguous():
+            raise ThinKError(ERR_INVALID_ARG, where + ": out")
+        if lse is None and return_lse:
+            lse = torch.empty(q.shape[:3], dtype=torch.float32, device=self.device)
+        elif lse is not None and (lse.shape != q.shape[:3] or lse.dtype != torch.float32 or lse.device != q.device
+                                  or not lse.is_contiguous()):
+            raise ThinKError(ERR_INVALID_ARG, where + ": lse")
+        if scratch is not None and (scratch.dtype != torch.uint8 or scratch.device != self.device
+                                    or not scratch.is_contiguous()):
+            raise ThinKError(ERR_INVALID_ARG, where + ": scratch")
+        t = self._table(table, q.shape[0], where)
+        lens = self._vector(seq_lens, q.shape[0], where + ": seq_lens")
+        self._on(lambda s: lib.thinK_paged_decode_attn(
+            self.handle, q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(), t, lens,
+            None if scratch is None else scratch.data_ptr(), 0 if scratch is None else scratch.numel(), layer0, n, s),
+            stream, where)
+        return out if lse is None else (out, lse)
+
+    def device_error(self) -> int:
+        code = C.c_int32(0)
+        with torch.cuda.device(self.device):
+            torch.cuda.current_stream().synchronize()
+            _check(lib.thinK_paged_device_error(self.handle, C.byref(code)), "thinK_paged_device_error")
+        return code.value
+
+    def close(self):
+        if getattr(self, "handle", None):
+            lib.thinK_paged_destroy(self.handle)
             self.handle = None
 
     def __del__(self):

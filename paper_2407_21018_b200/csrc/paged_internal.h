@@ -1,0 +1,112 @@
+// Shared by the translation units of the paged key-value cache.
+#pragma once
+#include "think_internal.h"
+
+namespace think {
+
+constexpr uint32_t kErrPage = 16u;     // device error word: page-table entry, position, length or row count out of range
+constexpr int kPageTokens = kTileTokens;
+constexpr int kGroupChannels = 32;     // channels that share a scale in 4-bit pages
+constexpr int kMaxPagedBatch = 4096;
+constexpr int kMaxPagedGroup = 8;      // query heads per key head
+
+// The pool: [L][num_pages][N_kv] blocks of 64 key rows | 64 value rows | key scales | value scales.
+struct PageGeom {
+  int L, N_kv, D, num_pages;
+  int row_bytes;             // one row of D codes
+  int scale_bytes;           // scales of one row (0, 1 or 2 * D / 32)
+  int block_bytes;
+};
+
+__host__ __device__ inline int page_part_offset(const PageGeom& g, int part) {
+  const int a = kPageTokens * g.row_bytes, b = kPageTokens * g.scale_bytes;
+  return part < 2 ? part * a : 2 * a + (part - 2) * b;
+}
+__host__ __device__ inline int64_t page_block_offset(const PageGeom& g, int layer, int page, int head) {
+  return (((int64_t)layer * g.num_pages + page) * g.N_kv + head) * g.block_bytes;
+}
+
+// x / d and x % d for 0 <= x < 2^31 by one 32 x 32 -> 64 bit product (round-up reciprocal; exact over that range
+// because the error of the reciprocal times x stays below 1 / d)
+struct FastDiv {
+  uint32_t d, mul, shift;
+  FastDiv() = default;
+  explicit FastDiv(uint32_t d_) : d(d_), mul(0), shift(0) {
+    if (d_ <= 1) return;
+    uint32_t s = 0;
+    while ((1ull << s) < d_) ++s;                             // ceil(log2 d)
+    shift = s - 1;
+    mul = (uint32_t)(((1ull << (32 + shift)) + d_ - 1) / d_);
+  }
+  __host__ __device__ __forceinline__ uint32_t div(uint32_t x) const {
+    if (d <= 1) return x;
+#ifdef __CUDA_ARCH__
+    return __umulhi(x, mul) >> shift;
+#else
+    return (uint32_t)(((uint64_t)x * mul) >> 32) >> shift;
+#endif
+  }
+};
+
+struct PageTableView {
+  const int32_t* table;
+  int64_t stride;
+  int max_pages, B;
+};
+
+struct PagedRowsParams {     // rows <-> pages
+  PageGeom g;
+  View5 k, v;                // [b][s][layer - layer0][head][D], element strides
+  uint8_t* pages;
+  PageTableView table;
+  const int32_t* pos;        // or null: 0
+  const int32_t* rows;       // or null: max_rows
+  int max_rows;
+  int layer0, nlayers;
+  FastDiv by_heads, by_layers;
+  uint32_t* error;
+};
+
+struct PagedDecodeParams {
+  PageGeom g;
+  const uint8_t* pages;
+  const void* q;             // [B][nlayers][N_q][D]
+  void* out;
+  float* lse;                // [B][nlayers][N_q] or null
+  PageTableView table;
+  const int32_t* seq_len;
+  int N_q, G;
+  int layer0, nlayers;
+  float scale_log2;          // softmax scale * log2(e)
+  uint32_t* error;
+  uint32_t* counters;        // one ticket per unit of the call, zero between calls
+  uint8_t* records;          // partial states
+  int grid;
+};
+
+cudaError_t launch_paged_rows(const PagedRowsParams& p, int dtype, int format, bool write, cudaStream_t s);
+cudaError_t launch_paged_decode(const PagedDecodeParams& p, int dtype, int format, cudaStream_t s);
+cudaError_t paged_decode_setup(int dtype, int format, int D);
+// CTAs of a decode launch at most, and bytes of their partial states
+int paged_decode_max_ctas(int num_sms);
+size_t paged_decode_record_bytes(int D, int G);
+
+#ifdef __CUDACC__
+// Page that holds token t of entry b, or -1 (error bit) if the table or the position is out of range.
+__device__ __forceinline__ int page_of(const PageTableView& t, const PageGeom& g, int b, int64_t tok, uint32_t* error) {
+  int page = -1;
+  if (tok >= 0 && tok < (int64_t)t.max_pages * kPageTokens) page = __ldg(t.table + b * t.stride + (tok >> 6));
+  if ((uint32_t)page >= (uint32_t)g.num_pages) {
+    atomicOr(error, kErrPage);
+    return -1;
+  }
+  return page;
+}
+
+// value of a scale byte e of an e4m3 row: 2^(e - 127); byte 0 is 2^-127 (a subnormal), byte 255 is NaN
+__device__ __forceinline__ float e8m0(uint32_t e) {
+  return __uint_as_float(e == 0 ? 0x00400000u : e == 255 ? 0x7fc00000u : e << 23);
+}
+#endif
+
+}  // namespace think

@@ -1,0 +1,130 @@
+"""CPU checks of the paged cache's host side: sizes, offsets, refusals, and the kernels' index arithmetic compiled for
+the host.  No kernel is launched here."""
+import ctypes as C
+import os
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def tk():
+    from paper_2407_21018_b200 import build
+    build.build()
+    from paper_2407_21018_b200 import binding
+    return binding
+
+
+def cfg_of(tk, **kw):
+    base = dict(L=2, N_q=8, N_kv=4, D=128, num_pages=10, max_batch=3, dtype=tk.BF16, page_format=tk.PAGE_PLAIN)
+    base.update(kw)
+    return tk.make_paged_config(**base)
+
+
+@pytest.mark.parametrize("fmt,dtype,D,row,scale", [
+    (0, 0, 128, 256, 0), (0, 0, 64, 128, 0), (0, 1, 128, 512, 0), (0, 1, 64, 256, 0),
+    (1, 0, 128, 128, 1), (1, 0, 64, 64, 1), (2, 0, 128, 64, 8), (2, 0, 64, 32, 4),
+])
+def test_sizes_and_offsets(tk, fmt, dtype, D, row, scale):
+    c = cfg_of(tk, page_format=fmt, dtype=dtype, D=D)
+    s = tk.paged_bytes(c)
+    block = 2 * 64 * (row + scale)
+    assert s.block == block and s.pages == 2 * 10 * 4 * block and block % 16 == 0
+    at = lambda *a: tk.paged_offset(c, *a)  # noqa: E731
+    base = ((1 * 10 + 7) * 4 + 3) * block
+    assert at(1, 7, 3, 5, tk.PART_K) == base + 5 * row
+    assert at(1, 7, 3, 5, tk.PART_V) == base + 64 * row + 5 * row
+    assert at(1, 7, 3, 63, tk.PART_K_SCALE) == (base + 128 * row + 63 * scale if scale else -1)
+    assert at(1, 7, 3, 63, tk.PART_V_SCALE) == (base + 128 * row + 64 * scale + 63 * scale if scale else -1)
+    for bad in ((2, 0, 0, 0, 0), (-1, 0, 0, 0, 0), (0, 10, 0, 0, 0), (0, -1, 0, 0, 0), (0, 0, 4, 0, 0), (0, 0, 0, 64, 0),
+                (0, 0, 0, -1, 0), (0, 0, 0, 0, 4), (0, 0, 0, 0, -1)):
+        assert at(*bad) == -1
+
+
+def test_offsets_past_32_bits(tk):
+    c = cfg_of(tk, L=32, N_kv=8, N_q=32, num_pages=100000)
+    assert tk.paged_offset(c, 31, 99999, 7, 63, tk.PART_V) == ((31 * 100000 + 99999) * 8 + 7) * 32768 + 127 * 256
+    assert tk.paged_bytes(c).pages == 32 * 100000 * 8 * 32768
+
+
+@pytest.mark.parametrize("kw", [
+    dict(D=96), dict(D=0), dict(N_q=6), dict(N_q=36), dict(L=0), dict(N_kv=0), dict(num_pages=0), dict(max_batch=0),
+    dict(max_batch=4097), dict(dtype=7), dict(page_format=3), dict(page_format=-1), dict(softmax_scale=-1.0),
+    dict(softmax_scale=float("nan")), dict(softmax_scale=float("inf")), dict(dtype=1, page_format=1),
+    dict(dtype=1, page_format=2), dict(L=2 ** 30, num_pages=2 ** 30, N_kv=2 ** 20, N_q=2 ** 20),
+])
+def test_invalid_configs_are_refused(tk, kw):
+    with pytest.raises(tk.ThinKError) as e:
+        tk.paged_bytes(cfg_of(tk, **kw))
+    assert e.value.status in (tk.ERR_INVALID_ARG, tk.ERR_UNSUPPORTED)
+
+
+def test_create_refusals(tk):
+    c = cfg_of(tk)
+    need = tk.paged_bytes(c)
+    h = C.c_void_p()
+    create = tk.lib.thinK_paged_create
+    ok = (C.byref(c), C.byref(need), 4096, 4096, C.byref(h))
+    for i in range(5):
+        a = list(ok)
+        a[i] = None
+        assert create(*a) == tk.ERR_INVALID_ARG
+    for i in (2, 3):                                  # misaligned buffers
+        a = list(ok)
+        a[i] = 4096 + 16
+        assert create(*a) == tk.ERR_INVALID_ARG
+    for name in ("pages", "workspace"):
+        have = tk.paged_bytes(c)
+        setattr(have, name, getattr(have, name) - 1)
+        assert create(C.byref(c), C.byref(have), 4096, 4096, C.byref(h)) == tk.ERR_CAPACITY
+    assert not h.value
+    assert tk.lib.thinK_paged_bytes(C.byref(c), None) == tk.ERR_INVALID_ARG
+    assert tk.lib.thinK_paged_bytes(None, C.byref(need)) == tk.ERR_INVALID_ARG
+    assert tk.lib.thinK_paged_destroy(None) == tk.ERR_INVALID_ARG
+    assert tk.lib.thinK_paged_device_error(None, None) == tk.ERR_INVALID_ARG
+
+
+def test_calls_without_a_handle(tk):
+    t5, tab = tk.Tensor5(4096, 0, 0, 0, 0), tk.PageTable(4096, 4, 4, 1)
+    for fn in (tk.lib.thinK_paged_write, tk.lib.thinK_paged_read):
+        assert fn(None, t5, t5, tab, None, None, 1, 0, 1, None) == tk.ERR_INVALID_ARG
+    assert tk.lib.thinK_paged_decode_attn(None, 4096, 4096, None, tab, 4096, None, 0, 0, 1, None) == tk.ERR_INVALID_ARG
+
+
+def compile_and_run(tmp_path, source: str) -> str:
+    src, exe = tmp_path / "probe.cu", tmp_path / "probe"
+    src.write_text(source)
+    nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
+    subprocess.run([nvcc, "-std=c++17", "-O1", "-gencode", "arch=compute_100a,code=sm_100a", "-I",
+                    os.path.join(ROOT, "include"), "-I", os.path.join(ROOT, "paper_2407_21018_b200", "csrc"), str(src),
+                    "-o", str(exe)], check=True, capture_output=True)
+    r = subprocess.run([str(exe)], check=True, capture_output=True, text=True, timeout=120)
+    return r.stdout
+
+
+def test_row_index_division(tmp_path):
+    """The reciprocal division that splits a row index into token, layer and head is exact below 2^31."""
+    out = compile_and_run(tmp_path, r"""
+#include <stdio.h>
+#include "paged_internal.h"
+int main() {
+  long bad = 0;
+  uint32_t ds[] = {1, 2, 3, 4, 5, 6, 7, 8, 9, 12, 31, 32, 33, 80, 96, 127, 128, 1000, 4095, 65535, 65537, (1u << 30) - 1, 1u << 30};
+  for (uint32_t d : ds) {
+    think::FastDiv f(d);
+    for (uint64_t i = 0; i < 400000; ++i) {
+      uint64_t x[4] = {i, 0x7fffffffull - i, (i * 2654435761ull) & 0x7fffffffull, (i * (uint64_t)d) & 0x7fffffffull};
+      for (uint64_t y : x)
+        for (long o = -1; o <= 1; ++o) {
+          long z = (long)y + o;
+          if (z < 0 || z > 0x7fffffffl) continue;
+          bad += f.div((uint32_t)z) != (uint32_t)z / d;
+        }
+    }
+  }
+  printf("%ld\n", bad);
+}
+""")
+    assert out.strip() == "0"
