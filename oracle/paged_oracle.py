@@ -91,13 +91,15 @@ def decode_row(codes: np.ndarray, scales: np.ndarray, fmt: str) -> np.ndarray:
 
 def attention(q: np.ndarray, k: np.ndarray, v: np.ndarray, scale: float):
     """One key head: q [G, D], k and v [n, D].  Returns (out [G, D], lse [G], out of |v| [G, D], largest sum of
-    |scale q_i k_i| over the tokens [G]); the last two are what the error bounds of the tests are made of."""
+    |scale q_i k_i| over the tokens [G], largest weight times largest |v| of its row [G]); the last three are what the
+    error bounds of the tests are made of."""
     G, D = q.shape
     if k.shape[0] == 0:
-        return np.zeros((G, D)), np.full(G, -np.inf), np.zeros((G, D)), np.zeros(G)
+        return np.zeros((G, D)), np.full(G, -np.inf), np.zeros((G, D)), np.zeros(G), np.zeros(G)
     x = scale * (q @ k.T)
     m = x.max(axis=1, keepdims=True)
     p = np.exp(x - m)
     z = p.sum(axis=1, keepdims=True)
     w = p / z
-    return w @ v, (m + np.log(z))[:, 0], w @ np.abs(v), (abs(scale) * (np.abs(q) @ np.abs(k).T)).max(axis=1)
+    top = (w * np.abs(v).max(axis=1)).max(axis=1)
+    return w @ v, (m + np.log(z))[:, 0], w @ np.abs(v), (abs(scale) * (np.abs(q) @ np.abs(k).T)).max(axis=1), top

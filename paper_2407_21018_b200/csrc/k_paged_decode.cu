@@ -1,133 +1,1074 @@
-// Attention of one new token per sequence over the paged cache.
+// Attention of one new token per sequence over the paged cache: out = softmax(scale q K^T) V, lse.
 //
-// One CTA per (entry, layer, key head); its four warps take tokens in turn, a lane owns D / 32 channels, the softmax
-// runs online with fp32 maximum, sum and accumulators, and the warps' states are joined in warp order.
+// Every byte of the pages is read once and used for at most 8 query heads, so the stream of pages is the bound and
+// the kernel is built around it:
+//  * The tiles (64-token pages) of all (entry, layer, key head) units form one flat list, cut evenly over the CTAs
+//    of one wave and inside a CTA over its warps, whatever the lengths: one long sequence uses the whole card and a
+//    ragged batch leaves no SM idle.  Lengths and page table are device memory; each CTA scans the lengths itself.
+//  * A warp is the worker.  It owns a ring of stages in shared memory that it fills with cp.async, crossing page and
+//    unit borders, and waits for nobody until its range is done.
+//  * Rows are stored token-major.  16-byte chunks are XOR-swizzled on the way into shared memory so that ldmatrix
+//    reads without bank conflicts: plain for q K^T (contraction over channels), transposed for p V (over tokens).
+//    Products run on mma.sync m16n8k16 with the group's query heads as rows 0..7 of A; one query row per head fills
+//    at most 8 of the 128 rows that a tcgen05 tile would have.
+//      bf16  weights as a bf16 pair: the high halves are rows 0..7, the low halves rows 8..15 of the same
+//            instruction, so the second half costs no instruction and weights carry 2^-17 instead of 2^-9.
+//      e4m3, int4  codes become f16 exactly (byte conversion; 1024 + n by bit patterns) and never see their scales:
+//            a key's scale multiplies its logit, a value's scale goes into the weight.  Weights are rounded to f16,
+//            2^-11, relative to the largest weight * scale so far, which sits at 2^15: f16 leaves 29 binary orders
+//            below it before its step stops shrinking.  q is f16 times a power of two, exact unless its channels
+//            are more than 2^29 apart.
+//      fp32  CUDA cores: fp32 products summed over lanes pairwise.
+//  * The softmax is online in base 2 with fp32 maximum, sum and accumulators.  Units that several warps share leave
+//    partial states; the warps' states are joined by their CTA, the CTAs' states by the CTA that arrives last at
+//    the unit's ticket, always in token order, so results do not depend on timing.
+#include <cuda_fp16.h>
 #include <cuda_fp8.h>
 #include <math.h>
 
 #include "paged_internal.h"
+#include "paged_split.h"
 
 namespace think {
 namespace {
 
-constexpr int kThreads = 128;
-constexpr int kWarps = kThreads / 32;
+constexpr int kWarps = 8;
+constexpr int kThreads = kWarps * 32;
+constexpr int kMaxG = kMaxPagedGroup;
 
-// channels [c0, c0 + N) of a stored row as fp32
-template <int E, int FMT, int N>
-__device__ __forceinline__ void load_row(const uint8_t* row, const uint8_t* scales, int c0, float (&x)[N]) {
-  float f = 1.f;
-  if (FMT == THINK_PAGE_E4M3) f = e8m0(*scales);
-  if (FMT == THINK_PAGE_INT4) f = __uint_as_float((uint32_t)((const uint16_t*)scales)[c0 / kGroupChannels] << 16);
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int c = c0 + i;
-    if (FMT == THINK_PAGE_PLAIN) {
-      x[i] = E == 4 ? ((const float*)row)[c] : __bfloat162float(((const __nv_bfloat16*)row)[c]);
-    } else if (FMT == THINK_PAGE_E4M3) {
-      const __half_raw h = __nv_cvt_fp8_to_halfraw(row[c], __NV_E4M3);
-      x[i] = __half2float(*(const __half*)&h) * f;
-    } else {
-      x[i] = (float)((int)(row[c >> 1] >> (4 * (c & 1)) & 15) - 8) * f;
+template <int D, int E, int FMT>
+struct Shape {
+  static constexpr bool F32 = E == 4;
+  static constexpr int RB = FMT == THINK_PAGE_PLAIN ? D * E : FMT == THINK_PAGE_E4M3 ? D : D / 2;   // bytes of a row
+  static constexpr int SB = FMT == THINK_PAGE_PLAIN ? 0 : FMT == THINK_PAGE_E4M3 ? 1 : D / 16;      // bytes of its scales
+  // tokens of a step: 8 KB of keys and values, at most 32 tokens
+  static constexpr int ST = 4096 / RB < 32 ? 4096 / RB : 32;
+  static constexpr int HALF = ST * RB;                       // key (or value) bytes of a stage
+  static constexpr int STAGE = (2 * (HALF + ST * SB) + 127) / 128 * 128;
+  static constexpr int STAGES = 24960 / STAGE < 8 ? 24960 / STAGE : 8;
+  static constexpr int RING = STAGES * STAGE;
+  static_assert(RING >= (3 * kMaxG + kMaxG * D) * 4, "a warp's partial state reuses its ring");
+};
+
+// Partial state of one (worker, unit): m[8], M[8], l[8], o[8][D].  m: running maximum of the logits (base 2); M: that
+// of logit + exponent of the value's scale, the unit of the accumulators; l: sum of exp2(logit - m).
+template <int D>
+struct Record {
+  float m[kMaxG], M[kMaxG], l[kMaxG], o[kMaxG][D];
+};
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+// copies src_bytes (0..16) and zero-fills the rest of the 16 bytes
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, int src_bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
+}
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+template <bool BF16>
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if (BF16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *(uint32_t*)&v;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  __half2 v = __floats2half2_rn(lo, hi);
+  return *(uint32_t*)&v;
+}
+__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t two) {          // low 16 bits
+  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
+  return (uint32_t)h.x | ((uint32_t)h.y << 16);
+}
+// the codes at bits 0..3 and 16..19 of w, minus 8, as f16
+__device__ __forceinline__ uint32_t int4x2_to_f16x2(uint32_t w) {
+  const uint32_t t = (w & 0x000f000fu) | 0x64006400u, eight = 0x64086408u;    // 1024 + code, 1024 + 8
+  const __half2 r = __hsub2(*(const __half2*)&t, *(const __half2*)&eight);
+  return *(const uint32_t*)&r;
+}
+// the same at bits 4..7 and 20..23: 1024 + 16 code = 16 (64 + code)
+__device__ __forceinline__ uint32_t int4x2_hi_to_f16x2(uint32_t w) {
+  const uint32_t t = (w & 0x00f000f0u) | 0x64006400u, k = 0x2c002c00u, o = 0xd480d480u;    // 1/16, -72
+  const __half2 r = __hfma2(*(const __half2*)&t, *(const __half2*)&k, *(const __half2*)&o);
+  return *(const uint32_t*)&r;
+}
+// 2^k for -126 <= k <= 127
+__device__ __forceinline__ float pow2i(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }
+
+// where chunk ck (16 bytes) of row r lands: a permutation within the row under which 8 rows' equal chunks fall into
+// different banks
+template <int RB>
+__device__ __forceinline__ int swz(int r, int ck) {
+  if (RB >= 128) return r * RB + ((ck ^ (r & 7)) << 4);
+  if (RB == 64) return r * RB + ((ck ^ ((r >> 1) & 3)) << 4);
+  return r * RB + ((ck ^ ((r >> 2) & 1)) << 4);
+}
+
+// Tables of a launch in shared memory: cumulative tiles and the tokens of each sequence's last tile.
+struct Tables {
+  const int* cum;            // [B + 1]
+  const uint8_t* last;       // tokens in the last tile, minus 1
+};
+struct Cursor {              // a tile of the flat list
+  int b, u;                  // entry, unit of the entry (layer * heads + head)
+  int j, nt;                 // tile and tiles of the unit
+  int len;
+};
+__device__ __forceinline__ void seq_of(const Tables& t, Cursor& c) {
+  c.nt = t.cum[c.b + 1] - t.cum[c.b];
+  c.len = (c.nt - 1) * kPageTokens + t.last[c.b] + 1;
+}
+__device__ __forceinline__ Cursor locate(const Tables& t, int B, int LH, int64_t f) {
+  int lo = 0, hi = B - 1;                      // last entry with cum * LH <= f that has tiles
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if ((int64_t)t.cum[mid] * LH <= f) lo = mid; else hi = mid - 1;
+  }
+  Cursor c;
+  c.b = lo;
+  seq_of(t, c);
+  const int64_t rem = f - (int64_t)t.cum[lo] * LH;
+  c.u = (int)(rem / c.nt);
+  c.j = (int)(rem - (int64_t)c.u * c.nt);
+  return c;
+}
+// to the first tile of the next unit
+__device__ __forceinline__ void next_unit(const Tables& t, int B, int LH, Cursor& c) {
+  c.j = 0;
+  if (++c.u < LH) return;
+  c.u = 0;
+  do ++c.b; while (c.b < B && t.cum[c.b + 1] == t.cum[c.b]);
+  if (c.b < B) seq_of(t, c);
+}
+
+// What a warp tells its CTA about the range it has done.
+struct WarpInfo {
+  int64_t f0, f1;            // empty if equal
+  int64_t last_us, last_ue;  // flat range of the last unit
+  int first_unit, last_unit; // index of the unit in the call
+  int64_t first_us, first_ue;
+};
+
+// Joins n partial states of one unit (rec(i), in token order).  Returns with the block's threads holding elements
+// i = tid + kThreads * k of the joined accumulators in acc[k]; `stat` (shared) gets m, M and l per query head.
+// GLOBAL: the states were written by other CTAs (read from L2); otherwise by this one, in either memory.
+template <bool GLOBAL>
+__device__ __forceinline__ float rec_load(const float* p) { return GLOBAL ? __ldcg(p) : *p; }
+template <int D, bool GLOBAL, typename RecOf>
+__device__ __forceinline__ void join(int n, int G, RecOf rec, float* weight /* shared [8][n] */, float (*stat)[kMaxG],
+                                     float (&acc)[kMaxG * D / kThreads]) {
+  const int tid = threadIdx.x, lane = tid & 31, g = tid >> 5;
+  static_assert(kWarps >= kMaxG, "one warp per query head");
+  if (g < G) {
+    float m = -INFINITY, M = -INFINITY, l = 0.f;
+    for (int i = lane; i < n; i += 32) {
+      m = fmaxf(m, rec_load<GLOBAL>(&rec(i)->m[g]));
+      M = fmaxf(M, rec_load<GLOBAL>(&rec(i)->M[g]));
     }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+      M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+    }
+    const float ms = m == -INFINITY ? 0.f : m, Ms = M == -INFINITY ? 0.f : M;
+    for (int i = lane; i < n; i += 32) {
+      l += rec_load<GLOBAL>(&rec(i)->l[g]) * exp2f(rec_load<GLOBAL>(&rec(i)->m[g]) - ms);
+      weight[g * n + i] = exp2f(rec_load<GLOBAL>(&rec(i)->M[g]) - Ms);
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    if (lane == 0) {
+      stat[0][g] = m;
+      stat[1][g] = M;
+      stat[2][g] = l;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kMaxG * D / kThreads; ++k) {
+    const int e = tid + kThreads * k, ge = e / D;
+    acc[k] = 0.f;
+    if (ge < G) {
+#pragma unroll 8
+      for (int i = 0; i < n; ++i) acc[k] = fmaf(weight[ge * n + i], rec_load<GLOBAL>(&rec(i)->o[0][0] + e), acc[k]);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------
+// Tensor-core formats: fragments of a warp.  Lane (row = lane / 4, qd = lane % 4): query head `row`, tokens
+// 8 n + 2 qd, + 1 of the n-th group of 8 tokens.
+template <int D, int FMT>
+struct MmaState {
+  using S = Shape<D, 2, FMT>;
+  static constexpr bool PLAIN = FMT == THINK_PAGE_PLAIN;
+  static constexpr bool INT4 = FMT == THINK_PAGE_INT4;
+  static constexpr int NT = S::ST / 8;          // groups of 8 tokens of a step
+  static constexpr int KS = D / 16;
+  static constexpr int NG = D / kGroupChannels;
+  static constexpr int OT = D / 8;
+  static constexpr int WIDTH = PLAIN ? 2 : FMT == THINK_PAGE_E4M3 ? 4 : 8;   // consecutive output channels of a lane
+
+  uint32_t q[KS][2];
+  float rs;                  // base-2 logit per unit of the q k product
+  float m, M, l;
+  float o[OT][4];
+
+  // the unit's queries as A fragments; qg: its first query row
+  __device__ __forceinline__ void begin(const void* qg_, int G, float scale_log2, int lane) {
+    const __nv_bfloat16* qr = (const __nv_bfloat16*)qg_ + (lane >> 2) * D;
+    const int qd = lane & 3;
+    const bool on = (lane >> 2) < G;
+    if constexpr (PLAIN) {
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        q[s][0] = on ? *(const uint32_t*)(qr + 16 * s + 2 * qd) : 0u;
+        q[s][1] = on ? *(const uint32_t*)(qr + 16 * s + 2 * qd + 8) : 0u;
+      }
+      rs = scale_log2;
+    } else {
+      uint32_t w[D / 8];                        // the lane's channels as bf16 pairs, 4 (e4m3) or 8 (int4) in a row
+      if constexpr (INT4) {
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          const uint4 x = on ? *(const uint4*)(qr + 32 * g + 8 * qd) : make_uint4(0u, 0u, 0u, 0u);
+          w[4 * g] = x.x; w[4 * g + 1] = x.y; w[4 * g + 2] = x.z; w[4 * g + 3] = x.w;
+        }
+      } else {
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          const uint2 x = on ? *(const uint2*)(qr + 16 * s + 4 * qd) : make_uint2(0u, 0u);
+          w[2 * s] = x.x; w[2 * s + 1] = x.y;
+        }
+      }
+      uint32_t t = 0;
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i) t = __vmaxu2(t, w[i] & 0x7fff7fffu);
+      t = max(t & 0xffffu, t >> 16);
+      t = max(t, __shfl_xor_sync(0xffffffffu, t, 1));
+      t = max(t, __shfl_xor_sync(0xffffffffu, t, 2));
+      // the row's largest channel goes to [2^14, 2^15)
+      const int k = min(141 - (int)(t >> 7), 100);
+      const float up = pow2i(k);
+      rs = scale_log2 * pow2i(-k);
+      if constexpr (INT4) {                     // the codes of a word pair up as channels (0,4) (1,5) (2,6) (3,7)
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t a = w[4 * g + j], b = w[4 * g + 2 + j];
+            q[2 * g + j][0] = pack_f16(bf16lo(a) * up, bf16lo(b) * up);
+            q[2 * g + j][1] = pack_f16(bf16hi(a) * up, bf16hi(b) * up);
+          }
+      } else {
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          q[s][0] = pack_f16(bf16lo(w[2 * s]) * up, bf16hi(w[2 * s]) * up);
+          q[s][1] = pack_f16(bf16lo(w[2 * s + 1]) * up, bf16hi(w[2 * s + 1]) * up);
+        }
+      }
+    }
+    m = M = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int t = 0; t < OT; ++t) o[t][0] = o[t][1] = o[t][2] = o[t][3] = 0.f;
+  }
+
+  // one step: keys at sb, values at sb + HALF, scales behind; ntok of its tokens count
+  __device__ __forceinline__ void step(uint32_t sb, int ntok, int lane) {
+    const int qd = lane & 3, mi = lane >> 3, tr = lane & 7;
+    float x[NT][2];
+    // ---- logits
+    if constexpr (PLAIN) {
+      const int off = (tr + 8 * (mi >> 1)) * S::RB + (((mi & 1) ^ tr) << 4);
+#pragma unroll
+      for (int n = 0; n < NT; n += 2) {
+        float c[4][4] = {};                     // even and odd channel groups in chains of their own
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          uint32_t k[4];
+          ldsm4(sb + n * 8 * S::RB + (off ^ (s << 5)), k);
+          mma<true>(c[s & 1], q[s][0], 0u, q[s][1], 0u, k[0], k[1]);
+          mma<true>(c[2 + (s & 1)], q[s][0], 0u, q[s][1], 0u, k[2], k[3]);
+        }
+        x[n][0] = (c[0][0] + c[1][0]) * rs; x[n][1] = (c[0][1] + c[1][1]) * rs;
+        x[n + 1][0] = (c[2][0] + c[3][0]) * rs; x[n + 1][1] = (c[2][1] + c[3][1]) * rs;
+      }
+    } else if constexpr (!INT4) {
+      const int off = S::RB == 128 ? tr * 128 + ((mi ^ tr) << 4) : tr * 64 + ((mi ^ (tr >> 1)) << 4);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float c[2][4] = {};
+#pragma unroll
+        for (int i = 0; i < KS / 4; ++i) {
+          uint32_t k[4];
+          ldsm4(sb + n * 8 * S::RB + (off ^ (i << 6)), k);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            mma<false>(c[j & 1], q[4 * i + j][0], 0u, q[4 * i + j][1], 0u, e4m3x2_to_f16x2(k[j] & 0xffffu), e4m3x2_to_f16x2(k[j] >> 16));
+        }
+        uint32_t sc;
+        asm volatile("ld.shared.u16 %0, [%1];" : "=r"(sc) : "r"(sb + 2 * S::HALF + 8 * n + 2 * qd));
+        x[n][0] = (c[0][0] + c[1][0]) * rs * __uint_as_float((sc & 0xffu) << 23);
+        x[n][1] = (c[0][1] + c[1][1]) * rs * __uint_as_float((sc >> 8) << 23);
+      }
+    } else {
+      const int off = S::RB == 64 ? tr * 64 + ((mi ^ (tr >> 1)) << 4) : (tr + 8 * (mi >> 1)) * 32 + (((mi & 1) ^ (tr >> 2)) << 4);
+      constexpr int PER = 4 / NG;               // token groups per ldmatrix
+#pragma unroll
+      for (int n0 = 0; n0 < NT; n0 += PER) {
+        uint32_t k[4];
+        ldsm4(sb + n0 * 8 * S::RB + off, k);
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+          const int n = n0 + p;
+          uint32_t sc[2 * NG / 2];              // scales of the lane's two tokens, bf16 pairs
+          load_scales(sb + 2 * S::HALF, n, qd, sc);
+          float y0 = 0.f, y1 = 0.f;
+#pragma unroll
+          for (int g = 0; g < NG; ++g) {
+            const uint32_t w = k[p * NG + g], w8 = w >> 8;
+            float c[4] = {};
+            mma<false>(c, q[2 * g][0], 0u, q[2 * g][1], 0u, int4x2_to_f16x2(w), int4x2_hi_to_f16x2(w));
+            mma<false>(c, q[2 * g + 1][0], 0u, q[2 * g + 1][1], 0u, int4x2_to_f16x2(w8), int4x2_hi_to_f16x2(w8));
+            y0 = fmaf(c[0], (g & 1) ? bf16hi(sc[g >> 1]) : bf16lo(sc[g >> 1]), y0);
+            y1 = fmaf(c[1], (g & 1) ? bf16hi(sc[NG / 2 + (g >> 1)]) : bf16lo(sc[NG / 2 + (g >> 1)]), y1);
+          }
+          x[n][0] = y0 * rs;
+          x[n][1] = y1 * rs;
+        }
+      }
+    }
+    if (ntok < S::ST) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        if (8 * n + 2 * qd >= ntok) x[n][0] = -INFINITY;
+        if (8 * n + 2 * qd + 1 >= ntok) x[n][1] = -INFINITY;
+      }
+    }
+    // ---- exponents of the values' scales, running maxima
+    int es[NT][2];
+    float mx = -INFINITY, Mx = -INFINITY;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      if constexpr (PLAIN) {
+        mx = fmaxf(mx, fmaxf(x[n][0], x[n][1]));
+      } else {
+        if constexpr (INT4) {
+          uint32_t sc[NG];
+          load_scales(sb + 2 * S::HALF + S::ST * S::SB, n, qd, sc);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            uint32_t t = NG == 4 ? __vmaxu2(sc[2 * i], sc[2 * i + 1]) : sc[i];
+            t = max(t & 0xffffu, t >> 16) >> 7;
+            es[n][i] = t == 255u ? 0 : min(max((int)t - 126, -100), 126);      // every scale of the row is below 2^es
+          }
+        } else {
+          uint32_t sc;
+          asm volatile("ld.shared.u16 %0, [%1];" : "=r"(sc) : "r"(sb + 2 * S::HALF + S::ST + 8 * n + 2 * qd));
+          es[n][0] = (int)(sc & 0xffu) - 127;
+          es[n][1] = (int)(sc >> 8) - 127;
+        }
+        mx = fmaxf(mx, fmaxf(x[n][0], x[n][1]));
+        Mx = fmaxf(Mx, fmaxf(x[n][0] + es[n][0], x[n][1] + es[n][1]));
+      }
+    }
+    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+    if constexpr (PLAIN) Mx = mx;
+    else {
+      Mx = fmaxf(Mx, __shfl_xor_sync(0xffffffffu, Mx, 1));
+      Mx = fmaxf(Mx, __shfl_xor_sync(0xffffffffu, Mx, 2));
+    }
+    if (__any_sync(0xffffffffu, mx > m || Mx > M)) {
+      const float mn = fmaxf(m, mx), Mn = fmaxf(M, Mx);
+      l *= m == -INFINITY ? 0.f : ex2(m - mn);
+      const float sc = M == -INFINITY ? 0.f : ex2(M - Mn);
+      m = mn;
+      M = Mn;
+#pragma unroll
+      for (int t = 0; t < OT; ++t) {
+        o[t][0] *= sc; o[t][1] *= sc;
+        if (PLAIN) { o[t][2] *= sc; o[t][3] *= sc; }
+      }
+    }
+    const float mr = m == -INFINITY ? 0.f : m;
+    // ---- weights and p V, 16 tokens at a time
+#pragma unroll
+    for (int kk = 0; kk < NT / 2; ++kk) {
+      const uint32_t vb = sb + S::HALF + kk * 16 * S::RB;
+      float w[2][2];
+      const float Mr = M == -INFINITY ? 0.f : M - 15.f;
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float p = ex2(x[2 * kk + j][i] - mr);
+          l += p;
+          w[j][i] = PLAIN ? p : ex2(x[2 * kk + j][i] + es[2 * kk + j][i] - Mr);
+        }
+      if constexpr (PLAIN) {
+        const uint32_t h0 = pack_bf16(w[0][0], w[0][1]), h2 = pack_bf16(w[1][0], w[1][1]);
+        const uint32_t l0 = pack_bf16(w[0][0] - bf16lo(h0), w[0][1] - bf16hi(h0));
+        const uint32_t l2 = pack_bf16(w[1][0] - bf16lo(h2), w[1][1] - bf16hi(h2));
+        const int off = (((mi & 1) << 3) + tr) * S::RB + (((mi >> 1) ^ tr) << 4);
+#pragma unroll
+        for (int t = 0; t < OT / 2; ++t) {
+          uint32_t v[4];
+          ldsm4t(vb + (off ^ (t << 5)), v);
+          mma<true>(o[2 * t], h0, l0, h2, l2, v[0], v[1]);
+          mma<true>(o[2 * t + 1], h0, l0, h2, l2, v[2], v[3]);
+        }
+      } else if constexpr (!INT4) {
+        const uint32_t a0 = pack_f16(w[0][0], w[0][1]), a2 = pack_f16(w[1][0], w[1][1]);
+        const int r = ((mi & 1) << 3) + tr;
+        const int off = S::RB == 128 ? r * 128 + (((mi >> 1) ^ tr) << 4) : r * 64 + (((mi >> 1) ^ (tr >> 1)) << 4);
+#pragma unroll
+        for (int i = 0; i < KS / 2; ++i) {
+          uint32_t v[4];
+          ldsm4t(vb + (off ^ (i << 5)), v);
+          // bytes (channel 2r, 2r + 1 of token 2qd | the same of token 2qd + 1) to (even channel's tokens | odd's)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] = __byte_perm(v[j], 0u, 0x3120);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            mma<false>(o[4 * i + 2 * j], a0, 0u, a2, 0u, e4m3x2_to_f16x2(v[2 * j] & 0xffffu), e4m3x2_to_f16x2(v[2 * j + 1] & 0xffffu));
+            mma<false>(o[4 * i + 2 * j + 1], a0, 0u, a2, 0u, e4m3x2_to_f16x2(v[2 * j] >> 16), e4m3x2_to_f16x2(v[2 * j + 1] >> 16));
+          }
+        }
+      } else {
+        uint32_t s0[NG], s1[NG];
+        load_scales(sb + 2 * S::HALF + S::ST * S::SB, 2 * kk, qd, s0);
+        load_scales(sb + 2 * S::HALF + S::ST * S::SB, 2 * kk + 1, qd, s1);
+        float f[2][2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) f[j][i] = w[j][i] * pow2i(-es[2 * kk + j][i]);
+        // a masked token's weight is 0 whatever its scale (zero-filled) says
+        const int r = ((mi & 1) << 3) + tr;
+        const int off = S::RB == 64 ? r * 64 + (((mi >> 1) ^ (tr >> 1)) << 4) : r * 32 + (((mi >> 1) ^ (tr >> 2)) << 4);
+#pragma unroll
+        for (int g2 = 0; g2 < NG / 2; ++g2) {
+          uint32_t v[4];
+          ldsm4t(vb + (off ^ (g2 << 5)), v);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int g = 2 * g2 + j;
+            const uint32_t a0 = pack_f16(f[0][0] * (j ? bf16hi(s0[g2]) : bf16lo(s0[g2])), f[0][1] * (j ? bf16hi(s0[NG / 2 + g2]) : bf16lo(s0[NG / 2 + g2])));
+            const uint32_t a2 = pack_f16(f[1][0] * (j ? bf16hi(s1[g2]) : bf16lo(s1[g2])), f[1][1] * (j ? bf16hi(s1[NG / 2 + g2]) : bf16lo(s1[NG / 2 + g2])));
+            const uint32_t b0 = v[2 * j], b1 = v[2 * j + 1];
+            mma<false>(o[4 * g], a0, 0u, a2, 0u, int4x2_to_f16x2(b0), int4x2_to_f16x2(b1));
+            mma<false>(o[4 * g + 1], a0, 0u, a2, 0u, int4x2_hi_to_f16x2(b0), int4x2_hi_to_f16x2(b1));
+            mma<false>(o[4 * g + 2], a0, 0u, a2, 0u, int4x2_to_f16x2(b0 >> 8), int4x2_to_f16x2(b1 >> 8));
+            mma<false>(o[4 * g + 3], a0, 0u, a2, 0u, int4x2_hi_to_f16x2(b0 >> 8), int4x2_hi_to_f16x2(b1 >> 8));
+          }
+        }
+      }
+    }
+  }
+
+  // bf16 scales of tokens 8n + 2qd (first NG / 2 words) and 8n + 2qd + 1
+  static __device__ __forceinline__ void load_scales(uint32_t base, int n, int qd, uint32_t (&sc)[NG]) {
+    const uint32_t a = base + (8 * n + 2 * qd) * S::SB;
+    if constexpr (NG == 4)
+      asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(sc[0]), "=r"(sc[1]), "=r"(sc[2]), "=r"(sc[3]) : "r"(a));
+    else
+      asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(sc[0]), "=r"(sc[1]) : "r"(a));
+  }
+
+  // the lane's output channels: f(first channel, values[WIDTH])
+  template <typename F>
+  __device__ __forceinline__ void each(int lane, F f) const {
+    const int qd = lane & 3;
+#pragma unroll
+    for (int i = 0; i < D / (4 * WIDTH); ++i) {
+      float v[WIDTH];
+      if constexpr (PLAIN) {
+        v[0] = o[i][0] + o[i][2];
+        v[1] = o[i][1] + o[i][3];
+      } else if constexpr (!INT4) {
+        v[0] = o[2 * i][0]; v[1] = o[2 * i + 1][0]; v[2] = o[2 * i][1]; v[3] = o[2 * i + 1][1];
+      } else {
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          v[a] = o[4 * i + a][0];
+          v[4 + a] = o[4 * i + a][1];
+        }
+      }
+      f(4 * WIDTH * i + WIDTH * qd, v);
+    }
+  }
+  __device__ __forceinline__ void end() {
+    l += __shfl_xor_sync(0xffffffffu, l, 1);
+    l += __shfl_xor_sync(0xffffffffu, l, 2);
+  }
+  __device__ __forceinline__ void store_record(Record<D>* r, int G, int lane) const {
+    const int row = lane >> 2;
+    if (row >= G) return;
+    if ((lane & 3) == 0) {
+      r->m[row] = m;
+      r->M[row] = M;
+      r->l[row] = l;
+    }
+    each(lane, [&](int c, const float (&v)[WIDTH]) {
+#pragma unroll
+      for (int i = 0; i < WIDTH; i += 2) *(float2*)&r->o[row][c + i] = make_float2(v[i], v[i + 1]);
+    });
+  }
+  __device__ __forceinline__ void store_out(void* out, float* lse, int G, int lane) const;
+};
+
+// factor that turns joined accumulators into outputs, and the log of the softmax sum
+template <bool PLAIN>
+__device__ __forceinline__ float finish(float m, float M, float l) {
+  if (m == -INFINITY) return 0.f;
+  if (PLAIN) return 1.f / l;
+  const float h = exp2f(0.5f * (M - 15.f - m));              // in two factors: the exponent may pass 127
+  return h / l * h;
+}
+__device__ __forceinline__ float log_sum(float m, float l) {
+  return m == -INFINITY ? -INFINITY : (m + log2f(l)) * 0.693147180559945309f;
+}
+
+template <int D, int FMT>
+__device__ __forceinline__ void MmaState<D, FMT>::store_out(void* out, float* lse, int G, int lane) const {
+  const int row = lane >> 2;
+  if (row >= G) return;
+  const float f = finish<PLAIN>(m, M, l);
+  __nv_bfloat16* po = (__nv_bfloat16*)out + row * D;
+  each(lane, [&](int c, const float (&v)[WIDTH]) {
+    uint32_t w[WIDTH / 2];
+#pragma unroll
+    for (int i = 0; i < WIDTH / 2; ++i) w[i] = f == 0.f ? 0u : pack_bf16(v[2 * i] * f, v[2 * i + 1] * f);
+    if constexpr (WIDTH == 2) *(uint32_t*)(po + c) = w[0];
+    else if constexpr (WIDTH == 4) *(uint2*)(po + c) = make_uint2(w[0], w[1]);
+    else *(uint4*)(po + c) = make_uint4(w[0], w[1], w[2], w[3]);
+  });
+  if (lse && (lane & 3) == 0) lse[row] = log_sum(m, l);
+}
+
+// ---------------------------------------------------------------------------------------------------------
+// fp32: a lane owns D / 32 channels.  The products of a step's tokens with the group's queries are NV partial sums a
+// lane, reduced over the lanes by halving exchanges (each exchange adds two lanes' halves and keeps one half), after
+// which the lane owns the logits idx = owner(lane) .. of (query g = idx / ST, token t = idx % ST).
+template <int D, int GP>
+struct F32State {
+  using S = Shape<D, 4, THINK_PAGE_PLAIN>;
+  static constexpr int N = D / 32, ST = S::ST, NV = GP * ST;
+  static __host__ __device__ constexpr int log2c(int x) { return x <= 1 ? 0 : 1 + log2c(x / 2); }
+  static constexpr int NB = log2c(NV), LB = NB < 5 ? NB : 5, R = NV >> LB;   // idx bits, of which in the lane, values a lane
+  static constexpr int TB = log2c(ST);
+
+  float q[GP][N], o[GP][N];
+  float m, l;                // of query owner(lane) / ST; l: this lane's tokens only
+  float* sp;                 // the warp's NV weights in shared memory
+
+  static __device__ __forceinline__ int owner(int lane) { return (lane >> (5 - LB)) * R; }
+
+  __device__ __forceinline__ void begin(const void* qg, int G, float scale_log2, int lane) {
+#pragma unroll
+    for (int g = 0; g < GP; ++g)
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        q[g][i] = g < G ? ((const float*)qg)[g * D + lane * N + i] * scale_log2 : 0.f;
+        o[g][i] = 0.f;
+      }
+    m = -INFINITY;
+    l = 0.f;
+  }
+  static __device__ __forceinline__ void load(uint32_t a, float (&v)[N]) {
+    if constexpr (N == 4)
+      asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(a));
+    else
+      asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v[0]), "=f"(v[1]) : "r"(a));
+  }
+  __device__ __forceinline__ void step(uint32_t sb, int ntok, int lane) {
+    float x[NV];
+#pragma unroll
+    for (int t = 0; t < ST; ++t) {
+      float k[N];
+      load(sb + t * S::RB + lane * N * 4, k);
+#pragma unroll
+      for (int g = 0; g < GP; ++g) {
+        float a = q[g][0] * k[0];
+#pragma unroll
+        for (int i = 1; i < N; ++i) a = fmaf(q[g][i], k[i], a);
+        x[g * ST + t] = a;
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < LB; ++b) {
+      const bool up = lane & (16 >> b);
+#pragma unroll
+      for (int i = 0; i < (NV >> (b + 1)); ++i) {
+        const float lo = x[i], hi = x[i + (NV >> (b + 1))];
+        x[i] = (up ? hi : lo) + __shfl_xor_sync(0xffffffffu, up ? lo : hi, 16 >> b);
+      }
+    }
+#pragma unroll
+    for (int b = LB; b < 5; ++b)
+#pragma unroll
+      for (int i = 0; i < R; ++i) x[i] += __shfl_xor_sync(0xffffffffu, x[i], 16 >> b);
+    const int idx = owner(lane);
+    float mx = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      if (((idx + i) & (ST - 1)) >= ntok) x[i] = -INFINITY;
+      mx = fmaxf(mx, x[i]);
+    }
+    // over the other lanes of the same query: idx bits log2(R) .. TB - 1
+    constexpr int RB_ = log2c(R);
+#pragma unroll
+    for (int b = RB_; b < TB; ++b) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1 << (b - RB_ + 5 - LB)));
+    if (__any_sync(0xffffffffu, mx > m)) {
+      const float mn = fmaxf(m, mx), sc = m == -INFINITY ? 0.f : exp2f(m - mn);
+      m = mn;
+      l *= sc;
+#pragma unroll
+      for (int g = 0; g < GP; ++g) {
+        const float s = __shfl_sync(0xffffffffu, sc, (g * ST / R) << (5 - LB));
+#pragma unroll
+        for (int i = 0; i < N; ++i) o[g][i] *= s;
+      }
+    }
+    const float mr = m == -INFINITY ? 0.f : m;
+    const bool first = (lane & ((1 << (5 - LB)) - 1)) == 0;     // lanes that share logits: one of them counts
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const float p = exp2f(x[i] - mr);
+      if (first) {
+        l += p;
+        sp[idx + i] = p;
+      }
+    }
+    __syncwarp();
+#pragma unroll
+    for (int t0 = 0; t0 < ST; t0 += 4) {
+      float v[4][N];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) load(sb + S::HALF + (t0 + t) * S::RB + lane * N * 4, v[t]);
+#pragma unroll
+      for (int g = 0; g < GP; ++g) {
+        const float4 p = *(const float4*)(sp + g * ST + t0);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          o[g][i] = fmaf(p.w, v[3][i], fmaf(p.z, v[2][i], fmaf(p.y, v[1][i], fmaf(p.x, v[0][i], o[g][i]))));
+      }
+    }
+    __syncwarp();
+  }
+  __device__ __forceinline__ void end() {
+    constexpr int RB_ = log2c(R);
+#pragma unroll
+    for (int b = RB_; b < TB; ++b) l += __shfl_xor_sync(0xffffffffu, l, 1 << (b - RB_ + 5 - LB));
+    l = __shfl_sync(0xffffffffu, l, threadIdx.x & 31 & ~((1 << (5 - LB)) - 1));
+  }
+  __device__ __forceinline__ void store_record(Record<D>* r, int G, int lane) const {
+#pragma unroll
+    for (int g = 0; g < GP; ++g) {
+      if (g >= G) break;
+      if (lane == (g * ST / R) << (5 - LB)) {
+        r->m[g] = m;
+        r->M[g] = m;
+        r->l[g] = l;
+      }
+#pragma unroll
+      for (int i = 0; i < N; i += 2) *(float2*)&r->o[g][lane * N + i] = make_float2(o[g][i], o[g][i + 1]);
+    }
+  }
+  __device__ __forceinline__ void store_out(void* out, float* lse, int G, int lane) const {
+#pragma unroll
+    for (int g = 0; g < GP; ++g) {
+      const int src = (g * ST / R) << (5 - LB);
+      const float mg = __shfl_sync(0xffffffffu, m, src), lg = __shfl_sync(0xffffffffu, l, src);
+      if (g < G) {
+        const float f = finish<true>(mg, mg, lg);
+#pragma unroll
+        for (int i = 0; i < N; ++i) ((float*)out)[g * D + lane * N + i] = f == 0.f ? 0.f : o[g][i] * f;
+        if (lse && lane == 0) lse[g] = log_sum(mg, lg);
+      }
+    }
+  }
+};
+
+template <int D, int E, int FMT, int GP>
+struct StateOf { using type = MmaState<D, FMT>; };
+template <int D, int GP>
+struct StateOf<D, 4, THINK_PAGE_PLAIN, GP> { using type = F32State<D, GP>; };
+
+// shared memory behind the rings
+struct alignas(16) Shared {
+  alignas(16) float sp[kWarps][128];            // fp32: weights of a step, read 16 bytes at a time
+  WarpInfo info[kWarps];
+  float weight[kMaxG * kWarps];
+  float stat[3][kMaxG];
+  int warp_sum[kWarps];
+  int valid[kWarps][8];      // tokens that count in the stage
+  int arrived[2];
+};
+
+template <int D, int E, int FMT, int GP>
+__global__ void __launch_bounds__(kThreads, 1) k_paged_decode(const PagedDecodeParams p) {
+  using S = Shape<D, E, FMT>;
+  using State = typename StateOf<D, E, FMT, GP>::type;
+  constexpr int EO = E;                         // bytes of an output element
+  extern __shared__ __align__(128) unsigned char smem[];
+  Shared& sh = *(Shared*)(smem + kWarps * S::RING);
+  int* const cum = (int*)(&sh + 1);
+  uint8_t* const last = (uint8_t*)(cum + p.table.B + 1);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int B = p.table.B, LH = p.nlayers * p.g.N_kv, grid = gridDim.x, cta = blockIdx.x;
+
+  // ---- tiles of every sequence, cumulated
+  bool empty = false;
+  {
+    const int per = (B + kThreads - 1) / kThreads, b0 = min(B, tid * per), b1 = min(B, b0 + per);
+    const int cap = p.table.max_pages * kPageTokens;
+    int mine = 0;
+    for (int b = b0; b < b1; ++b) {
+      int n = __ldg(p.seq_len + b);
+      if (n > cap) {
+        n = cap;
+        if (cta == 0) atomicOr(p.error, kErrPage);
+      }
+      const int nt = n > 0 ? (n + kPageTokens - 1) / kPageTokens : 0;
+      empty |= nt == 0;
+      last[b] = (uint8_t)((n - 1) & (kPageTokens - 1));
+      cum[b + 1] = nt;
+      mine += nt;
+    }
+    int x = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 31) sh.warp_sum[warp] = x;
+    empty = __syncthreads_or(empty);
+    int base = x - mine;
+    for (int w = 0; w < warp; ++w) base += sh.warp_sum[w];
+    for (int b = b0; b < b1; ++b) {
+      base += cum[b + 1];
+      cum[b + 1] = base;
+    }
+    if (tid == 0) cum[0] = 0;
+    __syncthreads();
+  }
+  const Tables tab = {cum, last};
+
+  // ---- sequences without tokens
+  if (empty) {
+    for (int64_t i = (int64_t)cta * kWarps + warp; i < (int64_t)B * LH; i += (int64_t)grid * kWarps) {
+      const int b = (int)(i / LH);
+      if (cum[b + 1] != cum[b]) continue;
+      const int64_t row = i * p.G;              // units in order are query rows in order
+      uint4* const o = (uint4*)((uint8_t*)p.out + row * D * EO);
+      for (int e = lane; e < p.G * D * EO / 16; e += 32) o[e] = make_uint4(0u, 0u, 0u, 0u);
+      if (p.lse && lane < p.G) p.lse[row + lane] = -INFINITY;
+    }
+  }
+
+  const int64_t total = (int64_t)cum[B] * LH;
+  const int64_t F0 = split_begin(total, grid, cta), F1 = split_begin(total, grid, cta + 1);
+  if (F0 == F1) return;
+  const int64_t f0 = F0 + split_begin(F1 - F0, kWarps, warp), f1 = F0 + split_begin(F1 - F0, kWarps, warp + 1);
+  Record<D>* const records = (Record<D>*)p.records;
+  Record<D>* const cta_rec = records + 2 * cta;                                         // units shared with other CTAs
+  Record<D>* const head_rec = records + 2 * grid + (cta * kWarps + warp);               // the warp's first unit
+  Record<D>* const tail_rec = (Record<D>*)(smem + warp * S::RING);                      // its last unit
+  if (lane == 0) {
+    sh.info[warp].f0 = f0;
+    sh.info[warp].f1 = f1;
+  }
+
+  if (f0 < f1) {
+    const uint32_t ring = smem_u32(smem) + warp * S::RING;
+    State st;
+    if constexpr (E == 4) st.sp = sh.sp[warp];
+
+    // ---- producer: fills the ring tile after tile
+    Cursor pc = locate(tab, B, LH, f0);
+    int64_t p_left = f1 - f0;                   // tiles not begun, the current one included
+    int p_slot = 0, p_row = 0, p_ntok = 0;      // ring slot; next row of the current tile and its rows
+    const uint8_t* p_block = nullptr;
+    bool p_ok = false;
+    int p_page = __ldg(p.table.table + pc.b * p.table.stride + pc.j);       // of the current tile
+    auto open_tile = [&]() {
+      p_ok = (uint32_t)p_page < (uint32_t)p.g.num_pages;
+      if (!p_ok && lane == 0) atomicOr(p.error, kErrPage);
+      const int ll = pc.u / p.g.N_kv, h = pc.u - ll * p.g.N_kv;
+      p_block = p.pages + page_block_offset(p.g, p.layer0 + ll, p_ok ? p_page : 0, h);
+      p_row = 0;
+      p_ntok = min(kPageTokens, pc.len - pc.j * kPageTokens);
+      if (--p_left > 0) {                       // look the next tile's page up ahead of time
+        if (++pc.j == pc.nt) next_unit(tab, B, LH, pc);
+        p_page = __ldg(p.table.table + pc.b * p.table.stride + pc.j);
+      }
+    };
+    auto issue = [&]() {
+      if (p_row >= p_ntok && p_left > 0) open_tile();
+      if (p_row < p_ntok) {
+        const uint32_t sb = ring + p_slot * S::STAGE;
+        const int n = p_ok ? min(S::ST, p_ntok - p_row) : 0;
+        const uint8_t* const kr = p_block + p_row * S::RB;
+        constexpr int CPR = S::RB / 16, RPI = 32 / CPR > 0 ? 32 / CPR : 1, IT = S::HALF / 512;
+        const int r0 = CPR < 32 ? lane / CPR : 0, ck = lane % CPR;
+#pragma unroll
+        for (int it = 0; it < IT; ++it) {
+          const int r = it * RPI + r0;
+          const uint32_t d = sb + (S::F32 ? (it * 512 + lane * 16) : swz<S::RB>(r, ck));
+          const int row = S::F32 ? (it * 512 + lane * 16) / S::RB : r;
+          if (n == S::ST) {
+            cp16(d, kr + it * 512 + lane * 16);
+            cp16(d + S::HALF, kr + kPageTokens * S::RB + it * 512 + lane * 16);
+          } else {                              // rows that do not count become zeros
+            const bool on = row < n;
+            cp16(d, on ? kr + it * 512 + lane * 16 : p_block, on ? 16 : 0);
+            cp16(d + S::HALF, on ? kr + kPageTokens * S::RB + it * 512 + lane * 16 : p_block, on ? 16 : 0);
+          }
+        }
+        if constexpr (S::SB > 0) {
+          constexpr int C = S::ST * S::SB / 16;              // 16-byte pieces of the key scales
+          static_assert(2 * C <= 32 && S::ST * S::SB % 16 == 0, "one piece a lane");
+          if (lane < 2 * C) {
+            const int part = lane / C, i = lane % C;
+            const int bytes = max(0, min(16, n * S::SB - 16 * i));
+            const uint8_t* src = p_block + 2 * kPageTokens * S::RB + part * kPageTokens * S::SB + p_row * S::SB + 16 * i;
+            cp16(sb + 2 * S::HALF + part * S::ST * S::SB + 16 * i, bytes ? src : p_block, bytes);
+          }
+        }
+        if (lane == 0) sh.valid[warp][p_slot] = n;
+        p_row += S::ST;
+      }
+      cp_commit();                              // one group a call, possibly empty
+      p_slot = p_slot + 1 == S::STAGES ? 0 : p_slot + 1;
+    };
+#pragma unroll 1
+    for (int i = 0; i < S::STAGES - 1; ++i) issue();
+
+    // ---- consumer: unit after unit
+    int slot = 0;
+    Cursor c = locate(tab, B, LH, f0);
+    int64_t f = f0;
+    while (true) {
+      const int64_t us = f - c.j, ue = us + c.nt, se = f1 < ue ? f1 : ue;
+      const int j1 = c.j + (int)(se - f);
+      const int ntok = min(c.len, j1 * kPageTokens) - c.j * kPageTokens;
+      const int64_t row = ((int64_t)c.b * LH + c.u) * p.G;   // first query row
+      st.begin((const uint8_t*)p.q + row * D * E, p.G, p.scale_log2, lane);
+#pragma unroll 1
+      for (int left = ntok; left > 0; left -= S::ST) {
+        cp_wait<S::STAGES - 2>();
+        __syncwarp();                           // the step has landed; all lanes are done with the slot before
+        const int n = sh.valid[warp][slot];
+        issue();
+        st.step(ring + slot * S::STAGE, n, lane);
+        slot = slot + 1 == S::STAGES ? 0 : slot + 1;
+      }
+      st.end();
+      const bool whole = f == us && se == ue, is_last = se == f1;
+      if (whole) {
+        st.store_out((uint8_t*)p.out + row * D * EO, p.lse ? p.lse + row : nullptr, p.G, lane);
+      } else if (is_last) {
+        cp_wait<0>();
+        __syncwarp();
+        st.store_record(tail_rec, p.G, lane);
+      } else {
+        st.store_record(head_rec, p.G, lane);
+      }
+      if (lane == 0) {
+        WarpInfo& wi = sh.info[warp];
+        if (f == f0) {
+          wi.first_unit = c.b * LH + c.u;
+          wi.first_us = us;
+          wi.first_ue = ue;
+        }
+        wi.last_unit = c.b * LH + c.u;
+        wi.last_us = us;
+        wi.last_ue = ue;
+      }
+      f = se;
+      if (is_last) break;
+      next_unit(tab, B, LH, c);
+    }
+    cp_wait<0>();
+  }
+  __syncthreads();
+
+  // ---- join what the warps of this CTA share; `leader`: the first warp of the CTA that worked on the unit
+  float acc[kMaxG * D / kThreads];
+  auto emit = [&](const int64_t row) {          // joined accumulators -> output
+#pragma unroll
+    for (int k = 0; k < kMaxG * D / kThreads; ++k) {
+      const int e = tid + kThreads * k, g = e / D;
+      if (g < p.G) {
+        const float fa = finish<FMT == THINK_PAGE_PLAIN>(sh.stat[0][g], sh.stat[1][g], sh.stat[2][g]);
+        const float x = fa == 0.f ? 0.f : acc[k] * fa;
+        if (EO == 4) ((float*)p.out)[row * D + e] = x;
+        else ((__nv_bfloat16*)p.out)[row * D + e] = __float2bfloat16_rn(x);
+        if (p.lse && e % D == 0) p.lse[row + g] = log_sum(sh.stat[0][g], sh.stat[2][g]);
+      }
+    }
+  };
+  int first_warp = 0;
+  while (sh.info[first_warp].f0 == sh.info[first_warp].f1) ++first_warp;
+  bool shared_before = false, shared_after = false;          // units shared with other CTAs
+  for (int w = first_warp - 1; w < kWarps; ++w) {
+    // round first_warp - 1: the unit that the CTA's first warp finishes for earlier CTAs; then every warp's last unit
+    const bool head = w < first_warp;
+    const WarpInfo& wi = sh.info[head ? first_warp : w];
+    if (wi.f0 == wi.f1) continue;
+    const int64_t us = head ? wi.first_us : wi.last_us, ue = head ? wi.first_ue : wi.last_ue;
+    const int unit = head ? wi.first_unit : wi.last_unit;
+    if (head) {
+      if (wi.first_unit == wi.last_unit || us >= F0) continue;       // one unit only, or a whole one
+    } else {
+      if (us >= wi.f0 && ue <= wi.f1) continue;                      // whole
+      if (us < wi.f0 && w != first_warp) continue;                   // an earlier warp leads
+    }
+    const int lead = head ? first_warp : w;
+    const int64_t end = ue < F1 ? ue : F1;
+    const int until = head ? lead : split_owner(F1 - F0, kWarps, end - 1 - F0);
+    // contributors: warps lead .. until that have tiles
+    int n = 0;
+    uint32_t who = 0;                                                // 4 bits a contributor
+    for (int v = lead; v <= until; ++v)
+      if (sh.info[v].f0 < sh.info[v].f1) who |= (uint32_t)v << (4 * n++);
+    auto rec = [&](int i) -> const Record<D>* {
+      const int v = (int)(who >> (4 * i)) & 15;
+      return sh.info[v].last_unit == unit ? (const Record<D>*)(smem + v * S::RING) : records + 2 * grid + (cta * kWarps + v);
+    };
+    // states in shared or global memory written by this CTA: plain loads
+    join<D, false>(n, p.G, rec, sh.weight, sh.stat, acc);
+    if (us >= F0 && ue <= F1) {
+      emit((int64_t)unit * p.G);
+    } else {
+      const int slot = us < F0 ? 0 : 1;
+      shared_before |= slot == 0;
+      shared_after |= slot == 1;
+      Record<D>* const r = cta_rec + slot;
+#pragma unroll
+      for (int k = 0; k < kMaxG * D / kThreads; ++k) {
+        const int e = tid + kThreads * k, g = e / D;
+        if (g < p.G) {
+          (&r->o[0][0])[e] = acc[k];
+          if (e % D == 0) {
+            r->m[g] = sh.stat[0][g];
+            r->M[g] = sh.stat[1][g];
+            r->l[g] = sh.stat[2][g];
+          }
+        }
+      }
+    }
+    __syncthreads();                            // stat and weight are free again
+  }
+  if (!shared_before && !shared_after) return;
+
+  // ---- tickets of the units shared with other CTAs; the last to arrive joins them
+  __threadfence();
+  __syncthreads();
+  // the first unit of the CTA if it began in an earlier one; the last one if it goes on
+  int lw = kWarps - 1;
+  while (sh.info[lw].f0 == sh.info[lw].f1) --lw;
+  for (int k = 0; k < 2; ++k) {
+    if (!(k == 0 ? shared_before : shared_after)) continue;
+    const WarpInfo& wi = sh.info[k == 0 ? first_warp : lw];
+    const int64_t us = k == 0 ? wi.first_us : wi.last_us, ue = k == 0 ? wi.first_ue : wi.last_ue;
+    const int unit = k == 0 ? wi.first_unit : wi.last_unit;
+    const int c0 = split_owner(total, grid, us), c1 = split_owner(total, grid, ue - 1);
+    // CTAs without tiles (fewer tiles than CTAs) take no part
+    int n = 0;
+    const bool sparse = total < grid;
+    n = sparse ? (int)(ue - us) : c1 - c0 + 1;
+    if (tid == 0) {
+      const unsigned t = atomicAdd(p.counters + unit, 1u);
+      sh.arrived[k] = t == (unsigned)(n - 1);
+      if (sh.arrived[k]) p.counters[unit] = 0u;              // ready for the next call
+    }
+    __syncthreads();
+    if (!sh.arrived[k]) continue;
+    __threadfence();
+    auto rec = [&](int i) -> const Record<D>* {
+      const int ci = sparse ? split_owner(total, grid, us + i) : c0 + i;
+      return records + 2 * ci + (split_begin(total, grid, ci) > us ? 0 : 1);
+    };
+    join<D, true>(n, p.G, rec, (float*)smem, sh.stat, acc);
+    emit((int64_t)unit * p.G);
+    __syncthreads();
   }
 }
 
 template <int D, int E, int FMT>
-__global__ void __launch_bounds__(kThreads) k_paged_decode(const PagedDecodeParams p) {
-  constexpr int N = D / 32;
-  __shared__ float so[kWarps][kMaxPagedGroup][D];
-  __shared__ float sm[kWarps][kMaxPagedGroup], sl[kWarps][kMaxPagedGroup];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int h = blockIdx.x % p.g.N_kv, ll = blockIdx.x / p.g.N_kv, b = blockIdx.y;
-  const int cap = p.table.max_pages * kPageTokens;
-  int len = __ldg(p.seq_len + b);
-  if (len > cap) {
-    if (threadIdx.x == 0) atomicOr(p.error, kErrPage);
-    len = cap;
-  }
-  const int64_t q0 = ((int64_t)(b * p.nlayers + ll) * p.N_q + h * p.G);
-  float q[kMaxPagedGroup][N], o[kMaxPagedGroup][N], m[kMaxPagedGroup], l[kMaxPagedGroup];
-#pragma unroll
-  for (int g = 0; g < kMaxPagedGroup; ++g) {
-    m[g] = -INFINITY;
-    l[g] = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      o[g][i] = 0.f;
-      const int64_t e = (q0 + g) * D + lane * N + i;
-      q[g][i] = g >= p.G ? 0.f : E == 4 ? ((const float*)p.q)[e] : __bfloat162float(((const __nv_bfloat16*)p.q)[e]);
-      q[g][i] *= p.scale_log2;
-    }
-  }
-  for (int t = warp; t < len; t += kWarps) {
-    const int page = page_of(p.table, p.g, b, t, p.error);
-    if (page < 0) continue;
-    const uint8_t* block = p.pages + page_block_offset(p.g, p.layer0 + ll, page, h);
-    const int slot = t & (kPageTokens - 1);
-    float k[N], v[N];
-    load_row<E, FMT, N>(block + page_part_offset(p.g, 0) + slot * p.g.row_bytes, block + page_part_offset(p.g, 2) + slot * p.g.scale_bytes, lane * N, k);
-    load_row<E, FMT, N>(block + page_part_offset(p.g, 1) + slot * p.g.row_bytes, block + page_part_offset(p.g, 3) + slot * p.g.scale_bytes, lane * N, v);
-#pragma unroll
-    for (int g = 0; g < kMaxPagedGroup; ++g) {
-      if (g >= p.G) break;
-      float x = 0.f;
-#pragma unroll
-      for (int i = 0; i < N; ++i) x = fmaf(q[g][i], k[i], x);
-#pragma unroll
-      for (int i = 1; i < 32; i <<= 1) x += __shfl_xor_sync(0xffffffffu, x, i);
-      const float mn = fmaxf(m[g], x), a = exp2f(m[g] - mn), w = exp2f(x - mn);
-      m[g] = mn;
-      l[g] = l[g] * a + w;
-#pragma unroll
-      for (int i = 0; i < N; ++i) o[g][i] = fmaf(w, v[i], o[g][i] * a);
-    }
-  }
-#pragma unroll
-  for (int g = 0; g < kMaxPagedGroup; ++g) {
-    if (lane == 0) {
-      sm[warp][g] = m[g];
-      sl[warp][g] = l[g];
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i) so[warp][g][lane * N + i] = o[g][i];
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i < p.G * D; i += kThreads) {
-    const int g = i / D, c = i % D;
-    float M = -INFINITY, L = 0.f, x = 0.f;
-    for (int w = 0; w < kWarps; ++w) M = fmaxf(M, sm[w][g]);
-    if (M > -INFINITY) {
-      for (int w = 0; w < kWarps; ++w) {
-        const float a = exp2f(sm[w][g] - M);
-        L += a * sl[w][g];
-        x += a * so[w][g][c];
-      }
-      x /= L;
-    }
-    if (E == 4) ((float*)p.out)[(q0 + g) * D + c] = x;
-    else ((__nv_bfloat16*)p.out)[(q0 + g) * D + c] = __float2bfloat16_rn(x);
-    if (c == 0 && p.lse) p.lse[q0 + g] = M > -INFINITY ? (M + log2f(L)) * 0.69314718055994530942f : -INFINITY;
-  }
-}
+constexpr size_t smem_fixed() { return (size_t)kWarps * Shape<D, E, FMT>::RING + sizeof(Shared); }
+inline size_t smem_tables(int B) { return ((size_t)(B + 1) * 4 + B + 15) / 16 * 16; }
 
-template <int D>
-cudaError_t launch_d(const PagedDecodeParams& p, int dtype, int format, cudaStream_t s) {
-  const dim3 grid((unsigned)(p.nlayers * p.g.N_kv), (unsigned)p.table.B);
-  if (dtype == THINK_F32) k_paged_decode<D, 4, THINK_PAGE_PLAIN><<<grid, kThreads, 0, s>>>(p);
-  else if (format == THINK_PAGE_PLAIN) k_paged_decode<D, 2, THINK_PAGE_PLAIN><<<grid, kThreads, 0, s>>>(p);
-  else if (format == THINK_PAGE_E4M3) k_paged_decode<D, 2, THINK_PAGE_E4M3><<<grid, kThreads, 0, s>>>(p);
-  else k_paged_decode<D, 2, THINK_PAGE_INT4><<<grid, kThreads, 0, s>>>(p);
+template <int D, int E, int FMT, int GP>
+cudaError_t launch_k(const PagedDecodeParams& p, cudaStream_t s) {
+  const size_t smem = smem_fixed<D, E, FMT>() + smem_tables(p.table.B);
+  k_paged_decode<D, E, FMT, GP><<<p.grid, kThreads, smem, s>>>(p);
   return cudaGetLastError();
 }
+template <int D, int E, int FMT, int GP>
+cudaError_t setup_k() {
+  static_assert(smem_fixed<D, E, FMT>() + kMaxPagedBatch * 5 + 32 <= 227 * 1024, "shared memory of a CTA");
+  return cudaFuncSetAttribute(k_paged_decode<D, E, FMT, GP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)(smem_fixed<D, E, FMT>() + smem_tables(kMaxPagedBatch)));
+}
+
+#define THINK_PAGED_DISPATCH(FN, ...)                                                          \
+  do {                                                                                         \
+    if (dtype == THINK_F32) switch (gp) {                                                      \
+      case 1: return D == 128 ? FN<128, 4, THINK_PAGE_PLAIN, 1>(__VA_ARGS__) : FN<64, 4, THINK_PAGE_PLAIN, 1>(__VA_ARGS__); \
+      case 2: return D == 128 ? FN<128, 4, THINK_PAGE_PLAIN, 2>(__VA_ARGS__) : FN<64, 4, THINK_PAGE_PLAIN, 2>(__VA_ARGS__); \
+      case 4: return D == 128 ? FN<128, 4, THINK_PAGE_PLAIN, 4>(__VA_ARGS__) : FN<64, 4, THINK_PAGE_PLAIN, 4>(__VA_ARGS__); \
+      default: return D == 128 ? FN<128, 4, THINK_PAGE_PLAIN, 8>(__VA_ARGS__) : FN<64, 4, THINK_PAGE_PLAIN, 8>(__VA_ARGS__); \
+    }                                                                                          \
+    switch (format) {                                                                          \
+      case THINK_PAGE_PLAIN: return D == 128 ? FN<128, 2, THINK_PAGE_PLAIN, 8>(__VA_ARGS__) : FN<64, 2, THINK_PAGE_PLAIN, 8>(__VA_ARGS__); \
+      case THINK_PAGE_E4M3: return D == 128 ? FN<128, 2, THINK_PAGE_E4M3, 8>(__VA_ARGS__) : FN<64, 2, THINK_PAGE_E4M3, 8>(__VA_ARGS__); \
+      default: return D == 128 ? FN<128, 2, THINK_PAGE_INT4, 8>(__VA_ARGS__) : FN<64, 2, THINK_PAGE_INT4, 8>(__VA_ARGS__); \
+    }                                                                                          \
+  } while (0)
+
+int padded_group(int G) { return G <= 1 ? 1 : G <= 2 ? 2 : G <= 4 ? 4 : 8; }
 
 }  // namespace
 
 cudaError_t launch_paged_decode(const PagedDecodeParams& p, int dtype, int format, cudaStream_t s) {
-  return p.g.D == 128 ? launch_d<128>(p, dtype, format, s) : launch_d<64>(p, dtype, format, s);
+  const int D = p.g.D, gp = padded_group(p.G);
+  THINK_PAGED_DISPATCH(launch_k, p, s);
 }
-cudaError_t paged_decode_setup(int, int, int) { return cudaSuccess; }
-int paged_decode_max_ctas(int num_sms) { return num_sms; }
-size_t paged_decode_record_bytes(int D, int G) { return rec_size(D, G); }
+cudaError_t paged_decode_setup(int dtype, int format, int D, int G) {
+  const int gp = padded_group(G);
+  THINK_PAGED_DISPATCH(setup_k);
+}
+// two records a CTA for units shared between CTAs, one a warp for units shared between warps
+size_t paged_decode_record_bytes(int D, int ctas) {
+  return (size_t)ctas * (2 + kWarps) * (D == 128 ? sizeof(Record<128>) : sizeof(Record<64>));
+}
 
 }  // namespace think

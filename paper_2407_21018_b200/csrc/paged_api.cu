@@ -66,7 +66,7 @@ thinK_status make_geometry(const thinK_paged_config* c, Geometry* o) {
 void make_layout(const Geometry& g, Layout* w) {
   w->counters = 256;                                   // the error word is in front
   w->records = align_up(w->counters + sizeof(uint32_t) * (size_t)g.max_batch * g.g.L * g.g.N_kv, 256);
-  w->total = w->records + (size_t)paged_decode_max_ctas(kSMs) * 2 * paged_decode_record_bytes(g.g.D, g.G);
+  w->total = align_up(w->records + paged_decode_record_bytes(g.g.D, kSMs), 256);
 }
 
 bool table_ok(const Geometry& g, const thinK_page_table& t) {
@@ -160,12 +160,12 @@ thinK_status thinK_paged_create(const thinK_paged_config* cfg, const thinK_paged
   p->ws = (uint8_t*)workspace;
   int dev = 0, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
-      paged_decode_setup(p->g.dtype, p->g.format, p->g.g.D) != cudaSuccess ||
+      paged_decode_setup(p->g.dtype, p->g.format, p->g.g.D, p->g.G) != cudaSuccess ||
       cudaMemset(p->ws, 0, p->w.records) != cudaSuccess || cudaStreamSynchronize(cudaStreamLegacy) != cudaSuccess) {
     delete p;
     return THINK_ERR_CUDA;
   }
-  p->grid = paged_decode_max_ctas(sms < kSMs ? sms : kSMs);
+  p->grid = sms < kSMs ? sms : kSMs;                 // one wave, one CTA an SM
   *out = p;
   return THINK_OK;
 }
@@ -204,6 +204,9 @@ thinK_status thinK_paged_decode_attn(thinK_paged* p, const void* q, void* out, f
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(seq_len, 4)) return THINK_ERR_INVALID_ARG;
   if (scratch && !aligned(scratch, 256)) return THINK_ERR_INVALID_ARG;
   if (scratch && scratch_bytes < p->w.total) return THINK_ERR_CAPACITY;
+  // tiles are counted in 32 bits per sequence set, in 52 over all layers and heads
+  const int64_t tiles = (int64_t)table.B * table.max_pages;
+  if (tiles > INT32_MAX || (double)tiles * nlayers * p->g.g.N_kv > 4.0e15) return THINK_ERR_UNSUPPORTED;
   uint8_t* const ws = scratch ? (uint8_t*)scratch : p->ws;
   PagedDecodeParams d;
   memset((void*)&d, 0, sizeof(d));

@@ -86,10 +86,8 @@ struct PagedDecodeParams {
 
 cudaError_t launch_paged_rows(const PagedRowsParams& p, int dtype, int format, bool write, cudaStream_t s);
 cudaError_t launch_paged_decode(const PagedDecodeParams& p, int dtype, int format, cudaStream_t s);
-cudaError_t paged_decode_setup(int dtype, int format, int D);
-// CTAs of a decode launch at most, and bytes of their partial states
-int paged_decode_max_ctas(int num_sms);
-size_t paged_decode_record_bytes(int D, int G);
+cudaError_t paged_decode_setup(int dtype, int format, int D, int G);   // kernel attributes on the current device
+size_t paged_decode_record_bytes(int D, int ctas);                     // partial states of a launch of that many CTAs
 
 #ifdef __CUDACC__
 // Page that holds token t of entry b, or -1 (error bit) if the table or the position is out of range.

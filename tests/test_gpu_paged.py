@@ -104,8 +104,8 @@ class Paged:
                         continue
                     hs = slice(h * self.G, (h + 1) * self.G)
                     k, v = self.stored(b, l, h, lens[b])
-                    out, lse, absv, mag = po.attention(q64[b, l, hs], k, v, self.scale)
-                    yield (b, l, hs, out, lse) + bounds(out, lse, absv, mag, lens[b], self.D, self.dtype)
+                    r = po.attention(q64[b, l, hs], k, v, self.scale)
+                    yield (b, l, hs, r[0], r[1]) + bounds(*r, lens[b], self.D, self.dtype)
 
     def check(self, q, out, lse=None, lens=None, units=None):
         o64 = out.double().cpu().numpy()
@@ -125,7 +125,7 @@ class Paged:
         return worst
 
 
-def bounds(out, lse, absv, mag, n, D, dtype):
+def bounds(out, lse, absv, mag, top, n, D, dtype):
     """Error bounds of one head, first order in the roundings.
 
     With u = 2^-23 (one fp32 operation, also where the tensor core's adder truncates):
@@ -133,12 +133,17 @@ def bounds(out, lse, absv, mag, n, D, dtype):
                 base 2 and the maximum's subtraction included.  A weight exp(x) then carries twice that (its own and
                 the denominator's) relative error, plus 2^-21 for exp2 and 2^-11 where weights are rounded to 16 bits.
       sums      n terms added in fp32 in any order: n u, numerator and denominator.
+      floor     a 16-bit weight has a smallest step of 2^-24, with the largest weight * scale between 2^14 and 2^15:
+                each token is off by at most 2^-39 of that product, whose codes are at most 448 (7) of a scale of
+                which the row's largest value has at least 224 (7/2): 2^-38 of top = max w |v|.
     Weighted with |v| these are relative to absv = sum w |v|.  The output is rounded once to its type: half a step,
     finfo.eps / 2 relative."""
     u = 2.0 ** -23
     delta = (D + 4) * u * np.asarray(mag)
     weights = 2 * delta + 2.0 ** -21 + (2.0 ** -11 if dtype == torch.bfloat16 else 0.0) + 2 * (n + 8) * u
     tol = torch.finfo(dtype).eps / 2 * np.abs(out) + weights[:, None] * absv * (1 + 2.0 ** -7) + 1e-30
+    if dtype == torch.bfloat16:
+        tol = tol + n * 2.0 ** -38 * np.asarray(top)[:, None]
     ltol = delta + (n + 8) * u + 2.0 ** -21 + 4 * u * np.abs(np.where(np.isfinite(lse), lse, 0.0))
     return tol, ltol
 
@@ -424,8 +429,9 @@ def test_attention_bad_pages_and_lengths(fmt, dtype):
         for h in range(2):
             hs = slice(2 * h, 2 * h + 2)
             kk, vv = p.stored(b, 0, h, lens[b])
-            w, wl_, absv, mag = po.attention(q64[b, 0, hs], kk[keep], vv[keep], p.scale)
-            tol, ltol = bounds(w, wl_, absv, mag, len(keep), 128, dtype)
+            r = po.attention(q64[b, 0, hs], kk[keep], vv[keep], p.scale)
+            w, wl_ = r[:2]
+            tol, ltol = bounds(*r, len(keep), 128, dtype)
             assert (np.abs(out[b, 0, hs].double().cpu().numpy() - w) <= tol).all()
             assert (np.abs(lse[b, 0, hs].double().cpu().numpy() - wl_) <= ltol).all()
     # longer than the table

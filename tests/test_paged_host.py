@@ -128,3 +128,28 @@ int main() {
 }
 """)
     assert out.strip() == "0"
+
+
+def test_split_of_tiles(tmp_path):
+    """Parts of a flat tile list are contiguous, differ by one tile at most, and the owner of a tile is the part that
+    holds it - at sizes of a few tiles and of 2^50."""
+    out = compile_and_run(tmp_path, r"""
+#include <stdio.h>
+#include "paged_split.h"
+using namespace think;
+int main() {
+  long bad = 0;
+  for (int parts : {1, 2, 7, 8, 132, 148})
+    for (int64_t n : {int64_t(1), int64_t(2), int64_t(7), int64_t(147), int64_t(148), int64_t(149), int64_t(1000), int64_t(54321), int64_t(1) << 50}) {
+      bad += split_begin(n, parts, 0) != 0 || split_begin(n, parts, parts) != n;
+      for (int i = 0; i < parts; ++i) {
+        const int64_t a = split_begin(n, parts, i), b = split_begin(n, parts, i + 1);
+        bad += b < a || b - a > n / parts + 1;
+        for (int64_t f : {a, a + 1, (a + b) / 2, b - 1})
+          if (f >= a && f < b) bad += split_owner(n, parts, f) != i;
+      }
+    }
+  printf("%ld\n", bad);
+}
+""")
+    assert out.strip() == "0"
