@@ -151,7 +151,7 @@ __device__ __forceinline__ Cursor locate(const Tables& t, int B, int LH, int64_t
   c.b = lo;
   seq_of(t, c);
   const int64_t rem = f - (int64_t)t.cum[lo] * LH;
-  c.u = (int)(rem / c.nt);
+  c.u = (int)div_wide(rem, c.nt);
   c.j = (int)(rem - (int64_t)c.u * c.nt);
   return c;
 }
@@ -783,7 +783,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_decode(const PagedDecodeP
   // ---- sequences without tokens
   if (empty) {
     for (int64_t i = (int64_t)cta * kWarps + warp; i < (int64_t)B * LH; i += (int64_t)grid * kWarps) {
-      const int b = (int)(i / LH);
+      const int b = (int)div_wide(i, LH);
       if (cum[b + 1] != cum[b]) continue;
       const int64_t row = i * p.G;              // units in order are query rows in order
       uint4* const o = (uint4*)((uint8_t*)p.out + row * D * EO);
@@ -1012,11 +1012,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_decode(const PagedDecodeP
     __syncthreads();
     if (!sh.arrived[k]) continue;
     __threadfence();
-    auto rec = [&](int i) -> const Record<D>* {
-      const int ci = sparse ? split_owner(total, grid, us + i) : c0 + i;
-      return records + 2 * ci + (split_begin(total, grid, ci) > us ? 0 : 1);
-    };
-    join<D, true>(n, p.G, rec, (float*)smem, sh.stat, acc);
+    // the unit began in the first contributor (its record 1); for all others it is the unit that they began with
+    int* const cta_of = (int*)smem;
+    for (int i = tid; i < n; i += kThreads) cta_of[i] = sparse ? split_owner(total, grid, us + i) : c0 + i;
+    __syncthreads();
+    auto rec = [&](int i) -> const Record<D>* { return records + 2 * cta_of[i] + (i == 0); };
+    join<D, true>(n, p.G, rec, (float*)smem + kSMs, sh.stat, acc);
     emit((int64_t)unit * p.G);
     __syncthreads();
   }

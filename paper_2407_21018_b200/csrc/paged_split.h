@@ -11,9 +11,13 @@
 
 namespace think {
 
+// a / b, through the 32-bit division where both fit (a 64-bit one is a routine of a hundred instructions)
+THINK_HD int64_t div_wide(int64_t a, int64_t b) {
+  return (uint64_t)(a | b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
+}
 // part i of n tiles cut into `parts`: [split_begin(i), split_begin(i + 1)); n * parts fits 62 bits
-THINK_HD int64_t split_begin(int64_t n, int parts, int i) { return (int64_t)i * n / parts; }
+THINK_HD int64_t split_begin(int64_t n, int parts, int i) { return div_wide((int64_t)i * n, parts); }
 // the part that owns tile f, 0 <= f < n
-THINK_HD int split_owner(int64_t n, int parts, int64_t f) { return (int)(((f + 1) * parts - 1) / n); }
+THINK_HD int split_owner(int64_t n, int parts, int64_t f) { return (int)div_wide((f + 1) * parts - 1, n); }
 
 }  // namespace think
