@@ -8,17 +8,23 @@
 //  * A warp is the worker.  It owns a ring of stages in shared memory that it fills with cp.async, crossing page and
 //    unit borders, and waits for nobody until its range is done.
 //  * Rows are stored token-major.  16-byte chunks are XOR-swizzled on the way into shared memory so that ldmatrix
-//    reads without bank conflicts: plain for q K^T (contraction over channels), transposed for p V (over tokens).
-//    Products run on mma.sync m16n8k16 with the group's query heads as rows 0..7 of A; one query row per head fills
-//    at most 8 of the 128 rows that a tcgen05 tile would have.
-//      bf16  weights as a bf16 pair: the high halves are rows 0..7, the low halves rows 8..15 of the same
-//            instruction, so the second half costs no instruction and weights carry 2^-17 instead of 2^-9.
-//      e4m3, int4  codes become f16 exactly (byte conversion; 1024 + n by bit patterns) and never see their scales:
-//            a key's scale multiplies its logit, a value's scale goes into the weight.  Weights are rounded to f16,
-//            2^-11, relative to the largest weight * scale so far, which sits at 2^15: f16 leaves 29 binary orders
-//            below it before its step stops shrinking.  q is f16 times a power of two, exact unless its channels
-//            are more than 2^29 apart.
-//      fp32  CUDA cores: fp32 products summed over lanes pairwise.
+//    reads without bank conflicts.  Products run on mma.sync (a group has at most 8 query rows: 8 of the 128 rows
+//    that a tcgen05 tile would have), arranged so that all 16 x 8 results of an instruction count:
+//      logits  A = queries (16 rows), B = keys.  e4m3 and 4-bit keys go to the fp8 instruction (m16n8k32, four times
+//              the rate of f16 per product) as they are: an e4m3 byte is its own operand and a 4-bit code c, as a byte
+//              0..15, IS the e4m3 number c * 2^-9, so unpacking is a mask.  The query is split into two e4m3 parts,
+//              high parts in rows 0..7 and 16 * low parts in rows 8..15: exact for bf16 queries whose channels lie
+//              within 2^13 of the row's largest, else off by at most 2^-21 of that one.  The instruction sums 32
+//              products to 2^-22 of their magnitudes (measured), like the 16-bit ones.  bf16 keys use m16n8k16.
+//      values  A = values transposed (16 channels x 16 tokens, ldmatrix.trans), B = weights.  bf16: the weights are a
+//              bf16 pair high + low (two instructions), 2^-17.  e4m3: bytes become f16 exactly.  4-bit: a code
+//              under the exponent of 64 is the f16 number 64 + c, a shift and a bit select.  The offset 72 = 64 + 8 is
+//              taken off at the end: 72 * sum of the very same rounded weights comes from one more product with a
+//              constant A.  (A code as a subnormal f16 would need no offset of 64, but the instruction aligns products
+//              by exponent fields: its sums then keep 2^-15 instead of 2^-22, measured.)
+//      scales  of keys multiply logits, those of values go into the weights, which are rounded to f16 (2^-11)
+//              relative to the largest weight * scale so far, put at 2^15: f16 leaves 29 binary orders below it.
+//      fp32    CUDA cores: fp32 products summed over lanes pairwise.
 //  * The softmax is online in base 2 with fp32 maximum, sum and accumulators.  Units that several warps share leave
 //    partial states; the warps' states are joined by their CTA, the CTAs' states by the CTA that arrives last at
 //    the unit's ticket, always in token order, so results do not depend on timing.
@@ -32,21 +38,39 @@
 namespace think {
 namespace {
 
-constexpr int kWarps = 8;
-constexpr int kThreads = kWarps * 32;
+constexpr int kMaxWarps = 16;
 constexpr int kMaxG = kMaxPagedGroup;
 
+#ifndef THINK_PW_PLAIN
+#define THINK_PW_PLAIN 8
+#endif
+#ifndef THINK_PW_E4M3
+#define THINK_PW_E4M3 12
+#endif
+#ifndef THINK_PW_INT4
+#define THINK_PW_INT4 12
+#endif
+#ifndef THINK_ST_E4M3
+#define THINK_ST_E4M3 32
+#endif
+#ifndef THINK_ST_INT4
+#define THINK_ST_INT4 32
+#endif
 template <int D, int E, int FMT>
 struct Shape {
   static constexpr bool F32 = E == 4;
+  static constexpr int WARPS = FMT == THINK_PAGE_PLAIN ? THINK_PW_PLAIN : FMT == THINK_PAGE_E4M3 ? THINK_PW_E4M3 : THINK_PW_INT4;
+  static constexpr int THREADS = WARPS * 32;
   static constexpr int RB = FMT == THINK_PAGE_PLAIN ? D * E : FMT == THINK_PAGE_E4M3 ? D : D / 2;   // bytes of a row
   static constexpr int SB = FMT == THINK_PAGE_PLAIN ? 0 : FMT == THINK_PAGE_E4M3 ? 1 : D / 16;      // bytes of its scales
-  // tokens of a step: 8 KB of keys and values, at most 32 tokens
-  static constexpr int ST = 4096 / RB < 32 ? 4096 / RB : 32;
+  // tokens of a step: at most 8 KB of keys and values, at most 32
+  static constexpr int ST = FMT == THINK_PAGE_E4M3 ? THINK_ST_E4M3 : FMT == THINK_PAGE_INT4 ? THINK_ST_INT4 : 4096 / RB < 32 ? 4096 / RB : 32;
   static constexpr int HALF = ST * RB;                       // key (or value) bytes of a stage
   static constexpr int STAGE = (2 * (HALF + ST * SB) + 127) / 128 * 128;
-  static constexpr int STAGES = 24960 / STAGE < 8 ? 24960 / STAGE : 8;
+  static constexpr int SPACE = 200 * 1024 / WARPS;           // shared memory of a warp
+  static constexpr int STAGES = SPACE / STAGE < 8 ? SPACE / STAGE : 8;
   static constexpr int RING = STAGES * STAGE;
+  static_assert(STAGES >= 2 && WARPS <= kMaxWarps && WARPS >= kMaxG, "ring");
   static_assert(RING >= (3 * kMaxG + kMaxG * D) * 4, "a warp's partial state reuses its ring");
 };
 
@@ -86,6 +110,17 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// d = a b + (c0, c0, c1, c1), e4m3
+__device__ __forceinline__ void mma_fp8(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, float c0, float c1) {
+  asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%11,%11};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1));
+}
+__device__ __forceinline__ void mma_fp8(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -103,18 +138,20 @@ __device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t two) {          // 
   const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
   return (uint32_t)h.x | ((uint32_t)h.y << 16);
 }
-// the codes at bits 0..3 and 16..19 of w, minus 8, as f16
-__device__ __forceinline__ uint32_t int4x2_to_f16x2(uint32_t w) {
-  const uint32_t t = (w & 0x000f000fu) | 0x64006400u, eight = 0x64086408u;    // 1024 + code, 1024 + 8
-  const __half2 r = __hsub2(*(const __half2*)&t, *(const __half2*)&eight);
-  return *(const uint32_t*)&r;
+// four floats to e4m3 bytes
+__device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
+  const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+  const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
+  return lo | (hi << 16);
 }
-// the same at bits 4..7 and 20..23: 1024 + 16 code = 16 (64 + code)
-__device__ __forceinline__ uint32_t int4x2_hi_to_f16x2(uint32_t w) {
-  const uint32_t t = (w & 0x00f000f0u) | 0x64006400u, k = 0x2c002c00u, o = 0xd480d480u;    // 1/16, -72
-  const __half2 r = __hfma2(*(const __half2*)&t, *(const __half2*)&k, *(const __half2*)&o);
-  return *(const uint32_t*)&r;
+__device__ __forceinline__ float2 e4m3x2_to_float2(uint32_t two) {
+  const uint32_t h = e4m3x2_to_f16x2(two & 0xffffu);
+  return __half22float2(*(const __half2*)&h);
 }
+// codes c at bits 4..7 and 20..23 as the f16 numbers 64 + c
+__device__ __forceinline__ uint32_t plus64(uint32_t w) { return (w & 0x00f000f0u) | 0x54005400u; }
+// small integers to float without the conversion unit: 2^23 + n
+__device__ __forceinline__ float magic(uint32_t n) { return __uint_as_float(0x4b000000u | n); }
 // 2^k for -126 <= k <= 127
 __device__ __forceinline__ float pow2i(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }
 
@@ -173,15 +210,14 @@ struct WarpInfo {
 };
 
 // Joins n partial states of one unit (rec(i), in token order).  Returns with the block's threads holding elements
-// i = tid + kThreads * k of the joined accumulators in acc[k]; `stat` (shared) gets m, M and l per query head.
+// i = tid + THREADS * k of the joined accumulators in acc[k]; `stat` (shared) gets m, M and l per query head.
 // GLOBAL: the states were written by other CTAs (read from L2); otherwise by this one, in either memory.
 template <bool GLOBAL>
 __device__ __forceinline__ float rec_load(const float* p) { return GLOBAL ? __ldcg(p) : *p; }
-template <int D, bool GLOBAL, typename RecOf>
+template <int D, int THREADS, bool GLOBAL, typename RecOf>
 __device__ __forceinline__ void join(int n, int G, RecOf rec, float* weight /* shared [8][n] */, float (*stat)[kMaxG],
-                                     float (&acc)[kMaxG * D / kThreads]) {
+                                     float (&acc)[(kMaxG * D + THREADS - 1) / THREADS]) {
   const int tid = threadIdx.x, lane = tid & 31, g = tid >> 5;
-  static_assert(kWarps >= kMaxG, "one warp per query head");
   if (g < G) {
     float m = -INFINITY, M = -INFINITY, l = 0.f;
     for (int i = lane; i < n; i += 32) {
@@ -208,8 +244,8 @@ __device__ __forceinline__ void join(int n, int G, RecOf rec, float* weight /* s
   }
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < kMaxG * D / kThreads; ++k) {
-    const int e = tid + kThreads * k, ge = e / D;
+  for (int k = 0; k < (kMaxG * D + THREADS - 1) / THREADS; ++k) {
+    const int e = tid + THREADS * k, ge = e / D;
     acc[k] = 0.f;
     if (ge < G) {
 #pragma unroll 8
@@ -219,23 +255,27 @@ __device__ __forceinline__ void join(int n, int G, RecOf rec, float* weight /* s
 }
 
 // ---------------------------------------------------------------------------------------------------------
-// Tensor-core formats: fragments of a warp.  Lane (row = lane / 4, qd = lane % 4): query head `row`, tokens
-// 8 n + 2 qd, + 1 of the n-th group of 8 tokens.
+// Tensor-core formats: fragments of a warp.  Lane (r = lane / 4, qd = lane % 4).  Logits: query r, tokens 8 n + 2 qd,
+// + 1 of the n-th group of 8 tokens.  Accumulators o: channels by r (and by tile), queries 2 qd, 2 qd + 1.
+template <int FMT>
+__device__ __forceinline__ float finish(float m, float M, float l);
+
 template <int D, int FMT>
 struct MmaState {
   using S = Shape<D, 2, FMT>;
   static constexpr bool PLAIN = FMT == THINK_PAGE_PLAIN;
   static constexpr bool INT4 = FMT == THINK_PAGE_INT4;
   static constexpr int NT = S::ST / 8;          // groups of 8 tokens of a step
-  static constexpr int KS = D / 16;
-  static constexpr int NG = D / kGroupChannels;
-  static constexpr int OT = D / 8;
-  static constexpr int WIDTH = PLAIN ? 2 : FMT == THINK_PAGE_E4M3 ? 4 : 8;   // consecutive output channels of a lane
+  static constexpr int NG = D / 32;             // k32 blocks of a row; scale groups of 4-bit rows
+  static constexpr int OT = D / 16;
+  static constexpr int WIDTH = PLAIN ? 1 : INT4 ? 4 : 2;     // consecutive channels that a lane holds
 
-  uint32_t q[KS][2];
+  uint32_t q[NG][4];         // A fragments.  bf16: k16 block s has q[s / 2][2 (s % 2)], [.. + 1] as rows 0..7
+  float corr[INT4 ? NG : 1][2];                 // 4-bit: -8 * 2^-9 * sum of the block's query parts (high, low)
   float rs;                  // base-2 logit per unit of the q k product
-  float m, M, l;
+  float m, M, l;             // of query r; l: this lane's tokens only
   float o[OT][4];
+  float bias[INT4 ? NG : 1][4];                 // 4-bit: 72 * sum of the weights
 
   // the unit's queries as A fragments; qg: its first query row
   __device__ __forceinline__ void begin(const void* qg_, int G, float scale_log2, int lane) {
@@ -244,50 +284,66 @@ struct MmaState {
     const bool on = (lane >> 2) < G;
     if constexpr (PLAIN) {
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        q[s][0] = on ? *(const uint32_t*)(qr + 16 * s + 2 * qd) : 0u;
-        q[s][1] = on ? *(const uint32_t*)(qr + 16 * s + 2 * qd + 8) : 0u;
-      }
+      for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[g][i] = on ? *(const uint32_t*)(qr + 32 * g + 8 * i + 2 * qd) : 0u;
       rs = scale_log2;
     } else {
-      uint32_t w[D / 8];                        // the lane's channels as bf16 pairs, 4 (e4m3) or 8 (int4) in a row
-      if constexpr (INT4) {
+      uint32_t w[NG][4];                        // the lane's channels as bf16 pairs
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
+      for (int g = 0; g < NG; ++g) {
+        if constexpr (INT4) {                   // 32 g + 8 qd .. + 7
           const uint4 x = on ? *(const uint4*)(qr + 32 * g + 8 * qd) : make_uint4(0u, 0u, 0u, 0u);
-          w[4 * g] = x.x; w[4 * g + 1] = x.y; w[4 * g + 2] = x.z; w[4 * g + 3] = x.w;
-        }
-      } else {
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-          const uint2 x = on ? *(const uint2*)(qr + 16 * s + 4 * qd) : make_uint2(0u, 0u);
-          w[2 * s] = x.x; w[2 * s + 1] = x.y;
+          w[g][0] = x.x; w[g][1] = x.y; w[g][2] = x.z; w[g][3] = x.w;
+        } else {                                // 32 g + 4 qd .. + 3 and 16 behind
+          const uint2 x = on ? *(const uint2*)(qr + 32 * g + 4 * qd) : make_uint2(0u, 0u);
+          const uint2 y = on ? *(const uint2*)(qr + 32 * g + 16 + 4 * qd) : make_uint2(0u, 0u);
+          w[g][0] = x.x; w[g][1] = x.y; w[g][2] = y.x; w[g][3] = y.y;
         }
       }
       uint32_t t = 0;
 #pragma unroll
-      for (int i = 0; i < D / 8; ++i) t = __vmaxu2(t, w[i] & 0x7fff7fffu);
+      for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) t = __vmaxu2(t, w[g][i] & 0x7fff7fffu);
       t = max(t & 0xffffu, t >> 16);
       t = max(t, __shfl_xor_sync(0xffffffffu, t, 1));
       t = max(t, __shfl_xor_sync(0xffffffffu, t, 2));
-      // the row's largest channel goes to [2^14, 2^15)
-      const int k = min(141 - (int)(t >> 7), 100);
+      // the row's largest channel goes to [2^7, 2^8)
+      const int k = min(134 - (int)(t >> 7), 100);
       const float up = pow2i(k);
       rs = scale_log2 * pow2i(-k);
-      if constexpr (INT4) {                     // the codes of a word pair up as channels (0,4) (1,5) (2,6) (3,7)
+      if (INT4) rs *= 512.f;                    // a code is c * 2^-9
 #pragma unroll
-        for (int g = 0; g < NG; ++g)
+      for (int g = 0; g < NG; ++g) {
+        float x[8], part[2] = {0.f, 0.f};       // the channels of the first and of the second half of the k32 block
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const uint32_t a = w[4 * g + j], b = w[4 * g + 2 + j];
-            q[2 * g + j][0] = pack_f16(bf16lo(a) * up, bf16lo(b) * up);
-            q[2 * g + j][1] = pack_f16(bf16hi(a) * up, bf16hi(b) * up);
+        for (int i = 0; i < 4; ++i) {
+          const float lo = bf16lo(w[g][i]) * up, hi = bf16hi(w[g][i]) * up;
+          x[INT4 ? i : 2 * i] = lo;             // 4-bit: the even codes of a word are its first operand, the odd its second
+          x[INT4 ? 4 + i : 2 * i + 1] = hi;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float* y = x + 4 * h;
+          const uint32_t a = e4m3x4(y[0], y[1], y[2], y[3]);
+          const float2 u = e4m3x2_to_float2(a), v = e4m3x2_to_float2(a >> 16);
+          const uint32_t b = e4m3x4((y[0] - u.x) * 16.f, (y[1] - u.y) * 16.f, (y[2] - v.x) * 16.f, (y[3] - v.y) * 16.f);
+          q[g][2 * h] = a;
+          q[g][2 * h + 1] = b;
+          if constexpr (INT4) {
+            const float2 c = e4m3x2_to_float2(b), d = e4m3x2_to_float2(b >> 16);
+            part[0] += (u.x + u.y) + (v.x + v.y);
+            part[1] += (c.x + c.y) + (d.x + d.y);
           }
-      } else {
+        }
+        if constexpr (INT4) {
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {
-          q[s][0] = pack_f16(bf16lo(w[2 * s]) * up, bf16hi(w[2 * s]) * up);
-          q[s][1] = pack_f16(bf16lo(w[2 * s + 1]) * up, bf16hi(w[2 * s + 1]) * up);
+          for (int h = 0; h < 2; ++h) {
+            part[h] += __shfl_xor_sync(0xffffffffu, part[h], 1);
+            part[h] += __shfl_xor_sync(0xffffffffu, part[h], 2);
+            corr[g][h] = part[h] * (-8.f / 512.f);
+          }
         }
       }
     }
@@ -295,11 +351,29 @@ struct MmaState {
     l = 0.f;
 #pragma unroll
     for (int t = 0; t < OT; ++t) o[t][0] = o[t][1] = o[t][2] = o[t][3] = 0.f;
+    if constexpr (INT4)
+#pragma unroll
+      for (int g = 0; g < NG; ++g) bias[g][0] = bias[g][1] = bias[g][2] = bias[g][3] = 0.f;
+  }
+
+  // bf16 scales of tokens 8n + 2qd (first NG / 2 words) and 8n + 2qd + 1
+  static __device__ __forceinline__ void load_scales(uint32_t base, int n, int qd, uint32_t (&sc)[NG]) {
+    const uint32_t a = base + (8 * n + 2 * qd) * S::SB;
+    if constexpr (NG == 4)
+      asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(sc[0]), "=r"(sc[1]), "=r"(sc[2]), "=r"(sc[3]) : "r"(a));
+    else
+      asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(sc[0]), "=r"(sc[1]) : "r"(a));
+  }
+  // scale of group g of the i-th of the two tokens
+  static __device__ __forceinline__ float scale_of(const uint32_t (&sc)[NG], int i, int g) {
+    const uint32_t w = sc[i * (NG / 2) + (g >> 1)];
+    return (g & 1) ? bf16hi(w) : bf16lo(w);
   }
 
   // one step: keys at sb, values at sb + HALF, scales behind; ntok of its tokens count
   __device__ __forceinline__ void step(uint32_t sb, int ntok, int lane) {
     const int qd = lane & 3, mi = lane >> 3, tr = lane & 7;
+    const uint32_t ks = sb + 2 * S::HALF, vs = ks + S::ST * S::SB;
     float x[NT][2];
     // ---- logits
     if constexpr (PLAIN) {
@@ -308,11 +382,11 @@ struct MmaState {
       for (int n = 0; n < NT; n += 2) {
         float c[4][4] = {};                     // even and odd channel groups in chains of their own
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {
+        for (int s = 0; s < D / 16; ++s) {
           uint32_t k[4];
           ldsm4(sb + n * 8 * S::RB + (off ^ (s << 5)), k);
-          mma<true>(c[s & 1], q[s][0], 0u, q[s][1], 0u, k[0], k[1]);
-          mma<true>(c[2 + (s & 1)], q[s][0], 0u, q[s][1], 0u, k[2], k[3]);
+          mma<true>(c[s & 1], q[s >> 1][2 * (s & 1)], 0u, q[s >> 1][2 * (s & 1) + 1], 0u, k[0], k[1]);
+          mma<true>(c[2 + (s & 1)], q[s >> 1][2 * (s & 1)], 0u, q[s >> 1][2 * (s & 1) + 1], 0u, k[2], k[3]);
         }
         x[n][0] = (c[0][0] + c[1][0]) * rs; x[n][1] = (c[0][1] + c[1][1]) * rs;
         x[n + 1][0] = (c[2][0] + c[3][0]) * rs; x[n + 1][1] = (c[2][1] + c[3][1]) * rs;
@@ -321,19 +395,18 @@ struct MmaState {
       const int off = S::RB == 128 ? tr * 128 + ((mi ^ tr) << 4) : tr * 64 + ((mi ^ (tr >> 1)) << 4);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        float c[2][4] = {};
+        float c[4] = {};
 #pragma unroll
-        for (int i = 0; i < KS / 4; ++i) {
+        for (int i = 0; i < NG / 2; ++i) {
           uint32_t k[4];
           ldsm4(sb + n * 8 * S::RB + (off ^ (i << 6)), k);
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            mma<false>(c[j & 1], q[4 * i + j][0], 0u, q[4 * i + j][1], 0u, e4m3x2_to_f16x2(k[j] & 0xffffu), e4m3x2_to_f16x2(k[j] >> 16));
+          mma_fp8(c, q[2 * i], k[0], k[1]);
+          mma_fp8(c, q[2 * i + 1], k[2], k[3]);
         }
         uint32_t sc;
-        asm volatile("ld.shared.u16 %0, [%1];" : "=r"(sc) : "r"(sb + 2 * S::HALF + 8 * n + 2 * qd));
-        x[n][0] = (c[0][0] + c[1][0]) * rs * __uint_as_float((sc & 0xffu) << 23);
-        x[n][1] = (c[0][1] + c[1][1]) * rs * __uint_as_float((sc >> 8) << 23);
+        asm volatile("ld.shared.u16 %0, [%1];" : "=r"(sc) : "r"(ks + 8 * n + 2 * qd));
+        x[n][0] = fmaf(c[2], 0.0625f, c[0]) * (rs * __uint_as_float((sc & 0xffu) << 23));
+        x[n][1] = fmaf(c[3], 0.0625f, c[1]) * (rs * __uint_as_float((sc >> 8) << 23));
       }
     } else {
       const int off = S::RB == 64 ? tr * 64 + ((mi ^ (tr >> 1)) << 4) : (tr + 8 * (mi >> 1)) * 32 + (((mi & 1) ^ (tr >> 2)) << 4);
@@ -345,17 +418,16 @@ struct MmaState {
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
           const int n = n0 + p;
-          uint32_t sc[2 * NG / 2];              // scales of the lane's two tokens, bf16 pairs
-          load_scales(sb + 2 * S::HALF, n, qd, sc);
+          uint32_t sc[NG];
+          load_scales(ks, n, qd, sc);
           float y0 = 0.f, y1 = 0.f;
 #pragma unroll
           for (int g = 0; g < NG; ++g) {
-            const uint32_t w = k[p * NG + g], w8 = w >> 8;
-            float c[4] = {};
-            mma<false>(c, q[2 * g][0], 0u, q[2 * g][1], 0u, int4x2_to_f16x2(w), int4x2_hi_to_f16x2(w));
-            mma<false>(c, q[2 * g + 1][0], 0u, q[2 * g + 1][1], 0u, int4x2_to_f16x2(w8), int4x2_hi_to_f16x2(w8));
-            y0 = fmaf(c[0], (g & 1) ? bf16hi(sc[g >> 1]) : bf16lo(sc[g >> 1]), y0);
-            y1 = fmaf(c[1], (g & 1) ? bf16hi(sc[NG / 2 + (g >> 1)]) : bf16lo(sc[NG / 2 + (g >> 1)]), y1);
+            const uint32_t w = k[p * NG + g];
+            float c[4];
+            mma_fp8(c, q[g], w & 0x0f0f0f0fu, (w >> 4) & 0x0f0f0f0fu, corr[g][0], corr[g][1]);
+            y0 = fmaf(fmaf(c[2], 0.0625f, c[0]), scale_of(sc, 0, g), y0);
+            y1 = fmaf(fmaf(c[3], 0.0625f, c[1]), scale_of(sc, 1, g), y1);
           }
           x[n][0] = y0 * rs;
           x[n][1] = y1 * rs;
@@ -369,32 +441,29 @@ struct MmaState {
         if (8 * n + 2 * qd + 1 >= ntok) x[n][1] = -INFINITY;
       }
     }
-    // ---- exponents of the values' scales, running maxima
-    int es[NT][2];
-    float mx = -INFINITY, Mx = -INFINITY;
+    // ---- running maxima of the logits and of logit + log2 of the value's scale.  The latter only has to keep weights
+    // within f16: for 4-bit rows it is the largest scale's bits read as a piecewise linear logarithm (low by < 0.09)
+    float es[NT][2], mx = -INFINITY, Mx = -INFINITY;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      if constexpr (PLAIN) {
-        mx = fmaxf(mx, fmaxf(x[n][0], x[n][1]));
-      } else {
-        if constexpr (INT4) {
-          uint32_t sc[NG];
-          load_scales(sb + 2 * S::HALF + S::ST * S::SB, n, qd, sc);
+      mx = fmaxf(mx, fmaxf(x[n][0], x[n][1]));
+      if constexpr (INT4) {
+        uint32_t sc[NG];
+        load_scales(vs, n, qd, sc);
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            uint32_t t = NG == 4 ? __vmaxu2(sc[2 * i], sc[2 * i + 1]) : sc[i];
-            t = max(t & 0xffffu, t >> 16) >> 7;
-            es[n][i] = t == 255u ? 0 : min(max((int)t - 126, -100), 126);      // every scale of the row is below 2^es
-          }
-        } else {
-          uint32_t sc;
-          asm volatile("ld.shared.u16 %0, [%1];" : "=r"(sc) : "r"(sb + 2 * S::HALF + S::ST + 8 * n + 2 * qd));
-          es[n][0] = (int)(sc & 0xffu) - 127;
-          es[n][1] = (int)(sc >> 8) - 127;
+        for (int i = 0; i < 2; ++i) {
+          uint32_t t = sc[i * (NG / 2)];
+          if (NG == 4) t = __vmaxu2(t, sc[i * (NG / 2) + NG / 2 - 1]);
+          t = max(max(t & 0xffffu, t >> 16), 27u << 7);      // 2^-100 at least: the weight's other factor stays finite
+          es[n][i] = fmaf(magic(t) - 8388608.f, 0.0078125f, x[n][i] - 127.f);
         }
-        mx = fmaxf(mx, fmaxf(x[n][0], x[n][1]));
-        Mx = fmaxf(Mx, fmaxf(x[n][0] + es[n][0], x[n][1] + es[n][1]));
+      } else if constexpr (!PLAIN) {
+        uint32_t sc;
+        asm volatile("ld.shared.u16 %0, [%1];" : "=r"(sc) : "r"(vs + 8 * n + 2 * qd));
+        es[n][0] = x[n][0] + (magic(sc & 0xffu) - 8388735.f);
+        es[n][1] = x[n][1] + (magic(sc >> 8) - 8388735.f);
       }
+      if constexpr (!PLAIN) Mx = fmaxf(Mx, fmaxf(es[n][0], es[n][1]));
     }
     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
@@ -409,144 +478,134 @@ struct MmaState {
       const float sc = M == -INFINITY ? 0.f : ex2(M - Mn);
       m = mn;
       M = Mn;
+      const float s0 = __shfl_sync(0xffffffffu, sc, 8 * qd), s1 = __shfl_sync(0xffffffffu, sc, 8 * qd + 4);
 #pragma unroll
       for (int t = 0; t < OT; ++t) {
-        o[t][0] *= sc; o[t][1] *= sc;
-        if (PLAIN) { o[t][2] *= sc; o[t][3] *= sc; }
+        o[t][0] *= s0; o[t][1] *= s1; o[t][2] *= s0; o[t][3] *= s1;
       }
+      if constexpr (INT4)
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          bias[g][0] *= s0; bias[g][1] *= s1; bias[g][2] *= s0; bias[g][3] *= s1;
+        }
     }
-    const float mr = m == -INFINITY ? 0.f : m;
-    // ---- weights and p V, 16 tokens at a time
+    const float mr = m == -INFINITY ? 0.f : m, Mr = M == -INFINITY ? 0.f : M - 15.f;
+    // ---- weights and V p, 16 tokens at a time
 #pragma unroll
     for (int kk = 0; kk < NT / 2; ++kk) {
       const uint32_t vb = sb + S::HALF + kk * 16 * S::RB;
+      const int r = ((mi & 1) << 3) + tr;
       float w[2][2];
-      const float Mr = M == -INFINITY ? 0.f : M - 15.f;
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const float p = ex2(x[2 * kk + j][i] - mr);
           l += p;
-          w[j][i] = PLAIN ? p : ex2(x[2 * kk + j][i] + es[2 * kk + j][i] - Mr);
+          w[j][i] = PLAIN ? p : ex2((INT4 ? x[2 * kk + j][i] : es[2 * kk + j][i]) - Mr);
         }
       if constexpr (PLAIN) {
-        const uint32_t h0 = pack_bf16(w[0][0], w[0][1]), h2 = pack_bf16(w[1][0], w[1][1]);
+        const uint32_t h0 = pack_bf16(w[0][0], w[0][1]), h1 = pack_bf16(w[1][0], w[1][1]);
         const uint32_t l0 = pack_bf16(w[0][0] - bf16lo(h0), w[0][1] - bf16hi(h0));
-        const uint32_t l2 = pack_bf16(w[1][0] - bf16lo(h2), w[1][1] - bf16hi(h2));
-        const int off = (((mi & 1) << 3) + tr) * S::RB + (((mi >> 1) ^ tr) << 4);
+        const uint32_t l1 = pack_bf16(w[1][0] - bf16lo(h1), w[1][1] - bf16hi(h1));
+        const int off = r * S::RB + (((mi >> 1) ^ tr) << 4);
 #pragma unroll
-        for (int t = 0; t < OT / 2; ++t) {
+        for (int t = 0; t < OT; ++t) {
           uint32_t v[4];
           ldsm4t(vb + (off ^ (t << 5)), v);
-          mma<true>(o[2 * t], h0, l0, h2, l2, v[0], v[1]);
-          mma<true>(o[2 * t + 1], h0, l0, h2, l2, v[2], v[3]);
+          mma<true>(o[t], v[0], v[2], v[1], v[3], h0, h1);
+          mma<true>(o[t], v[0], v[2], v[1], v[3], l0, l1);
         }
       } else if constexpr (!INT4) {
-        const uint32_t a0 = pack_f16(w[0][0], w[0][1]), a2 = pack_f16(w[1][0], w[1][1]);
-        const int r = ((mi & 1) << 3) + tr;
+        const uint32_t b0 = pack_f16(w[0][0], w[0][1]), b1 = pack_f16(w[1][0], w[1][1]);
         const int off = S::RB == 128 ? r * 128 + (((mi >> 1) ^ tr) << 4) : r * 64 + (((mi >> 1) ^ (tr >> 1)) << 4);
 #pragma unroll
-        for (int i = 0; i < KS / 2; ++i) {
+        for (int i = 0; i < OT / 2; ++i) {
           uint32_t v[4];
           ldsm4t(vb + (off ^ (i << 5)), v);
-          // bytes (channel 2r, 2r + 1 of token 2qd | the same of token 2qd + 1) to (even channel's tokens | odd's)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) v[j] = __byte_perm(v[j], 0u, 0x3120);
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            mma<false>(o[4 * i + 2 * j], a0, 0u, a2, 0u, e4m3x2_to_f16x2(v[2 * j] & 0xffffu), e4m3x2_to_f16x2(v[2 * j + 1] & 0xffffu));
-            mma<false>(o[4 * i + 2 * j + 1], a0, 0u, a2, 0u, e4m3x2_to_f16x2(v[2 * j] >> 16), e4m3x2_to_f16x2(v[2 * j + 1] >> 16));
+          for (int j = 0; j < 2; ++j) {         // a word: channels 2r, 2r + 1 of token 2qd, the same of token 2qd + 1
+            const uint32_t a = v[2 * j], b = v[2 * j + 1];
+            mma<false>(o[2 * i + j], e4m3x2_to_f16x2(__byte_perm(a, 0u, 0x4420)), e4m3x2_to_f16x2(__byte_perm(a, 0u, 0x4431)),
+                       e4m3x2_to_f16x2(__byte_perm(b, 0u, 0x4420)), e4m3x2_to_f16x2(__byte_perm(b, 0u, 0x4431)), b0, b1);
           }
         }
       } else {
         uint32_t s0[NG], s1[NG];
-        load_scales(sb + 2 * S::HALF + S::ST * S::SB, 2 * kk, qd, s0);
-        load_scales(sb + 2 * S::HALF + S::ST * S::SB, 2 * kk + 1, qd, s1);
-        float f[2][2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int i = 0; i < 2; ++i) f[j][i] = w[j][i] * pow2i(-es[2 * kk + j][i]);
-        // a masked token's weight is 0 whatever its scale (zero-filled) says
-        const int r = ((mi & 1) << 3) + tr;
+        load_scales(vs, 2 * kk, qd, s0);
+        load_scales(vs, 2 * kk + 1, qd, s1);
         const int off = S::RB == 64 ? r * 64 + (((mi >> 1) ^ (tr >> 1)) << 4) : r * 32 + (((mi >> 1) ^ (tr >> 2)) << 4);
 #pragma unroll
         for (int g2 = 0; g2 < NG / 2; ++g2) {
           uint32_t v[4];
           ldsm4t(vb + (off ^ (g2 << 5)), v);
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
+          for (int j = 0; j < 2; ++j) {         // a word: channels 4r .. 4r + 3 of token 2qd, the same of token 2qd + 1
             const int g = 2 * g2 + j;
-            const uint32_t a0 = pack_f16(f[0][0] * (j ? bf16hi(s0[g2]) : bf16lo(s0[g2])), f[0][1] * (j ? bf16hi(s0[NG / 2 + g2]) : bf16lo(s0[NG / 2 + g2])));
-            const uint32_t a2 = pack_f16(f[1][0] * (j ? bf16hi(s1[g2]) : bf16lo(s1[g2])), f[1][1] * (j ? bf16hi(s1[NG / 2 + g2]) : bf16lo(s1[NG / 2 + g2])));
-            const uint32_t b0 = v[2 * j], b1 = v[2 * j + 1];
-            mma<false>(o[4 * g], a0, 0u, a2, 0u, int4x2_to_f16x2(b0), int4x2_to_f16x2(b1));
-            mma<false>(o[4 * g + 1], a0, 0u, a2, 0u, int4x2_hi_to_f16x2(b0), int4x2_hi_to_f16x2(b1));
-            mma<false>(o[4 * g + 2], a0, 0u, a2, 0u, int4x2_to_f16x2(b0 >> 8), int4x2_to_f16x2(b1 >> 8));
-            mma<false>(o[4 * g + 3], a0, 0u, a2, 0u, int4x2_hi_to_f16x2(b0 >> 8), int4x2_hi_to_f16x2(b1 >> 8));
+            const uint32_t b0 = pack_f16(w[0][0] * scale_of(s0, 0, g), w[0][1] * scale_of(s0, 1, g));
+            const uint32_t b1 = pack_f16(w[1][0] * scale_of(s1, 0, g), w[1][1] * scale_of(s1, 1, g));
+            const uint32_t a = v[2 * j], b = v[2 * j + 1];
+            mma<false>(o[2 * g], plus64(a << 4), plus64(a), plus64(b << 4), plus64(b), b0, b1);
+            mma<false>(o[2 * g + 1], plus64(a >> 4), plus64(a >> 8), plus64(b >> 4), plus64(b >> 8), b0, b1);
+            mma<false>(bias[g], 0x54805480u, 0x54805480u, 0x54805480u, 0x54805480u, b0, b1);
           }
         }
       }
     }
   }
 
-  // bf16 scales of tokens 8n + 2qd (first NG / 2 words) and 8n + 2qd + 1
-  static __device__ __forceinline__ void load_scales(uint32_t base, int n, int qd, uint32_t (&sc)[NG]) {
-    const uint32_t a = base + (8 * n + 2 * qd) * S::SB;
-    if constexpr (NG == 4)
-      asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(sc[0]), "=r"(sc[1]), "=r"(sc[2]), "=r"(sc[3]) : "r"(a));
-    else
-      asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(sc[0]), "=r"(sc[1]) : "r"(a));
-  }
-
-  // the lane's output channels: f(first channel, values[WIDTH])
+  // the lane's accumulators: f(first channel, values[WIDTH] of query 2qd, of query 2qd + 1)
   template <typename F>
   __device__ __forceinline__ void each(int lane, F f) const {
-    const int qd = lane & 3;
+    const int r = lane >> 2;
 #pragma unroll
-    for (int i = 0; i < D / (4 * WIDTH); ++i) {
-      float v[WIDTH];
+    for (int i = 0; i < D / (8 * WIDTH); ++i) {
+      float a[WIDTH], b[WIDTH];
       if constexpr (PLAIN) {
-        v[0] = o[i][0] + o[i][2];
-        v[1] = o[i][1] + o[i][3];
+        a[0] = o[i >> 1][2 * (i & 1)];
+        b[0] = o[i >> 1][2 * (i & 1) + 1];
       } else if constexpr (!INT4) {
-        v[0] = o[2 * i][0]; v[1] = o[2 * i + 1][0]; v[2] = o[2 * i][1]; v[3] = o[2 * i + 1][1];
+        a[0] = o[i][0]; a[1] = o[i][2];
+        b[0] = o[i][1]; b[1] = o[i][3];
       } else {
 #pragma unroll
-        for (int a = 0; a < 4; ++a) {
-          v[a] = o[4 * i + a][0];
-          v[4 + a] = o[4 * i + a][1];
+        for (int h = 0; h < 2; ++h) {
+          a[2 * h] = o[2 * i + h][0] - bias[i][0];
+          a[2 * h + 1] = o[2 * i + h][2] - bias[i][0];
+          b[2 * h] = o[2 * i + h][1] - bias[i][1];
+          b[2 * h + 1] = o[2 * i + h][3] - bias[i][1];
         }
       }
-      f(4 * WIDTH * i + WIDTH * qd, v);
+      f(8 * WIDTH * i + WIDTH * r, a, b);
     }
   }
   __device__ __forceinline__ void end() {
     l += __shfl_xor_sync(0xffffffffu, l, 1);
     l += __shfl_xor_sync(0xffffffffu, l, 2);
   }
-  __device__ __forceinline__ void store_record(Record<D>* r, int G, int lane) const {
-    const int row = lane >> 2;
-    if (row >= G) return;
-    if ((lane & 3) == 0) {
-      r->m[row] = m;
-      r->M[row] = M;
-      r->l[row] = l;
+  __device__ __forceinline__ void store_record(Record<D>* rec, int G, int lane) const {
+    const int r = lane >> 2, q0 = 2 * (lane & 3);
+    if ((lane & 3) == 0 && r < G) {
+      rec->m[r] = m;
+      rec->M[r] = M;
+      rec->l[r] = l;
     }
-    each(lane, [&](int c, const float (&v)[WIDTH]) {
+    each(lane, [&](int c, const float (&a)[WIDTH], const float (&b)[WIDTH]) {
 #pragma unroll
-      for (int i = 0; i < WIDTH; i += 2) *(float2*)&r->o[row][c + i] = make_float2(v[i], v[i + 1]);
+      for (int i = 0; i < WIDTH; ++i) {
+        if (q0 < G) rec->o[q0][c + i] = a[i];
+        if (q0 + 1 < G) rec->o[q0 + 1][c + i] = b[i];
+      }
     });
   }
   __device__ __forceinline__ void store_out(void* out, float* lse, int G, int lane) const;
 };
 
-// factor that turns joined accumulators into outputs, and the log of the softmax sum
-template <bool PLAIN>
+// factor that turns joined accumulators into outputs
+template <int FMT>
 __device__ __forceinline__ float finish(float m, float M, float l) {
   if (m == -INFINITY) return 0.f;
-  if (PLAIN) return 1.f / l;
+  if (FMT == THINK_PAGE_PLAIN) return 1.f / l;
   const float h = exp2f(0.5f * (M - 15.f - m));              // in two factors: the exponent may pass 127
   return h / l * h;
 }
@@ -556,19 +615,26 @@ __device__ __forceinline__ float log_sum(float m, float l) {
 
 template <int D, int FMT>
 __device__ __forceinline__ void MmaState<D, FMT>::store_out(void* out, float* lse, int G, int lane) const {
-  const int row = lane >> 2;
-  if (row >= G) return;
-  const float f = finish<PLAIN>(m, M, l);
-  __nv_bfloat16* po = (__nv_bfloat16*)out + row * D;
-  each(lane, [&](int c, const float (&v)[WIDTH]) {
-    uint32_t w[WIDTH / 2];
+  const int r = lane >> 2, qd = lane & 3, q0 = 2 * qd;
+  const float fr = finish<FMT>(m, M, l);
+  const float f0 = __shfl_sync(0xffffffffu, fr, 8 * qd), f1 = __shfl_sync(0xffffffffu, fr, 8 * qd + 4);
+  __nv_bfloat16* const po = (__nv_bfloat16*)out + q0 * D;
+  auto put = [&](__nv_bfloat16* to, const float (&v)[WIDTH], float f) {
+    if constexpr (WIDTH == 1) {
+      *to = __float2bfloat16_rn(f == 0.f ? 0.f : v[0] * f);
+    } else {
+      uint32_t w[(WIDTH + 1) / 2];
 #pragma unroll
-    for (int i = 0; i < WIDTH / 2; ++i) w[i] = f == 0.f ? 0u : pack_bf16(v[2 * i] * f, v[2 * i + 1] * f);
-    if constexpr (WIDTH == 2) *(uint32_t*)(po + c) = w[0];
-    else if constexpr (WIDTH == 4) *(uint2*)(po + c) = make_uint2(w[0], w[1]);
-    else *(uint4*)(po + c) = make_uint4(w[0], w[1], w[2], w[3]);
+      for (int i = 0; i < WIDTH / 2; ++i) w[i] = f == 0.f ? 0u : pack_bf16(v[2 * i] * f, v[2 * i + 1] * f);
+      if constexpr (WIDTH == 2) *(uint32_t*)to = w[0];
+      else *(uint2*)to = make_uint2(w[0], w[1]);
+    }
+  };
+  each(lane, [&](int c, const float (&a)[WIDTH], const float (&b)[WIDTH]) {
+    if (q0 < G) put(po + c, a, f0);
+    if (q0 + 1 < G) put(po + D + c, b, f1);
   });
-  if (lse && (lane & 3) == 0) lse[row] = log_sum(m, l);
+  if (lse && qd == 0 && r < G) lse[r] = log_sum(m, l);
 }
 
 // ---------------------------------------------------------------------------------------------------------
@@ -706,7 +772,7 @@ struct F32State {
       const int src = (g * ST / R) << (5 - LB);
       const float mg = __shfl_sync(0xffffffffu, m, src), lg = __shfl_sync(0xffffffffu, l, src);
       if (g < G) {
-        const float f = finish<true>(mg, mg, lg);
+        const float f = finish<THINK_PAGE_PLAIN>(mg, mg, lg);
 #pragma unroll
         for (int i = 0; i < N; ++i) ((float*)out)[g * D + lane * N + i] = f == 0.f ? 0.f : o[g][i] * f;
         if (lse && lane == 0) lse[g] = log_sum(mg, lg);
@@ -720,24 +786,26 @@ struct StateOf { using type = MmaState<D, FMT>; };
 template <int D, int GP>
 struct StateOf<D, 4, THINK_PAGE_PLAIN, GP> { using type = F32State<D, GP>; };
 
+constexpr int kSpBytes = 512;        // fp32: a warp's weights of a step, read 16 bytes at a time
+
 // shared memory behind the rings
 struct alignas(16) Shared {
-  alignas(16) float sp[kWarps][128];            // fp32: weights of a step, read 16 bytes at a time
-  WarpInfo info[kWarps];
-  float weight[kMaxG * kWarps];
+  WarpInfo info[kMaxWarps];
+  float weight[kMaxG * kMaxWarps];
   float stat[3][kMaxG];
-  int warp_sum[kWarps];
-  int valid[kWarps][8];      // tokens that count in the stage
+  int warp_sum[kMaxWarps];
+  int valid[kMaxWarps][8];   // tokens that count in the stage
   int arrived[2];
 };
 
 template <int D, int E, int FMT, int GP>
-__global__ void __launch_bounds__(kThreads, 1) k_paged_decode(const PagedDecodeParams p) {
+__global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode(const PagedDecodeParams p) {
   using S = Shape<D, E, FMT>;
+  constexpr int kWarps = S::WARPS, kThreads = S::THREADS, kElems = (kMaxG * D + kThreads - 1) / kThreads;
   using State = typename StateOf<D, E, FMT, GP>::type;
   constexpr int EO = E;                         // bytes of an output element
   extern __shared__ __align__(128) unsigned char smem[];
-  Shared& sh = *(Shared*)(smem + kWarps * S::RING);
+  Shared& sh = *(Shared*)(smem + kWarps * (S::RING + (E == 4 ? kSpBytes : 0)));
   int* const cum = (int*)(&sh + 1);
   uint8_t* const last = (uint8_t*)(cum + p.table.B + 1);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -808,7 +876,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_decode(const PagedDecodeP
   if (f0 < f1) {
     const uint32_t ring = smem_u32(smem) + warp * S::RING;
     State st;
-    if constexpr (E == 4) st.sp = sh.sp[warp];
+    if constexpr (E == 4) st.sp = (float*)(smem + kWarps * S::RING + warp * kSpBytes);
 
     // ---- producer: fills the ring tile after tile
     Cursor pc = locate(tab, B, LH, f0);
@@ -920,13 +988,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_decode(const PagedDecodeP
   __syncthreads();
 
   // ---- join what the warps of this CTA share; `leader`: the first warp of the CTA that worked on the unit
-  float acc[kMaxG * D / kThreads];
+  float acc[kElems];
   auto emit = [&](const int64_t row) {          // joined accumulators -> output
 #pragma unroll
-    for (int k = 0; k < kMaxG * D / kThreads; ++k) {
+    for (int k = 0; k < kElems; ++k) {
       const int e = tid + kThreads * k, g = e / D;
       if (g < p.G) {
-        const float fa = finish<FMT == THINK_PAGE_PLAIN>(sh.stat[0][g], sh.stat[1][g], sh.stat[2][g]);
+        const float fa = finish<FMT>(sh.stat[0][g], sh.stat[1][g], sh.stat[2][g]);
         const float x = fa == 0.f ? 0.f : acc[k] * fa;
         if (EO == 4) ((float*)p.out)[row * D + e] = x;
         else ((__nv_bfloat16*)p.out)[row * D + e] = __float2bfloat16_rn(x);
@@ -955,15 +1023,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_decode(const PagedDecodeP
     const int until = head ? lead : split_owner(F1 - F0, kWarps, end - 1 - F0);
     // contributors: warps lead .. until that have tiles
     int n = 0;
-    uint32_t who = 0;                                                // 4 bits a contributor
+    uint64_t who = 0;                                                // 4 bits a contributor
     for (int v = lead; v <= until; ++v)
-      if (sh.info[v].f0 < sh.info[v].f1) who |= (uint32_t)v << (4 * n++);
+      if (sh.info[v].f0 < sh.info[v].f1) who |= (uint64_t)v << (4 * n++);
     auto rec = [&](int i) -> const Record<D>* {
       const int v = (int)(who >> (4 * i)) & 15;
       return sh.info[v].last_unit == unit ? (const Record<D>*)(smem + v * S::RING) : records + 2 * grid + (cta * kWarps + v);
     };
     // states in shared or global memory written by this CTA: plain loads
-    join<D, false>(n, p.G, rec, sh.weight, sh.stat, acc);
+    join<D, kThreads, false>(n, p.G, rec, sh.weight, sh.stat, acc);
     if (us >= F0 && ue <= F1) {
       emit((int64_t)unit * p.G);
     } else {
@@ -972,7 +1040,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_decode(const PagedDecodeP
       shared_after |= slot == 1;
       Record<D>* const r = cta_rec + slot;
 #pragma unroll
-      for (int k = 0; k < kMaxG * D / kThreads; ++k) {
+      for (int k = 0; k < kElems; ++k) {
         const int e = tid + kThreads * k, g = e / D;
         if (g < p.G) {
           (&r->o[0][0])[e] = acc[k];
@@ -1017,20 +1085,22 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_decode(const PagedDecodeP
     for (int i = tid; i < n; i += kThreads) cta_of[i] = sparse ? split_owner(total, grid, us + i) : c0 + i;
     __syncthreads();
     auto rec = [&](int i) -> const Record<D>* { return records + 2 * cta_of[i] + (i == 0); };
-    join<D, true>(n, p.G, rec, (float*)smem + kSMs, sh.stat, acc);
+    join<D, kThreads, true>(n, p.G, rec, (float*)smem + kSMs, sh.stat, acc);
     emit((int64_t)unit * p.G);
     __syncthreads();
   }
 }
 
 template <int D, int E, int FMT>
-constexpr size_t smem_fixed() { return (size_t)kWarps * Shape<D, E, FMT>::RING + sizeof(Shared); }
+constexpr size_t smem_fixed() {
+  return (size_t)Shape<D, E, FMT>::WARPS * (Shape<D, E, FMT>::RING + (E == 4 ? kSpBytes : 0)) + sizeof(Shared);
+}
 inline size_t smem_tables(int B) { return ((size_t)(B + 1) * 4 + B + 15) / 16 * 16; }
 
 template <int D, int E, int FMT, int GP>
 cudaError_t launch_k(const PagedDecodeParams& p, cudaStream_t s) {
   const size_t smem = smem_fixed<D, E, FMT>() + smem_tables(p.table.B);
-  k_paged_decode<D, E, FMT, GP><<<p.grid, kThreads, smem, s>>>(p);
+  k_paged_decode<D, E, FMT, GP><<<p.grid, Shape<D, E, FMT>::THREADS, smem, s>>>(p);
   return cudaGetLastError();
 }
 template <int D, int E, int FMT, int GP>
@@ -1069,7 +1139,7 @@ cudaError_t paged_decode_setup(int dtype, int format, int D, int G) {
 }
 // two records a CTA for units shared between CTAs, one a warp for units shared between warps
 size_t paged_decode_record_bytes(int D, int ctas) {
-  return (size_t)ctas * (2 + kWarps) * (D == 128 ? sizeof(Record<128>) : sizeof(Record<64>));
+  return (size_t)ctas * (2 + kMaxWarps) * (D == 128 ? sizeof(Record<128>) : sizeof(Record<64>));
 }
 
 }  // namespace think

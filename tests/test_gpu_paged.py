@@ -105,7 +105,7 @@ class Paged:
                     hs = slice(h * self.G, (h + 1) * self.G)
                     k, v = self.stored(b, l, h, lens[b])
                     r = po.attention(q64[b, l, hs], k, v, self.scale)
-                    yield (b, l, hs, r[0], r[1]) + bounds(*r, lens[b], self.D, self.dtype)
+                    yield (b, l, hs, r[0], r[1]) + bounds(*r, lens[b], self.D, self.fmt, self.dtype)
 
     def check(self, q, out, lse=None, lens=None, units=None):
         o64 = out.double().cpu().numpy()
@@ -125,25 +125,39 @@ class Paged:
         return worst
 
 
-def bounds(out, lse, absv, mag, top, n, D, dtype):
-    """Error bounds of one head, first order in the roundings.
+def bounds(out, lse, sizes, n, D, fmt, dtype):
+    """Error bounds of one head, first order in the roundings; the sizes are oracle.attention's.
 
     With u = 2^-23 (one fp32 operation, also where the tensor core's adder truncates):
-      logit     a dot product of D terms whose magnitudes sum to `mag` (scaled): error <= (D + 4) u mag, the scale in
-                base 2 and the maximum's subtraction included.  A weight exp(x) then carries twice that (its own and
-                the denominator's) relative error, plus 2^-21 for exp2 and 2^-11 where weights are rounded to 16 bits.
+      logit     a dot product of D terms whose magnitudes sum to qk: error <= (D + 4) u qk, the scale in base 2 and the
+                maximum's subtraction included.  A weight exp(x) then carries twice that (its own and the
+                denominator's) relative error, plus 2^-21 for exp2 and 2^-11 where weights are rounded to 16 bits.
       sums      n terms added in fp32 in any order: n u, numerator and denominator.
-      floor     a 16-bit weight has a smallest step of 2^-24, with the largest weight * scale between 2^14 and 2^15:
+      16 bits   a 16-bit weight has a smallest step of 2^-24, with the largest weight * scale between 2^14 and 2^15:
                 each token is off by at most 2^-39 of that product, whose codes are at most 448 (7) of a scale of
-                which the row's largest value has at least 224 (7/2): 2^-38 of top = max w |v|.
-    Weighted with |v| these are relative to absv = sum w |v|.  The output is rounded once to its type: half a step,
+                which the row's largest value has at least 224 (7/2): 2^-38 of top.
+    Quantised pages add
+      query     two e4m3 parts, the second 16 times: the smallest step is 2^-9 / 16 with the row's largest channel in
+                [2^7, 2^8), so a channel is off by at most 2^-21 of the largest: 2^-21 q_max.
+      offsets   4-bit key codes enter as n + 8 <= 15, value codes as n + 72 <= 79, and the 8 or 72 is taken off
+                afterwards; a group's scale is 1/7 of its largest value, so the sums hold (15 + 8) / 7 < 4 and
+                (79 + 72) / 7 < 22 times the largest value where n itself may be 0.  An instruction rounds its sum of 32
+                or 16 terms once, 2 u of their magnitudes: (2 + D / 32) u 4 k_max and 2 u (n / 16 + 8) 22 rows, where
+                8 stands for the steps that end before 16 tokens and the joins of partial sums.
+    Weighted with |v| the weights' errors are relative to absv.  The output is rounded once to its type: half a step,
     finfo.eps / 2 relative."""
     u = 2.0 ** -23
-    delta = (D + 4) * u * np.asarray(mag)
+    delta = (D + 4) * u * sizes["qk"]
+    if fmt != "plain":
+        delta = delta + 2.0 ** -21 * sizes["q_max"]
+    if fmt == "int4":
+        delta = delta + (2 + D // 32) * u * 4 * sizes["k_max"]
     weights = 2 * delta + 2.0 ** -21 + (2.0 ** -11 if dtype == torch.bfloat16 else 0.0) + 2 * (n + 8) * u
-    tol = torch.finfo(dtype).eps / 2 * np.abs(out) + weights[:, None] * absv * (1 + 2.0 ** -7) + 1e-30
+    tol = torch.finfo(dtype).eps / 2 * np.abs(out) + weights[:, None] * sizes["absv"] * (1 + 2.0 ** -7) + 1e-30
     if dtype == torch.bfloat16:
-        tol = tol + n * 2.0 ** -38 * np.asarray(top)[:, None]
+        tol = tol + n * 2.0 ** -38 * sizes["top"][:, None]
+    if fmt == "int4":
+        tol = tol + 22 * 2 * (n / 16 + 8) * u * sizes["rows"][:, None]
     ltol = delta + (n + 8) * u + 2.0 ** -21 + 4 * u * np.abs(np.where(np.isfinite(lse), lse, 0.0))
     return tol, ltol
 
@@ -431,7 +445,7 @@ def test_attention_bad_pages_and_lengths(fmt, dtype):
             kk, vv = p.stored(b, 0, h, lens[b])
             r = po.attention(q64[b, 0, hs], kk[keep], vv[keep], p.scale)
             w, wl_ = r[:2]
-            tol, ltol = bounds(*r, len(keep), 128, dtype)
+            tol, ltol = bounds(*r, len(keep), 128, fmt, dtype)
             assert (np.abs(out[b, 0, hs].double().cpu().numpy() - w) <= tol).all()
             assert (np.abs(lse[b, 0, hs].double().cpu().numpy() - wl_) <= ltol).all()
     # longer than the table

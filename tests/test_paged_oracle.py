@@ -41,7 +41,7 @@ def test_attention_hand_value():
     q = np.array([[1.0, 0.0]])
     k = np.array([[0.0, 5.0], [np.log(3.0), 0.0]])
     v = np.array([[1.0, 0.0], [0.0, 1.0]])
-    out, lse, _, _, _ = po.attention(q, k, v, 1.0)
+    out, lse, _ = po.attention(q, k, v, 1.0)
     assert np.allclose(out, [[0.25, 0.75]]) and np.allclose(lse, np.log(4.0))
-    out, lse, _, _, _ = po.attention(q, k[:0], v[:0], 1.0)
+    out, lse, _ = po.attention(q, k[:0], v[:0], 1.0)
     assert (out == 0).all() and np.isneginf(lse).all()
