@@ -23,7 +23,8 @@
 //              constant A.  (A code as a subnormal f16 would need no offset of 64, but the instruction aligns products
 //              by exponent fields: its sums then keep 2^-15 instead of 2^-22, measured.)
 //      scales  of keys multiply logits, those of values go into the weights, which are rounded to f16 (2^-11)
-//              relative to the largest weight * scale so far, put at 2^15: f16 leaves 29 binary orders below it.
+//              relative to the largest weight * scale so far, kept between 2^7 and 2^15: f16 leaves 21 binary orders
+//              below that.
 //      fp32    CUDA cores: fp32 products summed over lanes pairwise.
 //  * The softmax is online in base 2 with fp32 maximum, sum and accumulators.  Units that several warps share leave
 //    partial states; the warps' states are joined by their CTA, the CTAs' states by the CTA that arrives last at
@@ -39,6 +40,7 @@ namespace think {
 namespace {
 
 constexpr int kMaxWarps = 16;
+constexpr float kSlack = 8.f, kTop = 7.f;     // running maxima: how far they may lag, and where they put weights (log2)
 constexpr int kMaxG = kMaxPagedGroup;
 
 #ifndef THINK_PW_PLAIN
@@ -134,9 +136,16 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   __half2 v = __floats2half2_rn(lo, hi);
   return *(uint32_t*)&v;
 }
-__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t two) {          // low 16 bits
-  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
-  return (uint32_t)h.x | ((uint32_t)h.y << 16);
+// two e4m3 bytes as f16: the lower and the upper half of a word
+__device__ __forceinline__ uint32_t e4m3_lo_to_f16x2(uint32_t w) {
+  uint32_t d;
+  asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\t}" : "=r"(d) : "r"(w));
+  return d;
+}
+__device__ __forceinline__ uint32_t e4m3_hi_to_f16x2(uint32_t w) {
+  uint32_t d;
+  asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, hi;\n\t}" : "=r"(d) : "r"(w));
+  return d;
 }
 // four floats to e4m3 bytes
 __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
@@ -145,7 +154,7 @@ __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
   return lo | (hi << 16);
 }
 __device__ __forceinline__ float2 e4m3x2_to_float2(uint32_t two) {
-  const uint32_t h = e4m3x2_to_f16x2(two & 0xffffu);
+  const uint32_t h = e4m3_lo_to_f16x2(two);
   return __half22float2(*(const __half2*)&h);
 }
 // codes c at bits 4..7 and 20..23 as the f16 numbers 64 + c
@@ -170,7 +179,7 @@ struct Tables {
   const uint8_t* last;       // tokens in the last tile, minus 1
 };
 struct Cursor {              // a tile of the flat list
-  int b, u;                  // entry, unit of the entry (layer * heads + head)
+  int b, ll, h;              // entry, layer of the call, key head
   int j, nt;                 // tile and tiles of the unit
   int len;
 };
@@ -178,7 +187,7 @@ __device__ __forceinline__ void seq_of(const Tables& t, Cursor& c) {
   c.nt = t.cum[c.b + 1] - t.cum[c.b];
   c.len = (c.nt - 1) * kPageTokens + t.last[c.b] + 1;
 }
-__device__ __forceinline__ Cursor locate(const Tables& t, int B, int LH, int64_t f) {
+__device__ __forceinline__ Cursor locate(const Tables& t, int B, int LH, int N_kv, int64_t f) {
   int lo = 0, hi = B - 1;                      // last entry with cum * LH <= f that has tiles
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -188,15 +197,19 @@ __device__ __forceinline__ Cursor locate(const Tables& t, int B, int LH, int64_t
   c.b = lo;
   seq_of(t, c);
   const int64_t rem = f - (int64_t)t.cum[lo] * LH;
-  c.u = (int)div_wide(rem, c.nt);
-  c.j = (int)(rem - (int64_t)c.u * c.nt);
+  const int u = (int)div_wide(rem, c.nt);
+  c.j = (int)(rem - (int64_t)u * c.nt);
+  c.ll = (int)((unsigned)u / (unsigned)N_kv);
+  c.h = u - c.ll * N_kv;
   return c;
 }
 // to the first tile of the next unit
-__device__ __forceinline__ void next_unit(const Tables& t, int B, int LH, Cursor& c) {
+__device__ __forceinline__ void next_unit(const Tables& t, int B, int nlayers, int N_kv, Cursor& c) {
   c.j = 0;
-  if (++c.u < LH) return;
-  c.u = 0;
+  if (++c.h < N_kv) return;
+  c.h = 0;
+  if (++c.ll < nlayers) return;
+  c.ll = 0;
   do ++c.b; while (c.b < B && t.cum[c.b + 1] == t.cum[c.b]);
   if (c.b < B) seq_of(t, c);
 }
@@ -472,7 +485,8 @@ struct MmaState {
       Mx = fmaxf(Mx, __shfl_xor_sync(0xffffffffu, Mx, 1));
       Mx = fmaxf(Mx, __shfl_xor_sync(0xffffffffu, Mx, 2));
     }
-    if (__any_sync(0xffffffffu, mx > m || Mx > M)) {
+    // the maxima in use move only when one is exceeded 2^8 times: weights then stay below 2^15 (2^8 in fp32)
+    if (__any_sync(0xffffffffu, mx > m + kSlack || Mx > M + kSlack)) {
       const float mn = fmaxf(m, mx), Mn = fmaxf(M, Mx);
       l *= m == -INFINITY ? 0.f : ex2(m - mn);
       const float sc = M == -INFINITY ? 0.f : ex2(M - Mn);
@@ -489,7 +503,7 @@ struct MmaState {
           bias[g][0] *= s0; bias[g][1] *= s1; bias[g][2] *= s0; bias[g][3] *= s1;
         }
     }
-    const float mr = m == -INFINITY ? 0.f : m, Mr = M == -INFINITY ? 0.f : M - 15.f;
+    const float mr = m == -INFINITY ? 0.f : m, Mr = M == -INFINITY ? 0.f : M - kTop;
     // ---- weights and V p, 16 tokens at a time
 #pragma unroll
     for (int kk = 0; kk < NT / 2; ++kk) {
@@ -525,9 +539,8 @@ struct MmaState {
           ldsm4t(vb + (off ^ (i << 5)), v);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {         // a word: channels 2r, 2r + 1 of token 2qd, the same of token 2qd + 1
-            const uint32_t a = v[2 * j], b = v[2 * j + 1];
-            mma<false>(o[2 * i + j], e4m3x2_to_f16x2(__byte_perm(a, 0u, 0x4420)), e4m3x2_to_f16x2(__byte_perm(a, 0u, 0x4431)),
-                       e4m3x2_to_f16x2(__byte_perm(b, 0u, 0x4420)), e4m3x2_to_f16x2(__byte_perm(b, 0u, 0x4431)), b0, b1);
+            const uint32_t a = __byte_perm(v[2 * j], 0u, 0x3120), b = __byte_perm(v[2 * j + 1], 0u, 0x3120);
+            mma<false>(o[2 * i + j], e4m3_lo_to_f16x2(a), e4m3_hi_to_f16x2(a), e4m3_lo_to_f16x2(b), e4m3_hi_to_f16x2(b), b0, b1);
           }
         }
       } else {
@@ -606,7 +619,7 @@ template <int FMT>
 __device__ __forceinline__ float finish(float m, float M, float l) {
   if (m == -INFINITY) return 0.f;
   if (FMT == THINK_PAGE_PLAIN) return 1.f / l;
-  const float h = exp2f(0.5f * (M - 15.f - m));              // in two factors: the exponent may pass 127
+  const float h = exp2f(0.5f * (M - kTop - m));              // in two factors: the exponent may pass 127
   return h / l * h;
 }
 __device__ __forceinline__ float log_sum(float m, float l) {
@@ -879,7 +892,7 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
     if constexpr (E == 4) st.sp = (float*)(smem + kWarps * S::RING + warp * kSpBytes);
 
     // ---- producer: fills the ring tile after tile
-    Cursor pc = locate(tab, B, LH, f0);
+    Cursor pc = locate(tab, B, LH, p.g.N_kv, f0);
     int64_t p_left = f1 - f0;                   // tiles not begun, the current one included
     int p_slot = 0, p_row = 0, p_ntok = 0;      // ring slot; next row of the current tile and its rows
     const uint8_t* p_block = nullptr;
@@ -888,12 +901,11 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
     auto open_tile = [&]() {
       p_ok = (uint32_t)p_page < (uint32_t)p.g.num_pages;
       if (!p_ok && lane == 0) atomicOr(p.error, kErrPage);
-      const int ll = pc.u / p.g.N_kv, h = pc.u - ll * p.g.N_kv;
-      p_block = p.pages + page_block_offset(p.g, p.layer0 + ll, p_ok ? p_page : 0, h);
+      p_block = p.pages + page_block_offset(p.g, p.layer0 + pc.ll, p_ok ? p_page : 0, pc.h);
       p_row = 0;
       p_ntok = min(kPageTokens, pc.len - pc.j * kPageTokens);
       if (--p_left > 0) {                       // look the next tile's page up ahead of time
-        if (++pc.j == pc.nt) next_unit(tab, B, LH, pc);
+        if (++pc.j == pc.nt) next_unit(tab, B, p.nlayers, p.g.N_kv, pc);
         p_page = __ldg(p.table.table + pc.b * p.table.stride + pc.j);
       }
     };
@@ -905,18 +917,22 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
         const uint8_t* const kr = p_block + p_row * S::RB;
         constexpr int CPR = S::RB / 16, RPI = 32 / CPR > 0 ? 32 / CPR : 1, IT = S::HALF / 512;
         const int r0 = CPR < 32 ? lane / CPR : 0, ck = lane % CPR;
+        const uint8_t* const kl = kr + lane * 16;
+        if (n == S::ST) {
 #pragma unroll
-        for (int it = 0; it < IT; ++it) {
-          const int r = it * RPI + r0;
-          const uint32_t d = sb + (S::F32 ? (it * 512 + lane * 16) : swz<S::RB>(r, ck));
-          const int row = S::F32 ? (it * 512 + lane * 16) / S::RB : r;
-          if (n == S::ST) {
-            cp16(d, kr + it * 512 + lane * 16);
-            cp16(d + S::HALF, kr + kPageTokens * S::RB + it * 512 + lane * 16);
-          } else {                              // rows that do not count become zeros
-            const bool on = row < n;
-            cp16(d, on ? kr + it * 512 + lane * 16 : p_block, on ? 16 : 0);
-            cp16(d + S::HALF, on ? kr + kPageTokens * S::RB + it * 512 + lane * 16 : p_block, on ? 16 : 0);
+          for (int it = 0; it < IT; ++it) {
+            const uint32_t d = sb + (S::F32 ? it * 512 + lane * 16 : swz<S::RB>(it * RPI + r0, ck));
+            cp16(d, kl + it * 512);
+            cp16(d + S::HALF, kl + kPageTokens * S::RB + it * 512);
+          }
+        } else {                                // rows that do not count become zeros
+#pragma unroll 1
+          for (int it = 0; it < IT; ++it) {
+            const int r = S::F32 ? (it * 512 + lane * 16) / S::RB : it * RPI + r0;
+            const uint32_t d = sb + (S::F32 ? it * 512 + lane * 16 : swz<S::RB>(r, ck));
+            const bool on = r < n;
+            cp16(d, on ? kl + it * 512 : p_block, on ? 16 : 0);
+            cp16(d + S::HALF, on ? kl + kPageTokens * S::RB + it * 512 : p_block, on ? 16 : 0);
           }
         }
         if constexpr (S::SB > 0) {
@@ -940,13 +956,14 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
 
     // ---- consumer: unit after unit
     int slot = 0;
-    Cursor c = locate(tab, B, LH, f0);
+    Cursor c = locate(tab, B, LH, p.g.N_kv, f0);
     int64_t f = f0;
     while (true) {
       const int64_t us = f - c.j, ue = us + c.nt, se = f1 < ue ? f1 : ue;
       const int j1 = c.j + (int)(se - f);
       const int ntok = min(c.len, j1 * kPageTokens) - c.j * kPageTokens;
-      const int64_t row = ((int64_t)c.b * LH + c.u) * p.G;   // first query row
+      const int unit = c.b * LH + c.ll * p.g.N_kv + c.h;
+      const int64_t row = (int64_t)unit * p.G;   // first query row
       st.begin((const uint8_t*)p.q + row * D * E, p.G, p.scale_log2, lane);
 #pragma unroll 1
       for (int left = ntok; left > 0; left -= S::ST) {
@@ -971,17 +988,17 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
       if (lane == 0) {
         WarpInfo& wi = sh.info[warp];
         if (f == f0) {
-          wi.first_unit = c.b * LH + c.u;
+          wi.first_unit = unit;
           wi.first_us = us;
           wi.first_ue = ue;
         }
-        wi.last_unit = c.b * LH + c.u;
+        wi.last_unit = unit;
         wi.last_us = us;
         wi.last_ue = ue;
       }
       f = se;
       if (is_last) break;
-      next_unit(tab, B, LH, c);
+      next_unit(tab, B, p.nlayers, p.g.N_kv, c);
     }
     cp_wait<0>();
   }

@@ -133,9 +133,9 @@ def bounds(out, lse, sizes, n, D, fmt, dtype):
                 maximum's subtraction included.  A weight exp(x) then carries twice that (its own and the
                 denominator's) relative error, plus 2^-21 for exp2 and 2^-11 where weights are rounded to 16 bits.
       sums      n terms added in fp32 in any order: n u, numerator and denominator.
-      16 bits   a 16-bit weight has a smallest step of 2^-24, with the largest weight * scale between 2^14 and 2^15:
-                each token is off by at most 2^-39 of that product, whose codes are at most 448 (7) of a scale of
-                which the row's largest value has at least 224 (7/2): 2^-38 of top.
+      16 bits   a 16-bit weight has a smallest step of 2^-24, with the largest weight * scale between 2^7 and 2^15:
+                each token is off by at most 2^-32 of that product, whose codes are at most 448 (7) of a scale of
+                which the row's largest value has at least 224 (7/2): 2^-31 of top.
     Quantised pages add
       query     two e4m3 parts, the second 16 times: the smallest step is 2^-9 / 16 with the row's largest channel in
                 [2^7, 2^8), so a channel is off by at most 2^-21 of the largest: 2^-21 q_max.
@@ -155,7 +155,7 @@ def bounds(out, lse, sizes, n, D, fmt, dtype):
     weights = 2 * delta + 2.0 ** -21 + (2.0 ** -11 if dtype == torch.bfloat16 else 0.0) + 2 * (n + 8) * u
     tol = torch.finfo(dtype).eps / 2 * np.abs(out) + weights[:, None] * sizes["absv"] * (1 + 2.0 ** -7) + 1e-30
     if dtype == torch.bfloat16:
-        tol = tol + n * 2.0 ** -38 * sizes["top"][:, None]
+        tol = tol + n * 2.0 ** -31 * sizes["top"][:, None]
     if fmt == "int4":
         tol = tol + 22 * 2 * (n / 16 + 8) * u * sizes["rows"][:, None]
     ltol = delta + (n + 8) * u + 2.0 ** -21 + 4 * u * np.abs(np.where(np.isfinite(lse), lse, 0.0))
