@@ -73,7 +73,8 @@ struct Shape {
   static constexpr int STAGES = SPACE / STAGE < 8 ? SPACE / STAGE : 8;
   static constexpr int RING = STAGES * STAGE;
   static_assert(STAGES >= 2 && WARPS <= kMaxWarps && WARPS >= kMaxG, "ring");
-  static_assert(RING >= (3 * kMaxG + kMaxG * D) * 4, "a warp's partial state reuses its ring");
+  // a warp's partial state reuses its ring; the weights of a join lie at the end of the last warp's
+  static_assert(RING >= (3 * kMaxG + kMaxG * D) * 4 + kMaxG * kSMs * 4, "ring");
 };
 
 // Partial state of one (worker, unit): m[8], M[8], l[8], o[8][D].  m: running maximum of the logits (base 2); M: that
@@ -222,49 +223,15 @@ struct WarpInfo {
   int64_t first_us, first_ue;
 };
 
-// Joins n partial states of one unit (rec(i), in token order).  Returns with the block's threads holding elements
-// i = tid + THREADS * k of the joined accumulators in acc[k]; `stat` (shared) gets m, M and l per query head.
-// GLOBAL: the states were written by other CTAs (read from L2); otherwise by this one, in either memory.
-template <bool GLOBAL>
-__device__ __forceinline__ float rec_load(const float* p) { return GLOBAL ? __ldcg(p) : *p; }
-template <int D, int THREADS, bool GLOBAL, typename RecOf>
-__device__ __forceinline__ void join(int n, int G, RecOf rec, float* weight /* shared [8][n] */, float (*stat)[kMaxG],
-                                     float (&acc)[(kMaxG * D + THREADS - 1) / THREADS]) {
-  const int tid = threadIdx.x, lane = tid & 31, g = tid >> 5;
-  if (g < G) {
-    float m = -INFINITY, M = -INFINITY, l = 0.f;
-    for (int i = lane; i < n; i += 32) {
-      m = fmaxf(m, rec_load<GLOBAL>(&rec(i)->m[g]));
-      M = fmaxf(M, rec_load<GLOBAL>(&rec(i)->M[g]));
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-      M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-    }
-    const float ms = m == -INFINITY ? 0.f : m, Ms = M == -INFINITY ? 0.f : M;
-    for (int i = lane; i < n; i += 32) {
-      l += rec_load<GLOBAL>(&rec(i)->l[g]) * exp2f(rec_load<GLOBAL>(&rec(i)->m[g]) - ms);
-      weight[g * n + i] = exp2f(rec_load<GLOBAL>(&rec(i)->M[g]) - Ms);
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-    if (lane == 0) {
-      stat[0][g] = m;
-      stat[1][g] = M;
-      stat[2][g] = l;
-    }
-  }
-  __syncthreads();
-#pragma unroll
-  for (int k = 0; k < (kMaxG * D + THREADS - 1) / THREADS; ++k) {
-    const int e = tid + THREADS * k, ge = e / D;
-    acc[k] = 0.f;
-    if (ge < G) {
-#pragma unroll 8
-      for (int i = 0; i < n; ++i) acc[k] = fmaf(weight[ge * n + i], rec_load<GLOBAL>(&rec(i)->o[0][0] + e), acc[k]);
-    }
-  }
+__device__ __forceinline__ float rec_load(const float* p) {           // past L1: other CTAs' states; also for shared memory
+  float x;
+  asm volatile("ld.relaxed.gpu.f32 %0, [%1];" : "=f"(x) : "l"(p) : "memory");
+  return x;
+}
+__device__ __forceinline__ float4 rec_load4(const float* p) {
+  float4 x;
+  asm volatile("ld.relaxed.gpu.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "l"(p) : "memory");
+  return x;
 }
 
 // ---------------------------------------------------------------------------------------------------------
@@ -804,7 +771,7 @@ constexpr int kSpBytes = 512;        // fp32: a warp's weights of a step, read 1
 // shared memory behind the rings
 struct alignas(16) Shared {
   WarpInfo info[kMaxWarps];
-  float weight[kMaxG * kMaxWarps];
+  const void* state[kSMs > kMaxWarps ? kSMs : kMaxWarps];    // states of a join, in token order
   float stat[3][kMaxG];
   int warp_sum[kMaxWarps];
   int valid[kMaxWarps][8];   // tokens that count in the stage
@@ -814,7 +781,7 @@ struct alignas(16) Shared {
 template <int D, int E, int FMT, int GP>
 __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode(const PagedDecodeParams p) {
   using S = Shape<D, E, FMT>;
-  constexpr int kWarps = S::WARPS, kThreads = S::THREADS, kElems = (kMaxG * D + kThreads - 1) / kThreads;
+  constexpr int kWarps = S::WARPS, kThreads = S::THREADS;
   using State = typename StateOf<D, E, FMT, GP>::type;
   constexpr int EO = E;                         // bytes of an output element
   extern __shared__ __align__(128) unsigned char smem[];
@@ -1004,107 +971,128 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
   }
   __syncthreads();
 
-  // ---- join what the warps of this CTA share; `leader`: the first warp of the CTA that worked on the unit
-  float acc[kElems];
-  auto emit = [&](const int64_t row) {          // joined accumulators -> output
-#pragma unroll
-    for (int k = 0; k < kElems; ++k) {
-      const int e = tid + kThreads * k, g = e / D;
-      if (g < p.G) {
-        const float fa = finish<FMT>(sh.stat[0][g], sh.stat[1][g], sh.stat[2][g]);
-        const float x = fa == 0.f ? 0.f : acc[k] * fa;
-        if (EO == 4) ((float*)p.out)[row * D + e] = x;
-        else ((__nv_bfloat16*)p.out)[row * D + e] = __float2bfloat16_rn(x);
-        if (p.lse && e % D == 0) p.lse[row + g] = log_sum(sh.stat[0][g], sh.stat[2][g]);
-      }
-    }
-  };
-  int first_warp = 0;
+  // ---- Joins.  Rounds: the unit that the CTA's first warp finishes for earlier CTAs; every warp's last unit, if the
+  // warp is the first of this CTA that worked on it; then, by ticket, the (at most two) units shared with other CTAs.
+  // One loop body for all of them: this code runs once or twice a CTA and is fetched cold, so it is kept small.
+  int first_warp = 0, last_warp = kWarps - 1;
   while (sh.info[first_warp].f0 == sh.info[first_warp].f1) ++first_warp;
-  bool shared_before = false, shared_after = false;          // units shared with other CTAs
-  for (int w = first_warp - 1; w < kWarps; ++w) {
-    // round first_warp - 1: the unit that the CTA's first warp finishes for earlier CTAs; then every warp's last unit
-    const bool head = w < first_warp;
-    const WarpInfo& wi = sh.info[head ? first_warp : w];
-    if (wi.f0 == wi.f1) continue;
-    const int64_t us = head ? wi.first_us : wi.last_us, ue = head ? wi.first_ue : wi.last_ue;
-    const int unit = head ? wi.first_unit : wi.last_unit;
-    if (head) {
-      if (wi.first_unit == wi.last_unit || us >= F0) continue;       // one unit only, or a whole one
-    } else {
-      if (us >= wi.f0 && ue <= wi.f1) continue;                      // whole
-      if (us < wi.f0 && w != first_warp) continue;                   // an earlier warp leads
+  while (sh.info[last_warp].f0 == sh.info[last_warp].f1) --last_warp;
+  bool shared[2] = {false, false};              // a unit shared with earlier, with later CTAs
+#pragma unroll 1
+  for (int round = first_warp - 1; round < kWarps + 2; ++round) {
+    const bool head = round < first_warp, ticket = round >= kWarps;
+    if (round == kWarps) {
+      if (!shared[0] && !shared[1]) return;
+      __threadfence();
+      __syncthreads();
     }
-    const int lead = head ? first_warp : w;
-    const int64_t end = ue < F1 ? ue : F1;
-    const int until = head ? lead : split_owner(F1 - F0, kWarps, end - 1 - F0);
-    // contributors: warps lead .. until that have tiles
+    if (ticket && !shared[round - kWarps]) continue;
+    const WarpInfo& wi = sh.info[head || round == kWarps ? first_warp : ticket ? last_warp : round];
+    if (wi.f0 == wi.f1) continue;
+    const bool first_of = head || round == kWarps;           // the first unit of that warp, else its last
+    const int64_t us = first_of ? wi.first_us : wi.last_us, ue = first_of ? wi.first_ue : wi.last_ue;
+    const int unit = first_of ? wi.first_unit : wi.last_unit;
     int n = 0;
-    uint64_t who = 0;                                                // 4 bits a contributor
-    for (int v = lead; v <= until; ++v)
-      if (sh.info[v].f0 < sh.info[v].f1) who |= (uint64_t)v << (4 * n++);
-    auto rec = [&](int i) -> const Record<D>* {
-      const int v = (int)(who >> (4 * i)) & 15;
-      return sh.info[v].last_unit == unit ? (const Record<D>*)(smem + v * S::RING) : records + 2 * grid + (cta * kWarps + v);
-    };
-    // states in shared or global memory written by this CTA: plain loads
-    join<D, kThreads, false>(n, p.G, rec, sh.weight, sh.stat, acc);
-    if (us >= F0 && ue <= F1) {
-      emit((int64_t)unit * p.G);
+    Record<D>* to = nullptr;                    // joined state goes there; null: it is complete
+    if (!ticket) {
+      if (head) {
+        if (wi.first_unit == wi.last_unit || us >= F0) continue;     // one unit only, or a whole one
+      } else {
+        if (us >= wi.f0 && ue <= wi.f1) continue;                    // whole
+        if (us < wi.f0 && round != first_warp) continue;             // an earlier warp leads
+      }
+      const int lead = head ? first_warp : round;
+      const int until = head ? lead : split_owner(F1 - F0, kWarps, (ue < F1 ? ue : F1) - 1 - F0);
+      const bool mine = lane >= lead && lane <= until && sh.info[lane < kWarps ? lane : 0].f0 < sh.info[lane < kWarps ? lane : 0].f1;
+      const uint32_t who = __ballot_sync(0xffffffffu, mine);
+      n = __popc(who);
+      if (warp == 0 && mine)
+        sh.state[__popc(who & ((1u << lane) - 1u))] = sh.info[lane].last_unit == unit ? (const void*)(smem + lane * S::RING)
+                                                                                      : (const void*)(records + 2 * grid + (cta * kWarps + lane));
+      if (us < F0 || ue > F1) {
+        to = cta_rec + (us < F0 ? 0 : 1);
+        shared[us < F0 ? 0 : 1] = true;
+      }
     } else {
-      const int slot = us < F0 ? 0 : 1;
-      shared_before |= slot == 0;
-      shared_after |= slot == 1;
-      Record<D>* const r = cta_rec + slot;
+      // CTAs without tiles (fewer tiles than CTAs) take no part
+      const bool sparse = total < grid;
+      const int c0 = split_owner(total, grid, us);
+      n = sparse ? (int)(ue - us) : split_owner(total, grid, ue - 1) - c0 + 1;
+      if (tid == 0) {
+        const bool all = atomicAdd(p.counters + unit, 1u) == (unsigned)(n - 1);
+        sh.arrived[round - kWarps] = all;
+        if (all) p.counters[unit] = 0u;                      // ready for the next call
+      }
+      __syncthreads();
+      if (!sh.arrived[round - kWarps]) continue;
+      __threadfence();
+      // the unit began in the first contributor (its record 1); for all others it is the unit that they began with
+      for (int i = tid; i < n; i += kThreads)
+        sh.state[i] = records + 2 * (sparse ? split_owner(total, grid, us + i) : c0 + i) + (i == 0);
+    }
+    __syncthreads();
+    // statistics: a warp per query head
+    const Record<D>* const* const st = (const Record<D>* const*)sh.state;
+    float* const weight = (float*)(smem + kWarps * S::RING) - kMaxG * kSMs;      // [8][n], behind the warps' states
+    if (warp < p.G) {
+      float m = -INFINITY, M = -INFINITY, l = 0.f;
+#pragma unroll 1
+      for (int i = lane; i < n; i += 32) {
+        m = fmaxf(m, rec_load(&st[i]->m[warp]));
+        M = fmaxf(M, rec_load(&st[i]->M[warp]));
+      }
 #pragma unroll
-      for (int k = 0; k < kElems; ++k) {
-        const int e = tid + kThreads * k, g = e / D;
-        if (g < p.G) {
-          (&r->o[0][0])[e] = acc[k];
-          if (e % D == 0) {
-            r->m[g] = sh.stat[0][g];
-            r->M[g] = sh.stat[1][g];
-            r->l[g] = sh.stat[2][g];
-          }
-        }
+      for (int o = 16; o; o >>= 1) {
+        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+      }
+      const float ms = m == -INFINITY ? 0.f : m, Ms = M == -INFINITY ? 0.f : M;
+#pragma unroll 1
+      for (int i = lane; i < n; i += 32) {
+        l += rec_load(&st[i]->l[warp]) * exp2f(rec_load(&st[i]->m[warp]) - ms);
+        weight[warp * n + i] = exp2f(rec_load(&st[i]->M[warp]) - Ms);
+      }
+#pragma unroll
+      for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+      if (lane == 0) {
+        sh.stat[0][warp] = m;
+        sh.stat[1][warp] = M;
+        sh.stat[2][warp] = l;
       }
     }
-    __syncthreads();                            // stat and weight are free again
-  }
-  if (!shared_before && !shared_after) return;
-
-  // ---- tickets of the units shared with other CTAs; the last to arrive joins them
-  __threadfence();
-  __syncthreads();
-  // the first unit of the CTA if it began in an earlier one; the last one if it goes on
-  int lw = kWarps - 1;
-  while (sh.info[lw].f0 == sh.info[lw].f1) --lw;
-  for (int k = 0; k < 2; ++k) {
-    if (!(k == 0 ? shared_before : shared_after)) continue;
-    const WarpInfo& wi = sh.info[k == 0 ? first_warp : lw];
-    const int64_t us = k == 0 ? wi.first_us : wi.last_us, ue = k == 0 ? wi.first_ue : wi.last_ue;
-    const int unit = k == 0 ? wi.first_unit : wi.last_unit;
-    const int c0 = split_owner(total, grid, us), c1 = split_owner(total, grid, ue - 1);
-    // CTAs without tiles (fewer tiles than CTAs) take no part
-    int n = 0;
-    const bool sparse = total < grid;
-    n = sparse ? (int)(ue - us) : c1 - c0 + 1;
-    if (tid == 0) {
-      const unsigned t = atomicAdd(p.counters + unit, 1u);
-      sh.arrived[k] = t == (unsigned)(n - 1);
-      if (sh.arrived[k]) p.counters[unit] = 0u;              // ready for the next call
+    __syncthreads();
+    // accumulators: a thread owns four channels of a query head
+    for (int e = 4 * tid; e < p.G * D; e += 4 * kThreads) {
+      const int g = e / D;
+      const float* const wg = weight + g * n;
+      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+      for (int i = 0; i < n; ++i) {
+        const float4 x = rec_load4(&st[i]->o[0][0] + e);
+        a.x = fmaf(wg[i], x.x, a.x);
+        a.y = fmaf(wg[i], x.y, a.y);
+        a.z = fmaf(wg[i], x.z, a.z);
+        a.w = fmaf(wg[i], x.w, a.w);
+      }
+      const float m = sh.stat[0][g], M = sh.stat[1][g], l = sh.stat[2][g];
+      const bool one = e % D == 0;              // the thread that writes the query head's statistics
+      if (to) {
+        *(float4*)(&to->o[0][0] + e) = a;
+        if (one) {
+          to->m[g] = m;
+          to->M[g] = M;
+          to->l[g] = l;
+        }
+      } else {
+        const int64_t row = (int64_t)unit * p.G;
+        const float f = finish<FMT>(m, M, l);
+        if (f == 0.f) a = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (EO == 4) *(float4*)((float*)p.out + row * D + e) = make_float4(a.x * f, a.y * f, a.z * f, a.w * f);
+        else *(uint2*)((__nv_bfloat16*)p.out + row * D + e) = make_uint2(pack_bf16(a.x * f, a.y * f), pack_bf16(a.z * f, a.w * f));
+        if (one && p.lse) p.lse[row + g] = log_sum(m, l);
+      }
     }
-    __syncthreads();
-    if (!sh.arrived[k]) continue;
-    __threadfence();
-    // the unit began in the first contributor (its record 1); for all others it is the unit that they began with
-    int* const cta_of = (int*)smem;
-    for (int i = tid; i < n; i += kThreads) cta_of[i] = sparse ? split_owner(total, grid, us + i) : c0 + i;
-    __syncthreads();
-    auto rec = [&](int i) -> const Record<D>* { return records + 2 * cta_of[i] + (i == 0); };
-    join<D, kThreads, true>(n, p.G, rec, (float*)smem + kSMs, sh.stat, acc);
-    emit((int64_t)unit * p.G);
-    __syncthreads();
+    __syncthreads();                            // the lists and statistics are free again
   }
 }
 
