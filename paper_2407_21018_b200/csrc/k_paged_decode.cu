@@ -73,8 +73,8 @@ struct Shape {
   static constexpr int STAGES = SPACE / STAGE < 8 ? SPACE / STAGE : 8;
   static constexpr int RING = STAGES * STAGE;
   static_assert(STAGES >= 2 && WARPS <= kMaxWarps && WARPS >= kMaxG, "ring");
-  // a warp's partial state reuses its ring; the weights of a join lie at the end of the last warp's
-  static_assert(RING >= (3 * kMaxG + kMaxG * D) * 4 + kMaxG * kSMs * 4, "ring");
+  // a warp's ring takes its partial state and the weights of a join afterwards, or a join's statistics
+  static_assert(RING >= (3 * kMaxG + kMaxG * D + kMaxWarps * kMaxG) * 4 && RING >= kSMs * 2 * 16, "ring");
 };
 
 // Partial state of one (worker, unit): m[8], M[8], l[8], o[8][D].  m: running maximum of the logits (base 2); M: that
@@ -222,17 +222,6 @@ struct WarpInfo {
   int first_unit, last_unit; // index of the unit in the call
   int64_t first_us, first_ue;
 };
-
-__device__ __forceinline__ float rec_load(const float* p) {           // past L1: other CTAs' states; also for shared memory
-  float x;
-  asm volatile("ld.relaxed.gpu.f32 %0, [%1];" : "=f"(x) : "l"(p) : "memory");
-  return x;
-}
-__device__ __forceinline__ float4 rec_load4(const float* p) {
-  float4 x;
-  asm volatile("ld.relaxed.gpu.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "l"(p) : "memory");
-  return x;
-}
 
 // ---------------------------------------------------------------------------------------------------------
 // Tensor-core formats: fragments of a warp.  Lane (r = lane / 4, qd = lane % 4).  Logits: query r, tokens 8 n + 2 qd,
@@ -589,6 +578,13 @@ __device__ __forceinline__ float finish(float m, float M, float l) {
   const float h = exp2f(0.5f * (M - kTop - m));              // in two factors: the exponent may pass 127
   return h / l * h;
 }
+// four joined accumulators to four outputs of EO bytes
+template <int EO>
+__device__ __forceinline__ void put4(void* to, const float4& a, float f) {
+  const float4 x = f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(a.x * f, a.y * f, a.z * f, a.w * f);
+  if (EO == 4) *(float4*)to = x;
+  else *(uint2*)to = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
+}
 __device__ __forceinline__ float log_sum(float m, float l) {
   return m == -INFINITY ? -INFINITY : (m + log2f(l)) * 0.693147180559945309f;
 }
@@ -771,8 +767,6 @@ constexpr int kSpBytes = 512;        // fp32: a warp's weights of a step, read 1
 // shared memory behind the rings
 struct alignas(16) Shared {
   WarpInfo info[kMaxWarps];
-  const void* state[kSMs > kMaxWarps ? kSMs : kMaxWarps];    // states of a join, in token order
-  float stat[3][kMaxG];
   int warp_sum[kMaxWarps];
   int valid[kMaxWarps][8];   // tokens that count in the stage
   int arrived[2];
@@ -949,8 +943,8 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
         cp_wait<0>();
         __syncwarp();
         st.store_record(tail_rec, p.G, lane);
-      } else {
-        st.store_record(head_rec, p.G, lane);
+      } else {                                  // the end of a unit that an earlier warp, or CTA, began
+        st.store_record(f == F0 ? cta_rec : head_rec, p.G, lane);
       }
       if (lane == 0) {
         WarpInfo& wi = sh.info[warp];
@@ -971,128 +965,172 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
   }
   __syncthreads();
 
-  // ---- Joins.  Rounds: the unit that the CTA's first warp finishes for earlier CTAs; every warp's last unit, if the
-  // warp is the first of this CTA that worked on it; then, by ticket, the (at most two) units shared with other CTAs.
-  // One loop body for all of them: this code runs once or twice a CTA and is fetched cold, so it is kept small.
-  int first_warp = 0, last_warp = kWarps - 1;
-  while (sh.info[first_warp].f0 == sh.info[first_warp].f1) ++first_warp;
-  while (sh.info[last_warp].f0 == sh.info[last_warp].f1) --last_warp;
-  bool shared[2] = {false, false};              // a unit shared with earlier, with later CTAs
+  // ---- Joins inside the CTA: the first warp that worked on a unit joins what the warps have of it, all such units at
+  // the same time.  (A unit that the CTA's first warp only finishes is one state, already where it belongs.)
+  const uint32_t busy = __ballot_sync(0xffffffffu, lane < kWarps && sh.info[lane < kWarps ? lane : 0].f0 < sh.info[lane < kWarps ? lane : 0].f1);
+  const int first_warp = __ffs(busy) - 1, last_warp = 31 - __clz(busy);
+  const int64_t us = sh.info[warp].last_us, ue = sh.info[warp].last_ue;
+  if (f0 < f1 && !(us >= f0 && ue <= f1) && (us >= f0 || warp == first_warp)) {
+    const int unit = sh.info[warp].last_unit;
+    const int until = split_owner(F1 - F0, kWarps, (ue < F1 ? ue : F1) - 1 - F0);
+    const uint32_t who = busy & (2u << until) - (1u << warp);        // warps from this one on that have a state
+    auto rec = [&](int v) -> const Record<D>* {
+      return sh.info[v].last_unit == unit ? (const Record<D>*)(smem + v * S::RING) : records + 2 * grid + (cta * kWarps + v);
+    };
+    // statistics: lane = query head + 8 * (one of four warps at a time)
+    float* const weight = (float*)(smem + warp * S::RING + sizeof(Record<D>));        // [warp][query head]
+    const int g8 = lane & 7;
+    float m = -INFINITY, M = -INFINITY, l = 0.f;
+    if (g8 < p.G) {
 #pragma unroll 1
-  for (int round = first_warp - 1; round < kWarps + 2; ++round) {
-    const bool head = round < first_warp, ticket = round >= kWarps;
-    if (round == kWarps) {
-      if (!shared[0] && !shared[1]) return;
-      __threadfence();
-      __syncthreads();
+      for (int v = warp + (lane >> 3); v <= until; v += 4)
+        if (who >> v & 1) {
+          const Record<D>* const r = rec(v);
+          m = fmaxf(m, r->m[g8]);
+          M = fmaxf(M, r->M[g8]);
+        }
     }
-    if (ticket && !shared[round - kWarps]) continue;
-    const WarpInfo& wi = sh.info[head || round == kWarps ? first_warp : ticket ? last_warp : round];
-    if (wi.f0 == wi.f1) continue;
-    const bool first_of = head || round == kWarps;           // the first unit of that warp, else its last
-    const int64_t us = first_of ? wi.first_us : wi.last_us, ue = first_of ? wi.first_ue : wi.last_ue;
-    const int unit = first_of ? wi.first_unit : wi.last_unit;
-    int n = 0;
-    Record<D>* to = nullptr;                    // joined state goes there; null: it is complete
-    if (!ticket) {
-      if (head) {
-        if (wi.first_unit == wi.last_unit || us >= F0) continue;     // one unit only, or a whole one
-      } else {
-        if (us >= wi.f0 && ue <= wi.f1) continue;                    // whole
-        if (us < wi.f0 && round != first_warp) continue;             // an earlier warp leads
+    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+    M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, 8));
+    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+    M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, 16));
+    if (g8 < p.G) {
+      const float ms = m == -INFINITY ? 0.f : m, Ms = M == -INFINITY ? 0.f : M;
+#pragma unroll 1
+      for (int v = warp + (lane >> 3); v <= until; v += 4)
+        if (who >> v & 1) {
+          const Record<D>* const r = rec(v);
+          l += r->l[g8] * exp2f(r->m[g8] - ms);
+          weight[v * kMaxG + g8] = exp2f(r->M[g8] - Ms);
+        }
+    }
+    l += __shfl_xor_sync(0xffffffffu, l, 8);
+    l += __shfl_xor_sync(0xffffffffu, l, 16);
+    __syncwarp();
+    // accumulators: a lane owns four channels of every (D = 128) or every other (D = 64) query head
+    constexpr int NK = kMaxG * D / 128;
+    float4 a[NK];
+#pragma unroll
+    for (int k = 0; k < NK; ++k) a[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+    for (int v = warp; v <= until; ++v) {
+      if (!(who >> v & 1)) continue;
+      const Record<D>* const r = rec(v);
+#pragma unroll
+      for (int k = 0; k < NK; ++k) {
+        const int e = 128 * k + 4 * lane;
+        if (e < p.G * D) {
+          const float w = weight[v * kMaxG + e / D];
+          const float4 x = *(const float4*)(&r->o[0][0] + e);
+          a[k].x = fmaf(w, x.x, a[k].x);
+          a[k].y = fmaf(w, x.y, a[k].y);
+          a[k].z = fmaf(w, x.z, a[k].z);
+          a[k].w = fmaf(w, x.w, a[k].w);
+        }
       }
-      const int lead = head ? first_warp : round;
-      const int until = head ? lead : split_owner(F1 - F0, kWarps, (ue < F1 ? ue : F1) - 1 - F0);
-      const bool mine = lane >= lead && lane <= until && sh.info[lane < kWarps ? lane : 0].f0 < sh.info[lane < kWarps ? lane : 0].f1;
-      const uint32_t who = __ballot_sync(0xffffffffu, mine);
-      n = __popc(who);
-      if (warp == 0 && mine)
-        sh.state[__popc(who & ((1u << lane) - 1u))] = sh.info[lane].last_unit == unit ? (const void*)(smem + lane * S::RING)
-                                                                                      : (const void*)(records + 2 * grid + (cta * kWarps + lane));
-      if (us < F0 || ue > F1) {
-        to = cta_rec + (us < F0 ? 0 : 1);
-        shared[us < F0 ? 0 : 1] = true;
+    }
+    const bool open = us < F0 || ue > F1;
+    Record<D>* const to = cta_rec + (us < F0 ? 0 : 1);
+    const int64_t row = (int64_t)unit * p.G;
+    const float f = finish<FMT>(m, M, l);
+    if (lane < p.G) {
+      if (open) {
+        to->m[lane] = m;
+        to->M[lane] = M;
+        to->l[lane] = l;
+      } else if (p.lse) {
+        p.lse[row + lane] = log_sum(m, l);
       }
-    } else {
+    }
+#pragma unroll
+    for (int k = 0; k < NK; ++k) {
+      const int e = 128 * k + 4 * lane;
+      const float fk = __shfl_sync(0xffffffffu, f, (e / D) & 7);
+      if (e < p.G * D) {
+        if (open) *(float4*)(&to->o[0][0] + e) = a[k];
+        else put4<EO>((uint8_t*)p.out + (row * D + e) * EO, a[k], fk);
+      }
+    }
+  }
+
+  // ---- Units shared between CTAs, at most one with earlier and one with later CTAs: the last to arrive joins.
+  const WarpInfo& wa = sh.info[first_warp];
+  const WarpInfo& wb = sh.info[last_warp];
+  const bool before = wa.first_us < F0, after = wb.last_us >= F0 && wb.last_ue > F1;
+  if (!before && !after) return;
+  __threadfence();
+  __syncthreads();
+  if (tid < 2) {
+    bool all = false;
+    if (tid == 0 ? before : after) {
+      const int64_t ts = tid == 0 ? wa.first_us : wb.last_us, te = tid == 0 ? wa.first_ue : wb.last_ue;
+      uint32_t* const ticket = p.counters + (tid == 0 ? wa.first_unit : wb.last_unit);
       // CTAs without tiles (fewer tiles than CTAs) take no part
-      const bool sparse = total < grid;
-      const int c0 = split_owner(total, grid, us);
-      n = sparse ? (int)(ue - us) : split_owner(total, grid, ue - 1) - c0 + 1;
-      if (tid == 0) {
-        const bool all = atomicAdd(p.counters + unit, 1u) == (unsigned)(n - 1);
-        sh.arrived[round - kWarps] = all;
-        if (all) p.counters[unit] = 0u;                      // ready for the next call
-      }
-      __syncthreads();
-      if (!sh.arrived[round - kWarps]) continue;
-      __threadfence();
-      // the unit began in the first contributor (its record 1); for all others it is the unit that they began with
-      for (int i = tid; i < n; i += kThreads)
-        sh.state[i] = records + 2 * (sparse ? split_owner(total, grid, us + i) : c0 + i) + (i == 0);
+      const int n = total < grid ? (int)(te - ts) : split_owner(total, grid, te - 1) - split_owner(total, grid, ts) + 1;
+      all = atomicAdd(ticket, 1u) == (unsigned)(n - 1);
+      if (all) *ticket = 0u;                    // ready for the next call
     }
-    __syncthreads();
-    // statistics: a warp per query head
-    const Record<D>* const* const st = (const Record<D>* const*)sh.state;
-    float* const weight = (float*)(smem + kWarps * S::RING) - kMaxG * kSMs;      // [8][n], behind the warps' states
-    if (warp < p.G) {
+    sh.arrived[tid] = all;
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int k = 0; k < 2; ++k) {
+    if (!sh.arrived[k]) continue;
+    __threadfence();
+    const int64_t ts = k == 0 ? wa.first_us : wb.last_us, te = k == 0 ? wa.first_ue : wb.last_ue;
+    const int c0 = split_owner(total, grid, ts);
+    const int n = total < grid ? (int)(te - ts) : split_owner(total, grid, te - 1) - c0 + 1;
+    const int64_t row = (int64_t)(k == 0 ? wa.first_unit : wb.last_unit) * p.G;
+    // a warp takes 128 accumulators, LPG lanes a query head; the lanes of a head go over the contributors
+    constexpr int LPG = D / 4;
+#pragma unroll 1
+    for (int e = 128 * warp + 4 * lane; e - 4 * lane < p.G * D; e += 128 * kWarps) {
+      const bool on = e < p.G * D;
+      const int g = on ? e / D : 0;
+      float4* const st = (float4*)(smem + warp * S::RING) + (lane / LPG) * kSMs;      // m, M, l, record of contributor i
       float m = -INFINITY, M = -INFINITY, l = 0.f;
 #pragma unroll 1
-      for (int i = lane; i < n; i += 32) {
-        m = fmaxf(m, rec_load(&st[i]->m[warp]));
-        M = fmaxf(M, rec_load(&st[i]->M[warp]));
+      for (int i = lane % LPG; i < n; i += LPG) {
+        // the unit began in the first contributor (its record 1); for all others it is the unit that they began with
+        const int ri = 2 * (total < grid ? split_owner(total, grid, ts + i) : c0 + i) + (i == 0);
+        const Record<D>* const r = records + ri;
+        const float4 x = make_float4(__ldcg(&r->m[g]), __ldcg(&r->M[g]), __ldcg(&r->l[g]), __int_as_float(ri));
+        st[i] = x;
+        m = fmaxf(m, x.x);
+        M = fmaxf(M, x.y);
       }
 #pragma unroll
-      for (int o = 16; o; o >>= 1) {
+      for (int o = 1; o < LPG; o <<= 1) {
         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
         M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
       }
       const float ms = m == -INFINITY ? 0.f : m, Ms = M == -INFINITY ? 0.f : M;
 #pragma unroll 1
-      for (int i = lane; i < n; i += 32) {
-        l += rec_load(&st[i]->l[warp]) * exp2f(rec_load(&st[i]->m[warp]) - ms);
-        weight[warp * n + i] = exp2f(rec_load(&st[i]->M[warp]) - Ms);
+      for (int i = lane % LPG; i < n; i += LPG) {
+        const float4 x = st[i];
+        l += x.z * exp2f(x.x - ms);
+        st[i].y = exp2f(x.y - Ms);
       }
 #pragma unroll
-      for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-      if (lane == 0) {
-        sh.stat[0][warp] = m;
-        sh.stat[1][warp] = M;
-        sh.stat[2][warp] = l;
-      }
-    }
-    __syncthreads();
-    // accumulators: a thread owns four channels of a query head
-    for (int e = 4 * tid; e < p.G * D; e += 4 * kThreads) {
-      const int g = e / D;
-      const float* const wg = weight + g * n;
+      for (int o = 1; o < LPG; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+      __syncwarp();
       float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (on) {
 #pragma unroll 4
-      for (int i = 0; i < n; ++i) {
-        const float4 x = rec_load4(&st[i]->o[0][0] + e);
-        a.x = fmaf(wg[i], x.x, a.x);
-        a.y = fmaf(wg[i], x.y, a.y);
-        a.z = fmaf(wg[i], x.z, a.z);
-        a.w = fmaf(wg[i], x.w, a.w);
-      }
-      const float m = sh.stat[0][g], M = sh.stat[1][g], l = sh.stat[2][g];
-      const bool one = e % D == 0;              // the thread that writes the query head's statistics
-      if (to) {
-        *(float4*)(&to->o[0][0] + e) = a;
-        if (one) {
-          to->m[g] = m;
-          to->M[g] = M;
-          to->l[g] = l;
+        for (int i = 0; i < n; ++i) {
+          const float2 x = *(const float2*)&st[i].z;         // (l, record)
+          const float w = st[i].y;
+          const float4 y = __ldcg((const float4*)(&records[__float_as_int(x.y)].o[0][0] + e));
+          a.x = fmaf(w, y.x, a.x);
+          a.y = fmaf(w, y.y, a.y);
+          a.z = fmaf(w, y.z, a.z);
+          a.w = fmaf(w, y.w, a.w);
         }
-      } else {
-        const int64_t row = (int64_t)unit * p.G;
-        const float f = finish<FMT>(m, M, l);
-        if (f == 0.f) a = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (EO == 4) *(float4*)((float*)p.out + row * D + e) = make_float4(a.x * f, a.y * f, a.z * f, a.w * f);
-        else *(uint2*)((__nv_bfloat16*)p.out + row * D + e) = make_uint2(pack_bf16(a.x * f, a.y * f), pack_bf16(a.z * f, a.w * f));
-        if (one && p.lse) p.lse[row + g] = log_sum(m, l);
+        put4<EO>((uint8_t*)p.out + (row * D + e) * EO, a, finish<FMT>(m, M, l));
+        if (p.lse && e % D == 0) p.lse[row + g] = log_sum(m, l);
       }
+      __syncwarp();
     }
-    __syncthreads();                            // the lists and statistics are free again
   }
 }
 
