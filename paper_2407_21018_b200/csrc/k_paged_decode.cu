@@ -17,11 +17,11 @@
 //              within 2^13 of the row's largest, else off by at most 2^-21 of that one.  The instruction sums 32
 //              products to 2^-22 of their magnitudes (measured), like the 16-bit ones.  bf16 keys use m16n8k16.
 //      values  A = values transposed (16 channels x 16 tokens, ldmatrix.trans), B = weights.  bf16: the weights are a
-//              bf16 pair high + low (two instructions), 2^-17.  e4m3: bytes become f16 exactly.  4-bit: a code
-//              under the exponent of 64 is the f16 number 64 + c, a shift and a bit select.  The offset 72 = 64 + 8 is
-//              taken off at the end: 72 * sum of the very same rounded weights comes from one more product with a
-//              constant A.  (A code as a subnormal f16 would need no offset of 64, but the instruction aligns products
-//              by exponent fields: its sums then keep 2^-15 instead of 2^-22, measured.)
+//              bf16 pair high + low (two instructions), 2^-17.  e4m3: bytes become f16 exactly.  4-bit: a code under
+//              the exponent of 1024 is the f16 number 1024 + c (or 1024 + 16 c), one more instruction makes it n.
+//              (As a subnormal f16 a code would need no instruction at all, but the tensor core aligns products by
+//              exponent fields: its sums then keep 2^-15 instead of 2^-22, measured.  As 64 + c with the offset
+//              taken off the sums at the end it takes two more shifts, 16 more registers and loses 3 bits.)
 //      scales  of keys multiply logits, those of values go into the weights, which are rounded to f16 (2^-11)
 //              relative to the largest weight * scale so far, kept between 2^7 and 2^15: f16 leaves 21 binary orders
 //              below that.
@@ -113,11 +113,11 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// d = a b + (c0, c0, c1, c1), e4m3
-__device__ __forceinline__ void mma_fp8(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, float c0, float c1) {
-  asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%11,%11};"
+// d = a b, e4m3
+__device__ __forceinline__ void mma_fp8_new(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1));
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ void mma_fp8(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -128,6 +128,35 @@ __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+// two fp32 in a register pair: one instruction for both
+using f32x2 = unsigned long long;
+__device__ __forceinline__ f32x2 two(float a, float b) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void split(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// larger of two pairs of bf16
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
@@ -158,8 +187,18 @@ __device__ __forceinline__ float2 e4m3x2_to_float2(uint32_t two) {
   const uint32_t h = e4m3_lo_to_f16x2(two);
   return __half22float2(*(const __half2*)&h);
 }
-// codes c at bits 4..7 and 20..23 as the f16 numbers 64 + c
-__device__ __forceinline__ uint32_t plus64(uint32_t w) { return (w & 0x00f000f0u) | 0x54005400u; }
+// the codes at bits 0..3 and 16..19 of w, minus 8, as f16
+__device__ __forceinline__ uint32_t int4_lo_to_f16x2(uint32_t w) {
+  const uint32_t t = (w & 0x000f000fu) | 0x64006400u, eight = 0x64086408u;    // 1024 + code, 1024 + 8
+  const __half2 r = __hsub2(*(const __half2*)&t, *(const __half2*)&eight);
+  return *(const uint32_t*)&r;
+}
+// the same at bits 4..7 and 20..23: (1024 + 16 code) / 16 - 72
+__device__ __forceinline__ uint32_t int4_hi_to_f16x2(uint32_t w) {
+  const uint32_t t = (w & 0x00f000f0u) | 0x64006400u, k = 0x2c002c00u, o = 0xd480d480u;
+  const __half2 r = __hfma2(*(const __half2*)&t, *(const __half2*)&k, *(const __half2*)&o);
+  return *(const uint32_t*)&r;
+}
 // small integers to float without the conversion unit: 2^23 + n
 __device__ __forceinline__ float magic(uint32_t n) { return __uint_as_float(0x4b000000u | n); }
 // 2^k for -126 <= k <= 127
@@ -240,11 +279,11 @@ struct MmaState {
   static constexpr int WIDTH = PLAIN ? 1 : INT4 ? 4 : 2;     // consecutive channels that a lane holds
 
   uint32_t q[NG][4];         // A fragments.  bf16: k16 block s has q[s / 2][2 (s % 2)], [.. + 1] as rows 0..7
-  float corr[INT4 ? NG : 1][2];                 // 4-bit: -8 * 2^-9 * sum of the block's query parts (high, low)
+  float corr[INT4 ? NG : 1];                    // 4-bit: -8 * 2^-9 * sum of the block's query (as its parts stand for it)
   float rs;                  // base-2 logit per unit of the q k product
-  float m, M, l;             // of query r; l: this lane's tokens only
+  float m, M, l;             // of query r; l: complete after end()
+  f32x2 l2;                  // sum over this lane's tokens, even and odd ones
   float o[OT][4];
-  float bias[INT4 ? NG : 1][4];                 // 4-bit: 72 * sum of the weights
 
   // the unit's queries as A fragments; qg: its first query row
   __device__ __forceinline__ void begin(const void* qg_, int G, float scale_log2, int lane) {
@@ -307,22 +346,17 @@ struct MmaState {
           }
         }
         if constexpr (INT4) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            part[h] += __shfl_xor_sync(0xffffffffu, part[h], 1);
-            part[h] += __shfl_xor_sync(0xffffffffu, part[h], 2);
-            corr[g][h] = part[h] * (-8.f / 512.f);
-          }
+          float t = fmaf(part[1], 0.0625f, part[0]);
+          t += __shfl_xor_sync(0xffffffffu, t, 1);
+          t += __shfl_xor_sync(0xffffffffu, t, 2);
+          corr[g] = t * (-8.f / 512.f);
         }
       }
     }
     m = M = -INFINITY;
-    l = 0.f;
+    l2 = 0;
 #pragma unroll
     for (int t = 0; t < OT; ++t) o[t][0] = o[t][1] = o[t][2] = o[t][3] = 0.f;
-    if constexpr (INT4)
-#pragma unroll
-      for (int g = 0; g < NG; ++g) bias[g][0] = bias[g][1] = bias[g][2] = bias[g][3] = 0.f;
   }
 
   // bf16 scales of tokens 8n + 2qd (first NG / 2 words) and 8n + 2qd + 1
@@ -343,7 +377,7 @@ struct MmaState {
   __device__ __forceinline__ void step(uint32_t sb, int ntok, int lane) {
     const int qd = lane & 3, mi = lane >> 3, tr = lane & 7;
     const uint32_t ks = sb + 2 * S::HALF, vs = ks + S::ST * S::SB;
-    float x[NT][2];
+    f32x2 x[NT];                                // the lane's two tokens of each group
     // ---- logits
     if constexpr (PLAIN) {
       const int off = (tr + 8 * (mi >> 1)) * S::RB + (((mi & 1) ^ tr) << 4);
@@ -357,25 +391,26 @@ struct MmaState {
           mma<true>(c[s & 1], q[s >> 1][2 * (s & 1)], 0u, q[s >> 1][2 * (s & 1) + 1], 0u, k[0], k[1]);
           mma<true>(c[2 + (s & 1)], q[s >> 1][2 * (s & 1)], 0u, q[s >> 1][2 * (s & 1) + 1], 0u, k[2], k[3]);
         }
-        x[n][0] = (c[0][0] + c[1][0]) * rs; x[n][1] = (c[0][1] + c[1][1]) * rs;
-        x[n + 1][0] = (c[2][0] + c[3][0]) * rs; x[n + 1][1] = (c[2][1] + c[3][1]) * rs;
+        x[n] = mul2(add2(two(c[0][0], c[0][1]), two(c[1][0], c[1][1])), two(rs, rs));
+        x[n + 1] = mul2(add2(two(c[2][0], c[2][1]), two(c[3][0], c[3][1])), two(rs, rs));
       }
     } else if constexpr (!INT4) {
       const int off = S::RB == 128 ? tr * 128 + ((mi ^ tr) << 4) : tr * 64 + ((mi ^ (tr >> 1)) << 4);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        float c[4] = {};
+        float c[4];
 #pragma unroll
         for (int i = 0; i < NG / 2; ++i) {
           uint32_t k[4];
           ldsm4(sb + n * 8 * S::RB + (off ^ (i << 6)), k);
-          mma_fp8(c, q[2 * i], k[0], k[1]);
+          if (i == 0) mma_fp8_new(c, q[0], k[0], k[1]);
+          else mma_fp8(c, q[2 * i], k[0], k[1]);
           mma_fp8(c, q[2 * i + 1], k[2], k[3]);
         }
         uint32_t sc;
         asm volatile("ld.shared.u16 %0, [%1];" : "=r"(sc) : "r"(ks + 8 * n + 2 * qd));
-        x[n][0] = fmaf(c[2], 0.0625f, c[0]) * (rs * __uint_as_float((sc & 0xffu) << 23));
-        x[n][1] = fmaf(c[3], 0.0625f, c[1]) * (rs * __uint_as_float((sc >> 8) << 23));
+        const f32x2 f = mul2(two(__uint_as_float((sc & 0xffu) << 23), __uint_as_float((sc >> 8) << 23)), two(rs, rs));
+        x[n] = mul2(fma2(two(c[2], c[3]), two(0.0625f, 0.0625f), two(c[0], c[1])), f);
       }
     } else {
       const int off = S::RB == 64 ? tr * 64 + ((mi ^ (tr >> 1)) << 4) : (tr + 8 * (mi >> 1)) * 32 + (((mi & 1) ^ (tr >> 2)) << 4);
@@ -389,75 +424,83 @@ struct MmaState {
           const int n = n0 + p;
           uint32_t sc[NG];
           load_scales(ks, n, qd, sc);
-          float y0 = 0.f, y1 = 0.f;
+          f32x2 y = 0;
 #pragma unroll
           for (int g = 0; g < NG; ++g) {
             const uint32_t w = k[p * NG + g];
             float c[4];
-            mma_fp8(c, q[g], w & 0x0f0f0f0fu, (w >> 4) & 0x0f0f0f0fu, corr[g][0], corr[g][1]);
-            y0 = fmaf(fmaf(c[2], 0.0625f, c[0]), scale_of(sc, 0, g), y0);
-            y1 = fmaf(fmaf(c[3], 0.0625f, c[1]), scale_of(sc, 1, g), y1);
+            mma_fp8_new(c, q[g], w & 0x0f0f0f0fu, (w >> 4) & 0x0f0f0f0fu);
+            const f32x2 t = add2(fma2(two(c[2], c[3]), two(0.0625f, 0.0625f), two(c[0], c[1])), two(corr[g], corr[g]));
+            y = fma2(t, two(scale_of(sc, 0, g), scale_of(sc, 1, g)), y);
           }
-          x[n][0] = y0 * rs;
-          x[n][1] = y1 * rs;
+          x[n] = mul2(y, two(rs, rs));
         }
       }
     }
     if (ntok < S::ST) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        if (8 * n + 2 * qd >= ntok) x[n][0] = -INFINITY;
-        if (8 * n + 2 * qd + 1 >= ntok) x[n][1] = -INFINITY;
+        float a, b;
+        split(x[n], a, b);
+        if (8 * n + 2 * qd >= ntok) a = -INFINITY;
+        if (8 * n + 2 * qd + 1 >= ntok) b = -INFINITY;
+        x[n] = two(a, b);
       }
     }
-    // ---- running maxima of the logits and of logit + log2 of the value's scale.  The latter only has to keep weights
-    // within f16: for 4-bit rows it is the largest scale's bits read as a piecewise linear logarithm (low by < 0.09)
-    float es[NT][2], mx = -INFINITY, Mx = -INFINITY;
+    // ---- running maxima of the logits and of logit + log2 of the value's scale.  For 4-bit rows the latter only has to
+    // keep weights within f16: it is the largest scale's bits read as a piecewise linear logarithm (low by < 0.09),
+    // 65536 + 127 too large until the end, which leaves it 7 fraction bits
+    f32x2 es[NT];
+    float mx = -INFINITY, Mx = -INFINITY;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      mx = fmaxf(mx, fmaxf(x[n][0], x[n][1]));
+      float a, b;
+      split(x[n], a, b);
+      mx = fmaxf(mx, fmaxf(a, b));
       if constexpr (INT4) {
-        uint32_t sc[NG];
+        uint32_t sc[NG], t[2];
         load_scales(vs, n, qd, sc);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          uint32_t t = sc[i * (NG / 2)];
-          if (NG == 4) t = __vmaxu2(t, sc[i * (NG / 2) + NG / 2 - 1]);
-          t = max(max(t & 0xffffu, t >> 16), 27u << 7);      // 2^-100 at least: the weight's other factor stays finite
-          es[n][i] = fmaf(magic(t) - 8388608.f, 0.0078125f, x[n][i] - 127.f);
+          t[i] = sc[i * (NG / 2)];
+          if (NG == 4) t[i] = max_bf16x2(t[i], sc[i * (NG / 2) + NG / 2 - 1]);
+          t[i] = max_bf16x2(t[i], __byte_perm(t[i], 0u, 0x1032));
+          t[i] = __byte_perm(t[i], 0x4b000000u, 0x7410);     // as a float: 2^23 + bits
         }
+        es[n] = fma2(two(__uint_as_float(t[0]), __uint_as_float(t[1])), two(0.0078125f, 0.0078125f), x[n]);
       } else if constexpr (!PLAIN) {
         uint32_t sc;
         asm volatile("ld.shared.u16 %0, [%1];" : "=r"(sc) : "r"(vs + 8 * n + 2 * qd));
-        es[n][0] = x[n][0] + (magic(sc & 0xffu) - 8388735.f);
-        es[n][1] = x[n][1] + (magic(sc >> 8) - 8388735.f);
+        es[n] = add2(x[n], add2(two(magic(sc & 0xffu), magic(sc >> 8)), two(-8388735.f, -8388735.f)));
       }
-      if constexpr (!PLAIN) Mx = fmaxf(Mx, fmaxf(es[n][0], es[n][1]));
+      if constexpr (!PLAIN) {
+        split(es[n], a, b);
+        Mx = fmaxf(Mx, fmaxf(a, b));
+      }
     }
+    if constexpr (INT4) Mx -= 65663.f;
     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
     if constexpr (PLAIN) Mx = mx;
     else {
       Mx = fmaxf(Mx, __shfl_xor_sync(0xffffffffu, Mx, 1));
       Mx = fmaxf(Mx, __shfl_xor_sync(0xffffffffu, Mx, 2));
+      if (INT4) Mx = fmaxf(Mx, mx - 100.f);     // scales below 2^-100: the weight's other factor stays finite
     }
     // the maxima in use move only when one is exceeded 2^8 times: weights then stay below 2^15 (2^8 in fp32)
     if (__any_sync(0xffffffffu, mx > m + kSlack || Mx > M + kSlack)) {
       const float mn = fmaxf(m, mx), Mn = fmaxf(M, Mx);
-      l *= m == -INFINITY ? 0.f : ex2(m - mn);
+      const float ml = m == -INFINITY ? 0.f : ex2(m - mn);
+      l2 = mul2(l2, two(ml, ml));
       const float sc = M == -INFINITY ? 0.f : ex2(M - Mn);
       m = mn;
       M = Mn;
-      const float s0 = __shfl_sync(0xffffffffu, sc, 8 * qd), s1 = __shfl_sync(0xffffffffu, sc, 8 * qd + 4);
+      const f32x2 s01 = two(__shfl_sync(0xffffffffu, sc, 8 * qd), __shfl_sync(0xffffffffu, sc, 8 * qd + 4));
 #pragma unroll
       for (int t = 0; t < OT; ++t) {
-        o[t][0] *= s0; o[t][1] *= s1; o[t][2] *= s0; o[t][3] *= s1;
+        split(mul2(two(o[t][0], o[t][1]), s01), o[t][0], o[t][1]);
+        split(mul2(two(o[t][2], o[t][3]), s01), o[t][2], o[t][3]);
       }
-      if constexpr (INT4)
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          bias[g][0] *= s0; bias[g][1] *= s1; bias[g][2] *= s0; bias[g][3] *= s1;
-        }
     }
     const float mr = m == -INFINITY ? 0.f : m, Mr = M == -INFINITY ? 0.f : M - kTop;
     // ---- weights and V p, 16 tokens at a time
@@ -467,13 +510,20 @@ struct MmaState {
       const int r = ((mi & 1) << 3) + tr;
       float w[2][2];
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const float p = ex2(x[2 * kk + j][i] - mr);
-          l += p;
-          w[j][i] = PLAIN ? p : ex2((INT4 ? x[2 * kk + j][i] : es[2 * kk + j][i]) - Mr);
+      for (int j = 0; j < 2; ++j) {
+        float a, b;
+        split(add2(x[2 * kk + j], two(-mr, -mr)), a, b);
+        a = ex2(a);
+        b = ex2(b);
+        l2 = add2(l2, two(a, b));
+        if constexpr (!PLAIN) {
+          split(add2(INT4 ? x[2 * kk + j] : es[2 * kk + j], two(-Mr, -Mr)), a, b);
+          a = ex2(a);
+          b = ex2(b);
         }
+        w[j][0] = a;
+        w[j][1] = b;
+      }
       if constexpr (PLAIN) {
         const uint32_t h0 = pack_bf16(w[0][0], w[0][1]), h1 = pack_bf16(w[1][0], w[1][1]);
         const uint32_t l0 = pack_bf16(w[0][0] - bf16lo(h0), w[0][1] - bf16hi(h0));
@@ -511,12 +561,14 @@ struct MmaState {
 #pragma unroll
           for (int j = 0; j < 2; ++j) {         // a word: channels 4r .. 4r + 3 of token 2qd, the same of token 2qd + 1
             const int g = 2 * g2 + j;
-            const uint32_t b0 = pack_f16(w[0][0] * scale_of(s0, 0, g), w[0][1] * scale_of(s0, 1, g));
-            const uint32_t b1 = pack_f16(w[1][0] * scale_of(s1, 0, g), w[1][1] * scale_of(s1, 1, g));
+            float f[4];
+            split(mul2(two(w[0][0], w[0][1]), two(scale_of(s0, 0, g), scale_of(s0, 1, g))), f[0], f[1]);
+            split(mul2(two(w[1][0], w[1][1]), two(scale_of(s1, 0, g), scale_of(s1, 1, g))), f[2], f[3]);
+            const uint32_t b0 = pack_f16(f[0], f[1]), b1 = pack_f16(f[2], f[3]);
             const uint32_t a = v[2 * j], b = v[2 * j + 1];
-            mma<false>(o[2 * g], plus64(a << 4), plus64(a), plus64(b << 4), plus64(b), b0, b1);
-            mma<false>(o[2 * g + 1], plus64(a >> 4), plus64(a >> 8), plus64(b >> 4), plus64(b >> 8), b0, b1);
-            mma<false>(bias[g], 0x54805480u, 0x54805480u, 0x54805480u, 0x54805480u, b0, b1);
+            const uint32_t a8 = a >> 8, b8 = b >> 8;
+            mma<false>(o[2 * g], int4_lo_to_f16x2(a), int4_hi_to_f16x2(a), int4_lo_to_f16x2(b), int4_hi_to_f16x2(b), b0, b1);
+            mma<false>(o[2 * g + 1], int4_lo_to_f16x2(a8), int4_hi_to_f16x2(a8), int4_lo_to_f16x2(b8), int4_hi_to_f16x2(b8), b0, b1);
           }
         }
       }
@@ -539,16 +591,19 @@ struct MmaState {
       } else {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          a[2 * h] = o[2 * i + h][0] - bias[i][0];
-          a[2 * h + 1] = o[2 * i + h][2] - bias[i][0];
-          b[2 * h] = o[2 * i + h][1] - bias[i][1];
-          b[2 * h + 1] = o[2 * i + h][3] - bias[i][1];
+          a[2 * h] = o[2 * i + h][0];
+          a[2 * h + 1] = o[2 * i + h][2];
+          b[2 * h] = o[2 * i + h][1];
+          b[2 * h + 1] = o[2 * i + h][3];
         }
       }
       f(8 * WIDTH * i + WIDTH * r, a, b);
     }
   }
   __device__ __forceinline__ void end() {
+    float a, b;
+    split(l2, a, b);
+    l = a + b;
     l += __shfl_xor_sync(0xffffffffu, l, 1);
     l += __shfl_xor_sync(0xffffffffu, l, 2);
   }

@@ -139,11 +139,9 @@ def bounds(out, lse, sizes, n, D, fmt, dtype):
     Quantised pages add
       query     two e4m3 parts, the second 16 times: the smallest step is 2^-9 / 16 with the row's largest channel in
                 [2^7, 2^8), so a channel is off by at most 2^-21 of the largest: 2^-21 q_max.
-      offsets   4-bit key codes enter as n + 8 <= 15, value codes as n + 72 <= 79, and the 8 or 72 is taken off
-                afterwards; a group's scale is 1/7 of its largest value, so the sums hold (15 + 8) / 7 < 4 and
-                (79 + 72) / 7 < 22 times the largest value where n itself may be 0.  An instruction rounds its sum of 32
-                or 16 terms once, 2 u of their magnitudes: (2 + D / 32) u 4 k_max and 2 u (n / 16 + 8) 22 rows, where
-                8 stands for the steps that end before 16 tokens and the joins of partial sums.
+      offsets   4-bit key codes enter as n + 8 <= 15 and the 8 is taken off afterwards; a group's scale is 1/7 of its
+                largest value, so the sums hold (15 + 8) / 7 < 4 times the largest value where n itself may be 0.  An
+                instruction rounds its sum of 32 terms once, 2 u of their magnitudes: (2 + D / 32) u 4 k_max.
     Weighted with |v| the weights' errors are relative to absv.  The output is rounded once to its type: half a step,
     finfo.eps / 2 relative."""
     u = 2.0 ** -23
@@ -156,8 +154,6 @@ def bounds(out, lse, sizes, n, D, fmt, dtype):
     tol = torch.finfo(dtype).eps / 2 * np.abs(out) + weights[:, None] * sizes["absv"] * (1 + 2.0 ** -7) + 1e-30
     if dtype == torch.bfloat16:
         tol = tol + n * 2.0 ** -31 * sizes["top"][:, None]
-    if fmt == "int4":
-        tol = tol + 22 * 2 * (n / 16 + 8) * u * sizes["rows"][:, None]
     ltol = delta + (n + 8) * u + 2.0 ** -21 + 4 * u * np.abs(np.where(np.isfinite(lse), lse, 0.0))
     return tol, ltol
 
