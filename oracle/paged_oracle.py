@@ -93,18 +93,17 @@ def attention(q: np.ndarray, k: np.ndarray, v: np.ndarray, scale: float):
     """One key head: q [G, D], k and v [n, D].  Returns (out [G, D], lse [G], sizes), where sizes holds the magnitudes
     that the error bounds of the tests are made of (maxima over the tokens t, weights w):
       absv [G, D]   sum of w |v|                 qk     max over t of sum |scale q_i k_i|
-      top           max over t of w max|v|       q_max  max over t of |scale| max|q| sum |k_i|
-      rows          sum of w max|v|              k_max  |scale| sum |q_i| max|k|"""
+      top           max over t of w max|v|       q_max  max over t of |scale| max|q| sum |k_i|"""
     G, D = q.shape
     if k.shape[0] == 0:
         z = np.zeros(G)
-        return np.zeros((G, D)), np.full(G, -np.inf), dict(absv=np.zeros((G, D)), top=z, rows=z, qk=z, q_max=z, k_max=z)
+        return np.zeros((G, D)), np.full(G, -np.inf), dict(absv=np.zeros((G, D)), top=z, qk=z, q_max=z)
     x = scale * (q @ k.T)
     m = x.max(axis=1, keepdims=True)
     p = np.exp(x - m)
     z = p.sum(axis=1, keepdims=True)
     w = p / z
     aq, ak, vm, s = np.abs(q), np.abs(k), np.abs(v).max(axis=1), abs(scale)
-    sizes = dict(absv=w @ np.abs(v), top=(w * vm).max(axis=1), rows=w @ vm, qk=s * (aq @ ak.T).max(axis=1),
-                 q_max=s * aq.max(axis=1) * ak.sum(axis=1).max(), k_max=s * aq.sum(axis=1) * ak.max())
+    sizes = dict(absv=w @ np.abs(v), top=(w * vm).max(axis=1), qk=s * (aq @ ak.T).max(axis=1),
+                 q_max=s * aq.max(axis=1) * ak.sum(axis=1).max())
     return w @ v, (m + np.log(z))[:, 0], sizes

@@ -8,20 +8,17 @@
 //  * A warp is the worker.  It owns a ring of stages in shared memory that it fills with cp.async, crossing page and
 //    unit borders, and waits for nobody until its range is done.
 //  * Rows are stored token-major.  16-byte chunks are XOR-swizzled on the way into shared memory so that ldmatrix
-//    reads without bank conflicts.  Products run on mma.sync (a group has at most 8 query rows: 8 of the 128 rows
-//    that a tcgen05 tile would have), arranged so that all 16 x 8 results of an instruction count:
-//      logits  A = queries (16 rows), B = keys.  e4m3 and 4-bit keys go to the fp8 instruction (m16n8k32, four times
-//              the rate of f16 per product) as they are: an e4m3 byte is its own operand and a 4-bit code c, as a byte
-//              0..15, IS the e4m3 number c * 2^-9, so unpacking is a mask.  The query is split into two e4m3 parts,
-//              high parts in rows 0..7 and 16 * low parts in rows 8..15: exact for bf16 queries whose channels lie
-//              within 2^13 of the row's largest, else off by at most 2^-21 of that one.  The instruction sums 32
-//              products to 2^-22 of their magnitudes (measured), like the 16-bit ones.  bf16 keys use m16n8k16.
-//      values  A = values transposed (16 channels x 16 tokens, ldmatrix.trans), B = weights.  bf16: the weights are a
-//              bf16 pair high + low (two instructions), 2^-17.  e4m3: bytes become f16 exactly.  4-bit: a code under
-//              the exponent of 1024 is the f16 number 1024 + c (or 1024 + 16 c), one more instruction makes it n.
-//              (As a subnormal f16 a code would need no instruction at all, but the tensor core aligns products by
-//              exponent fields: its sums then keep 2^-15 instead of 2^-22, measured.  As 64 + c with the offset
-//              taken off the sums at the end it takes two more shifts, 16 more registers and loses 3 bits.)
+//    reads without bank conflicts.  Products run on mma.sync m16n8k16 (a group has at most 8 query rows: 8 of the 128
+//    rows that a tcgen05 tile would have).
+//      logits  A = queries (rows 0..7), B = keys.  e4m3 and 4-bit codes become f16 exactly (byte conversion; a masked
+//              4-bit code is the subnormal c * 2^-24 or c * 2^-20, one multiply-add makes it (c - 8) * 2^-9); the query is f16 times a power of two, exact unless its channels are more than 2^28 apart.
+//              (The fp8 form of the instruction takes the codes as they are, but on this machine it is a sequence of
+//              conversions and two f16 instructions: 22 cycles against 8.3, measured.)
+//      values  A = values transposed (16 channels x 16 tokens, ldmatrix.trans), B = weights, so all 16 x 8 results count
+//              and the accumulators take half the registers.  bf16: the weights are a bf16 pair high + low (two
+//              instructions), 2^-17.  e4m3, 4-bit: f16 codes as above.  (The subnormals as they are
+//              would do with the 8 taken off the sums, but the tensor core aligns products by exponent fields: sums then keep 2^-15 instead of
+//              2^-22, measured.)
 //      scales  of keys multiply logits, those of values go into the weights, which are rounded to f16 (2^-11)
 //              relative to the largest weight * scale so far, kept between 2^7 and 2^15: f16 leaves 21 binary orders
 //              below that.
@@ -113,16 +110,15 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// d = a b, e4m3
-__device__ __forceinline__ void mma_fp8_new(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
-      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
-}
-__device__ __forceinline__ void mma_fp8(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+// rows 0..7 of A only, no accumulator yet
+template <bool BF16>
+__device__ __forceinline__ void mma_first(float (&d)[4], uint32_t a0, uint32_t a2, uint32_t b0, uint32_t b1) {
+  if (BF16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%8,%5,%8}, {%6,%7}, {%9,%9,%9,%9};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a2), "r"(b0), "r"(b1), "r"(0u), "f"(0.f));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%8,%5,%8}, {%6,%7}, {%9,%9,%9,%9};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a2), "r"(b0), "r"(b1), "r"(0u), "f"(0.f));
 }
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -177,25 +173,15 @@ __device__ __forceinline__ uint32_t e4m3_hi_to_f16x2(uint32_t w) {
   asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, hi;\n\t}" : "=r"(d) : "r"(w));
   return d;
 }
-// four floats to e4m3 bytes
-__device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
-  const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
-  const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
-  return lo | (hi << 16);
-}
-__device__ __forceinline__ float2 e4m3x2_to_float2(uint32_t two) {
-  const uint32_t h = e4m3_lo_to_f16x2(two);
-  return __half22float2(*(const __half2*)&h);
-}
-// the codes at bits 0..3 and 16..19 of w, minus 8, as f16
+// the codes at bits 0..3 and 16..19 of w as f16 numbers n * 2^-9: the masked word holds subnormals c * 2^-24
 __device__ __forceinline__ uint32_t int4_lo_to_f16x2(uint32_t w) {
-  const uint32_t t = (w & 0x000f000fu) | 0x64006400u, eight = 0x64086408u;    // 1024 + code, 1024 + 8
-  const __half2 r = __hsub2(*(const __half2*)&t, *(const __half2*)&eight);
+  const uint32_t t = w & 0x000f000fu, k = 0x78007800u, o = 0xa400a400u;       // 2^15, -8 * 2^-9
+  const __half2 r = __hfma2(*(const __half2*)&t, *(const __half2*)&k, *(const __half2*)&o);
   return *(const uint32_t*)&r;
 }
-// the same at bits 4..7 and 20..23: (1024 + 16 code) / 16 - 72
+// the same at bits 4..7 and 20..23: c * 2^-20
 __device__ __forceinline__ uint32_t int4_hi_to_f16x2(uint32_t w) {
-  const uint32_t t = (w & 0x00f000f0u) | 0x64006400u, k = 0x2c002c00u, o = 0xd480d480u;
+  const uint32_t t = w & 0x00f000f0u, k = 0x68006800u, o = 0xa400a400u;       // 2^11
   const __half2 r = __hfma2(*(const __half2*)&t, *(const __half2*)&k, *(const __half2*)&o);
   return *(const uint32_t*)&r;
 }
@@ -254,6 +240,12 @@ __device__ __forceinline__ void next_unit(const Tables& t, int B, int nlayers, i
   if (c.b < B) seq_of(t, c);
 }
 
+// brings `bytes` (a multiple of 128, at most 4096) towards the SM; the values are not waited for
+__device__ __forceinline__ void touch(const uint8_t* p, int bytes, int lane) {
+  uint32_t x;
+  if (lane * 128 < bytes) asm volatile("ld.global.ca.u32 %0, [%1];" : "=r"(x) : "l"(p + lane * 128));
+}
+
 // What a warp tells its CTA about the range it has done.
 struct WarpInfo {
   int64_t f0, f1;            // empty if equal
@@ -274,12 +266,11 @@ struct MmaState {
   static constexpr bool PLAIN = FMT == THINK_PAGE_PLAIN;
   static constexpr bool INT4 = FMT == THINK_PAGE_INT4;
   static constexpr int NT = S::ST / 8;          // groups of 8 tokens of a step
-  static constexpr int NG = D / 32;             // k32 blocks of a row; scale groups of 4-bit rows
+  static constexpr int NG = D / 32;             // blocks of 32 channels, the scale groups of 4-bit rows
   static constexpr int OT = D / 16;
   static constexpr int WIDTH = PLAIN ? 1 : INT4 ? 4 : 2;     // consecutive channels that a lane holds
 
-  uint32_t q[NG][4];         // A fragments.  bf16: k16 block s has q[s / 2][2 (s % 2)], [.. + 1] as rows 0..7
-  float corr[INT4 ? NG : 1];                    // 4-bit: -8 * 2^-9 * sum of the block's query (as its parts stand for it)
+  uint32_t q[NG][4];         // A fragments, rows 0..7: (a0, a2) of the two k16 instructions of a block
   float rs;                  // base-2 logit per unit of the q k product
   float m, M, l;             // of query r; l: complete after end()
   f32x2 l2;                  // sum over this lane's tokens, even and odd ones
@@ -317,39 +308,23 @@ struct MmaState {
       t = max(t & 0xffffu, t >> 16);
       t = max(t, __shfl_xor_sync(0xffffffffu, t, 1));
       t = max(t, __shfl_xor_sync(0xffffffffu, t, 2));
-      // the row's largest channel goes to [2^7, 2^8)
-      const int k = min(134 - (int)(t >> 7), 100);
+      // the row's largest channel goes to [2^14, 2^15)
+      const int k = min(141 - (int)(t >> 7), 100);
       const float up = pow2i(k);
       rs = scale_log2 * pow2i(-k);
-      if (INT4) rs *= 512.f;                    // a code is c * 2^-9
+      if (INT4) rs *= 512.f;                    // codes are n * 2^-9
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
-        float x[8], part[2] = {0.f, 0.f};       // the channels of the first and of the second half of the k32 block
+        if constexpr (INT4) {                   // the codes of a word pair up as channels (0,4) (1,5) | (2,6) (3,7)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float lo = bf16lo(w[g][i]) * up, hi = bf16hi(w[g][i]) * up;
-          x[INT4 ? i : 2 * i] = lo;             // 4-bit: the even codes of a word are its first operand, the odd its second
-          x[INT4 ? 4 + i : 2 * i + 1] = hi;
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float* y = x + 4 * h;
-          const uint32_t a = e4m3x4(y[0], y[1], y[2], y[3]);
-          const float2 u = e4m3x2_to_float2(a), v = e4m3x2_to_float2(a >> 16);
-          const uint32_t b = e4m3x4((y[0] - u.x) * 16.f, (y[1] - u.y) * 16.f, (y[2] - v.x) * 16.f, (y[3] - v.y) * 16.f);
-          q[g][2 * h] = a;
-          q[g][2 * h + 1] = b;
-          if constexpr (INT4) {
-            const float2 c = e4m3x2_to_float2(b), d = e4m3x2_to_float2(b >> 16);
-            part[0] += (u.x + u.y) + (v.x + v.y);
-            part[1] += (c.x + c.y) + (d.x + d.y);
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t a = w[g][j], b = w[g][2 + j];
+            q[g][2 * j] = pack_f16(bf16lo(a) * up, bf16lo(b) * up);
+            q[g][2 * j + 1] = pack_f16(bf16hi(a) * up, bf16hi(b) * up);
           }
-        }
-        if constexpr (INT4) {
-          float t = fmaf(part[1], 0.0625f, part[0]);
-          t += __shfl_xor_sync(0xffffffffu, t, 1);
-          t += __shfl_xor_sync(0xffffffffu, t, 2);
-          corr[g] = t * (-8.f / 512.f);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) q[g][i] = pack_f16(bf16lo(w[g][i]) * up, bf16hi(w[g][i]) * up);
         }
       }
     }
@@ -383,13 +358,19 @@ struct MmaState {
       const int off = (tr + 8 * (mi >> 1)) * S::RB + (((mi & 1) ^ tr) << 4);
 #pragma unroll
       for (int n = 0; n < NT; n += 2) {
-        float c[4][4] = {};                     // even and odd channel groups in chains of their own
+        float c[4][4];                          // even and odd channel groups in chains of their own
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) {
+          const uint32_t a0 = q[s >> 1][2 * (s & 1)], a2 = q[s >> 1][2 * (s & 1) + 1];
           uint32_t k[4];
           ldsm4(sb + n * 8 * S::RB + (off ^ (s << 5)), k);
-          mma<true>(c[s & 1], q[s >> 1][2 * (s & 1)], 0u, q[s >> 1][2 * (s & 1) + 1], 0u, k[0], k[1]);
-          mma<true>(c[2 + (s & 1)], q[s >> 1][2 * (s & 1)], 0u, q[s >> 1][2 * (s & 1) + 1], 0u, k[2], k[3]);
+          if (s < 2) {
+            mma_first<true>(c[s], a0, a2, k[0], k[1]);
+            mma_first<true>(c[2 + s], a0, a2, k[2], k[3]);
+          } else {
+            mma<true>(c[s & 1], a0, 0u, a2, 0u, k[0], k[1]);
+            mma<true>(c[2 + (s & 1)], a0, 0u, a2, 0u, k[2], k[3]);
+          }
         }
         x[n] = mul2(add2(two(c[0][0], c[0][1]), two(c[1][0], c[1][1])), two(rs, rs));
         x[n + 1] = mul2(add2(two(c[2][0], c[2][1]), two(c[3][0], c[3][1])), two(rs, rs));
@@ -398,19 +379,22 @@ struct MmaState {
       const int off = S::RB == 128 ? tr * 128 + ((mi ^ tr) << 4) : tr * 64 + ((mi ^ (tr >> 1)) << 4);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        float c[4];
+        float c[2][4];                          // two chains
 #pragma unroll
         for (int i = 0; i < NG / 2; ++i) {
           uint32_t k[4];
           ldsm4(sb + n * 8 * S::RB + (off ^ (i << 6)), k);
-          if (i == 0) mma_fp8_new(c, q[0], k[0], k[1]);
-          else mma_fp8(c, q[2 * i], k[0], k[1]);
-          mma_fp8(c, q[2 * i + 1], k[2], k[3]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {         // a word: channels 4qd .. 4qd + 3 of 16
+            const uint32_t a0 = q[2 * i + (j >> 1)][2 * (j & 1)], a2 = q[2 * i + (j >> 1)][2 * (j & 1) + 1];
+            if (i == 0 && j < 2) mma_first<false>(c[j], a0, a2, e4m3_lo_to_f16x2(k[j]), e4m3_hi_to_f16x2(k[j]));
+            else mma<false>(c[j & 1], a0, 0u, a2, 0u, e4m3_lo_to_f16x2(k[j]), e4m3_hi_to_f16x2(k[j]));
+          }
         }
         uint32_t sc;
         asm volatile("ld.shared.u16 %0, [%1];" : "=r"(sc) : "r"(ks + 8 * n + 2 * qd));
         const f32x2 f = mul2(two(__uint_as_float((sc & 0xffu) << 23), __uint_as_float((sc >> 8) << 23)), two(rs, rs));
-        x[n] = mul2(fma2(two(c[2], c[3]), two(0.0625f, 0.0625f), two(c[0], c[1])), f);
+        x[n] = mul2(add2(two(c[0][0], c[0][1]), two(c[1][0], c[1][1])), f);
       }
     } else {
       const int off = S::RB == 64 ? tr * 64 + ((mi ^ (tr >> 1)) << 4) : (tr + 8 * (mi >> 1)) * 32 + (((mi & 1) ^ (tr >> 2)) << 4);
@@ -428,10 +412,11 @@ struct MmaState {
 #pragma unroll
           for (int g = 0; g < NG; ++g) {
             const uint32_t w = k[p * NG + g];
+            const uint32_t w8 = w >> 8;
             float c[4];
-            mma_fp8_new(c, q[g], w & 0x0f0f0f0fu, (w >> 4) & 0x0f0f0f0fu);
-            const f32x2 t = add2(fma2(two(c[2], c[3]), two(0.0625f, 0.0625f), two(c[0], c[1])), two(corr[g], corr[g]));
-            y = fma2(t, two(scale_of(sc, 0, g), scale_of(sc, 1, g)), y);
+            mma_first<false>(c, q[g][0], q[g][1], int4_lo_to_f16x2(w), int4_hi_to_f16x2(w));
+            mma<false>(c, q[g][2], 0u, q[g][3], 0u, int4_lo_to_f16x2(w8), int4_hi_to_f16x2(w8));
+            y = fma2(two(c[0], c[1]), two(scale_of(sc, 0, g), scale_of(sc, 1, g)), y);
           }
           x[n] = mul2(y, two(rs, rs));
         }
@@ -630,7 +615,8 @@ template <int FMT>
 __device__ __forceinline__ float finish(float m, float M, float l) {
   if (m == -INFINITY) return 0.f;
   if (FMT == THINK_PAGE_PLAIN) return 1.f / l;
-  const float h = exp2f(0.5f * (M - kTop - m));              // in two factors: the exponent may pass 127
+  // accumulators are in units of 2^(M - kTop), 4-bit ones of 512 times that; two factors: the exponent may pass 127
+  const float h = exp2f(0.5f * (M - (FMT == THINK_PAGE_INT4 ? kTop - 9.f : kTop) - m));
   return h / l * h;
 }
 // four joined accumulators to four outputs of EO bytes
@@ -908,70 +894,93 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
     if constexpr (E == 4) st.sp = (float*)(smem + kWarps * S::RING + warp * kSpBytes);
 
     // ---- producer: fills the ring tile after tile
+    const int q_bytes = p.G * D * E;            // queries of a unit, in the order of units
+    const int64_t page_bytes = (int64_t)p.g.N_kv * p.g.block_bytes;
     Cursor pc = locate(tab, B, LH, p.g.N_kv, f0);
-    int64_t p_left = f1 - f0;                   // tiles not begun, the current one included
-    int p_slot = 0, p_row = 0, p_ntok = 0;      // ring slot; next row of the current tile and its rows
-    const uint8_t* p_block = nullptr;
+    touch((const uint8_t*)p.q + (int64_t)(pc.b * LH + pc.ll * p.g.N_kv + pc.h) * q_bytes, q_bytes, lane);
+    const int32_t* p_entry = p.table.table + pc.b * p.table.stride + pc.j;       // table entry of the next tile
+    int p_page = __ldg(p_entry);                // looked up a tile ahead
+    const uint8_t* p_base = p.pages + page_block_offset(p.g, p.layer0 + pc.ll, 0, pc.h);    // of the unit
+    int p_tiles = (int)min((int64_t)(pc.nt - pc.j), f1 - f0);                    // of the unit, not begun
+    int p_toks = pc.len - pc.j * kPageTokens;                                    // of the unit, not begun
+    int64_t p_left = f1 - f0 - p_tiles;         // tiles of later units
+    uint32_t p_slot = ring;                     // next stage to fill
+    int p_ntok = 0;                             // rows of the current tile that are left
     bool p_ok = false;
-    int p_page = __ldg(p.table.table + pc.b * p.table.stride + pc.j);       // of the current tile
+    const uint8_t* p_row = nullptr;             // its next key row
+    const uint8_t* p_scale = nullptr;           // and scale
+    int* p_valid = sh.valid[warp];
     auto open_tile = [&]() {
       p_ok = (uint32_t)p_page < (uint32_t)p.g.num_pages;
       if (!p_ok && lane == 0) atomicOr(p.error, kErrPage);
-      p_block = p.pages + page_block_offset(p.g, p.layer0 + pc.ll, p_ok ? p_page : 0, pc.h);
-      p_row = 0;
-      p_ntok = min(kPageTokens, pc.len - pc.j * kPageTokens);
-      if (--p_left > 0) {                       // look the next tile's page up ahead of time
-        if (++pc.j == pc.nt) next_unit(tab, B, p.nlayers, p.g.N_kv, pc);
-        p_page = __ldg(p.table.table + pc.b * p.table.stride + pc.j);
+      p_row = p_base + (p_ok ? p_page : 0) * page_bytes;
+      if (S::SB > 0) p_scale = p_row + 2 * kPageTokens * S::RB;
+      p_ntok = min(kPageTokens, p_toks);
+      p_toks -= kPageTokens;
+      ++p_entry;
+      if (--p_tiles == 0 && p_left > 0) {
+        next_unit(tab, B, p.nlayers, p.g.N_kv, pc);
+        p_entry = p.table.table + pc.b * p.table.stride;
+        p_base = p.pages + page_block_offset(p.g, p.layer0 + pc.ll, 0, pc.h);
+        p_tiles = (int)min((int64_t)pc.nt, p_left);
+        p_toks = pc.len;
+        p_left -= p_tiles;
       }
+      if (p_tiles > 0) p_page = __ldg(p_entry);
     };
+    constexpr int CPR = S::RB / 16, RPI = 32 / CPR > 0 ? 32 / CPR : 1, IT = S::HALF / 512;
+    constexpr int SC = S::SB > 0 ? S::ST * S::SB / 16 : 1;   // 16-byte pieces of a step's key scales
+    static_assert(2 * SC <= 32 && S::ST * S::SB % 16 == 0, "one piece a lane");
+    const int r0 = CPR < 32 ? lane / CPR : 0, ck = lane % CPR;
+    const int s_part = lane / SC, s_at = 16 * (lane % SC);
+    const uint32_t s_dst = 2 * S::HALF + s_part * S::ST * S::SB + s_at;
+    const int s_src = s_part * kPageTokens * S::SB + s_at;
     auto issue = [&]() {
-      if (p_row >= p_ntok && p_left > 0) open_tile();
-      if (p_row < p_ntok) {
-        const uint32_t sb = ring + p_slot * S::STAGE;
-        const int n = p_ok ? min(S::ST, p_ntok - p_row) : 0;
-        const uint8_t* const kr = p_block + p_row * S::RB;
-        constexpr int CPR = S::RB / 16, RPI = 32 / CPR > 0 ? 32 / CPR : 1, IT = S::HALF / 512;
-        const int r0 = CPR < 32 ? lane / CPR : 0, ck = lane % CPR;
-        const uint8_t* const kl = kr + lane * 16;
+      if (p_ntok <= 0 && p_tiles > 0) open_tile();
+      if (p_ntok > 0) {
+        const int n = p_ok ? min(S::ST, p_ntok) : 0;
+        const uint8_t* const kl = p_row + lane * 16;
         if (n == S::ST) {
 #pragma unroll
           for (int it = 0; it < IT; ++it) {
-            const uint32_t d = sb + (S::F32 ? it * 512 + lane * 16 : swz<S::RB>(it * RPI + r0, ck));
+            const uint32_t d = p_slot + (S::F32 ? it * 512 + lane * 16 : swz<S::RB>(it * RPI + r0, ck));
             cp16(d, kl + it * 512);
             cp16(d + S::HALF, kl + kPageTokens * S::RB + it * 512);
           }
+          if (S::SB > 0 && lane < 2 * SC) cp16(p_slot + s_dst, p_scale + s_src);
         } else {                                // rows that do not count become zeros
 #pragma unroll 1
           for (int it = 0; it < IT; ++it) {
             const int r = S::F32 ? (it * 512 + lane * 16) / S::RB : it * RPI + r0;
-            const uint32_t d = sb + (S::F32 ? it * 512 + lane * 16 : swz<S::RB>(r, ck));
+            const uint32_t d = p_slot + (S::F32 ? it * 512 + lane * 16 : swz<S::RB>(r, ck));
             const bool on = r < n;
-            cp16(d, on ? kl + it * 512 : p_block, on ? 16 : 0);
-            cp16(d + S::HALF, on ? kl + kPageTokens * S::RB + it * 512 : p_block, on ? 16 : 0);
+            cp16(d, on ? kl + it * 512 : p.pages, on ? 16 : 0);
+            cp16(d + S::HALF, on ? kl + kPageTokens * S::RB + it * 512 : p.pages, on ? 16 : 0);
+          }
+          if (S::SB > 0 && lane < 2 * SC) {
+            const int bytes = max(0, min(16, n * S::SB - s_at));
+            cp16(p_slot + s_dst, bytes ? p_scale + s_src : p.pages, bytes);
           }
         }
-        if constexpr (S::SB > 0) {
-          constexpr int C = S::ST * S::SB / 16;              // 16-byte pieces of the key scales
-          static_assert(2 * C <= 32 && S::ST * S::SB % 16 == 0, "one piece a lane");
-          if (lane < 2 * C) {
-            const int part = lane / C, i = lane % C;
-            const int bytes = max(0, min(16, n * S::SB - 16 * i));
-            const uint8_t* src = p_block + 2 * kPageTokens * S::RB + part * kPageTokens * S::SB + p_row * S::SB + 16 * i;
-            cp16(sb + 2 * S::HALF + part * S::ST * S::SB + 16 * i, bytes ? src : p_block, bytes);
-          }
-        }
-        if (lane == 0) sh.valid[warp][p_slot] = n;
-        p_row += S::ST;
+        if (lane == 0) *p_valid = n;
+        p_ntok -= S::ST;
+        p_row += S::HALF;
+        if (S::SB > 0) p_scale += S::ST * S::SB;
       }
       cp_commit();                              // one group a call, possibly empty
-      p_slot = p_slot + 1 == S::STAGES ? 0 : p_slot + 1;
+      p_slot += S::STAGE;
+      ++p_valid;
+      if (p_slot == ring + S::RING) {
+        p_slot = ring;
+        p_valid = sh.valid[warp];
+      }
     };
 #pragma unroll 1
     for (int i = 0; i < S::STAGES - 1; ++i) issue();
 
     // ---- consumer: unit after unit
-    int slot = 0;
+    uint32_t c_slot = ring;
+    const int* c_valid = sh.valid[warp];
     Cursor c = locate(tab, B, LH, p.g.N_kv, f0);
     int64_t f = f0;
     while (true) {
@@ -981,14 +990,21 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
       const int unit = c.b * LH + c.ll * p.g.N_kv + c.h;
       const int64_t row = (int64_t)unit * p.G;   // first query row
       st.begin((const uint8_t*)p.q + row * D * E, p.G, p.scale_log2, lane);
+      // the next unit's queries come while this one is worked on (it may be one of an empty sequence)
+      if (se < f1) touch((const uint8_t*)p.q + (row + p.G) * D * E, q_bytes, lane);
 #pragma unroll 1
       for (int left = ntok; left > 0; left -= S::ST) {
         cp_wait<S::STAGES - 2>();
         __syncwarp();                           // the step has landed; all lanes are done with the slot before
-        const int n = sh.valid[warp][slot];
+        const int n = *c_valid;
         issue();
-        st.step(ring + slot * S::STAGE, n, lane);
-        slot = slot + 1 == S::STAGES ? 0 : slot + 1;
+        st.step(c_slot, n, lane);
+        c_slot += S::STAGE;
+        ++c_valid;
+        if (c_slot == ring + S::RING) {
+          c_slot = ring;
+          c_valid = sh.valid[warp];
+        }
       }
       st.end();
       const bool whole = f == us && se == ue, is_last = se == f1;
@@ -1020,30 +1036,37 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
   }
   __syncthreads();
 
-  // ---- Joins inside the CTA: the first warp that worked on a unit joins what the warps have of it, all such units at
-  // the same time.  (A unit that the CTA's first warp only finishes is one state, already where it belongs.)
+  // ---- Joins inside the CTA.  The warps whose last unit is the same share its join: each takes some of the
+  // accumulators.  The states: those of these warps, and of the next one if it finished the unit and went on.  (A unit
+  // that the CTA's first warp only finishes is one state, already where it belongs.)
   const uint32_t busy = __ballot_sync(0xffffffffu, lane < kWarps && sh.info[lane < kWarps ? lane : 0].f0 < sh.info[lane < kWarps ? lane : 0].f1);
   const int first_warp = __ffs(busy) - 1, last_warp = 31 - __clz(busy);
   const int64_t us = sh.info[warp].last_us, ue = sh.info[warp].last_ue;
-  if (f0 < f1 && !(us >= f0 && ue <= f1) && (us >= f0 || warp == first_warp)) {
+  if (f0 < f1 && !(us >= f0 && ue <= f1)) {
     const int unit = sh.info[warp].last_unit;
-    const int until = split_owner(F1 - F0, kWarps, (ue < F1 ? ue : F1) - 1 - F0);
-    const uint32_t who = busy & (2u << until) - (1u << warp);        // warps from this one on that have a state
-    auto rec = [&](int v) -> const Record<D>* {
-      return sh.info[v].last_unit == unit ? (const Record<D>*)(smem + v * S::RING) : records + 2 * grid + (cta * kWarps + v);
+    const uint32_t same = busy & __ballot_sync(0xffffffffu, lane < kWarps && sh.info[lane < kWarps ? lane : 0].last_unit == unit);
+    const int lead = __ffs(same) - 1, helpers = __popc(same), me = __popc(same & ((1u << warp) - 1u));
+    const int end_warp = 32 - __clz(same);                             // behind the last of them
+    const uint32_t on = busy >> end_warp << end_warp;                  // the next one that has tiles
+    const int extra = on ? __ffs(on) - 1 : -1;
+    const bool more = extra >= 0 && sh.info[extra].first_unit == unit;
+    const int n = helpers + more;
+    // state i, in token order (warps without tiles between them are left out: fewer tiles than warps)
+    auto rec = [&](int i) -> const Record<D>* {
+      return i == helpers ? records + 2 * grid + (cta * kWarps + extra)
+                          : (const Record<D>*)(smem + (F1 - F0 >= kWarps ? lead + i : (int)__fns(same, 0, i + 1)) * S::RING);
     };
-    // statistics: lane = query head + 8 * (one of four warps at a time)
-    float* const weight = (float*)(smem + warp * S::RING + sizeof(Record<D>));        // [warp][query head]
+    // statistics: lane = query head + 8 * (one of four states at a time)
+    float* const weight = (float*)(smem + warp * S::RING + sizeof(Record<D>));        // [state][query head]
     const int g8 = lane & 7;
     float m = -INFINITY, M = -INFINITY, l = 0.f;
     if (g8 < p.G) {
 #pragma unroll 1
-      for (int v = warp + (lane >> 3); v <= until; v += 4)
-        if (who >> v & 1) {
-          const Record<D>* const r = rec(v);
-          m = fmaxf(m, r->m[g8]);
-          M = fmaxf(M, r->M[g8]);
-        }
+      for (int i = lane >> 3; i < n; i += 4) {
+        const Record<D>* const r = rec(i);
+        m = fmaxf(m, r->m[g8]);
+        M = fmaxf(M, r->M[g8]);
+      }
     }
     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
     M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, 8));
@@ -1052,43 +1075,20 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
     if (g8 < p.G) {
       const float ms = m == -INFINITY ? 0.f : m, Ms = M == -INFINITY ? 0.f : M;
 #pragma unroll 1
-      for (int v = warp + (lane >> 3); v <= until; v += 4)
-        if (who >> v & 1) {
-          const Record<D>* const r = rec(v);
-          l += r->l[g8] * exp2f(r->m[g8] - ms);
-          weight[v * kMaxG + g8] = exp2f(r->M[g8] - Ms);
-        }
+      for (int i = lane >> 3; i < n; i += 4) {
+        const Record<D>* const r = rec(i);
+        l += r->l[g8] * exp2f(r->m[g8] - ms);
+        weight[i * kMaxG + g8] = exp2f(r->M[g8] - Ms);
+      }
     }
     l += __shfl_xor_sync(0xffffffffu, l, 8);
     l += __shfl_xor_sync(0xffffffffu, l, 16);
     __syncwarp();
-    // accumulators: a lane owns four channels of every (D = 128) or every other (D = 64) query head
-    constexpr int NK = kMaxG * D / 128;
-    float4 a[NK];
-#pragma unroll
-    for (int k = 0; k < NK; ++k) a[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 1
-    for (int v = warp; v <= until; ++v) {
-      if (!(who >> v & 1)) continue;
-      const Record<D>* const r = rec(v);
-#pragma unroll
-      for (int k = 0; k < NK; ++k) {
-        const int e = 128 * k + 4 * lane;
-        if (e < p.G * D) {
-          const float w = weight[v * kMaxG + e / D];
-          const float4 x = *(const float4*)(&r->o[0][0] + e);
-          a[k].x = fmaf(w, x.x, a[k].x);
-          a[k].y = fmaf(w, x.y, a[k].y);
-          a[k].z = fmaf(w, x.z, a[k].z);
-          a[k].w = fmaf(w, x.w, a[k].w);
-        }
-      }
-    }
     const bool open = us < F0 || ue > F1;
     Record<D>* const to = cta_rec + (us < F0 ? 0 : 1);
     const int64_t row = (int64_t)unit * p.G;
     const float f = finish<FMT>(m, M, l);
-    if (lane < p.G) {
+    if (me == 0 && lane < p.G) {
       if (open) {
         to->m[lane] = m;
         to->M[lane] = M;
@@ -1097,13 +1097,24 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
         p.lse[row + lane] = log_sum(m, l);
       }
     }
-#pragma unroll
-    for (int k = 0; k < NK; ++k) {
-      const int e = 128 * k + 4 * lane;
-      const float fk = __shfl_sync(0xffffffffu, f, (e / D) & 7);
+    // accumulators, 128 at a time, four a lane
+#pragma unroll 1
+    for (int e = 128 * me + 4 * lane; e - 4 * lane < p.G * D; e += 128 * helpers) {
+      const int g = (e / D) & 7;
+      const float fg = __shfl_sync(0xffffffffu, f, g);
       if (e < p.G * D) {
-        if (open) *(float4*)(&to->o[0][0] + e) = a[k];
-        else put4<EO>((uint8_t*)p.out + (row * D + e) * EO, a[k], fk);
+        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int i = 0; i < n; ++i) {
+          const float w = weight[i * kMaxG + g];
+          const float4 x = *(const float4*)(&rec(i)->o[0][0] + e);
+          a.x = fmaf(w, x.x, a.x);
+          a.y = fmaf(w, x.y, a.y);
+          a.z = fmaf(w, x.z, a.z);
+          a.w = fmaf(w, x.w, a.w);
+        }
+        if (open) *(float4*)(&to->o[0][0] + e) = a;
+        else put4<EO>((uint8_t*)p.out + (row * D + e) * EO, a, fg);
       }
     }
   }

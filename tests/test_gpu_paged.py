@@ -136,20 +136,14 @@ def bounds(out, lse, sizes, n, D, fmt, dtype):
       16 bits   a 16-bit weight has a smallest step of 2^-24, with the largest weight * scale between 2^7 and 2^15:
                 each token is off by at most 2^-32 of that product, whose codes are at most 448 (7) of a scale of
                 which the row's largest value has at least 224 (7/2): 2^-31 of top.
-    Quantised pages add
-      query     two e4m3 parts, the second 16 times: the smallest step is 2^-9 / 16 with the row's largest channel in
-                [2^7, 2^8), so a channel is off by at most 2^-21 of the largest: 2^-21 q_max.
-      offsets   4-bit key codes enter as n + 8 <= 15 and the 8 is taken off afterwards; a group's scale is 1/7 of its
-                largest value, so the sums hold (15 + 8) / 7 < 4 times the largest value where n itself may be 0.  An
-                instruction rounds its sum of 32 terms once, 2 u of their magnitudes: (2 + D / 32) u 4 k_max.
+      query     of quantised pages: f16 with the row's largest channel in [2^14, 2^15) and a smallest step of 2^-24, so
+                a channel is off by at most 2^-39 of the largest: 2^-39 q_max.
     Weighted with |v| the weights' errors are relative to absv.  The output is rounded once to its type: half a step,
     finfo.eps / 2 relative."""
     u = 2.0 ** -23
     delta = (D + 4) * u * sizes["qk"]
     if fmt != "plain":
-        delta = delta + 2.0 ** -21 * sizes["q_max"]
-    if fmt == "int4":
-        delta = delta + (2 + D // 32) * u * 4 * sizes["k_max"]
+        delta = delta + 2.0 ** -39 * sizes["q_max"]
     weights = 2 * delta + 2.0 ** -21 + (2.0 ** -11 if dtype == torch.bfloat16 else 0.0) + 2 * (n + 8) * u
     tol = torch.finfo(dtype).eps / 2 * np.abs(out) + weights[:, None] * sizes["absv"] * (1 + 2.0 ** -7) + 1e-30
     if dtype == torch.bfloat16:
