@@ -71,14 +71,15 @@ struct Shape {
   static constexpr int RING = STAGES * STAGE;
   static_assert(STAGES >= 2 && WARPS <= kMaxWarps && WARPS >= kMaxG, "ring");
   // a warp's ring takes its partial state and the weights of a join afterwards, or a join's statistics
-  static_assert(RING >= (3 * kMaxG + kMaxG * D + kMaxWarps * kMaxG) * 4 && RING >= kSMs * 2 * 16, "ring");
+  static_assert(RING >= (3 * kMaxG + kMaxG * (D + 4) + kMaxWarps * kMaxG) * 4 && RING >= kSMs * 2 * 16, "ring");
 };
 
 // Partial state of one (worker, unit): m[8], M[8], l[8], o[8][D].  m: running maximum of the logits (base 2); M: that
 // of logit + exponent of the value's scale, the unit of the accumulators; l: sum of exp2(logit - m).
+// Rows are 4 floats longer than D: the lanes of a fragment, two rows apart, then store to different banks.
 template <int D>
 struct Record {
-  float m[kMaxG], M[kMaxG], l[kMaxG], o[kMaxG][D];
+  float m[kMaxG], M[kMaxG], l[kMaxG], o[kMaxG][D + 4];
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -110,15 +111,21 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// rows 0..7 of A only, no accumulator yet
+// the same without an accumulator yet
 template <bool BF16>
-__device__ __forceinline__ void mma_first(float (&d)[4], uint32_t a0, uint32_t a2, uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   if (BF16)
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%8,%5,%8}, {%6,%7}, {%9,%9,%9,%9};"
-        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a2), "r"(b0), "r"(b1), "r"(0u), "f"(0.f));
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
   else
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%8,%5,%8}, {%6,%7}, {%9,%9,%9,%9};"
-        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a2), "r"(b0), "r"(b1), "r"(0u), "f"(0.f));
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+// 8 x 8 matrix of 16-bit elements, rows over lanes / 4: its transpose
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
 }
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -246,6 +253,12 @@ __device__ __forceinline__ void touch(const uint8_t* p, int bytes, int lane) {
   if (lane * 128 < bytes) asm volatile("ld.global.ca.u32 %0, [%1];" : "=r"(x) : "l"(p + lane * 128));
 }
 
+__device__ __forceinline__ uint32_t ticket_add(uint32_t* p) {
+  uint32_t x;
+  asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(x) : "l"(p) : "memory");
+  return x;
+}
+
 // What a warp tells its CTA about the range it has done.
 struct WarpInfo {
   int64_t f0, f1;            // empty if equal
@@ -255,8 +268,8 @@ struct WarpInfo {
 };
 
 // ---------------------------------------------------------------------------------------------------------
-// Tensor-core formats: fragments of a warp.  Lane (r = lane / 4, qd = lane % 4).  Logits: query r, tokens 8 n + 2 qd,
-// + 1 of the n-th group of 8 tokens.  Accumulators o: channels by r (and by tile), queries 2 qd, 2 qd + 1.
+// Tensor-core formats: fragments of a warp.  Lane (r = lane / 4, qd = lane % 4).  Logits and accumulators have the
+// lane's queries 2 qd, 2 qd + 1 in register pairs: logits of tokens 8 n + r of the step, accumulators of channels by r.
 template <int FMT>
 __device__ __forceinline__ float finish(float m, float M, float l);
 
@@ -270,13 +283,13 @@ struct MmaState {
   static constexpr int OT = D / 16;
   static constexpr int WIDTH = PLAIN ? 1 : INT4 ? 4 : 2;     // consecutive channels that a lane holds
 
-  uint32_t q[NG][4];         // A fragments, rows 0..7: (a0, a2) of the two k16 instructions of a block
-  float rs;                  // base-2 logit per unit of the q k product
-  float m, M, l;             // of query r; l: complete after end()
-  f32x2 l2;                  // sum over this lane's tokens, even and odd ones
+  uint32_t q[NG][4];         // B fragments of the two k16 instructions of a block: query r
+  f32x2 rs;                  // base-2 logit per unit of the q k product
+  float m[2], M[2];          // running maxima in use
+  f32x2 l;                   // of this lane's tokens until end()
   float o[OT][4];
 
-  // the unit's queries as A fragments; qg: its first query row
+  // the unit's queries as B fragments; qg: its first query row
   __device__ __forceinline__ void begin(const void* qg_, int G, float scale_log2, int lane) {
     const __nv_bfloat16* qr = (const __nv_bfloat16*)qg_ + (lane >> 2) * D;
     const int qd = lane & 3;
@@ -286,7 +299,7 @@ struct MmaState {
       for (int g = 0; g < NG; ++g)
 #pragma unroll
         for (int i = 0; i < 4; ++i) q[g][i] = on ? *(const uint32_t*)(qr + 32 * g + 8 * i + 2 * qd) : 0u;
-      rs = scale_log2;
+      rs = two(scale_log2, scale_log2);
     } else {
       uint32_t w[NG][4];                        // the lane's channels as bf16 pairs
 #pragma unroll
@@ -300,19 +313,18 @@ struct MmaState {
           w[g][0] = x.x; w[g][1] = x.y; w[g][2] = y.x; w[g][3] = y.y;
         }
       }
-      uint32_t t = 0;
+      uint32_t t = 0;                           // largest magnitude's bits (as numbers: NaN counts as none)
 #pragma unroll
       for (int g = 0; g < NG; ++g)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) t = __vmaxu2(t, w[g][i] & 0x7fff7fffu);
+        for (int i = 0; i < 4; ++i) t = max_bf16x2(t, w[g][i] & 0x7fff7fffu);
       t = max(t & 0xffffu, t >> 16);
       t = max(t, __shfl_xor_sync(0xffffffffu, t, 1));
       t = max(t, __shfl_xor_sync(0xffffffffu, t, 2));
       // the row's largest channel goes to [2^14, 2^15)
       const int k = min(141 - (int)(t >> 7), 100);
-      const float up = pow2i(k);
-      rs = scale_log2 * pow2i(-k);
-      if (INT4) rs *= 512.f;                    // codes are n * 2^-9
+      const float up = pow2i(k), down = scale_log2 * pow2i(-k) * (INT4 ? 512.f : 1.f);       // 4-bit codes are n * 2^-9
+      rs = two(__shfl_sync(0xffffffffu, down, 8 * qd), __shfl_sync(0xffffffffu, down, 8 * qd + 4));
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
         if constexpr (INT4) {                   // the codes of a word pair up as channels (0,4) (1,5) | (2,6) (3,7)
@@ -328,202 +340,201 @@ struct MmaState {
         }
       }
     }
-    m = M = -INFINITY;
-    l2 = 0;
+    m[0] = m[1] = M[0] = M[1] = -INFINITY;
+    l = 0;
 #pragma unroll
     for (int t = 0; t < OT; ++t) o[t][0] = o[t][1] = o[t][2] = o[t][3] = 0.f;
   }
 
-  // bf16 scales of tokens 8n + 2qd (first NG / 2 words) and 8n + 2qd + 1
-  static __device__ __forceinline__ void load_scales(uint32_t base, int n, int qd, uint32_t (&sc)[NG]) {
-    const uint32_t a = base + (8 * n + 2 * qd) * S::SB;
+  // bf16 scales of a token: NG / 2 words
+  static __device__ __forceinline__ void load_scales(uint32_t a, uint32_t (&sc)[NG / 2]) {
     if constexpr (NG == 4)
-      asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(sc[0]), "=r"(sc[1]), "=r"(sc[2]), "=r"(sc[3]) : "r"(a));
-    else
       asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(sc[0]), "=r"(sc[1]) : "r"(a));
+    else
+      asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sc[0]) : "r"(a));
   }
-  // scale of group g of the i-th of the two tokens
-  static __device__ __forceinline__ float scale_of(const uint32_t (&sc)[NG], int i, int g) {
-    const uint32_t w = sc[i * (NG / 2) + (g >> 1)];
-    return (g & 1) ? bf16hi(w) : bf16lo(w);
+  static __device__ __forceinline__ f32x2 scale_of(const uint32_t (&sc)[NG / 2], int g) {
+    const float s = (g & 1) ? bf16hi(sc[g >> 1]) : bf16lo(sc[g >> 1]);
+    return two(s, s);
+  }
+  static __device__ __forceinline__ uint32_t load_byte(uint32_t a) {
+    uint32_t x;
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(x) : "r"(a));
+    return x;
   }
 
   // one step: keys at sb, values at sb + HALF, scales behind; ntok of its tokens count
   __device__ __forceinline__ void step(uint32_t sb, int ntok, int lane) {
-    const int qd = lane & 3, mi = lane >> 3, tr = lane & 7;
-    const uint32_t ks = sb + 2 * S::HALF, vs = ks + S::ST * S::SB;
-    f32x2 x[NT];                                // the lane's two tokens of each group
-    // ---- logits
-    if constexpr (PLAIN) {
-      const int off = (tr + 8 * (mi >> 1)) * S::RB + (((mi & 1) ^ tr) << 4);
+    const int r = lane >> 2, mi = lane >> 3, tr = lane & 7;
+    const uint32_t ks = sb + 2 * S::HALF + r * S::SB, vs = ks + S::ST * S::SB;     // scales of token r
+    f32x2 x[NT];
+    // ---- logits, 16 tokens at a time
 #pragma unroll
-      for (int n = 0; n < NT; n += 2) {
-        float c[4][4];                          // even and odd channel groups in chains of their own
-#pragma unroll
-        for (int s = 0; s < D / 16; ++s) {
-          const uint32_t a0 = q[s >> 1][2 * (s & 1)], a2 = q[s >> 1][2 * (s & 1) + 1];
-          uint32_t k[4];
-          ldsm4(sb + n * 8 * S::RB + (off ^ (s << 5)), k);
-          if (s < 2) {
-            mma_first<true>(c[s], a0, a2, k[0], k[1]);
-            mma_first<true>(c[2 + s], a0, a2, k[2], k[3]);
-          } else {
-            mma<true>(c[s & 1], a0, 0u, a2, 0u, k[0], k[1]);
-            mma<true>(c[2 + (s & 1)], a0, 0u, a2, 0u, k[2], k[3]);
-          }
-        }
-        x[n] = mul2(add2(two(c[0][0], c[0][1]), two(c[1][0], c[1][1])), two(rs, rs));
-        x[n + 1] = mul2(add2(two(c[2][0], c[2][1]), two(c[3][0], c[3][1])), two(rs, rs));
-      }
-    } else if constexpr (!INT4) {
-      const int off = S::RB == 128 ? tr * 128 + ((mi ^ tr) << 4) : tr * 64 + ((mi ^ (tr >> 1)) << 4);
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
+    for (int n = 0; n < NT; n += 2) {
+      if constexpr (PLAIN) {
+        const int off = (tr + 8 * (mi >> 1)) * S::RB + (((mi & 1) ^ tr) << 4);
         float c[2][4];                          // two chains
 #pragma unroll
-        for (int i = 0; i < NG / 2; ++i) {
+        for (int s = 0; s < D / 16; ++s) {
+          const uint32_t b0 = q[s >> 1][2 * (s & 1)], b1 = q[s >> 1][2 * (s & 1) + 1];
           uint32_t k[4];
+          ldsm4(sb + n * 8 * S::RB + (off ^ (s << 5)), k);
+          if (s < 2) mma_first<true>(c[s], k[0], k[2], k[1], k[3], b0, b1);
+          else mma<true>(c[s & 1], k[0], k[2], k[1], k[3], b0, b1);
+        }
+        x[n] = mul2(add2(two(c[0][0], c[0][1]), two(c[1][0], c[1][1])), rs);
+        x[n + 1] = mul2(add2(two(c[0][2], c[0][3]), two(c[1][2], c[1][3])), rs);
+      } else if constexpr (!INT4) {
+        const int off = S::RB == 128 ? tr * 128 + ((mi ^ tr) << 4) : tr * 64 + ((mi ^ (tr >> 1)) << 4);
+        float c[2][4];
+#pragma unroll
+        for (int i = 0; i < NG / 2; ++i) {
+          uint32_t k[4], k8[4];                 // tokens r and r + 8; a word: channels 4qd .. 4qd + 3 of 16
           ldsm4(sb + n * 8 * S::RB + (off ^ (i << 6)), k);
+          ldsm4(sb + (n + 1) * 8 * S::RB + (off ^ (i << 6)), k8);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {         // a word: channels 4qd .. 4qd + 3 of 16
-            const uint32_t a0 = q[2 * i + (j >> 1)][2 * (j & 1)], a2 = q[2 * i + (j >> 1)][2 * (j & 1) + 1];
-            if (i == 0 && j < 2) mma_first<false>(c[j], a0, a2, e4m3_lo_to_f16x2(k[j]), e4m3_hi_to_f16x2(k[j]));
-            else mma<false>(c[j & 1], a0, 0u, a2, 0u, e4m3_lo_to_f16x2(k[j]), e4m3_hi_to_f16x2(k[j]));
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t b0 = q[2 * i + (j >> 1)][2 * (j & 1)], b1 = q[2 * i + (j >> 1)][2 * (j & 1) + 1];
+            const uint32_t a0 = e4m3_lo_to_f16x2(k[j]), a1 = e4m3_lo_to_f16x2(k8[j]), a2 = e4m3_hi_to_f16x2(k[j]), a3 = e4m3_hi_to_f16x2(k8[j]);
+            if (i == 0 && j < 2) mma_first<false>(c[j], a0, a1, a2, a3, b0, b1);
+            else mma<false>(c[j & 1], a0, a1, a2, a3, b0, b1);
           }
         }
-        uint32_t sc;
-        asm volatile("ld.shared.u16 %0, [%1];" : "=r"(sc) : "r"(ks + 8 * n + 2 * qd));
-        const f32x2 f = mul2(two(__uint_as_float((sc & 0xffu) << 23), __uint_as_float((sc >> 8) << 23)), two(rs, rs));
-        x[n] = mul2(add2(two(c[0][0], c[0][1]), two(c[1][0], c[1][1])), f);
-      }
-    } else {
-      const int off = S::RB == 64 ? tr * 64 + ((mi ^ (tr >> 1)) << 4) : (tr + 8 * (mi >> 1)) * 32 + (((mi & 1) ^ (tr >> 2)) << 4);
-      constexpr int PER = 4 / NG;               // token groups per ldmatrix
-#pragma unroll
-      for (int n0 = 0; n0 < NT; n0 += PER) {
-        uint32_t k[4];
-        ldsm4(sb + n0 * 8 * S::RB + off, k);
-#pragma unroll
-        for (int p = 0; p < PER; ++p) {
-          const int n = n0 + p;
-          uint32_t sc[NG];
-          load_scales(ks, n, qd, sc);
-          f32x2 y = 0;
-#pragma unroll
-          for (int g = 0; g < NG; ++g) {
-            const uint32_t w = k[p * NG + g];
-            const uint32_t w8 = w >> 8;
-            float c[4];
-            mma_first<false>(c, q[g][0], q[g][1], int4_lo_to_f16x2(w), int4_hi_to_f16x2(w));
-            mma<false>(c, q[g][2], 0u, q[g][3], 0u, int4_lo_to_f16x2(w8), int4_hi_to_f16x2(w8));
-            y = fma2(two(c[0], c[1]), two(scale_of(sc, 0, g), scale_of(sc, 1, g)), y);
-          }
-          x[n] = mul2(y, two(rs, rs));
+        const float s0 = __uint_as_float(load_byte(ks + 8 * n) << 23), s1 = __uint_as_float(load_byte(ks + 8 * n + 8) << 23);
+        x[n] = mul2(add2(two(c[0][0], c[0][1]), two(c[1][0], c[1][1])), mul2(rs, two(s0, s0)));
+        x[n + 1] = mul2(add2(two(c[0][2], c[0][3]), two(c[1][2], c[1][3])), mul2(rs, two(s1, s1)));
+      } else {
+        uint32_t k[NG], k8[NG], s0[NG / 2], s1[NG / 2];      // tokens r and r + 8; a word: channels 8qd .. 8qd + 7 of 32
+        if constexpr (NG == 4) {
+          const int off = tr * 64 + ((mi ^ (tr >> 1)) << 4);
+          ldsm4(sb + n * 8 * S::RB + off, k);
+          ldsm4(sb + (n + 1) * 8 * S::RB + off, k8);
+        } else {
+          uint32_t t[4];
+          ldsm4(sb + n * 8 * S::RB + (tr + 8 * (mi >> 1)) * 32 + (((mi & 1) ^ (tr >> 2)) << 4), t);
+          k[0] = t[0]; k[1] = t[1]; k8[0] = t[2]; k8[1] = t[3];
         }
+        load_scales(ks + 8 * n * S::SB, s0);
+        load_scales(ks + (8 * n + 8) * S::SB, s1);
+        f32x2 y0 = 0, y1 = 0;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          const uint32_t a = k[g], b = k8[g], ah = a >> 8, bh = b >> 8;
+          float c[4];
+          mma_first<false>(c, int4_lo_to_f16x2(a), int4_lo_to_f16x2(b), int4_hi_to_f16x2(a), int4_hi_to_f16x2(b), q[g][0], q[g][1]);
+          mma<false>(c, int4_lo_to_f16x2(ah), int4_lo_to_f16x2(bh), int4_hi_to_f16x2(ah), int4_hi_to_f16x2(bh), q[g][2], q[g][3]);
+          y0 = fma2(two(c[0], c[1]), scale_of(s0, g), y0);
+          y1 = fma2(two(c[2], c[3]), scale_of(s1, g), y1);
+        }
+        x[n] = mul2(y0, rs);
+        x[n + 1] = mul2(y1, rs);
       }
     }
     if (ntok < S::ST) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        float a, b;
-        split(x[n], a, b);
-        if (8 * n + 2 * qd >= ntok) a = -INFINITY;
-        if (8 * n + 2 * qd + 1 >= ntok) b = -INFINITY;
-        x[n] = two(a, b);
-      }
+      for (int n = 0; n < NT; ++n)
+        if (8 * n + r >= ntok) x[n] = two(-INFINITY, -INFINITY);
     }
-    // ---- running maxima of the logits and of logit + log2 of the value's scale.  For 4-bit rows the latter only has to
-    // keep weights within f16: it is the largest scale's bits read as a piecewise linear logarithm (low by < 0.09),
-    // 65536 + 127 too large until the end, which leaves it 7 fraction bits
-    f32x2 es[NT];
-    float mx = -INFINITY, Mx = -INFINITY;
+    // ---- maxima of the logits and of logit + log2 of the value's scale.  For 4-bit rows the latter only has to keep
+    // weights within f16: it is the largest scale's bits read as a piecewise linear logarithm (low by < 0.09), 65536 +
+    // 127 too large until the end, which leaves it 7 fraction bits
+    f32x2 es[PLAIN || INT4 ? 1 : NT];
+    float mx[2] = {-INFINITY, -INFINITY}, Mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       float a, b;
       split(x[n], a, b);
-      mx = fmaxf(mx, fmaxf(a, b));
-      if constexpr (INT4) {
-        uint32_t sc[NG], t[2];
-        load_scales(vs, n, qd, sc);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          t[i] = sc[i * (NG / 2)];
-          if (NG == 4) t[i] = max_bf16x2(t[i], sc[i * (NG / 2) + NG / 2 - 1]);
-          t[i] = max_bf16x2(t[i], __byte_perm(t[i], 0u, 0x1032));
-          t[i] = __byte_perm(t[i], 0x4b000000u, 0x7410);     // as a float: 2^23 + bits
-        }
-        es[n] = fma2(two(__uint_as_float(t[0]), __uint_as_float(t[1])), two(0.0078125f, 0.0078125f), x[n]);
-      } else if constexpr (!PLAIN) {
-        uint32_t sc;
-        asm volatile("ld.shared.u16 %0, [%1];" : "=r"(sc) : "r"(vs + 8 * n + 2 * qd));
-        es[n] = add2(x[n], add2(two(magic(sc & 0xffu), magic(sc >> 8)), two(-8388735.f, -8388735.f)));
-      }
+      mx[0] = fmaxf(mx[0], a);
+      mx[1] = fmaxf(mx[1], b);
       if constexpr (!PLAIN) {
-        split(es[n], a, b);
-        Mx = fmaxf(Mx, fmaxf(a, b));
+        f32x2 e;
+        if constexpr (INT4) {
+          uint32_t sc[NG / 2], t;
+          load_scales(vs + 8 * n * S::SB, sc);
+          t = NG == 4 ? max_bf16x2(sc[0], sc[NG / 2 - 1]) : sc[0];
+          t = max_bf16x2(t, __byte_perm(t, 0u, 0x1032));
+          const float f = __uint_as_float(__byte_perm(t, 0x4b000000u, 0x7410));    // 2^23 + bits
+          e = fma2(two(f, f), two(0.0078125f, 0.0078125f), x[n]);
+        } else {
+          const float f = magic(load_byte(vs + 8 * n)) - 8388735.f;
+          e = es[n] = add2(x[n], two(f, f));
+        }
+        split(e, a, b);
+        Mx[0] = fmaxf(Mx[0], a);
+        Mx[1] = fmaxf(Mx[1], b);
       }
     }
-    if constexpr (INT4) Mx -= 65663.f;
-    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-    if constexpr (PLAIN) Mx = mx;
-    else {
-      Mx = fmaxf(Mx, __shfl_xor_sync(0xffffffffu, Mx, 1));
-      Mx = fmaxf(Mx, __shfl_xor_sync(0xffffffffu, Mx, 2));
-      if (INT4) Mx = fmaxf(Mx, mx - 100.f);     // scales below 2^-100: the weight's other factor stays finite
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (PLAIN) Mx[i] = mx[i];
+      if (INT4) Mx[i] = fmaxf(Mx[i] - 65663.f, mx[i] - 100.f);       // (scales below 2^-100: the weight's other factor stays finite)
     }
-    // the maxima in use move only when one is exceeded 2^8 times: weights then stay below 2^15 (2^8 in fp32)
-    if (__any_sync(0xffffffffu, mx > m + kSlack || Mx > M + kSlack)) {
-      const float mn = fmaxf(m, mx), Mn = fmaxf(M, Mx);
-      const float ml = m == -INFINITY ? 0.f : ex2(m - mn);
-      l2 = mul2(l2, two(ml, ml));
-      const float sc = M == -INFINITY ? 0.f : ex2(M - Mn);
-      m = mn;
-      M = Mn;
-      const f32x2 s01 = two(__shfl_sync(0xffffffffu, sc, 8 * qd), __shfl_sync(0xffffffffu, sc, 8 * qd + 4));
+    // the maxima in use move only when a token exceeds one 2^8 times: weights then stay below 2^15 (2^8 in fp32)
+    if (__any_sync(0xffffffffu, mx[0] > m[0] + kSlack || mx[1] > m[1] + kSlack || Mx[0] > M[0] + kSlack || Mx[1] > M[1] + kSlack)) {
+      float sm[2], sM[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int k = 4; k < 32; k <<= 1) {
+          mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], k));
+          if (!PLAIN) Mx[i] = fmaxf(Mx[i], __shfl_xor_sync(0xffffffffu, Mx[i], k));
+        }
+        if (PLAIN) Mx[i] = mx[i];
+        mx[i] = fmaxf(m[i], mx[i]);
+        Mx[i] = fmaxf(M[i], Mx[i]);
+        sm[i] = m[i] == -INFINITY ? 0.f : ex2(m[i] - mx[i]);
+        sM[i] = M[i] == -INFINITY ? 0.f : ex2(M[i] - Mx[i]);
+        m[i] = mx[i];
+        M[i] = Mx[i];
+      }
+      l = mul2(l, two(sm[0], sm[1]));
+      const f32x2 s01 = two(sM[0], sM[1]);
 #pragma unroll
       for (int t = 0; t < OT; ++t) {
         split(mul2(two(o[t][0], o[t][1]), s01), o[t][0], o[t][1]);
         split(mul2(two(o[t][2], o[t][3]), s01), o[t][2], o[t][3]);
       }
     }
-    const float mr = m == -INFINITY ? 0.f : m, Mr = M == -INFINITY ? 0.f : M - kTop;
+    // (a query that no token had a weight for yet has no maximum to subtract)
+    const f32x2 mr = two(m[0] == -INFINITY ? 0.f : -m[0], m[1] == -INFINITY ? 0.f : -m[1]);
+    const f32x2 Mr = two(M[0] == -INFINITY ? 0.f : kTop - M[0], M[1] == -INFINITY ? 0.f : kTop - M[1]);
     // ---- weights and V p, 16 tokens at a time
 #pragma unroll
     for (int kk = 0; kk < NT / 2; ++kk) {
       const uint32_t vb = sb + S::HALF + kk * 16 * S::RB;
-      const int r = ((mi & 1) << 3) + tr;
+      const int vr = ((mi & 1) << 3) + tr;
       float w[2][2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        float a, b;
-        split(add2(x[2 * kk + j], two(-mr, -mr)), a, b);
-        a = ex2(a);
-        b = ex2(b);
-        l2 = add2(l2, two(a, b));
+        split(add2(x[2 * kk + j], mr), w[j][0], w[j][1]);
+        w[j][0] = ex2(w[j][0]);
+        w[j][1] = ex2(w[j][1]);
+        l = add2(l, two(w[j][0], w[j][1]));
         if constexpr (!PLAIN) {
-          split(add2(INT4 ? x[2 * kk + j] : es[2 * kk + j], two(-Mr, -Mr)), a, b);
-          a = ex2(a);
-          b = ex2(b);
+          split(add2(INT4 ? x[2 * kk + j] : es[INT4 ? 0 : 2 * kk + j], Mr), w[j][0], w[j][1]);
+          w[j][0] = ex2(w[j][0]);
+          w[j][1] = ex2(w[j][1]);
         }
-        w[j][0] = a;
-        w[j][1] = b;
       }
       if constexpr (PLAIN) {
-        const uint32_t h0 = pack_bf16(w[0][0], w[0][1]), h1 = pack_bf16(w[1][0], w[1][1]);
-        const uint32_t l0 = pack_bf16(w[0][0] - bf16lo(h0), w[0][1] - bf16hi(h0));
-        const uint32_t l1 = pack_bf16(w[1][0] - bf16lo(h1), w[1][1] - bf16hi(h1));
-        const int off = r * S::RB + (((mi >> 1) ^ tr) << 4);
+        uint32_t hi[2], lo[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          hi[j] = pack_bf16(w[j][0], w[j][1]);
+          lo[j] = transpose8(pack_bf16(w[j][0] - bf16lo(hi[j]), w[j][1] - bf16hi(hi[j])));
+          hi[j] = transpose8(hi[j]);
+        }
+        const int off = vr * S::RB + (((mi >> 1) ^ tr) << 4);
 #pragma unroll
         for (int t = 0; t < OT; ++t) {
           uint32_t v[4];
           ldsm4t(vb + (off ^ (t << 5)), v);
-          mma<true>(o[t], v[0], v[2], v[1], v[3], h0, h1);
-          mma<true>(o[t], v[0], v[2], v[1], v[3], l0, l1);
+          mma<true>(o[t], v[0], v[2], v[1], v[3], hi[0], hi[1]);
+          mma<true>(o[t], v[0], v[2], v[1], v[3], lo[0], lo[1]);
         }
       } else if constexpr (!INT4) {
-        const uint32_t b0 = pack_f16(w[0][0], w[0][1]), b1 = pack_f16(w[1][0], w[1][1]);
-        const int off = S::RB == 128 ? r * 128 + (((mi >> 1) ^ tr) << 4) : r * 64 + (((mi >> 1) ^ (tr >> 1)) << 4);
+        const uint32_t b0 = transpose8(pack_f16(w[0][0], w[0][1])), b1 = transpose8(pack_f16(w[1][0], w[1][1]));
+        const int off = S::RB == 128 ? vr * 128 + (((mi >> 1) ^ tr) << 4) : vr * 64 + (((mi >> 1) ^ (tr >> 1)) << 4);
 #pragma unroll
         for (int i = 0; i < OT / 2; ++i) {
           uint32_t v[4];
@@ -535,10 +546,10 @@ struct MmaState {
           }
         }
       } else {
-        uint32_t s0[NG], s1[NG];
-        load_scales(vs, 2 * kk, qd, s0);
-        load_scales(vs, 2 * kk + 1, qd, s1);
-        const int off = S::RB == 64 ? r * 64 + (((mi >> 1) ^ (tr >> 1)) << 4) : r * 32 + (((mi >> 1) ^ (tr >> 2)) << 4);
+        uint32_t s0[NG / 2], s1[NG / 2];
+        load_scales(vs + 16 * kk * S::SB, s0);
+        load_scales(vs + (16 * kk + 8) * S::SB, s1);
+        const int off = S::RB == 64 ? vr * 64 + (((mi >> 1) ^ (tr >> 1)) << 4) : vr * 32 + (((mi >> 1) ^ (tr >> 2)) << 4);
 #pragma unroll
         for (int g2 = 0; g2 < NG / 2; ++g2) {
           uint32_t v[4];
@@ -547,11 +558,10 @@ struct MmaState {
           for (int j = 0; j < 2; ++j) {         // a word: channels 4r .. 4r + 3 of token 2qd, the same of token 2qd + 1
             const int g = 2 * g2 + j;
             float f[4];
-            split(mul2(two(w[0][0], w[0][1]), two(scale_of(s0, 0, g), scale_of(s0, 1, g))), f[0], f[1]);
-            split(mul2(two(w[1][0], w[1][1]), two(scale_of(s1, 0, g), scale_of(s1, 1, g))), f[2], f[3]);
-            const uint32_t b0 = pack_f16(f[0], f[1]), b1 = pack_f16(f[2], f[3]);
-            const uint32_t a = v[2 * j], b = v[2 * j + 1];
-            const uint32_t a8 = a >> 8, b8 = b >> 8;
+            split(mul2(two(w[0][0], w[0][1]), scale_of(s0, g)), f[0], f[1]);
+            split(mul2(two(w[1][0], w[1][1]), scale_of(s1, g)), f[2], f[3]);
+            const uint32_t b0 = transpose8(pack_f16(f[0], f[1])), b1 = transpose8(pack_f16(f[2], f[3]));
+            const uint32_t a = v[2 * j], b = v[2 * j + 1], a8 = a >> 8, b8 = b >> 8;
             mma<false>(o[2 * g], int4_lo_to_f16x2(a), int4_hi_to_f16x2(a), int4_lo_to_f16x2(b), int4_hi_to_f16x2(b), b0, b1);
             mma<false>(o[2 * g + 1], int4_lo_to_f16x2(a8), int4_hi_to_f16x2(a8), int4_lo_to_f16x2(b8), int4_hi_to_f16x2(b8), b0, b1);
           }
@@ -570,16 +580,13 @@ struct MmaState {
       if constexpr (PLAIN) {
         a[0] = o[i >> 1][2 * (i & 1)];
         b[0] = o[i >> 1][2 * (i & 1) + 1];
-      } else if constexpr (!INT4) {
-        a[0] = o[i][0]; a[1] = o[i][2];
-        b[0] = o[i][1]; b[1] = o[i][3];
       } else {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          a[2 * h] = o[2 * i + h][0];
-          a[2 * h + 1] = o[2 * i + h][2];
-          b[2 * h] = o[2 * i + h][1];
-          b[2 * h + 1] = o[2 * i + h][3];
+        for (int h = 0; h < WIDTH / 2; ++h) {
+          a[2 * h] = o[i * (WIDTH / 2) + h][0];
+          a[2 * h + 1] = o[i * (WIDTH / 2) + h][2];
+          b[2 * h] = o[i * (WIDTH / 2) + h][1];
+          b[2 * h + 1] = o[i * (WIDTH / 2) + h][3];
         }
       }
       f(8 * WIDTH * i + WIDTH * r, a, b);
@@ -587,24 +594,35 @@ struct MmaState {
   }
   __device__ __forceinline__ void end() {
     float a, b;
-    split(l2, a, b);
-    l = a + b;
-    l += __shfl_xor_sync(0xffffffffu, l, 1);
-    l += __shfl_xor_sync(0xffffffffu, l, 2);
+    split(l, a, b);
+#pragma unroll
+    for (int k = 4; k < 32; k <<= 1) {
+      a += __shfl_xor_sync(0xffffffffu, a, k);
+      b += __shfl_xor_sync(0xffffffffu, b, k);
+    }
+    l = two(a, b);
+  }
+  static __device__ __forceinline__ void put(float* to, const float (&v)[WIDTH]) {
+    if constexpr (WIDTH == 1) *to = v[0];
+    else if constexpr (WIDTH == 2) *(float2*)to = make_float2(v[0], v[1]);
+    else *(float4*)to = make_float4(v[0], v[1], v[2], v[3]);
   }
   __device__ __forceinline__ void store_record(Record<D>* rec, int G, int lane) const {
-    const int r = lane >> 2, q0 = 2 * (lane & 3);
-    if ((lane & 3) == 0 && r < G) {
-      rec->m[r] = m;
-      rec->M[r] = M;
-      rec->l[r] = l;
+    const int q0 = 2 * (lane & 3);
+    float ls[2];
+    split(l, ls[0], ls[1]);
+    if (lane < 4) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (q0 + i < G) {
+          rec->m[q0 + i] = m[i];
+          rec->M[q0 + i] = M[i];
+          rec->l[q0 + i] = ls[i];
+        }
     }
     each(lane, [&](int c, const float (&a)[WIDTH], const float (&b)[WIDTH]) {
-#pragma unroll
-      for (int i = 0; i < WIDTH; ++i) {
-        if (q0 < G) rec->o[q0][c + i] = a[i];
-        if (q0 + 1 < G) rec->o[q0 + 1][c + i] = b[i];
-      }
+      if (q0 < G) put(&rec->o[q0][c], a);
+      if (q0 + 1 < G) put(&rec->o[q0 + 1][c], b);
     });
   }
   __device__ __forceinline__ void store_out(void* out, float* lse, int G, int lane) const;
@@ -632,11 +650,12 @@ __device__ __forceinline__ float log_sum(float m, float l) {
 
 template <int D, int FMT>
 __device__ __forceinline__ void MmaState<D, FMT>::store_out(void* out, float* lse, int G, int lane) const {
-  const int r = lane >> 2, qd = lane & 3, q0 = 2 * qd;
-  const float fr = finish<FMT>(m, M, l);
-  const float f0 = __shfl_sync(0xffffffffu, fr, 8 * qd), f1 = __shfl_sync(0xffffffffu, fr, 8 * qd + 4);
+  const int q0 = 2 * (lane & 3);
+  float ls[2];
+  split(l, ls[0], ls[1]);
+  const float f0 = finish<FMT>(m[0], M[0], ls[0]), f1 = finish<FMT>(m[1], M[1], ls[1]);
   __nv_bfloat16* const po = (__nv_bfloat16*)out + q0 * D;
-  auto put = [&](__nv_bfloat16* to, const float (&v)[WIDTH], float f) {
+  auto write = [&](__nv_bfloat16* to, const float (&v)[WIDTH], float f) {
     if constexpr (WIDTH == 1) {
       *to = __float2bfloat16_rn(f == 0.f ? 0.f : v[0] * f);
     } else {
@@ -648,10 +667,14 @@ __device__ __forceinline__ void MmaState<D, FMT>::store_out(void* out, float* ls
     }
   };
   each(lane, [&](int c, const float (&a)[WIDTH], const float (&b)[WIDTH]) {
-    if (q0 < G) put(po + c, a, f0);
-    if (q0 + 1 < G) put(po + D + c, b, f1);
+    if (q0 < G) write(po + c, a, f0);
+    if (q0 + 1 < G) write(po + D + c, b, f1);
   });
-  if (lse && qd == 0 && r < G) lse[r] = log_sum(m, l);
+  if (lse && lane < 4) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (q0 + i < G) lse[q0 + i] = log_sum(m[i], ls[i]);
+  }
 }
 
 // ---------------------------------------------------------------------------------------------------------
@@ -1107,13 +1130,13 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
 #pragma unroll 4
         for (int i = 0; i < n; ++i) {
           const float w = weight[i * kMaxG + g];
-          const float4 x = *(const float4*)(&rec(i)->o[0][0] + e);
+          const float4 x = *(const float4*)&rec(i)->o[g][e % D];
           a.x = fmaf(w, x.x, a.x);
           a.y = fmaf(w, x.y, a.y);
           a.z = fmaf(w, x.z, a.z);
           a.w = fmaf(w, x.w, a.w);
         }
-        if (open) *(float4*)(&to->o[0][0] + e) = a;
+        if (open) *(float4*)&to->o[g][e % D] = a;
         else put4<EO>((uint8_t*)p.out + (row * D + e) * EO, a, fg);
       }
     }
@@ -1124,7 +1147,6 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
   const WarpInfo& wb = sh.info[last_warp];
   const bool before = wa.first_us < F0, after = wb.last_us >= F0 && wb.last_ue > F1;
   if (!before && !after) return;
-  __threadfence();
   __syncthreads();
   if (tid < 2) {
     bool all = false;
@@ -1133,7 +1155,8 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
       uint32_t* const ticket = p.counters + (tid == 0 ? wa.first_unit : wb.last_unit);
       // CTAs without tiles (fewer tiles than CTAs) take no part
       const int n = total < grid ? (int)(te - ts) : split_owner(total, grid, te - 1) - split_owner(total, grid, ts) + 1;
-      all = atomicAdd(ticket, 1u) == (unsigned)(n - 1);
+      // after the barrier the whole CTA's states are ordered before this thread's release
+      all = ticket_add(ticket) == (unsigned)(n - 1);
       if (all) *ticket = 0u;                    // ready for the next call
     }
     sh.arrived[tid] = all;
@@ -1142,7 +1165,6 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
 #pragma unroll 1
   for (int k = 0; k < 2; ++k) {
     if (!sh.arrived[k]) continue;
-    __threadfence();
     const int64_t ts = k == 0 ? wa.first_us : wb.last_us, te = k == 0 ? wa.first_ue : wb.last_ue;
     const int c0 = split_owner(total, grid, ts);
     const int n = total < grid ? (int)(te - ts) : split_owner(total, grid, te - 1) - c0 + 1;
@@ -1155,12 +1177,17 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
       const int g = on ? e / D : 0;
       float4* const st = (float4*)(smem + warp * S::RING) + (lane / LPG) * kSMs;      // m, M, l, record of contributor i
       float m = -INFINITY, M = -INFINITY, l = 0.f;
+      // the unit began in the first contributor (its record 1); for all others it is the unit that they began with
+      auto record = [&](int i) { return 2 * (total < grid ? split_owner(total, grid, ts + i) : c0 + i) + (i == 0); };
+      constexpr int AHEAD = 6;                  // states whose accumulators come while the statistics are made
+      float4 y[AHEAD];
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i)
+        if (on && i < n) y[i] = __ldcg((const float4*)&records[record(i)].o[g][e % D]);
 #pragma unroll 1
       for (int i = lane % LPG; i < n; i += LPG) {
-        // the unit began in the first contributor (its record 1); for all others it is the unit that they began with
-        const int ri = 2 * (total < grid ? split_owner(total, grid, ts + i) : c0 + i) + (i == 0);
-        const Record<D>* const r = records + ri;
-        const float4 x = make_float4(__ldcg(&r->m[g]), __ldcg(&r->M[g]), __ldcg(&r->l[g]), __int_as_float(ri));
+        const Record<D>* const r = records + record(i);
+        const float4 x = make_float4(__ldcg(&r->m[g]), __ldcg(&r->M[g]), __ldcg(&r->l[g]), 0.f);
         st[i] = x;
         m = fmaxf(m, x.x);
         M = fmaxf(M, x.y);
@@ -1180,18 +1207,19 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
 #pragma unroll
       for (int o = 1; o < LPG; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
       __syncwarp();
-      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
       if (on) {
+        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+        auto add = [&](float w, const float4& v) {
+          a.x = fmaf(w, v.x, a.x);
+          a.y = fmaf(w, v.y, a.y);
+          a.z = fmaf(w, v.z, a.z);
+          a.w = fmaf(w, v.w, a.w);
+        };
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+          if (i < n) add(st[i].y, y[i]);
 #pragma unroll 4
-        for (int i = 0; i < n; ++i) {
-          const float2 x = *(const float2*)&st[i].z;         // (l, record)
-          const float w = st[i].y;
-          const float4 y = __ldcg((const float4*)(&records[__float_as_int(x.y)].o[0][0] + e));
-          a.x = fmaf(w, y.x, a.x);
-          a.y = fmaf(w, y.y, a.y);
-          a.z = fmaf(w, y.z, a.z);
-          a.w = fmaf(w, y.w, a.w);
-        }
+        for (int i = AHEAD; i < n; ++i) add(st[i].y, __ldcg((const float4*)&records[record(i)].o[g][e % D]));
         put4<EO>((uint8_t*)p.out + (row * D + e) * EO, a, finish<FMT>(m, M, l));
         if (p.lse && e % D == 0) p.lse[row + g] = log_sum(m, l);
       }
