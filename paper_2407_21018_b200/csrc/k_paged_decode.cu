@@ -71,7 +71,7 @@ struct Shape {
   static constexpr int RING = STAGES * STAGE;
   static_assert(STAGES >= 2 && WARPS <= kMaxWarps && WARPS >= kMaxG, "ring");
   // a warp's ring takes its partial state and the weights of a join afterwards, or a join's statistics
-  static_assert(RING >= (3 * kMaxG + kMaxG * (D + 4) + kMaxWarps * kMaxG) * 4 && RING >= kSMs * 2 * 16, "ring");
+  static_assert(RING >= (3 * kMaxG + kMaxG * (D + 4) + kMaxWarps * kMaxG) * 4 && RING >= kSMs * 2 * 16 + WARPS * 512, "ring");
 };
 
 // Partial state of one (worker, unit): m[8], M[8], l[8], o[8][D].  m: running maximum of the logits (base 2); M: that
@@ -289,30 +289,39 @@ struct MmaState {
   f32x2 l;                   // of this lane's tokens until end()
   float o[OT][4];
 
-  // the unit's queries as B fragments; qg: its first query row
-  __device__ __forceinline__ void begin(const void* qg_, int G, float scale_log2, int lane) {
-    const __nv_bfloat16* qr = (const __nv_bfloat16*)qg_ + (lane >> 2) * D;
+  // the unit's queries in the order of the fragments, as they lie in memory; qg: its first query row
+  struct Raw { uint32_t w[NG][4]; };
+  static __device__ __forceinline__ void fetch(const void* qg, int G, int lane, Raw& raw) {
+    const __nv_bfloat16* qr = (const __nv_bfloat16*)qg + (lane >> 2) * D;
     const int qd = lane & 3;
     const bool on = (lane >> 2) < G;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      uint32_t (&w)[4] = raw.w[g];
+      if constexpr (PLAIN) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = on ? *(const uint32_t*)(qr + 32 * g + 8 * i + 2 * qd) : 0u;
+      } else if constexpr (INT4) {              // channels 32 g + 8 qd .. + 7
+        const uint4 x = on ? *(const uint4*)(qr + 32 * g + 8 * qd) : make_uint4(0u, 0u, 0u, 0u);
+        w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+      } else {                                  // 32 g + 4 qd .. + 3 and 16 behind
+        const uint2 x = on ? *(const uint2*)(qr + 32 * g + 4 * qd) : make_uint2(0u, 0u);
+        const uint2 y = on ? *(const uint2*)(qr + 32 * g + 16 + 4 * qd) : make_uint2(0u, 0u);
+        w[0] = x.x; w[1] = x.y; w[2] = y.x; w[3] = y.y;
+      }
+    }
+  }
+  // starts a unit: its queries as B fragments, no tokens yet
+  __device__ __forceinline__ void begin(const Raw& raw, float scale_log2, int lane) {
+    const uint32_t (&w)[NG][4] = raw.w;
     if constexpr (PLAIN) {
 #pragma unroll
       for (int g = 0; g < NG; ++g)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[g][i] = on ? *(const uint32_t*)(qr + 32 * g + 8 * i + 2 * qd) : 0u;
+        for (int i = 0; i < 4; ++i) q[g][i] = w[g][i];
       rs = two(scale_log2, scale_log2);
     } else {
-      uint32_t w[NG][4];                        // the lane's channels as bf16 pairs
-#pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        if constexpr (INT4) {                   // 32 g + 8 qd .. + 7
-          const uint4 x = on ? *(const uint4*)(qr + 32 * g + 8 * qd) : make_uint4(0u, 0u, 0u, 0u);
-          w[g][0] = x.x; w[g][1] = x.y; w[g][2] = x.z; w[g][3] = x.w;
-        } else {                                // 32 g + 4 qd .. + 3 and 16 behind
-          const uint2 x = on ? *(const uint2*)(qr + 32 * g + 4 * qd) : make_uint2(0u, 0u);
-          const uint2 y = on ? *(const uint2*)(qr + 32 * g + 16 + 4 * qd) : make_uint2(0u, 0u);
-          w[g][0] = x.x; w[g][1] = x.y; w[g][2] = y.x; w[g][3] = y.y;
-        }
-      }
+      const int qd = lane & 3;
       uint32_t t = 0;                           // largest magnitude's bits (as numbers: NaN counts as none)
 #pragma unroll
       for (int g = 0; g < NG; ++g)
@@ -695,12 +704,19 @@ struct F32State {
 
   static __device__ __forceinline__ int owner(int lane) { return (lane >> (5 - LB)) * R; }
 
-  __device__ __forceinline__ void begin(const void* qg, int G, float scale_log2, int lane) {
+  struct Raw { float q[GP][N]; };
+  static __device__ __forceinline__ void fetch(const void* qg, int G, int lane, Raw& raw) {
+#pragma unroll
+    for (int g = 0; g < GP; ++g)
+#pragma unroll
+      for (int i = 0; i < N; ++i) raw.q[g][i] = g < G ? ((const float*)qg)[g * D + lane * N + i] : 0.f;
+  }
+  __device__ __forceinline__ void begin(const Raw& raw, float scale_log2, int lane) {
 #pragma unroll
     for (int g = 0; g < GP; ++g)
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        q[g][i] = g < G ? ((const float*)qg)[g * D + lane * N + i] * scale_log2 : 0.f;
+        q[g][i] = raw.q[g][i] * scale_log2;
         o[g][i] = 0.f;
       }
     m = -INFINITY;
@@ -920,7 +936,8 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
     const int q_bytes = p.G * D * E;            // queries of a unit, in the order of units
     const int64_t page_bytes = (int64_t)p.g.N_kv * p.g.block_bytes;
     Cursor pc = locate(tab, B, LH, p.g.N_kv, f0);
-    touch((const uint8_t*)p.q + (int64_t)(pc.b * LH + pc.ll * p.g.N_kv + pc.h) * q_bytes, q_bytes, lane);
+    typename State::Raw raw;                    // the first unit's queries, asked for ahead of the pages
+    State::fetch((const uint8_t*)p.q + (int64_t)(pc.b * LH + pc.ll * p.g.N_kv + pc.h) * q_bytes, p.G, lane, raw);
     const int32_t* p_entry = p.table.table + pc.b * p.table.stride + pc.j;       // table entry of the next tile
     int p_page = __ldg(p_entry);                // looked up a tile ahead
     const uint8_t* p_base = p.pages + page_block_offset(p.g, p.layer0 + pc.ll, 0, pc.h);    // of the unit
@@ -1012,7 +1029,8 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
       const int ntok = min(c.len, j1 * kPageTokens) - c.j * kPageTokens;
       const int unit = c.b * LH + c.ll * p.g.N_kv + c.h;
       const int64_t row = (int64_t)unit * p.G;   // first query row
-      st.begin((const uint8_t*)p.q + row * D * E, p.G, p.scale_log2, lane);
+      if (f != f0) State::fetch((const uint8_t*)p.q + row * D * E, p.G, lane, raw);
+      st.begin(raw, p.scale_log2, lane);
       // the next unit's queries come while this one is worked on (it may be one of an empty sequence)
       if (se < f1) touch((const uint8_t*)p.q + (row + p.G) * D * E, q_bytes, lane);
 #pragma unroll 1
@@ -1169,62 +1187,71 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
     const int c0 = split_owner(total, grid, ts);
     const int n = total < grid ? (int)(te - ts) : split_owner(total, grid, te - 1) - c0 + 1;
     const int64_t row = (int64_t)(k == 0 ? wa.first_unit : wb.last_unit) * p.G;
-    // a warp takes 128 accumulators, LPG lanes a query head; the lanes of a head go over the contributors
+    // a warp takes 128 accumulators (four a lane, LPG lanes a query head) of every `slices`-th contributor
     constexpr int LPG = D / 4;
+    const int chunks = (p.G * D + 127) / 128, slices = kWarps / chunks;
+    const int chunk = warp % chunks, slice = warp / chunks;
+    const int e = 128 * chunk + 4 * lane;
+    const bool on = e < p.G * D && slice < slices;
+    const int g = on ? e / D : 0;
+    // the unit began in the first contributor (its record 1); for all others it is the unit that they began with
+    auto record = [&](int i) -> const Record<D>* {
+      return records + 2 * (total < grid ? split_owner(total, grid, ts + i) : c0 + i) + (i == 0);
+    };
+    constexpr int AHEAD = 6;                    // states whose accumulators come while the statistics are made
+    float4 y[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j)
+      if (on && slice + j * slices < n) y[j] = __ldcg((const float4*)&record(slice + j * slices)->o[g][e % D]);
+    float4* const st = (float4*)(smem + warp * S::RING) + (lane / LPG) * kSMs;          // m, M, l of contributor i
+    float m = -INFINITY, M = -INFINITY, l = 0.f;
 #pragma unroll 1
-    for (int e = 128 * warp + 4 * lane; e - 4 * lane < p.G * D; e += 128 * kWarps) {
-      const bool on = e < p.G * D;
-      const int g = on ? e / D : 0;
-      float4* const st = (float4*)(smem + warp * S::RING) + (lane / LPG) * kSMs;      // m, M, l, record of contributor i
-      float m = -INFINITY, M = -INFINITY, l = 0.f;
-      // the unit began in the first contributor (its record 1); for all others it is the unit that they began with
-      auto record = [&](int i) { return 2 * (total < grid ? split_owner(total, grid, ts + i) : c0 + i) + (i == 0); };
-      constexpr int AHEAD = 6;                  // states whose accumulators come while the statistics are made
-      float4 y[AHEAD];
-#pragma unroll
-      for (int i = 0; i < AHEAD; ++i)
-        if (on && i < n) y[i] = __ldcg((const float4*)&records[record(i)].o[g][e % D]);
-#pragma unroll 1
-      for (int i = lane % LPG; i < n; i += LPG) {
-        const Record<D>* const r = records + record(i);
-        const float4 x = make_float4(__ldcg(&r->m[g]), __ldcg(&r->M[g]), __ldcg(&r->l[g]), 0.f);
-        st[i] = x;
-        m = fmaxf(m, x.x);
-        M = fmaxf(M, x.y);
-      }
-#pragma unroll
-      for (int o = 1; o < LPG; o <<= 1) {
-        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-        M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-      }
-      const float ms = m == -INFINITY ? 0.f : m, Ms = M == -INFINITY ? 0.f : M;
-#pragma unroll 1
-      for (int i = lane % LPG; i < n; i += LPG) {
-        const float4 x = st[i];
-        l += x.z * exp2f(x.x - ms);
-        st[i].y = exp2f(x.y - Ms);
-      }
-#pragma unroll
-      for (int o = 1; o < LPG; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-      __syncwarp();
-      if (on) {
-        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-        auto add = [&](float w, const float4& v) {
-          a.x = fmaf(w, v.x, a.x);
-          a.y = fmaf(w, v.y, a.y);
-          a.z = fmaf(w, v.z, a.z);
-          a.w = fmaf(w, v.w, a.w);
-        };
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i)
-          if (i < n) add(st[i].y, y[i]);
-#pragma unroll 4
-        for (int i = AHEAD; i < n; ++i) add(st[i].y, __ldcg((const float4*)&records[record(i)].o[g][e % D]));
-        put4<EO>((uint8_t*)p.out + (row * D + e) * EO, a, finish<FMT>(m, M, l));
-        if (p.lse && e % D == 0) p.lse[row + g] = log_sum(m, l);
-      }
-      __syncwarp();
+    for (int i = lane % LPG; i < n; i += LPG) {
+      const Record<D>* const r = record(i);
+      const float4 x = make_float4(__ldcg(&r->m[g]), __ldcg(&r->M[g]), __ldcg(&r->l[g]), 0.f);
+      st[i] = x;
+      m = fmaxf(m, x.x);
+      M = fmaxf(M, x.y);
     }
+#pragma unroll
+    for (int o = 1; o < LPG; o <<= 1) {
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+      M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+    }
+    const float ms = m == -INFINITY ? 0.f : m, Ms = M == -INFINITY ? 0.f : M;
+#pragma unroll 1
+    for (int i = lane % LPG; i < n; i += LPG) {
+      const float4 x = st[i];
+      l += x.z * exp2f(x.x - ms);
+      st[i].y = exp2f(x.y - Ms);
+    }
+#pragma unroll
+    for (int o = 1; o < LPG; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    __syncwarp();
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](float w, const float4& v) {
+      a.x = fmaf(w, v.x, a.x);
+      a.y = fmaf(w, v.y, a.y);
+      a.z = fmaf(w, v.z, a.z);
+      a.w = fmaf(w, v.w, a.w);
+    };
+    if (on) {
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j)
+        if (slice + j * slices < n) add(st[slice + j * slices].y, y[j]);
+#pragma unroll 4
+      for (int i = slice + AHEAD * slices; i < n; i += slices) add(st[i].y, __ldcg((const float4*)&record(i)->o[g][e % D]));
+    }
+    float4* const part = (float4*)(smem + chunk * S::RING + kSMs * 2 * sizeof(float4));     // [slice][lane]
+    if (slice > 0 && slice < slices) part[slice * 32 + lane] = a;
+    __syncthreads();
+    if (on && slice == 0) {
+#pragma unroll 1
+      for (int s = 1; s < slices; ++s) add(1.f, part[s * 32 + lane]);
+      put4<EO>((uint8_t*)p.out + (row * D + e) * EO, a, finish<FMT>(m, M, l));
+      if (p.lse && e % D == 0) p.lse[row + g] = log_sum(m, l);
+    }
+    __syncthreads();                            // before the other unit's join takes the same memory
   }
 }
 
