@@ -348,21 +348,25 @@ def paged_offset(cfg: PagedConfig, layer: int, page: int, head: int, slot: int, 
     return int(lib.thinK_paged_offset(C.byref(cfg), layer, page, head, slot, part))
 
 
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 class PagedKVCache:
     """Pool of 64-token pages with device-side page tables and lengths: write, read back, one-token attention.
 
     Tables are int32 [B, max_pages] (rows may be strided), lengths, positions and row counts int32 [B], all on the
-    cache's device.  `pages`: an existing pool (uint8, cfg's size) to work on; by default one is allocated."""
+    cache's device.  `pages`: an existing pool (uint8, cfg's size) to work on; by default one is allocated.  Calls
+    run on the device's current stream unless one is given."""
 
     def __init__(self, cfg: PagedConfig, device="cuda", pages: Optional[torch.Tensor] = None):
-        self.cfg = cfg
         self.handle = None
+        self.cfg = cfg
         self.sizes = paged_bytes(cfg)
         device = torch.device(device) if pages is None else pages.device
         if device.type != "cuda":
             raise ThinKError(ERR_INVALID_ARG, "PagedKVCache: device")
         self.device = torch.device("cuda", torch.cuda.current_device() if device.index is None else device.index)
-        self.torch_dtype = torch.bfloat16 if cfg.dtype == BF16 else torch.float32
         if pages is None:
             pages = torch.empty(int(self.sizes.pages), dtype=torch.uint8, device=self.device)
         elif pages.dtype != torch.uint8 or not pages.is_contiguous():
@@ -377,6 +381,15 @@ class PagedKVCache:
             _check(lib.thinK_paged_create(C.byref(cfg), C.byref(have), pages.data_ptr(), self.workspace.data_ptr(),
                                           C.byref(h)), "thinK_paged_create")
         self.handle = h
+        self._remember()
+
+    def _remember(self):
+        """Plain copies of what every call looks at: reading a field of a C structure or a device object costs more
+        host time than the smallest kernels take."""
+        c = self.cfg
+        self.torch_dtype = torch.bfloat16 if c.dtype == BF16 else torch.float32
+        self._index = self.device.index
+        self._L, self._N_q, self._N_kv, self._D, self._max_batch = c.L, c.N_q, c.N_kv, c.D, c.max_batch
 
     def new_scratch(self) -> torch.Tensor:
         """A scratch buffer for attention calls that may run at the same time as others of this cache."""
@@ -384,45 +397,48 @@ class PagedKVCache:
 
     # -- argument marshalling -------------------------------------------
     def _table(self, table: torch.Tensor, B: int, where: str) -> PageTable:
-        if (table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] < B or table.device != self.device
-                or (table.shape[1] > 1 and table.stride(1) != 1)):
+        if table.dtype != torch.int32 or table.dim() != 2 or table.get_device() != self._index:
             raise ThinKError(ERR_INVALID_ARG, where + ": page table")
-        return PageTable(table.data_ptr(), max(table.stride(0), table.shape[1]) if B == 1 else table.stride(0),
-                         table.shape[1], B)
+        rows, width = table.shape
+        stride, step = table.stride()
+        if rows < B or (width > 1 and step != 1):
+            raise ThinKError(ERR_INVALID_ARG, where + ": page table")
+        return PageTable(table.data_ptr(), max(stride, width) if B == 1 else stride, width, B)
 
     def _vector(self, x: Optional[torch.Tensor], B: int, where: str):
         if x is None:
             return None
-        if (x.dtype != torch.int32 or x.dim() != 1 or x.shape[0] < B or x.device != self.device
+        if (x.dtype != torch.int32 or x.dim() != 1 or x.shape[0] < B or x.get_device() != self._index
                 or (B > 1 and x.stride(0) != 1)):
             raise ThinKError(ERR_INVALID_ARG, where)
         return x.data_ptr()
 
-    def _layers(self, layer0: int, nlayers: Optional[int]) -> int:
-        return self.cfg.L - layer0 if nlayers is None else nlayers
+    def _call(self, fn, where: str, *args):
+        """fn(handle, *args) with the cache's device current."""
+        if _current_device() == self._index:
+            status = fn(self.handle, *args)
+        else:
+            with torch.cuda.device(self._index):
+                status = fn(self.handle, *args)
+        if status != THINK_OK:
+            raise ThinKError(status, where)
 
-    def _on(self, call, stream, where: str):
-        """Runs call(stream pointer) with the cache's device current."""
-        if torch.cuda.current_device() == self.device.index:
-            s = torch.cuda.current_stream() if stream is None else stream
-            _check(call(s.cuda_stream), where)
-            return
-        with torch.cuda.device(self.device):
-            s = torch.cuda.current_stream() if stream is None else stream
-            _check(call(s.cuda_stream), where)
+    def _rows_view(self, x: torch.Tensor, n: int, where: str) -> Tensor5:
+        shape, stride = x.shape, x.stride()
+        if (len(shape) != 5 or shape[2] != n or shape[3] != self._N_kv or shape[4] != self._D or stride[4] != 1
+                or x.dtype != self.torch_dtype or x.get_device() != self._index):
+            raise ThinKError(ERR_INVALID_ARG, where + ": rows")
+        return Tensor5(x.data_ptr(), stride[0], stride[1], stride[2], stride[3])
 
     def _rows(self, fn, where, k, v, table, pos, rows, layer0, nlayers, stream):
-        n = self._layers(layer0, nlayers)
-        want = (n, self.cfg.N_kv, self.cfg.D)
-        for x in (k, v):
-            if (x.dim() != 5 or tuple(x.shape[2:]) != want or x.shape[:2] != k.shape[:2] or x.dtype != self.torch_dtype
-                    or x.device != self.device or x.stride(4) != 1):
-                raise ThinKError(ERR_INVALID_ARG, where + ": rows")
-        B, max_rows = k.shape[0], k.shape[1]
-        t = self._table(table, B, where)
-        pp, rp = self._vector(pos, B, where + ": pos"), self._vector(rows, B, where + ": rows")
-        k5, v5 = tensor5(k), tensor5(v)
-        self._on(lambda s: fn(self.handle, k5, v5, t, pp, rp, max_rows, layer0, n, s), stream, where)
+        n = self._L - layer0 if nlayers is None else nlayers
+        k5, v5 = self._rows_view(k, n, where), self._rows_view(v, n, where)
+        B, max_rows = k.shape[:2]
+        if v.shape[:2] != (B, max_rows):
+            raise ThinKError(ERR_INVALID_ARG, where + ": rows")
+        self._call(fn, where, k5, v5, self._table(table, B, where), self._vector(pos, B, where + ": pos"),
+                   self._vector(rows, B, where + ": rows"), max_rows, layer0, n,
+                   _raw_stream(self._index) if stream is None else stream.cuda_stream)
 
     # -- the calls ------------------------------------------------------
     def write(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, pos: Optional[torch.Tensor] = None,
@@ -441,28 +457,31 @@ class PagedKVCache:
         """Attention of one token per sequence, q [B, nlayers, N_q, D], over its first seq_lens[b] tokens.  Returns
         out, or (out, lse) when lse (fp32 [B, nlayers, N_q]) is given or asked for."""
         where = "thinK_paged_decode_attn"
-        n = self._layers(layer0, nlayers)
-        if (q.dim() != 4 or tuple(q.shape[1:]) != (n, self.cfg.N_q, self.cfg.D) or q.dtype != self.torch_dtype
-                or q.device != self.device or not q.is_contiguous()):
+        n = self._L - layer0 if nlayers is None else nlayers
+        shape = q.shape
+        if (len(shape) != 4 or shape[1] != n or shape[2] != self._N_q or shape[3] != self._D
+                or q.dtype != self.torch_dtype or q.get_device() != self._index or not q.is_contiguous()):
             raise ThinKError(ERR_INVALID_ARG, where + ": q")
+        B = shape[0]
         if out is None:
             out = torch.empty_like(q)
-        elif out.shape != q.shape or out.dtype != q.dtype or out.device != q.device or not out.is_contiguous():
+        elif out.shape != shape or out.dtype != q.dtype or out.get_device() != self._index or not out.is_contiguous():
             raise ThinKError(ERR_INVALID_ARG, where + ": out")
-        if lse is None and return_lse:
-            lse = torch.empty(q.shape[:3], dtype=torch.float32, device=self.device)
-        elif lse is not None and (lse.shape != q.shape[:3] or lse.dtype != torch.float32 or lse.device != q.device
-                                  or not lse.is_contiguous()):
-            raise ThinKError(ERR_INVALID_ARG, where + ": lse")
-        if scratch is not None and (scratch.dtype != torch.uint8 or scratch.device != self.device
-                                    or not scratch.is_contiguous()):
-            raise ThinKError(ERR_INVALID_ARG, where + ": scratch")
-        t = self._table(table, q.shape[0], where)
-        lens = self._vector(seq_lens, q.shape[0], where + ": seq_lens")
-        self._on(lambda s: lib.thinK_paged_decode_attn(
-            self.handle, q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(), t, lens,
-            None if scratch is None else scratch.data_ptr(), 0 if scratch is None else scratch.numel(), layer0, n, s),
-            stream, where)
+        if lse is not None:
+            if (lse.shape != shape[:3] or lse.dtype != torch.float32 or lse.get_device() != self._index
+                    or not lse.is_contiguous()):
+                raise ThinKError(ERR_INVALID_ARG, where + ": lse")
+        elif return_lse:
+            lse = q.new_empty(shape[:3], dtype=torch.float32)
+        work, work_bytes = None, 0
+        if scratch is not None:
+            if scratch.dtype != torch.uint8 or scratch.get_device() != self._index or not scratch.is_contiguous():
+                raise ThinKError(ERR_INVALID_ARG, where + ": scratch")
+            work, work_bytes = scratch.data_ptr(), scratch.numel()
+        self._call(lib.thinK_paged_decode_attn, where, q.data_ptr(), out.data_ptr(),
+                   None if lse is None else lse.data_ptr(), self._table(table, B, where),
+                   self._vector(seq_lens, B, where + ": seq_lens"), work, work_bytes, layer0, n,
+                   _raw_stream(self._index) if stream is None else stream.cuda_stream)
         return out if lse is None else (out, lse)
 
     def device_error(self) -> int:

@@ -626,6 +626,11 @@ def test_refusals():
     refused(lambda: c.write(k.cpu(), v, p.table))
     refused(lambda: c.write(k, v, p.table.long()))
     refused(lambda: c.write(k, v, p.table[:1]))
+    refused(lambda: c.write(k, v, p.table[0]))
+    refused(lambda: c.write(k, v, p.table[:1].expand(2, -1)))          # one row for all: its stride is 0
+    refused(lambda: c.write(k[0], v, p.table))
+    refused(lambda: c.write(k, v[0], p.table))
+    refused(lambda: c.decode_attn(q[0], p.table, p.seq))
     refused(lambda: c.write(k, v, p.table.cpu()))
     refused(lambda: c.write(k, v, p.table.t().contiguous().t()))
     refused(lambda: c.write(k, v, p.table, pos=p.seq[:1]))
