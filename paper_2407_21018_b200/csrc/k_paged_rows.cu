@@ -13,7 +13,14 @@
 namespace think {
 namespace {
 
-constexpr int kRowThreads = 256;
+#ifndef THINK_ROWS_U
+#define THINK_ROWS_U 2
+#endif
+#ifndef THINK_ROWS_T
+#define THINK_ROWS_T 128
+#endif
+constexpr int kRowThreads = THINK_ROWS_T;
+constexpr int kRowsPerThread = THINK_ROWS_U;
 
 // largest |x| of 8 bf16 as the integer of its bits: orders finite < infinite < NaN
 __device__ __forceinline__ uint32_t amax_bits(const uint4& w) {
@@ -52,8 +59,11 @@ __device__ __forceinline__ uint2 encode_e4m3(const uint4& w, uint32_t& e, bool& 
 }
 
 // 8 bf16 -> 8 4-bit codes; 4 lanes hold the group of 32 channels.  `sbits` receives the bf16 scale.
-// The quotient is an IEEE division: x and s have 8 significant bits each, so a quotient that is no tie is at least
-// 2^-12 away from one and the fp32 rounding cannot cross it.
+// x / s to the nearest integer, ties to even, without eight divisions: x and s have 8 significant bits, so a quotient
+// that is no tie is at least 1 / 510 away from one.  x * (1 / s) is off by less than 2^-20; rounding it to multiples of
+// 2^-12 first (adding and subtracting 1.5 * 2^11) makes ties exact again and moves nothing else across one.  The
+// second rounding adds 1.5 * 2^23 + 8, which leaves n + 8 in the low bits.  A scale below 2^-126 takes the division:
+// its own rounding error is large there, and n needs its limits.
 __device__ __forceinline__ uint32_t encode_int4(const uint4& w, uint32_t& sbits, bool& bad) {
   const uint32_t top = lane_max<4>(amax_bits(w));
   bad = top >= kInfBits;
@@ -61,15 +71,25 @@ __device__ __forceinline__ uint32_t encode_int4(const uint4& w, uint32_t& sbits,
   sbits = bad ? 0x7fc0u : (uint32_t)__bfloat16_as_ushort(sb);
   const float s = __bfloat162float(sb);
   if (bad || s == 0.f) return 0x88888888u;
-  uint32_t out = 0;
   const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+  uint32_t c[4];                                // two codes each in the low byte
+  if (s >= 1.17549435e-38f) {
+    const float inv = __frcp_rn(s);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float x = (i & 1) ? bf16hi(ws[i >> 1]) : bf16lo(ws[i >> 1]);
-    const int n = max(-7, min(7, __float2int_rn(__fdiv_rn(x, s))));
-    out |= (uint32_t)(n + 8) << (4 * i);
+    for (int i = 0; i < 4; ++i) {
+      const float a = __fadd_rn(__fadd_rn(__fmul_rn(bf16lo(ws[i]), inv), 3072.f), -3072.f);
+      const float b = __fadd_rn(__fadd_rn(__fmul_rn(bf16hi(ws[i]), inv), 3072.f), -3072.f);
+      c[i] = __float_as_uint(__fadd_rn(a, 12582920.f)) + (__float_as_uint(__fadd_rn(b, 12582920.f)) << 4);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int a = max(-7, min(7, __float2int_rn(__fdiv_rn(bf16lo(ws[i]), s))));
+      const int b = max(-7, min(7, __float2int_rn(__fdiv_rn(bf16hi(ws[i]), s))));
+      c[i] = (uint32_t)(a + 8) | (uint32_t)(b + 8) << 4;
+    }
   }
-  return out;
+  return __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
 }
 
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
@@ -82,100 +102,148 @@ __device__ __forceinline__ uint32_t decode_e4m3x2(uint32_t two, float s) {
   return pack2(f.x * s, f.y * s);
 }
 
-// FMT: thinK_page_format.  E: bytes of an element (2 bf16, 4 fp32).
+// 8 4-bit codes times their scale to bf16
+__device__ __forceinline__ uint4 decode_int4(uint32_t w, float f) {
+  auto one = [&](int i) {                       // 2^23 + code, less 2^23 + 8
+    return __fmul_rn(__fadd_rn(__uint_as_float((w >> (4 * i) & 15u) | 0x4b000000u), -8388616.f), f);
+  };
+  return make_uint4(pack2(one(0), one(1)), pack2(one(2), one(3)), pack2(one(4), one(5)), pack2(one(6), one(7)));
+}
+__device__ __forceinline__ uint4 decode_e4m3(const uint2& w, float f) {
+  return make_uint4(decode_e4m3x2(w.x, f), decode_e4m3x2(w.x >> 16, f), decode_e4m3x2(w.y, f), decode_e4m3x2(w.y >> 16, f));
+}
+
+// FMT: thinK_page_format.  E: bytes of an element (2 bf16, 4 fp32).  A block takes kRowsPerThread * kRowThreads / LANES
+// consecutive rows of one entry (head fastest, then layer, then token).
 template <int D, int E, int FMT, bool WRITE>
 __global__ void __launch_bounds__(kRowThreads) k_paged_rows(const PagedRowsParams p) {
   constexpr int LANES = D * E / 16;             // lanes of a row, 16 bytes of elements each
   constexpr int CH = 16 / E;                    // channels of a lane
+  constexpr int RPB = kRowThreads / LANES, U = kRowsPerThread;
   const int b = blockIdx.y;
   const int nrows_raw = p.rows ? __ldg(p.rows + b) : p.max_rows;
+  const int pos = p.pos ? __ldg(p.pos + b) : 0;
   const int nrows = min(nrows_raw, p.max_rows);
   if (blockIdx.x == 0 && threadIdx.x == 0 && nrows_raw > p.max_rows) atomicOr(p.error, kErrPage);
-  if (nrows <= 0) return;
-  const uint32_t r = blockIdx.x * (kRowThreads / LANES) + threadIdx.x / LANES;     // row of the entry, head fastest
-  const uint32_t rl = p.by_heads.div(r), h = r - rl * p.g.N_kv;
-  const uint32_t s = p.by_layers.div(rl), ll = rl - s * p.nlayers;
-  if (blockIdx.x * (kRowThreads / LANES) >= (uint64_t)nrows * p.nlayers * p.g.N_kv) return;   // whole block: no row
-  const bool on = s < (uint32_t)nrows;          // lanes of a row agree; idle rows still take part in the shuffles
+  const uint32_t first = blockIdx.x * (RPB * U);
+  if (nrows <= 0 || first >= (uint64_t)nrows * p.nlayers * p.g.N_kv) return;      // whole block: no row
   const int c = threadIdx.x % LANES;
-  const int64_t tok = (int64_t)(p.pos ? __ldg(p.pos + b) : 0) + s;
-  const int64_t ek = b * p.k.sb + (int64_t)s * p.k.ss + ll * p.k.sl + h * p.k.sn + c * CH;
-  const int64_t ev = b * p.v.sb + (int64_t)s * p.v.ss + ll * p.v.sl + h * p.v.sn + c * CH;
-  uint4* const kx = (uint4*)((uint8_t*)p.k.ptr + ek * E);
-  uint4* const vx = (uint4*)((uint8_t*)p.v.ptr + ev * E);
-  uint4 k = make_uint4(0u, 0u, 0u, 0u), v = k;
-  if (WRITE && on) {
-    k = __ldcs(kx);
-    v = __ldcs(vx);
+  uint4 k[U], v[U];
+  uint4 *kx[U], *vx[U];
+  uint8_t* block[U];
+  int slot[U];
+  bool on[U];                                   // lanes of a row agree; idle rows still take part in the shuffles
+  uint32_t layer[U], head[U];
+  int64_t tok[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const uint32_t r = first + u * RPB + threadIdx.x / LANES;
+    const uint32_t rl = p.by_heads.div(r), h = r - rl * p.g.N_kv;
+    const uint32_t s = p.by_layers.div(rl), ll = rl - s * p.nlayers;
+    on[u] = s < (uint32_t)nrows;
+    layer[u] = ll;
+    head[u] = h;
+    tok[u] = (int64_t)pos + s;
+    kx[u] = (uint4*)((uint8_t*)p.k.ptr + (b * p.k.sb + (int64_t)s * p.k.ss + ll * p.k.sl + h * p.k.sn + c * CH) * E);
+    vx[u] = (uint4*)((uint8_t*)p.v.ptr + (b * p.v.sb + (int64_t)s * p.v.ss + ll * p.v.sl + h * p.v.sn + c * CH) * E);
+    k[u] = v[u] = make_uint4(0u, 0u, 0u, 0u);
+    if (WRITE && on[u]) {
+      k[u] = __ldcs(kx[u]);
+      v[u] = __ldcs(vx[u]);
+    }
   }
-  const int page = on ? page_of(p.table, p.g, b, tok, p.error) : -1;
-  const bool ok = page >= 0;
-  const int slot = (int)(tok & (kPageTokens - 1));
-  uint8_t* const block = p.pages + page_block_offset(p.g, p.layer0 + (int)ll, ok ? page : 0, (int)h);
-  uint8_t* const kc = block + slot * p.g.row_bytes;
-  uint8_t* const vc = kc + kPageTokens * p.g.row_bytes;
-  uint8_t* const ks = block + 2 * kPageTokens * p.g.row_bytes + slot * p.g.scale_bytes;
-  uint8_t* const vs = ks + kPageTokens * p.g.scale_bytes;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int page = on[u] ? page_of(p.table, p.g, b, tok[u], p.error) : -1;
+    on[u] = page >= 0;
+    slot[u] = (int)(tok[u] & (kPageTokens - 1));
+    block[u] = p.pages + page_block_offset(p.g, p.layer0 + (int)layer[u], on[u] ? page : 0, (int)head[u]);
+  }
+  const int row_bytes = FMT == THINK_PAGE_PLAIN ? D * E : FMT == THINK_PAGE_E4M3 ? D : D / 2;
+  const int scale_bytes = FMT == THINK_PAGE_PLAIN ? 0 : FMT == THINK_PAGE_E4M3 ? 1 : D / 16;
   if (WRITE) {
-    if (FMT == THINK_PAGE_PLAIN) {
-      if (ok) {
-        ((uint4*)kc)[c] = k;
-        ((uint4*)vc)[c] = v;
-      }
-    } else if (FMT == THINK_PAGE_E4M3) {
-      uint32_t ke, ve;
-      bool kbad, vbad;
-      const uint2 k8 = encode_e4m3<LANES>(k, ke, kbad), v8 = encode_e4m3<LANES>(v, ve, vbad);
-      if (ok) {
-        ((uint2*)kc)[c] = k8;
-        ((uint2*)vc)[c] = v8;
-        if (c == 0) {
-          *ks = (uint8_t)ke;
-          *vs = (uint8_t)ve;
-          if (kbad || vbad) atomicOr(p.error, kErrNonFinite);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      uint8_t* const kc = block[u] + slot[u] * row_bytes;
+      uint8_t* const vc = kc + kPageTokens * row_bytes;
+      uint8_t* const ks = block[u] + 2 * kPageTokens * row_bytes + slot[u] * scale_bytes;
+      uint8_t* const vs = ks + kPageTokens * scale_bytes;
+      if (FMT == THINK_PAGE_PLAIN) {
+        if (on[u]) {
+          ((uint4*)kc)[c] = k[u];
+          ((uint4*)vc)[c] = v[u];
         }
-      }
-    } else {
-      uint32_t ke, ve;
-      bool kbad, vbad;
-      const uint32_t k4 = encode_int4(k, ke, kbad), v4 = encode_int4(v, ve, vbad);
-      if (ok) {
-        ((uint32_t*)kc)[c] = k4;
-        ((uint32_t*)vc)[c] = v4;
-        if ((c & 3) == 0) {
-          ((uint16_t*)ks)[c >> 2] = (uint16_t)ke;
-          ((uint16_t*)vs)[c >> 2] = (uint16_t)ve;
-          if (kbad || vbad) atomicOr(p.error, kErrNonFinite);
+      } else if (FMT == THINK_PAGE_E4M3) {
+        uint32_t ke, ve;
+        bool kbad, vbad;
+        const uint2 k8 = encode_e4m3<LANES>(k[u], ke, kbad), v8 = encode_e4m3<LANES>(v[u], ve, vbad);
+        if (on[u]) {
+          ((uint2*)kc)[c] = k8;
+          ((uint2*)vc)[c] = v8;
+          if (c == 0) {
+            *ks = (uint8_t)ke;
+            *vs = (uint8_t)ve;
+            if (kbad || vbad) atomicOr(p.error, kErrNonFinite);
+          }
+        }
+      } else {
+        uint32_t ke, ve;
+        bool kbad, vbad;
+        const uint32_t k4 = encode_int4(k[u], ke, kbad), v4 = encode_int4(v[u], ve, vbad);
+        if (on[u]) {
+          ((uint32_t*)kc)[c] = k4;
+          ((uint32_t*)vc)[c] = v4;
+          if ((c & 3) == 0) {
+            ((uint16_t*)ks)[c >> 2] = (uint16_t)ke;
+            ((uint16_t*)vs)[c >> 2] = (uint16_t)ve;
+            if (kbad || vbad) atomicOr(p.error, kErrNonFinite);
+          }
         }
       }
     }
-  } else if (ok) {
+    return;
+  }
+  uint32_t ke[U], ve[U];                        // scales' bits
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (!on[u]) continue;
+    const uint8_t* const kc = block[u] + slot[u] * row_bytes;
+    const uint8_t* const vc = kc + kPageTokens * row_bytes;
+    const uint8_t* const ks = block[u] + 2 * kPageTokens * row_bytes + slot[u] * scale_bytes;
+    const uint8_t* const vs = ks + kPageTokens * scale_bytes;
     if (FMT == THINK_PAGE_PLAIN) {
-      k = __ldcs((const uint4*)kc + c);
-      v = __ldcs((const uint4*)vc + c);
+      k[u] = __ldcs((const uint4*)kc + c);
+      v[u] = __ldcs((const uint4*)vc + c);
     } else if (FMT == THINK_PAGE_E4M3) {
-      const uint2 k8 = __ldcs((const uint2*)kc + c), v8 = __ldcs((const uint2*)vc + c);
-      const float fk = e8m0(*ks), fv = e8m0(*vs);
-      k = make_uint4(decode_e4m3x2(k8.x, fk), decode_e4m3x2(k8.x >> 16, fk), decode_e4m3x2(k8.y, fk), decode_e4m3x2(k8.y >> 16, fk));
-      v = make_uint4(decode_e4m3x2(v8.x, fv), decode_e4m3x2(v8.x >> 16, fv), decode_e4m3x2(v8.y, fv), decode_e4m3x2(v8.y >> 16, fv));
+      *(uint2*)&k[u] = __ldcs((const uint2*)kc + c);
+      *(uint2*)&v[u] = __ldcs((const uint2*)vc + c);
+      ke[u] = *ks;
+      ve[u] = *vs;
     } else {
-      const uint32_t k4 = __ldcs((const uint32_t*)kc + c), v4 = __ldcs((const uint32_t*)vc + c);
-      const float fk = __uint_as_float((uint32_t)((const uint16_t*)ks)[c >> 2] << 16);
-      const float fv = __uint_as_float((uint32_t)((const uint16_t*)vs)[c >> 2] << 16);
-      auto two = [](uint32_t w, int i, float f) {
-        return pack2((float)((int)(w >> (8 * i) & 15u) - 8) * f, (float)((int)(w >> (8 * i + 4) & 15u) - 8) * f);
-      };
-      k = make_uint4(two(k4, 0, fk), two(k4, 1, fk), two(k4, 2, fk), two(k4, 3, fk));
-      v = make_uint4(two(v4, 0, fv), two(v4, 1, fv), two(v4, 2, fv), two(v4, 3, fv));
+      k[u].x = __ldcs((const uint32_t*)kc + c);
+      v[u].x = __ldcs((const uint32_t*)vc + c);
+      ke[u] = ((const uint16_t*)ks)[c >> 2];
+      ve[u] = ((const uint16_t*)vs)[c >> 2];
     }
-    __stcs(kx, k);
-    __stcs(vx, v);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (!on[u]) continue;
+    if (FMT == THINK_PAGE_E4M3) {
+      k[u] = decode_e4m3(make_uint2(k[u].x, k[u].y), e8m0(ke[u]));
+      v[u] = decode_e4m3(make_uint2(v[u].x, v[u].y), e8m0(ve[u]));
+    } else if (FMT == THINK_PAGE_INT4) {
+      k[u] = decode_int4(k[u].x, __uint_as_float(ke[u] << 16));
+      v[u] = decode_int4(v[u].x, __uint_as_float(ve[u] << 16));
+    }
+    __stcs(kx[u], k[u]);
+    __stcs(vx[u], v[u]);
   }
 }
 
 template <int D, int E, int FMT>
 cudaError_t launch_rows(const PagedRowsParams& p, bool write, cudaStream_t s) {
-  constexpr int rpb = kRowThreads / (D * E / 16);
+  constexpr int rpb = kRowsPerThread * kRowThreads / (D * E / 16);
   const int64_t rows = (int64_t)p.max_rows * p.nlayers * p.g.N_kv;
   const dim3 grid((unsigned)((rows + rpb - 1) / rpb), (unsigned)p.table.B);
   if (write) k_paged_rows<D, E, FMT, true><<<grid, kRowThreads, 0, s>>>(p);
