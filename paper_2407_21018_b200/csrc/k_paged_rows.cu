@@ -1,8 +1,9 @@
 // Rows of the paged cache: quantised as they are written, dequantised as they are read back.
 //
 // Both directions only move bytes (512 bytes of bf16 key and value against 258 or 144 stored ones a row at
-// D = 128), so the DRAM stream is the bound and the kernels are one pass: a lane owns 16 bytes of a row's elements
-// (8 bf16 or 4 fp32 channels) of the key AND of the value, both loads in flight before anything waits, the row's (or
+// D = 128), so the DRAM stream is the bound and the kernels are one pass: a lane owns two 16-byte pieces of a row's
+// elements (8 bf16 or 4 fp32 channels each) of the key AND of the value, all four loads in flight before
+// anything waits (one piece a lane spent most of its instructions on addresses), the row's (or
 // group's) maximum goes over the lanes of the row by shuffles, and codes leave from registers.  The lanes of a warp
 // hold consecutive rows with the head running fastest, which is the order of the [b, s, l, n, d] tensors: loads are
 // whole 128-byte lines, and the stores of a row are one contiguous piece of its page.
@@ -13,14 +14,8 @@
 namespace think {
 namespace {
 
-#ifndef THINK_ROWS_U
-#define THINK_ROWS_U 2
-#endif
-#ifndef THINK_ROWS_T
-#define THINK_ROWS_T 128
-#endif
-constexpr int kRowThreads = THINK_ROWS_T;
-constexpr int kRowsPerThread = THINK_ROWS_U;
+constexpr int kRowThreads = 128;
+constexpr int kPieces = 2;            // 16-byte pieces of a row that a lane holds, half a row apart
 
 // largest |x| of 8 bf16 as the integer of its bits: orders finite < infinite < NaN
 __device__ __forceinline__ uint32_t amax_bits(const uint4& w) {
@@ -41,19 +36,15 @@ __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
   return lo | (hi << 16);
 }
 
-// 8 bf16 -> 8 e4m3 codes; LANES lanes hold the row.  `e` receives the scale byte.
-template <int LANES>
-__device__ __forceinline__ uint2 encode_e4m3(const uint4& w, uint32_t& e, bool& bad) {
-  const uint32_t top = lane_max<LANES>(amax_bits(w));
-  bad = top >= kInfBits;
-  // top = 1.m * 2^(E - 127): 448 = 1.75 * 2^8, so the scale's exponent is E - 8, one more if 1.m > 1.75
+// A row's scale byte from its largest magnitude's bits; the factor 2^-k that brings it to codes.
+// top = 1.m * 2^(E - 127): 448 = 1.75 * 2^8, so the scale's exponent k is E - 8, one more if 1.m > 1.75
+__device__ __forceinline__ uint32_t scale_e4m3(uint32_t top, float& inv) {
   const int k = max((int)(top >> 7) - 127 - 8 + ((top & 0x7fu) > 0x60u ? 1 : 0), -126);
-  e = (uint32_t)(k + 127);
-  if (bad) {
-    e = 127u;
-    return make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);
-  }
-  const float inv = __uint_as_float((uint32_t)(127 - k) << 23);    // 2^-k: the product is exact, the code rounds once
+  inv = __uint_as_float((uint32_t)(127 - k) << 23);
+  return (uint32_t)(k + 127);
+}
+// 8 bf16 -> 8 e4m3 codes: the products are exact, the codes round once
+__device__ __forceinline__ uint2 encode_e4m3(const uint4& w, float inv) {
   return make_uint2(e4m3x4(bf16lo(w.x) * inv, bf16hi(w.x) * inv, bf16lo(w.y) * inv, bf16hi(w.y) * inv),
                     e4m3x4(bf16lo(w.z) * inv, bf16hi(w.z) * inv, bf16lo(w.w) * inv, bf16hi(w.w) * inv));
 }
@@ -113,89 +104,96 @@ __device__ __forceinline__ uint4 decode_e4m3(const uint2& w, float f) {
   return make_uint4(decode_e4m3x2(w.x, f), decode_e4m3x2(w.x >> 16, f), decode_e4m3x2(w.y, f), decode_e4m3x2(w.y >> 16, f));
 }
 
-// FMT: thinK_page_format.  E: bytes of an element (2 bf16, 4 fp32).  A block takes kRowsPerThread * kRowThreads / LANES
-// consecutive rows of one entry (head fastest, then layer, then token).
+// FMT: thinK_page_format.  E: bytes of an element (2 bf16, 4 fp32).  A block takes kRowThreads / LANES consecutive
+// rows of one entry (head fastest, then layer, then token).
 template <int D, int E, int FMT, bool WRITE>
 __global__ void __launch_bounds__(kRowThreads) k_paged_rows(const PagedRowsParams p) {
-  constexpr int LANES = D * E / 16;             // lanes of a row, 16 bytes of elements each
-  constexpr int CH = 16 / E;                    // channels of a lane
-  constexpr int RPB = kRowThreads / LANES, U = kRowsPerThread;
+  constexpr int P = kPieces;
+  constexpr int LANES = D * E / 16 / P;         // lanes of a row
+  constexpr int RPB = kRowThreads / LANES;
+  constexpr int RB = FMT == THINK_PAGE_PLAIN ? D * E : FMT == THINK_PAGE_E4M3 ? D : D / 2;
+  constexpr int SB = FMT == THINK_PAGE_PLAIN ? 0 : FMT == THINK_PAGE_E4M3 ? 1 : D / 16;
   const int b = blockIdx.y;
   const int nrows_raw = p.rows ? __ldg(p.rows + b) : p.max_rows;
   const int pos = p.pos ? __ldg(p.pos + b) : 0;
   const int nrows = min(nrows_raw, p.max_rows);
   if (blockIdx.x == 0 && threadIdx.x == 0 && nrows_raw > p.max_rows) atomicOr(p.error, kErrPage);
-  const uint32_t first = blockIdx.x * (RPB * U);
+  const uint32_t first = blockIdx.x * RPB;
   if (nrows <= 0 || first >= (uint64_t)nrows * p.nlayers * p.g.N_kv) return;      // whole block: no row
   const int c = threadIdx.x % LANES;
-  uint4 k[U], v[U];
-  uint4 *kx[U], *vx[U];
-  uint8_t* block[U];
-  int slot[U];
-  bool on[U];                                   // lanes of a row agree; idle rows still take part in the shuffles
-  uint32_t layer[U], head[U];
-  int64_t tok[U];
+  const uint8_t* const kb = (const uint8_t*)p.k.ptr + (b * p.k.sb) * E + c * 16;
+  const uint8_t* const vb = (const uint8_t*)p.v.ptr + (b * p.v.sb) * E + c * 16;
+  const uint32_t r = first + threadIdx.x / LANES;
+  const uint32_t rl = p.by_heads.div(r), h = r - rl * p.g.N_kv;
+  const uint32_t s = p.by_layers.div(rl), ll = rl - s * p.nlayers;
+  bool on = s < (uint32_t)nrows;                // lanes of a row agree; idle rows still take part in the shuffles
+  uint4* const kx = (uint4*)(kb + (s * p.k.ss + ll * p.k.sl + h * p.k.sn) * E);
+  uint4* const vx = (uint4*)(vb + (s * p.v.ss + ll * p.v.sl + h * p.v.sn) * E);
+  uint4 k[P], v[P];
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const uint32_t r = first + u * RPB + threadIdx.x / LANES;
-    const uint32_t rl = p.by_heads.div(r), h = r - rl * p.g.N_kv;
-    const uint32_t s = p.by_layers.div(rl), ll = rl - s * p.nlayers;
-    on[u] = s < (uint32_t)nrows;
-    layer[u] = ll;
-    head[u] = h;
-    tok[u] = (int64_t)pos + s;
-    kx[u] = (uint4*)((uint8_t*)p.k.ptr + (b * p.k.sb + (int64_t)s * p.k.ss + ll * p.k.sl + h * p.k.sn + c * CH) * E);
-    vx[u] = (uint4*)((uint8_t*)p.v.ptr + (b * p.v.sb + (int64_t)s * p.v.ss + ll * p.v.sl + h * p.v.sn + c * CH) * E);
-    k[u] = v[u] = make_uint4(0u, 0u, 0u, 0u);
-    if (WRITE && on[u]) {
-      k[u] = __ldcs(kx[u]);
-      v[u] = __ldcs(vx[u]);
+  for (int i = 0; i < P; ++i) {
+    k[i] = v[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (WRITE && on) {
+      k[i] = __ldcs(kx + i * LANES);
+      v[i] = __ldcs(vx + i * LANES);
     }
   }
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int page = on[u] ? page_of(p.table, p.g, b, tok[u], p.error) : -1;
-    on[u] = page >= 0;
-    slot[u] = (int)(tok[u] & (kPageTokens - 1));
-    block[u] = p.pages + page_block_offset(p.g, p.layer0 + (int)layer[u], on[u] ? page : 0, (int)head[u]);
-  }
-  const int row_bytes = FMT == THINK_PAGE_PLAIN ? D * E : FMT == THINK_PAGE_E4M3 ? D : D / 2;
-  const int scale_bytes = FMT == THINK_PAGE_PLAIN ? 0 : FMT == THINK_PAGE_E4M3 ? 1 : D / 16;
+  const int64_t tok = (int64_t)pos + s;
+  const int page = on ? page_of(p.table, p.g, b, tok, p.error) : -1;
+  on = page >= 0;
+  const int slot = (int)(tok & (kPageTokens - 1));
+  uint8_t* const block = p.pages + page_block_offset(p.g, p.layer0 + (int)ll, on ? page : 0, (int)h);
+  uint8_t* const kc = block + slot * RB;        // values: 64 rows behind
+  uint8_t* const ks = block + 2 * kPageTokens * RB + slot * SB;
   if (WRITE) {
+    uint8_t* const vc = kc + kPageTokens * RB;
+    uint8_t* const vs = ks + kPageTokens * SB;
+    if (FMT == THINK_PAGE_PLAIN) {
+      if (on) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      uint8_t* const kc = block[u] + slot[u] * row_bytes;
-      uint8_t* const vc = kc + kPageTokens * row_bytes;
-      uint8_t* const ks = block[u] + 2 * kPageTokens * row_bytes + slot[u] * scale_bytes;
-      uint8_t* const vs = ks + kPageTokens * scale_bytes;
-      if (FMT == THINK_PAGE_PLAIN) {
-        if (on[u]) {
-          ((uint4*)kc)[c] = k[u];
-          ((uint4*)vc)[c] = v[u];
+        for (int i = 0; i < P; ++i) {
+          ((uint4*)kc)[c + i * LANES] = k[i];
+          ((uint4*)vc)[c + i * LANES] = v[i];
         }
-      } else if (FMT == THINK_PAGE_E4M3) {
+      }
+    } else if (FMT == THINK_PAGE_E4M3) {
+      uint32_t kt = 0, vt = 0;
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        kt = max(kt, amax_bits(k[i]));
+        vt = max(vt, amax_bits(v[i]));
+      }
+      kt = lane_max<LANES>(kt);
+      vt = lane_max<LANES>(vt);
+      float ki, vi;
+      const uint32_t ke = scale_e4m3(kt, ki), ve = scale_e4m3(vt, vi);
+      const bool kbad = kt >= kInfBits, vbad = vt >= kInfBits;
+      const uint2 nan = make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);
+      if (on) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          const uint2 k8 = encode_e4m3(k[i], ki), v8 = encode_e4m3(v[i], vi);
+          ((uint2*)kc)[c + i * LANES] = kbad ? nan : k8;
+          ((uint2*)vc)[c + i * LANES] = vbad ? nan : v8;
+        }
+        if (c == 0) {
+          *ks = (uint8_t)(kbad ? 127u : ke);
+          *vs = (uint8_t)(vbad ? 127u : ve);
+          if (kbad || vbad) atomicOr(p.error, kErrNonFinite);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
         uint32_t ke, ve;
         bool kbad, vbad;
-        const uint2 k8 = encode_e4m3<LANES>(k[u], ke, kbad), v8 = encode_e4m3<LANES>(v[u], ve, vbad);
-        if (on[u]) {
-          ((uint2*)kc)[c] = k8;
-          ((uint2*)vc)[c] = v8;
-          if (c == 0) {
-            *ks = (uint8_t)ke;
-            *vs = (uint8_t)ve;
-            if (kbad || vbad) atomicOr(p.error, kErrNonFinite);
-          }
-        }
-      } else {
-        uint32_t ke, ve;
-        bool kbad, vbad;
-        const uint32_t k4 = encode_int4(k[u], ke, kbad), v4 = encode_int4(v[u], ve, vbad);
-        if (on[u]) {
-          ((uint32_t*)kc)[c] = k4;
-          ((uint32_t*)vc)[c] = v4;
+        const uint32_t k4 = encode_int4(k[i], ke, kbad), v4 = encode_int4(v[i], ve, vbad);
+        if (on) {
+          ((uint32_t*)kc)[c + i * LANES] = k4;
+          ((uint32_t*)vc)[c + i * LANES] = v4;
           if ((c & 3) == 0) {
-            ((uint16_t*)ks)[c >> 2] = (uint16_t)ke;
-            ((uint16_t*)vs)[c >> 2] = (uint16_t)ve;
+            ((uint16_t*)ks)[(c + i * LANES) >> 2] = (uint16_t)ke;
+            ((uint16_t*)vs)[(c + i * LANES) >> 2] = (uint16_t)ve;
             if (kbad || vbad) atomicOr(p.error, kErrNonFinite);
           }
         }
@@ -203,47 +201,45 @@ __global__ void __launch_bounds__(kRowThreads) k_paged_rows(const PagedRowsParam
     }
     return;
   }
-  uint32_t ke[U], ve[U];                        // scales' bits
+  if (!on) return;
+  uint32_t ke[P], ve[P];                        // scales' bits
+  const uint8_t* const vc = kc + kPageTokens * RB;
+  const uint8_t* const vs = ks + kPageTokens * SB;
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    if (!on[u]) continue;
-    const uint8_t* const kc = block[u] + slot[u] * row_bytes;
-    const uint8_t* const vc = kc + kPageTokens * row_bytes;
-    const uint8_t* const ks = block[u] + 2 * kPageTokens * row_bytes + slot[u] * scale_bytes;
-    const uint8_t* const vs = ks + kPageTokens * scale_bytes;
+  for (int i = 0; i < P; ++i) {
+    const int ci = c + i * LANES;
     if (FMT == THINK_PAGE_PLAIN) {
-      k[u] = __ldcs((const uint4*)kc + c);
-      v[u] = __ldcs((const uint4*)vc + c);
+      k[i] = __ldcs((const uint4*)kc + ci);
+      v[i] = __ldcs((const uint4*)vc + ci);
     } else if (FMT == THINK_PAGE_E4M3) {
-      *(uint2*)&k[u] = __ldcs((const uint2*)kc + c);
-      *(uint2*)&v[u] = __ldcs((const uint2*)vc + c);
-      ke[u] = *ks;
-      ve[u] = *vs;
+      *(uint2*)&k[i] = __ldcs((const uint2*)kc + ci);
+      *(uint2*)&v[i] = __ldcs((const uint2*)vc + ci);
+      ke[i] = i == 0 ? *ks : ke[0];
+      ve[i] = i == 0 ? *vs : ve[0];
     } else {
-      k[u].x = __ldcs((const uint32_t*)kc + c);
-      v[u].x = __ldcs((const uint32_t*)vc + c);
-      ke[u] = ((const uint16_t*)ks)[c >> 2];
-      ve[u] = ((const uint16_t*)vs)[c >> 2];
+      k[i].x = __ldcs((const uint32_t*)kc + ci);
+      v[i].x = __ldcs((const uint32_t*)vc + ci);
+      ke[i] = ((const uint16_t*)ks)[ci >> 2];
+      ve[i] = ((const uint16_t*)vs)[ci >> 2];
     }
   }
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    if (!on[u]) continue;
+  for (int i = 0; i < P; ++i) {
     if (FMT == THINK_PAGE_E4M3) {
-      k[u] = decode_e4m3(make_uint2(k[u].x, k[u].y), e8m0(ke[u]));
-      v[u] = decode_e4m3(make_uint2(v[u].x, v[u].y), e8m0(ve[u]));
+      k[i] = decode_e4m3(make_uint2(k[i].x, k[i].y), e8m0(ke[i]));
+      v[i] = decode_e4m3(make_uint2(v[i].x, v[i].y), e8m0(ve[i]));
     } else if (FMT == THINK_PAGE_INT4) {
-      k[u] = decode_int4(k[u].x, __uint_as_float(ke[u] << 16));
-      v[u] = decode_int4(v[u].x, __uint_as_float(ve[u] << 16));
+      k[i] = decode_int4(k[i].x, __uint_as_float(ke[i] << 16));
+      v[i] = decode_int4(v[i].x, __uint_as_float(ve[i] << 16));
     }
-    __stcs(kx[u], k[u]);
-    __stcs(vx[u], v[u]);
+    __stcs(kx + i * LANES, k[i]);
+    __stcs(vx + i * LANES, v[i]);
   }
 }
 
 template <int D, int E, int FMT>
 cudaError_t launch_rows(const PagedRowsParams& p, bool write, cudaStream_t s) {
-  constexpr int rpb = kRowsPerThread * kRowThreads / (D * E / 16);
+  constexpr int rpb = kRowThreads / (D * E / 16 / kPieces);
   const int64_t rows = (int64_t)p.max_rows * p.nlayers * p.g.N_kv;
   const dim3 grid((unsigned)((rows + rpb - 1) / rpb), (unsigned)p.table.B);
   if (write) k_paged_rows<D, E, FMT, true><<<grid, kRowThreads, 0, s>>>(p);
