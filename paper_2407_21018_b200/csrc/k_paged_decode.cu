@@ -44,7 +44,7 @@ constexpr int kMaxG = kMaxPagedGroup;
 #define THINK_PW_PLAIN 8
 #endif
 #ifndef THINK_PW_E4M3
-#define THINK_PW_E4M3 12
+#define THINK_PW_E4M3 8
 #endif
 #ifndef THINK_PW_INT4
 #define THINK_PW_INT4 12

@@ -58,14 +58,17 @@ __device__ __forceinline__ uint2 encode_e4m3(const uint4& w, float inv) {
 __device__ __forceinline__ uint32_t encode_int4(const uint4& w, uint32_t& sbits, bool& bad) {
   const uint32_t top = lane_max<4>(amax_bits(w));
   bad = top >= kInfBits;
-  const __nv_bfloat16 sb = __float2bfloat16_rn(__fdiv_rn(__uint_as_float(top << 16), 7.f));
+  // amax / 7 to bf16: the quotient of an 8-bit number by 7 is never a tie and at least 2^-12 away from one, so the
+  // product with 1 / 7 rounds the same
+  const __nv_bfloat16 sb = __float2bfloat16_rn(__fmul_rn(__uint_as_float(top << 16), 1.f / 7.f));
   sbits = bad ? 0x7fc0u : (uint32_t)__bfloat16_as_ushort(sb);
   const float s = __bfloat162float(sb);
   if (bad || s == 0.f) return 0x88888888u;
   const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
   uint32_t c[4];                                // two codes each in the low byte
   if (s >= 1.17549435e-38f) {
-    const float inv = __frcp_rn(s);
+    float inv;                                  // within an ulp
+    asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(s));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float a = __fadd_rn(__fadd_rn(__fmul_rn(bf16lo(ws[i]), inv), 3072.f), -3072.f);
