@@ -853,7 +853,7 @@ struct alignas(16) Shared {
 };
 
 template <int D, int E, int FMT, int GP>
-__global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode(const PagedDecodeParams p) {
+__global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode(PagedDecodeParams p) {
   using S = Shape<D, E, FMT>;
   constexpr int kWarps = S::WARPS, kThreads = S::THREADS;
   using State = typename StateOf<D, E, FMT, GP>::type;
@@ -865,6 +865,7 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int B = p.table.B, LH = p.nlayers * p.g.N_kv, grid = gridDim.x, cta = blockIdx.x;
 
+  begin_dependent();
   // ---- tiles of every sequence, cumulated
   bool empty = false;
   {
@@ -1264,8 +1265,7 @@ inline size_t smem_tables(int B) { return ((size_t)(B + 1) * 4 + B + 15) / 16 * 
 template <int D, int E, int FMT, int GP>
 cudaError_t launch_k(const PagedDecodeParams& p, cudaStream_t s) {
   const size_t smem = smem_fixed<D, E, FMT>() + smem_tables(p.table.B);
-  k_paged_decode<D, E, FMT, GP><<<p.grid, Shape<D, E, FMT>::THREADS, smem, s>>>(p);
-  return cudaGetLastError();
+  return launch_dependent(k_paged_decode<D, E, FMT, GP>, dim3(p.grid), Shape<D, E, FMT>::THREADS, smem, s, p);
 }
 template <int D, int E, int FMT, int GP>
 cudaError_t setup_k() {

@@ -110,12 +110,13 @@ __device__ __forceinline__ uint4 decode_e4m3(const uint2& w, float f) {
 // FMT: thinK_page_format.  E: bytes of an element (2 bf16, 4 fp32).  A block takes kRowThreads / LANES consecutive
 // rows of one entry (head fastest, then layer, then token).
 template <int D, int E, int FMT, bool WRITE>
-__global__ void __launch_bounds__(kRowThreads) k_paged_rows(const PagedRowsParams p) {
+__global__ void __launch_bounds__(kRowThreads) k_paged_rows(PagedRowsParams p) {
   constexpr int P = kPieces;
   constexpr int LANES = D * E / 16 / P;         // lanes of a row
   constexpr int RPB = kRowThreads / LANES;
   constexpr int RB = FMT == THINK_PAGE_PLAIN ? D * E : FMT == THINK_PAGE_E4M3 ? D : D / 2;
   constexpr int SB = FMT == THINK_PAGE_PLAIN ? 0 : FMT == THINK_PAGE_E4M3 ? 1 : D / 16;
+  begin_dependent();
   const int b = blockIdx.y;
   const int nrows_raw = p.rows ? __ldg(p.rows + b) : p.max_rows;
   const int pos = p.pos ? __ldg(p.pos + b) : 0;
@@ -245,9 +246,7 @@ cudaError_t launch_rows(const PagedRowsParams& p, bool write, cudaStream_t s) {
   constexpr int rpb = kRowThreads / (D * E / 16 / kPieces);
   const int64_t rows = (int64_t)p.max_rows * p.nlayers * p.g.N_kv;
   const dim3 grid((unsigned)((rows + rpb - 1) / rpb), (unsigned)p.table.B);
-  if (write) k_paged_rows<D, E, FMT, true><<<grid, kRowThreads, 0, s>>>(p);
-  else k_paged_rows<D, E, FMT, false><<<grid, kRowThreads, 0, s>>>(p);
-  return cudaGetLastError();
+  return launch_dependent(write ? k_paged_rows<D, E, FMT, true> : k_paged_rows<D, E, FMT, false>, grid, kRowThreads, 0, s, p);
 }
 
 template <int D>

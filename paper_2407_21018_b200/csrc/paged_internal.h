@@ -89,7 +89,32 @@ cudaError_t launch_paged_decode(const PagedDecodeParams& p, int dtype, int forma
 cudaError_t paged_decode_setup(int dtype, int format, int D, int G);   // kernel attributes on the current device
 size_t paged_decode_record_bytes(int D, int ctas);                     // partial states of a launch of that many CTAs
 
+// Launches a kernel that begins with begin_dependent(): it may be set up while the kernel ahead of it in the stream
+// finishes.
+template <typename Params>
+inline cudaError_t launch_dependent(void (*kernel)(Params), dim3 grid, int threads, size_t smem, cudaStream_t s, const Params& p) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, p);
+}
+
 #ifdef __CUDACC__
+// Lets the next kernel of the stream be set up, then waits until everything ahead of this one has completed and can be
+// read.  Every thread of such a kernel calls it before anything else and before any return: the next kernel only waits
+// for this one, so this one must not complete ahead of its own predecessors.
+__device__ __forceinline__ void begin_dependent() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 // Page that holds token t of entry b, or -1 (error bit) if the table or the position is out of range.
 __device__ __forceinline__ int page_of(const PageTableView& t, const PageGeom& g, int b, int64_t tok, uint32_t* error) {
   int page = -1;
