@@ -2,9 +2,9 @@
 //
 // Every byte of the pages is read once and used for at most 8 query heads, so the stream of pages is the bound and
 // the kernel is built around it:
-//  * The tiles (64-token pages) of all (entry, layer, key head) units form one flat list, cut evenly over the CTAs
-//    of one wave and inside a CTA over its warps, whatever the lengths: one long sequence uses the whole card and a
-//    ragged batch leaves no SM idle.  Lengths and page table are device memory; each CTA scans the lengths itself.
+//  * The tiles (64-token pages) of all (entry, layer, key head) units stand on one line, with half a tile's place
+//    for starting and ending a unit; it is cut evenly over the CTAs of one wave and inside a CTA over its warps,
+//    whatever the lengths: one long sequence uses the whole card and a ragged batch leaves no SM idle.  Lengths and page table are device memory; each CTA scans the lengths itself.
 //  * A warp is the worker.  It owns a ring of stages in shared memory that it fills with cp.async, crossing page and
 //    unit borders, and waits for nobody until its range is done.
 //  * Rows are stored token-major.  16-byte chunks are XOR-swizzled on the way into shared memory so that ldmatrix
@@ -206,22 +206,39 @@ __device__ __forceinline__ int swz(int r, int ck) {
   return r * RB + ((ck ^ ((r >> 2) & 1)) << 4);
 }
 
-// Tables of a launch in shared memory: cumulative tiles and the tokens of each sequence's last tile.
+// Tables of a launch in shared memory: cumulative places (per layer and head) and the tokens of each sequence's last
+// tile.
 struct Tables {
   const int* cum;            // [B + 1]
   const uint8_t* last;       // tokens in the last tile, minus 1
+  Weights w;
+  int B, nlayers, N_kv;
 };
-struct Cursor {              // a tile of the flat list
+struct Cursor {              // a tile of the line
   int b, ll, h;              // entry, layer of the call, key head
   int j, nt;                 // tile and tiles of the unit
   int len;
+  int64_t us;                // place of the unit's first tile
 };
 __device__ __forceinline__ void seq_of(const Tables& t, Cursor& c) {
-  c.nt = t.cum[c.b + 1] - t.cum[c.b];
+  c.nt = t.w.tiles(t.cum[c.b + 1] - t.cum[c.b]);
   c.len = (c.nt - 1) * kPageTokens + t.last[c.b] + 1;
 }
-__device__ __forceinline__ Cursor locate(const Tables& t, int B, int LH, int N_kv, int64_t f) {
-  int lo = 0, hi = B - 1;                      // last entry with cum * LH <= f that has tiles
+// to the first tile of the next unit, if there is one
+__device__ __forceinline__ void next_unit(const Tables& t, Cursor& c) {
+  c.us += t.w.cost(c.nt);
+  c.j = 0;
+  if (++c.h < t.N_kv) return;
+  c.h = 0;
+  if (++c.ll < t.nlayers) return;
+  c.ll = 0;
+  do ++c.b; while (c.b < t.B && t.cum[c.b + 1] == t.cum[c.b]);
+  if (c.b < t.B) seq_of(t, c);
+}
+// the first tile at place f or behind, f below the line's end; none if the result's place is the line's end
+__device__ __forceinline__ Cursor locate(const Tables& t, int64_t f) {
+  const int LH = t.nlayers * t.N_kv;
+  int lo = 0, hi = t.B - 1;                    // last entry that begins at f or before: it has tiles
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if ((int64_t)t.cum[mid] * LH <= f) lo = mid; else hi = mid - 1;
@@ -229,22 +246,15 @@ __device__ __forceinline__ Cursor locate(const Tables& t, int B, int LH, int N_k
   Cursor c;
   c.b = lo;
   seq_of(t, c);
+  const int cost = t.w.cost(c.nt);
   const int64_t rem = f - (int64_t)t.cum[lo] * LH;
-  const int u = (int)div_wide(rem, c.nt);
-  c.j = (int)(rem - (int64_t)u * c.nt);
-  c.ll = (int)((unsigned)u / (unsigned)N_kv);
-  c.h = u - c.ll * N_kv;
+  const int u = (int)div_wide(rem, cost);
+  c.us = f - rem + (int64_t)u * cost;
+  c.ll = (int)((unsigned)u / (unsigned)t.N_kv);
+  c.h = u - c.ll * t.N_kv;
+  c.j = t.w.first_tile(f - c.us);
+  if (c.j >= c.nt) next_unit(t, c);
   return c;
-}
-// to the first tile of the next unit
-__device__ __forceinline__ void next_unit(const Tables& t, int B, int nlayers, int N_kv, Cursor& c) {
-  c.j = 0;
-  if (++c.h < N_kv) return;
-  c.h = 0;
-  if (++c.ll < nlayers) return;
-  c.ll = 0;
-  do ++c.b; while (c.b < B && t.cum[c.b + 1] == t.cum[c.b]);
-  if (c.b < B) seq_of(t, c);
 }
 
 // brings `bytes` (a multiple of 128, at most 4096) towards the SM; the values are not waited for
@@ -259,12 +269,11 @@ __device__ __forceinline__ uint32_t ticket_add(uint32_t* p) {
   return x;
 }
 
-// What a warp tells its CTA about the range it has done.
+// What a warp tells its CTA: its first and its last unit, with the places of their first and last tiles.
 struct WarpInfo {
-  int64_t f0, f1;            // empty if equal
-  int64_t last_us, last_ue;  // flat range of the last unit
+  int64_t first_us, first_ul, last_us, last_ul;
   int first_unit, last_unit; // index of the unit in the call
-  int64_t first_us, first_ue;
+  int busy;                  // has tiles
 };
 
 // ---------------------------------------------------------------------------------------------------------
@@ -847,7 +856,7 @@ constexpr int kSpBytes = 512;        // fp32: a warp's weights of a step, read 1
 // shared memory behind the rings
 struct alignas(16) Shared {
   WarpInfo info[kMaxWarps];
-  int warp_sum[kMaxWarps];
+  int2 warp_sum[kMaxWarps];
   int valid[kMaxWarps][8];   // tokens that count in the stage
   int arrived[2];
 };
@@ -868,10 +877,11 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
   begin_dependent();
   // ---- tiles of every sequence, cumulated
   bool empty = false;
+  Weights wt;
   {
     const int per = (B + kThreads - 1) / kThreads, b0 = min(B, tid * per), b1 = min(B, b0 + per);
     const int cap = p.table.max_pages * kPageTokens;
-    int mine = 0;
+    int mine = 0, some = 0;                     // tiles, sequences that have any
     for (int b = b0; b < b1; ++b) {
       int n = __ldg(p.seq_len + b);
       if (n > cap) {
@@ -880,28 +890,43 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
       }
       const int nt = n > 0 ? (n + kPageTokens - 1) / kPageTokens : 0;
       empty |= nt == 0;
+      some += nt > 0;
       last[b] = (uint8_t)((n - 1) & (kPageTokens - 1));
       cum[b + 1] = nt;
       mine += nt;
     }
-    int x = mine;
+    int x = mine, y = some;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, x, o);
-      if (lane >= o) x += y;
+      const int xo = __shfl_up_sync(0xffffffffu, x, o), yo = __shfl_up_sync(0xffffffffu, y, o);
+      if (lane >= o) {
+        x += xo;
+        y += yo;
+      }
     }
-    if (lane == 31) sh.warp_sum[warp] = x;
+    if (lane == 31) sh.warp_sum[warp] = make_int2(x, y);
     empty = __syncthreads_or(empty);
-    int base = x - mine;
-    for (int w = 0; w < warp; ++w) base += sh.warp_sum[w];
+    int tiles = x - mine, seqs = y - some, all_tiles = 0, all_seqs = 0;
+    for (int w = 0; w < kWarps; ++w) {
+      const int2 t = sh.warp_sum[w];
+      if (w < warp) {
+        tiles += t.x;
+        seqs += t.y;
+      }
+      all_tiles += t.x;
+      all_seqs += t.y;
+    }
+    wt = weights_for((int64_t)all_tiles * LH, (int64_t)all_seqs * LH, grid);
     for (int b = b0; b < b1; ++b) {
-      base += cum[b + 1];
-      cum[b + 1] = base;
+      const int nt = cum[b + 1];
+      tiles += nt;
+      seqs += nt > 0;
+      cum[b + 1] = wt.tile * tiles + wt.unit * seqs;
     }
     if (tid == 0) cum[0] = 0;
     __syncthreads();
   }
-  const Tables tab = {cum, last};
+  const Tables tab = {cum, last, wt, B, p.nlayers, p.g.N_kv};
 
   // ---- sequences without tokens
   if (empty) {
@@ -916,19 +941,22 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
   }
 
   const int64_t total = (int64_t)cum[B] * LH;
+  if (total == 0) return;
   const int64_t F0 = split_begin(total, grid, cta), F1 = split_begin(total, grid, cta + 1);
-  if (F0 == F1) return;
   const int64_t f0 = F0 + split_begin(F1 - F0, kWarps, warp), f1 = F0 + split_begin(F1 - F0, kWarps, warp + 1);
+  // fewer tiles than CTAs: a CTA has one tile or none
+  const bool sparse = wt.unit == 0 && total < grid;
+  if (sparse && F0 == F1) return;
+  Cursor c = {};
+  if (f0 < f1) c = locate(tab, f0);
+  const bool busy_warp = f0 < f1 && c.us + wt.slot(c.j) < f1;
   Record<D>* const records = (Record<D>*)p.records;
   Record<D>* const cta_rec = records + 2 * cta;                                         // units shared with other CTAs
   Record<D>* const head_rec = records + 2 * grid + (cta * kWarps + warp);               // the warp's first unit
   Record<D>* const tail_rec = (Record<D>*)(smem + warp * S::RING);                      // its last unit
-  if (lane == 0) {
-    sh.info[warp].f0 = f0;
-    sh.info[warp].f1 = f1;
-  }
+  if (lane == 0) sh.info[warp].busy = busy_warp;
 
-  if (f0 < f1) {
+  if (busy_warp) {
     const uint32_t ring = smem_u32(smem) + warp * S::RING;
     State st;
     if constexpr (E == 4) st.sp = (float*)(smem + kWarps * S::RING + warp * kSpBytes);
@@ -936,15 +964,14 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
     // ---- producer: fills the ring tile after tile
     const int q_bytes = p.G * D * E;            // queries of a unit, in the order of units
     const int64_t page_bytes = (int64_t)p.g.N_kv * p.g.block_bytes;
-    Cursor pc = locate(tab, B, LH, p.g.N_kv, f0);
+    Cursor pc = c;
     typename State::Raw raw;                    // the first unit's queries, asked for ahead of the pages
     State::fetch((const uint8_t*)p.q + (int64_t)(pc.b * LH + pc.ll * p.g.N_kv + pc.h) * q_bytes, p.G, lane, raw);
     const int32_t* p_entry = p.table.table + pc.b * p.table.stride + pc.j;       // table entry of the next tile
     int p_page = __ldg(p_entry);                // looked up a tile ahead
     const uint8_t* p_base = p.pages + page_block_offset(p.g, p.layer0 + pc.ll, 0, pc.h);    // of the unit
-    int p_tiles = (int)min((int64_t)(pc.nt - pc.j), f1 - f0);                    // of the unit, not begun
+    int p_tiles = min(pc.nt, wt.first_tile(f1 - pc.us)) - pc.j;                  // of the unit, not begun
     int p_toks = pc.len - pc.j * kPageTokens;                                    // of the unit, not begun
-    int64_t p_left = f1 - f0 - p_tiles;         // tiles of later units
     uint32_t p_slot = ring;                     // next stage to fill
     int p_ntok = 0;                             // rows of the current tile that are left
     bool p_ok = false;
@@ -959,13 +986,12 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
       p_ntok = min(kPageTokens, p_toks);
       p_toks -= kPageTokens;
       ++p_entry;
-      if (--p_tiles == 0 && p_left > 0) {
-        next_unit(tab, B, p.nlayers, p.g.N_kv, pc);
+      if (--p_tiles == 0 && pc.us + wt.cost(pc.nt) < f1) {
+        next_unit(tab, pc);
         p_entry = p.table.table + pc.b * p.table.stride;
         p_base = p.pages + page_block_offset(p.g, p.layer0 + pc.ll, 0, pc.h);
-        p_tiles = (int)min((int64_t)pc.nt, p_left);
+        p_tiles = min(pc.nt, wt.first_tile(f1 - pc.us));
         p_toks = pc.len;
-        p_left -= p_tiles;
       }
       if (p_tiles > 0) p_page = __ldg(p_entry);
     };
@@ -1022,18 +1048,18 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
     // ---- consumer: unit after unit
     uint32_t c_slot = ring;
     const int* c_valid = sh.valid[warp];
-    Cursor c = locate(tab, B, LH, p.g.N_kv, f0);
-    int64_t f = f0;
+    bool first = true;                          // the warp's first unit
     while (true) {
-      const int64_t us = f - c.j, ue = us + c.nt, se = f1 < ue ? f1 : ue;
-      const int j1 = c.j + (int)(se - f);
+      const int j1 = min(c.nt, wt.first_tile(f1 - c.us));    // its tiles c.j .. j1 - 1
+      const int64_t ul = c.us + wt.slot(c.nt - 1);
+      const bool is_last = c.us + wt.cost(c.nt) >= f1, whole = c.j == 0 && j1 == c.nt;
       const int ntok = min(c.len, j1 * kPageTokens) - c.j * kPageTokens;
       const int unit = c.b * LH + c.ll * p.g.N_kv + c.h;
       const int64_t row = (int64_t)unit * p.G;   // first query row
-      if (f != f0) State::fetch((const uint8_t*)p.q + row * D * E, p.G, lane, raw);
+      if (!first) State::fetch((const uint8_t*)p.q + row * D * E, p.G, lane, raw);
       st.begin(raw, p.scale_log2, lane);
       // the next unit's queries come while this one is worked on (it may be one of an empty sequence)
-      if (se < f1) touch((const uint8_t*)p.q + (row + p.G) * D * E, q_bytes, lane);
+      if (!is_last) touch((const uint8_t*)p.q + (row + p.G) * D * E, q_bytes, lane);
 #pragma unroll 1
       for (int left = ntok; left > 0; left -= S::ST) {
         cp_wait<S::STAGES - 2>();
@@ -1049,7 +1075,6 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
         }
       }
       st.end();
-      const bool whole = f == us && se == ue, is_last = se == f1;
       if (whole) {
         st.store_out((uint8_t*)p.out + row * D * EO, p.lse ? p.lse + row : nullptr, p.G, lane);
       } else if (is_last) {
@@ -1057,22 +1082,23 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
         __syncwarp();
         st.store_record(tail_rec, p.G, lane);
       } else {                                  // the end of a unit that an earlier warp, or CTA, began
-        st.store_record(f == F0 ? cta_rec : head_rec, p.G, lane);
+        const bool from_before = c.us < F0 && wt.first_tile(F0 - c.us) == c.j;     // an earlier CTA, no earlier warp
+        st.store_record(from_before ? cta_rec : head_rec, p.G, lane);
       }
       if (lane == 0) {
         WarpInfo& wi = sh.info[warp];
-        if (f == f0) {
+        if (first) {
           wi.first_unit = unit;
-          wi.first_us = us;
-          wi.first_ue = ue;
+          wi.first_us = c.us;
+          wi.first_ul = ul;
         }
         wi.last_unit = unit;
-        wi.last_us = us;
-        wi.last_ue = ue;
+        wi.last_us = c.us;
+        wi.last_ul = ul;
       }
-      f = se;
+      first = false;
       if (is_last) break;
-      next_unit(tab, B, p.nlayers, p.g.N_kv, c);
+      next_unit(tab, c);
     }
     cp_wait<0>();
   }
@@ -1081,10 +1107,11 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
   // ---- Joins inside the CTA.  The warps whose last unit is the same share its join: each takes some of the
   // accumulators.  The states: those of these warps, and of the next one if it finished the unit and went on.  (A unit
   // that the CTA's first warp only finishes is one state, already where it belongs.)
-  const uint32_t busy = __ballot_sync(0xffffffffu, lane < kWarps && sh.info[lane < kWarps ? lane : 0].f0 < sh.info[lane < kWarps ? lane : 0].f1);
+  const uint32_t busy = __ballot_sync(0xffffffffu, lane < kWarps && sh.info[lane < kWarps ? lane : 0].busy);
+  if (busy == 0) return;
   const int first_warp = __ffs(busy) - 1, last_warp = 31 - __clz(busy);
-  const int64_t us = sh.info[warp].last_us, ue = sh.info[warp].last_ue;
-  if (f0 < f1 && !(us >= f0 && ue <= f1)) {
+  const int64_t us = sh.info[warp].last_us, ul = sh.info[warp].last_ul;
+  if (busy_warp && !(us >= f0 && ul < f1)) {
     const int unit = sh.info[warp].last_unit;
     const uint32_t same = busy & __ballot_sync(0xffffffffu, lane < kWarps && sh.info[lane < kWarps ? lane : 0].last_unit == unit);
     const int lead = __ffs(same) - 1, helpers = __popc(same), me = __popc(same & ((1u << warp) - 1u));
@@ -1096,7 +1123,7 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
     // state i, in token order (warps without tiles between them are left out: fewer tiles than warps)
     auto rec = [&](int i) -> const Record<D>* {
       return i == helpers ? records + 2 * grid + (cta * kWarps + extra)
-                          : (const Record<D>*)(smem + (F1 - F0 >= kWarps ? lead + i : (int)__fns(same, 0, i + 1)) * S::RING);
+                          : (const Record<D>*)(smem + (busy == (1u << kWarps) - 1u ? lead + i : (int)__fns(same, 0, i + 1)) * S::RING);
     };
     // statistics: lane = query head + 8 * (one of four states at a time)
     float* const weight = (float*)(smem + warp * S::RING + sizeof(Record<D>));        // [state][query head]
@@ -1126,7 +1153,7 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
     l += __shfl_xor_sync(0xffffffffu, l, 8);
     l += __shfl_xor_sync(0xffffffffu, l, 16);
     __syncwarp();
-    const bool open = us < F0 || ue > F1;
+    const bool open = us < F0 || ul >= F1;
     Record<D>* const to = cta_rec + (us < F0 ? 0 : 1);
     const int64_t row = (int64_t)unit * p.G;
     const float f = finish<FMT>(m, M, l);
@@ -1164,16 +1191,15 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
   // ---- Units shared between CTAs, at most one with earlier and one with later CTAs: the last to arrive joins.
   const WarpInfo& wa = sh.info[first_warp];
   const WarpInfo& wb = sh.info[last_warp];
-  const bool before = wa.first_us < F0, after = wb.last_us >= F0 && wb.last_ue > F1;
+  const bool before = wa.first_us < F0, after = wb.last_us >= F0 && wb.last_ul >= F1;
   if (!before && !after) return;
   __syncthreads();
   if (tid < 2) {
     bool all = false;
     if (tid == 0 ? before : after) {
-      const int64_t ts = tid == 0 ? wa.first_us : wb.last_us, te = tid == 0 ? wa.first_ue : wb.last_ue;
+      const int64_t ts = tid == 0 ? wa.first_us : wb.last_us, tl = tid == 0 ? wa.first_ul : wb.last_ul;
       uint32_t* const ticket = p.counters + (tid == 0 ? wa.first_unit : wb.last_unit);
-      // CTAs without tiles (fewer tiles than CTAs) take no part
-      const int n = total < grid ? (int)(te - ts) : split_owner(total, grid, te - 1) - split_owner(total, grid, ts) + 1;
+      const int n = sparse ? (int)(tl - ts) + 1 : split_owner(total, grid, tl) - split_owner(total, grid, ts) + 1;
       // after the barrier the whole CTA's states are ordered before this thread's release
       all = ticket_add(ticket) == (unsigned)(n - 1);
       if (all) *ticket = 0u;                    // ready for the next call
@@ -1184,9 +1210,9 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
 #pragma unroll 1
   for (int k = 0; k < 2; ++k) {
     if (!sh.arrived[k]) continue;
-    const int64_t ts = k == 0 ? wa.first_us : wb.last_us, te = k == 0 ? wa.first_ue : wb.last_ue;
+    const int64_t ts = k == 0 ? wa.first_us : wb.last_us, tl = k == 0 ? wa.first_ul : wb.last_ul;
     const int c0 = split_owner(total, grid, ts);
-    const int n = total < grid ? (int)(te - ts) : split_owner(total, grid, te - 1) - c0 + 1;
+    const int n = sparse ? (int)(tl - ts) + 1 : split_owner(total, grid, tl) - c0 + 1;
     const int64_t row = (int64_t)(k == 0 ? wa.first_unit : wb.last_unit) * p.G;
     // a warp takes 128 accumulators (four a lane, LPG lanes a query head) of every `slices`-th contributor
     constexpr int LPG = D / 4;
@@ -1197,7 +1223,7 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
     const int g = on ? e / D : 0;
     // the unit began in the first contributor (its record 1); for all others it is the unit that they began with
     auto record = [&](int i) -> const Record<D>* {
-      return records + 2 * (total < grid ? split_owner(total, grid, ts + i) : c0 + i) + (i == 0);
+      return records + 2 * (sparse ? split_owner(total, grid, ts + i) : c0 + i) + (i == 0);
     };
     constexpr int AHEAD = 6;                    // states whose accumulators come while the statistics are made
     float4 y[AHEAD];

@@ -1,5 +1,9 @@
-// How the flat tile list of a paged attention call is cut: N tiles over `grid` CTAs, a CTA's tiles over its warps.
-// Plain integer arithmetic, shared with the host's tests.
+// How the tiles of a paged attention call are cut over CTAs and warps.  Plain integer arithmetic, shared with the
+// host's tests.
+//
+// A unit (entry, layer, key head) of nt tiles takes tile_cost * nt + unit_cost places on a line: starting and ending a
+// unit costs about as much as half a tile.  Tile j stands at slot(j) of its unit's places.  The line is cut evenly, and
+// a part owns the tiles that stand in it.
 #pragma once
 #include <stdint.h>
 
@@ -15,9 +19,26 @@ namespace think {
 THINK_HD int64_t div_wide(int64_t a, int64_t b) {
   return (uint64_t)(a | b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
 }
-// part i of n tiles cut into `parts`: [split_begin(i), split_begin(i + 1)); n * parts fits 62 bits
+// part i of n places cut into `parts`: [split_begin(i), split_begin(i + 1)); n * parts fits 62 bits
 THINK_HD int64_t split_begin(int64_t n, int parts, int i) { return div_wide((int64_t)i * n, parts); }
-// the part that owns tile f, 0 <= f < n
+// the part that holds place f, 0 <= f < n
 THINK_HD int split_owner(int64_t n, int parts, int64_t f) { return (int)div_wide((f + 1) * parts - 1, n); }
+
+struct Weights {
+  int tile, unit;            // (2, 1), or (1, 0) where there are too few tiles to weigh
+  THINK_HD int cost(int nt) const { return tile * nt + unit; }
+  THINK_HD int tiles(int cost) const { return (cost - unit) / tile; }
+  // where tile j stands, and the first tile that stands at x or behind (may be none: nt or more)
+  THINK_HD int slot(int j) const { return j == 0 ? 0 : unit + tile * j; }
+  THINK_HD int first_tile(int64_t x) const {
+    if (x <= 0) return 0;
+    const int64_t j = (x - unit + tile - 1) / tile;
+    return j < 1 ? 1 : j > 0x7fffffff ? 0x7fffffff : (int)j;
+  }
+};
+// Any 3 neighbouring places hold a tile's under (2, 1), so no part of 3 or more is without one.
+THINK_HD Weights weights_for(int64_t tiles, int64_t units, int parts) {
+  return 2 * tiles + units >= 3 * (int64_t)parts ? Weights{2, 1} : Weights{1, 0};
+}
 
 }  // namespace think

@@ -130,9 +130,10 @@ int main() {
     assert out.strip() == "0"
 
 
-def test_split_of_tiles(tmp_path):
-    """Parts of a flat tile list are contiguous, differ by one tile at most, and the owner of a tile is the part that
-    holds it - at sizes of a few tiles and of 2^50."""
+def test_split_of_places(tmp_path):
+    """Parts of a line are contiguous, differ by one place at most, and the owner of a place is the part that holds
+    it - at lengths of a few places and of 2^50.  Tiles of a unit stand where `slot` says and are found again, and no
+    part of a weighted line is without a tile."""
     out = compile_and_run(tmp_path, r"""
 #include <stdio.h>
 #include "paged_split.h"
@@ -149,6 +150,28 @@ int main() {
           if (f >= a && f < b) bad += split_owner(n, parts, f) != i;
       }
     }
+  for (Weights w : {Weights{2, 1}, Weights{1, 0}})
+    for (int nt = 1; nt < 40; ++nt) {
+      bad += w.tiles(w.cost(nt)) != nt;
+      for (int64_t x = -2; x < w.cost(nt) + 3; ++x) {
+        int j = 0;
+        while (j < nt && w.slot(j) < x) ++j;
+        const int got = w.first_tile(x);
+        bad += j < nt ? got != j : got < nt;
+      }
+      bad += w.slot(nt - 1) >= w.cost(nt);
+    }
+  // places without a tile: never three in a row across units of any length
+  for (int a = 1; a < 6; ++a)
+    for (int b = 1; b < 6; ++b) {
+      const Weights w{2, 1};
+      bool at[64] = {};
+      for (int j = 0; j < a; ++j) at[w.slot(j)] = true;
+      for (int j = 0; j < b; ++j) at[w.cost(a) + w.slot(j)] = true;
+      at[w.cost(a) + w.cost(b)] = true;                      // a third unit
+      for (int i = 0; i + 2 < w.cost(a) + w.cost(b); ++i) bad += !at[i] && !at[i + 1] && !at[i + 2];
+    }
+  bad += weights_for(100, 100, 148).unit != 0 || weights_for(148, 148, 148).unit != 1 || weights_for(221, 1, 148).unit != 0;
   printf("%ld\n", bad);
 }
 """)
