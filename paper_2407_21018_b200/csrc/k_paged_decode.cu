@@ -71,15 +71,16 @@ struct Shape {
   static constexpr int RING = STAGES * STAGE;
   static_assert(STAGES >= 2 && WARPS <= kMaxWarps && WARPS >= kMaxG, "ring");
   // a warp's ring takes its partial state and the weights of a join afterwards, or a join's statistics
-  static_assert(RING >= (3 * kMaxG + kMaxG * (D + 4) + kMaxWarps * kMaxG) * 4 && RING >= kSMs * 2 * 16 + WARPS * 512, "ring");
+  static_assert(RING >= (4 * kMaxG + kMaxG * (D + 4) + kMaxWarps * kMaxG) * 4 && RING >= kSMs * 2 * 16 + WARPS * 512, "ring");
 };
 
-// Partial state of one (worker, unit): m[8], M[8], l[8], o[8][D].  m: running maximum of the logits (base 2); M: that
+// Partial state of one (worker, unit).  m: running maximum of the logits (base 2); M: that
 // of logit + exponent of the value's scale, the unit of the accumulators; l: sum of exp2(logit - m).
 // Rows are 4 floats longer than D: the lanes of a fragment, two rows apart, then store to different banks.
 template <int D>
 struct Record {
-  float m[kMaxG], M[kMaxG], l[kMaxG], o[kMaxG][D + 4];
+  float4 s[kMaxG];           // m, M, l
+  float o[kMaxG][D + 4];
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -632,11 +633,7 @@ struct MmaState {
     if (lane < 4) {
 #pragma unroll
       for (int i = 0; i < 2; ++i)
-        if (q0 + i < G) {
-          rec->m[q0 + i] = m[i];
-          rec->M[q0 + i] = M[i];
-          rec->l[q0 + i] = ls[i];
-        }
+        if (q0 + i < G) rec->s[q0 + i] = make_float4(m[i], M[i], ls[i], 0.f);
     }
     each(lane, [&](int c, const float (&a)[WIDTH], const float (&b)[WIDTH]) {
       if (q0 < G) put(&rec->o[q0][c], a);
@@ -822,11 +819,7 @@ struct F32State {
 #pragma unroll
     for (int g = 0; g < GP; ++g) {
       if (g >= G) break;
-      if (lane == (g * ST / R) << (5 - LB)) {
-        r->m[g] = m;
-        r->M[g] = m;
-        r->l[g] = l;
-      }
+      if (lane == (g * ST / R) << (5 - LB)) r->s[g] = make_float4(m, m, l, 0.f);
 #pragma unroll
       for (int i = 0; i < N; i += 2) *(float2*)&r->o[g][lane * N + i] = make_float2(o[g][i], o[g][i + 1]);
     }
@@ -1125,30 +1118,29 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
       return i == helpers ? records + 2 * grid + (cta * kWarps + extra)
                           : (const Record<D>*)(smem + (busy == (1u << kWarps) - 1u ? lead + i : (int)__fns(same, 0, i + 1)) * S::RING);
     };
-    // statistics: lane = query head + 8 * (one of four states at a time)
+    // statistics: lane = query head + 8 * (a quarter of the states)
     float* const weight = (float*)(smem + warp * S::RING + sizeof(Record<D>));        // [state][query head]
     const int g8 = lane & 7;
+    constexpr int QN = kWarps / 4 + 1;          // states of a lane at most
+    float4 t[QN];
     float m = -INFINITY, M = -INFINITY, l = 0.f;
-    if (g8 < p.G) {
-#pragma unroll 1
-      for (int i = lane >> 3; i < n; i += 4) {
-        const Record<D>* const r = rec(i);
-        m = fmaxf(m, r->m[g8]);
-        M = fmaxf(M, r->M[g8]);
-      }
+#pragma unroll
+    for (int k = 0; k < QN; ++k) {
+      const int i = (lane >> 3) + 4 * k;
+      t[k] = i < n && g8 < p.G ? rec(i)->s[g8] : make_float4(-INFINITY, -INFINITY, 0.f, 0.f);
+      m = fmaxf(m, t[k].x);
+      M = fmaxf(M, t[k].y);
     }
     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
     M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, 8));
     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
     M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, 16));
-    if (g8 < p.G) {
-      const float ms = m == -INFINITY ? 0.f : m, Ms = M == -INFINITY ? 0.f : M;
-#pragma unroll 1
-      for (int i = lane >> 3; i < n; i += 4) {
-        const Record<D>* const r = rec(i);
-        l += r->l[g8] * exp2f(r->m[g8] - ms);
-        weight[i * kMaxG + g8] = exp2f(r->M[g8] - Ms);
-      }
+    const float ms = m == -INFINITY ? 0.f : m, Ms = M == -INFINITY ? 0.f : M;
+#pragma unroll
+    for (int k = 0; k < QN; ++k) {
+      const int i = (lane >> 3) + 4 * k;
+      l = fmaf(t[k].z, ex2(t[k].x - ms), l);
+      if (i < n) weight[i * kMaxG + g8] = ex2(t[k].y - Ms);
     }
     l += __shfl_xor_sync(0xffffffffu, l, 8);
     l += __shfl_xor_sync(0xffffffffu, l, 16);
@@ -1159,9 +1151,7 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
     const float f = finish<FMT>(m, M, l);
     if (me == 0 && lane < p.G) {
       if (open) {
-        to->m[lane] = m;
-        to->M[lane] = M;
-        to->l[lane] = l;
+        to->s[lane] = make_float4(m, M, l, 0.f);
       } else if (p.lse) {
         p.lse[row + lane] = log_sum(m, l);
       }
@@ -1234,8 +1224,7 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
     float m = -INFINITY, M = -INFINITY, l = 0.f;
 #pragma unroll 1
     for (int i = lane % LPG; i < n; i += LPG) {
-      const Record<D>* const r = record(i);
-      const float4 x = make_float4(__ldcg(&r->m[g]), __ldcg(&r->M[g]), __ldcg(&r->l[g]), 0.f);
+      const float4 x = __ldcg(&record(i)->s[g]);
       st[i] = x;
       m = fmaxf(m, x.x);
       M = fmaxf(M, x.y);
@@ -1249,8 +1238,8 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
 #pragma unroll 1
     for (int i = lane % LPG; i < n; i += LPG) {
       const float4 x = st[i];
-      l += x.z * exp2f(x.x - ms);
-      st[i].y = exp2f(x.y - Ms);
+      l = fmaf(x.z, ex2(x.x - ms), l);
+      st[i].y = ex2(x.y - Ms);
     }
 #pragma unroll
     for (int o = 1; o < LPG; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
