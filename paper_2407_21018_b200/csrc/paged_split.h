@@ -1,9 +1,9 @@
 // How the tiles of a paged attention call are cut over CTAs and warps.  Plain integer arithmetic, shared with the
 // host's tests.
 //
-// A unit (entry, layer, key head) of nt tiles takes tile_cost * nt + unit_cost places on a line: starting and ending a
-// unit costs about as much as half a tile.  Tile j stands at slot(j) of its unit's places.  The line is cut evenly, and
-// a part owns the tiles that stand in it.
+// A unit (entry, layer, key head) of nt tiles takes tile * nt + unit places on a line: starting and ending a unit costs
+// time too.  Tile j stands at slot(j) of its unit's places.  The line is cut evenly, and a part owns the tiles that
+// stand in it.
 #pragma once
 #include <stdint.h>
 
@@ -25,7 +25,7 @@ THINK_HD int64_t split_begin(int64_t n, int parts, int i) { return div_wide((int
 THINK_HD int split_owner(int64_t n, int parts, int64_t f) { return (int)div_wide((f + 1) * parts - 1, n); }
 
 struct Weights {
-  int tile, unit;            // (2, 1), or (1, 0) where there are too few tiles to weigh
+  int tile, unit;
   THINK_HD int cost(int nt) const { return tile * nt + unit; }
   THINK_HD int tiles(int cost) const { return (cost - unit) / tile; }
   // where tile j stands, and the first tile that stands at x or behind (may be none: nt or more)
@@ -36,9 +36,10 @@ struct Weights {
     return j < 1 ? 1 : j > 0x7fffffff ? 0x7fffffff : (int)j;
   }
 };
-// Any 3 neighbouring places hold a tile's under (2, 1), so no part of 3 or more is without one.
-THINK_HD Weights weights_for(int64_t tiles, int64_t units, int parts) {
-  return 2 * tiles + units >= 3 * (int64_t)parts ? Weights{2, 1} : Weights{1, 0};
+// The weights `w`, or (1, 0) where there are too few tiles to weigh: any tile + unit neighbouring places hold a tile's,
+// so no part of that many is without one.
+THINK_HD Weights weights_for(Weights w, int64_t tiles, int64_t units, int parts) {
+  return w.tile * tiles + w.unit * units >= (int64_t)(w.tile + w.unit) * parts ? w : Weights{1, 0};
 }
 
 }  // namespace think

@@ -150,7 +150,7 @@ int main() {
           if (f >= a && f < b) bad += split_owner(n, parts, f) != i;
       }
     }
-  for (Weights w : {Weights{2, 1}, Weights{1, 0}})
+  for (Weights w : {Weights{4, 1}, Weights{2, 1}, Weights{1, 1}, Weights{1, 0}})
     for (int nt = 1; nt < 40; ++nt) {
       bad += w.tiles(w.cost(nt)) != nt;
       for (int64_t x = -2; x < w.cost(nt) + 3; ++x) {
@@ -161,17 +161,21 @@ int main() {
       }
       bad += w.slot(nt - 1) >= w.cost(nt);
     }
-  // places without a tile: never three in a row across units of any length
-  for (int a = 1; a < 6; ++a)
-    for (int b = 1; b < 6; ++b) {
-      const Weights w{2, 1};
-      bool at[64] = {};
-      for (int j = 0; j < a; ++j) at[w.slot(j)] = true;
-      for (int j = 0; j < b; ++j) at[w.cost(a) + w.slot(j)] = true;
-      at[w.cost(a) + w.cost(b)] = true;                      // a third unit
-      for (int i = 0; i + 2 < w.cost(a) + w.cost(b); ++i) bad += !at[i] && !at[i + 1] && !at[i + 2];
-    }
-  bad += weights_for(100, 100, 148).unit != 0 || weights_for(148, 148, 148).unit != 1 || weights_for(221, 1, 148).unit != 0;
+  // tile + unit places in a row always hold a tile's, across units of any length
+  for (Weights w : {Weights{4, 1}, Weights{1, 1}})
+    for (int a = 1; a < 6; ++a)
+      for (int b = 1; b < 6; ++b) {
+        bool at[64] = {};
+        for (int j = 0; j < a; ++j) at[w.slot(j)] = true;
+        for (int j = 0; j < b; ++j) at[w.cost(a) + w.slot(j)] = true;
+        at[w.cost(a) + w.cost(b)] = true;                    // a third unit
+        for (int i = 0; i < w.cost(a) + w.cost(b); ++i) {
+          bool any = false;
+          for (int k = 0; k < w.tile + w.unit; ++k) any |= at[i + k];
+          bad += i + w.tile + w.unit <= w.cost(a) + w.cost(b) + 1 && !any;
+        }
+      }
+  bad += weights_for({1, 1}, 100, 100, 148).unit != 0 || weights_for({1, 1}, 148, 148, 148).unit != 1 || weights_for({4, 1}, 184, 1, 148).unit != 0;
   printf("%ld\n", bad);
 }
 """)
