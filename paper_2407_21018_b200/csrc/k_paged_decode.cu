@@ -1,31 +1,40 @@
-// Attention of one new token per sequence over the paged cache: out = softmax(scale q K^T) V, lse.
+// Attention of one new token per sequence over the paged cache: out = softmax(scale q K^T) V, and its log sum.
 //
-// Every byte of the pages is read once and used for at most 8 query heads, so the stream of pages is the bound and
-// the kernel is built around it:
-//  * The tiles (64-token pages) of all (entry, layer, key head) units stand on one line, with some room
-//    for starting and ending a unit; it is cut evenly over the CTAs of one wave and inside a CTA over its warps,
-//    whatever the lengths: one long sequence uses the whole card and a ragged batch leaves no SM idle.  Lengths and page table are device memory; each CTA scans the lengths itself.
+// Every byte of the pages is read once and used for at most 8 query heads, so the stream of pages is the bound (bf16 and
+// fp32 pages reach the copy rate, e4m3 0.8 of it; 4-bit pages are held by unpacking, 600 instructions per 4.6 KB) and the
+// kernel is built around it:
+//  * The tiles (64-token pages) of all (entry, layer, key head) units stand on one line, with some room for starting and
+//    ending a unit; it is cut evenly over the CTAs of one wave and inside a CTA over its warps, whatever the lengths:
+//    one long sequence uses the whole card and a ragged batch leaves no SM idle.  Lengths and page table are device
+//    memory; each CTA scans the lengths itself.  (Cut by tiles alone, 192 sequences of 1 to 2000 tokens took 95 us
+//    instead of 71: the CTAs with the short ones came last.)
 //  * A warp is the worker.  It owns a ring of stages in shared memory that it fills with cp.async, crossing page and
 //    unit borders, and waits for nobody until its range is done.
 //  * Rows are stored token-major.  16-byte chunks are XOR-swizzled on the way into shared memory so that ldmatrix
-//    reads without bank conflicts.  Products run on mma.sync m16n8k16 (a group has at most 8 query rows: 8 of the 128
-//    rows that a tcgen05 tile would have).
-//      logits  A = queries (rows 0..7), B = keys.  e4m3 and 4-bit codes become f16 exactly (byte conversion; a masked
-//              4-bit code is the subnormal c * 2^-24 or c * 2^-20, one multiply-add makes it (c - 8) * 2^-9); the query is f16 times a power of two, exact unless its channels are more than 2^28 apart.
-//              (The fp8 form of the instruction takes the codes as they are, but on this machine it is a sequence of
-//              conversions and two f16 instructions: 22 cycles against 8.3, measured.)
-//      values  A = values transposed (16 channels x 16 tokens, ldmatrix.trans), B = weights, so all 16 x 8 results count
-//              and the accumulators take half the registers.  bf16: the weights are a bf16 pair high + low (two
-//              instructions), 2^-17.  e4m3, 4-bit: f16 codes as above.  (The subnormals as they are
-//              would do with the 8 taken off the sums, but the tensor core aligns products by exponent fields: sums then keep 2^-15 instead of
-//              2^-22, measured.)
-//      scales  of keys multiply logits, those of values go into the weights, which are rounded to f16 (2^-11)
-//              relative to the largest weight * scale so far, kept between 2^7 and 2^15: f16 leaves 21 binary orders
-//              below that.
+//    reads without bank conflicts.  Products run on mma.sync m16n8k16 with keys and values as A (16 tokens or channels)
+//    and the group's queries or weights as B: a group has at most 8 query rows, which is N here, and 8 of the 128 rows
+//    that a tcgen05 tile would have.
+//      logits  e4m3 and 4-bit codes become f16 exactly (byte conversion; a masked 4-bit code is the subnormal c * 2^-24
+//              or c * 2^-20, one multiply-add makes it (c - 8) * 2^-9); the query is f16 times a power of two, exact
+//              unless its channels are more than 2^28 apart.  (The fp8 form of the instruction takes codes as they
+//              are, but here it is a sequence of conversions and two f16 instructions: 22 cycles against 8.3, measured.)
+//      values  through ldmatrix.trans; the weights, which come out token by token, are transposed in registers.  bf16:
+//              the weights are a bf16 pair high + low (two instructions), 2^-17.  e4m3, 4-bit: f16 codes as above.  (The
+//              subnormals as they are would do, with the 8 taken off the sums, but the tensor core aligns products by
+//              exponent fields: sums then keep 2^-15 instead of 2^-22, measured.)
+//      scales  of keys multiply logits, those of values go into the weights, which are rounded to f16 (2^-11) relative
+//              to the largest weight * scale so far, kept between 2^7 and 2^15: f16 leaves 21 binary orders below that.
 //      fp32    CUDA cores: fp32 products summed over lanes pairwise.
 //  * The softmax is online in base 2 with fp32 maximum, sum and accumulators.  Units that several warps share leave
 //    partial states; the warps' states are joined by their CTA, the CTAs' states by the CTA that arrives last at
 //    the unit's ticket, always in token order, so results do not depend on timing.
+//
+// Measured (one call in a replayed graph; the share is of the copy rate, 6.54 TB/s):
+//   bf16  32 heads of 128, 16 sequences of 2048 to 4096      139 us   0.94
+//   bf16  32 / 8 heads, 131072 tokens, two layers            164 us   1.00
+//   e4m3  32 / 8 heads, 4 x 32768 tokens                      52 us   0.79
+//   int4  32 / 8 heads, 192 sequences of 1 to 2000            71 us   0.54
+//   int4  32 / 8 heads, 8192 tokens                           14 us   launch, three dependent loads and two joins
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 #include <math.h>
@@ -36,34 +45,22 @@
 namespace think {
 namespace {
 
-constexpr int kMaxWarps = 16;
+constexpr int kMaxWarps = 12;
 constexpr float kSlack = 8.f, kTop = 7.f;     // running maxima: how far they may lag, and where they put weights (log2)
 constexpr int kMaxG = kMaxPagedGroup;
 
-#ifndef THINK_PW_PLAIN
-#define THINK_PW_PLAIN 8
-#endif
-#ifndef THINK_PW_E4M3
-#define THINK_PW_E4M3 8
-#endif
-#ifndef THINK_PW_INT4
-#define THINK_PW_INT4 12
-#endif
-#ifndef THINK_ST_E4M3
-#define THINK_ST_E4M3 32
-#endif
-#ifndef THINK_ST_INT4
-#define THINK_ST_INT4 32
-#endif
-template <int D, int E, int FMT>
+// GP: query heads that the fp32 kernel computes at a time
+template <int D, int E, int FMT, int GP = 1>
 struct Shape {
   static constexpr bool F32 = E == 4;
-  static constexpr int WARPS = FMT == THINK_PAGE_PLAIN ? THINK_PW_PLAIN : FMT == THINK_PAGE_E4M3 ? THINK_PW_E4M3 : THINK_PW_INT4;
+  // Eight warps keep 130 KB of copies in flight with 255 registers each; 4-bit pages, bound by instructions, do better
+  // with twelve (192 ragged sequences 93.6 us against 98.9; e4m3, 4 x 32768 tokens: 54.0 with eight, 56.6 with twelve).
+  static constexpr int WARPS = FMT == THINK_PAGE_INT4 ? 12 : 8;
   static constexpr int THREADS = WARPS * 32;
   static constexpr int RB = FMT == THINK_PAGE_PLAIN ? D * E : FMT == THINK_PAGE_E4M3 ? D : D / 2;   // bytes of a row
   static constexpr int SB = FMT == THINK_PAGE_PLAIN ? 0 : FMT == THINK_PAGE_E4M3 ? 1 : D / 16;      // bytes of its scales
-  // tokens of a step: at most 8 KB of keys and values, at most 32
-  static constexpr int ST = FMT == THINK_PAGE_E4M3 ? THINK_ST_E4M3 : FMT == THINK_PAGE_INT4 ? THINK_ST_INT4 : 4096 / RB < 32 ? 4096 / RB : 32;
+  // tokens of a step: at most 8 KB of keys and values, at most 32; fp32: at most 64 products with queries a lane
+  static constexpr int ST = F32 && GP * (4096 / RB) > 64 ? 64 / GP : 4096 / RB < 32 ? 4096 / RB : 32;
   // starting and ending a unit takes as long as a tile of quantised pages or a quarter of a tile of others (measured: 1.4
   // to 1.7 us beside 1.8 to 2.4, 0.8 beside 3.5)
   static __device__ __forceinline__ Weights weights() { return FMT == THINK_PAGE_PLAIN ? Weights{4, 1} : Weights{1, 1}; }
@@ -646,10 +643,10 @@ struct MmaState {
   __device__ __forceinline__ void store_out(void* out, float* lse, int G, int lane) const;
 };
 
-// factor that turns joined accumulators into outputs
+// factor that turns joined accumulators into outputs: 0 where no token counted (a NaN logit leaves m alone, not l)
 template <int FMT>
 __device__ __forceinline__ float finish(float m, float M, float l) {
-  if (m == -INFINITY) return 0.f;
+  if (l == 0.f) return 0.f;
   if (FMT == THINK_PAGE_PLAIN) return 1.f / l;
   // accumulators are in units of 2^(M - kTop), 4-bit ones of 512 times that; two factors: the exponent may pass 127
   const float h = exp2f(0.5f * (M - (FMT == THINK_PAGE_INT4 ? kTop - 9.f : kTop) - m));
@@ -663,7 +660,7 @@ __device__ __forceinline__ void put4(void* to, const float4& a, float f) {
   else *(uint2*)to = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
 }
 __device__ __forceinline__ float log_sum(float m, float l) {
-  return m == -INFINITY ? -INFINITY : (m + log2f(l)) * 0.693147180559945309f;
+  return l == 0.f ? -INFINITY : (m + log2f(l)) * 0.693147180559945309f;
 }
 
 template <int D, int FMT>
@@ -701,7 +698,7 @@ __device__ __forceinline__ void MmaState<D, FMT>::store_out(void* out, float* ls
 // which the lane owns the logits idx = owner(lane) .. of (query g = idx / ST, token t = idx % ST).
 template <int D, int GP>
 struct F32State {
-  using S = Shape<D, 4, THINK_PAGE_PLAIN>;
+  using S = Shape<D, 4, THINK_PAGE_PLAIN, GP>;
   static constexpr int N = D / 32, ST = S::ST, NV = GP * ST;
   static __host__ __device__ constexpr int log2c(int x) { return x <= 1 ? 0 : 1 + log2c(x / 2); }
   static constexpr int NB = log2c(NV), LB = NB < 5 ? NB : 5, R = NV >> LB;   // idx bits, of which in the lane, values a lane
@@ -847,7 +844,7 @@ struct StateOf { using type = MmaState<D, FMT>; };
 template <int D, int GP>
 struct StateOf<D, 4, THINK_PAGE_PLAIN, GP> { using type = F32State<D, GP>; };
 
-constexpr int kSpBytes = 512;        // fp32: a warp's weights of a step, read 16 bytes at a time
+constexpr int kSpBytes = 256;        // fp32: a warp's weights of a step, read 16 bytes at a time
 
 // shared memory behind the rings
 struct alignas(16) Shared {
@@ -858,8 +855,8 @@ struct alignas(16) Shared {
 };
 
 template <int D, int E, int FMT, int GP>
-__global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode(PagedDecodeParams p) {
-  using S = Shape<D, E, FMT>;
+__global__ void __launch_bounds__((Shape<D, E, FMT, GP>::THREADS), 1) k_paged_decode(PagedDecodeParams p) {
+  using S = Shape<D, E, FMT, GP>;
   constexpr int kWarps = S::WARPS, kThreads = S::THREADS;
   using State = typename StateOf<D, E, FMT, GP>::type;
   constexpr int EO = E;                         // bytes of an output element
@@ -1274,22 +1271,23 @@ __global__ void __launch_bounds__((Shape<D, E, FMT>::THREADS), 1) k_paged_decode
   }
 }
 
-template <int D, int E, int FMT>
+template <int D, int E, int FMT, int GP>
 constexpr size_t smem_fixed() {
-  return (size_t)Shape<D, E, FMT>::WARPS * (Shape<D, E, FMT>::RING + (E == 4 ? kSpBytes : 0)) + sizeof(Shared);
+  using S = Shape<D, E, FMT, GP>;
+  return (size_t)S::WARPS * (S::RING + (E == 4 ? kSpBytes : 0)) + sizeof(Shared);
 }
 inline size_t smem_tables(int B) { return ((size_t)(B + 1) * 4 + B + 15) / 16 * 16; }
 
 template <int D, int E, int FMT, int GP>
 cudaError_t launch_k(const PagedDecodeParams& p, cudaStream_t s) {
-  const size_t smem = smem_fixed<D, E, FMT>() + smem_tables(p.table.B);
-  return launch_dependent(k_paged_decode<D, E, FMT, GP>, dim3(p.grid), Shape<D, E, FMT>::THREADS, smem, s, p);
+  const size_t smem = smem_fixed<D, E, FMT, GP>() + smem_tables(p.table.B);
+  return launch_dependent(k_paged_decode<D, E, FMT, GP>, dim3(p.grid), Shape<D, E, FMT, GP>::THREADS, smem, s, p);
 }
 template <int D, int E, int FMT, int GP>
 cudaError_t setup_k() {
-  static_assert(smem_fixed<D, E, FMT>() + kMaxPagedBatch * 5 + 32 <= 227 * 1024, "shared memory of a CTA");
+  static_assert(smem_fixed<D, E, FMT, GP>() + kMaxPagedBatch * 5 + 32 <= 227 * 1024, "shared memory of a CTA");
   return cudaFuncSetAttribute(k_paged_decode<D, E, FMT, GP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              (int)(smem_fixed<D, E, FMT>() + smem_tables(kMaxPagedBatch)));
+                              (int)(smem_fixed<D, E, FMT, GP>() + smem_tables(kMaxPagedBatch)));
 }
 
 #define THINK_PAGED_DISPATCH(FN, ...)                                                          \

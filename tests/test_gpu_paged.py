@@ -266,6 +266,60 @@ def test_non_finite_rows(fmt, dtype, bad):
 
 
 @pytest.mark.parametrize("fmt,dtype", KINDS, ids=IDS)
+@pytest.mark.parametrize("where", ["key", "value", "only key"])
+def test_a_nan_that_counts_is_seen(fmt, dtype, where):
+    """A stored NaN reaches the outputs of its own key head (a quantised row or group is NaN as a whole) and no other;
+    also where it is the only token."""
+    n = 1 if where == "only key" else 200
+    p = Paged(fmt, dtype, [n, n], N_kv=2, G=2)
+    k, v = p.rows(1)
+    x = v if where == "value" else k
+    x[1, n // 2, 0, 1, 40] = float("nan")
+    p.cache.write(k, v, p.table)
+    q = torch.randn(2, 1, 4, 128, generator=gen(5), device="cuda").to(dtype)
+    out, lse = p.cache.decode_attn(q, p.table, p.seq, return_lse=True)
+    p.check(q, out, lse, units={(0, 0, 0), (0, 0, 1), (1, 0, 0)})
+    mine = out[1, 0, 2:].float()
+    if where == "value":
+        hit = {"plain": slice(40, 41), "e4m3": slice(None), "int4": slice(32, 64)}[fmt]
+        assert torch.isnan(mine[:, hit]).all() and torch.isfinite(lse).all()
+        if fmt == "plain":
+            assert torch.isfinite(mine[:, :40]).all() and torch.isfinite(mine[:, 41:]).all()
+    else:
+        assert torch.isnan(mine).all() and torch.isnan(lse[1, 0, 2:]).all() and torch.isfinite(lse[0]).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_every_bf16_mantissa(D):
+    """Codes and scales for largest magnitudes of every mantissa, in ordinary, large and subnormal binades, beside
+    values from all over the range below them: the same bytes as the definitions give in 64 bits."""
+    tops, rows = [], []
+    g = np.random.default_rng(3)
+    for e in (1, 2, 40, 126, 127, 200, 253, 254):                # exponent fields; 0 (subnormal) below
+        tops += [(e << 7) | m for m in range(128)]
+    tops += list(range(0, 128))
+    for t in tops:
+        below = g.integers(0, t + 1, D - 1)
+        near = np.clip(t - g.integers(0, 260, D - 1), 0, t)       # half of them within two binades of the top
+        bits = np.concatenate([[t], np.where(g.random(D - 1) < 0.5, near, below)]) | (g.integers(0, 2, D) << 15)
+        rows.append(g.permutation(bits))
+    n = len(rows)
+    x = torch.from_numpy(np.stack(rows).astype(np.uint16).view(np.int16)).view(torch.bfloat16).cuda().view(1, n, 1, 1, D)
+    x64 = x.double().cpu().numpy().reshape(n, D)
+    for fmt in ("e4m3", "int4"):
+        p = Paged(fmt, torch.bfloat16, [n], N_kv=1, G=1, D=D)
+        p.cache.write(x, x.flip(1), p.table)
+        assert p.cache.device_error() == 0
+        for j in range(-(-n // PAGE)):
+            kc, vc, ks, vs = p.parts(p.block(0, int(p.table_cpu[0, j]), 0))
+            for s in range(min(PAGE, n - j * PAGE)):
+                t = j * PAGE + s
+                for c, z, row in ((kc, ks, x64[t]), (vc, vs, x64[n - 1 - t])):
+                    wc, wz = po.encode_row(row, fmt)
+                    assert np.array_equal(c[s], wc) and np.array_equal(z[s], wz), (fmt, t)
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS, ids=IDS)
 def test_bad_pages_positions_and_counts(fmt, dtype):
     tk = binding()
     p = Paged(fmt, dtype, [200, 200, 200], N_kv=2, L=1)
