@@ -372,9 +372,8 @@ struct MmaState {
     else
       asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sc[0]) : "r"(a));
   }
-  static __device__ __forceinline__ f32x2 scale_of(const uint32_t (&sc)[NG / 2], int g) {
-    const float s = (g & 1) ? bf16hi(sc[g >> 1]) : bf16lo(sc[g >> 1]);
-    return two(s, s);
+  static __device__ __forceinline__ float scale_of(const uint32_t (&sc)[NG / 2], int g) {
+    return (g & 1) ? bf16hi(sc[g >> 1]) : bf16lo(sc[g >> 1]);
   }
   static __device__ __forceinline__ uint32_t load_byte(uint32_t a) {
     uint32_t x;
@@ -442,8 +441,9 @@ struct MmaState {
           float c[4];
           mma_first<false>(c, int4_lo_to_f16x2(a), int4_lo_to_f16x2(b), int4_hi_to_f16x2(a), int4_hi_to_f16x2(b), q[g][0], q[g][1]);
           mma<false>(c, int4_lo_to_f16x2(ah), int4_lo_to_f16x2(bh), int4_hi_to_f16x2(ah), int4_hi_to_f16x2(bh), q[g][2], q[g][3]);
-          y0 = fma2(two(c[0], c[1]), scale_of(s0, g), y0);
-          y1 = fma2(two(c[2], c[3]), scale_of(s1, g), y1);
+          const float f0 = scale_of(s0, g), f1 = scale_of(s1, g);
+          y0 = fma2(two(c[0], c[1]), two(f0, f0), y0);
+          y1 = fma2(two(c[2], c[3]), two(f1, f1), y1);
         }
         x[n] = mul2(y0, rs);
         x[n + 1] = mul2(y1, rs);
@@ -454,10 +454,10 @@ struct MmaState {
       for (int n = 0; n < NT; ++n)
         if (8 * n + r >= ntok) x[n] = two(-INFINITY, -INFINITY);
     }
-    // ---- maxima of the logits and of logit + log2 of the value's scale.  For 4-bit rows the latter only has to keep
-    // weights within f16: it is the largest scale's bits read as a piecewise linear logarithm (low by < 0.09), 65536 +
-    // 127 too large until the end, which leaves it 7 fraction bits
-    f32x2 es[PLAIN || INT4 ? 1 : NT];
+    // ---- maxima of the logits and of logit + log2 of the value's scale.  For 4-bit rows that is the largest scale's
+    // bits read as a piecewise linear logarithm (low by < 0.09); the scales are divided by the same power below
+    f32x2 es[PLAIN ? 1 : NT];
+    float down[INT4 ? NT : 1];                  // 4-bit: 2^-(that logarithm) of token 8n + r
     float mx[2] = {-INFINITY, -INFINITY}, Mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -466,27 +466,26 @@ struct MmaState {
       mx[0] = fmaxf(mx[0], a);
       mx[1] = fmaxf(mx[1], b);
       if constexpr (!PLAIN) {
-        f32x2 e;
+        float e;
         if constexpr (INT4) {
           uint32_t sc[NG / 2], t;
           load_scales(vs + 8 * n * S::SB, sc);
           t = NG == 4 ? max_bf16x2(sc[0], sc[NG / 2 - 1]) : sc[0];
           t = max_bf16x2(t, __byte_perm(t, 0u, 0x1032));
-          const float f = __uint_as_float(__byte_perm(t, 0x4b000000u, 0x7410));    // 2^23 + bits
-          e = fma2(two(f, f), two(0.0078125f, 0.0078125f), x[n]);
+          e = fmaf(__uint_as_float(__byte_perm(t, 0x4b000000u, 0x7410)) - 8388608.f, 0.0078125f, -127.f);    // 2^23 + bits
+          down[n] = ex2(-e);
         } else {
-          const float f = magic(load_byte(vs + 8 * n)) - 8388735.f;
-          e = es[n] = add2(x[n], two(f, f));
+          e = magic(load_byte(vs + 8 * n)) - 8388735.f;
         }
-        split(e, a, b);
+        es[n] = add2(x[n], two(e, e));
+        split(es[n], a, b);
         Mx[0] = fmaxf(Mx[0], a);
         Mx[1] = fmaxf(Mx[1], b);
       }
     }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      if (PLAIN) Mx[i] = mx[i];
-      if (INT4) Mx[i] = fmaxf(Mx[i] - 65663.f, mx[i] - 100.f);       // (scales below 2^-100: the weight's other factor stays finite)
+    if (PLAIN) {
+      Mx[0] = mx[0];
+      Mx[1] = mx[1];
     }
     // the maxima in use move only when a token exceeds one 2^8 times: weights then stay below 2^15 (2^8 in fp32)
     if (__any_sync(0xffffffffu, mx[0] > m[0] + kSlack || mx[1] > m[1] + kSlack || Mx[0] > M[0] + kSlack || Mx[1] > M[1] + kSlack)) {
@@ -530,7 +529,7 @@ struct MmaState {
         w[j][1] = ex2(w[j][1]);
         l = add2(l, two(w[j][0], w[j][1]));
         if constexpr (!PLAIN) {
-          split(add2(INT4 ? x[2 * kk + j] : es[INT4 ? 0 : 2 * kk + j], Mr), w[j][0], w[j][1]);
+          split(add2(es[PLAIN ? 0 : 2 * kk + j], Mr), w[j][0], w[j][1]);
           w[j][0] = ex2(w[j][0]);
           w[j][1] = ex2(w[j][1]);
         }
@@ -576,9 +575,10 @@ struct MmaState {
 #pragma unroll
           for (int j = 0; j < 2; ++j) {         // a word: channels 4r .. 4r + 3 of token 2qd, the same of token 2qd + 1
             const int g = 2 * g2 + j;
+            const float f0 = scale_of(s0, g) * down[2 * kk], f1 = scale_of(s1, g) * down[2 * kk + 1];
             float f[4];
-            split(mul2(two(w[0][0], w[0][1]), scale_of(s0, g)), f[0], f[1]);
-            split(mul2(two(w[1][0], w[1][1]), scale_of(s1, g)), f[2], f[3]);
+            split(mul2(two(w[0][0], w[0][1]), two(f0, f0)), f[0], f[1]);
+            split(mul2(two(w[1][0], w[1][1]), two(f1, f1)), f[2], f[3]);
             const uint32_t b0 = transpose8(pack_f16(f[0], f[1])), b1 = transpose8(pack_f16(f[2], f[3]));
             const uint32_t a = v[2 * j], b = v[2 * j + 1], a8 = a >> 8, b8 = b >> 8;
             mma<false>(o[2 * g], int4_lo_to_f16x2(a), int4_hi_to_f16x2(a), int4_lo_to_f16x2(b), int4_hi_to_f16x2(b), b0, b1);

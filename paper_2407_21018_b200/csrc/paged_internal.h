@@ -103,7 +103,9 @@ inline cudaError_t launch_dependent(void (*kernel)(Params), dim3 grid, int threa
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, p);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p);
+  if (e != cudaSuccess) (void)cudaGetLastError();            // reported here, not by the caller's next check
+  return e;
 }
 
 #ifdef __CUDACC__

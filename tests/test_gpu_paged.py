@@ -447,6 +447,25 @@ def test_attention_large_logits_and_uneven_scales(fmt, dtype):
 
 
 @pytest.mark.parametrize("fmt,dtype", KINDS, ids=IDS)
+@pytest.mark.parametrize("power", [-100, 100, 118])
+def test_attention_values_of_any_magnitude(fmt, dtype, power):
+    """All value rows near the ends of the exponent range: small weights keep their share."""
+    p = Paged(fmt, dtype, [300], N_kv=1, G=4)
+    k, v = p.rows(83)
+    v = (v.float() * 2.0 ** power).to(dtype)
+    p.cache.write(k, v, p.table)
+    assert p.cache.device_error() == 0
+    q = torch.randn(1, 1, 4, 128, generator=gen(89), device="cuda").to(dtype)
+    out, lse = p.cache.decode_attn(q, p.table, p.seq, return_lse=True)
+    if power < 0:                                     # bounds in units of the values
+        for b, l, hs, want, wlse, tol, ltol in p.want(q):
+            err = np.abs(out.double().cpu().numpy()[b, l, hs] - want) * 2.0 ** -power
+            assert (err <= (tol - 1e-30) * 2.0 ** -power + 1e-6).all() and (np.abs(lse.double().cpu().numpy()[b, l, hs] - wlse) <= ltol).all()
+    else:
+        p.check(q, out, lse)
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS, ids=IDS)
 def test_attention_query_magnitudes(fmt, dtype):
     """Queries far from 1: all zero, tiny, and large against tiny keys; channels 2^30 apart in one row."""
     p = Paged(fmt, dtype, [150], N_kv=1, G=4)
