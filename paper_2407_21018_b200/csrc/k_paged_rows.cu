@@ -69,11 +69,12 @@ __device__ __forceinline__ uint32_t encode_int4(const uint4& w, uint32_t& sbits,
   if (s >= 1.17549435e-38f) {
     float inv;                                  // within an ulp
     asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(s));
+    const f32x2 inv2 = two(inv, inv), up = two(3072.f, 3072.f), down = two(-3072.f, -3072.f), magic = two(12582920.f, 12582920.f);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float a = __fadd_rn(__fadd_rn(__fmul_rn(bf16lo(ws[i]), inv), 3072.f), -3072.f);
-      const float b = __fadd_rn(__fadd_rn(__fmul_rn(bf16hi(ws[i]), inv), 3072.f), -3072.f);
-      c[i] = __float_as_uint(__fadd_rn(a, 12582920.f)) + (__float_as_uint(__fadd_rn(b, 12582920.f)) << 4);
+      float a, b;
+      split(add2(add2(add2(mul2(two(bf16lo(ws[i]), bf16hi(ws[i])), inv2), up), down), magic), a, b);
+      c[i] = __float_as_uint(a) + (__float_as_uint(b) << 4);
     }
   } else {
 #pragma unroll
@@ -96,12 +97,18 @@ __device__ __forceinline__ uint32_t decode_e4m3x2(uint32_t two, float s) {
   return pack2(f.x * s, f.y * s);
 }
 
-// 8 4-bit codes times their scale to bf16
+// 8 4-bit codes times their scale to bf16: a code as the low byte of 2^23 + code, less 2^23 + 8
 __device__ __forceinline__ uint4 decode_int4(uint32_t w, float f) {
-  auto one = [&](int i) {                       // 2^23 + code, less 2^23 + 8
-    return __fmul_rn(__fadd_rn(__uint_as_float((w >> (4 * i) & 15u) | 0x4b000000u), -8388616.f), f);
-  };
-  return make_uint4(pack2(one(0), one(1)), pack2(one(2), one(3)), pack2(one(4), one(5)), pack2(one(6), one(7)));
+  const uint32_t even = w & 0x0f0f0f0fu, odd = (w >> 4) & 0x0f0f0f0fu;
+  const f32x2 f2 = two(f, f), off = two(-8388616.f, -8388616.f);
+  uint32_t r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float a = __uint_as_float(__byte_perm(even, 0x4b000000u, 0x7440 | i)), b = __uint_as_float(__byte_perm(odd, 0x4b000000u, 0x7440 | i));
+    split(mul2(add2(two(a, b), off), f2), a, b);
+    r[i] = pack2(a, b);
+  }
+  return make_uint4(r[0], r[1], r[2], r[3]);
 }
 __device__ __forceinline__ uint4 decode_e4m3(const uint2& w, float f) {
   return make_uint4(decode_e4m3x2(w.x, f), decode_e4m3x2(w.x >> 16, f), decode_e4m3x2(w.y, f), decode_e4m3x2(w.y >> 16, f));
