@@ -331,7 +331,7 @@ thinK_status thinK_destroy(thinK_cache* c);
  *     64 key rows | 64 value rows | scales of the 64 key rows | scales of the 64 value rows
  * and a row is the D channels of one token in order (no swizzle, no padding):
  *   THINK_PAGE_PLAIN  the elements themselves (cfg.dtype), no scales.
- *   THINK_PAGE_E4M3   one e4m3 byte per channel, one scale byte per row: byte e stands for 2^(e - 127).  Written
+ *   THINK_PAGE_E4M3   one e4m3 byte per channel, one scale byte per row: byte e, 1 to 254, is 2^(e - 127).  Written
  *                     rows use the smallest power of two >= 2^-126 under which the row's largest magnitude is at
  *                     most 448; codes are x / scale rounded to nearest even.  bf16 caches only.
  *   THINK_PAGE_INT4   4 bits per channel (the even channel of a pair in the low half of the byte), code = n + 8,

@@ -551,6 +551,70 @@ def test_pool_past_32_bits():
     p.check(q, out, lse, units={(0, 1, 7), (1, 1, 7), (0, 0, 0), (1, 0, 3)})
 
 
+@pytest.mark.parametrize("fmt,dtype", KINDS, ids=IDS)
+def test_largest_batch(fmt, dtype):
+    """4096 sequences, most of them empty or a token long, a few of several pages."""
+    g = np.random.default_rng(5)
+    lens = [int(x) for x in g.choice([0, 0, 1, 2, 3], size=4096)]
+    for b, n in ((0, 130), (1000, 65), (4095, 300)):
+        lens[b] = n
+    p = Paged(fmt, dtype, lens, N_kv=1, G=5, D=64)
+    k, v = p.rows(3)
+    p.cache.write(k, v, p.table, rows=p.seq)
+    q = torch.randn(4096, 1, 5, 64, generator=gen(5), device="cuda").to(dtype)
+    out, lse = p.cache.decode_attn(q, p.table, p.seq, return_lse=True)
+    assert p.cache.device_error() == 0
+    p.check(q, out, lse, units={(b, 0, 0) for b in (*range(0, 4096, 97), 1000, 4095)})
+    none = torch.tensor(lens, device="cuda") == 0
+    assert (out[none] == 0).all() and torch.isneginf(lse[none]).all() and torch.isfinite(lse[~none]).all()
+    # all of them empty
+    zero = torch.zeros(4096, dtype=torch.int32, device="cuda")
+    out, lse = p.cache.decode_attn(q, p.table, zero, return_lse=True)
+    assert (out == 0).all() and torch.isneginf(lse).all()
+    assert torch.equal(p.cache.decode_attn(q, p.table, p.seq)[~none], p.cache.decode_attn(q, p.table, p.seq)[~none])
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS, ids=IDS)
+def test_shared_pages_and_explicit_stream(fmt, dtype):
+    """Two sequences that begin with the same page, and one whose table names a page twice; a stream by argument."""
+    p = Paged(fmt, dtype, [64, 200, 128], N_kv=2, G=6)
+    k, v = p.rows(3)
+    p.cache.write(k, v, p.table, rows=p.seq)
+    p.table[1, 0] = p.table[0, 0]
+    p.table_cpu[1, 0] = p.table_cpu[0, 0]
+    p.table[2, 1] = p.table[2, 0]
+    p.table_cpu[2, 1] = p.table_cpu[2, 0]
+    q = torch.randn(3, 1, 12, 128, generator=gen(5), device="cuda").to(dtype)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    out, lse = p.cache.decode_attn(q, p.table, p.seq, return_lse=True, stream=side)
+    ko, vo = torch.zeros_like(k), torch.zeros_like(v)
+    side.synchronize()
+    torch.cuda.synchronize()
+    p.cache.read(ko, vo, p.table, rows=p.seq, stream=side)
+    side.synchronize()
+    p.check(q, out, lse)
+    assert torch.equal(ko[1, :64], ko[0, :64]) and torch.equal(vo[2, 64:128], vo[2, :64])
+    assert p.cache.device_error() == 0
+
+
+def test_many_layers_and_rows_in_one_call():
+    """A call whose row count takes more than one launch (layers are split), with almost all rows unused."""
+    L, S = 160, 1 << 20
+    p = Paged("e4m3", torch.bfloat16, [40], L=L, N_kv=8, G=1, D=64)
+    k, v = (x.expand(1, 3, L, 8, 64).contiguous() for x in p.rows(3, 1))
+    n = torch.tensor([3], dtype=torch.int32, device="cuda")
+    p.cache.write(k[:, :1].expand(1, S, L, 8, 64), v[:, :1].expand(1, S, L, 8, 64), p.table, rows=n)
+    ko, vo = torch.zeros_like(k), torch.zeros_like(v)
+    p.cache.read(ko, vo, p.table, rows=n)
+    ref = Paged("e4m3", torch.bfloat16, [40], L=L, N_kv=8, G=1, D=64)
+    ref.cache.write(k, v, ref.table)
+    kr, vr = torch.zeros_like(k), torch.zeros_like(v)
+    ref.cache.read(kr, vr, ref.table)
+    assert torch.equal(p.pool, ref.pool) and torch.equal(ko, kr) and torch.equal(vo, vr)
+    assert p.cache.device_error() == 0
+
+
 # ---------------------------------------------------------------------------
 # streams, graphs, use together
 # ---------------------------------------------------------------------------
@@ -714,6 +778,11 @@ def test_refusals():
     refused(lambda: c.read(k, v.float(), p.table))
     odd = torch.zeros(2, 80, 2, 2, 129, dtype=torch.bfloat16, device="cuda")[..., :128]      # rows off 16 bytes
     refused(lambda: c.write(odd, v, p.table))
+    off = torch.zeros(q.numel() + 1, dtype=q.dtype, device="cuda")[1:].view(q.shape)        # not on 16 bytes
+    refused(lambda: c.decode_attn(off, p.table, p.seq))
+    refused(lambda: c.decode_attn(q, p.table, p.seq, out=off))
+    refused(lambda: c.decode_attn(q, p.table, p.seq, layer0=2, nlayers=0))
+    refused(lambda: c.write(k.as_strided((2, 1 << 30, 2, 2, 128), (0, 0, 0, 0, 1)), v.as_strided((2, 1 << 30, 2, 2, 128), (0, 0, 0, 0, 1)), p.table))
     refused(lambda: c.decode_attn(q.float(), p.table, p.seq))
     refused(lambda: c.decode_attn(q[:, :1], p.table, p.seq))
     refused(lambda: c.decode_attn(q[:, :, :2], p.table, p.seq))
