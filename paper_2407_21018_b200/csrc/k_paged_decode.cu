@@ -1047,6 +1047,8 @@ __global__ void __launch_bounds__((Shape<D, E, FMT, GP>::THREADS), 1) k_paged_de
       st.end();
       if (whole) {
         st.store_out((uint8_t*)p.out + row * D * EO, p.lse ? p.lse + row : nullptr, p.G, lane);
+      } else if (sparse) {                      // the CTA's only tile: nothing to join here
+        st.store_record(cta_rec + (c.us < F0 ? 0 : 1), p.G, lane);
       } else if (is_last) {
         cp_wait<0>();
         __syncwarp();
@@ -1081,19 +1083,24 @@ __global__ void __launch_bounds__((Shape<D, E, FMT, GP>::THREADS), 1) k_paged_de
   if (busy == 0) return;
   const int first_warp = __ffs(busy) - 1, last_warp = 31 - __clz(busy);
   const int64_t us = sh.info[warp].last_us, ul = sh.info[warp].last_ul;
-  if (busy_warp && !(us >= f0 && ul < f1)) {
+  if (busy_warp && !sparse && !(us >= f0 && ul < f1)) {
     const int unit = sh.info[warp].last_unit;
     const uint32_t same = busy & __ballot_sync(0xffffffffu, lane < kWarps && sh.info[lane < kWarps ? lane : 0].last_unit == unit);
-    const int lead = __ffs(same) - 1, helpers = __popc(same), me = __popc(same & ((1u << warp) - 1u));
+    const int helpers = __popc(same), me = __popc(same & ((1u << warp) - 1u));
+    uint64_t list = 0;                          // these warps, 4 bits each (with few tiles, not all neighbours have any)
+#pragma unroll
+    for (int v = 0, k = 0; v < kWarps; ++v)
+      if (same >> v & 1) {
+        list |= (uint64_t)v << k;
+        k += 4;
+      }
     const int end_warp = 32 - __clz(same);                             // behind the last of them
     const uint32_t on = busy >> end_warp << end_warp;                  // the next one that has tiles
     const int extra = on ? __ffs(on) - 1 : -1;
     const bool more = extra >= 0 && sh.info[extra].first_unit == unit;
     const int n = helpers + more;
-    // state i, in token order (warps without tiles between them are left out: fewer tiles than warps)
-    auto rec = [&](int i) -> const Record<D>* {
-      return i == helpers ? records + 2 * grid + (cta * kWarps + extra)
-                          : (const Record<D>*)(smem + (busy == (1u << kWarps) - 1u ? lead + i : (int)__fns(same, 0, i + 1)) * S::RING);
+    auto rec = [&](int i) -> const Record<D>* {                        // state i, in token order
+      return i == helpers ? records + 2 * grid + (cta * kWarps + extra) : (const Record<D>*)(smem + ((int)(list >> (4 * i)) & 15) * S::RING);
     };
     // statistics: lane = query head + 8 * (a quarter of the states)
     float* const weight = (float*)(smem + warp * S::RING + sizeof(Record<D>));        // [state][query head]
