@@ -69,7 +69,7 @@ struct Shape {
   static constexpr int SPACE = 200 * 1024 / WARPS;           // shared memory of a warp
   static constexpr int STAGES = SPACE / STAGE < 8 ? SPACE / STAGE : 8;
   static constexpr int RING = STAGES * STAGE;
-  static_assert(STAGES >= 2 && WARPS <= kMaxWarps && WARPS >= kMaxG, "ring");
+  static_assert(STAGES >= 2 && WARPS <= kMaxWarps && WARPS >= kMaxG && WARPS % 4 == 0, "ring");
   // a warp's ring takes its partial state and the weights of a join afterwards, or a join's statistics
   static_assert(RING >= (4 * kMaxG + kMaxG * (D + 4) + kMaxWarps * kMaxG) * 4 && RING >= kSMs * 2 * 16 + WARPS * 512, "ring");
 };
@@ -841,7 +841,10 @@ __global__ void __launch_bounds__((Shape<D, E, FMT, GP>::THREADS), 1) k_paged_de
   Shared& sh = *(Shared*)(smem + kWarps * (S::RING + (E == 4 ? kSpBytes : 0)));
   int* const cum = (int*)(&sh + 1);
   uint8_t* const last = (uint8_t*)(cum + p.table.B + 1);
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31;
+  // Which part of the CTA's tiles this warp takes.  Parts that are a tile larger come at regular distances; neighbours
+  // share a scheduler (the hardware's warps w, w + 4, ...), so that whatever the distance each gets its share of them.
+  const int warp = (tid >> 5 & 3) * (kWarps / 4) + (tid >> 7);
   const int B = p.table.B, LH = p.nlayers * p.g.N_kv, grid = gridDim.x, cta = blockIdx.x;
 
   begin_dependent();
@@ -874,12 +877,12 @@ __global__ void __launch_bounds__((Shape<D, E, FMT, GP>::THREADS), 1) k_paged_de
         y += yo;
       }
     }
-    if (lane == 31) sh.warp_sum[warp] = make_int2(x, y);
+    if (lane == 31) sh.warp_sum[tid >> 5] = make_int2(x, y);
     empty = __syncthreads_or(empty);
     int tiles = x - mine, seqs = y - some, all_tiles = 0, all_seqs = 0;
     for (int w = 0; w < kWarps; ++w) {
       const int2 t = sh.warp_sum[w];
-      if (w < warp) {
+      if (w < tid >> 5) {
         tiles += t.x;
         seqs += t.y;
       }
