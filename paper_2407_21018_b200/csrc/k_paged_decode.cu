@@ -61,9 +61,10 @@ struct Shape {
   static constexpr int SB = FMT == THINK_PAGE_PLAIN ? 0 : FMT == THINK_PAGE_E4M3 ? 1 : D / 16;      // bytes of its scales
   // tokens of a step: at most 8 KB of keys and values, at most 32; fp32: at most 64 products with queries a lane
   static constexpr int ST = F32 && GP * (4096 / RB) > 64 ? 64 / GP : 4096 / RB < 32 ? 4096 / RB : 32;
-  // starting and ending a unit takes as long as a tile of quantised pages or a quarter of a tile of others (measured: 1.4
-  // to 1.7 us beside 1.8 to 2.4, 0.8 beside 3.5)
-  static __device__ __forceinline__ Weights weights() { return FMT == THINK_PAGE_PLAIN ? Weights{4, 1} : Weights{1, 1}; }
+  // starting and ending a unit takes about as long as a tile of quantised pages or a quarter of a tile of others
+  // (measured: 1.4 to 1.7 us beside 1.8 to 2.4, 0.8 beside 3.5; half as much weight: 95 us instead of 84 for 192 ragged
+  // sequences of e4m3).  Two places a tile cut a little more evenly than one (4 x 32768 tokens 50.8 against 52.9 us).
+  static __device__ __forceinline__ Weights weights() { return FMT == THINK_PAGE_PLAIN ? Weights{4, 1} : Weights{2, 2}; }
   static constexpr int HALF = ST * RB;                       // key (or value) bytes of a stage
   static constexpr int STAGE = (2 * (HALF + ST * SB) + 127) / 128 * 128;
   static constexpr int SPACE = 200 * 1024 / WARPS;           // shared memory of a warp
@@ -993,14 +994,11 @@ __global__ void __launch_bounds__((Shape<D, E, FMT, GP>::THREADS), 1) k_paged_de
           for (int it = 0; it < IT; ++it) {
             const int r = S::F32 ? (it * 512 + lane * 16) / S::RB : it * RPI + r0;
             const uint32_t d = p_slot + (S::F32 ? it * 512 + lane * 16 : swz<S::RB>(r, ck));
-            const bool on = r < n;
-            cp16(d, on ? kl + it * 512 : p.pages, on ? 16 : 0);
-            cp16(d + S::HALF, on ? kl + kPageTokens * S::RB + it * 512 : p.pages, on ? 16 : 0);
+            const int bytes = r < n ? 16 : 0;   // (the address is in the pool in any case)
+            cp16(d, kl + it * 512, bytes);
+            cp16(d + S::HALF, kl + kPageTokens * S::RB + it * 512, bytes);
           }
-          if (S::SB > 0 && lane < 2 * SC) {
-            const int bytes = max(0, min(16, n * S::SB - s_at));
-            cp16(p_slot + s_dst, bytes ? p_scale + s_src : p.pages, bytes);
-          }
+          if (S::SB > 0 && lane < 2 * SC) cp16(p_slot + s_dst, p_scale + s_src, max(0, min(16, n * S::SB - s_at)));
         }
         if (lane == 0) *p_valid = n;
         p_ntok -= S::ST;

@@ -204,9 +204,9 @@ thinK_status thinK_paged_decode_attn(thinK_paged* p, const void* q, void* out, f
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(seq_len, 4)) return THINK_ERR_INVALID_ARG;
   if (scratch && !aligned(scratch, 256)) return THINK_ERR_INVALID_ARG;
   if (scratch && scratch_bytes < p->w.total) return THINK_ERR_CAPACITY;
-  // four places a tile and one a sequence are counted in 32 bits, over all layers and heads in 54
+  // four places a tile and two a sequence are counted in 32 bits, over all layers and heads in 54
   const int64_t tiles = (int64_t)table.B * table.max_pages;
-  if (4 * tiles + table.B > INT32_MAX || (double)tiles * nlayers * p->g.g.N_kv > 4.0e15) return THINK_ERR_UNSUPPORTED;
+  if (4 * tiles + 2 * (int64_t)table.B > INT32_MAX || (double)tiles * nlayers * p->g.g.N_kv > 4.0e15) return THINK_ERR_UNSUPPORTED;
   uint8_t* const ws = scratch ? (uint8_t*)scratch : p->ws;
   PagedDecodeParams d;
   memset((void*)&d, 0, sizeof(d));

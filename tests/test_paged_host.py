@@ -150,7 +150,7 @@ int main() {
           if (f >= a && f < b) bad += split_owner(n, parts, f) != i;
       }
     }
-  for (Weights w : {Weights{4, 1}, Weights{2, 1}, Weights{1, 1}, Weights{1, 0}})
+  for (Weights w : {Weights{4, 1}, Weights{2, 2}, Weights{1, 1}, Weights{1, 0}})
     for (int nt = 1; nt < 40; ++nt) {
       bad += w.tiles(w.cost(nt)) != nt;
       for (int64_t x = -2; x < w.cost(nt) + 3; ++x) {
@@ -162,7 +162,7 @@ int main() {
       bad += w.slot(nt - 1) >= w.cost(nt);
     }
   // tile + unit places in a row always hold a tile's, across units of any length
-  for (Weights w : {Weights{4, 1}, Weights{1, 1}})
+  for (Weights w : {Weights{4, 1}, Weights{2, 2}})
     for (int a = 1; a < 6; ++a)
       for (int b = 1; b < 6; ++b) {
         bool at[64] = {};
