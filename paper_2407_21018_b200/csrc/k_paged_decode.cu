@@ -72,7 +72,7 @@ struct Shape {
   static constexpr int RING = STAGES * STAGE;
   static_assert(STAGES >= 2 && WARPS <= kMaxWarps && WARPS >= kMaxG && WARPS % 4 == 0, "ring");
   // a warp's ring takes its partial state and the weights of a join afterwards, or a join's statistics
-  static_assert(RING >= (4 * kMaxG + kMaxG * (D + 4) + kMaxWarps * kMaxG) * 4 && RING >= kSMs * 2 * 16 + WARPS * 512, "ring");
+  static_assert(RING >= (4 * kMaxG + kMaxG * (D + 4) + kMaxWarps * kMaxG) * 4 && RING >= kSMs * 2 * 16 + 512, "ring");
 };
 
 // Partial state of one (worker, unit).  m: running maximum of the logits (base 2); M: that
@@ -1243,12 +1243,13 @@ __global__ void __launch_bounds__((Shape<D, E, FMT, GP>::THREADS), 1) k_paged_de
 #pragma unroll 4
       for (int i = slice + AHEAD * slices; i < n; i += slices) add(st[i].y, __ldcg((const float4*)&record(i)->o[g][e % D]));
     }
-    float4* const part = (float4*)(smem + chunk * S::RING + kSMs * 2 * sizeof(float4));     // [slice][lane]
-    if (slice > 0 && slice < slices) part[slice * 32 + lane] = a;
+    // a slice leaves its sums behind its statistics
+    auto part = [&](int s) { return (float4*)(smem + (s * chunks + chunk) * S::RING + kSMs * 2 * sizeof(float4)) + lane; };
+    if (slice > 0 && slice < slices) *part(slice) = a;
     __syncthreads();
     if (on && slice == 0) {
 #pragma unroll 1
-      for (int s = 1; s < slices; ++s) add(1.f, part[s * 32 + lane]);
+      for (int s = 1; s < slices; ++s) add(1.f, *part(s));
       put4<EO>((uint8_t*)p.out + (row * D + e) * EO, a, finish<FMT>(m, M, l));
       if (p.lse && e % D == 0) p.lse[row + g] = log_sum(m, l);
     }
