@@ -32,9 +32,9 @@
 // Measured (one call in a replayed graph; the share is of the copy rate, 6.54 TB/s):
 //   bf16  32 heads of 128, 16 sequences of 2048 to 4096      139 us   0.94
 //   bf16  32 / 8 heads, 131072 tokens, two layers            164 us   1.00
-//   e4m3  32 / 8 heads, 4 x 32768 tokens                      52 us   0.79
-//   int4  32 / 8 heads, 192 sequences of 1 to 2000            71 us   0.54
-//   int4  32 / 8 heads, 8192 tokens                           14 us   launch, three dependent loads and two joins
+//   e4m3  32 / 8 heads, 4 x 32768 tokens                      51 us   0.81
+//   int4  32 / 8 heads, 192 sequences of 1 to 2000            70 us   0.55
+//   int4  32 / 8 heads, 8192 tokens                           13 us   launch, three dependent loads and two joins
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 #include <math.h>
@@ -54,7 +54,8 @@ template <int D, int E, int FMT, int GP = 1>
 struct Shape {
   static constexpr bool F32 = E == 4;
   // Eight warps keep 130 KB of copies in flight with 255 registers each; 4-bit pages, bound by instructions, do better
-  // with twelve (192 ragged sequences 93.6 us against 98.9; e4m3, 4 x 32768 tokens: 54.0 with eight, 56.6 with twelve).
+  // with twelve (192 ragged sequences 69 us; 72 with eight; 76 with sixteen of 128 registers.  e4m3, 4 x 32768 tokens: 54
+  // with eight, 57 with twelve).
   static constexpr int WARPS = FMT == THINK_PAGE_INT4 ? 12 : 8;
   static constexpr int THREADS = WARPS * 32;
   static constexpr int RB = FMT == THINK_PAGE_PLAIN ? D * E : FMT == THINK_PAGE_E4M3 ? D : D / 2;   // bytes of a row
