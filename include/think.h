@@ -416,7 +416,7 @@ thinK_status thinK_paged_read(thinK_paged* p, thinK_tensor5 k, thinK_tensor5 v, 
 /* Attention of one new token per sequence over its first seq_len[b] tokens (append the token's own key and value
  * first): out = softmax(softmax_scale * q K^T) V for every query head, head h of the queries reading key head
  * h / (N_q / N_kv).
- *   q, out: dense [B, nlayers, N_q, D] in cfg.dtype, not overlapping.
+ *   q, out: dense [B, nlayers, N_q, D] in cfg.dtype.  q, out and lse may not overlap.
  *   lse:    fp32 [B, nlayers, N_q], the natural logarithm of the softmax's sum (for joining with attention over
  *           other tokens), or NULL.
  *   seq_len: device int32 [B].  A sequence without tokens gets out = 0 and lse = -infinity.
@@ -424,13 +424,15 @@ thinK_status thinK_paged_read(thinK_paged* p, thinK_tensor5 k, thinK_tensor5 v, 
  *           256-byte aligned, that was filled with zeros once before its first use (a call leaves it ready for the
  *           next).  Calls that may run at the same time - on two streams, or as two captured graphs - need a scratch
  *           buffer each.
+ * A call names at most 2^29 table entries (4 * B * max_pages + 2 * B below 2^31), THINK_ERR_UNSUPPORTED otherwise.
  * Logits, softmax sums and outputs are accumulated in fp32.  Results do not depend on timing: partial results are
  * joined in token order. */
 thinK_status thinK_paged_decode_attn(thinK_paged* p, const void* q, void* out, float* lse, thinK_page_table table,
                                      const int32_t* seq_len, void* scratch, size_t scratch_bytes, int32_t layer0,
                                      int32_t nlayers, void* stream);
 
-/* The handle's error word (bits 8 and 16 above), read with a synchronous copy. */
+/* The handle's error word (bits 8 and 16 above), read with a synchronous copy; wait for the calls that it is to cover
+ * first.  The word keeps its bits as long as the handle lives. */
 thinK_status thinK_paged_device_error(thinK_paged* p, int32_t* out_code);
 
 thinK_status thinK_paged_destroy(thinK_paged* p);

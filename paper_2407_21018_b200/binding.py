@@ -401,7 +401,7 @@ class PagedKVCache:
             raise ThinKError(ERR_INVALID_ARG, where + ": page table")
         rows, width = table.shape
         stride, step = table.stride()
-        if rows < B or (width > 1 and step != 1):
+        if rows < B or (width > 1 and step != 1) or width >> 31:
             raise ThinKError(ERR_INVALID_ARG, where + ": page table")
         return PageTable(table.data_ptr(), max(stride, width) if B == 1 else stride, width, B)
 
@@ -432,9 +432,11 @@ class PagedKVCache:
 
     def _rows(self, fn, where, k, v, table, pos, rows, layer0, nlayers, stream):
         n = self._L - layer0 if nlayers is None else nlayers
+        if (n | layer0) >> 31:                 # (a C int would wrap around)
+            raise ThinKError(ERR_INVALID_ARG, where + ": layers")
         k5, v5 = self._rows_view(k, n, where), self._rows_view(v, n, where)
         B, max_rows = k.shape[:2]
-        if v.shape[:2] != (B, max_rows):
+        if v.shape[:2] != (B, max_rows) or max_rows >> 31:
             raise ThinKError(ERR_INVALID_ARG, where + ": rows")
         self._call(fn, where, k5, v5, self._table(table, B, where), self._vector(pos, B, where + ": pos"),
                    self._vector(rows, B, where + ": rows"), max_rows, layer0, n,
@@ -458,11 +460,19 @@ class PagedKVCache:
         out, or (out, lse) when lse (fp32 [B, nlayers, N_q]) is given or asked for."""
         where = "thinK_paged_decode_attn"
         n = self._L - layer0 if nlayers is None else nlayers
+        if (n | layer0) >> 31:
+            raise ThinKError(ERR_INVALID_ARG, where + ": layers")
         shape = q.shape
         if (len(shape) != 4 or shape[1] != n or shape[2] != self._N_q or shape[3] != self._D
                 or q.dtype != self.torch_dtype or q.get_device() != self._index or not q.is_contiguous()):
             raise ThinKError(ERR_INVALID_ARG, where + ": q")
         B = shape[0]
+        if stream is not None:                 # results in memory that this stream's earlier work has left
+            with torch.cuda.stream(stream):
+                if out is None:
+                    out = torch.empty_like(q)
+                if lse is None and return_lse:
+                    lse = q.new_empty(shape[:3], dtype=torch.float32)
         if out is None:
             out = torch.empty_like(q)
         elif out.shape != shape or out.dtype != q.dtype or out.get_device() != self._index or not out.is_contiguous():

@@ -858,7 +858,7 @@ __global__ void __launch_bounds__((Shape<D, E, FMT, GP>::THREADS), 1) k_paged_de
     const int cap = p.table.max_pages * kPageTokens;
     int mine = 0, some = 0;                     // tiles, sequences that have any
     for (int b = b0; b < b1; ++b) {
-      int n = __ldg(p.seq_len + b);
+      int n = load_now(p.seq_len + b);
       if (n > cap) {
         n = cap;
         if (cta == 0) atomicOr(p.error, kErrPage);
@@ -866,7 +866,7 @@ __global__ void __launch_bounds__((Shape<D, E, FMT, GP>::THREADS), 1) k_paged_de
       const int nt = n > 0 ? (n + kPageTokens - 1) / kPageTokens : 0;
       empty |= nt == 0;
       some += nt > 0;
-      last[b] = (uint8_t)((n - 1) & (kPageTokens - 1));
+      last[b] = (uint8_t)((n + kPageTokens - 1) & (kPageTokens - 1));
       cum[b + 1] = nt;
       mine += nt;
     }
@@ -943,7 +943,7 @@ __global__ void __launch_bounds__((Shape<D, E, FMT, GP>::THREADS), 1) k_paged_de
     typename State::Raw raw;                    // the first unit's queries, asked for ahead of the pages
     State::fetch((const uint8_t*)p.q + (int64_t)(pc.b * LH + pc.ll * p.g.N_kv + pc.h) * q_bytes, p.G, lane, raw);
     const int32_t* p_entry = p.table.table + pc.b * p.table.stride + pc.j;       // table entry of the next tile
-    int p_page = __ldg(p_entry);                // looked up a tile ahead
+    int p_page = load_now(p_entry);                // looked up a tile ahead
     const uint8_t* p_base = p.pages + page_block_offset(p.g, p.layer0 + pc.ll, 0, pc.h);    // of the unit
     int p_tiles = min(pc.nt, wt.first_tile(f1 - pc.us)) - pc.j;                  // of the unit, not begun
     int p_toks = pc.len - pc.j * kPageTokens;                                    // of the unit, not begun
@@ -968,7 +968,7 @@ __global__ void __launch_bounds__((Shape<D, E, FMT, GP>::THREADS), 1) k_paged_de
         p_tiles = min(pc.nt, wt.first_tile(f1 - pc.us));
         p_toks = pc.len;
       }
-      if (p_tiles > 0) p_page = __ldg(p_entry);
+      if (p_tiles > 0) p_page = load_now(p_entry);
     };
     constexpr int CPR = S::RB / 16, RPI = 32 / CPR > 0 ? 32 / CPR : 1, IT = S::HALF / 512;
     constexpr int SC = S::SB > 0 ? S::ST * S::SB / 16 : 1;   // 16-byte pieces of a step's key scales

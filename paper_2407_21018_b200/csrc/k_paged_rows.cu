@@ -69,7 +69,8 @@ __device__ __forceinline__ uint32_t encode_int4(const uint4& w, uint32_t& sbits,
   if (s >= 1.17549435e-38f) {
     float inv;                                  // within an ulp
     asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(s));
-    const f32x2 inv2 = two(inv, inv), up = two(3072.f, 3072.f), down = two(-3072.f, -3072.f), magic = two(12582920.f, 12582920.f);
+    constexpr float kTo12 = 1.5f * 2048.f;
+    const f32x2 inv2 = two(inv, inv), up = two(kTo12, kTo12), down = two(-kTo12, -kTo12), magic = two(12582920.f, 12582920.f);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float a, b;
@@ -125,8 +126,8 @@ __global__ void __launch_bounds__(kRowThreads) k_paged_rows(PagedRowsParams p) {
   constexpr int SB = FMT == THINK_PAGE_PLAIN ? 0 : FMT == THINK_PAGE_E4M3 ? 1 : D / 16;
   begin_dependent();
   const int b = blockIdx.y;
-  const int nrows_raw = p.rows ? __ldg(p.rows + b) : p.max_rows;
-  const int pos = p.pos ? __ldg(p.pos + b) : 0;
+  const int nrows_raw = p.rows ? load_now(p.rows + b) : p.max_rows;
+  const int pos = p.pos ? load_now(p.pos + b) : 0;
   const int nrows = min(nrows_raw, p.max_rows);
   if (blockIdx.x == 0 && threadIdx.x == 0 && nrows_raw > p.max_rows) atomicOr(p.error, kErrPage);
   const uint32_t first = blockIdx.x * RPB;

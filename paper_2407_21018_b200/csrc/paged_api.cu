@@ -18,6 +18,9 @@ struct Range {
 };
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  return a && b && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
 inline bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
 struct Geometry {
@@ -204,6 +207,9 @@ thinK_status thinK_paged_decode_attn(thinK_paged* p, const void* q, void* out, f
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(seq_len, 4)) return THINK_ERR_INVALID_ARG;
   if (scratch && !aligned(scratch, 256)) return THINK_ERR_INVALID_ARG;
   if (scratch && scratch_bytes < p->w.total) return THINK_ERR_CAPACITY;
+  // queries are read until the last output is written
+  const size_t heads = (size_t)table.B * nlayers * p->g.N_q, bytes = heads * p->g.g.D * p->g.elem;
+  if (overlap(q, bytes, out, bytes) || overlap(lse, heads * 4, q, bytes) || overlap(lse, heads * 4, out, bytes)) return THINK_ERR_INVALID_ARG;
   // four places a tile and two a sequence are counted in 32 bits, over all layers and heads in 54
   const int64_t tiles = (int64_t)table.B * table.max_pages;
   if (4 * tiles + 2 * (int64_t)table.B > INT32_MAX || (double)tiles * nlayers * p->g.g.N_kv > 4.0e15) return THINK_ERR_UNSUPPORTED;

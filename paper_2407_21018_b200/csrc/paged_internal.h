@@ -117,10 +117,18 @@ __device__ __forceinline__ void begin_dependent() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
+// A load that stays behind begin_dependent() and does not go by the read-only path: what it reads may have been written
+// by a kernel that was still running when this one was set up.
+__device__ __forceinline__ int32_t load_now(const int32_t* p) {
+  int32_t x;
+  asm volatile("ld.global.s32 %0, [%1];" : "=r"(x) : "l"(p));
+  return x;
+}
+
 // Page that holds token t of entry b, or -1 (error bit) if the table or the position is out of range.
 __device__ __forceinline__ int page_of(const PageTableView& t, const PageGeom& g, int b, int64_t tok, uint32_t* error) {
   int page = -1;
-  if (tok >= 0 && tok < (int64_t)t.max_pages * kPageTokens) page = __ldg(t.table + b * t.stride + (tok >> 6));
+  if (tok >= 0 && tok < (int64_t)t.max_pages * kPageTokens) page = load_now(t.table + b * t.stride + (tok >> 6));
   if ((uint32_t)page >= (uint32_t)g.num_pages) {
     atomicOr(error, kErrPage);
     return -1;

@@ -1,5 +1,9 @@
 """GPU tests of the paged key-value cache against the fp64 oracle: stored bytes and read-back bit-exact, attention
 within bounds that are derived from the kernels' roundings (see `bounds`)."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -742,6 +746,73 @@ def test_lse_joins_two_parts():
     # each part carries half a bf16 step of itself, the whole half a step of itself
     tol = 2.0 ** -8 * (w0 * o0.float().abs() + w1 * o1.float().abs() + whole.float().abs()) * 1.01 + 2.0 ** -10
     assert ((joined - whole.float()).abs() <= tol).all()
+
+
+def test_buffers_that_overlap_and_counts_past_32_bits_are_refused():
+    tk = binding()
+    p = Paged("plain", torch.float32, [70, 80], L=2, N_kv=2, G=2)
+    c, n = p.cache, 2 * 2 * 4 * 128
+    mem = torch.zeros(2 * n, device="cuda")
+    q = mem[:n].view(2, 2, 4, 128)
+    before = p.pool.clone()
+
+    def refused(call):
+        with pytest.raises(tk.ThinKError) as e:
+            call()
+        assert e.value.status == tk.ERR_INVALID_ARG
+
+    refused(lambda: c.decode_attn(q, p.table, p.seq, out=q))
+    refused(lambda: c.decode_attn(q, p.table, p.seq, out=mem[n - 4:2 * n - 4].view(q.shape)))
+    refused(lambda: c.decode_attn(q, p.table, p.seq, lse=mem[n - 1:n + 15].view(2, 2, 4)))
+    refused(lambda: c.decode_attn(q, p.table, p.seq, out=mem[n:].view(q.shape), lse=mem[2 * n - 16:].view(2, 2, 4)))
+    k, v = p.rows(3)
+    long = k[:, :1].expand(2, 1 << 32, 2, 2, 128)
+    refused(lambda: c.write(long, long, p.table))
+    refused(lambda: c.write(k, v, p.table, layer0=1 << 32, nlayers=2))
+    refused(lambda: c.decode_attn(q, p.table, p.seq, layer0=1 << 32, nlayers=2))
+    wide = p.table[:, :1].expand(2, 1 << 32)
+    refused(lambda: c.write(k, v, wide))
+    assert torch.equal(p.pool, before) and c.device_error() == 0
+    # side by side is not overlapping (the pool was NaN so far)
+    c.write(k, v, p.table, rows=p.seq)
+    got = c.decode_attn(q, p.table, p.seq, out=mem[n:].view(q.shape))
+    assert torch.isfinite(got).all() and torch.equal(got, c.decode_attn(q, p.table, p.seq))
+
+
+@pytest.mark.parametrize("fmt,dtype", [("plain", "float32"), ("int4", "bfloat16")])
+def test_first_calls_of_a_process_in_a_captured_graph(fmt, dtype):
+    """Nothing of a call depends on an earlier one: kernels that never ran may be captured."""
+    code = f"""
+import torch
+from paper_2407_21018_b200 import binding as tk
+dt = torch.{dtype}
+cfg = tk.make_paged_config(2, 4, 2, 128, 8, 2, dt, tk.PAGE_{fmt.upper()})
+c = tk.PagedKVCache(cfg)
+g = torch.Generator().manual_seed(3)
+k, v = (torch.randn(2, 90, 2, 2, 128, generator=g).to(dt).cuda() for _ in range(2))
+k2, v2 = torch.zeros_like(k), torch.zeros_like(v)
+q = torch.randn(2, 2, 4, 128, generator=g).to(dt).cuda()
+out = torch.zeros_like(q)
+table = torch.arange(4, dtype=torch.int32).view(2, 2).cuda()
+seq = torch.tensor([90, 33], dtype=torch.int32).cuda()
+graph = torch.cuda.CUDAGraph()
+torch.cuda.synchronize()
+with torch.cuda.graph(graph):
+    c.write(k, v, table, rows=seq)
+    c.decode_attn(q, table, seq, out=out)
+    c.read(k2, v2, table, rows=seq)
+graph.replay()
+torch.cuda.synchronize()
+want = c.decode_attn(q, table, seq)
+assert torch.equal(out, want) and out.abs().sum() > 0 and c.device_error() == 0
+k3, v3 = torch.zeros_like(k), torch.zeros_like(v)
+c.read(k3, v3, table, rows=seq)
+assert torch.equal(k2, k3) and torch.equal(v2, v3) and k2[0].abs().sum() > 0 and not k2[1, 33:].any()
+print("same")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "same" in r.stdout, r.stdout + r.stderr
 
 
 def test_refusals():
