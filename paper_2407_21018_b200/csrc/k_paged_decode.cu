@@ -30,10 +30,10 @@
 //    the unit's ticket, always in token order, so results do not depend on timing.
 //
 // Measured (one call in a replayed graph; the share is of the copy rate, 6.54 TB/s):
-//   bf16  32 heads of 128, 16 sequences of 2048 to 4096      139 us   0.94
+//   bf16  32 heads of 128, 16 sequences of 2048 to 4096      138 us   0.95
 //   bf16  32 / 8 heads, 131072 tokens, two layers            164 us   1.00
-//   e4m3  32 / 8 heads, 4 x 32768 tokens                      51 us   0.81
-//   int4  32 / 8 heads, 192 sequences of 1 to 2000            70 us   0.55
+//   e4m3  32 / 8 heads, 4 x 32768 tokens                      51 us   0.82
+//   int4  32 / 8 heads, 192 sequences of 1 to 2000            68 us   0.56
 //   int4  32 / 8 heads, 8192 tokens                           13 us   launch, three dependent loads and two joins
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -54,7 +54,7 @@ template <int D, int E, int FMT, int GP = 1>
 struct Shape {
   static constexpr bool F32 = E == 4;
   // Eight warps keep 130 KB of copies in flight with 255 registers each; 4-bit pages, bound by instructions, do better
-  // with twelve (192 ragged sequences 69 us; 72 with eight; 76 with sixteen of 128 registers.  e4m3, 4 x 32768 tokens: 54
+  // with twelve (192 ragged sequences 70 us; 72 with eight; 76 with sixteen of 128 registers.  e4m3, 4 x 32768 tokens: 54
   // with eight, 57 with twelve).
   static constexpr int WARPS = FMT == THINK_PAGE_INT4 ? 12 : 8;
   static constexpr int THREADS = WARPS * 32;
@@ -1183,17 +1183,22 @@ __global__ void __launch_bounds__((Shape<D, E, FMT, GP>::THREADS), 1) k_paged_de
     sh.arrived[tid] = all;
   }
   __syncthreads();
+  // a warp takes 128 accumulators (four a lane, LPG lanes a query head) of every `slices`-th contributor; half the warps
+  // take the one unit and half the other if there are enough of them (one after the other, the CTAs that end last cost 1
+  // to 2 us more: 192 ragged sequences of 4 bits 69.7 us, now 67.9)
+  constexpr int LPG = D / 4;
+  const int chunks = (p.G * D + 127) / 128;
+  const bool halves = sh.arrived[0] && sh.arrived[1] && 2 * chunks <= kWarps;
+  const int team = halves ? kWarps / 2 : kWarps, team0 = warp - warp % team, slices = team / chunks;
+  const int chunk = (warp - team0) % chunks, slice = (warp - team0) / chunks;
 #pragma unroll 1
-  for (int k = 0; k < 2; ++k) {
+  for (int round = 0; round < (halves ? 1 : 2); ++round) {
+    const int k = halves ? team0 > 0 : round;
     if (!sh.arrived[k]) continue;
     const int64_t ts = k == 0 ? wa.first_us : wb.last_us, tl = k == 0 ? wa.first_ul : wb.last_ul;
     const int c0 = split_owner(total, grid, ts);
     const int n = sparse ? (int)(tl - ts) + 1 : split_owner(total, grid, tl) - c0 + 1;
     const int64_t row = (int64_t)(k == 0 ? wa.first_unit : wb.last_unit) * p.G;
-    // a warp takes 128 accumulators (four a lane, LPG lanes a query head) of every `slices`-th contributor
-    constexpr int LPG = D / 4;
-    const int chunks = (p.G * D + 127) / 128, slices = kWarps / chunks;
-    const int chunk = warp % chunks, slice = warp / chunks;
     const int e = 128 * chunk + 4 * lane;
     const bool on = e < p.G * D && slice < slices;
     const int g = on ? e / D : 0;
@@ -1245,7 +1250,7 @@ __global__ void __launch_bounds__((Shape<D, E, FMT, GP>::THREADS), 1) k_paged_de
       for (int i = slice + AHEAD * slices; i < n; i += slices) add(st[i].y, __ldcg((const float4*)&record(i)->o[g][e % D]));
     }
     // a slice leaves its sums behind its statistics
-    auto part = [&](int s) { return (float4*)(smem + (s * chunks + chunk) * S::RING + kSMs * 2 * sizeof(float4)) + lane; };
+    auto part = [&](int s) { return (float4*)(smem + (team0 + s * chunks + chunk) * S::RING + kSMs * 2 * sizeof(float4)) + lane; };
     if (slice > 0 && slice < slices) *part(slice) = a;
     __syncthreads();
     if (on && slice == 0) {
