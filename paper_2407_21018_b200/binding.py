@@ -348,6 +348,7 @@ def paged_offset(cfg: PagedConfig, layer: int, page: int, head: int, slot: int, 
     return int(lib.thinK_paged_offset(C.byref(cfg), layer, page, head, slot, part))
 
 
+_INT32 = torch.int32
 _current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
@@ -397,7 +398,7 @@ class PagedKVCache:
 
     # -- argument marshalling -------------------------------------------
     def _table(self, table: torch.Tensor, B: int, where: str) -> PageTable:
-        if table.dtype != torch.int32 or table.dim() != 2 or table.get_device() != self._index:
+        if table.dtype is not _INT32 or table.dim() != 2 or table.get_device() != self._index:
             raise ThinKError(ERR_INVALID_ARG, where + ": page table")
         rows, width = table.shape
         stride, step = table.stride()
@@ -405,12 +406,12 @@ class PagedKVCache:
             raise ThinKError(ERR_INVALID_ARG, where + ": page table")
         return PageTable(table.data_ptr(), max(stride, width) if B == 1 else stride, width, B)
 
-    def _vector(self, x: Optional[torch.Tensor], B: int, where: str):
+    def _vector(self, x: Optional[torch.Tensor], B: int, where: str, what: str):
         if x is None:
             return None
-        if (x.dtype != torch.int32 or x.dim() != 1 or x.shape[0] < B or x.get_device() != self._index
+        if (x.dtype is not _INT32 or x.dim() != 1 or x.numel() < B or x.get_device() != self._index
                 or (B > 1 and x.stride(0) != 1)):
-            raise ThinKError(ERR_INVALID_ARG, where)
+            raise ThinKError(ERR_INVALID_ARG, where + what)
         return x.data_ptr()
 
     def _call(self, fn, where: str, *args):
@@ -423,24 +424,23 @@ class PagedKVCache:
         if status != THINK_OK:
             raise ThinKError(status, where)
 
-    def _rows_view(self, x: torch.Tensor, n: int, where: str) -> Tensor5:
-        shape, stride = x.shape, x.stride()
-        if (len(shape) != 5 or shape[2] != n or shape[3] != self._N_kv or shape[4] != self._D or stride[4] != 1
-                or x.dtype != self.torch_dtype or x.get_device() != self._index):
-            raise ThinKError(ERR_INVALID_ARG, where + ": rows")
-        return Tensor5(x.data_ptr(), stride[0], stride[1], stride[2], stride[3])
-
     def _rows(self, fn, where, k, v, table, pos, rows, layer0, nlayers, stream):
         n = self._L - layer0 if nlayers is None else nlayers
         if (n | layer0) >> 31:                 # (a C int would wrap around)
             raise ThinKError(ERR_INVALID_ARG, where + ": layers")
-        k5, v5 = self._rows_view(k, n, where), self._rows_view(v, n, where)
-        B, max_rows = k.shape[:2]
-        if v.shape[:2] != (B, max_rows) or max_rows >> 31:
+        shape, index, dtype = k.shape, self._index, self.torch_dtype
+        if (len(shape) != 5 or v.shape != shape or k.dtype is not dtype or v.dtype is not dtype
+                or k.get_device() != index or v.get_device() != index):
             raise ThinKError(ERR_INVALID_ARG, where + ": rows")
-        self._call(fn, where, k5, v5, self._table(table, B, where), self._vector(pos, B, where + ": pos"),
-                   self._vector(rows, B, where + ": rows"), max_rows, layer0, n,
-                   _raw_stream(self._index) if stream is None else stream.cuda_stream)
+        B, max_rows, layers, heads, width = shape
+        kb, ks, kl, kn, kd = k.stride()
+        vb, vs, vl, vn, vd = v.stride()
+        if layers != n or heads != self._N_kv or width != self._D or kd != 1 or vd != 1 or max_rows >> 31:
+            raise ThinKError(ERR_INVALID_ARG, where + ": rows")
+        self._call(fn, where, Tensor5(k.data_ptr(), kb, ks, kl, kn), Tensor5(v.data_ptr(), vb, vs, vl, vn),
+                   self._table(table, B, where), self._vector(pos, B, where, ": pos"),
+                   self._vector(rows, B, where, ": rows"), max_rows, layer0, n,
+                   _raw_stream(index) if stream is None else stream.cuda_stream)
 
     # -- the calls ------------------------------------------------------
     def write(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, pos: Optional[torch.Tensor] = None,
@@ -462,11 +462,12 @@ class PagedKVCache:
         n = self._L - layer0 if nlayers is None else nlayers
         if (n | layer0) >> 31:
             raise ThinKError(ERR_INVALID_ARG, where + ": layers")
-        shape = q.shape
-        if (len(shape) != 4 or shape[1] != n or shape[2] != self._N_q or shape[3] != self._D
-                or q.dtype != self.torch_dtype or q.get_device() != self._index or not q.is_contiguous()):
+        shape, index = q.shape, self._index
+        if len(shape) != 4 or q.dtype is not self.torch_dtype or q.get_device() != index or not q.is_contiguous():
             raise ThinKError(ERR_INVALID_ARG, where + ": q")
-        B = shape[0]
+        B, layers, heads, width = shape
+        if layers != n or heads != self._N_q or width != self._D:
+            raise ThinKError(ERR_INVALID_ARG, where + ": q")
         if stream is not None:                 # results in memory that this stream's earlier work has left
             with torch.cuda.stream(stream):
                 if out is None:
@@ -475,23 +476,23 @@ class PagedKVCache:
                     lse = q.new_empty(shape[:3], dtype=torch.float32)
         if out is None:
             out = torch.empty_like(q)
-        elif out.shape != shape or out.dtype != q.dtype or out.get_device() != self._index or not out.is_contiguous():
+        elif out.shape != shape or out.dtype != q.dtype or out.get_device() != index or not out.is_contiguous():
             raise ThinKError(ERR_INVALID_ARG, where + ": out")
         if lse is not None:
-            if (lse.shape != shape[:3] or lse.dtype != torch.float32 or lse.get_device() != self._index
+            if (lse.shape != shape[:3] or lse.dtype != torch.float32 or lse.get_device() != index
                     or not lse.is_contiguous()):
                 raise ThinKError(ERR_INVALID_ARG, where + ": lse")
         elif return_lse:
             lse = q.new_empty(shape[:3], dtype=torch.float32)
         work, work_bytes = None, 0
         if scratch is not None:
-            if scratch.dtype != torch.uint8 or scratch.get_device() != self._index or not scratch.is_contiguous():
+            if scratch.dtype != torch.uint8 or scratch.get_device() != index or not scratch.is_contiguous():
                 raise ThinKError(ERR_INVALID_ARG, where + ": scratch")
             work, work_bytes = scratch.data_ptr(), scratch.numel()
         self._call(lib.thinK_paged_decode_attn, where, q.data_ptr(), out.data_ptr(),
                    None if lse is None else lse.data_ptr(), self._table(table, B, where),
-                   self._vector(seq_lens, B, where + ": seq_lens"), work, work_bytes, layer0, n,
-                   _raw_stream(self._index) if stream is None else stream.cuda_stream)
+                   self._vector(seq_lens, B, where, ": seq_lens"), work, work_bytes, layer0, n,
+                   _raw_stream(index) if stream is None else stream.cuda_stream)
         return out if lse is None else (out, lse)
 
     def device_error(self) -> int:
