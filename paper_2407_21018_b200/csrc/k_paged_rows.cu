@@ -51,9 +51,9 @@ __device__ __forceinline__ uint2 encode_e4m3(const uint4& w, float inv) {
 
 // 8 bf16 -> 8 4-bit codes; 4 lanes hold the group of 32 channels.  `sbits` receives the bf16 scale.
 // x / s to the nearest integer, ties to even, without eight divisions: x and s have 8 significant bits, so a quotient
-// that is no tie is at least 1 / 510 away from one.  x * (1 / s) is off by less than 2^-20; rounding it to multiples of
-// 2^-12 first (adding and subtracting 1.5 * 2^11) makes ties exact again and moves nothing else across one.  The
-// second rounding adds 1.5 * 2^23 + 8, which leaves n + 8 in the low bits.  A scale below 2^-126 takes the division:
+// that is no tie is at least 1 / 510 away from one.  x * (1 / s) is off by less than 2^-20; adding 1.5 * 2^11 rounds it
+// to multiples of 2^-12, which makes ties exact again and moves nothing else across one.  A second addition makes that
+// offset 1.5 * 2^23 + 8 and rounds to integers: n + 8 is in the low bits.  A scale below 2^-126 takes the division:
 // its own rounding error is large there, and n needs its limits.
 __device__ __forceinline__ uint32_t encode_int4(const uint4& w, uint32_t& sbits, bool& bad) {
   const uint32_t top = lane_max<4>(amax_bits(w));
@@ -69,12 +69,12 @@ __device__ __forceinline__ uint32_t encode_int4(const uint4& w, uint32_t& sbits,
   if (s >= 1.17549435e-38f) {
     float inv;                                  // within an ulp
     asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(s));
-    constexpr float kTo12 = 1.5f * 2048.f;
-    const f32x2 inv2 = two(inv, inv), up = two(kTo12, kTo12), down = two(-kTo12, -kTo12), magic = two(12582920.f, 12582920.f);
+    constexpr float kTo12 = 1.5f * 2048.f, kToInt = 12582920.f - kTo12;
+    const f32x2 inv2 = two(inv, inv), to12 = two(kTo12, kTo12), to_int = two(kToInt, kToInt);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float a, b;
-      split(add2(add2(add2(mul2(two(bf16lo(ws[i]), bf16hi(ws[i])), inv2), up), down), magic), a, b);
+      split(add2(fma2(two(bf16lo(ws[i]), bf16hi(ws[i])), inv2, to12), to_int), a, b);
       c[i] = __float_as_uint(a) + (__float_as_uint(b) << 4);
     }
   } else {
