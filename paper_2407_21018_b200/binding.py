@@ -482,8 +482,8 @@ class PagedKVCache:
             if (lse.shape != shape[:3] or lse.dtype != torch.float32 or lse.get_device() != index
                     or not lse.is_contiguous()):
                 raise ThinKError(ERR_INVALID_ARG, where + ": lse")
-        elif return_lse:
-            lse = q.new_empty(shape[:3], dtype=torch.float32)
+        elif return_lse:                       # (strides given: torch.empty takes twice as long on the host)
+            lse = torch.empty_strided(shape[:3], (layers * heads, heads, 1), dtype=torch.float32, device=q.device)
         work, work_bytes = None, 0
         if scratch is not None:
             if scratch.dtype != torch.uint8 or scratch.get_device() != index or not scratch.is_contiguous():
