@@ -830,7 +830,7 @@ struct alignas(16) Shared {
   WarpInfo info[kMaxWarps];
   int2 warp_sum[kMaxWarps];
   int valid[kMaxWarps][8];   // tokens that count in the stage
-  int arrived[2];
+  int join[2];               // contributors to the units that this CTA joins
 };
 
 template <int D, int E, int FMT, int GP>
@@ -1171,33 +1171,38 @@ __global__ void __launch_bounds__((Shape<D, E, FMT, GP>::THREADS), 1) k_paged_de
   if (!before && !after) return;
   __syncthreads();
   if (tid < 2) {
-    bool all = false;
+    int join = 0;                               // contributors, if this CTA joins them
     if (tid == 0 ? before : after) {
       const int64_t ts = tid == 0 ? wa.first_us : wb.last_us, tl = tid == 0 ? wa.first_ul : wb.last_ul;
       uint32_t* const ticket = p.counters + (tid == 0 ? wa.first_unit : wb.last_unit);
       const int n = sparse ? (int)(tl - ts) + 1 : split_owner(total, grid, tl) - split_owner(total, grid, ts) + 1;
       // after the barrier the whole CTA's states are ordered before this thread's release
-      all = ticket_add(ticket) == (unsigned)(n - 1);
-      if (all) *ticket = 0u;                    // ready for the next call
+      if (ticket_add(ticket) == (unsigned)(n - 1)) {
+        *ticket = 0u;                           // ready for the next call
+        join = n;
+      }
     }
-    sh.arrived[tid] = all;
+    sh.join[tid] = join;
   }
   __syncthreads();
-  // a warp takes 128 accumulators (four a lane, LPG lanes a query head) of every `slices`-th contributor; half the warps
-  // take the one unit and half the other if there are enough of them (one after the other, the CTAs that end last cost 1
-  // to 2 us more: 192 ragged sequences of 4 bits 69.7 us, now 67.9)
+  // a warp takes 128 accumulators (four a lane, LPG lanes a query head) of every `slices`-th contributor: of all of them
+  // if they are few.  (The order of the sums must not depend on which CTA joins, and so on what else it joins.)  Two
+  // units with few take half of the warps each (one after the other, the CTAs that end last cost 1 to 2 us more: 192
+  // ragged sequences of 4 bits 69.7 us against 67.9)
   constexpr int LPG = D / 4;
-  const int chunks = (p.G * D + 127) / 128;
-  const bool halves = sh.arrived[0] && sh.arrived[1] && 2 * chunks <= kWarps;
-  const int team = halves ? kWarps / 2 : kWarps, team0 = warp - warp % team, slices = team / chunks;
+  constexpr int AHEAD = 6;                      // states whose accumulators come while the statistics are made
+  const int chunks = (p.G * D + 127) / 128, n0 = sh.join[0], n1 = sh.join[1];
+  const bool halves = n0 > 0 && n0 <= AHEAD && n1 > 0 && n1 <= AHEAD && 2 * chunks <= kWarps;
+  const int team = halves ? kWarps / 2 : kWarps, team0 = warp - warp % team;
   const int chunk = (warp - team0) % chunks, slice = (warp - team0) / chunks;
 #pragma unroll 1
   for (int round = 0; round < (halves ? 1 : 2); ++round) {
     const int k = halves ? team0 > 0 : round;
-    if (!sh.arrived[k]) continue;
-    const int64_t ts = k == 0 ? wa.first_us : wb.last_us, tl = k == 0 ? wa.first_ul : wb.last_ul;
+    const int n = k == 0 ? n0 : n1;
+    if (n == 0) continue;
+    const int slices = n <= AHEAD ? 1 : kWarps / chunks;
+    const int64_t ts = k == 0 ? wa.first_us : wb.last_us;
     const int c0 = split_owner(total, grid, ts);
-    const int n = sparse ? (int)(tl - ts) + 1 : split_owner(total, grid, tl) - c0 + 1;
     const int64_t row = (int64_t)(k == 0 ? wa.first_unit : wb.last_unit) * p.G;
     const int e = 128 * chunk + 4 * lane;
     const bool on = e < p.G * D && slice < slices;
@@ -1206,7 +1211,6 @@ __global__ void __launch_bounds__((Shape<D, E, FMT, GP>::THREADS), 1) k_paged_de
     auto record = [&](int i) -> const Record<D>* {
       return records + 2 * (sparse ? split_owner(total, grid, ts + i) : c0 + i) + (i == 0);
     };
-    constexpr int AHEAD = 6;                    // states whose accumulators come while the statistics are made
     float4 y[AHEAD];
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j)

@@ -619,6 +619,27 @@ def test_many_layers_and_rows_in_one_call():
     assert p.cache.device_error() == 0
 
 
+@pytest.mark.parametrize("lens,N_kv,G", [
+    ([1028, 5000, 2391, 112, 5000, 5000, 1136], 8, 4),      # most CTAs share a unit with the one before and the one behind
+    ([1028, 5000, 2391, 112, 5000, 5000, 1136], 8, 1),
+    ([700, 90, 1500, 64] * 12, 4, 2),
+    ([20000, 9000], 2, 8),                                   # units of many CTAs
+    ([30000], 3, 3)])
+@pytest.mark.parametrize("fmt,dtype", KINDS, ids=IDS)
+def test_results_do_not_depend_on_timing(fmt, dtype, lens, N_kv, G):
+    p = Paged(fmt, dtype, lens, N_kv=N_kv, G=G)
+    k, v = p.rows(3)
+    p.cache.write(k, v, p.table, rows=p.seq)
+    q = torch.randn(len(lens), 1, N_kv * G, 128, generator=gen(5), device="cuda").to(dtype)
+    want, wlse = p.cache.decode_attn(q, p.table, p.seq, return_lse=True)
+    assert torch.isfinite(want).all()
+    differ = torch.zeros((), dtype=torch.int64, device="cuda")
+    for _ in range(200):
+        out, lse = p.cache.decode_attn(q, p.table, p.seq, return_lse=True)
+        differ += (out != want).sum() + (lse != wlse).sum()
+    assert differ.item() == 0
+
+
 # ---------------------------------------------------------------------------
 # streams, graphs, use together
 # ---------------------------------------------------------------------------
