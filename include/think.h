@@ -420,10 +420,10 @@ thinK_status thinK_paged_read(thinK_paged* p, thinK_tensor5 k, thinK_tensor5 v, 
  *   lse:    fp32 [B, nlayers, N_q], the natural logarithm of the softmax's sum (for joining with attention over
  *           other tokens), or NULL.
  *   seq_len: device int32 [B].  A sequence without tokens gets out = 0 and lse = -infinity.
- *   scratch: NULL for the handle's own workspace, or a device buffer of scratch_bytes >= thinK_paged_sizes.workspace,
- *           256-byte aligned, that was filled with zeros once before its first use (a call leaves it ready for the
- *           next).  Calls that may run at the same time - on two streams, or as two captured graphs - need a scratch
- *           buffer each.
+ *   scratch: NULL for the handle's own workspace, or a device buffer of scratch_bytes >= thinK_paged_sizes.workspace
+ *           (of the handle that it is given to), 256-byte aligned, that was filled with zeros once before its first use.
+ *           A call leaves it ready for the next one, of the same handle or of any other.  Calls that may run at the
+ *           same time - on two streams, or as two captured graphs - need a scratch buffer each.
  * A call names at most 2^29 table entries (4 * B * max_pages + 2 * B below 2^31), THINK_ERR_UNSUPPORTED otherwise.
  * Logits, softmax sums and outputs are accumulated in fp32.  Results do not depend on timing: partial results are
  * joined in token order. */

@@ -393,7 +393,8 @@ class PagedKVCache:
         self._L, self._N_q, self._N_kv, self._D, self._max_batch = c.L, c.N_q, c.N_kv, c.D, c.max_batch
 
     def new_scratch(self) -> torch.Tensor:
-        """A scratch buffer for attention calls that may run at the same time as others of this cache."""
+        """A scratch buffer for attention calls that may run at the same time as others of this cache.  Any cache that
+        needs no more (sizes.workspace) may use it too, in turn."""
         return torch.zeros(int(self.sizes.workspace), dtype=torch.uint8, device=self.device)
 
     # -- argument marshalling -------------------------------------------

@@ -1314,8 +1314,9 @@ cudaError_t paged_decode_setup(int dtype, int format, int D, int G) {
   THINK_PAGED_DISPATCH(setup_k);
 }
 // two records a CTA for units shared between CTAs, one a warp for units shared between warps
-size_t paged_decode_record_bytes(int D, int ctas) {
-  return (size_t)ctas * (2 + kMaxWarps) * (D == 128 ? sizeof(Record<128>) : sizeof(Record<64>));
+size_t paged_decode_record_bytes(int ctas) {
+  static_assert(sizeof(Record<128>) >= sizeof(Record<64>), "the larger one");
+  return (size_t)ctas * (2 + kMaxWarps) * sizeof(Record<128>);
 }
 
 }  // namespace think

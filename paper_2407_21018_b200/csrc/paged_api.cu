@@ -29,9 +29,11 @@ struct Geometry {
   float scale_log2;
 };
 
-// offsets in the workspace (and in a scratch buffer, whose error word is not used)
+// Offsets in the workspace (and in a scratch buffer, whose error word is not used).  Partial states lie at the same
+// place and take the same room whatever the handle, tickets behind them: handles of any shape may take turns on one
+// scratch buffer without a state of one landing on a ticket of another.
 struct Layout {
-  size_t counters, records, total;
+  size_t records, counters, total;
 };
 
 thinK_status make_geometry(const thinK_paged_config* c, Geometry* o) {
@@ -67,9 +69,9 @@ thinK_status make_geometry(const thinK_paged_config* c, Geometry* o) {
 }
 
 void make_layout(const Geometry& g, Layout* w) {
-  w->counters = 256;                                   // the error word is in front
-  w->records = align_up(w->counters + sizeof(uint32_t) * (size_t)g.max_batch * g.g.L * g.g.N_kv, 256);
-  w->total = align_up(w->records + paged_decode_record_bytes(g.g.D, kSMs), 256);
+  w->records = 256;                                    // the error word is in front
+  w->counters = align_up(w->records + paged_decode_record_bytes(kSMs), 256);
+  w->total = align_up(w->counters + sizeof(uint32_t) * (size_t)g.max_batch * g.g.L * g.g.N_kv, 256);
 }
 
 bool table_ok(const Geometry& g, const thinK_page_table& t) {
@@ -164,7 +166,8 @@ thinK_status thinK_paged_create(const thinK_paged_config* cfg, const thinK_paged
   int dev = 0, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
       paged_decode_setup(p->g.dtype, p->g.format, p->g.g.D, p->g.G) != cudaSuccess ||
-      cudaMemset(p->ws, 0, p->w.records) != cudaSuccess || cudaStreamSynchronize(cudaStreamLegacy) != cudaSuccess) {
+      cudaMemset(p->ws, 0, p->w.records) != cudaSuccess ||
+      cudaMemset(p->ws + p->w.counters, 0, p->w.total - p->w.counters) != cudaSuccess || cudaStreamSynchronize(cudaStreamLegacy) != cudaSuccess) {
     delete p;
     return THINK_ERR_CUDA;
   }

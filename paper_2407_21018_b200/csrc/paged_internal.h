@@ -87,7 +87,7 @@ struct PagedDecodeParams {
 cudaError_t launch_paged_rows(const PagedRowsParams& p, int dtype, int format, bool write, cudaStream_t s);
 cudaError_t launch_paged_decode(const PagedDecodeParams& p, int dtype, int format, cudaStream_t s);
 cudaError_t paged_decode_setup(int dtype, int format, int D, int G);   // kernel attributes on the current device
-size_t paged_decode_record_bytes(int D, int ctas);                     // partial states of a launch of that many CTAs
+size_t paged_decode_record_bytes(int ctas);             // partial states of a launch of that many CTAs, any head dimension
 
 // Launches a kernel that begins with begin_dependent(): it may be set up while the kernel ahead of it in the stream
 // finishes.
