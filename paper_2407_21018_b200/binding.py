@@ -451,7 +451,8 @@ class PagedKVCache:
 
     def read(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, pos: Optional[torch.Tensor] = None,
              rows: Optional[torch.Tensor] = None, layer0=0, nlayers=None, stream=None):
-        """The reverse of write: fills row s < rows[b] of k[b], v[b] with token pos[b] + s of sequence b."""
+        """The reverse of write: fills row s < rows[b] of k[b], v[b] with token pos[b] + s of sequence b.  No two rows
+        of k and v may share memory."""
         self._rows(lib.thinK_paged_read, "thinK_paged_read", k, v, table, pos, rows, layer0, nlayers, stream)
 
     def decode_attn(self, q: torch.Tensor, table: torch.Tensor, seq_lens: torch.Tensor,

@@ -7,6 +7,7 @@
 #include <nvtx3/nvToolsExt.h>
 
 #include "paged_internal.h"
+#include "paged_views.h"
 
 using namespace think;
 
@@ -87,6 +88,17 @@ bool view_ok(const thinK_tensor5& t, int elem) {
   return true;
 }
 
+// rows that are written must not share memory: each is stored by threads of its own
+bool destinations_ok(const thinK_tensor5& k, const thinK_tensor5& v, const Geometry& g, int B, int rows, int layers) {
+  const int unit = 16 / g.elem;                        // view_ok: pointers and strides are multiples of 16 bytes
+  auto view = [&](const thinK_tensor5& t) {
+    return RowView{{t.stride_b / unit, t.stride_s / unit, t.stride_l / unit, t.stride_n / unit}, {B, rows, layers, g.g.N_kv}, g.g.D / unit};
+  };
+  const RowView a = view(k), b = view(v);
+  if (!a.spread_ok() || !b.spread_ok() || a.shares_with_itself() || b.shares_with_itself()) return false;
+  return !a.shares_with(b, (int64_t)((uintptr_t)v.ptr / 16) - (int64_t)((uintptr_t)k.ptr / 16));
+}
+
 }  // namespace
 
 struct thinK_paged {
@@ -109,6 +121,7 @@ thinK_status rows_impl(thinK_paged* p, const thinK_tensor5& k, const thinK_tenso
   if (max_rows < 0 || (int64_t)max_rows * p->g.g.N_kv > (1 << 30) || !aligned(pos, 4) || !aligned(rows, 4)) return THINK_ERR_INVALID_ARG;
   if (max_rows == 0) return THINK_OK;                  // views without rows may have no memory
   if (!view_ok(k, p->g.elem) || !view_ok(v, p->g.elem)) return THINK_ERR_INVALID_ARG;
+  if (!write && !destinations_ok(k, v, p->g, t.B, max_rows, nlayers)) return THINK_ERR_INVALID_ARG;
   PagedRowsParams r;
   memset((void*)&r, 0, sizeof(r));
   r.g = p->g.g;

@@ -39,3 +39,52 @@ def test_one_scratch_for_caches_of_different_shapes(d_small, d_large):
         p, q, want, _ = calls[1]
         assert torch.equal(p.cache.decode_attn(q, p.table, p.seq), want)
     assert small.cache.device_error() == 0 and large.cache.device_error() == 0
+
+
+# ---------------------------------------------------------------------------
+# destinations of the read-back
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("fmt,dtype", KINDS, ids=IDS)
+def test_read_refuses_destinations_that_share_memory(fmt, dtype):
+    tk = binding()
+    lens = [70, 33]
+    p = Paged(fmt, dtype, lens, L=2, N_kv=2, G=2)
+    k, v = p.rows(3)
+    p.cache.write(k, v, p.table, rows=p.seq)
+    ko, vo = torch.zeros_like(k), torch.zeros_like(v)
+
+    def refused(a, b):
+        with pytest.raises(tk.ThinKError) as e:
+            p.cache.read(a, b, p.table, rows=p.seq)
+        assert e.value.status == tk.ERR_INVALID_ARG
+
+    one = torch.zeros(2, 70, 2, 2, 128, dtype=dtype, device="cuda")
+    refused(one, one)                                             # the same rows for keys and values
+    refused(one[:, :1].expand_as(one), vo)                        # one row for all tokens
+    refused(ko, one[:, :, :1].expand_as(one))                     # for all layers
+    refused(one[:1].expand_as(one), vo)                           # for all sequences
+    refused(one[:, :, :, :1].expand_as(one), vo)                  # for all heads
+    mem = torch.zeros(2 * one.numel(), dtype=dtype, device="cuda")
+    refused(mem.as_strided(one.shape, (70 * 512, 512, 256, 120, 1)), vo)            # rows that run into one another
+    refused(mem.as_strided(one.shape, (69 * 512, 512, 256, 128, 1)), vo)            # sequences that do
+    half = one.numel() - 512
+    refused(mem[:one.numel()].view_as(one), mem[half:half + one.numel()].view_as(one))
+    assert not (ko.any() or vo.any() or one.any() or mem.any()) and p.cache.device_error() == 0
+    # disjoint views of one buffer
+    p.cache.read(ko, vo, p.table, rows=p.seq)
+    want = torch.cat([ko, vo], -1)
+    wide = torch.zeros(2, 70, 2, 2, 256, dtype=dtype, device="cuda")
+    p.cache.read(wide[..., :128], wide[..., 128:], p.table, rows=p.seq)
+    assert torch.equal(wide, want)
+    wide = torch.zeros(2, 2, 2, 2, 70, 128, dtype=dtype, device="cuda")             # [b][key, value][layer][head][token]
+    a, b = (wide[:, i].permute(0, 3, 1, 2, 4) for i in (0, 1))
+    p.cache.read(a, b, p.table, rows=p.seq)
+    assert torch.equal(a, ko) and torch.equal(b, vo)
+    wide = torch.zeros(2, 2, 2, 70, 2, 128, dtype=dtype, device="cuda")             # different orders within a sequence
+    a, b = wide[:, 0].permute(0, 2, 1, 3, 4), wide[:, 1].view(2, 70, 2, 2, 128)
+    p.cache.read(a, b, p.table, rows=p.seq)
+    assert torch.equal(a, ko) and torch.equal(b, vo)
+    # an index of one value may have any stride
+    k1, v1 = torch.zeros_like(k[:1, :, :1]), torch.zeros_like(v[:1, :, :1])
+    p.cache.read(k1.as_strided(k1.shape, (0, 256, 0, 128, 1)), v1.as_strided(v1.shape, (8, 256, 8, 128, 1)), p.table, rows=p.seq, nlayers=1)
+    assert torch.equal(k1, ko[:1, :, :1]) and torch.equal(v1, vo[:1, :, :1])

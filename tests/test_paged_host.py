@@ -180,3 +180,84 @@ int main() {
 }
 """)
     assert out.strip() == "0"
+
+
+def test_views_that_share_memory(tmp_path):
+    """Row views against marking every unit of memory: random strides, views of dense tensors in any order, pairs side by
+    side, interleaved and overlapping; extents of millions; a search that is cut short says that they share."""
+    out = compile_and_run(tmp_path, r"""
+#include <stdio.h>
+#include <string.h>
+#include <chrono>
+#include <random>
+#include "paged_views.h"
+using namespace think;
+static uint8_t mem[1 << 20];
+static long base = 4096;
+static bool mark(const RowView& v, long at) {               // true: a unit was marked already
+  bool twice = false;
+  for (long a = 0; a < v.extent[0]; ++a) for (long b = 0; b < v.extent[1]; ++b) for (long c = 0; c < v.extent[2]; ++c)
+    for (long d = 0; d < v.extent[3]; ++d) for (long r = 0; r < v.row; ++r) {
+      uint8_t& m = mem[base + at + a * v.stride[0] + b * v.stride[1] + c * v.stride[2] + d * v.stride[3] + r];
+      twice |= m; m = 1;
+    }
+  return twice;
+}
+int main() {
+  std::mt19937 g(7);
+  auto rnd = [&](int n) { return (int)(g() % n); };
+  long bad = 0, cases = 0, shared = 0;
+  for (int it = 0; it < 60000; ++it) {
+    RowView a, b;
+    for (RowView* v : {&a, &b}) {
+      v->row = 1 + rnd(4);
+      const bool dense = rnd(2);
+      int order[4] = {0, 1, 2, 3};
+      for (int i = 3; i > 0; --i) { int j = rnd(i + 1), t = order[i]; order[i] = order[j]; order[j] = t; }
+      long at = v->row + (rnd(3) ? 0 : rnd(5));
+      for (int i : order) {
+        v->extent[i] = 1 + rnd(4);
+        v->stride[i] = dense ? at : rnd(40);
+        if (dense) at *= v->extent[i] + (rnd(3) ? 0 : 1);
+      }
+    }
+    if (rnd(3) == 0) b = a;                                  // the same layout, shifted
+    memset(mem, 0, sizeof(mem));
+    const bool self = mark(a, 0);
+    bad += a.shares_with_itself() != self;
+    if (rnd(2)) b.row = a.row;
+    const long apart = rnd(600) - 300;
+    memset(mem, 0, sizeof(mem));
+    mark(a, 0);
+    bool both = false;
+    for (long x = 0; x < b.extent[0]; ++x) for (long y = 0; y < b.extent[1]; ++y) for (long z = 0; z < b.extent[2]; ++z)
+      for (long w = 0; w < b.extent[3]; ++w) for (long r = 0; r < b.row; ++r)
+        both |= mem[base + apart + x * b.stride[0] + y * b.stride[1] + z * b.stride[2] + w * b.stride[3] + r];
+    bad += a.shares_with(b, apart) != both || b.shares_with(a, -apart) != both;
+    ++cases; shared += both + self;
+  }
+  // [4096][131072][80][8] rows of 16: dense, key and value rows interleaved, one row too many
+  RowView big = {{131072ll * 80 * 8 * 32, 80 * 8 * 32, 8 * 32, 32}, {4096, 131072, 80, 8}, 16};
+  auto t0 = std::chrono::steady_clock::now();
+  bad += big.shares_with_itself() || big.shares_with(big, 16) || big.shares_with(big, -16) || !big.shares_with(big, 15) || big.shares_with(big, 48) || !big.shares_with(big, 40);
+  RowView heads = {{131072ll * 80 * 8 * 32, 16, 131072ll * 8 * 16, 131072ll * 16}, {4096, 131072, 80, 8}, 16};      // b l n s
+  RowView rows = {{131072ll * 80 * 8 * 32, 80 * 8 * 16, 8 * 16, 16}, {4096, 131072, 80, 8}, 16};                    // b s l n
+  bad += heads.shares_with(rows, 131072ll * 80 * 8 * 16) || !heads.shares_with(rows, 131072ll * 80 * 8 * 16 - 1) || heads.shares_with_itself();
+  bad += std::chrono::duration<double>(std::chrono::steady_clock::now() - t0).count() > 0.05;
+  RowView wide = big;
+  wide.extent[3] = 9;
+  bad += !wide.shares_with_itself();
+  RowView zero = big;
+  zero.stride[2] = 0;
+  bad += !zero.shares_with_itself();
+  zero.extent[2] = 1;
+  bad += zero.shares_with_itself();
+  bad += !big.spread_ok();
+  big.stride[1] = 1ll << 50;
+  bad += big.spread_ok();
+  RowView odd = {{1 << 20, (1 << 20) + 16, (1 << 20) + 48, (1 << 20) + 112}, {4000, 4000, 4000, 4000}, 16};      // long search
+  bad += !odd.shares_with_itself();
+  printf("%ld %d %d\n", bad, cases > 0, shared > cases / 10 && shared < cases * 19 / 10);
+}
+""")
+    assert out.split() == ["0", "1", "1"]
