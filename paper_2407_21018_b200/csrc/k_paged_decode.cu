@@ -19,7 +19,7 @@
 //              unless its channels are more than 2^28 apart.  (The fp8 form of the instruction takes codes as they
 //              are, but here it is a sequence of conversions and two f16 instructions: 22 cycles against 8.3, measured.)
 //      values  through ldmatrix.trans; the weights, which come out token by token, are transposed in registers.  bf16:
-//              the weights are a bf16 pair high + low (two instructions), 2^-17.  e4m3, 4-bit: f16 codes as above.  (The
+//              the weights are a bf16 pair high + low (two instructions), 2^-16.  e4m3, 4-bit: f16 codes as above.  (The
 //              subnormals as they are would do, with the 8 taken off the sums, but the tensor core aligns products by
 //              exponent fields: sums then keep 2^-15 instead of 2^-22, measured.)
 //      scales  of keys multiply logits, those of values go into the weights, which are rounded to f16 (2^-11) relative
@@ -148,6 +148,17 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   __half2 v = __floats2half2_rn(lo, hi);
   return *(uint32_t*)&v;
+}
+// Two weights w >= 0 as sums of two bf16: the first 8 bits, cut off, and the rest, rounded: within 2^-16.  Both parts
+// multiply a value, so neither may be zero or negative beside a weight: an infinite value would become a NaN.  Cutting
+// keeps the rest from being negative, w * 2^-23 on top of it (fused, one rounding) from being zero.
+__device__ __forceinline__ void pair_bf16(float w0, float w1, uint32_t& hi, uint32_t& lo) {
+  const uint32_t u0 = __float_as_uint(w0), u1 = __float_as_uint(w1);
+  hi = __byte_perm(u0, u1, 0x7632);
+  float a, b;
+  split(fma2(two(w0, w1), two(1.f + 0x1p-23f, 1.f + 0x1p-23f),
+             two(__uint_as_float((u0 & 0xffff0000u) ^ 0x80000000u), __uint_as_float((u1 & 0xffff0000u) ^ 0x80000000u))), a, b);
+  lo = pack_bf16(a, b);
 }
 // two e4m3 bytes as f16: the lower and the upper half of a word
 __device__ __forceinline__ uint32_t e4m3_lo_to_f16x2(uint32_t w) {
@@ -517,8 +528,8 @@ struct MmaState {
         uint32_t hi[2], lo[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          hi[j] = pack_bf16(w[j][0], w[j][1]);
-          lo[j] = transpose8(pack_bf16(w[j][0] - bf16lo(hi[j]), w[j][1] - bf16hi(hi[j])));
+          pair_bf16(w[j][0], w[j][1], hi[j], lo[j]);
+          lo[j] = transpose8(lo[j]);
           hi[j] = transpose8(hi[j]);
         }
         const int off = vr * S::RB + (((mi >> 1) ^ tr) << 4);

@@ -88,3 +88,33 @@ def test_read_refuses_destinations_that_share_memory(fmt, dtype):
     k1, v1 = torch.zeros_like(k[:1, :, :1]), torch.zeros_like(v[:1, :, :1])
     p.cache.read(k1.as_strided(k1.shape, (0, 256, 0, 128, 1)), v1.as_strided(v1.shape, (8, 256, 8, 128, 1)), p.table, rows=p.seq, nlayers=1)
     assert torch.equal(k1, ko[:1, :, :1]) and torch.equal(v1, vo[:1, :, :1])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=IDS[:2])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_infinite_values(dtype, D):
+    """A plain page may hold infinities.  A value of +-infinity with a weight makes its channel +-infinity, both signs a
+    NaN, and no other channel sees it; behind the sequence's end it counts nothing."""
+    lens = [1, 2, 63, 70, 3000]
+    p = Paged("plain", dtype, [n + 1 for n in lens], N_kv=2, G=4, D=D)
+    k, v = p.rows(19)
+    inf = float("inf")
+    for b, n in enumerate(lens):
+        v[b, n // 2, 0, 0, 3] = inf
+        v[b, n // 2, 0, 0, 9] = -inf
+        v[b, 0, 0, 0, 17], v[b, n - 1, 0, 0, 17] = inf, -inf
+        v[b, n] = inf
+    p.cache.write(k, v, p.table)
+    q = (0.1 * torch.randn(len(lens), 1, 8, D, generator=gen(23), device="cuda")).to(dtype)
+    seq = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    out, lse = p.cache.decode_attn(q, p.table, seq, return_lse=True)
+    mine = out[:, 0, :4].float()
+    assert (mine[..., 3] == inf).all() and (mine[..., 9] == -inf).all()
+    assert torch.isnan(mine[1:, :, 17]).all() and (mine[0, :, 17] == -inf).all()
+    # the rest as without them (the oracle reads the pool: put finite values there)
+    keep = [c for c in range(D) if c not in (3, 9, 17)]
+    v = torch.where(torch.isfinite(v), v, torch.ones_like(v))
+    p.cache.write(k, v, p.table)
+    want = p.cache.decode_attn(q, p.table, seq)
+    assert torch.equal(out[:, :, :4][..., keep], want[:, :, :4][..., keep]) and torch.equal(out[:, :, 4:], want[:, :, 4:])
+    p.check(q, want, lse, lens=lens)
