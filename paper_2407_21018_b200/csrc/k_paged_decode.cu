@@ -46,7 +46,7 @@ namespace think {
 namespace {
 
 constexpr int kMaxWarps = 12;
-constexpr float kSlack = 8.f, kTop = 7.f;     // running maxima: how far they may lag, and where they put weights (log2)
+constexpr float kAhead = 8.f;                 // how far above the largest logit weights' reference is put when it moves
 constexpr int kMaxG = kMaxPagedGroup;
 
 // GP: query heads that the fp32 kernel computes at a time
@@ -73,15 +73,15 @@ struct Shape {
   static constexpr int RING = STAGES * STAGE;
   static_assert(STAGES >= 2 && WARPS <= kMaxWarps && WARPS >= kMaxG && WARPS % 4 == 0, "ring");
   // a warp's ring takes its partial state and the weights of a join afterwards, or a join's statistics
-  static_assert(RING >= (4 * kMaxG + kMaxG * (D + 4) + kMaxWarps * kMaxG) * 4 && RING >= kSMs * 2 * 16 + 512, "ring");
+  static_assert(RING >= (2 * kMaxG + kMaxG * (D + 4) + kMaxWarps * kMaxG) * 4 && RING >= kSMs * 2 * 8 + 512, "ring");
 };
 
-// Partial state of one (worker, unit).  m: running maximum of the logits (base 2); M: that
-// of logit + exponent of the value's scale, the unit of the accumulators; l: sum of exp2(logit - m).
+// Partial state of one (worker, unit).  m: the logit (base 2) that weights are relative to, at least the largest one and
+// at most 8 above it; l: sum of the weights exp2(logit - m).
 // Rows are 4 floats longer than D: the lanes of a fragment, two rows apart, then store to different banks.
 template <int D>
 struct Record {
-  float4 s[kMaxG];           // m, M, l
+  float2 s[kMaxG];           // m, l
   float o[kMaxG][D + 4];
 };
 
@@ -171,20 +171,23 @@ __device__ __forceinline__ uint32_t e4m3_hi_to_f16x2(uint32_t w) {
   asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, hi;\n\t}" : "=r"(d) : "r"(w));
   return d;
 }
-// the codes at bits 0..3 and 16..19 of w as f16 numbers n * 2^-9: the masked word holds subnormals c * 2^-24
-__device__ __forceinline__ uint32_t int4_lo_to_f16x2(uint32_t w) {
-  const uint32_t t = w & 0x000f000fu, k = 0x78007800u, o = 0xa400a400u;       // 2^15, -8 * 2^-9
-  const __half2 r = __hfma2(*(const __half2*)&t, *(const __half2*)&k, *(const __half2*)&o);
+__device__ __forceinline__ uint32_t f16x2_to_bf16x2(uint32_t w) {
+  const float2 f = __half22float2(*(const __half2*)&w);
+  return pack_bf16(f.x, f.y);
+}
+// the codes at bits 0..3 and 16..19 of w as bf16 numbers n / 64: the masked word holds subnormals c * 2^-133
+__device__ __forceinline__ uint32_t int4_lo_to_bf16x2(uint32_t w) {
+  const uint32_t t = w & 0x000f000fu, k = 0x7f007f00u, o = 0xbe00be00u;       // 2^127, -8 / 64
+  const __nv_bfloat162 r = __hfma2(*(const __nv_bfloat162*)&t, *(const __nv_bfloat162*)&k, *(const __nv_bfloat162*)&o);
   return *(const uint32_t*)&r;
 }
-// the same at bits 4..7 and 20..23: c * 2^-20
-__device__ __forceinline__ uint32_t int4_hi_to_f16x2(uint32_t w) {
-  const uint32_t t = w & 0x00f000f0u, k = 0x68006800u, o = 0xa400a400u;       // 2^11
-  const __half2 r = __hfma2(*(const __half2*)&t, *(const __half2*)&k, *(const __half2*)&o);
+// the same at bits 4..7 and 20..23: c * 2^-129 (from c = 8 on the exponent field is 1, which goes on in the same steps)
+__device__ __forceinline__ uint32_t int4_hi_to_bf16x2(uint32_t w) {
+  const uint32_t t = w & 0x00f000f0u, k = 0x7d007d00u, o = 0xbe00be00u;       // 2^123
+  const __nv_bfloat162 r = __hfma2(*(const __nv_bfloat162*)&t, *(const __nv_bfloat162*)&k, *(const __nv_bfloat162*)&o);
   return *(const uint32_t*)&r;
 }
-// small integers to float without the conversion unit: 2^23 + n
-__device__ __forceinline__ float magic(uint32_t n) { return __uint_as_float(0x4b000000u | n); }
+constexpr float kInt4Unit = 64.f;
 // 2^k for -126 <= k <= 127
 __device__ __forceinline__ float pow2i(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }
 
@@ -271,7 +274,7 @@ struct WarpInfo {
 // Tensor-core formats: fragments of a warp.  Lane (r = lane / 4, qd = lane % 4).  Logits and accumulators have the
 // lane's queries 2 qd, 2 qd + 1 in register pairs: logits of tokens 8 n + r of the step, accumulators of channels by r.
 template <int FMT>
-__device__ __forceinline__ float finish(float m, float M, float l);
+__device__ __forceinline__ float finish(float l);
 
 template <int D, int FMT>
 struct MmaState {
@@ -285,7 +288,7 @@ struct MmaState {
 
   uint32_t q[NG][4];         // B fragments of the two k16 instructions of a block: query r
   f32x2 rs;                  // base-2 logit per unit of the q k product
-  float m[2], M[2];          // running maxima in use
+  float m[2];                // what weights are relative to
   f32x2 l;                   // of this lane's tokens until end()
   float o[OT][4];
 
@@ -320,6 +323,15 @@ struct MmaState {
 #pragma unroll
         for (int i = 0; i < 4; ++i) q[g][i] = w[g][i];
       rs = two(scale_log2, scale_log2);
+    } else if constexpr (INT4) {                // the codes of a word pair up as channels (0,4) (1,5) | (2,6) (3,7)
+#pragma unroll
+      for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          q[g][2 * j] = __byte_perm(w[g][j], w[g][2 + j], 0x5410);
+          q[g][2 * j + 1] = __byte_perm(w[g][j], w[g][2 + j], 0x7632);
+        }
+      rs = two(scale_log2 * kInt4Unit, scale_log2 * kInt4Unit);
     } else {
       const int qd = lane & 3;
       uint32_t t = 0;                           // largest magnitude's bits (as numbers: NaN counts as none)
@@ -332,24 +344,14 @@ struct MmaState {
       t = max(t, __shfl_xor_sync(0xffffffffu, t, 2));
       // the row's largest channel goes to [2^14, 2^15)
       const int k = min(141 - (int)(t >> 7), 100);
-      const float up = pow2i(k), down = scale_log2 * pow2i(-k) * (INT4 ? 512.f : 1.f);       // 4-bit codes are n * 2^-9
+      const float up = pow2i(k), down = scale_log2 * pow2i(-k);
       rs = two(__shfl_sync(0xffffffffu, down, 8 * qd), __shfl_sync(0xffffffffu, down, 8 * qd + 4));
 #pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        if constexpr (INT4) {                   // the codes of a word pair up as channels (0,4) (1,5) | (2,6) (3,7)
+      for (int g = 0; g < NG; ++g)
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const uint32_t a = w[g][j], b = w[g][2 + j];
-            q[g][2 * j] = pack_f16(bf16lo(a) * up, bf16lo(b) * up);
-            q[g][2 * j + 1] = pack_f16(bf16hi(a) * up, bf16hi(b) * up);
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) q[g][i] = pack_f16(bf16lo(w[g][i]) * up, bf16hi(w[g][i]) * up);
-        }
-      }
+        for (int i = 0; i < 4; ++i) q[g][i] = pack_f16(bf16lo(w[g][i]) * up, bf16hi(w[g][i]) * up);
     }
-    m[0] = m[1] = M[0] = M[1] = -INFINITY;
+    m[0] = m[1] = -INFINITY;
     l = 0;
 #pragma unroll
     for (int t = 0; t < OT; ++t) o[t][0] = o[t][1] = o[t][2] = o[t][3] = 0.f;
@@ -361,6 +363,13 @@ struct MmaState {
       asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(sc[0]), "=r"(sc[1]) : "r"(a));
     else
       asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sc[0]) : "r"(a));
+  }
+  // those of two neighbouring tokens, the first one even
+  static __device__ __forceinline__ void load_scales2(uint32_t a, uint32_t (&sc)[NG]) {
+    if constexpr (NG == 4)
+      asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(sc[0]), "=r"(sc[1]), "=r"(sc[2]), "=r"(sc[3]) : "r"(a));
+    else
+      asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(sc[0]), "=r"(sc[1]) : "r"(a));
   }
   static __device__ __forceinline__ float scale_of(const uint32_t (&sc)[NG / 2], int g) {
     return (g & 1) ? bf16hi(sc[g >> 1]) : bf16lo(sc[g >> 1]);
@@ -375,6 +384,7 @@ struct MmaState {
   __device__ __forceinline__ void step(uint32_t sb, int ntok, int lane) {
     const int r = lane >> 2, mi = lane >> 3, tr = lane & 7;
     const uint32_t ks = sb + 2 * S::HALF + r * S::SB, vs = ks + S::ST * S::SB;     // scales of token r
+    const uint32_t vs2 = sb + 2 * S::HALF + (S::ST + 2 * (lane & 3)) * S::SB;      // values' scales of token 2qd
     f32x2 x[NT];
     // ---- logits, 16 tokens at a time
 #pragma unroll
@@ -429,8 +439,8 @@ struct MmaState {
         for (int g = 0; g < NG; ++g) {
           const uint32_t a = k[g], b = k8[g], ah = a >> 8, bh = b >> 8;
           float c[4];
-          mma_first<false>(c, int4_lo_to_f16x2(a), int4_lo_to_f16x2(b), int4_hi_to_f16x2(a), int4_hi_to_f16x2(b), q[g][0], q[g][1]);
-          mma<false>(c, int4_lo_to_f16x2(ah), int4_lo_to_f16x2(bh), int4_hi_to_f16x2(ah), int4_hi_to_f16x2(bh), q[g][2], q[g][3]);
+          mma_first<true>(c, int4_lo_to_bf16x2(a), int4_lo_to_bf16x2(b), int4_hi_to_bf16x2(a), int4_hi_to_bf16x2(b), q[g][0], q[g][1]);
+          mma<true>(c, int4_lo_to_bf16x2(ah), int4_lo_to_bf16x2(bh), int4_hi_to_bf16x2(ah), int4_hi_to_bf16x2(bh), q[g][2], q[g][3]);
           const float f0 = scale_of(s0, g), f1 = scale_of(s1, g);
           y0 = fma2(two(c[0], c[1]), two(f0, f0), y0);
           y1 = fma2(two(c[2], c[3]), two(f1, f1), y1);
@@ -444,119 +454,97 @@ struct MmaState {
       for (int n = 0; n < NT; ++n)
         if (8 * n + r >= ntok) x[n] = two(-INFINITY, -INFINITY);
     }
-    // ---- maxima of the logits and of logit + log2 of the value's scale.  For 4-bit rows that is the largest scale's
-    // bits read as a piecewise linear logarithm (low by < 0.09); the scales are divided by the same power below
-    f32x2 es[PLAIN ? 1 : NT];
-    float down[INT4 ? NT : 1];                  // 4-bit: 2^-(that logarithm) of token 8n + r
-    float mx[2] = {-INFINITY, -INFINITY}, Mx[2] = {-INFINITY, -INFINITY};
+    float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       float a, b;
       split(x[n], a, b);
       mx[0] = fmaxf(mx[0], a);
       mx[1] = fmaxf(mx[1], b);
-      if constexpr (!PLAIN) {
-        float e;
-        if constexpr (INT4) {
-          uint32_t sc[NG / 2], t;
-          load_scales(vs + 8 * n * S::SB, sc);
-          t = NG == 4 ? max_bf16x2(sc[0], sc[NG / 2 - 1]) : sc[0];
-          t = max_bf16x2(t, __byte_perm(t, 0u, 0x1032));
-          e = fmaf(__uint_as_float(__byte_perm(t, 0x4b000000u, 0x7410)) - 8388608.f, 0.0078125f, -127.f);    // 2^23 + bits
-          down[n] = ex2(-e);
-        } else {
-          e = magic(load_byte(vs + 8 * n)) - 8388735.f;
-        }
-        es[n] = add2(x[n], two(e, e));
-        split(es[n], a, b);
-        Mx[0] = fmaxf(Mx[0], a);
-        Mx[1] = fmaxf(Mx[1], b);
-      }
     }
-    if (PLAIN) {
-      Mx[0] = mx[0];
-      Mx[1] = mx[1];
-    }
-    // the maxima in use move only when a token exceeds one 2^8 times: weights then stay below 2^15 (2^8 in fp32)
-    if (__any_sync(0xffffffffu, mx[0] > m[0] + kSlack || mx[1] > m[1] + kSlack || Mx[0] > M[0] + kSlack || Mx[1] > M[1] + kSlack)) {
-      float sm[2], sM[2];
+    // The reference moves when a logit exceeds it, and is then put 8 above, so that it seldom moves.  Weights are at most
+    // 1, the largest at least 2^-8: weight times value keeps to the value's range.
+    if (__any_sync(0xffffffffu, mx[0] > m[0] || mx[1] > m[1])) {
+      float sm[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
 #pragma unroll
-        for (int k = 4; k < 32; k <<= 1) {
-          mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], k));
-          if (!PLAIN) Mx[i] = fmaxf(Mx[i], __shfl_xor_sync(0xffffffffu, Mx[i], k));
-        }
-        if (PLAIN) Mx[i] = mx[i];
-        mx[i] = fmaxf(m[i], mx[i]);
-        Mx[i] = fmaxf(M[i], Mx[i]);
-        sm[i] = m[i] == -INFINITY ? 0.f : ex2(m[i] - mx[i]);
-        sM[i] = M[i] == -INFINITY ? 0.f : ex2(M[i] - Mx[i]);
-        m[i] = mx[i];
-        M[i] = Mx[i];
+        for (int k = 4; k < 32; k <<= 1) mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], k));
+        const float to = mx[i] > m[i] ? mx[i] + kAhead : m[i];
+        sm[i] = m[i] == -INFINITY ? 0.f : ex2(m[i] - to);
+        m[i] = to;
       }
-      l = mul2(l, two(sm[0], sm[1]));
-      const f32x2 s01 = two(sM[0], sM[1]);
+      const f32x2 s01 = two(sm[0], sm[1]);
+      l = mul2(l, s01);
 #pragma unroll
       for (int t = 0; t < OT; ++t) {
         split(mul2(two(o[t][0], o[t][1]), s01), o[t][0], o[t][1]);
         split(mul2(two(o[t][2], o[t][3]), s01), o[t][2], o[t][3]);
       }
     }
-    // (a query that no token had a weight for yet has no maximum to subtract)
+    // (a query that no token had a weight for yet has nothing to subtract)
     const f32x2 mr = two(m[0] == -INFINITY ? 0.f : -m[0], m[1] == -INFINITY ? 0.f : -m[1]);
-    const f32x2 Mr = two(M[0] == -INFINITY ? 0.f : kTop - M[0], M[1] == -INFINITY ? 0.f : kTop - M[1]);
     // ---- weights and V p, 16 tokens at a time
 #pragma unroll
     for (int kk = 0; kk < NT / 2; ++kk) {
       const uint32_t vb = sb + S::HALF + kk * 16 * S::RB;
       const int vr = ((mi & 1) << 3) + tr;
-      float w[2][2];
+      float w[2][2];                            // of tokens r and r + 8
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         split(add2(x[2 * kk + j], mr), w[j][0], w[j][1]);
         w[j][0] = ex2(w[j][0]);
         w[j][1] = ex2(w[j][1]);
         l = add2(l, two(w[j][0], w[j][1]));
-        if constexpr (!PLAIN) {
-          split(add2(es[PLAIN ? 0 : 2 * kk + j], Mr), w[j][0], w[j][1]);
-          w[j][0] = ex2(w[j][0]);
-          w[j][1] = ex2(w[j][1]);
-        }
       }
-      if constexpr (PLAIN) {
+      if constexpr (!INT4) {
         uint32_t hi[2], lo[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
+          if constexpr (!PLAIN) {               // the row's scale
+            const float f = __uint_as_float(load_byte(vs + 16 * kk + 8 * j) << 23);
+            split(mul2(two(w[j][0], w[j][1]), two(f, f)), w[j][0], w[j][1]);
+          }
           pair_bf16(w[j][0], w[j][1], hi[j], lo[j]);
-          lo[j] = transpose8(lo[j]);
           hi[j] = transpose8(hi[j]);
+          lo[j] = transpose8(lo[j]);
         }
-        const int off = vr * S::RB + (((mi >> 1) ^ tr) << 4);
+        if constexpr (PLAIN) {
+          const int off = vr * S::RB + (((mi >> 1) ^ tr) << 4);
 #pragma unroll
-        for (int t = 0; t < OT; ++t) {
-          uint32_t v[4];
-          ldsm4t(vb + (off ^ (t << 5)), v);
-          mma<true>(o[t], v[0], v[2], v[1], v[3], hi[0], hi[1]);
-          mma<true>(o[t], v[0], v[2], v[1], v[3], lo[0], lo[1]);
-        }
-      } else if constexpr (!INT4) {
-        const uint32_t b0 = transpose8(pack_f16(w[0][0], w[0][1])), b1 = transpose8(pack_f16(w[1][0], w[1][1]));
-        const int off = S::RB == 128 ? vr * 128 + (((mi >> 1) ^ tr) << 4) : vr * 64 + (((mi >> 1) ^ (tr >> 1)) << 4);
+          for (int t = 0; t < OT; ++t) {
+            uint32_t v[4];
+            ldsm4t(vb + (off ^ (t << 5)), v);
+            mma<true>(o[t], v[0], v[2], v[1], v[3], hi[0], hi[1]);
+            mma<true>(o[t], v[0], v[2], v[1], v[3], lo[0], lo[1]);
+          }
+        } else {
+          const int off = S::RB == 128 ? vr * 128 + (((mi >> 1) ^ tr) << 4) : vr * 64 + (((mi >> 1) ^ (tr >> 1)) << 4);
 #pragma unroll
-        for (int i = 0; i < OT / 2; ++i) {
-          uint32_t v[4];
-          ldsm4t(vb + (off ^ (i << 5)), v);
+          for (int i = 0; i < OT / 2; ++i) {
+            uint32_t v[4];
+            ldsm4t(vb + (off ^ (i << 5)), v);
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {         // a word: channels 2r, 2r + 1 of token 2qd, the same of token 2qd + 1
-            const uint32_t a = __byte_perm(v[2 * j], 0u, 0x3120), b = __byte_perm(v[2 * j + 1], 0u, 0x3120);
-            mma<false>(o[2 * i + j], e4m3_lo_to_f16x2(a), e4m3_hi_to_f16x2(a), e4m3_lo_to_f16x2(b), e4m3_hi_to_f16x2(b), b0, b1);
+            for (int j = 0; j < 2; ++j) {       // a word: channels 2r, 2r + 1 of token 2qd, the same of token 2qd + 1
+              const uint32_t a = __byte_perm(v[2 * j], 0u, 0x3120), b = __byte_perm(v[2 * j + 1], 0u, 0x3120);
+              const uint32_t a0 = f16x2_to_bf16x2(e4m3_lo_to_f16x2(a)), a1 = f16x2_to_bf16x2(e4m3_hi_to_f16x2(a));
+              const uint32_t a2 = f16x2_to_bf16x2(e4m3_lo_to_f16x2(b)), a3 = f16x2_to_bf16x2(e4m3_hi_to_f16x2(b));
+              mma<true>(o[2 * i + j], a0, a1, a2, a3, hi[0], hi[1]);
+              mma<true>(o[2 * i + j], a0, a1, a2, a3, lo[0], lo[1]);
+            }
           }
         }
       } else {
-        uint32_t s0[NG / 2], s1[NG / 2];
-        load_scales(vs + 16 * kk * S::SB, s0);
-        load_scales(vs + (16 * kk + 8) * S::SB, s1);
+        // weights are transposed once, as they are (two halves each), and meet the scales of their tokens behind that
+        f32x2 wt[2];                            // query r, tokens 2qd, 2qd + 1 and the same + 8
+        uint32_t sc[2][NG];                     // their scales: NG / 2 words a token
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t u0 = __float_as_uint(w[j][0]), u1 = __float_as_uint(w[j][1]);
+          const uint32_t lo = transpose8(__byte_perm(u0, u1, 0x5410)), hi = transpose8(__byte_perm(u0, u1, 0x7632));
+          wt[j] = two(__uint_as_float(__byte_perm(lo, hi, 0x5410)), __uint_as_float(__byte_perm(lo, hi, 0x7632)));
+          load_scales2(vs2 + (16 * kk + 8 * j) * S::SB, sc[j]);
+        }
         const int off = S::RB == 64 ? vr * 64 + (((mi >> 1) ^ (tr >> 1)) << 4) : vr * 32 + (((mi >> 1) ^ (tr >> 2)) << 4);
 #pragma unroll
         for (int g2 = 0; g2 < NG / 2; ++g2) {
@@ -565,14 +553,21 @@ struct MmaState {
 #pragma unroll
           for (int j = 0; j < 2; ++j) {         // a word: channels 4r .. 4r + 3 of token 2qd, the same of token 2qd + 1
             const int g = 2 * g2 + j;
-            const float f0 = scale_of(s0, g) * down[2 * kk], f1 = scale_of(s1, g) * down[2 * kk + 1];
-            float f[4];
-            split(mul2(two(w[0][0], w[0][1]), two(f0, f0)), f[0], f[1]);
-            split(mul2(two(w[1][0], w[1][1]), two(f1, f1)), f[2], f[3]);
-            const uint32_t b0 = transpose8(pack_f16(f[0], f[1])), b1 = transpose8(pack_f16(f[2], f[3]));
+            uint32_t hi[2], lo[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              const uint32_t s0 = sc[t][g2], s1 = sc[t][NG / 2 + g2];
+              float f0, f1;
+              split(mul2(wt[t], j ? two(bf16hi(s0), bf16hi(s1)) : two(bf16lo(s0), bf16lo(s1))), f0, f1);
+              pair_bf16(f0, f1, hi[t], lo[t]);
+            }
             const uint32_t a = v[2 * j], b = v[2 * j + 1], a8 = a >> 8, b8 = b >> 8;
-            mma<false>(o[2 * g], int4_lo_to_f16x2(a), int4_hi_to_f16x2(a), int4_lo_to_f16x2(b), int4_hi_to_f16x2(b), b0, b1);
-            mma<false>(o[2 * g + 1], int4_lo_to_f16x2(a8), int4_hi_to_f16x2(a8), int4_lo_to_f16x2(b8), int4_hi_to_f16x2(b8), b0, b1);
+            uint32_t a0 = int4_lo_to_bf16x2(a), a1 = int4_hi_to_bf16x2(a), a2 = int4_lo_to_bf16x2(b), a3 = int4_hi_to_bf16x2(b);
+            mma<true>(o[2 * g], a0, a1, a2, a3, hi[0], hi[1]);
+            mma<true>(o[2 * g], a0, a1, a2, a3, lo[0], lo[1]);
+            a0 = int4_lo_to_bf16x2(a8), a1 = int4_hi_to_bf16x2(a8), a2 = int4_lo_to_bf16x2(b8), a3 = int4_hi_to_bf16x2(b8);
+            mma<true>(o[2 * g + 1], a0, a1, a2, a3, hi[0], hi[1]);
+            mma<true>(o[2 * g + 1], a0, a1, a2, a3, lo[0], lo[1]);
           }
         }
       }
@@ -623,7 +618,7 @@ struct MmaState {
     if (lane < 4) {
 #pragma unroll
       for (int i = 0; i < 2; ++i)
-        if (q0 + i < G) rec->s[q0 + i] = make_float4(m[i], M[i], ls[i], 0.f);
+        if (q0 + i < G) rec->s[q0 + i] = make_float2(m[i], ls[i]);
     }
     each(lane, [&](int c, const float (&a)[WIDTH], const float (&b)[WIDTH]) {
       if (q0 < G) put(&rec->o[q0][c], a);
@@ -635,12 +630,8 @@ struct MmaState {
 
 // factor that turns joined accumulators into outputs: 0 where no token counted (a NaN logit leaves m alone, not l)
 template <int FMT>
-__device__ __forceinline__ float finish(float m, float M, float l) {
-  if (l == 0.f) return 0.f;
-  if (FMT == THINK_PAGE_PLAIN) return 1.f / l;
-  // accumulators are in units of 2^(M - kTop), 4-bit ones of 512 times that; two factors: the exponent may pass 127
-  const float h = exp2f(0.5f * (M - (FMT == THINK_PAGE_INT4 ? kTop - 9.f : kTop) - m));
-  return h / l * h;
+__device__ __forceinline__ float finish(float l) {
+  return l == 0.f ? 0.f : (FMT == THINK_PAGE_INT4 ? kInt4Unit : 1.f) / l;
 }
 // four joined accumulators to four outputs of EO bytes
 template <int EO>
@@ -658,7 +649,7 @@ __device__ __forceinline__ void MmaState<D, FMT>::store_out(void* out, float* ls
   const int q0 = 2 * (lane & 3);
   float ls[2];
   split(l, ls[0], ls[1]);
-  const float f0 = finish<FMT>(m[0], M[0], ls[0]), f1 = finish<FMT>(m[1], M[1], ls[1]);
+  const float f0 = finish<FMT>(ls[0]), f1 = finish<FMT>(ls[1]);
   __nv_bfloat16* const po = (__nv_bfloat16*)out + q0 * D;
   auto write = [&](__nv_bfloat16* to, const float (&v)[WIDTH], float f) {
     if constexpr (WIDTH == 1) {
@@ -809,7 +800,7 @@ struct F32State {
 #pragma unroll
     for (int g = 0; g < GP; ++g) {
       if (g >= G) break;
-      if (lane == (g * ST / R) << (5 - LB)) r->s[g] = make_float4(m, m, l, 0.f);
+      if (lane == (g * ST / R) << (5 - LB)) r->s[g] = make_float2(m, l);
 #pragma unroll
       for (int i = 0; i < N; i += 2) *(float2*)&r->o[g][lane * N + i] = make_float2(o[g][i], o[g][i + 1]);
     }
@@ -820,7 +811,7 @@ struct F32State {
       const int src = (g * ST / R) << (5 - LB);
       const float mg = __shfl_sync(0xffffffffu, m, src), lg = __shfl_sync(0xffffffffu, l, src);
       if (g < G) {
-        const float f = finish<THINK_PAGE_PLAIN>(mg, mg, lg);
+        const float f = finish<THINK_PAGE_PLAIN>(lg);
 #pragma unroll
         for (int i = 0; i < N; ++i) ((float*)out)[g * D + lane * N + i] = f == 0.f ? 0.f : o[g][i] * f;
         if (lse && lane == 0) lse[g] = log_sum(mg, lg);
@@ -1119,25 +1110,23 @@ __global__ void __launch_bounds__((Shape<D, E, FMT, GP>::THREADS), 1) k_paged_de
     float* const weight = (float*)(smem + warp * S::RING + sizeof(Record<D>));        // [state][query head]
     const int g8 = lane & 7;
     constexpr int QN = kWarps / 4 + 1;          // states of a lane at most
-    float4 t[QN];
-    float m = -INFINITY, M = -INFINITY, l = 0.f;
+    float2 t[QN];
+    float m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int k = 0; k < QN; ++k) {
       const int i = (lane >> 3) + 4 * k;
-      t[k] = i < n && g8 < p.G ? rec(i)->s[g8] : make_float4(-INFINITY, -INFINITY, 0.f, 0.f);
+      t[k] = i < n && g8 < p.G ? rec(i)->s[g8] : make_float2(-INFINITY, 0.f);
       m = fmaxf(m, t[k].x);
-      M = fmaxf(M, t[k].y);
     }
     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
-    M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, 8));
     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-    M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, 16));
-    const float ms = m == -INFINITY ? 0.f : m, Ms = M == -INFINITY ? 0.f : M;
+    const float ms = m == -INFINITY ? 0.f : m;
 #pragma unroll
     for (int k = 0; k < QN; ++k) {
       const int i = (lane >> 3) + 4 * k;
-      l = fmaf(t[k].z, ex2(t[k].x - ms), l);
-      if (i < n) weight[i * kMaxG + g8] = ex2(t[k].y - Ms);
+      const float w = ex2(t[k].x - ms);
+      l = fmaf(t[k].y, w, l);
+      if (i < n) weight[i * kMaxG + g8] = w;
     }
     l += __shfl_xor_sync(0xffffffffu, l, 8);
     l += __shfl_xor_sync(0xffffffffu, l, 16);
@@ -1145,10 +1134,10 @@ __global__ void __launch_bounds__((Shape<D, E, FMT, GP>::THREADS), 1) k_paged_de
     const bool open = us < F0 || ul >= F1;
     Record<D>* const to = cta_rec + (us < F0 ? 0 : 1);
     const int64_t row = (int64_t)unit * p.G;
-    const float f = finish<FMT>(m, M, l);
+    const float f = finish<FMT>(l);
     if (me == 0 && lane < p.G) {
       if (open) {
-        to->s[lane] = make_float4(m, M, l, 0.f);
+        to->s[lane] = make_float2(m, l);
       } else if (p.lse) {
         p.lse[row + lane] = log_sum(m, l);
       }
@@ -1226,26 +1215,23 @@ __global__ void __launch_bounds__((Shape<D, E, FMT, GP>::THREADS), 1) k_paged_de
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j)
       if (on && slice + j * slices < n) y[j] = __ldcg((const float4*)&record(slice + j * slices)->o[g][e % D]);
-    float4* const st = (float4*)(smem + warp * S::RING) + (lane / LPG) * kSMs;          // m, M, l of contributor i
-    float m = -INFINITY, M = -INFINITY, l = 0.f;
+    float2* const st = (float2*)(smem + warp * S::RING) + (lane / LPG) * kSMs;          // m, l of contributor i, then its weight
+    float m = -INFINITY, l = 0.f;
 #pragma unroll 1
     for (int i = lane % LPG; i < n; i += LPG) {
-      const float4 x = __ldcg(&record(i)->s[g]);
+      const float2 x = __ldcg(&record(i)->s[g]);
       st[i] = x;
       m = fmaxf(m, x.x);
-      M = fmaxf(M, x.y);
     }
 #pragma unroll
-    for (int o = 1; o < LPG; o <<= 1) {
-      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-      M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-    }
-    const float ms = m == -INFINITY ? 0.f : m, Ms = M == -INFINITY ? 0.f : M;
+    for (int o = 1; o < LPG; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const float ms = m == -INFINITY ? 0.f : m;
 #pragma unroll 1
     for (int i = lane % LPG; i < n; i += LPG) {
-      const float4 x = st[i];
-      l = fmaf(x.z, ex2(x.x - ms), l);
-      st[i].y = ex2(x.y - Ms);
+      const float2 x = st[i];
+      const float w = ex2(x.x - ms);
+      l = fmaf(x.y, w, l);
+      st[i].x = w;
     }
 #pragma unroll
     for (int o = 1; o < LPG; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
@@ -1260,18 +1246,18 @@ __global__ void __launch_bounds__((Shape<D, E, FMT, GP>::THREADS), 1) k_paged_de
     if (on) {
 #pragma unroll
       for (int j = 0; j < AHEAD; ++j)
-        if (slice + j * slices < n) add(st[slice + j * slices].y, y[j]);
+        if (slice + j * slices < n) add(st[slice + j * slices].x, y[j]);
 #pragma unroll 4
-      for (int i = slice + AHEAD * slices; i < n; i += slices) add(st[i].y, __ldcg((const float4*)&record(i)->o[g][e % D]));
+      for (int i = slice + AHEAD * slices; i < n; i += slices) add(st[i].x, __ldcg((const float4*)&record(i)->o[g][e % D]));
     }
     // a slice leaves its sums behind its statistics
-    auto part = [&](int s) { return (float4*)(smem + (team0 + s * chunks + chunk) * S::RING + kSMs * 2 * sizeof(float4)) + lane; };
+    auto part = [&](int s) { return (float4*)(smem + (team0 + s * chunks + chunk) * S::RING + kSMs * 2 * sizeof(float2)) + lane; };
     if (slice > 0 && slice < slices) *part(slice) = a;
     __syncthreads();
     if (on && slice == 0) {
 #pragma unroll 1
       for (int s = 1; s < slices; ++s) add(1.f, *part(s));
-      put4<EO>((uint8_t*)p.out + (row * D + e) * EO, a, finish<FMT>(m, M, l));
+      put4<EO>((uint8_t*)p.out + (row * D + e) * EO, a, finish<FMT>(l));
       if (p.lse && e % D == 0) p.lse[row + g] = log_sum(m, l);
     }
     __syncthreads();                            // before the other unit's join takes the same memory

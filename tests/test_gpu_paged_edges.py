@@ -118,3 +118,71 @@ def test_attention_infinite_values(dtype, D):
     want = p.cache.decode_attn(q, p.table, seq)
     assert torch.equal(out[:, :, :4][..., keep], want[:, :, :4][..., keep]) and torch.equal(out[:, :, 4:], want[:, :, 4:])
     p.check(q, want, lse, lens=lens)
+
+
+# ---------------------------------------------------------------------------
+# attention: values, scales and logits at the ends of their ranges
+# ---------------------------------------------------------------------------
+def own_bounds(out, lse, sizes, n, D, dtype, same_keys=False):
+    """As test_gpu_paged.bounds, but every channel by its own magnitudes (absv): a weight times its value's scale is kept
+    as a pair of bf16, the first cut (2^-7 left at most), the second to the nearest (2^-9 of that), 2^-16 in all, plus
+    2^-23 that the second is raised by.  Weights below 2^-117 of the largest may vanish.  Equal keys have equal logits,
+    whatever their rounding: the weights are then exact up to exp2."""
+    u = 2.0 ** -23
+    delta = (D + 4) * u * sizes["qk"] + (2.0 ** -39 * sizes["q_max"] if dtype == torch.bfloat16 else 0.0)
+    weights = (0.0 if same_keys else 2 * delta) + 2.0 ** -21 + (2.0 ** -16 + u if dtype == torch.bfloat16 else 0.0) + 2 * (n + 8) * u
+    tol = torch.finfo(dtype).eps / 2 * np.abs(out) + np.reshape(weights, (-1, 1)) * sizes["absv"] * (1 + 2.0 ** -7) + 1e-30
+    ltol = delta + (n + 8) * u + 2.0 ** -21 + 4 * u * np.abs(np.where(np.isfinite(lse), lse, 0.0))
+    return tol, ltol
+
+
+def check_own(p, q, out, lse, same_keys=False):
+    q64, o64, l64 = (x.double().cpu().numpy() for x in (q, out, lse))
+    for b in range(q.shape[0]):
+        for l in range(p.L):
+            for h in range(p.N_kv):
+                hs = slice(h * p.G, (h + 1) * p.G)
+                k, v = p.stored(b, l, h, p.lens[b])
+                r = po.attention(q64[b, l, hs], k, v, p.scale)
+                tol, ltol = own_bounds(*r, p.lens[b], p.D, p.dtype, same_keys)
+                err, e = np.abs(o64[b, l, hs] - r[0]), np.abs(l64[b, l, hs] - r[1])
+                assert (err <= tol).all(), f"{(b, l, hs)}: {(err / tol).max():.3g} of the bound at channel {(err / tol).max(0).argmax()}"
+                assert (e <= ltol).all(), f"lse {(b, l, hs)}: {e.max():.3g} > {ltol.min():.3g}"
+
+
+@pytest.mark.parametrize("fmt", ["plain", "e4m3", "int4"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("power", [10, 20, 30, 45, 60])
+def test_attention_channels_far_apart(fmt, D, power):
+    """Value channels whose magnitudes differ by 2^10 to 2^60 in a row (4 bits: its groups), and one token that is
+    2^power larger than all others, in its first channel alone: the other channels keep their share."""
+    p = Paged(fmt, torch.bfloat16, [200, 200, 3000], N_kv=2, G=3, D=D)
+    k, v = p.rows(7)
+    v = v.float()
+    if fmt != "e4m3":                                 # (an e4m3 row has one scale: such channels would be stored as zeros)
+        v[0, :, :, :, 32:64] *= 2.0 ** -power
+    v[1, 90, :, :, 1:] = 0
+    v[1, 90, :, :, 0] = 2.0 ** power
+    v[2, 1700, :, :, 1:] = 0
+    v[2, 1700, :, :, 0] = -(2.0 ** power)
+    p.cache.write(k, v.bfloat16(), p.table, rows=p.seq)
+    q = torch.randn(3, 1, 6, D, generator=gen(11), device="cuda").bfloat16()
+    out, lse = p.cache.decode_attn(q, p.table, p.seq, return_lse=True)
+    check_own(p, q, out, lse)
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS, ids=IDS)
+@pytest.mark.parametrize("power", [0, 8, 16, 24, 40])
+def test_attention_large_logits_of_equal_keys(fmt, dtype, power):
+    """Logits of any size, the same for every token of a sequence (one token's is): the output is the mean of the values,
+    whatever a logit's rounding is."""
+    lens = [1, 1, 2, 40, 300, 5000]
+    p = Paged(fmt, dtype, lens, N_kv=2, G=4)
+    k, v = p.rows(13)
+    k = k[:, :1].expand_as(k)
+    mags = 2.0 ** torch.randint(-20, 21, v.shape[:4] + (1,), generator=gen(37), device="cuda").float()
+    v = (v.float() * mags).to(dtype)
+    p.cache.write(k, v, p.table, rows=p.seq)
+    q = (torch.randn(len(lens), 1, 8, 128, generator=gen(17), device="cuda") * 2.0 ** power).to(dtype)
+    out, lse = p.cache.decode_attn(q, p.table, p.seq, return_lse=True)
+    check_own(p, q, out, lse, same_keys=True)
