@@ -14,16 +14,18 @@
 //    reads without bank conflicts.  Products run on mma.sync m16n8k16 with keys and values as A (16 tokens or channels)
 //    and the group's queries or weights as B: a group has at most 8 query rows, which is N here, and 8 of the 128 rows
 //    that a tcgen05 tile would have.
-//      logits  e4m3 and 4-bit codes become f16 exactly (byte conversion; a masked 4-bit code is the subnormal c * 2^-24
-//              or c * 2^-20, one multiply-add makes it (c - 8) * 2^-9); the query is f16 times a power of two, exact
-//              unless its channels are more than 2^28 apart.  (The fp8 form of the instruction takes codes as they
-//              are, but here it is a sequence of conversions and two f16 instructions: 22 cycles against 8.3, measured.)
-//      values  through ldmatrix.trans; the weights, which come out token by token, are transposed in registers.  bf16:
-//              the weights are a bf16 pair high + low (two instructions), 2^-16.  e4m3, 4-bit: f16 codes as above.  (The
-//              subnormals as they are would do, with the 8 taken off the sums, but the tensor core aligns products by
-//              exponent fields: sums then keep 2^-15 instead of 2^-22, measured.)
-//      scales  of keys multiply logits, those of values go into the weights, which are rounded to f16 (2^-11) relative
-//              to the largest weight * scale so far, kept between 2^7 and 2^15: f16 leaves 21 binary orders below that.
+//      logits  bf16 and 4-bit pages: bf16 products, exact (a masked 4-bit code is the subnormal c * 2^-133 or c * 2^-129,
+//              one multiply-add makes it (c - 8) / 64).  e4m3 codes become f16 by byte conversion; the query is f16
+//              times a power of two, exact unless its channels are more than 2^28 apart.  (The fp8 form of the
+//              instruction takes codes as they are, but here it is a sequence of conversions and two f16
+//              instructions: 22 cycles against 8.3, measured.)
+//      values  through ldmatrix.trans, as bf16 (4-bit codes as above, e4m3 through f16 and fp32); the weights, which
+//              come out token by token, are transposed in registers.  A weight, times its value's scale, is a bf16 pair
+//              high + low (two instructions), 2^-16: it has the range of fp32, so that no channel's or token's share
+//              is lost to larger ones.  (f16 weights relative to the largest weight * scale so far took one instruction
+//              - e4m3, 4 x 32768 tokens: 51 us against 53; 4-bit ragged: 68 against 73 - but left 21 binary orders
+//              below that largest one, over all channels and tokens.)
+//      scales  of keys multiply logits, those of values the weights.
 //      fp32    CUDA cores: fp32 products summed over lanes pairwise.
 //  * The softmax is online in base 2 with fp32 maximum, sum and accumulators.  Units that several warps share leave
 //    partial states; the warps' states are joined by their CTA, the CTAs' states by the CTA that arrives last at
@@ -159,6 +161,15 @@ __device__ __forceinline__ void pair_bf16(float w0, float w1, uint32_t& hi, uint
   split(fma2(two(w0, w1), two(1.f + 0x1p-23f, 1.f + 0x1p-23f),
              two(__uint_as_float((u0 & 0xffff0000u) ^ 0x80000000u), __uint_as_float((u1 & 0xffff0000u) ^ 0x80000000u))), a, b);
   lo = pack_bf16(a, b);
+}
+// Two such pairs (here the first part is rounded to the nearest) times two bf16 scales, as pairs again: the product's
+// first 8 bits, and what they leave of it (exact, it has 8 more) plus the second part's product.  Within 2^-17.
+__device__ __forceinline__ void scale_pair(uint32_t wh, uint32_t wl, uint32_t f, uint32_t& hi, uint32_t& lo) {
+  const __nv_bfloat162 a = *(const __nv_bfloat162*)&wh, b = *(const __nv_bfloat162*)&wl, s = *(const __nv_bfloat162*)&f;
+  const __nv_bfloat162 h = __hmul2_rn(a, s);
+  const __nv_bfloat162 r = __hfma2(b, s, __hfma2(a, s, __hneg2(h)));
+  hi = *(const uint32_t*)&h;
+  lo = *(const uint32_t*)&r;
 }
 // two e4m3 bytes as f16: the lower and the upper half of a word
 __device__ __forceinline__ uint32_t e4m3_lo_to_f16x2(uint32_t w) {
@@ -535,14 +546,14 @@ struct MmaState {
           }
         }
       } else {
-        // weights are transposed once, as they are (two halves each), and meet the scales of their tokens behind that
-        f32x2 wt[2];                            // query r, tokens 2qd, 2qd + 1 and the same + 8
+        // weights are transposed as pairs, once, and meet the scales of their tokens behind that
+        uint32_t wh[2], wl[2];                  // query r, tokens 2qd, 2qd + 1 and the same + 8
         uint32_t sc[2][NG];                     // their scales: NG / 2 words a token
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const uint32_t u0 = __float_as_uint(w[j][0]), u1 = __float_as_uint(w[j][1]);
-          const uint32_t lo = transpose8(__byte_perm(u0, u1, 0x5410)), hi = transpose8(__byte_perm(u0, u1, 0x7632));
-          wt[j] = two(__uint_as_float(__byte_perm(lo, hi, 0x5410)), __uint_as_float(__byte_perm(lo, hi, 0x7632)));
+          wh[j] = pack_bf16(w[j][0], w[j][1]);
+          wl[j] = transpose8(pack_bf16(w[j][0] - bf16lo(wh[j]), w[j][1] - bf16hi(wh[j])));
+          wh[j] = transpose8(wh[j]);
           load_scales2(vs2 + (16 * kk + 8 * j) * S::SB, sc[j]);
         }
         const int off = S::RB == 64 ? vr * 64 + (((mi >> 1) ^ (tr >> 1)) << 4) : vr * 32 + (((mi >> 1) ^ (tr >> 2)) << 4);
@@ -556,10 +567,8 @@ struct MmaState {
             uint32_t hi[2], lo[2];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-              const uint32_t s0 = sc[t][g2], s1 = sc[t][NG / 2 + g2];
-              float f0, f1;
-              split(mul2(wt[t], j ? two(bf16hi(s0), bf16hi(s1)) : two(bf16lo(s0), bf16lo(s1))), f0, f1);
-              pair_bf16(f0, f1, hi[t], lo[t]);
+              const uint32_t f = __byte_perm(sc[t][g2], sc[t][NG / 2 + g2], j ? 0x7632 : 0x5410);
+              scale_pair(wh[t], wl[t], f, hi[t], lo[t]);
             }
             const uint32_t a = v[2 * j], b = v[2 * j + 1], a8 = a >> 8, b8 = b >> 8;
             uint32_t a0 = int4_lo_to_bf16x2(a), a1 = int4_hi_to_bf16x2(a), a2 = int4_lo_to_bf16x2(b), a3 = int4_hi_to_bf16x2(b);
