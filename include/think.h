@@ -421,7 +421,8 @@ thinK_status thinK_paged_read(thinK_paged* p, thinK_tensor5 k, thinK_tensor5 v, 
  *   q, out: dense [B, nlayers, N_q, D] in cfg.dtype.  q, out and lse may not overlap.
  *   lse:    fp32 [B, nlayers, N_q], the natural logarithm of the softmax's sum (for joining with attention over
  *           other tokens), or NULL.
- *   seq_len: device int32 [B].  A sequence without tokens gets out = 0 and lse = -infinity.
+ *   seq_len: device int32 [B].  A sequence without tokens gets out = 0 and lse = -infinity; one with tokens
+ *           whose logits are all -infinity (keys of infinities) gets out = NaN and lse = -infinity.
  *   scratch: NULL for the handle's own workspace, or a device buffer of scratch_bytes >= thinK_paged_sizes.workspace
  *           (of the handle that it is given to), 256-byte aligned, that was filled with zeros once before its first use.
  *           A call leaves it ready for the next one, of the same handle or of any other.  Calls that may run at the

@@ -39,6 +39,7 @@
 //   int4  32 / 8 heads, 8192 tokens                           13 us   launch, three dependent loads and two joins
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
+#include <float.h>
 #include <math.h>
 
 #include "paged_internal.h"
@@ -48,6 +49,8 @@ namespace think {
 namespace {
 
 constexpr int kMaxWarps = 12;
+// reference of a unit whose tokens had no logit above -infinity so far; without any token it is -infinity
+constexpr float kLowest = -FLT_MAX;
 constexpr float kAhead = 8.f;                 // how far above the largest logit weights' reference is put when it moves
 constexpr int kMaxG = kMaxPagedGroup;
 
@@ -285,7 +288,7 @@ struct WarpInfo {
 // Tensor-core formats: fragments of a warp.  Lane (r = lane / 4, qd = lane % 4).  Logits and accumulators have the
 // lane's queries 2 qd, 2 qd + 1 in register pairs: logits of tokens 8 n + r of the step, accumulators of channels by r.
 template <int FMT>
-__device__ __forceinline__ float finish(float l);
+__device__ __forceinline__ float finish(float m, float l);
 
 template <int D, int FMT>
 struct MmaState {
@@ -465,7 +468,7 @@ struct MmaState {
       for (int n = 0; n < NT; ++n)
         if (8 * n + r >= ntok) x[n] = two(-INFINITY, -INFINITY);
     }
-    float mx[2] = {-INFINITY, -INFINITY};
+    float mx[2] = {ntok > 0 ? kLowest : -INFINITY, ntok > 0 ? kLowest : -INFINITY};
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       float a, b;
@@ -637,10 +640,11 @@ struct MmaState {
   __device__ __forceinline__ void store_out(void* out, float* lse, int G, int lane) const;
 };
 
-// factor that turns joined accumulators into outputs: 0 where no token counted (a NaN logit leaves m alone, not l)
+// Factor that turns joined accumulators into outputs: 0 where no token counted.  Tokens whose logits are all -infinity
+// have no softmax: 1 / 0 times accumulators of 0, a NaN.  (A NaN logit leaves m alone, not l.)
 template <int FMT>
-__device__ __forceinline__ float finish(float l) {
-  return l == 0.f ? 0.f : (FMT == THINK_PAGE_INT4 ? kInt4Unit : 1.f) / l;
+__device__ __forceinline__ float finish(float m, float l) {
+  return m == -INFINITY && l == 0.f ? 0.f : (FMT == THINK_PAGE_INT4 ? kInt4Unit : 1.f) / l;
 }
 // four joined accumulators to four outputs of EO bytes
 template <int EO>
@@ -658,7 +662,7 @@ __device__ __forceinline__ void MmaState<D, FMT>::store_out(void* out, float* ls
   const int q0 = 2 * (lane & 3);
   float ls[2];
   split(l, ls[0], ls[1]);
-  const float f0 = finish<FMT>(ls[0]), f1 = finish<FMT>(ls[1]);
+  const float f0 = finish<FMT>(m[0], ls[0]), f1 = finish<FMT>(m[1], ls[1]);
   __nv_bfloat16* const po = (__nv_bfloat16*)out + q0 * D;
   auto write = [&](__nv_bfloat16* to, const float (&v)[WIDTH], float f) {
     if constexpr (WIDTH == 1) {
@@ -752,7 +756,7 @@ struct F32State {
 #pragma unroll
       for (int i = 0; i < R; ++i) x[i] += __shfl_xor_sync(0xffffffffu, x[i], 16 >> b);
     const int idx = owner(lane);
-    float mx = -INFINITY;
+    float mx = ntok > 0 ? kLowest : -INFINITY;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       if (((idx + i) & (ST - 1)) >= ntok) x[i] = -INFINITY;
@@ -820,7 +824,7 @@ struct F32State {
       const int src = (g * ST / R) << (5 - LB);
       const float mg = __shfl_sync(0xffffffffu, m, src), lg = __shfl_sync(0xffffffffu, l, src);
       if (g < G) {
-        const float f = finish<THINK_PAGE_PLAIN>(lg);
+        const float f = finish<THINK_PAGE_PLAIN>(mg, lg);
 #pragma unroll
         for (int i = 0; i < N; ++i) ((float*)out)[g * D + lane * N + i] = f == 0.f ? 0.f : o[g][i] * f;
         if (lse && lane == 0) lse[g] = log_sum(mg, lg);
@@ -1143,7 +1147,7 @@ __global__ void __launch_bounds__((Shape<D, E, FMT, GP>::THREADS), 1) k_paged_de
     const bool open = us < F0 || ul >= F1;
     Record<D>* const to = cta_rec + (us < F0 ? 0 : 1);
     const int64_t row = (int64_t)unit * p.G;
-    const float f = finish<FMT>(l);
+    const float f = finish<FMT>(m, l);
     if (me == 0 && lane < p.G) {
       if (open) {
         to->s[lane] = make_float2(m, l);
@@ -1266,7 +1270,7 @@ __global__ void __launch_bounds__((Shape<D, E, FMT, GP>::THREADS), 1) k_paged_de
     if (on && slice == 0) {
 #pragma unroll 1
       for (int s = 1; s < slices; ++s) add(1.f, *part(s));
-      put4<EO>((uint8_t*)p.out + (row * D + e) * EO, a, finish<FMT>(l));
+      put4<EO>((uint8_t*)p.out + (row * D + e) * EO, a, finish<FMT>(m, l));
       if (p.lse && e % D == 0) p.lse[row + g] = log_sum(m, l);
     }
     __syncthreads();                            // before the other unit's join takes the same memory

@@ -186,3 +186,27 @@ def test_attention_large_logits_of_equal_keys(fmt, dtype, power):
     q = (torch.randn(len(lens), 1, 8, 128, generator=gen(17), device="cuda") * 2.0 ** power).to(dtype)
     out, lse = p.cache.decode_attn(q, p.table, p.seq, return_lse=True)
     check_own(p, q, out, lse, same_keys=True)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=IDS[:2])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_logits_of_minus_infinity(dtype, D):
+    """Keys of -infinity.  A sequence whose every logit is -infinity has no softmax: NaN, not the zeros of a sequence
+    without tokens (the sum's logarithm is -infinity for both); one finite logit takes all of the weight."""
+    inf = float("inf")
+    lens = [1, 70, 5000, 1, 70, 5000, 0]
+    p = Paged("plain", dtype, lens, N_kv=2, G=4, D=D)
+    k, v = p.rows(29)
+    k[:, :, :, 0, 5] = -inf
+    last = [n - 1 for n in lens]
+    for b in (3, 4, 5):
+        k[b, last[b], 0, 0, 5] = 1
+    p.cache.write(k, v, p.table, rows=p.seq)
+    q = torch.randn(len(lens), 1, 8, D, generator=gen(31), device="cuda").to(dtype)
+    q[..., 5] = q[..., 5].abs() + 1
+    out, lse = p.cache.decode_attn(q, p.table, p.seq, return_lse=True)
+    assert torch.isnan(out[:3, 0, :4]).all() and torch.isneginf(lse[:3, 0, :4]).all()
+    assert (out[6] == 0).all() and torch.isneginf(lse[6]).all()
+    for b in (3, 4, 5):
+        assert torch.equal(out[b, 0, :4], v[b, last[b], 0, 0].expand(4, D)) and torch.isfinite(lse[b]).all()
+    p.check(q, out, lse, units={(b, 0, 1) for b in range(6)})
