@@ -356,8 +356,9 @@ struct MmaState {
       t = max(t & 0xffffu, t >> 16);
       t = max(t, __shfl_xor_sync(0xffffffffu, t, 1));
       t = max(t, __shfl_xor_sync(0xffffffffu, t, 2));
-      // the row's largest channel goes to [2^14, 2^15)
-      const int k = min(141 - (int)(t >> 7), 100);
+      // the row's largest channel goes to [2^14, 2^15), as far as the power and the factor that takes it back are
+      // ordinary numbers
+      const int k = min(141 - (int)(t >> 7), min(126, (int)(__float_as_uint(scale_log2) >> 23) - 1));
       const float up = pow2i(k), down = scale_log2 * pow2i(-k);
       rs = two(__shfl_sync(0xffffffffu, down, 8 * qd), __shfl_sync(0xffffffffu, down, 8 * qd + 4));
 #pragma unroll

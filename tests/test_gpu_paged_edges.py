@@ -210,3 +210,16 @@ def test_attention_logits_of_minus_infinity(dtype, D):
     for b in (3, 4, 5):
         assert torch.equal(out[b, 0, :4], v[b, last[b], 0, 0].expand(4, D)) and torch.isfinite(lse[b]).all()
     p.check(q, out, lse, units={(b, 0, 1) for b in range(6)})
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS, ids=IDS)
+@pytest.mark.parametrize("q_pow,k_pow,scale", [(-120, 120, 0.0), (-90, 91, 0.0), (-100, 118, 2.0 ** -20), (110, -109, 0.0), (60, -80, 2.0 ** 20)])
+def test_attention_tiny_queries_and_huge_keys(fmt, dtype, q_pow, k_pow, scale):
+    """Queries and keys at opposite ends of the exponent range, logits of ordinary size."""
+    p = Paged(fmt, dtype, [1, 150], N_kv=2, G=4, scale=scale)
+    k, v = p.rows(43, outliers=False)
+    p.cache.write((k.float() * 2.0 ** k_pow).to(dtype), v, p.table, rows=p.seq)
+    q = (torch.randn(2, 1, 8, 128, generator=gen(47), device="cuda") * 2.0 ** q_pow).to(dtype)
+    out, lse = p.cache.decode_attn(q, p.table, p.seq, return_lse=True)
+    assert (lse[0].abs() > 2.0 ** -8).all()
+    p.check(q, out, lse)
