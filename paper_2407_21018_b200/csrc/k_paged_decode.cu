@@ -52,6 +52,10 @@ constexpr int kMaxWarps = 12;
 // reference of a unit whose tokens had no logit above -infinity so far; without any token it is -infinity
 constexpr float kLowest = -FLT_MAX;
 constexpr float kAhead = 8.f;                 // how far above the largest logit weights' reference is put when it moves
+// While all value scales of a unit are below 2^-80 the reference is put 48 below the largest logit, and moves when that
+// is 8 more: weights from 2^48 on keep products with scales down to 2^-133 away from the ends of bf16 and fp32.
+constexpr float kSmallBehind = 48.f, kSmallLead = 56.f;
+constexpr uint32_t kSmallScale = 127 - 80;    // exponent field
 constexpr int kMaxG = kMaxPagedGroup;
 
 // GP: query heads that the fp32 kernel computes at a time
@@ -81,8 +85,8 @@ struct Shape {
   static_assert(RING >= (2 * kMaxG + kMaxG * (D + 4) + kMaxWarps * kMaxG) * 4 && RING >= kSMs * 2 * 8 + 512, "ring");
 };
 
-// Partial state of one (worker, unit).  m: the logit (base 2) that weights are relative to, at least the largest one and
-// at most 8 above it; l: sum of the weights exp2(logit - m).
+// Partial state of one (worker, unit).  m: the logit (base 2) that weights are relative to, near the largest one; l: sum
+// of the weights exp2(logit - m).
 // Rows are 4 floats longer than D: the lanes of a fragment, two rows apart, then store to different banks.
 template <int D>
 struct Record {
@@ -303,6 +307,7 @@ struct MmaState {
   uint32_t q[NG][4];         // B fragments of the two k16 instructions of a block: query r
   f32x2 rs;                  // base-2 logit per unit of the q k product
   float m[2];                // what weights are relative to
+  float lead;                // how far a logit may exceed that: 0, or kSmallLead (value scales all small so far)
   f32x2 l;                   // of this lane's tokens until end()
   float o[OT][4];
 
@@ -367,6 +372,7 @@ struct MmaState {
         for (int i = 0; i < 4; ++i) q[g][i] = pack_f16(bf16lo(w[g][i]) * up, bf16hi(w[g][i]) * up);
     }
     m[0] = m[1] = -INFINITY;
+    lead = PLAIN ? 0.f : kSmallLead;
     l = 0;
 #pragma unroll
     for (int t = 0; t < OT; ++t) o[t][0] = o[t][1] = o[t][2] = o[t][3] = 0.f;
@@ -477,15 +483,32 @@ struct MmaState {
       mx[0] = fmaxf(mx[0], a);
       mx[1] = fmaxf(mx[1], b);
     }
+    if (!PLAIN && lead > 0.f) {
+      bool big = false;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        if constexpr (INT4) {                   // bit 15 of a half: its exponent field is at least kSmallScale
+          uint32_t sc[NG / 2];
+          load_scales(vs + 8 * n * S::SB, sc);
+#pragma unroll
+          for (int i = 0; i < NG / 2; ++i)
+            big |= (((sc[i] & 0x7fff7fffu) + 0x00010001u * (0x8000u - (kSmallScale << 7))) & 0x80008000u) != 0;
+        } else {
+          big |= load_byte(vs + 8 * n) >= kSmallScale;
+        }
+      }
+      if (__any_sync(0xffffffffu, big)) lead = 0.f;
+    }
     // The reference moves when a logit exceeds it, and is then put 8 above, so that it seldom moves.  Weights are at most
     // 1, the largest at least 2^-8: weight times value keeps to the value's range.
-    if (__any_sync(0xffffffffu, mx[0] > m[0] || mx[1] > m[1])) {
+    if (__any_sync(0xffffffffu, mx[0] > m[0] + lead || mx[1] > m[1] + lead)) {
+      const float ahead = lead > 0.f ? -kSmallBehind : kAhead;
       float sm[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
 #pragma unroll
         for (int k = 4; k < 32; k <<= 1) mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], k));
-        const float to = mx[i] > m[i] ? mx[i] + kAhead : m[i];
+        const float to = mx[i] > m[i] + lead ? mx[i] + ahead : m[i];
         sm[i] = m[i] == -INFINITY ? 0.f : ex2(m[i] - to);
         m[i] = to;
       }

@@ -123,7 +123,7 @@ def test_attention_infinite_values(dtype, D):
 # ---------------------------------------------------------------------------
 # attention: values, scales and logits at the ends of their ranges
 # ---------------------------------------------------------------------------
-def own_bounds(out, lse, sizes, n, D, dtype, same_keys=False):
+def own_bounds(out, lse, sizes, n, D, dtype, same_keys=False, floor=1e-30):
     """As test_gpu_paged.bounds, but every channel by its own magnitudes (absv): a weight times its value's scale is kept
     as a pair of bf16, the first cut (2^-7 left at most), the second to the nearest (2^-9 of that), 2^-16 in all, plus
     2^-23 that the second is raised by.  Weights below 2^-117 of the largest may vanish.  Equal keys have equal logits,
@@ -131,12 +131,12 @@ def own_bounds(out, lse, sizes, n, D, dtype, same_keys=False):
     u = 2.0 ** -23
     delta = (D + 4) * u * sizes["qk"] + (2.0 ** -39 * sizes["q_max"] if dtype == torch.bfloat16 else 0.0)
     weights = (0.0 if same_keys else 2 * delta) + 2.0 ** -21 + (2.0 ** -16 + u if dtype == torch.bfloat16 else 0.0) + 2 * (n + 8) * u
-    tol = torch.finfo(dtype).eps / 2 * np.abs(out) + np.reshape(weights, (-1, 1)) * sizes["absv"] * (1 + 2.0 ** -7) + 1e-30
+    tol = torch.finfo(dtype).eps / 2 * np.abs(out) + np.reshape(weights, (-1, 1)) * sizes["absv"] * (1 + 2.0 ** -7) + floor
     ltol = delta + (n + 8) * u + 2.0 ** -21 + 4 * u * np.abs(np.where(np.isfinite(lse), lse, 0.0))
     return tol, ltol
 
 
-def check_own(p, q, out, lse, same_keys=False):
+def check_own(p, q, out, lse, same_keys=False, floor=lambda b: 1e-30):
     q64, o64, l64 = (x.double().cpu().numpy() for x in (q, out, lse))
     for b in range(q.shape[0]):
         for l in range(p.L):
@@ -144,7 +144,7 @@ def check_own(p, q, out, lse, same_keys=False):
                 hs = slice(h * p.G, (h + 1) * p.G)
                 k, v = p.stored(b, l, h, p.lens[b])
                 r = po.attention(q64[b, l, hs], k, v, p.scale)
-                tol, ltol = own_bounds(*r, p.lens[b], p.D, p.dtype, same_keys)
+                tol, ltol = own_bounds(*r, p.lens[b], p.D, p.dtype, same_keys, floor(b))
                 err, e = np.abs(o64[b, l, hs] - r[0]), np.abs(l64[b, l, hs] - r[1])
                 assert (err <= tol).all(), f"{(b, l, hs)}: {(err / tol).max():.3g} of the bound at channel {(err / tol).max(0).argmax()}"
                 assert (e <= ltol).all(), f"lse {(b, l, hs)}: {e.max():.3g} > {ltol.min():.3g}"
@@ -223,3 +223,31 @@ def test_attention_tiny_queries_and_huge_keys(fmt, dtype, q_pow, k_pow, scale):
     out, lse = p.cache.decode_attn(q, p.table, p.seq, return_lse=True)
     assert (lse[0].abs() > 2.0 ** -8).all()
     p.check(q, out, lse)
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS, ids=IDS)
+@pytest.mark.parametrize("power", [-104, -112, -120, -126])
+def test_attention_tiny_values(fmt, dtype, power):
+    """Values down to the smallest ordinary numbers: outputs are as exact as those of any size, up to half a step of
+    bf16's smallest numbers where all of a sequence's values are tiny.  Sequences 1 and 2 hold one token of ordinary values that has next to no weight, in front
+    of all others and behind them; sequence 3 one that has weight."""
+    p = Paged(fmt, dtype, [1, 300, 300, 300, 5000], N_kv=2, G=4)
+    k, v = p.rows(83)
+    v = v.float() * 2.0 ** power
+    q = torch.randn(5, 1, 8, 128, generator=gen(89), device="cuda").to(dtype)
+    for b, t, like in ((1, 0, -4.0), (2, 299, -4.0), (3, 150, 0.5)):
+        v[b, t] = torch.randn(1, 2, 128, generator=gen(91), device="cuda")
+        k[b, t, 0] = (like * q[b, 0].view(2, 4, 128).float().sum(1)).to(dtype)
+    p.cache.write(k, v.to(dtype), p.table, rows=p.seq)
+    out, lse = p.cache.decode_attn(q, p.table, p.seq, return_lse=True)
+    # Half a step of the smallest outputs; fp32 sums of numbers below 2^-126 miss half of 2^-149 a token, weights (and so
+    # the sums) may be 2^-8 of what they are divided by.  Beside the ordinary token of sequences 1 to 3 (which flips the
+    # reference of the weights) a token's weight * scale may be below 2^-117: a pair of bf16 then misses up to 2^-133 of
+    # it, times its code (448 or 7 at most), divided by a sum of 2^-8 at least: 2^-125 code a token.  That shows in
+    # channels in which the ordinary token's code is 0, and absv with it of the tiny ones' size.
+    half, code = (2.0 ** -134 if dtype == torch.bfloat16 else 2.0 ** -150), {"plain": 0.0, "e4m3": 448.0, "int4": 7.0}[fmt]
+
+    def floor(b):
+        return half + p.lens[b] * (2.0 ** -142 + (code * 2.0 ** -125 if b in (1, 2, 3) else 0.0))
+
+    check_own(p, q, out, lse, floor=floor)
