@@ -331,12 +331,13 @@ thinK_status thinK_destroy(thinK_cache* c);
  *     64 key rows | 64 value rows | scales of the 64 key rows | scales of the 64 value rows
  * and a row is the D channels of one token in order (no swizzle, no padding):
  *   THINK_PAGE_PLAIN  the elements themselves (cfg.dtype), no scales.
- *   THINK_PAGE_E4M3   one e4m3 byte per channel, one scale byte per row: byte e, 1 to 254, is 2^(e - 127).  Written
- *                     rows use the smallest power of two >= 2^-126 under which the row's largest magnitude is at
+ *   THINK_PAGE_E4M3   one e4m3 byte per channel, one scale byte per row: byte e is 2^(e - 127), 255 a NaN.  Written rows
+ *                     use the smallest power of two >= 2^-126 under which the row's largest magnitude is at
  *                     most 448; codes are x / scale rounded to nearest even.  bf16 caches only.
  *   THINK_PAGE_INT4   4 bits per channel (the even channel of a pair in the low half of the byte), code = n + 8,
  *                     one bf16 scale per 32 channels, channel groups in order: s = amax / 7 rounded to bf16,
- *                     n = x / s rounded to nearest even and limited to [-7, 7]; s = 0 gives n = 0.  bf16 caches only.
+ *                     n = x / s rounded to nearest even and limited to [-7, 7]; s = 0 gives n = 0.  Stored scales
+ *                     are finite or NaN.  bf16 caches only.
  * A row (E4M3) or a group of 32 channels (INT4) that holds a NaN or an infinity is stored so that all of it reads
  * back as NaN, and sets bit 8 of the device error word.
  *

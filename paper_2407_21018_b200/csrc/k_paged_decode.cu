@@ -439,7 +439,7 @@ struct MmaState {
             else mma<false>(c[j & 1], a0, a1, a2, a3, b0, b1);
           }
         }
-        const float s0 = __uint_as_float(load_byte(ks + 8 * n) << 23), s1 = __uint_as_float(load_byte(ks + 8 * n + 8) << 23);
+        const float s0 = e8m0(load_byte(ks + 8 * n)), s1 = e8m0(load_byte(ks + 8 * n + 8));
         x[n] = mul2(add2(two(c[0][0], c[0][1]), two(c[1][0], c[1][1])), mul2(rs, two(s0, s0)));
         x[n + 1] = mul2(add2(two(c[0][2], c[0][3]), two(c[1][2], c[1][3])), mul2(rs, two(s1, s1)));
       } else {
@@ -540,7 +540,7 @@ struct MmaState {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           if constexpr (!PLAIN) {               // the row's scale
-            const float f = __uint_as_float(load_byte(vs + 16 * kk + 8 * j) << 23);
+            const float f = e8m0(load_byte(vs + 16 * kk + 8 * j));
             split(mul2(two(w[j][0], w[j][1]), two(f, f)), w[j][0], w[j][1]);
           }
           pair_bf16(w[j][0], w[j][1], hi[j], lo[j]);

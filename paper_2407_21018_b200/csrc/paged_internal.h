@@ -1,5 +1,7 @@
 // Shared by the translation units of the paged key-value cache.
 #pragma once
+#include <cuda_fp8.h>
+
 #include "think_internal.h"
 
 namespace think {
@@ -160,9 +162,10 @@ __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
   return r;
 }
 
-// value of a scale byte e of an e4m3 row: 2^(e - 127); byte 0 is 2^-127 (a subnormal), byte 255 is NaN
+// value of a scale byte e of an e4m3 row: 2^(e - 127), which for byte 0 is a subnormal; byte 255 is NaN.  (One conversion;
+// selecting the two ends by hand cost the attention 9 %.)
 __device__ __forceinline__ float e8m0(uint32_t e) {
-  return __uint_as_float(e == 0 ? 0x00400000u : e == 255 ? 0x7fc00000u : e << 23);
+  return __uint_as_float((uint32_t)__nv_cvt_e8m0_to_bf16raw((__nv_fp8_storage_t)e).x << 16);
 }
 #endif
 

@@ -251,3 +251,61 @@ def test_attention_tiny_values(fmt, dtype, power):
         return half + p.lens[b] * (2.0 ** -142 + (code * 2.0 ** -125 if b in (1, 2, 3) else 0.0))
 
     check_own(p, q, out, lse, floor=floor)
+
+
+@pytest.mark.parametrize("byte", [0, 1, 254, 255])
+@pytest.mark.parametrize("D", [64, 128])
+def test_scale_bytes_at_the_ends(byte, D):
+    """Scale bytes 0 (2^-127) and 255 (NaN) are never written, but mean the same to attention as to the read-back, as the
+    ends of the ordinary range do."""
+    tk = binding()
+    p = Paged("e4m3", torch.bfloat16, [1, 1, 70, 70], N_kv=2, G=3, D=D)
+    k, v = p.rows(41)
+    k[:2] *= 2.0 ** -6                                # codes far below 448: 2^127 times them stays in range
+    v[:2] *= 2.0 ** -6
+    p.cache.write(k, v, p.table, rows=p.seq)
+
+    def patch(b, tok, part):
+        page = int(p.table_cpu[b, tok // PAGE])
+        at = tk.paged_offset(p.cfg, 0, page, 0, tok % PAGE, part)
+        p.pool[at] = byte
+        if byte == 254:                               # codes that 2^127 keeps in bf16's range
+            row = tk.paged_offset(p.cfg, 0, page, 0, tok % PAGE, part - 2)
+            p.pool[row:row + D] = torch.tensor([0x38, 0xb8, 0x08, 0x00], dtype=torch.uint8, device="cuda").repeat(D // 4)
+
+    patch(0, 0, tk.PART_V_SCALE)
+    patch(1, 0, tk.PART_K_SCALE)
+    patch(2, 66, tk.PART_V_SCALE)
+    patch(3, 5, tk.PART_K_SCALE)
+    ko, vo = torch.zeros_like(k), torch.zeros_like(v)
+    p.cache.read(ko, vo, p.table, rows=p.seq)
+    small = byte >= 254                               # queries that bring the patched keys' logits to order 1
+    q = torch.randn(4, 1, 6, D, generator=gen(43), device="cuda")
+    q[1] *= 2.0 ** (-125 if small else 110)
+    q[3] *= 2.0 ** (-125 if small else 0)
+    q = q.bfloat16()
+    out, lse = p.cache.decode_attn(q, p.table, p.seq, return_lse=True)
+    if byte == 255:
+        assert torch.isnan(vo[0, 0, 0, 0]).all() and torch.isnan(ko[1, 0, 0, 0]).all()
+        assert torch.isnan(out[[0, 1, 2, 3], 0, :3]).all()
+        assert torch.isnan(lse[[1, 3], 0, :3]).all() and torch.isfinite(lse[[0, 2]]).all()
+    else:
+        assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+        # the only token's value as it is read back
+        assert torch.equal(out[0, 0, :3], vo[0, 0, 0, 0].expand(3, D)) and out[0, 0, :3].abs().sum() > 0
+        q64 = q.double().cpu().numpy()
+        for b in (1, 3):
+            kk, vv = p.stored(b, 0, 0, p.lens[b])
+            r = po.attention(q64[b, 0, :3], kk, vv, p.scale)
+            tol, ltol = bounds(*r, p.lens[b], D, "e4m3", torch.bfloat16)
+            assert (np.abs(out[b, 0, :3].double().cpu().numpy() - r[0]) <= tol).all()
+            assert (np.abs(lse[b, 0, :3].double().cpu().numpy() - r[1]) <= ltol).all()
+            if b == 1:
+                assert (lse[b, 0, :3].abs() > 2.0 ** -20).all()
+    other = slice(3, 6)
+    q0 = q[:, :, other]
+    for b in range(4):
+        kk, vv = p.stored(b, 0, 1, p.lens[b])
+        r = po.attention(q0[b, 0].double().cpu().numpy(), kk, vv, p.scale)
+        tol, _ = bounds(*r, p.lens[b], D, "e4m3", torch.bfloat16)
+        assert (np.abs(out[b, 0, other].double().cpu().numpy() - r[0]) <= tol).all()
