@@ -358,7 +358,8 @@ class PagedKVCache:
 
     Tables are int32 [B, max_pages] (rows may be strided), lengths, positions and row counts int32 [B], all on the
     cache's device.  `pages`: an existing pool (uint8, cfg's size) to work on; by default one is allocated.  Calls
-    run on the device's current stream unless one is given."""
+    run on the device's current stream unless one is given.  The cache may be dropped while calls on any stream are
+    under way; the tensors given to a call, and the cache a captured graph works on, are the caller's to keep."""
 
     def __init__(self, cfg: PagedConfig, device="cuda", pages: Optional[torch.Tensor] = None):
         self.handle = None
@@ -391,6 +392,19 @@ class PagedKVCache:
         self.torch_dtype = torch.bfloat16 if c.dtype == BF16 else torch.float32
         self._index = self.device.index
         self._L, self._N_q, self._N_kv, self._D, self._max_batch = c.L, c.N_q, c.N_kv, c.D, c.max_batch
+        self._streams = set()
+
+    def _stream(self, stream: Optional["torch.cuda.Stream"]) -> int:
+        """The raw stream of a call.  The first call on a stream tells torch's allocator that it uses the cache's memory:
+        dropping the cache then hands that memory out again only when the calls on all of its streams are done."""
+        raw = _raw_stream(self._index) if stream is None else stream.cuda_stream
+        if raw not in self._streams:
+            if stream is None:
+                stream = torch.cuda.current_stream(self._index)
+            self.workspace.record_stream(stream)
+            self.pages.record_stream(stream)
+            self._streams.add(raw)
+        return raw
 
     def new_scratch(self) -> torch.Tensor:
         """A scratch buffer for attention calls that may run at the same time as others of this cache.  Any cache that
@@ -441,7 +455,7 @@ class PagedKVCache:
         self._call(fn, where, Tensor5(k.data_ptr(), kb, ks, kl, kn), Tensor5(v.data_ptr(), vb, vs, vl, vn),
                    self._table(table, B, where), self._vector(pos, B, where, ": pos"),
                    self._vector(rows, B, where, ": rows"), max_rows, layer0, n,
-                   _raw_stream(index) if stream is None else stream.cuda_stream)
+                   self._stream(stream))
 
     # -- the calls ------------------------------------------------------
     def write(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, pos: Optional[torch.Tensor] = None,
@@ -494,7 +508,7 @@ class PagedKVCache:
         self._call(lib.thinK_paged_decode_attn, where, q.data_ptr(), out.data_ptr(),
                    None if lse is None else lse.data_ptr(), self._table(table, B, where),
                    self._vector(seq_lens, B, where, ": seq_lens"), work, work_bytes, layer0, n,
-                   _raw_stream(index) if stream is None else stream.cuda_stream)
+                   self._stream(stream))
         return out if lse is None else (out, lse)
 
     def device_error(self) -> int:

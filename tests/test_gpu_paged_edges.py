@@ -309,3 +309,43 @@ def test_scale_bytes_at_the_ends(byte, D):
         r = po.attention(q0[b, 0].double().cpu().numpy(), kk, vv, p.scale)
         tol, _ = bounds(*r, p.lens[b], D, "e4m3", torch.bfloat16)
         assert (np.abs(out[b, 0, other].double().cpu().numpy() - r[0]) <= tol).all()
+
+
+# ---------------------------------------------------------------------------
+# streams
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("by_argument", [True, False], ids=["argument", "current"])
+def test_a_cache_may_be_dropped_while_another_stream_uses_it(by_argument):
+    """The memory that a cache allocated is not handed out again before the calls on all of its streams are done."""
+    tk = binding()
+    lens = [9000, 5000]
+    cfg = tk.make_paged_config(1, 8, 2, 128, 232, 2, torch.bfloat16, tk.PAGE_PLAIN)
+    table = torch.full((2, 150), -1, dtype=torch.int32, device="cuda")
+    table[0, :141] = torch.arange(141, dtype=torch.int32, device="cuda")
+    table[1, :79] = torch.arange(141, 220, dtype=torch.int32, device="cuda")
+    seq = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    g = gen(3)
+    k = torch.randn(2, 9000, 1, 2, 128, generator=g, device="cuda").bfloat16()
+    v = torch.randn(2, 9000, 1, 2, 128, generator=g, device="cuda").bfloat16()
+    q = torch.randn(2, 1, 8, 128, generator=g, device="cuda").bfloat16()
+    ref = tk.PagedKVCache(cfg)
+    ref.write(k, v, table, rows=seq)
+    want = ref.decode_attn(q, table, seq)
+    cache = tk.PagedKVCache(cfg)
+    cache.write(k, v, table, rows=seq)
+    out = torch.zeros_like(q)
+    sizes = (cache.pages.numel(), cache.workspace.numel())
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(1_000_000_000)              # about 0.6 s: the call is still waiting when the cache goes
+    if by_argument:
+        cache.decode_attn(q, table, seq, out=out, stream=side)
+    else:
+        with torch.cuda.stream(side):
+            cache.decode_attn(q, table, seq, out=out)
+    cache.close()
+    del cache
+    taken = [torch.full((n,), 85, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(2)]
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and len(taken) == 4
