@@ -336,6 +336,7 @@ def test_a_cache_may_be_dropped_while_another_stream_uses_it(by_argument):
     out = torch.zeros_like(q)
     sizes = (cache.pages.numel(), cache.workspace.numel())
     side = torch.cuda.Stream()
+    torch.full((16,), 85, dtype=torch.uint8, device="cuda")        # (a kernel's first use may wait for the device)
     torch.cuda.synchronize()
     with torch.cuda.stream(side):
         torch.cuda._sleep(1_000_000_000)              # about 0.6 s: the call is still waiting when the cache goes
