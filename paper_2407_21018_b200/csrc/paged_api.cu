@@ -1,4 +1,5 @@
 // Host side of the paged key-value cache: validation, sizes, launches.
+#include <float.h>
 #include <math.h>
 #include <string.h>
 
@@ -43,7 +44,8 @@ thinK_status make_geometry(const thinK_paged_config* c, Geometry* o) {
   if (c->N_q % c->N_kv != 0) return THINK_ERR_INVALID_ARG;
   if (c->dtype != THINK_BF16 && c->dtype != THINK_F32) return THINK_ERR_UNSUPPORTED;
   if (c->page_format < THINK_PAGE_PLAIN || c->page_format > THINK_PAGE_INT4) return THINK_ERR_INVALID_ARG;
-  if (!(c->softmax_scale >= 0.0 && c->softmax_scale <= 3.0e38)) return THINK_ERR_INVALID_ARG;
+  constexpr double kLog2e = 1.4426950408889634074;
+  if (!(c->softmax_scale >= 0.0 && c->softmax_scale * kLog2e <= FLT_MAX)) return THINK_ERR_INVALID_ARG;      // fp32 below
   if (c->D != 64 && c->D != 128) return THINK_ERR_UNSUPPORTED;
   if (c->N_q / c->N_kv > kMaxPagedGroup) return THINK_ERR_UNSUPPORTED;
   if (c->dtype != THINK_BF16 && c->page_format != THINK_PAGE_PLAIN) return THINK_ERR_UNSUPPORTED;
@@ -64,7 +66,7 @@ thinK_status make_geometry(const thinK_paged_config* c, Geometry* o) {
   // the pool's size in bytes has to fit a signed 64-bit offset
   if ((double)c->L * c->num_pages * c->N_kv * r.g.block_bytes > 4.0e18) return THINK_ERR_UNSUPPORTED;
   const double scale = c->softmax_scale == 0.0 ? 1.0 / sqrt((double)c->D) : c->softmax_scale;
-  r.scale_log2 = (float)(scale * 1.4426950408889634074);
+  r.scale_log2 = (float)(scale * kLog2e);
   *o = r;
   return THINK_OK;
 }

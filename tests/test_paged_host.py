@@ -261,3 +261,13 @@ int main() {
 }
 """)
     assert out.split() == ["0", "1", "1"]
+
+
+def test_softmax_scale_in_base_2_stays_finite(tk):
+    """The kernels take the scale times log2(e) in fp32."""
+    top = 3.4028234e38 / 1.4426951
+    assert tk.paged_bytes(cfg_of(tk, softmax_scale=top * 0.999999)).block > 0
+    for scale in (top * 1.000001, 2.5e38, 3.0e38, 1e39):
+        with pytest.raises(tk.ThinKError) as e:
+            tk.paged_bytes(cfg_of(tk, softmax_scale=scale))
+        assert e.value.status == tk.ERR_INVALID_ARG
