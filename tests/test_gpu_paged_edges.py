@@ -230,25 +230,25 @@ def test_attention_tiny_queries_and_huge_keys(fmt, dtype, q_pow, k_pow, scale):
 def test_attention_tiny_values(fmt, dtype, power):
     """Values down to the smallest ordinary numbers: outputs are as exact as those of any size, up to half a step of
     bf16's smallest numbers where all of a sequence's values are tiny.  Sequences 1 and 2 hold one token of ordinary values that has next to no weight, in front
-    of all others and behind them; sequence 3 one that has weight."""
-    p = Paged(fmt, dtype, [1, 300, 300, 300, 5000], N_kv=2, G=4)
+    of all others and behind them; sequences 3 and 5 one that has weight."""
+    p = Paged(fmt, dtype, [1, 300, 300, 300, 5000, 5000], N_kv=2, G=4)
     k, v = p.rows(83)
     v = v.float() * 2.0 ** power
-    q = torch.randn(5, 1, 8, 128, generator=gen(89), device="cuda").to(dtype)
-    for b, t, like in ((1, 0, -4.0), (2, 299, -4.0), (3, 150, 0.5)):
+    q = torch.randn(6, 1, 8, 128, generator=gen(89), device="cuda").to(dtype)
+    for b, t, like in ((1, 0, -4.0), (2, 299, -4.0), (3, 150, 0.5), (5, 2600, 0.0)):
         v[b, t] = torch.randn(1, 2, 128, generator=gen(91), device="cuda")
         k[b, t, 0] = (like * q[b, 0].view(2, 4, 128).float().sum(1)).to(dtype)
     p.cache.write(k, v.to(dtype), p.table, rows=p.seq)
     out, lse = p.cache.decode_attn(q, p.table, p.seq, return_lse=True)
     # Half a step of the smallest outputs; fp32 sums of numbers below 2^-126 miss half of 2^-149 a token, weights (and so
-    # the sums) may be 2^-8 of what they are divided by.  Beside the ordinary token of sequences 1 to 3 (which flips the
+    # the sums) may be 2^-8 of what they are divided by.  Beside the ordinary token of those sequences (which flips the
     # reference of the weights) a token's weight * scale may be below 2^-117: a pair of bf16 then misses up to 2^-133 of
     # it, times its code (448 or 7 at most), divided by a sum of 2^-8 at least: 2^-125 code a token.  That shows in
     # channels in which the ordinary token's code is 0, and absv with it of the tiny ones' size.
     half, code = (2.0 ** -134 if dtype == torch.bfloat16 else 2.0 ** -150), {"plain": 0.0, "e4m3": 448.0, "int4": 7.0}[fmt]
 
     def floor(b):
-        return half + p.lens[b] * (2.0 ** -142 + (code * 2.0 ** -125 if b in (1, 2, 3) else 0.0))
+        return half + p.lens[b] * (2.0 ** -142 + (code * 2.0 ** -125 if b in (1, 2, 3, 5) else 0.0))
 
     check_own(p, q, out, lse, floor=floor)
 
@@ -350,3 +350,22 @@ def test_a_cache_may_be_dropped_while_another_stream_uses_it(by_argument):
     taken = [torch.full((n,), 85, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(2)]
     torch.cuda.synchronize()
     assert torch.equal(out, want) and len(taken) == 4
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS, ids=IDS)
+def test_one_layer_of_one_sequence(fmt, dtype):
+    """A call over a single layer of a single sequence out of a larger cache, against the oracle."""
+    p = Paged(fmt, dtype, [100, 260], L=3, N_kv=2, G=2, D=64, scale=0.31, max_batch=5)
+    k, v = p.rows(23)
+    p.cache.write(k, v, p.table, rows=p.seq)
+    q = torch.randn(2, 3, 4, 64, generator=gen(29), device="cuda").to(dtype)
+    for b in range(2):
+        for l in range(3):
+            out, lse = p.cache.decode_attn(q[b:b + 1, l:l + 1].contiguous(), p.table[b:], p.seq[b:], layer0=l, nlayers=1, return_lse=True)
+            for h in range(2):
+                hs = slice(2 * h, 2 * h + 2)
+                r = po.attention(q[b, l, hs].double().cpu().numpy(), *p.stored(b, l, h, p.lens[b]), 0.31)
+                tol, ltol = bounds(*r, p.lens[b], 64, fmt, dtype)
+                assert (np.abs(out[0, 0, hs].double().cpu().numpy() - r[0]) <= tol).all()
+                assert (np.abs(lse[0, 0, hs].double().cpu().numpy() - r[1]) <= ltol).all()
+    assert p.cache.device_error() == 0
