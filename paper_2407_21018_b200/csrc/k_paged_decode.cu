@@ -1,13 +1,14 @@
 // Attention of one new token per sequence over the paged cache: out = softmax(scale q K^T) V, and its log sum.
 //
-// Every byte of the pages is read once and used for at most 8 query heads, so the stream of pages is the bound (bf16 and
-// fp32 pages reach the copy rate, e4m3 0.8 of it; 4-bit pages are held by unpacking, 600 instructions per 4.6 KB) and the
-// kernel is built around it:
+// Every byte of the pages is read once and used for at most 8 query heads, so the stream of pages is the floor.  Pages of
+// bf16 and fp32 come near it (0.94 to 0.98 of the copy rate).  Quantised pages are held by latency: a scheduler has two
+// (e4m3) or three (4 bits) warps, each one chain of dependent steps (ldmatrix, unpack, mma, vote, ex2, transpose, mma), and
+// issues in 46 and 56 % of its cycles, with no unit above 44 % busy.  The kernel is built around the stream:
 //  * The tiles (64-token pages) of all (entry, layer, key head) units stand on one line, with some room for starting and
 //    ending a unit; it is cut evenly over the CTAs of one wave and inside a CTA over its warps, whatever the lengths:
 //    one long sequence uses the whole card and a ragged batch leaves no SM idle.  Lengths and page table are device
 //    memory; each CTA scans the lengths itself.  (Cut by tiles alone, 192 sequences of 1 to 2000 tokens took 95 us
-//    instead of 71: the CTAs with the short ones came last.)
+//    instead of 71 when that was tried: the CTAs with the short ones came last.)
 //  * A warp is the worker.  It owns a ring of stages in shared memory that it fills with cp.async, crossing page and
 //    unit borders, and waits for nobody until its range is done.
 //  * Rows are stored token-major.  16-byte chunks are XOR-swizzled on the way into shared memory so that ldmatrix
@@ -31,11 +32,12 @@
 //    partial states; the warps' states are joined by their CTA, the CTAs' states by the CTA that arrives last at
 //    the unit's ticket, always in token order, so results do not depend on timing.
 //
-// Measured (one call in a replayed graph; the share is of the copy rate, 6.54 TB/s):
-//   bf16  32 heads of 128, 16 sequences of 2048 to 4096      138 us   0.95
-//   bf16  32 / 8 heads, 131072 tokens, two layers            164 us   1.00
-//   e4m3  32 / 8 heads, 4 x 32768 tokens                      51 us   0.82
-//   int4  32 / 8 heads, 192 sequences of 1 to 2000            68 us   0.56
+// Measured (one call among others, buffers that change from call to call; the share is of the copy rate, 6.54 TB/s):
+//   bf16  32 heads of 128, 16 sequences of 2048 to 4096      139 us   0.94
+//   bf16  32 / 8 heads, 131072 tokens, two layers            168 us   0.98
+//   fp32  32 / 8 heads, 4 x 32768 tokens (replayed)          171 us   0.96
+//   e4m3  32 / 8 heads, 4 x 32768 tokens                      55 us   0.76
+//   int4  32 / 8 heads, 192 sequences of 1 to 2000            73 us   0.52
 //   int4  32 / 8 heads, 8192 tokens                           13 us   launch, three dependent loads and two joins
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -62,9 +64,9 @@ constexpr int kMaxG = kMaxPagedGroup;
 template <int D, int E, int FMT, int GP = 1>
 struct Shape {
   static constexpr bool F32 = E == 4;
-  // Eight warps keep 130 KB of copies in flight with 255 registers each; 4-bit pages, bound by instructions, do better
-  // with twelve (192 ragged sequences 70 us; 72 with eight; 76 with sixteen of 128 registers.  e4m3, 4 x 32768 tokens: 54
-  // with eight, 57 with twelve).
+  // Eight warps keep 130 KB of copies in flight with up to 255 registers each (e4m3 takes 245).  4-bit pages have twelve:
+  // against eight, 192 ragged sequences take the same 72.7 us, one of 8192 tokens 13.1 instead of 13.9, heads of 64
+  // 43.5 instead of 46.8, and 4 x 32768 tokens 46.4 instead of 45.3 (heads of 128 spill 72 bytes at 168 registers).
   static constexpr int WARPS = FMT == THINK_PAGE_INT4 ? 12 : 8;
   static constexpr int THREADS = WARPS * 32;
   static constexpr int RB = FMT == THINK_PAGE_PLAIN ? D * E : FMT == THINK_PAGE_E4M3 ? D : D / 2;   // bytes of a row
@@ -1224,8 +1226,7 @@ __global__ void __launch_bounds__((Shape<D, E, FMT, GP>::THREADS), 1) k_paged_de
   __syncthreads();
   // a warp takes 128 accumulators (four a lane, LPG lanes a query head) of every `slices`-th contributor: of all of them
   // if they are few.  (The order of the sums must not depend on which CTA joins, and so on what else it joins.)  Two
-  // units with few take half of the warps each (one after the other, the CTAs that end last cost 1 to 2 us more: 192
-  // ragged sequences of 4 bits 69.7 us against 67.9)
+  // units with few take half of the warps each (one after the other, the CTAs that end last cost 1 to 2 us more)
   constexpr int LPG = D / 4;
   constexpr int AHEAD = 6;                      // states whose accumulators come while the statistics are made
   const int chunks = (p.G * D + 127) / 128, n0 = sh.join[0], n1 = sh.join[1];

@@ -119,7 +119,8 @@ __device__ __forceinline__ uint4 decode_e4m3(const uint2& w, float f) {
 
 // FMT: thinK_page_format.  E: bytes of an element (2 bf16, 4 fp32).  A block takes kRowThreads / LANES consecutive
 // rows of one entry (head fastest, then layer, then token).  14 blocks an SM: the 4-bit kernels would take 40 registers
-// and 12 blocks (3 prompts written and read back 80.3 us, 79.2 so).
+// and 12 blocks (3 prompts written and read back, replayed: 80.3 us, 79.2 so, although the 4-bit writer then keeps 28
+// bytes a thread, 32 at D = 64, in local memory).
 template <int D, int E, int FMT, bool WRITE>
 __global__ void __launch_bounds__(kRowThreads, 14) k_paged_rows(PagedRowsParams p) {
   constexpr int P = kPieces;
