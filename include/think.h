@@ -410,8 +410,8 @@ thinK_status thinK_paged_write(thinK_paged* p, thinK_tensor5 k, thinK_tensor5 v,
 /* Reads rows back: the reverse of thinK_paged_write, same arguments; k and v are written.  Values are the stored
  * ones rounded to cfg.dtype (E4M3: exact; INT4: n * s to nearest even).  Rows at and behind rows[b] of the views, and
  * rows whose page is out of range, are left as they were.  No two rows of the views, k's and v's together, may share
- * memory, whether the call fills them or not (strides of 0 only where there is one index; interleaved views are fine):
- * THINK_ERR_INVALID_ARG. */
+ * memory, whether the call fills them or not: THINK_ERR_INVALID_ARG.  (Strides of 0 only where there is one index;
+ * interleaved views are fine; views so entangled that some ten thousand steps do not tell count as sharing.) */
 thinK_status thinK_paged_read(thinK_paged* p, thinK_tensor5 k, thinK_tensor5 v, thinK_page_table table,
                               const int32_t* pos, const int32_t* rows, int32_t max_rows, int32_t layer0,
                               int32_t nlayers, void* stream);

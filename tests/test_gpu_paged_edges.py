@@ -311,6 +311,24 @@ def test_scale_bytes_at_the_ends(byte, D):
         assert (np.abs(out[b, 0, other].double().cpu().numpy() - r[0]) <= tol).all()
 
 
+@pytest.mark.parametrize("fmt,dtype", KINDS, ids=IDS)
+@pytest.mark.parametrize("power", [-110, 0, 100])
+def test_log_sums_of_equal_logits(fmt, dtype, power):
+    """Logits of zero: the logarithm of the sum is that of the length, whatever weights are relative to (which goes by the
+    values).  The sums are exact; log2 of a number between 1 and 2 is off by 2^-23 at most, the sum with its exponent and
+    the product with ln 2 by half a step each, ln 2 itself by 2^-25: 2 u |lse| + u."""
+    lens = [1, 2, 3, 5, 7, 11, 100, 300, 5000, 12345]
+    p = Paged(fmt, dtype, lens, N_kv=1, G=4)
+    k, v = p.rows(83)
+    p.cache.write(k, (v.float() * 2.0 ** power).to(dtype), p.table, rows=p.seq)
+    q = torch.zeros(len(lens), 1, 4, 128, dtype=dtype, device="cuda")
+    out, lse = p.cache.decode_attn(q, p.table, p.seq, return_lse=True)
+    want = np.log(np.array(lens, dtype=np.float64)).reshape(-1, 1, 1)
+    u = 2.0 ** -23
+    err = np.abs(lse.double().cpu().numpy() - want)
+    assert (err <= 2 * u * want + u).all(), f"{(err / (2 * u * want + u)).max():.3g} of the bound"
+
+
 # ---------------------------------------------------------------------------
 # streams
 # ---------------------------------------------------------------------------
