@@ -682,9 +682,9 @@ __device__ __forceinline__ void put4(void* to, const float4& a, float f) {
 // m + log2(l) in natural logarithms; l's exponent meets m first, of which it takes back what weights' reference is off
 __device__ __forceinline__ float log_sum(float m, float l) {
   if (l == 0.f) return -INFINITY;
+  if (!(l <= FLT_MAX)) return l;                 // NaN
   const uint32_t u = __float_as_uint(l);
   const int e = (int)(u >> 23) - 127;            // (l is no subnormal: the largest weight is at least 2^-8)
-  if (e == 128) return l;                        // NaN
   return (m + (float)e + log2f(__uint_as_float((u & 0x007fffffu) | 0x3f800000u))) * 0.693147180559945309f;
 }
 
