@@ -430,7 +430,8 @@ thinK_status thinK_paged_read(thinK_paged* p, thinK_tensor5 k, thinK_tensor5 v, 
  *           same time - on two streams, or as two captured graphs - need a scratch buffer each.
  * A call names at most 2^29 table entries (4 * B * max_pages + 2 * B below 2^31), THINK_ERR_UNSUPPORTED otherwise.
  * Logits, softmax sums and outputs are accumulated in fp32.  On bf16 caches a weight (of quantised pages: times its
- * value's scale) meets the values as a pair of bf16, within 2^-16 of itself or, if it is smaller than 2^-117, 2^-133;
+ * value's scale) meets the values as a pair of bf16, within 2^-16 of itself or, if it is smaller than 2^-117, 2^-133
+ * (in any cache weights below 2^-117 of the largest may count as none);
  * queries are exact, on E4M3 pages relative to the row's largest channel, 2^-39 of which is the smallest step.  fp32
  * caches compute in fp32.  Results do not depend on timing: partial results are joined in token order. */
 thinK_status thinK_paged_decode_attn(thinK_paged* p, const void* q, void* out, float* lse, thinK_page_table table,
