@@ -323,7 +323,9 @@ def _prepare_plan(case, state, g):
     state.update(table=table, seq_lens=_ints(held), change=_ints(want), free_pages=free_pages, free_count=_ints([free]),
                  max_tokens=max(1, sum(max(w, 0) for w in want)))
     if own:
+        from paper_2407_21018_b200 import binding as tk
         state["cache"] = _cache(case, used + free, None, case["B"])
+        state["plan"] = tk.PagePlan(case["B"], state["max_tokens"])       # where every step's results go
     return state
 
 
@@ -543,7 +545,7 @@ def run(state):
         return {"plan": _plain_plan, "rope": _plain_rope, "write": _plain_write, "attn": _plain_attn}[op](state)
     if op == "plan":
         r = state["cache"].plan(state["change"], state["seq_lens"], state["table"], state["free_pages"], state["free_count"],
-                                state["max_tokens"])
+                                out=state["plan"])
         return {"pos": r.pos, "rows": r.rows, "start": r.start, "token_pos": r.token_pos, "slots": r.slots, "seq_lens": r.seq_lens,
                 "free_count": r.free_count, "table": state["table"], "free_pages": state["free_pages"]}
     if op == "rope":
