@@ -407,6 +407,50 @@ thinK_status thinK_paged_write(thinK_paged* p, thinK_tensor5 k, thinK_tensor5 v,
                                const int32_t* pos, const int32_t* rows, int32_t max_rows, int32_t layer0,
                                int32_t nlayers, void* stream);
 
+/* A step of a packed batch: the new tokens of all sequences stand one behind the other, sequence after sequence
+ * ("packed token" i).  From the tokens that each sequence holds and those it is to gain (change[b] > 0) or to lose (< 0,
+ * from its end; more than it holds: all) the call takes pages from the list of free ones, gives pages back to it, and says
+ * where each packed token goes.  Everything is device memory, so a captured graph plans every step.
+ *   free_pages: int32 [num_pages], the first free_count[0] of which are the free pages.  Pages given back are put
+ *           behind them, in the order of their sequences and tokens; pages are taken from the end, first sequence
+ *           first.  Entries behind the pages that are left hold whatever they held.
+ *   table:  the entries that a sequence gains are written; those that it loses stay as they are.
+ * A sequence gains what it asked for or nothing: nothing if it would pass 64 * max_pages tokens (it then counts as asking
+ * for nothing), if it needs pages and all that it and the sequences in front of it ask for are more than there are
+ * (those given back in this call among them), or if their tokens are more than max_tokens.
+ * Results:
+ *   pos:    int32 [B], tokens held before the new ones: the position of the first new token.
+ *   rows:   int32 [B], tokens gained.            start: int32 [B + 1], packed tokens in front of a sequence's first; the
+ *           last entry is their number.
+ *   token_pos, slots: int32 [max_tokens], position and slot (64 * page + place in the page) of every packed token; -1 behind
+ *           the last one.  16-byte aligned.
+ *   seq_len_out: int32 [B], pos + rows; may be seq_len itself.   free_left: int32 [1]; may be free_count itself.
+ * No other two of the arrays may overlap (THINK_ERR_INVALID_ARG).  A length above 64 * max_pages (cut), a change that does
+ * not fit the table, a count of free pages outside [0, num_pages] (cut) and a page outside the pool (it is moved as it is, its
+ * tokens get slot -1) set bit 16 of the error word.  Calls on one list of free pages must be ordered.
+ * THINK_ERR_UNSUPPORTED for more than 2^25 - 1 pages, or tables of more than 2^31 - 1 entries. */
+typedef struct {
+  int32_t* table;            /* [B][table_stride], the first max_pages entries of a row usable */
+  int64_t table_stride;
+  int32_t max_pages;
+  int32_t B;                 /* 1 <= B <= max_batch */
+  const int32_t* seq_len;    /* [B] tokens held */
+  const int32_t* change;     /* [B] tokens to gain or to lose */
+  int32_t* free_pages;       /* [num_pages] */
+  const int32_t* free_count; /* [1] */
+  int32_t *pos, *rows, *start, *token_pos, *slots, *seq_len_out, *free_left;
+  int32_t max_tokens;        /* room for packed tokens, at most 2^30 */
+} thinK_paged_step;
+
+thinK_status thinK_paged_plan(thinK_paged* p, const thinK_paged_step* step, void* stream);
+
+/* Writes packed rows to their slots, quantising them as thinK_paged_write does.  k, v: [tokens, nlayers, N_kv, D] views (the
+ * s axis of the view is the token, its b axis is not looked at).  Row i goes to slot slots[i] of thinK_paged_plan; a
+ * negative one means nowhere (the row is not stored), one behind the pool sets bit 16 of the error word.
+ * No two rows may go to the same slot. */
+thinK_status thinK_paged_write_slots(thinK_paged* p, thinK_tensor5 k, thinK_tensor5 v, const int32_t* slots, int32_t tokens,
+                                     int32_t layer0, int32_t nlayers, void* stream);
+
 /* Reads rows back: the reverse of thinK_paged_write, same arguments; k and v are written.  Values are the stored
  * ones rounded to cfg.dtype (E4M3: exact; INT4: n * s to nearest even).  Rows at and behind rows[b] of the views, and
  * rows whose page is out of range, are left as they were.  No two rows of the views, k's and v's together, may share
@@ -443,6 +487,63 @@ thinK_status thinK_paged_decode_attn(thinK_paged* p, const void* q, void* out, f
 thinK_status thinK_paged_device_error(thinK_paged* p, int32_t* out_code);
 
 thinK_status thinK_paged_destroy(thinK_paged* p);
+
+/* ---------------------------------------------------------------------------------------------------------
+ * Rotary positions, which queries and keys carry before they go to thinK_paged_write_slots, thinK_paged_write,
+ * thinK_append or thinK_prefill.  (The paper takes rotated keys as given.)  The first rot_dim channels of a row make
+ * rot_dim / 2 pairs; pair j of a token at position t becomes
+ *     (a, b) -> m (a cos(t f_j) - b sin(t f_j),  b cos(t f_j) + a sin(t f_j)),      f_j = theta^(-2 j / rot_dim)
+ * with frequencies scaled for contexts longer than the one that a model was trained on:
+ *   LINEAR  f_j / factor
+ *   NTK     theta * factor^(rot_dim / (rot_dim - 2)) in theta's place
+ *   YARN    f_j (1 - r_j) + r_j f_j / factor, r_j = (j - low) / (high - low) within [0, 1], where low and high are the pairs
+ *           that make `fast` (32) and `slow` (1) turns over the trained context, rot_dim ln(trained / (2 pi turns)) /
+ *           (2 ln theta), rounded down and up into [0, rot_dim - 1]; m = 0.1 ln(factor) + 1   (Peng et al., 2023)
+ *   BANDS   f_j (1 - r_j) + r_j f_j / factor, r_j = (fast - turns_j) / (fast - slow) within [0, 1] for the turns that the pair
+ *           makes over the trained context; slow 1, fast 4
+ * Angles are exact to 2^-27 turns at any position; products and sums are fp32, rounded once to the rows' type. */
+typedef enum {
+  THINK_ROPE_HALVES = 0, /* pair j: channels j and j + rot_dim / 2 */
+  THINK_ROPE_PAIRS = 1   /* pair j: channels 2 j and 2 j + 1       */
+} thinK_rope_layout;
+typedef enum {
+  THINK_ROPE_PLAIN = 0, THINK_ROPE_LINEAR = 1, THINK_ROPE_NTK = 2, THINK_ROPE_YARN = 3, THINK_ROPE_BANDS = 4
+} thinK_rope_scaling;
+
+typedef struct {
+  int32_t D;             /* channels of a row, at most 256; a row is a multiple of 16 bytes */
+  int32_t rot_dim;       /* channels that turn: even, 2 <= rot_dim <= D; the others stay as they are */
+  int32_t layout;        /* thinK_rope_layout */
+  int32_t scaling;       /* thinK_rope_scaling */
+  int32_t dtype;         /* thinK_dtype of the rows */
+  double theta;          /* base, at least 1 */
+  double factor;         /* context extension, at least 1 (not read for PLAIN) */
+  double trained;        /* tokens of the trained context (YARN, BANDS) */
+  double slow, fast;     /* turns; 0 means the defaults above (YARN, BANDS) */
+  double attention_factor; /* m; 0 means 1, for YARN 0.1 ln(factor) + 1 */
+} thinK_rope_config;
+
+typedef struct thinK_rope thinK_rope; /* opaque, host side, constant: any number of calls may use it at once */
+
+thinK_status thinK_rope_create(const thinK_rope_config* cfg, thinK_rope** out);
+
+/* Radians per token of a pair, -1 if there is no such pair. */
+double thinK_rope_frequency(const thinK_rope* r, int32_t pair);
+
+/* Turns queries and keys in one launch: q, q_out are [B, S, nlayers, N_q, D] views, k, k_out [B, S, nlayers, N_kv, D]; N_q or
+ * N_kv may be 0, the views concerned are then not looked at.
+ *   pos:    device int32.  pos_stride = 0: row s of entry b has position pos[b] + s; else pos[b * pos_stride + s].
+ *           A row whose position is negative (or passes 2^31 - 1) is left as it was in q_out and k_out.
+ *   rows:   device int32 [B], rows of an entry (the others are left as they were), or NULL for S.
+ *   transpose: 1 turns by -t f_j (with the same m): the gradient of a loss with respect to q and k from those with
+ *           respect to q_out and k_out.
+ * q_out may be q itself (same pointer and strides), k_out k; apart from that no row of q_out and k_out may share memory with
+ * another row of the two, nor with one of q or k (THINK_ERR_INVALID_ARG).  q and k may repeat rows (strides of 0). */
+thinK_status thinK_rope_apply(const thinK_rope* r, thinK_tensor5 q, thinK_tensor5 k, thinK_tensor5 q_out, thinK_tensor5 k_out,
+                              int32_t B, int32_t S, int32_t nlayers, int32_t N_q, int32_t N_kv, const int32_t* pos,
+                              int64_t pos_stride, const int32_t* rows, int32_t transpose, void* stream);
+
+thinK_status thinK_rope_destroy(thinK_rope* r);
 
 #ifdef __cplusplus
 }

@@ -33,6 +33,8 @@ PAGE_PLAIN, PAGE_E4M3, PAGE_INT4 = 0, 1, 2
 PART_K, PART_V, PART_K_SCALE, PART_V_SCALE = range(4)
 ERR_BIT_PAGE = 16
 PAGE_TOKENS = 64
+ROPE_HALVES, ROPE_PAIRS = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_NTK, ROPE_YARN, ROPE_BANDS = range(5)
 
 
 class Config(C.Structure):
@@ -64,6 +66,17 @@ class PagedSizes(C.Structure):
 
 class PageTable(C.Structure):
     _fields_ = [("table", C.c_void_p), ("table_stride", C.c_int64), ("max_pages", C.c_int32), ("B", C.c_int32)]
+
+
+class PagedStep(C.Structure):
+    _fields_ = ([("table", C.c_void_p), ("table_stride", C.c_int64), ("max_pages", C.c_int32), ("B", C.c_int32)] +
+                [(x, C.c_void_p) for x in ("seq_len", "change", "free_pages", "free_count", "pos", "rows", "start", "token_pos",
+                                           "slots", "seq_len_out", "free_left")] + [("max_tokens", C.c_int32)])
+
+
+class RopeConfig(C.Structure):
+    _fields_ = ([(x, C.c_int32) for x in ("D", "rot_dim", "layout", "scaling", "dtype")] +
+                [(x, C.c_double) for x in ("theta", "factor", "trained", "slow", "fast", "attention_factor")])
 
 
 EXPORTS = {
@@ -101,6 +114,13 @@ EXPORTS = {
                                    C.c_int32, C.c_int32, C.c_void_p]),
     "thinK_paged_decode_attn": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, PageTable, C.c_void_p,
                                           C.c_void_p, C.c_size_t, C.c_int32, C.c_int32, C.c_void_p]),
+    "thinK_paged_plan": (C.c_int, [C.c_void_p, C.POINTER(PagedStep), C.c_void_p]),
+    "thinK_paged_write_slots": (C.c_int, [C.c_void_p, Tensor5, Tensor5, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p]),
+    "thinK_rope_create": (C.c_int, [C.POINTER(RopeConfig), C.POINTER(C.c_void_p)]),
+    "thinK_rope_frequency": (C.c_double, [C.c_void_p, C.c_int32]),
+    "thinK_rope_apply": (C.c_int, [C.c_void_p] + [Tensor5] * 4 + [C.c_int32] * 5 + [C.c_void_p, C.c_int64, C.c_void_p, C.c_int32,
+                                                                                    C.c_void_p]),
+    "thinK_rope_destroy": (C.c_int, [C.c_void_p]),
     "thinK_paged_device_error": (C.c_int, [C.c_void_p, C.POINTER(C.c_int32)]),
     "thinK_paged_destroy": (C.c_int, [C.c_void_p]),
 }
@@ -353,8 +373,27 @@ _current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
+class PagePlan:
+    """Where PagedKVCache.plan puts its results (int32 tensors): pos, rows, seq_lens [B], start [B + 1], token_pos, slots
+    [max_tokens], free_count [1].  One plan may serve every step, of captured graphs too."""
+
+    def __init__(self, B: int, max_tokens: int, device="cuda"):
+        if not (0 < B <= 1 << 12 and 0 < max_tokens <= 1 << 30):
+            raise ThinKError(ERR_INVALID_ARG, "PagePlan")
+        room = -(-max_tokens // 4) * 4                 # token_pos and slots are 16-byte aligned
+        x = torch.zeros(2 * room + 4 * B + 2, dtype=torch.int32, device=device)
+        self.B, self.max_tokens = B, max_tokens
+        self.token_pos, self.slots = x[:max_tokens], x[room:room + max_tokens]
+        at = 2 * room
+        self.pos, self.rows, self.seq_lens = x[at:at + B], x[at + B:at + 2 * B], x[at + 2 * B:at + 3 * B]
+        self.start, self.free_count = x[at + 3 * B:at + 4 * B + 1], x[at + 4 * B + 1:]
+        self._index = x.get_device()
+        self._ptrs = [t.data_ptr() for t in (self.pos, self.rows, self.start, self.token_pos, self.slots, self.seq_lens,
+                                             self.free_count)]
+
+
 class PagedKVCache:
-    """Pool of 64-token pages with device-side page tables and lengths: write, read back, one-token attention.
+    """Pool of 64-token pages with device-side page tables and lengths: write, read back, attention of one or many tokens.
 
     Tables are int32 [B, max_pages] (rows may be strided), lengths, positions and row counts int32 [B], all on the
     cache's device.  `pages`: an existing pool (uint8, cfg's size) to work on; by default one is allocated.  Calls
@@ -469,6 +508,59 @@ class PagedKVCache:
         of k and v may share memory."""
         self._rows(lib.thinK_paged_read, "thinK_paged_read", k, v, table, pos, rows, layer0, nlayers, stream)
 
+    def write_slots(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, layer0=0, nlayers=None, stream=None):
+        """Row i of k and v ([tokens, nlayers, N_kv, D]) goes to slot slots[i] (int32, as PagePlan.slots), nowhere if that is
+        negative."""
+        where = "thinK_paged_write_slots"
+        n = self._L - layer0 if nlayers is None else nlayers
+        if (n | layer0) >> 31:
+            raise ThinKError(ERR_INVALID_ARG, where + ": layers")
+        shape, index, dtype = k.shape, self._index, self.torch_dtype
+        if (len(shape) != 4 or v.shape != shape or k.dtype is not dtype or v.dtype is not dtype
+                or k.get_device() != index or v.get_device() != index):
+            raise ThinKError(ERR_INVALID_ARG, where + ": rows")
+        tokens, layers, heads, width = shape
+        ks, kl, kn, kd = k.stride()
+        vs, vl, vn, vd = v.stride()
+        if layers != n or heads != self._N_kv or width != self._D or kd != 1 or vd != 1 or tokens >> 31:
+            raise ThinKError(ERR_INVALID_ARG, where + ": rows")
+        self._call(lib.thinK_paged_write_slots, where, Tensor5(k.data_ptr(), 0, ks, kl, kn), Tensor5(v.data_ptr(), 0, vs, vl, vn),
+                   self._vector(slots, tokens, where, ": slots"), tokens, layer0, n, self._stream(stream))
+
+    def plan(self, change: torch.Tensor, seq_lens: torch.Tensor, table: torch.Tensor, free_pages: torch.Tensor,
+             free_count: torch.Tensor, max_tokens: Optional[int] = None, in_place=False, out: Optional[PagePlan] = None,
+             stream=None) -> PagePlan:
+        """Pages, positions and slots of a step: sequence b of seq_lens[b] tokens gains change[b] of them, or loses -change[b]
+        (see thinK_paged_plan).  Writes the table and free_pages.  The new lengths and count are the plan's seq_lens and
+        free_count, with in_place those given.  `out`: a plan made before (else one for max_tokens is made)."""
+        where = "thinK_paged_plan"
+        index, B = self._index, change.shape[0] if change.dim() == 1 else 0
+        if out is None:
+            if max_tokens is None:
+                raise ThinKError(ERR_INVALID_ARG, where + ": max_tokens")
+            if stream is not None:
+                with torch.cuda.stream(stream):
+                    out = PagePlan(B, max_tokens, self.device)
+            else:
+                out = PagePlan(B, max_tokens, self.device)
+        elif out.B != B or out._index != index or max_tokens not in (None, out.max_tokens):
+            raise ThinKError(ERR_INVALID_ARG, where + ": out")
+        t = self._table(table, B, where)
+        lens, have = self._vector(seq_lens, B, where, ": seq_lens"), self._vector(free_count, 1, where, ": free_count")
+        pos, rows, start, token_pos, slots, new, left = out._ptrs
+        if in_place:
+            new, left = lens, have
+        if free_pages.numel() < self.cfg.num_pages:
+            raise ThinKError(ERR_INVALID_ARG, where + ": free_pages")
+        step = PagedStep(t.table, t.table_stride, t.max_pages, B, lens, self._vector(change, B, where, ": change"),
+                         self._vector(free_pages, 2, where, ": free_pages") if self.cfg.num_pages > 1 else
+                         self._vector(free_pages, 1, where, ": free_pages"),
+                         have, pos, rows, start, token_pos, slots, new, left, out.max_tokens)
+        self._call(lib.thinK_paged_plan, where, C.byref(step), self._stream(stream))
+        if in_place:
+            out.seq_lens, out.free_count = seq_lens, free_count
+        return out
+
     def decode_attn(self, q: torch.Tensor, table: torch.Tensor, seq_lens: torch.Tensor,
                     out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, return_lse: bool = False,
                     scratch: Optional[torch.Tensor] = None, layer0=0, nlayers=None, stream=None):
@@ -526,6 +618,107 @@ class PagedKVCache:
     def __del__(self):
         try:
             self.close()
+        except Exception:
+            pass
+
+
+# ---------------------------------------------------------------------------
+# Rotary positions
+# ---------------------------------------------------------------------------
+class Rope:
+    """Rotary positions of queries and keys (see thinK_rope_apply): layout ROPE_HALVES or ROPE_PAIRS, scaling ROPE_PLAIN,
+    ROPE_LINEAR, ROPE_NTK, ROPE_YARN or ROPE_BANDS."""
+
+    def __init__(self, D: int, dtype, rot_dim: Optional[int] = None, layout=ROPE_HALVES, theta=10000.0, scaling=ROPE_PLAIN, factor=1.0,
+                 trained=0.0, slow=0.0, fast=0.0, attention_factor=0.0):
+        self.handle = None
+        self.cfg = RopeConfig(D, D if rot_dim is None else rot_dim, layout, scaling,
+                              dtype if isinstance(dtype, int) else _dtype_code(dtype), theta, factor, trained, slow, fast,
+                              attention_factor)
+        h = C.c_void_p()
+        _check(lib.thinK_rope_create(C.byref(self.cfg), C.byref(h)), "thinK_rope_create")
+        self.handle, self._D = h, D
+        self.torch_dtype = torch.bfloat16 if self.cfg.dtype == BF16 else torch.float32
+
+    def frequency(self, pair: int) -> float:
+        """Radians per token of a pair, -1 if there is no such pair."""
+        return float(lib.thinK_rope_frequency(self.handle, pair))
+
+    def _view(self, x: torch.Tensor, like: torch.Tensor, what: str):
+        """[b, s, l, n, d] view of a padded or packed ([s, l, n, d]) tensor."""
+        if (x.dtype is not self.torch_dtype or x.dim() not in (4, 5) or x.dim() != like.dim() or x.shape[-1] != self._D
+                or x.stride(-1) != 1 or x.get_device() != like.get_device() or x.get_device() < 0 or x.shape[:-2] != like.shape[:-2]):
+            raise ThinKError(ERR_INVALID_ARG, "thinK_rope_apply: " + what)
+        s = x.stride()
+        return Tensor5(x.data_ptr(), *s[:4]) if len(s) == 5 else Tensor5(x.data_ptr(), 0, *s[:3])
+
+    def apply(self, q: Optional[torch.Tensor], k: Optional[torch.Tensor], pos: torch.Tensor, rows: Optional[torch.Tensor] = None,
+              q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, transpose=False, stream=None):
+        """Turns q [B, S, L, N_q, D] and k [B, S, L, N_kv, D] (or either one alone), in place unless q_out and k_out are given;
+        returns (q_out, k_out).  pos (int32): [B], of row 0 of each entry, or [B, S], of every row.  Packed tensors
+        [tokens, L, N, D] go with pos [tokens]."""
+        where = "thinK_rope_apply"
+        like = q if q is not None else k
+        if like is None:
+            raise ThinKError(ERR_INVALID_ARG, where)
+        index = like.get_device()
+        views, heads, outs = [], [], []
+        for x, y, what in ((q, q_out, "q"), (k, k_out, "k")):
+            if x is None:
+                if y is not None:
+                    raise ThinKError(ERR_INVALID_ARG, where + ": " + what)
+                views.append((Tensor5(), Tensor5()))
+                heads.append(0)
+                outs.append(None)
+                continue
+            a = self._view(x, like, what)
+            if y is None:
+                y, b = x, a
+            else:
+                b = self._view(y, like, what + "_out")
+                if y.shape != x.shape:
+                    raise ThinKError(ERR_INVALID_ARG, where + ": " + what + "_out")
+            views.append((a, b))
+            heads.append(x.shape[-2])
+            outs.append(y)
+        shape = like.shape
+        B, S, L = shape[:3] if len(shape) == 5 else (1,) + tuple(shape[:2])
+        if pos.dtype is not _INT32 or pos.get_device() != index or max(B, S, L, *heads) >> 31:
+            raise ThinKError(ERR_INVALID_ARG, where + ": pos")
+        if len(shape) == 4:
+            if pos.dim() != 1 or pos.shape[0] < S or (S > 1 and pos.stride(0) != 1):
+                raise ThinKError(ERR_INVALID_ARG, where + ": pos")
+            stride = max(S, 1)
+        elif pos.dim() == 2:
+            if pos.shape[0] < B or pos.shape[1] < S or (S > 1 and pos.stride(1) != 1) or (B > 1 and pos.stride(0) < max(S, 1)):
+                raise ThinKError(ERR_INVALID_ARG, where + ": pos")
+            stride = pos.stride(0) if B > 1 else max(S, 1)
+        else:
+            if pos.dim() != 1 or pos.shape[0] < B or (B > 1 and pos.stride(0) != 1):
+                raise ThinKError(ERR_INVALID_ARG, where + ": pos")
+            stride = 0
+        count = None
+        if rows is not None:
+            if rows.dtype is not _INT32 or rows.dim() != 1 or rows.shape[0] < B or rows.get_device() != index or (B > 1 and rows.stride(0) != 1):
+                raise ThinKError(ERR_INVALID_ARG, where + ": rows")
+            count = rows.data_ptr()
+        raw = _raw_stream(index) if stream is None else stream.cuda_stream
+        args = (self.handle, views[0][0], views[1][0], views[0][1], views[1][1], B, S, L, heads[0], heads[1], pos.data_ptr(), stride,
+                count, int(bool(transpose)), raw)
+        if _current_device() == index:
+            status = lib.thinK_rope_apply(*args)
+        else:
+            with torch.cuda.device(index):
+                status = lib.thinK_rope_apply(*args)
+        if status != THINK_OK:
+            raise ThinKError(status, where)
+        return outs[0], outs[1]
+
+    def __del__(self):
+        try:
+            if self.handle:
+                lib.thinK_rope_destroy(self.handle)
+                self.handle = None
         except Exception:
             pass
 

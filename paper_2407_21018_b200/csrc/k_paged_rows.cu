@@ -118,10 +118,10 @@ __device__ __forceinline__ uint4 decode_e4m3(const uint2& w, float f) {
 }
 
 // FMT: thinK_page_format.  E: bytes of an element (2 bf16, 4 fp32).  A block takes kRowThreads / LANES consecutive
-// rows of one entry (head fastest, then layer, then token).  14 blocks an SM: the 4-bit kernels would take 40 registers
+// rows of one entry (head fastest, then layer, then token).  SLOTS: a row's place is given, not looked up.  14 blocks an SM: the 4-bit kernels would take 40 registers
 // and 12 blocks (3 prompts written and read back, replayed: 80.3 us, 79.2 so, although the 4-bit writer then keeps 28
 // bytes a thread, 32 at D = 64, in local memory).
-template <int D, int E, int FMT, bool WRITE>
+template <int D, int E, int FMT, bool WRITE, bool SLOTS = false>
 __global__ void __launch_bounds__(kRowThreads, 14) k_paged_rows(PagedRowsParams p) {
   constexpr int P = kPieces;
   constexpr int LANES = D * E / 16 / P;         // lanes of a row
@@ -154,8 +154,18 @@ __global__ void __launch_bounds__(kRowThreads, 14) k_paged_rows(PagedRowsParams 
       v[i] = __ldcs(vx + i * LANES);
     }
   }
-  const int64_t tok = (int64_t)pos + s;
-  const int page = on ? page_of(p.table, p.g, b, tok, p.error) : -1;
+  int64_t tok = (int64_t)pos + s;
+  int page;
+  if constexpr (SLOTS) {
+    tok = on ? load_now(p.slots + s) : -1;      // a negative one: the row goes nowhere
+    page = (int)(tok >> 6);
+    if (page >= p.g.num_pages) {
+      atomicOr(p.error, kErrPage);
+      page = -1;
+    }
+  } else {
+    page = on ? page_of(p.table, p.g, b, tok, p.error) : -1;
+  }
   on = page >= 0;
   const int slot = (int)(tok & (kPageTokens - 1));
   uint8_t* const block = p.pages + page_block_offset(p.g, p.layer0 + (int)ll, on ? page : 0, (int)h);
@@ -258,6 +268,7 @@ cudaError_t launch_rows(const PagedRowsParams& p, bool write, cudaStream_t s) {
   constexpr int rpb = kRowThreads / (D * E / 16 / kPieces);
   const int64_t rows = (int64_t)p.max_rows * p.nlayers * p.g.N_kv;
   const dim3 grid((unsigned)((rows + rpb - 1) / rpb), (unsigned)p.table.B);
+  if (p.slots) return launch_dependent(k_paged_rows<D, E, FMT, true, true>, grid, kRowThreads, 0, s, p);
   return launch_dependent(write ? k_paged_rows<D, E, FMT, true> : k_paged_rows<D, E, FMT, false>, grid, kRowThreads, 0, s, p);
 }
 

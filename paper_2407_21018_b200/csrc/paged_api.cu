@@ -19,6 +19,8 @@ struct Range {
   ~Range() { nvtxRangePop(); }
 };
 
+constexpr int kMaxSlotPages = INT32_MAX / kPageTokens;   // slots are 32 bits wide
+
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   return a && b && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
@@ -117,9 +119,9 @@ bool layers_ok(const thinK_paged* p, int layer0, int nlayers) {
 }
 
 thinK_status rows_impl(thinK_paged* p, const thinK_tensor5& k, const thinK_tensor5& v, const thinK_page_table& t,
-                       const int32_t* pos, const int32_t* rows, int32_t max_rows, int32_t layer0, int32_t nlayers,
-                       void* stream, bool write) {
-  if (!p || !layers_ok(p, layer0, nlayers) || !table_ok(p->g, t)) return THINK_ERR_INVALID_ARG;
+                       const int32_t* pos, const int32_t* rows, const int32_t* slots, int32_t max_rows, int32_t layer0,
+                       int32_t nlayers, void* stream, bool write) {
+  if (!p || !layers_ok(p, layer0, nlayers) || (!slots && !table_ok(p->g, t))) return THINK_ERR_INVALID_ARG;
   if (max_rows < 0 || (int64_t)max_rows * p->g.g.N_kv > (1 << 30) || !aligned(pos, 4) || !aligned(rows, 4)) return THINK_ERR_INVALID_ARG;
   if (max_rows == 0) return THINK_OK;                  // views without rows may have no memory
   if (!view_ok(k, p->g.elem) || !view_ok(v, p->g.elem)) return THINK_ERR_INVALID_ARG;
@@ -129,7 +131,7 @@ thinK_status rows_impl(thinK_paged* p, const thinK_tensor5& k, const thinK_tenso
   r.g = p->g.g;
   r.pages = p->pages;
   r.table = PageTableView{t.table, t.table_stride, t.max_pages, t.B};
-  r.pos = pos; r.rows = rows; r.max_rows = max_rows;
+  r.pos = pos; r.rows = rows; r.slots = slots; r.max_rows = max_rows;
   r.by_heads = FastDiv((uint32_t)p->g.g.N_kv);
   r.error = (uint32_t*)p->ws;
   // row indices of an entry are 32 bits wide: as many layers per launch as fit
@@ -207,14 +209,64 @@ thinK_status thinK_paged_write(thinK_paged* p, thinK_tensor5 k, thinK_tensor5 v,
                                const int32_t* pos, const int32_t* rows, int32_t max_rows, int32_t layer0,
                                int32_t nlayers, void* stream) {
   Range nvtx_range("thinK_paged_write");
-  return rows_impl(p, k, v, table, pos, rows, max_rows, layer0, nlayers, stream, true);
+  return rows_impl(p, k, v, table, pos, rows, nullptr, max_rows, layer0, nlayers, stream, true);
 }
 
 thinK_status thinK_paged_read(thinK_paged* p, thinK_tensor5 k, thinK_tensor5 v, thinK_page_table table,
                               const int32_t* pos, const int32_t* rows, int32_t max_rows, int32_t layer0,
                               int32_t nlayers, void* stream) {
   Range nvtx_range("thinK_paged_read");
-  return rows_impl(p, k, v, table, pos, rows, max_rows, layer0, nlayers, stream, false);
+  return rows_impl(p, k, v, table, pos, rows, nullptr, max_rows, layer0, nlayers, stream, false);
+}
+
+thinK_status thinK_paged_write_slots(thinK_paged* p, thinK_tensor5 k, thinK_tensor5 v, const int32_t* slots, int32_t tokens,
+                                     int32_t layer0, int32_t nlayers, void* stream) {
+  Range nvtx_range("thinK_paged_write_slots");
+  if (!p || !layers_ok(p, layer0, nlayers) || tokens < 0) return THINK_ERR_INVALID_ARG;
+  if (tokens == 0) return THINK_OK;                    // arrays without tokens may have no memory
+  if (!slots || !aligned(slots, 4)) return THINK_ERR_INVALID_ARG;
+  if (p->g.g.num_pages > kMaxSlotPages) return THINK_ERR_UNSUPPORTED;
+  thinK_page_table one;
+  memset(&one, 0, sizeof(one));
+  one.B = 1;
+  k.stride_b = v.stride_b = 0;
+  return rows_impl(p, k, v, one, nullptr, nullptr, slots, tokens, layer0, nlayers, stream, true);
+}
+
+thinK_status thinK_paged_plan(thinK_paged* p, const thinK_paged_step* step, void* stream) {
+  Range nvtx_range("thinK_paged_plan");
+  if (!p || !step) return THINK_ERR_INVALID_ARG;
+  const thinK_paged_step& a = *step;
+  thinK_page_table t = {a.table, a.table_stride, a.max_pages, a.B};
+  if (!table_ok(p->g, t) || a.max_tokens < 1 || a.max_tokens > (1 << 30)) return THINK_ERR_INVALID_ARG;
+  const struct { const void* ptr; size_t bytes; bool out; } m[] = {
+      {a.seq_len, 4 * (size_t)a.B, false}, {a.change, 4 * (size_t)a.B, false}, {a.free_count, 4, false},
+      {a.table, 4 * ((size_t)a.table_stride * (a.B - 1) + a.max_pages), true},
+      {a.free_pages, 4 * (size_t)p->g.g.num_pages, true},
+      {a.pos, 4 * (size_t)a.B, true}, {a.rows, 4 * (size_t)a.B, true}, {a.start, 4 * ((size_t)a.B + 1), true},
+      {a.token_pos, 4 * (size_t)a.max_tokens, true}, {a.slots, 4 * (size_t)a.max_tokens, true},
+      {a.seq_len_out, 4 * (size_t)a.B, true}, {a.free_left, 4, true}};
+  constexpr int n = sizeof(m) / sizeof(m[0]);
+  for (int i = 0; i < n; ++i) {
+    if (!m[i].ptr || !aligned(m[i].ptr, m[i].ptr == a.token_pos || m[i].ptr == a.slots ? 16 : 4)) return THINK_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j) {
+      if (!m[i].out && !m[j].out) continue;
+      if ((m[i].ptr == a.seq_len_out && m[j].ptr == a.seq_len && j == 0) || (m[i].ptr == a.free_left && m[j].ptr == a.free_count && j == 2)) continue;
+      if (overlap(m[i].ptr, m[i].bytes, m[j].ptr, m[j].bytes)) return THINK_ERR_INVALID_ARG;
+    }
+  }
+  // pages of all sequences, and slots, are counted in 32 bits
+  if (p->g.g.num_pages > kMaxSlotPages || (int64_t)a.B * a.max_pages > INT32_MAX) return THINK_ERR_UNSUPPORTED;
+  PagedPlanParams d;
+  memset((void*)&d, 0, sizeof(d));
+  d.table = PageTableView{a.table, a.table_stride, a.max_pages, a.B};
+  d.table_out = a.table;
+  d.seq_len = a.seq_len; d.change = a.change; d.free_count = a.free_count; d.free_pages = a.free_pages;
+  d.pos = a.pos; d.rows = a.rows; d.start = a.start; d.token_pos = a.token_pos; d.slots = a.slots;
+  d.seq_len_out = a.seq_len_out; d.free_left = a.free_left;
+  d.max_tokens = a.max_tokens; d.num_pages = p->g.g.num_pages;
+  d.error = (uint32_t*)p->ws;
+  return launch_paged_plan(d, (cudaStream_t)stream) == cudaSuccess ? THINK_OK : THINK_ERR_CUDA;
 }
 
 thinK_status thinK_paged_decode_attn(thinK_paged* p, const void* q, void* out, float* lse, thinK_page_table table,

@@ -63,9 +63,20 @@ struct PagedRowsParams {     // rows <-> pages
   PageTableView table;
   const int32_t* pos;        // or null: 0
   const int32_t* rows;       // or null: max_rows
+  const int32_t* slots;      // or null; else row s goes to slots[s] = page * 64 + slot, and there is one entry
   int max_rows;
   int layer0, nlayers;
   FastDiv by_heads, by_layers;
+  uint32_t* error;
+};
+
+struct PagedPlanParams {
+  PageTableView table;
+  int32_t* table_out;        // the same table
+  const int32_t *seq_len, *change, *free_count;
+  int32_t* free_pages;
+  int32_t *pos, *rows, *start, *token_pos, *slots, *seq_len_out, *free_left;
+  int max_tokens, num_pages;
   uint32_t* error;
 };
 
@@ -87,6 +98,7 @@ struct PagedDecodeParams {
 };
 
 cudaError_t launch_paged_rows(const PagedRowsParams& p, int dtype, int format, bool write, cudaStream_t s);
+cudaError_t launch_paged_plan(const PagedPlanParams& p, cudaStream_t s);
 cudaError_t launch_paged_decode(const PagedDecodeParams& p, int dtype, int format, cudaStream_t s);
 cudaError_t paged_decode_setup(int dtype, int format, int D, int G);   // kernel attributes on the current device
 size_t paged_decode_record_bytes(int ctas);             // partial states of a launch of that many CTAs, any head dimension
