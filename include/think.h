@@ -482,6 +482,31 @@ thinK_status thinK_paged_decode_attn(thinK_paged* p, const void* q, void* out, f
                                      const int32_t* seq_len, void* scratch, size_t scratch_bytes, int32_t layer0,
                                      int32_t nlayers, void* stream);
 
+/* Attention of many new tokens per sequence, causal, over the pages (write the tokens' keys and values first): row s <
+ * rows[b] of entry b is the query of token pos[b] + s and sees tokens 0 .. pos[b] + s of its sequence.  Prompts from their
+ * beginning, later parts of a prompt, a few guessed tokens and single ones may stand side by side.
+ *   q, out: start = NULL: [B, max_rows, nlayers, N_q, D] views; else packed, [max_rows, nlayers, N_q, D] (their b axis is not
+ *           looked at), with row s of entry b at start[b] + s and max_rows the packed rows of all entries.  Rows that no
+ *           entry has are left as they were.  No row of out may share memory with another, nor with one of q.
+ *   lse:    fp32, dense [B, max_rows, nlayers, N_q] or [max_rows, nlayers, N_q], as in thinK_paged_decode_attn; or NULL.
+ *   pos, rows, start: device int32 [B]; NULL means 0 for all, max_rows for all (not with start), padded.
+ *   scratch: device buffer of scratch_bytes >= thinK_paged_prompt_scratch(p), 256-byte aligned; its contents do not matter.
+ *           Calls that may run at the same time need a scratch buffer each.
+ * A count of rows above max_rows, a start outside the packed rows, a negative position and tokens behind the table's end
+ * set bit 16 of the error word: rows are cut to what there is, tokens that have no page are left out.  A row without
+ * tokens gets out = 0 and lse = -infinity; one with tokens whose logits are all -infinity out = NaN and lse = -infinity.
+ * What a row does not see does not reach it, whatever it holds (NaN, infinities).
+ * Logits, softmax sums and outputs are accumulated in fp32 from the stored values, which enter exactly (4-bit ones, of 11
+ * bits, as the sum of two bf16).  On bf16 caches a weight meets the values rounded to bf16 (2^-8 of itself at most; weights
+ * below 2^-118 of the largest may count as none); the softmax sum takes it unrounded.  fp32 caches compute in fp32.  Results do not
+ * depend on timing. */
+thinK_status thinK_paged_prompt_attn(thinK_paged* p, thinK_tensor5 q, thinK_tensor5 out, float* lse, thinK_page_table table,
+                                     const int32_t* pos, const int32_t* rows, const int32_t* start, int32_t max_rows,
+                                     void* scratch, size_t scratch_bytes, int32_t layer0, int32_t nlayers, void* stream);
+
+/* Bytes of the scratch buffer of thinK_paged_prompt_attn (0 if p is NULL). */
+size_t thinK_paged_prompt_scratch(const thinK_paged* p);
+
 /* The handle's error word (bits 8 and 16 above), read with a synchronous copy; wait for the calls that it is to cover
  * first.  The word keeps its bits as long as the handle lives. */
 thinK_status thinK_paged_device_error(thinK_paged* p, int32_t* out_code);

@@ -116,6 +116,9 @@ EXPORTS = {
                                           C.c_void_p, C.c_size_t, C.c_int32, C.c_int32, C.c_void_p]),
     "thinK_paged_plan": (C.c_int, [C.c_void_p, C.POINTER(PagedStep), C.c_void_p]),
     "thinK_paged_write_slots": (C.c_int, [C.c_void_p, Tensor5, Tensor5, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p]),
+    "thinK_paged_prompt_scratch": (C.c_size_t, [C.c_void_p]),
+    "thinK_paged_prompt_attn": (C.c_int, [C.c_void_p, Tensor5, Tensor5, C.c_void_p, PageTable] + [C.c_void_p] * 3 +
+                                [C.c_int32, C.c_void_p, C.c_size_t, C.c_int32, C.c_int32, C.c_void_p]),
     "thinK_rope_create": (C.c_int, [C.POINTER(RopeConfig), C.POINTER(C.c_void_p)]),
     "thinK_rope_frequency": (C.c_double, [C.c_void_p, C.c_int32]),
     "thinK_rope_apply": (C.c_int, [C.c_void_p] + [Tensor5] * 4 + [C.c_int32] * 5 + [C.c_void_p, C.c_int64, C.c_void_p, C.c_int32,
@@ -432,6 +435,7 @@ class PagedKVCache:
         self._index = self.device.index
         self._L, self._N_q, self._N_kv, self._D, self._max_batch = c.L, c.N_q, c.N_kv, c.D, c.max_batch
         self._streams = set()
+        self._prompt_scratch = None
 
     def _stream(self, stream: Optional["torch.cuda.Stream"]) -> int:
         """The raw stream of a call.  The first call on a stream tells torch's allocator that it uses the cache's memory:
@@ -442,6 +446,8 @@ class PagedKVCache:
                 stream = torch.cuda.current_stream(self._index)
             self.workspace.record_stream(stream)
             self.pages.record_stream(stream)
+            if self._prompt_scratch is not None:
+                self._prompt_scratch.record_stream(stream)
             self._streams.add(raw)
         return raw
 
@@ -602,6 +608,70 @@ class PagedKVCache:
                    self._vector(seq_lens, B, where, ": seq_lens"), work, work_bytes, layer0, n,
                    self._stream(stream))
         return out if lse is None else (out, lse)
+
+    def new_prompt_scratch(self) -> torch.Tensor:
+        """A scratch buffer for prompt_attn calls that may run at the same time as others of this cache."""
+        return torch.empty(int(lib.thinK_paged_prompt_scratch(self.handle)), dtype=torch.uint8, device=self.device)
+
+    def prompt_attn(self, q: torch.Tensor, table: torch.Tensor, pos: Optional[torch.Tensor] = None,
+                    rows: Optional[torch.Tensor] = None, start: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                    lse: Optional[torch.Tensor] = None, return_lse: bool = False, scratch: Optional[torch.Tensor] = None,
+                    layer0=0, nlayers=None, stream=None):
+        """Causal attention of many new tokens per sequence: row s < rows[b] of q[b] ([B, S, nlayers, N_q, D]) is token
+        pos[b] + s and sees that token and those in front of it.  With `start` (PagePlan.start) q is packed,
+        [tokens, nlayers, N_q, D], and row s of sequence b stands at start[b] + s.  Returns out, or (out, lse) when lse (fp32,
+        contiguous, q's shape less D) is given or asked for; rows that no sequence has are left as they were, and hold
+        anything if out is not given.  `scratch`: see new_prompt_scratch; by default the cache's own, made by the first
+        call that needs it (outside of a graph capture: call once before)."""
+        where = "thinK_paged_prompt_attn"
+        n = self._L - layer0 if nlayers is None else nlayers
+        if (n | layer0) >> 31:
+            raise ThinKError(ERR_INVALID_ARG, where + ": layers")
+        shape, index = q.shape, self._index
+        packed = start is not None
+        if len(shape) != (4 if packed else 5) or q.dtype is not self.torch_dtype or q.get_device() != index:
+            raise ThinKError(ERR_INVALID_ARG, where + ": q")
+        max_rows, layers, heads, width = shape[-4:]
+        qs = q.stride()
+        if layers != n or heads != self._N_q or width != self._D or qs[-1] != 1 or max_rows >> 31:
+            raise ThinKError(ERR_INVALID_ARG, where + ": q")
+        if packed:
+            B = start.shape[0] if rows is None or start.dim() != 1 else rows.shape[0] if rows.dim() == 1 else 0
+        else:
+            B = shape[0]
+        if B < 1:
+            raise ThinKError(ERR_INVALID_ARG, where + ": sequences")
+        if stream is not None:                 # results in memory that this stream's earlier work has left
+            with torch.cuda.stream(stream):
+                out, lse, scratch = self._prompt_buffers(q, out, lse, return_lse, scratch)
+        else:
+            out, lse, scratch = self._prompt_buffers(q, out, lse, return_lse, scratch)
+        if out.shape != shape or out.dtype is not q.dtype or out.get_device() != index or out.stride(-1) != 1:
+            raise ThinKError(ERR_INVALID_ARG, where + ": out")
+        if lse is not None and (lse.shape != shape[:-1] or lse.dtype != torch.float32 or lse.get_device() != index
+                                or not lse.is_contiguous()):
+            raise ThinKError(ERR_INVALID_ARG, where + ": lse")
+        if scratch.dtype != torch.uint8 or scratch.get_device() != index or not scratch.is_contiguous():
+            raise ThinKError(ERR_INVALID_ARG, where + ": scratch")
+        os_ = out.stride()
+        b0, b1 = (0, 0) if packed else (qs[0], os_[0])
+        self._call(lib.thinK_paged_prompt_attn, where, Tensor5(q.data_ptr(), b0, *qs[-4:-1]), Tensor5(out.data_ptr(), b1, *os_[-4:-1]),
+                   None if lse is None else lse.data_ptr(), self._table(table, B, where), self._vector(pos, B, where, ": pos"),
+                   self._vector(rows, B, where, ": rows"), self._vector(start, B, where, ": start"), max_rows, scratch.data_ptr(),
+                   scratch.numel(), layer0, n, self._stream(stream))
+        return out if lse is None else (out, lse)
+
+    def _prompt_buffers(self, q, out, lse, return_lse, scratch):
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if lse is None and return_lse:
+            lse = torch.empty(q.shape[:-1], dtype=torch.float32, device=q.device)
+        if scratch is None:
+            scratch = self._prompt_scratch
+            if scratch is None:
+                scratch = self._prompt_scratch = self.new_prompt_scratch()
+                self._streams.clear()          # the next look at a stream tells the allocator about this buffer too
+        return out, lse, scratch
 
     def device_error(self) -> int:
         code = C.c_int32(0)

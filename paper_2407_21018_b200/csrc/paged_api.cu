@@ -8,6 +8,7 @@
 #include <nvtx3/nvToolsExt.h>
 
 #include "paged_internal.h"
+#include "paged_prompt_walk.cuh"
 #include "paged_views.h"
 
 using namespace think;
@@ -183,6 +184,7 @@ thinK_status thinK_paged_create(const thinK_paged_config* cfg, const thinK_paged
   int dev = 0, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
       paged_decode_setup(p->g.dtype, p->g.format, p->g.g.D, p->g.G) != cudaSuccess ||
+      paged_prompt_setup(p->g.dtype, p->g.format, p->g.g.D) != cudaSuccess ||
       cudaMemset(p->ws, 0, p->w.records) != cudaSuccess ||
       cudaMemset(p->ws + p->w.counters, 0, p->w.total - p->w.counters) != cudaSuccess || cudaStreamSynchronize(cudaStreamLegacy) != cudaSuccess) {
     delete p;
@@ -299,6 +301,66 @@ thinK_status thinK_paged_decode_attn(thinK_paged* p, const void* q, void* out, f
   d.records = ws + p->w.records;
   d.grid = p->grid;
   if (launch_paged_decode(d, p->g.dtype, p->g.format, (cudaStream_t)stream) != cudaSuccess) return THINK_ERR_CUDA;
+  return THINK_OK;
+}
+
+size_t thinK_paged_prompt_scratch(const thinK_paged* p) {
+  if (!p) return 0;
+  return align_up(sizeof(PromptDesc) * kSMs, 256) + align_up(sizeof(float) * 2 * kSMs * prompt_record_floats(paged_prompt_rows(p->g.dtype), p->g.g.D), 256);
+}
+
+thinK_status thinK_paged_prompt_attn(thinK_paged* p, thinK_tensor5 q, thinK_tensor5 out, float* lse, thinK_page_table table,
+                                     const int32_t* pos, const int32_t* rows, const int32_t* start, int32_t max_rows, void* scratch,
+                                     size_t scratch_bytes, int32_t layer0, int32_t nlayers, void* stream) {
+  Range nvtx_range("thinK_paged_prompt_attn");
+  if (!p || !layers_ok(p, layer0, nlayers) || !table_ok(p->g, table) || max_rows < 0) return THINK_ERR_INVALID_ARG;
+  if (!aligned(pos, 4) || !aligned(rows, 4) || !aligned(start, 4) || !aligned(lse, 4)) return THINK_ERR_INVALID_ARG;
+  if (start && !rows) return THINK_ERR_INVALID_ARG;
+  if (max_rows == 0) return THINK_OK;                  // views without rows may have no memory
+  if (!view_ok(q, p->g.elem) || !view_ok(out, p->g.elem) || !scratch || !aligned(scratch, 256)) return THINK_ERR_INVALID_ARG;
+  if (scratch_bytes < thinK_paged_prompt_scratch(p)) return THINK_ERR_CAPACITY;
+  const int B = start ? 1 : table.B, unit = 16 / p->g.elem;
+  if (start) q.stride_b = out.stride_b = 0;
+  auto view = [&](const thinK_tensor5& t) {
+    return RowView{{t.stride_b / unit, t.stride_s / unit, t.stride_l / unit, t.stride_n / unit}, {B, max_rows, nlayers, p->g.N_q}, p->g.g.D / unit};
+  };
+  const RowView a = view(q), b = view(out);
+  // a row is stored by threads of its own, and queries are read until the last output is written
+  if (!a.spread_ok() || !b.spread_ok() || b.shares_with_itself() ||
+      b.shares_with(a, (int64_t)((uintptr_t)q.ptr / 16) - (int64_t)((uintptr_t)out.ptr / 16))) return THINK_ERR_INVALID_ARG;
+  auto span = [&](const RowView& v) {
+    int64_t n = v.row;
+    for (int i = 0; i < 4; ++i) n += (v.extent[i] - 1) * v.stride[i];
+    return (size_t)n * 16;
+  };
+  const size_t lse_bytes = (size_t)B * max_rows * nlayers * p->g.N_q * 4;
+  if (overlap(lse, lse_bytes, q.ptr, span(a)) || overlap(lse, lse_bytes, out.ptr, span(b))) return THINK_ERR_INVALID_ARG;
+  PagedPromptParams d;
+  memset((void*)&d, 0, sizeof(d));
+  d.per = paged_prompt_rows(p->g.dtype) / p->g.G;
+  // positions fit 32 bits; so do the items of a sequence, and all places of the line 62
+  const int64_t tokens = (int64_t)table.max_pages * kPageTokens;
+  const PromptCut cut = paged_prompt_cut(p->g.dtype);
+  const double items = (double)max_rows / d.per + 1;
+  if (tokens + max_rows > INT32_MAX || (int64_t)nlayers * p->g.g.N_kv > INT32_MAX ||
+      items * ((double)tokens + max_rows + cut.extra) * table.B * nlayers * p->g.g.N_kv > 4.0e15) return THINK_ERR_UNSUPPORTED;
+  d.g = p->g.g;
+  d.pages = p->pages;
+  d.q = View5{q.ptr, q.stride_b, q.stride_s, q.stride_l, q.stride_n};
+  d.out = View5{out.ptr, out.stride_b, out.stride_s, out.stride_l, out.stride_n};
+  d.lse = lse;
+  d.table = PageTableView{table.table, table.table_stride, table.max_pages, table.B};
+  d.pos = pos; d.rows = rows; d.start = start; d.max_rows = max_rows;
+  d.N_q = p->g.N_q; d.G = p->g.G;
+  d.layer0 = layer0; d.nlayers = nlayers;
+  d.scale_log2 = p->g.scale_log2;
+  d.error = (uint32_t*)p->ws;
+  d.desc = (PromptDesc*)scratch;
+  d.records = (uint8_t*)scratch + align_up(sizeof(PromptDesc) * kSMs, 256);
+  d.grid = p->grid;
+  d.by_group = FastDiv((uint32_t)p->g.G);
+  d.by_heads = FastDiv((uint32_t)p->g.g.N_kv);
+  if (launch_paged_prompt(d, p->g.dtype, p->g.format, (cudaStream_t)stream) != cudaSuccess) return THINK_ERR_CUDA;
   return THINK_OK;
 }
 

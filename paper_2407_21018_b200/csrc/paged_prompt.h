@@ -1,0 +1,47 @@
+// How the attention of many new tokens over a paged cache is cut over CTAs.  Plain integer arithmetic, shared with the
+// host's tests.
+//
+// An item is one block of query rows of a sequence, layer and key head: `per` new tokens (fewer in a sequence's last item)
+// with all query heads of the key head.  Item i of a sequence at position pos sees its first pos + min((i + 1) per, rows)
+// tokens, tile by tile; it takes that many places on a line, and `extra` more for its start and end.  Sums over the
+// items of a sequence have a closed form, so a place is found without a list.  The line runs over layers and key heads,
+// in each over the sequences, and is cut evenly: a part owns the tiles that stand in it.
+#pragma once
+#include "paged_split.h"
+
+namespace think {
+
+struct PromptCut {
+  int tile, extra;            // tokens of a tile, places of an item besides its tokens
+  // tile j stands at slot(j) of its item: `extra` + tile neighbouring places always hold one
+  THINK_HD int64_t slot(int64_t j) const { return j == 0 ? 0 : extra + tile * j; }
+  THINK_HD int64_t first_tile(int64_t x) const {        // that stands at x or behind
+    if (x <= 0) return 0;
+    const int64_t j = div_wide(x - extra + tile - 1 > 0 ? x - extra + tile - 1 : 0, tile);
+    return j < 1 ? 1 : j;
+  }
+  // parts of a line so that every part holds a tile
+  THINK_HD int parts(int64_t total, int most) const {
+    const int64_t n = div_wide(total, extra + tile);
+    return n < 1 ? 1 : n < most ? (int)n : most;
+  }
+};
+
+struct PromptLine {           // a sequence's items
+  int64_t base;               // places of an item besides its tokens of this call: extra + max(pos, 0)
+  int rows, per;
+  THINK_HD int items() const { return (int)(((int64_t)rows + per - 1) / per); }
+  THINK_HD int64_t begin(int64_t i) const { return i * base + per * (i * (i + 1) / 2); }       // of item i < items()
+  THINK_HD int64_t cost(int64_t i) const { return base + ((i + 1) * per < rows ? (i + 1) * per : rows); }
+  THINK_HD int64_t total() const { return rows > 0 ? begin(items() - 1) + base + rows : 0; }
+  THINK_HD int find(int64_t place) const {              // the item that holds a place, 0 <= place < total()
+    int lo = 0, hi = items() - 1;
+    while (lo < hi) {
+      const int mid = lo + (hi - lo + 1) / 2;
+      if (begin(mid) <= place) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+  }
+};
+
+}  // namespace think

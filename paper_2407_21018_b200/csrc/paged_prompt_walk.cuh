@@ -1,0 +1,190 @@
+// Device side of paged_prompt.h: the sequences of a call and a CTA's way along its part of the line.
+#pragma once
+#include "paged_internal.h"
+#include "paged_prompt.h"
+
+namespace think {
+
+struct PromptDesc {           // an item that a CTA begins and others end: pieces of CTAs cta .. cta + pieces - 1
+  int lh, b, item, pieces;    // pieces 0: none
+};
+
+struct PagedPromptParams {
+  PageGeom g;
+  const uint8_t* pages;
+  View5 q, out;               // [b][s][layer - layer0][head][D] or [s][..] from start[b] on; element strides
+  float* lse;                 // dense, or null
+  PageTableView table;
+  const int32_t *pos, *rows, *start;      // or null: 0, max_rows, padded
+  int max_rows;
+  int N_q, G, per;            // per: new tokens of an item
+  int layer0, nlayers;
+  float scale_log2;
+  uint32_t* error;
+  PromptDesc* desc;           // one per CTA
+  uint8_t* records;           // two per CTA
+  int grid;
+  FastDiv by_group, by_heads;
+};
+
+// A piece's state, row by row: O [rows][D] (not divided by l), m, l [rows].  m: the largest logit in base 2 that the weights
+// are relative to.  l = 0 and m = -infinity: no token; l = 1 with that m: tokens, but all their logits are -infinity.
+__host__ __device__ inline size_t prompt_record_floats(int rows, int D) { return (size_t)rows * (D + 2); }
+
+cudaError_t launch_paged_prompt(const PagedPromptParams& p, int dtype, int format, cudaStream_t s);
+cudaError_t paged_prompt_setup(int dtype, int format, int D);       // kernel attributes on the current device
+int paged_prompt_rows(int dtype);                                   // query rows of an item
+PromptCut paged_prompt_cut(int dtype);
+
+#ifdef __CUDACC__
+struct PromptSeq {
+  int pos, rows, start;
+};
+// Sequence b of a call with its counts cut to what there is; `bad`: something was out of range.
+__device__ __forceinline__ PromptSeq prompt_seq(const PagedPromptParams& p, int b, bool& bad) {
+  PromptSeq s;
+  const int rows = p.rows ? load_now(p.rows + b) : p.max_rows;
+  const int pos = p.pos ? load_now(p.pos + b) : 0;
+  s.pos = min(pos, p.table.max_pages * kPageTokens);      // (pos + rows then fits 32 bits: checked on the host)
+  s.start = p.start ? load_now(p.start + b) : 0;
+  s.rows = max(0, min(rows, p.max_rows));
+  bad |= rows > p.max_rows;
+  if (p.start && s.rows > 0) {
+    const int room = s.start >= 0 && s.start < p.max_rows ? p.max_rows - s.start : 0;
+    bad |= s.rows > room;
+    s.rows = min(s.rows, room);
+  }
+  bad |= s.rows > 0 && (pos < 0 || (int64_t)pos + s.rows > (int64_t)p.table.max_pages * kPageTokens);
+  return s;
+}
+__device__ __forceinline__ PromptLine prompt_line(const PagedPromptParams& p, const PromptSeq& s, int extra) {
+  return PromptLine{(int64_t)extra + max(s.pos, 0), s.rows, p.per};
+}
+
+// Place of row s of a sequence in q or out (in elements, head and layer aside) and in lse (in rows).
+__device__ __forceinline__ int64_t prompt_row(const PagedPromptParams& p, const View5& v, int b, const PromptSeq& q, int s) {
+  return p.start ? (int64_t)(q.start + s) * v.ss : b * v.sb + (int64_t)s * v.ss;
+}
+__device__ __forceinline__ int64_t prompt_lse_row(const PagedPromptParams& p, int b, const PromptSeq& q, int s) {
+  return p.start ? q.start + s : (int64_t)b * p.max_rows + s;
+}
+
+struct PromptWalk {
+  int64_t at, begin, end;     // where the item begins; the CTA's part of the line
+  int64_t total;
+  int parts;
+  int lh, b, i;
+  PromptSeq s;
+};
+
+// All threads of a CTA; `scratch`: 40 64-bit words of shared memory, free again afterwards.  False: the CTA has no part.
+template <int THREADS>
+__device__ __forceinline__ bool prompt_walk_begin(const PagedPromptParams& p, const PromptCut& cut, PromptWalk& w, long long* scratch) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int B = p.table.B, per = (B + THREADS - 1) / THREADS, b0 = min(B, tid * per), b1 = min(B, b0 + per);
+  bool bad = false;
+  long long mine = 0;
+  for (int b = b0; b < b1; ++b) mine += prompt_line(p, prompt_seq(p, b, bad), cut.extra).total();
+  if (bad && blockIdx.x == 0) atomicOr(p.error, kErrPage);
+  long long upto = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long y = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += y;
+  }
+  if (lane == 31) scratch[warp] = upto;
+  __syncthreads();
+  long long sum = lane < THREADS / 32 ? scratch[lane] : 0;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long y = __shfl_up_sync(0xffffffffu, sum, o);
+    if (lane >= o) sum += y;
+  }
+  const long long W = __shfl_sync(0xffffffffu, sum, 31), before = __shfl_sync(0xffffffffu, sum, warp > 0 ? warp - 1 : 0);
+  upto += warp > 0 ? before : 0;
+  const int LH = p.nlayers * p.g.N_kv;
+  w.total = W * LH;
+  w.parts = cut.parts(w.total, p.grid);
+  if (W == 0 || (int)blockIdx.x >= w.parts) return false;
+  w.begin = split_begin(w.total, w.parts, blockIdx.x);
+  w.end = split_begin(w.total, w.parts, blockIdx.x + 1);
+  w.lh = (int)div_wide(w.begin, W);
+  const int64_t place = w.begin - w.lh * W;
+  if (mine > 0 && place < upto && place >= upto - mine) {      // one thread
+    long long x = upto - mine;
+    for (int b = b0; b < b1; ++b) {
+      const PromptLine line = prompt_line(p, prompt_seq(p, b, bad), cut.extra);
+      const long long n = line.total();
+      if (place < x + n) {
+        scratch[32] = b;
+        scratch[33] = line.find(place - x);
+        scratch[34] = w.lh * W + x + line.begin(scratch[33]);
+        break;
+      }
+      x += n;
+    }
+  }
+  __syncthreads();
+  w.b = (int)scratch[32];
+  w.i = (int)scratch[33];
+  w.at = scratch[34];
+  w.s = prompt_seq(p, w.b, bad);
+  __syncthreads();
+  return true;
+}
+
+// What of the current item belongs to this CTA.
+struct PromptPiece {
+  int s0, tokens;             // new tokens of the item: s0 .. s0 + tokens - 1
+  int n;                      // tokens that its last row sees
+  int tiles, t0, t1;          // tiles of the item, and those of this piece (none if t0 == t1)
+  int64_t cost;
+};
+__device__ __forceinline__ PromptPiece prompt_piece(const PagedPromptParams& p, const PromptCut& cut, const PromptWalk& w) {
+  PromptPiece x;
+  x.cost = prompt_line(p, w.s, cut.extra).cost(w.i);
+  x.s0 = w.i * p.per;
+  x.tokens = min(p.per, w.s.rows - x.s0);
+  x.n = (int)max((int64_t)0, min((int64_t)w.s.pos + x.s0 + x.tokens, (int64_t)p.table.max_pages * kPageTokens));
+  x.tiles = max(1, (x.n + cut.tile - 1) / cut.tile);
+  x.t0 = (int)min((int64_t)x.tiles, cut.first_tile(w.begin - w.at));
+  x.t1 = (int)min((int64_t)x.tiles, cut.first_tile(w.end - w.at));
+  return x;
+}
+// On to the next item; false at the end of the CTA's part.
+__device__ __forceinline__ bool prompt_walk_next(const PagedPromptParams& p, const PromptCut& cut, PromptWalk& w, int64_t cost) {
+  w.at += cost;
+  if (w.at >= w.end) return false;
+  bool bad = false;
+  if ((int64_t)(w.i + 1) * p.per < w.s.rows) {
+    ++w.i;
+    return true;
+  }
+  w.i = 0;
+  do {
+    if (++w.b == p.table.B) {
+      w.b = 0;
+      ++w.lh;
+    }
+    w.s = prompt_seq(p, w.b, bad);
+  } while (w.s.rows == 0);                  // some sequence has rows: the line is not at its end
+  return true;
+}
+
+// The description of an item that this CTA begins and does not end.
+__device__ __forceinline__ PromptDesc prompt_desc(const PromptCut& cut, const PromptWalk& w, const PromptPiece& x) {
+  const int last = split_owner(w.total, w.parts, w.at + cut.slot(x.tiles - 1));
+  return PromptDesc{w.lh, w.b, w.i, last - (int)blockIdx.x + 1};
+}
+
+// (m + log2 l) in natural logarithms; l's exponent meets m first, so that small sums keep their bits
+__device__ __forceinline__ float prompt_log_sum(float m, float l) {
+  if (!(l <= 3.402823466e38f)) return l;     // NaN
+  if (m == -INFINITY) return -INFINITY;
+  const uint32_t u = __float_as_uint(l);
+  const int e = (int)(u >> 23) - 127;
+  return (m + (float)e + log2f(__uint_as_float((u & 0x007fffffu) | 0x3f800000u))) * 0.693147180559945309f;
+}
+#endif
+
+}  // namespace think
