@@ -287,43 +287,33 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_paged_prompt_join(const Pag
 template <int D>
 constexpr size_t simple_smem() { return sizeof(float) * (size_t)((kRows + 2 * kTile) * (D + 4) + kRows * (kTile + 4)); }
 
-template <int D, int E, int FMT>
+template <int D>
 cudaError_t launch_simple(const PagedPromptParams& p, cudaStream_t s) {
-  cudaError_t e = launch_dependent(k_paged_prompt_simple<D, E, FMT>, dim3(p.grid), kThreads, simple_smem<D>(), s, p);
-  if (e == cudaSuccess) e = launch_dependent(k_paged_prompt_join<D, E, kRows>, dim3(p.grid, kRows / kJoinWarps), 32 * kJoinWarps, 0, s, p);
-  return e;
+  const cudaError_t e = launch_dependent(k_paged_prompt_simple<D, 4, THINK_PAGE_PLAIN>, dim3(p.grid), kThreads, simple_smem<D>(), s, p);
+  return e != cudaSuccess ? e : launch_dependent(k_paged_prompt_join<D, 4, kRows>, dim3(p.grid, kRows / kJoinWarps), 32 * kJoinWarps, 0, s, p);
 }
-
-template <int D, int E, int FMT>
+template <int D>
+cudaError_t launch_tc(const PagedPromptParams& p, int format, const void* map, cudaStream_t s) {
+  const cudaError_t e = launch_paged_prompt_tc(p, format, map, s);
+  return e != cudaSuccess ? e : launch_dependent(k_paged_prompt_join<D, 2, 256>, dim3(p.grid, 256 / kJoinWarps), 32 * kJoinWarps, 0, s, p);
+}
+template <int D>
 cudaError_t setup_simple() {
-  return cudaFuncSetAttribute(k_paged_prompt_simple<D, E, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)simple_smem<D>());
-}
-template <int D>
-cudaError_t setup_d(int dtype, int format) {
-  if (dtype == THINK_F32) return setup_simple<D, 4, THINK_PAGE_PLAIN>();
-  return format == THINK_PAGE_PLAIN ? setup_simple<D, 2, THINK_PAGE_PLAIN>()
-                                    : format == THINK_PAGE_E4M3 ? setup_simple<D, 2, THINK_PAGE_E4M3>() : setup_simple<D, 2, THINK_PAGE_INT4>();
-}
-
-template <int D>
-cudaError_t launch_d(const PagedPromptParams& p, int dtype, int format, cudaStream_t s) {
-  if (dtype == THINK_F32) return launch_simple<D, 4, THINK_PAGE_PLAIN>(p, s);
-  switch (format) {
-    case THINK_PAGE_PLAIN: return launch_simple<D, 2, THINK_PAGE_PLAIN>(p, s);
-    case THINK_PAGE_E4M3: return launch_simple<D, 2, THINK_PAGE_E4M3>(p, s);
-    case THINK_PAGE_INT4: return launch_simple<D, 2, THINK_PAGE_INT4>(p, s);
-  }
-  return cudaErrorInvalidValue;
+  return cudaFuncSetAttribute(k_paged_prompt_simple<D, 4, THINK_PAGE_PLAIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)simple_smem<D>());
 }
 
 }  // namespace
 
-cudaError_t paged_prompt_setup(int dtype, int format, int D) { return D == 128 ? setup_d<128>(dtype, format) : setup_d<64>(dtype, format); }
-int paged_prompt_rows(int dtype) { return kRows; }
-PromptCut paged_prompt_cut(int dtype) { return PromptCut{kTile, kExtra}; }
+cudaError_t paged_prompt_setup(int dtype, int format, int D) {
+  if (dtype == THINK_BF16) return paged_prompt_tc_setup(format, D);
+  return D == 128 ? setup_simple<128>() : setup_simple<64>();
+}
+int paged_prompt_rows(int dtype) { return dtype == THINK_BF16 ? paged_prompt_tc_rows() : kRows; }
+PromptCut paged_prompt_cut(int dtype, int format) { return dtype == THINK_BF16 ? paged_prompt_tc_cut(format) : PromptCut{kTile, kExtra}; }
 
-cudaError_t launch_paged_prompt(const PagedPromptParams& p, int dtype, int format, cudaStream_t s) {
-  return p.g.D == 128 ? launch_d<128>(p, dtype, format, s) : launch_d<64>(p, dtype, format, s);
+cudaError_t launch_paged_prompt(const PagedPromptParams& p, int dtype, int format, const void* map, cudaStream_t s) {
+  if (dtype == THINK_BF16) return p.g.D == 128 ? launch_tc<128>(p, format, map, s) : launch_tc<64>(p, format, map, s);
+  return p.g.D == 128 ? launch_simple<128>(p, s) : launch_simple<64>(p, s);
 }
 
 }  // namespace think

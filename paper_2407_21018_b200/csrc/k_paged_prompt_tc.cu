@@ -1,0 +1,798 @@
+// Attention of many new tokens of each sequence over its pages (causal) on the 5th-generation tensor cores, bf16 queries.
+//
+// An item is 256 rows of queries that share a key head (256 / G new tokens times the G heads), as two halves of 128 rows
+// that take turns on the tensor cores: while one half's logits pass through the softmax, the other's products run.
+//   S = Q K^T       tcgen05.mma into tensor memory, a tile of KT tokens; thread t of a half's four warps owns row t
+//   P = 2^(x - m)   read from tensor memory, written back over S as bf16: the A operand of
+//   O += P V        tcgen05.mma, V as stored ([token][channel]) is the MN-major B operand
+// Roles: warps 0-3 and 4-7 the softmax of a half each, warps 8-11 bring keys and values into a ring of shared-memory slots
+// (bf16 pages by TMA, others unpacked in registers), one thread of warp 12 issues all products.  m only moves when a row's
+// logits pass it by 2^8 (O is then rescaled in tensor memory), so the softmax seldom waits for the products.
+// 4-bit values n * s have 11 bits: they enter as the sum of two bf16, which is exact, at twice the products; their keys
+// and values need twice the room, so tiles are 64 tokens and Q is held in tensor memory too.
+// Every wait is bounded (about a second): on a time-out the CTA raises the error word, frees its tensor memory and leaves.
+#include <math.h>
+#include <string.h>
+
+#include <cuda.h>
+
+#include "paged_prompt_walk.cuh"
+
+namespace think {
+namespace {
+
+constexpr int kHalf = 128, kItemRows = 2 * kHalf, kThreads = 512;
+constexpr int kExtra = 256;             // places of an item besides its tokens: what starting and ending one costs
+
+// ---- PTX
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+// shared-memory matrix descriptor, 128-byte swizzle
+__device__ __forceinline__ uint64_t umma_desc(uint32_t saddr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
+  return (uint64_t)((saddr >> 4) & 0x3fffu) | ((uint64_t)((lbo_bytes >> 4) & 0x3fffu) << 16) |
+         ((uint64_t)((sbo_bytes >> 4) & 0x3fffu) << 32) | (1ull << 46) | (2ull << 61);
+}
+// instruction descriptor: fp32 accumulate, bf16 x bf16, M = 128; B K-major or MN-major
+__host__ __device__ constexpr uint32_t idesc(int n, bool b_mn) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24);
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t"
+      ".reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t"
+      "}\n"
+      :: "r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate), "r"(0u) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t"
+      ".reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t"
+      "}\n"
+      :: "r"(d), "r"(a), "l"(b), "r"(id), "r"(accumulate), "r"(0u) : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory");
+}
+__device__ __forceinline__ void bar_arrive_tx(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t"
+      ".reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t"
+      "}\n"
+      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+// bounded wait (about a second): false on time-out
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
+  if (bar_try(bar, parity)) return true;
+  const long long t0 = clock64();
+  while (!bar_try(bar, parity))
+    if (clock64() - t0 > 2000000000LL) return false;
+  return true;
+}
+// the same for a whole warp, whose lanes agree on the answer
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, bar_wait(bar, parity)); }
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+               :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};\n"
+      :: "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+         "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+         "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+         "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]),
+         "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *(const uint32_t*)&v;
+}
+
+// ---- what depends on the format and the head dimension
+template <int D, int FMT>
+struct Shape {
+  static constexpr bool kInt4 = FMT == THINK_PAGE_INT4, kPlain = FMT == THINK_PAGE_PLAIN;
+  static constexpr int KT = kInt4 ? 64 : 128;                 // tokens of a tile
+  static constexpr int PARTS = kInt4 ? 2 : 1;                 // bf16 operands that a key or value is the sum of
+  static constexpr bool kQTmem = kInt4;
+  static constexpr int kSlot = KT * D * 2;
+  static constexpr int kQBytes = kQTmem ? 0 : 2 * kHalf * D * 2;
+  static constexpr int kSlots = (196608 - kQBytes) / kSlot < 12 ? (196608 - kQBytes) / kSlot / (2 * PARTS) * 2 * PARTS : 12;
+  static constexpr int kSmem = kQBytes + kSlots * kSlot + 1024;
+  // tensor memory: S of each half, Q, O of each half
+  static constexpr int kColS = KT, kColQ = 2 * KT, kColO = 256;
+  static constexpr int RB = kPlain ? D * 2 : kInt4 ? D / 2 : D;       // bytes of a stored row
+  static constexpr int SB = kPlain ? 0 : kInt4 ? D / 16 : 1;          // bytes of its scales
+  static __host__ __device__ constexpr PromptCut cut() { return PromptCut{KT, kExtra}; }
+};
+
+struct Shared {
+  uint64_t full[12], empty[12], s_full[2], p_full[2], o_full[2], q_full[2], raw;
+  long long scratch[40];
+  uint32_t tmem;
+  // The loads are at most kSlots / (2 PARTS) + 1 <= 6 tiles, so as many items, ahead of the softmax.
+  uint32_t pages[8];           // of the tiles under way: bit i: the tile's i-th page is there
+  uint32_t bad[16];            // of the items under way: a value that some rows do not see is a NaN or an infinity
+  uint32_t failed;
+};
+
+// byte offset of 16-byte chunk ck of row r in an operand of `rows` rows: 64-channel blocks of 128-byte rows, swizzled
+__device__ __forceinline__ uint32_t swz(int rows, int r, int ck) {
+  return (uint32_t)((ck >> 3) * rows * 128 + r * 128 + (((ck & 7) ^ (r & 7)) << 4));
+}
+__device__ __forceinline__ void st_shared(uint32_t at, const uint4& w) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(at), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
+}
+__device__ __forceinline__ uint4 ld_shared(uint32_t at) {
+  uint4 w;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(at) : "memory");
+  return w;
+}
+// Sets the NaN and infinite ones of 8 bf16 to 0; whether there were any.
+__device__ __forceinline__ bool drop_non_finite(uint4& w) {
+  bool any = false;
+  uint32_t* const u = &w.x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bool lo = (u[i] & 0x7f80u) == 0x7f80u, hi = (u[i] & 0x7f800000u) == 0x7f800000u;
+    any |= lo | hi;
+    u[i] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+  }
+  return any;
+}
+
+// 4 e4m3 codes times a power of two as bf16 (exact)
+__device__ __forceinline__ uint2 e4m3_to_bf16(uint32_t w, float s) {
+  const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xffffu), __NV_E4M3);
+  const __half2_raw b = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3);
+  const float2 x = __half22float2(*(const __half2*)&a), y = __half22float2(*(const __half2*)&b);
+  return make_uint2(pack_bf16(x.x * s, x.y * s), pack_bf16(y.x * s, y.y * s));
+}
+// 8 4-bit codes times their scale as the sum of two bf16 (exact: 3 bits times 8; the first part is cut off)
+__device__ __forceinline__ void int4_to_bf16(uint32_t w, float s, uint4& hi, uint4& lo) {
+  const uint32_t even = w & 0x0f0f0f0fu, odd = (w >> 4) & 0x0f0f0f0fu;
+  const f32x2 s2 = two(s, s), off = two(-8388616.f, -8388616.f);
+  uint32_t h[4], l[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float a = __uint_as_float(__byte_perm(even, 0x4b000000u, 0x7440 | i)), b = __uint_as_float(__byte_perm(odd, 0x4b000000u, 0x7440 | i));
+    split(mul2(add2(two(a, b), off), s2), a, b);
+    h[i] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+    l[i] = pack_bf16(a - __uint_as_float(h[i] << 16), b - __uint_as_float(h[i] & 0xffff0000u));
+  }
+  hi = make_uint4(h[0], h[1], h[2], h[3]);
+  lo = make_uint4(l[0], l[1], l[2], l[3]);
+}
+
+// A value of the pool as fp32, for the few that are looked at one by one.
+template <int D, int FMT>
+__device__ float value_at(const uint8_t* block, int slot, int c) {
+  using T = Shape<D, FMT>;
+  const uint8_t* const row = block + (kPageTokens + slot) * T::RB;
+  const uint8_t* const sc = block + 2 * kPageTokens * T::RB + (kPageTokens + slot) * T::SB;
+  if constexpr (T::kPlain) return __uint_as_float((uint32_t)((const uint16_t*)row)[c] << 16);
+  else if constexpr (FMT == THINK_PAGE_E4M3) {
+    const __half_raw h = __nv_cvt_fp8_to_halfraw(row[c], __NV_E4M3);
+    return __half2float(*(const __half*)&h) * e8m0(*sc);
+  } else {
+    return ((row[c / 2] >> (4 * (c & 1)) & 15) - 8) * __uint_as_float((uint32_t)((const uint16_t*)sc)[c / kGroupChannels] << 16);
+  }
+}
+
+// Tiles of a half of a piece: those its rows see.
+struct Halves {
+  int rows[2];                // query rows
+  int see[2];                 // tokens that the half's first row sees
+  int t1[2];                  // end of its tiles
+};
+template <typename T>
+__device__ __forceinline__ Halves halves_of(const PagedPromptParams& p, const PromptWalk& w, const PromptPiece& x) {
+  Halves h;
+  const int rows = x.tokens * p.G;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    h.rows[i] = max(0, min(kHalf, rows - i * kHalf));
+    const int first = w.s.pos + x.s0 + (int)p.by_group.div(i * kHalf);
+    const int last = w.s.pos + x.s0 + (int)p.by_group.div(i * kHalf + max(h.rows[i], 1) - 1);
+    h.see[i] = first + 1;
+    const int n = max(0, min(x.n, last + 1));
+    h.t1[i] = h.rows[i] == 0 ? x.t0 : max(x.t0, min(x.t1, max(1, (n + T::KT - 1) / T::KT)));
+  }
+  return h;
+}
+
+struct Ring {                 // position in the ring of slots
+  int slot;
+  uint32_t phase;
+  template <typename T>
+  __device__ __forceinline__ void next() {
+    if (++slot == T::kSlots) {
+      slot = 0;
+      phase ^= 1;
+    }
+  }
+};
+
+// ---- warps 8-11: keys and values
+template <int D, int FMT>
+__device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUtensorMap* map, PromptWalk w, Shared& sh, uint32_t ring0) {
+  using T = Shape<D, FMT>;
+  constexpr PromptCut cut = T::cut();
+  const int tid = threadIdx.x & 127, lane = threadIdx.x & 31;
+  Ring r{0, 0};
+  uint32_t raw_phase = 0;
+  int tile_no = 0, item_no = 0;
+  PromptPiece x;
+  do {
+    x = prompt_piece(p, cut, w);
+    if (x.t0 == x.t1) continue;
+    const int ll = p.by_heads.div(w.lh), h = w.lh - ll * p.g.N_kv;
+    const int see = w.s.pos + x.s0 + 1;            // tokens that every row sees
+    for (int t = x.t0; t < x.t1; ++t, ++tile_no) {
+      const int tok0 = t * T::KT;
+      int page[T::KT / 64];
+      uint32_t there = 0;
+#pragma unroll
+      for (int i = 0; i < T::KT / 64; ++i) {
+        page[i] = tok0 + 64 * i < x.n ? page_of(p.table, p.g, w.b, tok0 + 64 * i, p.error) : -1;
+        there |= (page[i] >= 0 ? 1u : 0u) << i;
+      }
+#pragma unroll
+      for (int part = 0; part < 2; ++part) {
+        const bool edge = part == 1 && (tok0 + T::KT > see || there != (1u << (T::KT / 64)) - 1);     // some values must not be met
+        if constexpr (T::kPlain) {
+          const uint32_t slot = ring0 + r.slot * T::kSlot, full = smem_u32(&sh.full[r.slot]), raw = smem_u32(&sh.raw);
+          if (!warp_wait(smem_u32(&sh.empty[r.slot]), r.phase ^ 1)) return false;
+          if (tid == 0) {
+            if (part == 0) {
+              sh.pages[tile_no & 7] = there;
+              if (t == x.t0) sh.bad[(item_no + 8) & 15] = 0;
+            }
+            const uint32_t bar = edge ? raw : full;
+            bar_arrive_tx(bar, __popc(there) * 64 * D * 2);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+              if (page[i] >= 0) {
+                const int row = (int)((((int64_t)(p.layer0 + ll) * p.g.num_pages + page[i]) * p.g.N_kv + h) * 128) + part * 64;
+#pragma unroll
+                for (int c = 0; c < D / 64; ++c) tma_load(slot + c * T::KT * 128 + i * 8192, map, c * 64, row, bar);
+              }
+          }
+          if (edge) {
+            __syncwarp();
+            if (!warp_wait(raw, raw_phase)) return false;
+            raw_phase ^= 1;
+            // thread = token: what is behind the last one or on no page becomes 0, what only some rows see finite
+            const int tok = tok0 + tid;
+            const bool off = tok >= x.n || !(there >> (tid >> 6) & 1);
+            if (off || tok >= see) {
+              bool any = false;
+#pragma unroll
+              for (int ck = 0; ck < D / 8; ++ck) {
+                uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                if (!off) {
+                  v = ld_shared(slot + swz(T::KT, tid, ck));
+                  any |= drop_non_finite(v);
+                }
+                st_shared(slot + swz(T::KT, tid, ck), v);
+              }
+              if (any) sh.bad[item_no & 15] = 1;
+            }
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) bar_arrive(full);
+          } else if (tid != 0 && lane == 0) {
+            bar_arrive(full);
+          }
+          r.template next<T>();
+        } else {
+          // a unit is 16 stored bytes: 16 channels of e4m3, 32 of 4 bits
+          constexpr int CH = T::kInt4 ? 32 : 16, PER_ROW = D / CH, UNITS = T::KT * PER_ROW / 128, PASS = 128 / PER_ROW;
+          const int c = tid % PER_ROW, r0 = tid / PER_ROW;
+          uint4 w16[UNITS];
+          float sc[UNITS];
+#pragma unroll
+          for (int u = 0; u < UNITS; ++u) {
+            const int row = r0 + u * PASS, tok = tok0 + row;
+            w16[u] = T::kInt4 ? make_uint4(0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u) : make_uint4(0u, 0u, 0u, 0u);
+            sc[u] = 0.f;
+            const int pg = page[T::KT == 64 ? 0 : row >> 6];
+            if (pg >= 0 && tok < x.n) {
+              const uint8_t* const block = p.pages + page_block_offset(p.g, p.layer0 + ll, pg, h);
+              const int at = part * kPageTokens + (row & 63);
+              w16[u] = *(const uint4*)(block + at * T::RB + c * 16);
+              const uint8_t* const s = block + 2 * kPageTokens * T::RB + at * T::SB;
+              sc[u] = T::kInt4 ? __uint_as_float((uint32_t)((const uint16_t*)s)[c] << 16) : e8m0(*s);
+            }
+          }
+          const int slot0 = r.slot;
+#pragma unroll
+          for (int i = 0; i < T::PARTS; ++i) {
+            if (!warp_wait(smem_u32(&sh.empty[r.slot]), r.phase ^ 1)) return false;
+            r.template next<T>();
+          }
+          if (part == 0 && tid == 0) {
+            sh.pages[tile_no & 7] = there;
+            if (t == x.t0) sh.bad[(item_no + 8) & 15] = 0;
+          }
+          const uint32_t hi0 = ring0 + slot0 * T::kSlot, lo0 = hi0 + T::kSlot;       // (parts of a tile never wrap)
+          bool any = false;
+#pragma unroll
+          for (int u = 0; u < UNITS; ++u) {
+            const int row = r0 + u * PASS;
+            const bool check = edge && tok0 + row >= see;
+            const uint32_t* const q = &w16[u].x;
+            if constexpr (T::kInt4) {
+              const int turn = (c >> 1) ^ ((row & 1) << 1);          // neighbouring lanes store to different banks
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const int kk = k ^ turn;
+                const uint32_t word = kk == 0 ? q[0] : kk == 1 ? q[1] : kk == 2 ? q[2] : q[3];
+                uint4 hi, lo;
+                int4_to_bf16(word, sc[u], hi, lo);
+                if (check && !(fabsf(sc[u]) <= 3.4e38f)) {
+                  any = true;
+                  hi = lo = make_uint4(0u, 0u, 0u, 0u);
+                }
+                st_shared(hi0 + swz(T::KT, row, 4 * c + kk), hi);
+                st_shared(lo0 + swz(T::KT, row, 4 * c + kk), lo);
+              }
+            } else {
+              uint4 v[2];
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const uint2 a = e4m3_to_bf16(q[2 * k], sc[u]), b = e4m3_to_bf16(q[2 * k + 1], sc[u]);
+                v[k] = make_uint4(a.x, a.y, b.x, b.y);
+                if (check) any |= drop_non_finite(v[k]);
+              }
+              const int turn = c >> 2;
+              st_shared(hi0 + swz(T::KT, row, 2 * c + turn), v[turn]);
+              st_shared(hi0 + swz(T::KT, row, 2 * c + (turn ^ 1)), v[turn ^ 1]);
+            }
+          }
+          if (any) sh.bad[item_no & 15] = 1;
+          fence_proxy_async();
+          __syncwarp();
+          if (lane == 0)
+            for (int i = 0; i < T::PARTS; ++i) bar_arrive(smem_u32(&sh.full[slot0 + i]));
+        }
+      }
+    }
+    ++item_no;
+  } while (prompt_walk_next(p, cut, w, x.cost));
+  return true;
+}
+
+// ---- one thread of warp 12: products
+template <int D, int FMT>
+__device__ __forceinline__ bool mma_role(const PagedPromptParams& p, PromptWalk w, Shared& sh, uint32_t q0, uint32_t ring0, uint32_t tmem) {
+  using T = Shape<D, FMT>;
+  constexpr PromptCut cut = T::cut();
+  constexpr uint32_t kIdQK = idesc(T::KT, false), kIdPV = idesc(D, true);
+  Ring kr{0, 0};                        // of the next key tile
+  uint32_t q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
+  const uint64_t dq[2] = {umma_desc(q0, 16, 1024), umma_desc(q0 + kHalf * D * 2, 16, 1024)};
+  auto step = [&](Ring& r, int n) { for (int i = 0; i < n; ++i) r.template next<T>(); };
+  auto wait_full = [&](Ring r) {
+    for (int i = 0; i < T::PARTS; ++i, r.template next<T>())
+      if (!bar_wait(smem_u32(&sh.full[r.slot]), r.phase)) return false;
+    return true;
+  };
+  auto release = [&](const Ring& r) {
+    for (int i = 0; i < T::PARTS; ++i) mma_commit(smem_u32(&sh.empty[r.slot + i]));
+  };
+  auto qk = [&](int half, const Ring& r) {
+    const uint32_t d = tmem + half * T::kColS;
+#pragma unroll
+    for (int part = 0; part < T::PARTS; ++part) {
+      const uint64_t dk = umma_desc(ring0 + (r.slot + part) * T::kSlot, 16, 1024);
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) {
+        const uint64_t b = dk + (uint64_t)((ks >> 2) * (T::KT * 8) + (ks & 3) * 2);
+        if constexpr (T::kQTmem) mma_ts(d, tmem + T::kColQ + half * (D / 2) + ks * 8, b, kIdQK, part > 0 || ks > 0);
+        else mma_ss(d, dq[half] + (uint64_t)((ks >> 2) * (kHalf * 8) + (ks & 3) * 2), b, kIdQK, ks > 0);
+      }
+    }
+    mma_commit(smem_u32(&sh.s_full[half]));
+  };
+  auto pv = [&](int half, const Ring& r, bool first) {
+    const uint32_t a = tmem + half * T::kColS, d = tmem + T::kColO + half * D;
+#pragma unroll
+    for (int part = 0; part < T::PARTS; ++part) {
+      const uint64_t dv = umma_desc(ring0 + (r.slot + part) * T::kSlot, T::KT * 128, 1024);
+#pragma unroll
+      for (int ks = 0; ks < T::KT / 16; ++ks) mma_ts(d, a + ks * 8, dv + (uint64_t)(ks * 128), kIdPV, !first || part > 0 || ks > 0);
+    }
+    mma_commit(smem_u32(&sh.o_full[half]));
+  };
+  PromptPiece x;
+  do {
+    x = prompt_piece(p, cut, w);
+    if (x.t0 == x.t1) continue;
+    const Halves hv = halves_of<T>(p, w, x);
+    if (!wait_full(kr)) return false;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      if (x.t0 == hv.t1[half]) continue;
+      if (!bar_wait(smem_u32(&sh.q_full[half]), q_phase[half])) return false;
+      q_phase[half] ^= 1;
+      fence_after();
+      qk(half, kr);
+    }
+    release(kr);
+    for (int t = x.t0; t < x.t1; ++t) {
+      Ring vr = kr;
+      step(vr, T::PARTS);
+      kr = vr;
+      step(kr, T::PARTS);
+      if (!wait_full(vr)) return false;
+      const bool more = t + 1 < x.t1;
+      if (more && !wait_full(kr)) return false;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        if (t < hv.t1[half]) {
+          if (!bar_wait(smem_u32(&sh.p_full[half]), p_phase[half])) return false;
+          p_phase[half] ^= 1;
+          fence_after();
+          pv(half, vr, t == x.t0);
+        }
+        if (t + 1 < hv.t1[half]) qk(half, kr);
+      }
+      release(vr);
+      if (more) release(kr);
+    }
+  } while (prompt_walk_next(p, cut, w, x.cost));
+  return true;
+}
+
+// ---- warps 0-3, 4-7: the softmax of a half
+template <int D, int FMT>
+__device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, PromptWalk w, Shared& sh, uint32_t q0, uint32_t tmem) {
+  using T = Shape<D, FMT>;
+  constexpr PromptCut cut = T::cut();
+  constexpr int KT = T::KT;
+  const int half = threadIdx.x >> 7, row = threadIdx.x & 127, lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 3;
+  const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+  const uint32_t tS = tmem + lanes + half * T::kColS, tO = tmem + lanes + T::kColO + half * D, tQ = tmem + lanes + T::kColQ + half * (D / 2);
+  const uint32_t s_full = smem_u32(&sh.s_full[half]), p_full = smem_u32(&sh.p_full[half]), o_full = smem_u32(&sh.o_full[half]);
+  const uint32_t q_full = smem_u32(&sh.q_full[half]);
+  uint32_t s_phase = 0, o_phase = 0;
+  int tile_no = 0, item_no = 0;
+  PromptPiece x;
+  do {
+    x = prompt_piece(p, cut, w);
+    if (x.t0 == x.t1) continue;
+    const Halves hv = halves_of<T>(p, w, x);
+    const int ll = p.by_heads.div(w.lh), h = w.lh - ll * p.g.N_kv;
+    const int rows = half ? hv.rows[1] : hv.rows[0], see = half ? hv.see[1] : hv.see[0], t1 = half ? hv.t1[1] : hv.t1[0];
+    const int ri = half * kHalf + row, s = p.by_group.div(ri), head = h * p.G + ri - s * p.G;
+    const bool on = row < rows;
+
+    // ---- queries: a row each (the last product that read the former ones has been waited for)
+    if (t1 > x.t0) {
+      const uint4* src = (const uint4*)p.q.ptr;
+      if (on) src = (const uint4*)((const uint16_t*)p.q.ptr + prompt_row(p, p.q, w.b, w.s, x.s0 + s) + ll * p.q.sl + head * p.q.sn);
+      if constexpr (T::kQTmem) {
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) {
+          uint4 v[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] = on ? __ldg(src + c * 8 + i) : make_uint4(0u, 0u, 0u, 0u);
+          tmem_st32(tQ + c * 32, (const uint32_t*)v);
+        }
+        tmem_wait_st();
+        fence_before();
+      } else {
+        const uint32_t dst = q0 + half * kHalf * D * 2;
+#pragma unroll
+        for (int ck = 0; ck < D / 8; ++ck) cp_async16(dst + swz(kHalf, row, ck), src + (on ? ck : 0), on ? 16 : 0);
+        cp_async_wait_all();
+        fence_proxy_async();
+      }
+      __syncwarp();
+      if (lane == 0) bar_arrive(q_full);
+    }
+    const int limit = on ? min(x.n, w.s.pos + x.s0 + s + 1) : 0;      // tokens that the row sees
+    float m = -INFINITY, l = 0.f, lc = 0.f;                           // lc: what the additions to l have lost
+    bool seen = false;
+    const int tile0 = tile_no;
+    for (int t = x.t0; t < t1; ++t) {
+      if (!warp_wait(s_full, s_phase)) return false;
+      s_phase ^= 1;
+      fence_after();
+      uint32_t sr[KT];
+#pragma unroll
+      for (int c = 0; c < KT; c += 32) tmem_ld32(tS + c, sr + c);
+      const int tok0 = t * KT;
+      const uint32_t there = sh.pages[(tile0 + t - x.t0) & 7];
+      tmem_wait_ld();
+      seen |= ((there & 1) && limit > tok0) || ((there & 2) && limit > tok0 + 64);
+      if (tok0 + KT > see || there != (1u << (KT / 64)) - 1) {        // some tokens are not seen
+        const int last = limit - tok0;
+#pragma unroll
+        for (int j = 0; j < KT; ++j)
+          if (j >= last || !(there >> (j >> 6) & 1)) sr[j] = 0xff800000u;
+      }
+      float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+      for (int j = 0; j < KT; j += 8)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mx[i] = max3(mx[i], __uint_as_float(sr[j + 2 * i]), __uint_as_float(sr[j + 2 * i + 1]));
+      const float m_new = fmaxf(m, max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * p.scale_log2);
+      if (__any_sync(0xffffffffu, m_new > m + 8.f)) {
+        const float f = m == m_new ? 1.f : ex2(m - m_new);
+        if (t > x.t0) {
+          if (!warp_wait(o_full, o_phase ^ 1)) return false;           // the product before this tile's
+          fence_after();
+#pragma unroll 1
+          for (int c = 0; c < D; c += 32) {
+            uint32_t o[32];
+            tmem_ld32(tO + c, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+            tmem_st32(tO + c, o);
+          }
+          tmem_wait_st();
+        }
+        l *= f;
+        lc *= f;
+        m = m_new;
+      }
+      const float ref = m == -INFINITY ? 0.f : -m;
+      float ls[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < KT; c += 64) {
+        uint32_t pk[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          const float a = ex2(fmaf(__uint_as_float(sr[c + 2 * j]), p.scale_log2, ref)), b = ex2(fmaf(__uint_as_float(sr[c + 2 * j + 1]), p.scale_log2, ref));
+          ls[j & 3] += a + b;
+          pk[j] = pack_bf16(a, b);
+        }
+        tmem_st32(tS + c / 2, pk);
+      }
+      tmem_wait_st();
+      fence_before();
+      __syncwarp();
+      if (lane == 0) bar_arrive(p_full);
+      o_phase ^= 1;
+      const float add = ((ls[0] + ls[1]) + (ls[2] + ls[3])) - lc, sum = l + add;
+      lc = (sum - l) - add;
+      l = sum;
+    }
+    tile_no += x.t1 - x.t0;
+
+    // ---- outputs
+    const bool some = t1 > x.t0;
+    if (some) {
+      if (!warp_wait(o_full, o_phase ^ 1)) return false;
+      fence_after();
+    }
+    const bool whole = x.t0 == 0 && x.t1 == x.tiles;
+    const bool mend = sh.bad[item_no & 15] != 0;
+    const bool none = m == -INFINITY && !seen;
+    const float f = whole ? (none ? 0.f : 1.f / l) : 1.f;
+    float* const rec = (float*)p.records + (2 * blockIdx.x + (x.t0 == 0)) * prompt_record_floats(kItemRows, D);
+    uint16_t* dst = nullptr;
+    if (on && whole) dst = (uint16_t*)p.out.ptr + prompt_row(p, p.out, w.b, w.s, x.s0 + s) + ll * p.out.sl + head * p.out.sn;
+#pragma unroll 1
+    for (int c = 0; c < D; c += 32) {
+      uint32_t o[32];
+      if (some) {
+        tmem_ld32(tO + c, o);
+        tmem_wait_ld();
+      }
+      if (!some || none) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) o[j] = 0u;
+      }
+      if (mend && on) {                          // values that were left out because some rows do not see them
+        for (int tok = max(w.s.pos + x.s0 + 1, x.t0 * KT); tok < min(limit, t1 * KT); ++tok) {
+          const int page = tok >= 0 ? page_of(p.table, p.g, w.b, tok, p.error) : -1;
+          if (page < 0) continue;
+          const uint8_t* const block = p.pages + page_block_offset(p.g, p.layer0 + ll, page, h);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            const float v = value_at<D, FMT>(block, tok & 63, c + j);
+            if (!(fabsf(v) <= 3.4e38f)) o[j] = __float_as_uint(__uint_as_float(o[j]) + v);
+          }
+        }
+      }
+      if (on && whole) {
+#pragma unroll
+        for (int j = 0; j < 32; j += 8) {
+          uint32_t u[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) u[k] = none ? 0u : pack_bf16(__uint_as_float(o[j + 2 * k]) * f, __uint_as_float(o[j + 2 * k + 1]) * f);
+          *(uint4*)(dst + c + j) = make_uint4(u[0], u[1], u[2], u[3]);
+        }
+      } else if (on) {
+#pragma unroll
+        for (int j = 0; j < 32; j += 4) *(uint4*)(rec + (size_t)ri * D + c + j) = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+      }
+      __syncwarp();
+    }
+    if (on) {
+      if (!whole) {
+        rec[kItemRows * D + ri] = m;
+        rec[kItemRows * (D + 1) + ri] = m == -INFINITY && l == 0.f ? (seen ? 1.f : 0.f) : l;
+      } else if (p.lse) {
+        p.lse[(prompt_lse_row(p, w.b, w.s, x.s0 + s) * p.nlayers + ll) * p.N_q + head] = prompt_log_sum(m, l);
+      }
+    }
+    fence_before();
+    if (!whole && x.t0 == 0 && threadIdx.x == 0) p.desc[blockIdx.x] = prompt_desc(cut, w, x);
+    ++item_no;
+  } while (prompt_walk_next(p, cut, w, x.cost));
+  return true;
+}
+
+template <int D, int FMT>
+__global__ void __launch_bounds__(kThreads, 1) k_paged_prompt_tc(const __grid_constant__ PagedPromptParams p, const __grid_constant__ CUtensorMap map) {
+  using T = Shape<D, FMT>;
+  constexpr PromptCut cut = T::cut();
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ __align__(16) Shared sh;
+  begin_dependent();
+  const int tid = threadIdx.x, warp = tid >> 5;
+  if (tid == 0) p.desc[blockIdx.x].pieces = 0;
+  PromptWalk w;
+  if (!prompt_walk_begin<kThreads>(p, cut, w, sh.scratch)) return;
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t q0 = base, ring0 = base + T::kQBytes;
+  if (warp == 12) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_u32(&sh.tmem)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  if (tid == 0) {
+    for (int i = 0; i < T::kSlots; ++i) {
+      bar_init(smem_u32(&sh.full[i]), 4);
+      bar_init(smem_u32(&sh.empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      bar_init(smem_u32(&sh.s_full[i]), 1);
+      bar_init(smem_u32(&sh.p_full[i]), 4);
+      bar_init(smem_u32(&sh.o_full[i]), 1);
+      bar_init(smem_u32(&sh.q_full[i]), 4);
+    }
+    bar_init(smem_u32(&sh.raw), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    sh.failed = 0;
+    for (int i = 0; i < 16; ++i) sh.bad[i] = 0;
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = sh.tmem;
+  bool ok = true;
+  if (warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    ok = softmax_role<D, FMT>(p, w, sh, q0, tmem);
+  } else if (warp < 12) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+    ok = load_role<D, FMT>(p, &map, w, sh, ring0);
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    if (tid == 12 * 32) ok = mma_role<D, FMT>(p, w, sh, q0, ring0, tmem);
+    __syncwarp();
+  }
+  if (!ok) {
+    atomicOr(p.error, kErrWaitTimeout);
+    sh.failed = 1;
+  }
+  fence_before();
+  __syncthreads();
+  if (sh.failed) {                       // copies and products under way end before their memory is given up
+    const long long t0 = clock64();
+    while (clock64() - t0 < 4000000LL) {}
+  }
+  if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(512) : "memory");
+}
+
+template <int D, int FMT>
+cudaError_t setup() {
+  cudaError_t e = cudaFuncSetAttribute(k_paged_prompt_tc<D, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D, FMT>::kSmem);
+  cudaFuncAttributes a;
+  if (e == cudaSuccess) e = cudaFuncGetAttributes(&a, k_paged_prompt_tc<D, FMT>);
+  // the roles' shares of the registers add up to 128 a thread: less would be a wait without an end
+  if (e == cudaSuccess && a.numRegs < 128) e = cudaErrorLaunchOutOfResources;
+  return e;
+}
+template <int D, int FMT>
+cudaError_t launch(const PagedPromptParams& p, const CUtensorMap& map, cudaStream_t s) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(p.grid);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = Shape<D, FMT>::kSmem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, k_paged_prompt_tc<D, FMT>, p, map);
+  if (e != cudaSuccess) (void)cudaGetLastError();
+  return e;
+}
+
+}  // namespace
+
+PromptCut paged_prompt_tc_cut(int format) { return PromptCut{format == THINK_PAGE_INT4 ? 64 : 128, kExtra}; }
+int paged_prompt_tc_rows() { return kItemRows; }
+
+cudaError_t paged_prompt_tc_setup(int format, int D) {
+  switch (format * 256 + D) {
+    case THINK_PAGE_PLAIN * 256 + 64: return setup<64, THINK_PAGE_PLAIN>();
+    case THINK_PAGE_PLAIN * 256 + 128: return setup<128, THINK_PAGE_PLAIN>();
+    case THINK_PAGE_E4M3 * 256 + 64: return setup<64, THINK_PAGE_E4M3>();
+    case THINK_PAGE_E4M3 * 256 + 128: return setup<128, THINK_PAGE_E4M3>();
+    case THINK_PAGE_INT4 * 256 + 64: return setup<64, THINK_PAGE_INT4>();
+    case THINK_PAGE_INT4 * 256 + 128: return setup<128, THINK_PAGE_INT4>();
+  }
+  return cudaErrorInvalidValue;
+}
+cudaError_t launch_paged_prompt_tc(const PagedPromptParams& p, int format, const void* map, cudaStream_t s) {
+  CUtensorMap m;
+  memcpy(&m, map, sizeof(m));
+  switch (format * 256 + p.g.D) {
+    case THINK_PAGE_PLAIN * 256 + 64: return launch<64, THINK_PAGE_PLAIN>(p, m, s);
+    case THINK_PAGE_PLAIN * 256 + 128: return launch<128, THINK_PAGE_PLAIN>(p, m, s);
+    case THINK_PAGE_E4M3 * 256 + 64: return launch<64, THINK_PAGE_E4M3>(p, m, s);
+    case THINK_PAGE_E4M3 * 256 + 128: return launch<128, THINK_PAGE_E4M3>(p, m, s);
+    case THINK_PAGE_INT4 * 256 + 64: return launch<64, THINK_PAGE_INT4>(p, m, s);
+    case THINK_PAGE_INT4 * 256 + 128: return launch<128, THINK_PAGE_INT4>(p, m, s);
+  }
+  return cudaErrorInvalidValue;
+}
+
+}  // namespace think

@@ -5,6 +5,7 @@
 
 #include <new>
 
+#include <cuda.h>
 #include <nvtx3/nvToolsExt.h>
 
 #include "paged_internal.h"
@@ -112,9 +113,26 @@ struct thinK_paged {
   uint8_t* pages;
   uint8_t* ws;
   int grid;
+  CUtensorMap map;           // bf16 caches of plain pages: see launch_paged_prompt
+  bool mapped;
 };
 
 namespace {
+// The pool as rows of D bf16 in boxes of 64 channels x 64 rows, which arrive in shared memory with the 128-byte swizzle.
+bool map_pool(thinK_paged* p) {
+  const PageGeom& g = p->g.g;
+  const int64_t rows = (int64_t)g.L * g.num_pages * g.N_kv * 2 * kPageTokens;
+  if (rows > INT32_MAX) return false;                  // (more than any memory holds: a row has 128 bytes at least)
+  void* fn = nullptr;
+  cudaDriverEntryPointQueryResult found;
+  if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess || !fn) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)g.D, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)g.row_bytes};
+  const cuuint32_t box[2] = {64, (cuuint32_t)kPageTokens}, step[2] = {1, 1};
+  return ((decltype(&cuTensorMapEncodeTiled))fn)(&p->map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p->pages, dims, strides, box, step,
+                                                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool layers_ok(const thinK_paged* p, int layer0, int nlayers) {
   return layer0 >= 0 && nlayers >= 1 && layer0 <= p->g.g.L && nlayers <= p->g.g.L - layer0;
 }
@@ -191,6 +209,8 @@ thinK_status thinK_paged_create(const thinK_paged_config* cfg, const thinK_paged
     return THINK_ERR_CUDA;
   }
   p->grid = sms < kSMs ? sms : kSMs;                 // one wave, one CTA an SM
+  memset(&p->map, 0, sizeof(p->map));
+  p->mapped = p->g.dtype == THINK_BF16 && p->g.format == THINK_PAGE_PLAIN && map_pool(p);
   *out = p;
   return THINK_OK;
 }
@@ -319,6 +339,7 @@ thinK_status thinK_paged_prompt_attn(thinK_paged* p, thinK_tensor5 q, thinK_tens
   if (max_rows == 0) return THINK_OK;                  // views without rows may have no memory
   if (!view_ok(q, p->g.elem) || !view_ok(out, p->g.elem) || !scratch || !aligned(scratch, 256)) return THINK_ERR_INVALID_ARG;
   if (scratch_bytes < thinK_paged_prompt_scratch(p)) return THINK_ERR_CAPACITY;
+  if (p->g.dtype == THINK_BF16 && p->g.format == THINK_PAGE_PLAIN && !p->mapped) return THINK_ERR_UNSUPPORTED;
   const int B = start ? 1 : table.B, unit = 16 / p->g.elem;
   if (start) q.stride_b = out.stride_b = 0;
   auto view = [&](const thinK_tensor5& t) {
@@ -340,7 +361,7 @@ thinK_status thinK_paged_prompt_attn(thinK_paged* p, thinK_tensor5 q, thinK_tens
   d.per = paged_prompt_rows(p->g.dtype) / p->g.G;
   // positions fit 32 bits; so do the items of a sequence, and all places of the line 62
   const int64_t tokens = (int64_t)table.max_pages * kPageTokens;
-  const PromptCut cut = paged_prompt_cut(p->g.dtype);
+  const PromptCut cut = paged_prompt_cut(p->g.dtype, p->g.format);
   const double items = (double)max_rows / d.per + 1;
   if (tokens + max_rows > INT32_MAX || (int64_t)nlayers * p->g.g.N_kv > INT32_MAX ||
       items * ((double)tokens + max_rows + cut.extra) * table.B * nlayers * p->g.g.N_kv > 4.0e15) return THINK_ERR_UNSUPPORTED;
@@ -360,7 +381,7 @@ thinK_status thinK_paged_prompt_attn(thinK_paged* p, thinK_tensor5 q, thinK_tens
   d.grid = p->grid;
   d.by_group = FastDiv((uint32_t)p->g.G);
   d.by_heads = FastDiv((uint32_t)p->g.g.N_kv);
-  if (launch_paged_prompt(d, p->g.dtype, p->g.format, (cudaStream_t)stream) != cudaSuccess) return THINK_ERR_CUDA;
+  if (launch_paged_prompt(d, p->g.dtype, p->g.format, &p->map, (cudaStream_t)stream) != cudaSuccess) return THINK_ERR_CUDA;
   return THINK_OK;
 }
 

@@ -31,10 +31,16 @@ struct PagedPromptParams {
 // are relative to.  l = 0 and m = -infinity: no token; l = 1 with that m: tokens, but all their logits are -infinity.
 __host__ __device__ inline size_t prompt_record_floats(int rows, int D) { return (size_t)rows * (D + 2); }
 
-cudaError_t launch_paged_prompt(const PagedPromptParams& p, int dtype, int format, cudaStream_t s);
+// `map`: of a bf16 cache of plain pages, the pool as rows of D elements in boxes of 64 x 64 (a CUtensorMap)
+cudaError_t launch_paged_prompt(const PagedPromptParams& p, int dtype, int format, const void* map, cudaStream_t s);
 cudaError_t paged_prompt_setup(int dtype, int format, int D);       // kernel attributes on the current device
 int paged_prompt_rows(int dtype);                                   // query rows of an item
-PromptCut paged_prompt_cut(int dtype);
+PromptCut paged_prompt_cut(int dtype, int format);
+
+cudaError_t launch_paged_prompt_tc(const PagedPromptParams& p, int format, const void* map, cudaStream_t s);
+cudaError_t paged_prompt_tc_setup(int format, int D);
+int paged_prompt_tc_rows();
+PromptCut paged_prompt_tc_cut(int format);
 
 #ifdef __CUDACC__
 struct PromptSeq {
