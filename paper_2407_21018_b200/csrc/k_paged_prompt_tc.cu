@@ -5,8 +5,8 @@
 //   S = Q K^T       tcgen05.mma into tensor memory, a tile of KT tokens; thread t of a half's four warps owns row t
 //   P = 2^(x - m)   read from tensor memory, written back over S as bf16: the A operand of
 //   O += P V        tcgen05.mma, V as stored ([token][channel]) is the MN-major B operand
-// Roles: warps 0-3 and 4-7 the softmax of a half each, warps 8-11 bring keys and values into a ring of shared-memory slots
-// (bf16 pages by TMA, others unpacked in registers), one thread of warp 12 issues all products.  m only moves when a row's
+// Roles: warps 0-3 and 4-7 the softmax of a half each, three or four more bring keys and values into a ring of shared-memory
+// slots (bf16 pages by TMA, others unpacked in registers), one thread of another issues all products.  m only moves when a row's
 // logits pass it by 2^8 (O is then rescaled in tensor memory), so the softmax seldom waits for the products.
 // 4-bit values n * s have 11 bits: they enter as the sum of two bf16, which is exact, at twice the products; their keys
 // and values need twice the room, so tiles are 64 tokens and Q is held in tensor memory too.
@@ -21,7 +21,7 @@
 namespace think {
 namespace {
 
-constexpr int kHalf = 128, kItemRows = 2 * kHalf, kThreads = 512;
+constexpr int kHalf = 128, kItemRows = 2 * kHalf;
 constexpr int kExtra = 256;             // places of an item besides its tokens: what starting and ending one costs
 
 // ---- PTX
@@ -146,8 +146,16 @@ struct Shape {
   static constexpr bool kQTmem = kInt4;
   static constexpr int kSlot = KT * D * 2;
   static constexpr int kQBytes = kQTmem ? 0 : 2 * kHalf * D * 2;
-  static constexpr int kSlots = (196608 - kQBytes) / kSlot < 12 ? (196608 - kQBytes) / kSlot / (2 * PARTS) * 2 * PARTS : 12;
+  static constexpr int kFit = (229376 - kQBytes) / kSlot;     // 227 KB less the barriers and what alignment may take
+  static constexpr int kSlots = kFit / PARTS * PARTS < 12 ? kFit / PARTS * PARTS : 12;
   static constexpr int kSmem = kQBytes + kSlots * kSlot + 1024;
+  // roles: two halves' softmax, loads, products; with bf16 pages one warp of the loads' group issues the products
+  static constexpr int kThreads = kPlain ? 384 : 512;
+  static constexpr int kMmaWarp = kPlain ? 11 : 12;
+  static constexpr int kLoadWarps = kPlain ? 3 : 4;
+  static constexpr int kRegs = kPlain ? 168 : 128;            // a thread at launch
+  static constexpr int kSoftmaxRegs = kPlain ? 200 : 176, kLoadRegs = kPlain ? 104 : 96, kMmaRegs = 64;
+  static_assert(2 * kSoftmaxRegs + kLoadRegs + (kPlain ? 0 : kMmaRegs) <= kRegs * kThreads / 128, "more registers than the block has: a wait without end");
   // tensor memory: S of each half, Q, O of each half
   static constexpr int kColS = KT, kColQ = 2 * KT, kColO = 256;
   static constexpr int RB = kPlain ? D * 2 : kInt4 ? D / 2 : D;       // bytes of a stored row
@@ -262,13 +270,44 @@ struct Ring {                 // position in the ring of slots
   }
 };
 
-// ---- warps 8-11: keys and values
+// Pages of a sequence's tiles, 32 at a time in the lanes of a warp, the next ones on their way.
+struct PageWindow {
+  int32_t now, next;
+  int first;                  // page of the sequence that lane 0 holds
+  __device__ __forceinline__ int32_t fetch(const PageTableView& t, int b, int first_page, int pages) const {
+    const int i = first_page + (threadIdx.x & 31);
+    return i < pages ? load_now(t.table + b * t.stride + i) : -1;
+  }
+  __device__ __forceinline__ void begin(const PageTableView& t, int b, int page, int pages) {
+    first = page;
+    now = fetch(t, b, first, pages);
+    next = fetch(t, b, first + 32, pages);
+  }
+  // page i of the sequence (i grows); -1 if there is none, error bit if the table holds no page of the pool
+  __device__ __forceinline__ int at(const PageTableView& t, const PageGeom& g, int b, int i, int pages, uint32_t* error) {
+    if (i - first >= 32) {
+      first += 32;
+      now = next;
+      next = fetch(t, b, first + 32, pages);
+    }
+    const int page = __shfl_sync(0xffffffffu, now, i - first);
+    if (i >= pages) return -1;
+    if ((uint32_t)page >= (uint32_t)g.num_pages) {
+      if ((threadIdx.x & 127) == 0) atomicOr(error, kErrPage);
+      return -1;
+    }
+    return page;
+  }
+};
+
+// ---- loads: keys and values
 template <int D, int FMT>
 __device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUtensorMap* map, PromptWalk w, Shared& sh, uint32_t ring0) {
   using T = Shape<D, FMT>;
   constexpr PromptCut cut = T::cut();
-  const int tid = threadIdx.x & 127, lane = threadIdx.x & 31;
+  const int tid = threadIdx.x & 127, lane = threadIdx.x & 31;     // (of kLoadWarps warps)
   Ring r{0, 0};
+  PageWindow win;
   uint32_t raw_phase = 0;
   int tile_no = 0, item_no = 0;
   PromptPiece x;
@@ -277,13 +316,15 @@ __device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUte
     if (x.t0 == x.t1) continue;
     const int ll = p.by_heads.div(w.lh), h = w.lh - ll * p.g.N_kv;
     const int see = w.s.pos + x.s0 + 1;            // tokens that every row sees
+    const int pages = (x.n + 63) >> 6;
+    win.begin(p.table, w.b, x.t0 * (T::KT / 64), pages);
     for (int t = x.t0; t < x.t1; ++t, ++tile_no) {
       const int tok0 = t * T::KT;
       int page[T::KT / 64];
       uint32_t there = 0;
 #pragma unroll
       for (int i = 0; i < T::KT / 64; ++i) {
-        page[i] = tok0 + 64 * i < x.n ? page_of(p.table, p.g, w.b, tok0 + 64 * i, p.error) : -1;
+        page[i] = win.at(p.table, p.g, w.b, t * (T::KT / 64) + i, pages, p.error);
         there |= (page[i] >= 0 ? 1u : 0u) << i;
       }
 #pragma unroll
@@ -312,18 +353,19 @@ __device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUte
             if (!warp_wait(raw, raw_phase)) return false;
             raw_phase ^= 1;
             // thread = token: what is behind the last one or on no page becomes 0, what only some rows see finite
-            const int tok = tok0 + tid;
-            const bool off = tok >= x.n || !(there >> (tid >> 6) & 1);
-            if (off || tok >= see) {
+            for (int i = tid; i < T::KT; i += 32 * T::kLoadWarps) {
+              const int tok = tok0 + i;
+              const bool off = tok >= x.n || !(there >> (i >> 6) & 1);
+              if (!off && tok < see) continue;
               bool any = false;
 #pragma unroll
               for (int ck = 0; ck < D / 8; ++ck) {
                 uint4 v = make_uint4(0u, 0u, 0u, 0u);
                 if (!off) {
-                  v = ld_shared(slot + swz(T::KT, tid, ck));
+                  v = ld_shared(slot + swz(T::KT, i, ck));
                   any |= drop_non_finite(v);
                 }
-                st_shared(slot + swz(T::KT, tid, ck), v);
+                st_shared(slot + swz(T::KT, i, ck), v);
               }
               if (any) sh.bad[item_no & 15] = 1;
             }
@@ -412,7 +454,7 @@ __device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUte
   return true;
 }
 
-// ---- one thread of warp 12: products
+// ---- one thread: products
 template <int D, int FMT>
 __device__ __forceinline__ bool mma_role(const PagedPromptParams& p, PromptWalk w, Shared& sh, uint32_t q0, uint32_t ring0, uint32_t tmem) {
   using T = Shape<D, FMT>;
@@ -476,7 +518,7 @@ __device__ __forceinline__ bool mma_role(const PagedPromptParams& p, PromptWalk 
       step(kr, T::PARTS);
       if (!wait_full(vr)) return false;
       const bool more = t + 1 < x.t1;
-      if (more && !wait_full(kr)) return false;
+      bool keys = false;
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         if (t < hv.t1[half]) {
@@ -485,7 +527,11 @@ __device__ __forceinline__ bool mma_role(const PagedPromptParams& p, PromptWalk 
           fence_after();
           pv(half, vr, t == x.t0);
         }
-        if (t + 1 < hv.t1[half]) qk(half, kr);
+        if (t + 1 < hv.t1[half]) {
+          if (!keys && !wait_full(kr)) return false;
+          keys = true;
+          qk(half, kr);
+        }
       }
       release(vr);
       if (more) release(kr);
@@ -678,7 +724,7 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, PromptW
 }
 
 template <int D, int FMT>
-__global__ void __launch_bounds__(kThreads, 1) k_paged_prompt_tc(const __grid_constant__ PagedPromptParams p, const __grid_constant__ CUtensorMap map) {
+__global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(const __grid_constant__ PagedPromptParams p, const __grid_constant__ CUtensorMap map) {
   using T = Shape<D, FMT>;
   constexpr PromptCut cut = T::cut();
   extern __shared__ unsigned char smem_raw[];
@@ -687,16 +733,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_prompt_tc(const __grid_co
   const int tid = threadIdx.x, warp = tid >> 5;
   if (tid == 0) p.desc[blockIdx.x].pieces = 0;
   PromptWalk w;
-  if (!prompt_walk_begin<kThreads>(p, cut, w, sh.scratch)) return;
+  if (!prompt_walk_begin<T::kThreads>(p, cut, w, sh.scratch)) return;
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t q0 = base, ring0 = base + T::kQBytes;
-  if (warp == 12) {
+  if (warp == T::kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_u32(&sh.tmem)), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   if (tid == 0) {
     for (int i = 0; i < T::kSlots; ++i) {
-      bar_init(smem_u32(&sh.full[i]), 4);
+      bar_init(smem_u32(&sh.full[i]), T::kLoadWarps);
       bar_init(smem_u32(&sh.empty[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -716,15 +762,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_prompt_tc(const __grid_co
   const uint32_t tmem = sh.tmem;
   bool ok = true;
   if (warp < 8) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(T::kSoftmaxRegs));
     ok = softmax_role<D, FMT>(p, w, sh, q0, tmem);
-  } else if (warp < 12) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
-    ok = load_role<D, FMT>(p, &map, w, sh, ring0);
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-    if (tid == 12 * 32) ok = mma_role<D, FMT>(p, w, sh, q0, ring0, tmem);
-    __syncwarp();
+    if (T::kPlain || warp < 12) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(T::kLoadRegs));
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(T::kMmaRegs));
+    if (warp < 8 + T::kLoadWarps) {
+      ok = load_role<D, FMT>(p, &map, w, sh, ring0);
+    } else {
+      if (tid == T::kMmaWarp * 32) ok = mma_role<D, FMT>(p, w, sh, q0, ring0, tmem);
+      __syncwarp();
+    }
   }
   if (!ok) {
     atomicOr(p.error, kErrWaitTimeout);
@@ -736,7 +784,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_prompt_tc(const __grid_co
     const long long t0 = clock64();
     while (clock64() - t0 < 4000000LL) {}
   }
-  if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(512) : "memory");
+  if (warp == T::kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(512) : "memory");
 }
 
 template <int D, int FMT>
@@ -744,15 +792,15 @@ cudaError_t setup() {
   cudaError_t e = cudaFuncSetAttribute(k_paged_prompt_tc<D, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D, FMT>::kSmem);
   cudaFuncAttributes a;
   if (e == cudaSuccess) e = cudaFuncGetAttributes(&a, k_paged_prompt_tc<D, FMT>);
-  // the roles' shares of the registers add up to 128 a thread: less would be a wait without an end
-  if (e == cudaSuccess && a.numRegs < 128) e = cudaErrorLaunchOutOfResources;
+  // the roles' shares of the registers add up to these: fewer would be a wait without an end
+  if (e == cudaSuccess && a.numRegs < Shape<D, FMT>::kRegs) e = cudaErrorLaunchOutOfResources;
   return e;
 }
 template <int D, int FMT>
 cudaError_t launch(const PagedPromptParams& p, const CUtensorMap& map, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(p.grid);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(Shape<D, FMT>::kThreads);
   cfg.dynamicSmemBytes = Shape<D, FMT>::kSmem;
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
