@@ -107,6 +107,11 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, i
   asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
+// contiguous bytes (a multiple of 16, both addresses too)
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               :: "r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
@@ -146,30 +151,34 @@ struct Shape {
   static constexpr bool kQTmem = kInt4;
   static constexpr int kSlot = KT * D * 2;
   static constexpr int kQBytes = kQTmem ? 0 : 2 * kHalf * D * 2;
-  static constexpr int kFit = (229376 - kQBytes) / kSlot;     // 227 KB less the barriers and what alignment may take
+  static constexpr int RB = kPlain ? D * 2 : kInt4 ? D / 2 : D;       // bytes of a stored row
+  static constexpr int SB = kPlain ? 0 : kInt4 ? D / 16 : 1;          // bytes of its scales
+  // quantised pages: 64 stored rows and their scales a stage; two tiles' worth, or what there is room for
+  static constexpr int kStage = kPlain ? 0 : kPageTokens * RB + (kPageTokens * SB + 127) / 128 * 128;
+  static constexpr int kStages = kPlain ? 0 : kInt4 || D == 64 ? 8 : 4;
+  static constexpr int kFit = (229376 + 1536 - kQBytes - kStages * kStage) / kSlot;      // 227 KB less the barriers and what alignment may take
   static constexpr int kSlots = kFit / PARTS * PARTS < 12 ? kFit / PARTS * PARTS : 12;
-  static constexpr int kSmem = kQBytes + kSlots * kSlot + 1024;
+  static constexpr int kSmem = kQBytes + kSlots * kSlot + kStages * kStage + 1024;
   // roles: two halves' softmax, loads, products; with bf16 pages one warp of the loads' group issues the products
   static constexpr int kThreads = kPlain ? 384 : 512;
-  static constexpr int kMmaWarp = kPlain ? 11 : 12;
+  static constexpr int kMmaWarp = kPlain ? 11 : 12, kFetchWarp = 13;
   static constexpr int kLoadWarps = kPlain ? 3 : 4;
   static constexpr int kRegs = kPlain ? 168 : 128;            // a thread at launch
   static constexpr int kSoftmaxRegs = kPlain ? 200 : 176, kLoadRegs = kPlain ? 104 : 96, kMmaRegs = 64;
   static_assert(2 * kSoftmaxRegs + kLoadRegs + (kPlain ? 0 : kMmaRegs) <= kRegs * kThreads / 128, "more registers than the block has: a wait without end");
   // tensor memory: S of each half, Q, O of each half
   static constexpr int kColS = KT, kColQ = 2 * KT, kColO = 256;
-  static constexpr int RB = kPlain ? D * 2 : kInt4 ? D / 2 : D;       // bytes of a stored row
-  static constexpr int SB = kPlain ? 0 : kInt4 ? D / 16 : 1;          // bytes of its scales
   static __host__ __device__ constexpr PromptCut cut() { return PromptCut{KT, kExtra}; }
 };
 
 struct Shared {
-  uint64_t full[12], empty[12], s_full[2], p_full[2], o_full[2], q_full[2], raw;
+  uint64_t full[12], empty[12], s_full[2], p_full[2], o_full[2], q_full[2], raw, st_full[8], st_empty[8];
   long long scratch[40];
   uint32_t tmem;
   // The loads are at most kSlots / (2 PARTS) + 1 <= 6 tiles, so as many items, ahead of the softmax.
   uint32_t pages[8];           // of the tiles under way: bit i: the tile's i-th page is there
   uint32_t bad[16];            // of the items under way: a value that some rows do not see is a NaN or an infinity
+  uint32_t stage_there[8];     // the stage holds a page's rows
   uint32_t failed;
 };
 
@@ -184,6 +193,16 @@ __device__ __forceinline__ uint4 ld_shared(uint32_t at) {
   uint4 w;
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(at) : "memory");
   return w;
+}
+__device__ __forceinline__ uint32_t ld_shared16(uint32_t at) {
+  uint16_t x;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(at) : "memory");
+  return x;
+}
+__device__ __forceinline__ uint32_t ld_shared8(uint32_t at) {
+  uint32_t x;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
+  return x;
 }
 // Sets the NaN and infinite ones of 8 bf16 to 0; whether there were any.
 __device__ __forceinline__ bool drop_non_finite(uint4& w) {
@@ -202,23 +221,29 @@ __device__ __forceinline__ bool drop_non_finite(uint4& w) {
 __device__ __forceinline__ uint2 e4m3_to_bf16(uint32_t w, float s) {
   const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xffffu), __NV_E4M3);
   const __half2_raw b = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3);
-  const float2 x = __half22float2(*(const __half2*)&a), y = __half22float2(*(const __half2*)&b);
-  return make_uint2(pack_bf16(x.x * s, x.y * s), pack_bf16(y.x * s, y.y * s));
+  float2 x = __half22float2(*(const __half2*)&a), y = __half22float2(*(const __half2*)&b);
+  split(mul2(two(x.x, x.y), two(s, s)), x.x, x.y);
+  split(mul2(two(y.x, y.y), two(s, s)), y.x, y.y);
+  return make_uint2(pack_bf16(x.x, x.y), pack_bf16(y.x, y.y));
 }
-// 8 4-bit codes times their scale as the sum of two bf16 (exact: 3 bits times 8; the first part is cut off)
-__device__ __forceinline__ void int4_to_bf16(uint32_t w, float s, uint4& hi, uint4& lo) {
-  const uint32_t even = w & 0x0f0f0f0fu, odd = (w >> 4) & 0x0f0f0f0fu;
-  const f32x2 s2 = two(s, s), off = two(-8388616.f, -8388616.f);
+// 8 4-bit codes times their scale (bf16, twice) as the sum of two bf16: the product rounded, and what the rounding took away
+// (n s has 11 bits, so the rest fits).  Channels come out in the order 0 4 1 5 2 6 3 7, which saves sorting them: queries are
+// permuted alike, and outputs back.
+__device__ __forceinline__ void int4_to_bf16(uint32_t w, uint32_t s2, uint4& hi, uint4& lo) {
   uint32_t h[4], l[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    float a = __uint_as_float(__byte_perm(even, 0x4b000000u, 0x7440 | i)), b = __uint_as_float(__byte_perm(odd, 0x4b000000u, 0x7440 | i));
-    split(mul2(add2(two(a, b), off), s2), a, b);
-    h[i] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
-    l[i] = pack_bf16(a - __uint_as_float(h[i] << 16), b - __uint_as_float(h[i] & 0xffff0000u));
+    uint32_t n;
+    asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(n) : "r"(((w >> (4 * i)) & 0x000f000fu) | 0x43004300u), "r"(0xc308c308u));      // (128 + c) - 136
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(h[i]) : "r"(n), "r"(s2));
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(l[i]) : "r"(n), "r"(s2), "r"(h[i] ^ 0x80008000u));
   }
   hi = make_uint4(h[0], h[1], h[2], h[3]);
   lo = make_uint4(l[0], l[1], l[2], l[3]);
+}
+__device__ __forceinline__ constexpr int int4_channel(int j) { return (j & ~7) | ((j & 1) << 2) | ((j >> 1) & 3); }
+__device__ __forceinline__ uint4 int4_order(const uint4& v) {          // 8 channels of a query
+  return make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
 }
 
 // A value of the pool as fp32, for the few that are looked at one by one.
@@ -293,14 +318,14 @@ struct PageWindow {
     const int page = __shfl_sync(0xffffffffu, now, i - first);
     if (i >= pages) return -1;
     if ((uint32_t)page >= (uint32_t)g.num_pages) {
-      if ((threadIdx.x & 127) == 0) atomicOr(error, kErrPage);
+      if ((threadIdx.x & 31) == 0) atomicOr(error, kErrPage);
       return -1;
     }
     return page;
   }
 };
 
-// ---- loads: keys and values
+// ---- loads of bf16 pages: keys and values by TMA
 template <int D, int FMT>
 __device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUtensorMap* map, PromptWalk w, Shared& sh, uint32_t ring0) {
   using T = Shape<D, FMT>;
@@ -317,136 +342,222 @@ __device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUte
     const int ll = p.by_heads.div(w.lh), h = w.lh - ll * p.g.N_kv;
     const int see = w.s.pos + x.s0 + 1;            // tokens that every row sees
     const int pages = (x.n + 63) >> 6;
-    win.begin(p.table, w.b, x.t0 * (T::KT / 64), pages);
+    win.begin(p.table, w.b, x.t0 * 2, pages);
     for (int t = x.t0; t < x.t1; ++t, ++tile_no) {
       const int tok0 = t * T::KT;
-      int page[T::KT / 64];
-      uint32_t there = 0;
+      int page[2];
 #pragma unroll
-      for (int i = 0; i < T::KT / 64; ++i) {
-        page[i] = win.at(p.table, p.g, w.b, t * (T::KT / 64) + i, pages, p.error);
-        there |= (page[i] >= 0 ? 1u : 0u) << i;
-      }
+      for (int i = 0; i < 2; ++i) page[i] = win.at(p.table, p.g, w.b, t * 2 + i, pages, p.error);
+      const uint32_t there = (page[0] >= 0 ? 1u : 0u) | (page[1] >= 0 ? 2u : 0u);
 #pragma unroll
       for (int part = 0; part < 2; ++part) {
-        const bool edge = part == 1 && (tok0 + T::KT > see || there != (1u << (T::KT / 64)) - 1);     // some values must not be met
-        if constexpr (T::kPlain) {
-          const uint32_t slot = ring0 + r.slot * T::kSlot, full = smem_u32(&sh.full[r.slot]), raw = smem_u32(&sh.raw);
-          if (!warp_wait(smem_u32(&sh.empty[r.slot]), r.phase ^ 1)) return false;
-          if (tid == 0) {
-            if (part == 0) {
-              sh.pages[tile_no & 7] = there;
-              if (t == x.t0) sh.bad[(item_no + 8) & 15] = 0;
-            }
-            const uint32_t bar = edge ? raw : full;
-            bar_arrive_tx(bar, __popc(there) * 64 * D * 2);
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-              if (page[i] >= 0) {
-                const int row = (int)((((int64_t)(p.layer0 + ll) * p.g.num_pages + page[i]) * p.g.N_kv + h) * 128) + part * 64;
-#pragma unroll
-                for (int c = 0; c < D / 64; ++c) tma_load(slot + c * T::KT * 128 + i * 8192, map, c * 64, row, bar);
-              }
-          }
-          if (edge) {
-            __syncwarp();
-            if (!warp_wait(raw, raw_phase)) return false;
-            raw_phase ^= 1;
-            // thread = token: what is behind the last one or on no page becomes 0, what only some rows see finite
-            for (int i = tid; i < T::KT; i += 32 * T::kLoadWarps) {
-              const int tok = tok0 + i;
-              const bool off = tok >= x.n || !(there >> (i >> 6) & 1);
-              if (!off && tok < see) continue;
-              bool any = false;
-#pragma unroll
-              for (int ck = 0; ck < D / 8; ++ck) {
-                uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                if (!off) {
-                  v = ld_shared(slot + swz(T::KT, i, ck));
-                  any |= drop_non_finite(v);
-                }
-                st_shared(slot + swz(T::KT, i, ck), v);
-              }
-              if (any) sh.bad[item_no & 15] = 1;
-            }
-            fence_proxy_async();
-            __syncwarp();
-            if (lane == 0) bar_arrive(full);
-          } else if (tid != 0 && lane == 0) {
-            bar_arrive(full);
-          }
-          r.template next<T>();
-        } else {
-          // a unit is 16 stored bytes: 16 channels of e4m3, 32 of 4 bits
-          constexpr int CH = T::kInt4 ? 32 : 16, PER_ROW = D / CH, UNITS = T::KT * PER_ROW / 128, PASS = 128 / PER_ROW;
-          const int c = tid % PER_ROW, r0 = tid / PER_ROW;
-          uint4 w16[UNITS];
-          float sc[UNITS];
-#pragma unroll
-          for (int u = 0; u < UNITS; ++u) {
-            const int row = r0 + u * PASS, tok = tok0 + row;
-            w16[u] = T::kInt4 ? make_uint4(0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u) : make_uint4(0u, 0u, 0u, 0u);
-            sc[u] = 0.f;
-            const int pg = page[T::KT == 64 ? 0 : row >> 6];
-            if (pg >= 0 && tok < x.n) {
-              const uint8_t* const block = p.pages + page_block_offset(p.g, p.layer0 + ll, pg, h);
-              const int at = part * kPageTokens + (row & 63);
-              w16[u] = *(const uint4*)(block + at * T::RB + c * 16);
-              const uint8_t* const s = block + 2 * kPageTokens * T::RB + at * T::SB;
-              sc[u] = T::kInt4 ? __uint_as_float((uint32_t)((const uint16_t*)s)[c] << 16) : e8m0(*s);
-            }
-          }
-          const int slot0 = r.slot;
-#pragma unroll
-          for (int i = 0; i < T::PARTS; ++i) {
-            if (!warp_wait(smem_u32(&sh.empty[r.slot]), r.phase ^ 1)) return false;
-            r.template next<T>();
-          }
-          if (part == 0 && tid == 0) {
+        const bool edge = part == 1 && (tok0 + T::KT > see || there != 3u);     // some values must not be met
+        const uint32_t slot = ring0 + r.slot * T::kSlot, full = smem_u32(&sh.full[r.slot]), raw = smem_u32(&sh.raw);
+        if (!warp_wait(smem_u32(&sh.empty[r.slot]), r.phase ^ 1)) return false;
+        if (tid == 0) {
+          if (part == 0) {
             sh.pages[tile_no & 7] = there;
             if (t == x.t0) sh.bad[(item_no + 8) & 15] = 0;
           }
-          const uint32_t hi0 = ring0 + slot0 * T::kSlot, lo0 = hi0 + T::kSlot;       // (parts of a tile never wrap)
-          bool any = false;
+          const uint32_t bar = edge ? raw : full;
+          bar_arrive_tx(bar, __popc(there) * 64 * D * 2);
 #pragma unroll
-          for (int u = 0; u < UNITS; ++u) {
-            const int row = r0 + u * PASS;
-            const bool check = edge && tok0 + row >= see;
-            const uint32_t* const q = &w16[u].x;
-            if constexpr (T::kInt4) {
-              const int turn = (c >> 1) ^ ((row & 1) << 1);          // neighbouring lanes store to different banks
+          for (int i = 0; i < 2; ++i)
+            if (page[i] >= 0) {
+              const int row = (int)((((int64_t)(p.layer0 + ll) * p.g.num_pages + page[i]) * p.g.N_kv + h) * 128) + part * 64;
 #pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const int kk = k ^ turn;
-                const uint32_t word = kk == 0 ? q[0] : kk == 1 ? q[1] : kk == 2 ? q[2] : q[3];
-                uint4 hi, lo;
-                int4_to_bf16(word, sc[u], hi, lo);
-                if (check && !(fabsf(sc[u]) <= 3.4e38f)) {
-                  any = true;
-                  hi = lo = make_uint4(0u, 0u, 0u, 0u);
-                }
-                st_shared(hi0 + swz(T::KT, row, 4 * c + kk), hi);
-                st_shared(lo0 + swz(T::KT, row, 4 * c + kk), lo);
-              }
-            } else {
-              uint4 v[2];
-#pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const uint2 a = e4m3_to_bf16(q[2 * k], sc[u]), b = e4m3_to_bf16(q[2 * k + 1], sc[u]);
-                v[k] = make_uint4(a.x, a.y, b.x, b.y);
-                if (check) any |= drop_non_finite(v[k]);
-              }
-              const int turn = c >> 2;
-              st_shared(hi0 + swz(T::KT, row, 2 * c + turn), v[turn]);
-              st_shared(hi0 + swz(T::KT, row, 2 * c + (turn ^ 1)), v[turn ^ 1]);
+              for (int c = 0; c < D / 64; ++c) tma_load(slot + c * T::KT * 128 + i * 8192, map, c * 64, row, bar);
             }
+        }
+        if (edge) {
+          __syncwarp();
+          if (!warp_wait(raw, raw_phase)) return false;
+          raw_phase ^= 1;
+          // thread = token: what is behind the last one or on no page becomes 0, what only some rows see finite
+          for (int i = tid; i < T::KT; i += 32 * T::kLoadWarps) {
+            const int tok = tok0 + i;
+            const bool off = tok >= x.n || !(there >> (i >> 6) & 1);
+            if (!off && tok < see) continue;
+            bool any = false;
+#pragma unroll
+            for (int ck = 0; ck < D / 8; ++ck) {
+              uint4 v = make_uint4(0u, 0u, 0u, 0u);
+              if (!off) {
+                v = ld_shared(slot + swz(T::KT, i, ck));
+                any |= drop_non_finite(v);
+              }
+              st_shared(slot + swz(T::KT, i, ck), v);
+            }
+            if (any) sh.bad[item_no & 15] = 1;
           }
-          if (any) sh.bad[item_no & 15] = 1;
           fence_proxy_async();
           __syncwarp();
-          if (lane == 0)
-            for (int i = 0; i < T::PARTS; ++i) bar_arrive(smem_u32(&sh.full[slot0 + i]));
+          if (lane == 0) bar_arrive(full);
+        } else if (tid != 0 && lane == 0) {
+          bar_arrive(full);
         }
+        r.template next<T>();
+      }
+    }
+    ++item_no;
+  } while (prompt_walk_next(p, cut, w, x.cost));
+  return true;
+}
+
+// ---- quantised pages: one warp has their bytes copied to the stages, 64 rows and their scales each
+template <int D, int FMT>
+__device__ __forceinline__ bool fetch_role(const PagedPromptParams& p, PromptWalk w, Shared& sh, uint32_t stage0) {
+  using T = Shape<D, FMT>;
+  constexpr PromptCut cut = T::cut();
+  const int lane = threadIdx.x & 31;
+  int stage = 0;
+  uint32_t phase = 0;
+  PageWindow win;
+  PromptPiece x;
+  do {
+    x = prompt_piece(p, cut, w);
+    if (x.t0 == x.t1) continue;
+    const int ll = p.by_heads.div(w.lh), h = w.lh - ll * p.g.N_kv;
+    const int pages = (x.n + 63) >> 6;
+    win.begin(p.table, w.b, x.t0 * (T::KT / 64), pages);
+    for (int t = x.t0; t < x.t1; ++t) {
+      int page[T::KT / 64];
+#pragma unroll
+      for (int i = 0; i < T::KT / 64; ++i) page[i] = win.at(p.table, p.g, w.b, t * (T::KT / 64) + i, pages, p.error);
+#pragma unroll
+      for (int part = 0; part < 2; ++part)
+#pragma unroll
+        for (int i = 0; i < T::KT / 64; ++i) {
+          if (!warp_wait(smem_u32(&sh.st_empty[stage]), phase ^ 1)) return false;
+          if (lane == 0) {
+            const uint32_t bar = smem_u32(&sh.st_full[stage]), dst = stage0 + stage * T::kStage;
+            sh.stage_there[stage] = page[i] >= 0;
+            bar_arrive_tx(bar, page[i] >= 0 ? kPageTokens * (T::RB + T::SB) : 0);
+            if (page[i] >= 0) {
+              const uint8_t* const block = p.pages + page_block_offset(p.g, p.layer0 + ll, page[i], h);
+              bulk_load(dst, block + part * kPageTokens * T::RB, kPageTokens * T::RB, bar);
+              bulk_load(dst + kPageTokens * T::RB, block + kPageTokens * (2 * T::RB + part * T::SB), kPageTokens * T::SB, bar);
+            }
+          }
+          __syncwarp();
+          if (++stage == T::kStages) {
+            stage = 0;
+            phase ^= 1;
+          }
+        }
+    }
+  } while (prompt_walk_next(p, cut, w, x.cost));
+  return true;
+}
+
+// ---- four warps unpack the stages into the ring
+// 64 stored rows at `from` to rows of the operand at `to` (of 64-channel blocks of KT rows).  A unit is 16 stored bytes: 16
+// channels of e4m3, 32 of 4 bits.  EDGE: rows from `n` on become 0, values of rows from `see` on finite; whether any was not.
+template <int D, int FMT, bool EDGE>
+__device__ __forceinline__ bool unpack_rows(uint32_t from, uint32_t to, int n, int see) {
+  using T = Shape<D, FMT>;
+  constexpr int CH = T::kInt4 ? 32 : 16, PER_ROW = D / CH, UNITS = kPageTokens * PER_ROW / 128, PASS = 128 / PER_ROW;
+  static_assert(PASS % 8 == 0, "the swizzle of a lane's rows is the same");
+  const int tid = threadIdx.x & 127, c = tid % PER_ROW, r0 = tid / PER_ROW;
+  uint4 w16[UNITS];
+  uint32_t sb[UNITS];
+  const uint32_t src = from + r0 * T::RB + c * 16, ssrc = from + kPageTokens * T::RB + r0 * T::SB + (T::kInt4 ? 2 * c : 0);
+#pragma unroll
+  for (int u = 0; u < UNITS; ++u) {
+    w16[u] = ld_shared(src + u * PASS * T::RB);
+    sb[u] = T::kInt4 ? ld_shared16(ssrc + u * PASS * T::SB) : ld_shared8(ssrc + u * PASS * T::SB);
+  }
+  bool any = false;
+#pragma unroll
+  for (int u = 0; u < UNITS; ++u) {
+    const int row = r0 + u * PASS;
+    const uint32_t* const q = &w16[u].x;
+    if (EDGE && row >= n) {
+      w16[u] = T::kInt4 ? make_uint4(0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u) : make_uint4(0u, 0u, 0u, 0u);
+      sb[u] = 0;
+    }
+    if constexpr (T::kInt4) {
+      const uint32_t s2 = sb[u] | sb[u] << 16;
+      const int turn = (c >> 1) ^ ((r0 & 1) << 1);                   // neighbouring lanes store to different banks
+      const bool drop = EDGE && row >= see && (sb[u] & 0x7f80u) == 0x7f80u;
+      any |= drop;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int kk = k ^ turn;
+        const uint32_t word = kk & 2 ? (kk & 1 ? q[3] : q[2]) : (kk & 1 ? q[1] : q[0]);
+        uint4 hi, lo;
+        int4_to_bf16(word, s2, hi, lo);
+        if (drop) hi = lo = make_uint4(0u, 0u, 0u, 0u);
+        const uint32_t at = to + swz(T::KT, r0, 4 * c + kk) + u * PASS * 128;
+        st_shared(at, hi);
+        st_shared(at + T::kSlot, lo);
+      }
+    } else {
+      const float sc = e8m0(sb[u]);
+      uint4 v[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint2 a = e4m3_to_bf16(q[2 * k], sc), b = e4m3_to_bf16(q[2 * k + 1], sc);
+        v[k] = make_uint4(a.x, a.y, b.x, b.y);
+        if (EDGE && row >= see) any |= drop_non_finite(v[k]);
+      }
+      const bool turn = c >> 2 & 1;
+      st_shared(to + swz(T::KT, r0, 2 * c + turn) + u * PASS * 128, turn ? v[1] : v[0]);
+      st_shared(to + swz(T::KT, r0, 2 * c + !turn) + u * PASS * 128, turn ? v[0] : v[1]);
+    }
+  }
+  return any;
+}
+
+template <int D, int FMT>
+__device__ __forceinline__ bool unpack_role(const PagedPromptParams& p, PromptWalk w, Shared& sh, uint32_t ring0, uint32_t stage0) {
+  using T = Shape<D, FMT>;
+  constexpr PromptCut cut = T::cut();
+  const int tid = threadIdx.x & 127, lane = threadIdx.x & 31;
+  Ring r{0, 0};
+  int stage = 0, tile_no = 0, item_no = 0;
+  uint32_t phase = 0;
+  PromptPiece x;
+  do {
+    x = prompt_piece(p, cut, w);
+    if (x.t0 == x.t1) continue;
+    const int see = w.s.pos + x.s0 + 1;            // tokens that every row sees
+    for (int t = x.t0; t < x.t1; ++t, ++tile_no) {
+#pragma unroll 1
+      for (int part = 0; part < 2; ++part) {
+        const int slot0 = r.slot;
+#pragma unroll
+        for (int i = 0; i < T::PARTS; ++i) {                          // (parts of a tile never wrap)
+          if (!warp_wait(smem_u32(&sh.empty[r.slot]), r.phase ^ 1)) return false;
+          r.template next<T>();
+        }
+        uint32_t there = 0;
+        bool any = false;
+#pragma unroll 1
+        for (int i = 0; i < T::KT / 64; ++i) {
+          const int tok0 = t * T::KT + 64 * i;
+          if (!warp_wait(smem_u32(&sh.st_full[stage]), phase)) return false;
+          const uint32_t here = sh.stage_there[stage], from = stage0 + stage * T::kStage, to = ring0 + slot0 * T::kSlot + i * 64 * 128;
+          there |= here << i;
+          // rows that no row of queries sees become 0, values that only some see finite
+          if (!here || tok0 + 64 > (part ? see : x.n)) any |= unpack_rows<D, FMT, true>(from, to, here ? x.n - tok0 : 0, part ? see - tok0 : 64);
+          else unpack_rows<D, FMT, false>(from, to, 64, 64);
+          __syncwarp();
+          if (lane == 0) bar_arrive(smem_u32(&sh.st_empty[stage]));
+          if (++stage == T::kStages) {
+            stage = 0;
+            phase ^= 1;
+          }
+        }
+        if (part == 0 && tid == 0) {
+          sh.pages[tile_no & 7] = there;
+          if (t == x.t0) sh.bad[(item_no + 8) & 15] = 0;
+        }
+        if (any) sh.bad[item_no & 15] = 1;
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0)
+          for (int i = 0; i < T::PARTS; ++i) bar_arrive(smem_u32(&sh.full[slot0 + i]));
       }
     }
     ++item_no;
@@ -572,7 +683,7 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, PromptW
         for (int c = 0; c < D / 64; ++c) {
           uint4 v[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = on ? __ldg(src + c * 8 + i) : make_uint4(0u, 0u, 0u, 0u);
+          for (int i = 0; i < 8; ++i) v[i] = on ? int4_order(__ldg(src + c * 8 + i)) : make_uint4(0u, 0u, 0u, 0u);
           tmem_st32(tQ + c * 32, (const uint32_t*)v);
         }
         tmem_wait_st();
@@ -689,10 +800,17 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, PromptW
           const uint8_t* const block = p.pages + page_block_offset(p.g, p.layer0 + ll, page, h);
 #pragma unroll
           for (int j = 0; j < 32; ++j) {
-            const float v = value_at<D, FMT>(block, tok & 63, c + j);
+            const float v = value_at<D, FMT>(block, tok & 63, c + (T::kInt4 ? int4_channel(j) : j));
             if (!(fabsf(v) <= 3.4e38f)) o[j] = __float_as_uint(__uint_as_float(o[j]) + v);
           }
         }
+      }
+      if constexpr (T::kInt4) {              // back in the order of channels
+        uint32_t u[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) u[int4_channel(j)] = o[j];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) o[j] = u[j];
       }
       if (on && whole) {
 #pragma unroll
@@ -735,7 +853,7 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
   PromptWalk w;
   if (!prompt_walk_begin<T::kThreads>(p, cut, w, sh.scratch)) return;
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t q0 = base, ring0 = base + T::kQBytes;
+  const uint32_t q0 = base, ring0 = base + T::kQBytes, stage0 = ring0 + T::kSlots * T::kSlot;
   if (warp == T::kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_u32(&sh.tmem)), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -752,6 +870,10 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
       bar_init(smem_u32(&sh.q_full[i]), 4);
     }
     bar_init(smem_u32(&sh.raw), 1);
+    for (int i = 0; i < T::kStages; ++i) {
+      bar_init(smem_u32(&sh.st_full[i]), 1);
+      bar_init(smem_u32(&sh.st_empty[i]), T::kLoadWarps);
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     sh.failed = 0;
     for (int i = 0; i < 16; ++i) sh.bad[i] = 0;
@@ -768,7 +890,10 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
     if (T::kPlain || warp < 12) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(T::kLoadRegs));
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(T::kMmaRegs));
     if (warp < 8 + T::kLoadWarps) {
-      ok = load_role<D, FMT>(p, &map, w, sh, ring0);
+      if constexpr (T::kPlain) ok = load_role<D, FMT>(p, &map, w, sh, ring0);
+      else ok = unpack_role<D, FMT>(p, w, sh, ring0, stage0);
+    } else if (!T::kPlain && warp == T::kFetchWarp) {
+      ok = fetch_role<D, FMT>(p, w, sh, stage0);
     } else {
       if (tid == T::kMmaWarp * 32) ok = mma_role<D, FMT>(p, w, sh, q0, ring0, tmem);
       __syncwarp();
