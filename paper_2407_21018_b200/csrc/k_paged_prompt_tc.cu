@@ -5,9 +5,11 @@
 //   S = Q K^T       tcgen05.mma into tensor memory, a tile of KT tokens; thread t of a half's four warps owns row t
 //   P = 2^(x - m)   read from tensor memory, written back over S as bf16: the A operand of
 //   O += P V        tcgen05.mma, V as stored ([token][channel]) is the MN-major B operand
-// Roles: warps 0-3 and 4-7 the softmax of a half each, three or four more bring keys and values into a ring of shared-memory
-// slots (bf16 pages by TMA, others unpacked in registers), one thread of another issues all products.  m only moves when a row's
-// logits pass it by 2^8 (O is then rescaled in tensor memory), so the softmax seldom waits for the products.
+// Roles: warps 0-3 and 4-7 the softmax of a half each; three or four warps bring keys and values into a ring of shared-memory
+// slots (bf16 pages by TMA; others as bytes by bulk copies that one more warp issues, unpacked in registers); one thread issues
+// all products; four warps load the next item's queries and store the last item's outputs, so that the others go from item
+// to item without a pause.  m only moves when a row's logits pass it by 2^8 (O is then rescaled in tensor memory), so the
+// softmax seldom waits for the products.  Loops stay rolled: unrolled, the roles' code together missed the instruction cache.
 // 4-bit values n * s have 11 bits: they enter as the sum of two bf16, which is exact, at twice the products; their keys
 // and values need twice the room, so tiles are 64 tokens and Q is held in tensor memory too.
 // Every wait is bounded (about a second): on a time-out the CTA raises the error word, frees its tensor memory and leaves.
@@ -40,32 +42,38 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
   return y;
 }
-// shared-memory matrix descriptor, 128-byte swizzle
-__device__ __forceinline__ uint64_t umma_desc(uint32_t saddr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
-  return (uint64_t)((saddr >> 4) & 0x3fffu) | ((uint64_t)((lbo_bytes >> 4) & 0x3fffu) << 16) |
-         ((uint64_t)((sbo_bytes >> 4) & 0x3fffu) << 32) | (1ull << 46) | (2ull << 61);
-}
+// Shared-memory matrix descriptors, 128-byte swizzle, 8-row groups of 1024 bytes: the low word has the address and the leading
+// byte offset in 16-byte units, the high word is the same for all.
+__device__ __forceinline__ uint32_t desc_lo(uint32_t saddr, uint32_t lbo_bytes) { return (saddr >> 4) | (lbo_bytes >> 4) << 16; }
+constexpr uint32_t kDescHi = (1024u >> 4) | 1u << 14 | 2u << 29;
 // instruction descriptor: fp32 accumulate, bf16 x bf16, M = 128; B K-major or MN-major
 __host__ __device__ constexpr uint32_t idesc(int n, bool b_mn) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24);
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+// a, b: low words of descriptors
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t id, uint32_t accumulate) {
   asm volatile(
       "{\n\t"
       ".reg .pred p;\n\t"
+      ".reg .b64 da, db;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t"
+      "mov.b64 da, {%1, %6};\n\t"
+      "mov.b64 db, {%2, %6};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, {%5, %5, %5, %5}, p;\n\t"
       "}\n"
-      :: "r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate), "r"(0u) : "memory");
+      :: "r"(d), "r"(a), "r"(b), "r"(id), "r"(accumulate), "r"(0u), "r"(kDescHi) : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+// a: in tensor memory
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t id, uint32_t accumulate) {
   asm volatile(
       "{\n\t"
       ".reg .pred p;\n\t"
+      ".reg .b64 db;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t"
+      "mov.b64 db, {%2, %6};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, {%5, %5, %5, %5}, p;\n\t"
       "}\n"
-      :: "r"(d), "r"(a), "l"(b), "r"(id), "r"(accumulate), "r"(0u) : "memory");
+      :: "r"(d), "r"(a), "r"(b), "r"(id), "r"(accumulate), "r"(0u), "r"(kDescHi) : "memory");
 }
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
@@ -142,6 +150,24 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return *(const uint32_t*)&v;
 }
 
+constexpr int kMaxSlots = 12, kMaxStages = 8, kMaxSmem = 227 * 1024;
+
+struct Shared {
+  // full, empty: a slot holds operands, may be overwritten.  s_full, p_full: S of a half is there, P is.  o_full: the product
+  // with P has been added to O; o_empty: O has been read.  q_full, q_empty: the same of the queries.  stats_full: m and l.
+  uint64_t full[kMaxSlots], empty[kMaxSlots], s_full[2], p_full[2], o_full[2], o_empty[2], q_full[2], q_empty[2], stats_full[2], raw;
+  uint64_t st_full[kMaxStages], st_empty[kMaxStages];
+  uint32_t tmem, failed;
+  // The loads are at most kMaxSlots / 2 tiles, so as many items, and one ahead of what is still in use.
+  uint32_t pages[8];                     // of the tiles under way: bit i: the tile's i-th page is there
+  uint32_t bad[32];                      // of the items under way: a value that some rows do not see is a NaN or an infinity
+  uint32_t stage_there[kMaxStages];      // the stage holds a page's rows
+  union {
+    float stats[2][2][kHalf];            // of a half's rows: m, l as in a record
+    long long scratch[40];               // at the kernel's start
+  };
+};
+
 // ---- what depends on the format and the head dimension
 template <int D, int FMT>
 struct Shape {
@@ -154,32 +180,23 @@ struct Shape {
   static constexpr int RB = kPlain ? D * 2 : kInt4 ? D / 2 : D;       // bytes of a stored row
   static constexpr int SB = kPlain ? 0 : kInt4 ? D / 16 : 1;          // bytes of its scales
   // quantised pages: 64 stored rows and their scales a stage; two tiles' worth, or what there is room for
-  static constexpr int kStage = kPlain ? 0 : kPageTokens * RB + (kPageTokens * SB + 127) / 128 * 128;
+  static constexpr int kStage = kPlain ? 0 : kPageTokens * (RB + SB);
   static constexpr int kStages = kPlain ? 0 : kInt4 || D == 64 ? 8 : 4;
-  static constexpr int kFit = (229376 + 1536 - kQBytes - kStages * kStage) / kSlot;      // 227 KB less the barriers and what alignment may take
-  static constexpr int kSlots = kFit / PARTS * PARTS < 12 ? kFit / PARTS * PARTS : 12;
-  static constexpr int kSmem = kQBytes + kSlots * kSlot + kStages * kStage + 1024;
-  // roles: two halves' softmax, loads, products; with bf16 pages one warp of the loads' group issues the products
-  static constexpr int kThreads = kPlain ? 384 : 512;
-  static constexpr int kMmaWarp = kPlain ? 11 : 12, kFetchWarp = 13;
+  static constexpr int kFit = (kMaxSmem - (int)sizeof(Shared) - kQBytes - kStages * kStage) / kSlot;
+  static constexpr int kSlots = kFit / PARTS * PARTS < kMaxSlots ? kFit / PARTS * PARTS : kMaxSlots;
+  static constexpr int kStageAt = kQBytes + kSlots * kSlot, kSharedAt = kStageAt + kStages * kStage, kSmem = kSharedAt + (int)sizeof(Shared);
+  static_assert(kSharedAt % 16 == 0 && kSmem <= kMaxSmem && kSlots >= 4 * PARTS, "shared memory");
+  // warpgroups: two halves' softmax; loads (with bf16 pages their fourth warp issues the products); else products and
+  // fetching; rows
+  static constexpr int kGroups = kPlain ? 4 : 5, kThreads = 128 * kGroups;
+  static constexpr int kMmaWarp = kPlain ? 11 : 12, kFetchWarp = 13, kRowsWarp = kPlain ? 12 : 16;
   static constexpr int kLoadWarps = kPlain ? 3 : 4;
-  static constexpr int kRegs = kPlain ? 168 : 128;            // a thread at launch
-  static constexpr int kSoftmaxRegs = kPlain ? 200 : 176, kLoadRegs = kPlain ? 104 : 96, kMmaRegs = 64;
-  static_assert(2 * kSoftmaxRegs + kLoadRegs + (kPlain ? 0 : kMmaRegs) <= kRegs * kThreads / 128, "more registers than the block has: a wait without end");
+  static constexpr int kRegs = kPlain ? 128 : 96;             // a thread at launch
+  static constexpr int kSoftmaxRegs = kPlain ? 160 : 128, kLoadRegs = kPlain ? 88 : 80, kMmaRegs = 64, kRowsRegs = kPlain ? 104 : 80;
+  static_assert(2 * kSoftmaxRegs + kLoadRegs + (kPlain ? 0 : kMmaRegs) + kRowsRegs <= kRegs * kGroups, "more registers than the block has: a wait without end");
   // tensor memory: S of each half, Q, O of each half
   static constexpr int kColS = KT, kColQ = 2 * KT, kColO = 256;
   static __host__ __device__ constexpr PromptCut cut() { return PromptCut{KT, kExtra}; }
-};
-
-struct Shared {
-  uint64_t full[12], empty[12], s_full[2], p_full[2], o_full[2], q_full[2], raw, st_full[8], st_empty[8];
-  long long scratch[40];
-  uint32_t tmem;
-  // The loads are at most kSlots / (2 PARTS) + 1 <= 6 tiles, so as many items, ahead of the softmax.
-  uint32_t pages[8];           // of the tiles under way: bit i: the tile's i-th page is there
-  uint32_t bad[16];            // of the items under way: a value that some rows do not see is a NaN or an infinity
-  uint32_t stage_there[8];     // the stage holds a page's rows
-  uint32_t failed;
 };
 
 // byte offset of 16-byte chunk ck of row r in an operand of `rows` rows: 64-channel blocks of 128-byte rows, swizzled
@@ -357,7 +374,7 @@ __device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUte
         if (tid == 0) {
           if (part == 0) {
             sh.pages[tile_no & 7] = there;
-            if (t == x.t0) sh.bad[(item_no + 8) & 15] = 0;
+            if (t == x.t0) sh.bad[(item_no + 16) & 31] = 0;
           }
           const uint32_t bar = edge ? raw : full;
           bar_arrive_tx(bar, __popc(there) * 64 * D * 2);
@@ -388,7 +405,7 @@ __device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUte
               }
               st_shared(slot + swz(T::KT, i, ck), v);
             }
-            if (any) sh.bad[item_no & 15] = 1;
+            if (any) sh.bad[item_no & 31] = 1;
           }
           fence_proxy_async();
           __syncwarp();
@@ -551,9 +568,9 @@ __device__ __forceinline__ bool unpack_role(const PagedPromptParams& p, PromptWa
         }
         if (part == 0 && tid == 0) {
           sh.pages[tile_no & 7] = there;
-          if (t == x.t0) sh.bad[(item_no + 8) & 15] = 0;
+          if (t == x.t0) sh.bad[(item_no + 16) & 31] = 0;
         }
-        if (any) sh.bad[item_no & 15] = 1;
+        if (any) sh.bad[item_no & 31] = 1;
         fence_proxy_async();
         __syncwarp();
         if (lane == 0)
@@ -572,27 +589,32 @@ __device__ __forceinline__ bool mma_role(const PagedPromptParams& p, PromptWalk 
   constexpr PromptCut cut = T::cut();
   constexpr uint32_t kIdQK = idesc(T::KT, false), kIdPV = idesc(D, true);
   Ring kr{0, 0};                        // of the next key tile
-  uint32_t q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
-  const uint64_t dq[2] = {umma_desc(q0, 16, 1024), umma_desc(q0 + kHalf * D * 2, 16, 1024)};
-  auto step = [&](Ring& r, int n) { for (int i = 0; i < n; ++i) r.template next<T>(); };
+  uint32_t phases = 0;                  // bit h: p_full, 2 + h: q_full, 4 + h: o_empty
   auto wait_full = [&](Ring r) {
+#pragma unroll
     for (int i = 0; i < T::PARTS; ++i, r.template next<T>())
       if (!bar_wait(smem_u32(&sh.full[r.slot]), r.phase)) return false;
     return true;
   };
   auto release = [&](const Ring& r) {
+#pragma unroll
     for (int i = 0; i < T::PARTS; ++i) mma_commit(smem_u32(&sh.empty[r.slot + i]));
+  };
+  auto flip = [&](int bit) {            // the phase to wait for
+    const uint32_t x = phases >> bit & 1;
+    phases ^= 1u << bit;
+    return x;
   };
   auto qk = [&](int half, const Ring& r) {
     const uint32_t d = tmem + half * T::kColS;
 #pragma unroll
     for (int part = 0; part < T::PARTS; ++part) {
-      const uint64_t dk = umma_desc(ring0 + (r.slot + part) * T::kSlot, 16, 1024);
+      const uint32_t k = desc_lo(ring0 + (r.slot + part) * T::kSlot, 16), q = desc_lo(q0 + half * (kHalf * D * 2), 16);
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks) {
-        const uint64_t b = dk + (uint64_t)((ks >> 2) * (T::KT * 8) + (ks & 3) * 2);
+        const uint32_t b = k + (ks >> 2) * (T::KT * 8) + (ks & 3) * 2;
         if constexpr (T::kQTmem) mma_ts(d, tmem + T::kColQ + half * (D / 2) + ks * 8, b, kIdQK, part > 0 || ks > 0);
-        else mma_ss(d, dq[half] + (uint64_t)((ks >> 2) * (kHalf * 8) + (ks & 3) * 2), b, kIdQK, ks > 0);
+        else mma_ss(d, q + (ks >> 2) * (kHalf * 8) + (ks & 3) * 2, b, kIdQK, ks > 0);
       }
     }
     mma_commit(smem_u32(&sh.s_full[half]));
@@ -601,9 +623,9 @@ __device__ __forceinline__ bool mma_role(const PagedPromptParams& p, PromptWalk 
     const uint32_t a = tmem + half * T::kColS, d = tmem + T::kColO + half * D;
 #pragma unroll
     for (int part = 0; part < T::PARTS; ++part) {
-      const uint64_t dv = umma_desc(ring0 + (r.slot + part) * T::kSlot, T::KT * 128, 1024);
+      const uint32_t v = desc_lo(ring0 + (r.slot + part) * T::kSlot, T::KT * 128);
 #pragma unroll
-      for (int ks = 0; ks < T::KT / 16; ++ks) mma_ts(d, a + ks * 8, dv + (uint64_t)(ks * 128), kIdPV, !first || part > 0 || ks > 0);
+      for (int ks = 0; ks < T::KT / 16; ++ks) mma_ts(d, a + ks * 8, v + ks * 128, kIdPV, !first || part > 0 || ks > 0);
     }
     mma_commit(smem_u32(&sh.o_full[half]));
   };
@@ -613,36 +635,40 @@ __device__ __forceinline__ bool mma_role(const PagedPromptParams& p, PromptWalk 
     if (x.t0 == x.t1) continue;
     const Halves hv = halves_of<T>(p, w, x);
     if (!wait_full(kr)) return false;
-#pragma unroll
+#pragma unroll 1
     for (int half = 0; half < 2; ++half) {
-      if (x.t0 == hv.t1[half]) continue;
-      if (!bar_wait(smem_u32(&sh.q_full[half]), q_phase[half])) return false;
-      q_phase[half] ^= 1;
+      const int t1 = half ? hv.t1[1] : hv.t1[0];
+      if (x.t0 == t1) continue;
+      if (!bar_wait(smem_u32(&sh.q_full[half]), flip(2 + half))) return false;
       fence_after();
       qk(half, kr);
+      if (x.t0 + 1 == t1) mma_commit(smem_u32(&sh.q_empty[half]));
     }
     release(kr);
+#pragma unroll 1
     for (int t = x.t0; t < x.t1; ++t) {
       Ring vr = kr;
-      step(vr, T::PARTS);
-      kr = vr;
-      step(kr, T::PARTS);
-      if (!wait_full(vr)) return false;
-      const bool more = t + 1 < x.t1;
-      bool keys = false;
 #pragma unroll
+      for (int i = 0; i < T::PARTS; ++i) vr.template next<T>();
+      kr = vr;
+#pragma unroll
+      for (int i = 0; i < T::PARTS; ++i) kr.template next<T>();
+      const bool more = t + 1 < x.t1;
+      if (!wait_full(vr)) return false;
+      bool keys = false;
+#pragma unroll 1
       for (int half = 0; half < 2; ++half) {
-        if (t < hv.t1[half]) {
-          if (!bar_wait(smem_u32(&sh.p_full[half]), p_phase[half])) return false;
-          p_phase[half] ^= 1;
-          fence_after();
-          pv(half, vr, t == x.t0);
-        }
-        if (t + 1 < hv.t1[half]) {
-          if (!keys && !wait_full(kr)) return false;
-          keys = true;
-          qk(half, kr);
-        }
+        const int t1 = half ? hv.t1[1] : hv.t1[0];
+        if (t >= t1) continue;
+        if (t == x.t0 && !bar_wait(smem_u32(&sh.o_empty[half]), flip(4 + half) ^ 1)) return false;
+        if (!bar_wait(smem_u32(&sh.p_full[half]), flip(half))) return false;
+        fence_after();
+        pv(half, vr, t == x.t0);
+        if (t + 1 == t1) continue;
+        if (!keys && !wait_full(kr)) return false;
+        keys = true;
+        qk(half, kr);
+        if (t + 2 == t1) mma_commit(smem_u32(&sh.q_empty[half]));
       }
       release(vr);
       if (more) release(kr);
@@ -653,82 +679,64 @@ __device__ __forceinline__ bool mma_role(const PagedPromptParams& p, PromptWalk 
 
 // ---- warps 0-3, 4-7: the softmax of a half
 template <int D, int FMT>
-__device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, PromptWalk w, Shared& sh, uint32_t q0, uint32_t tmem) {
+__device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, PromptWalk w, Shared& sh, uint32_t tmem) {
   using T = Shape<D, FMT>;
   constexpr PromptCut cut = T::cut();
-  constexpr int KT = T::KT;
+  constexpr int KT = T::KT, C = 64;                    // columns at a time
   const int half = threadIdx.x >> 7, row = threadIdx.x & 127, lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 3;
   const uint32_t lanes = (uint32_t)(warp * 32) << 16;
-  const uint32_t tS = tmem + lanes + half * T::kColS, tO = tmem + lanes + T::kColO + half * D, tQ = tmem + lanes + T::kColQ + half * (D / 2);
+  const uint32_t tS = tmem + lanes + half * T::kColS, tO = tmem + lanes + T::kColO + half * D;
   const uint32_t s_full = smem_u32(&sh.s_full[half]), p_full = smem_u32(&sh.p_full[half]), o_full = smem_u32(&sh.o_full[half]);
-  const uint32_t q_full = smem_u32(&sh.q_full[half]);
-  uint32_t s_phase = 0, o_phase = 0;
-  int tile_no = 0, item_no = 0;
+  const int s = p.by_group.div(half * kHalf + row);    // token of the row in its item
+  const f32x2 scale2 = two(p.scale_log2, p.scale_log2);
+  uint32_t s_phase = 0, o_phase = 0, e_phase = 1;
+  int tile_no = 0;
   PromptPiece x;
   do {
     x = prompt_piece(p, cut, w);
     if (x.t0 == x.t1) continue;
     const Halves hv = halves_of<T>(p, w, x);
-    const int ll = p.by_heads.div(w.lh), h = w.lh - ll * p.g.N_kv;
     const int rows = half ? hv.rows[1] : hv.rows[0], see = half ? hv.see[1] : hv.see[0], t1 = half ? hv.t1[1] : hv.t1[0];
-    const int ri = half * kHalf + row, s = p.by_group.div(ri), head = h * p.G + ri - s * p.G;
-    const bool on = row < rows;
-
-    // ---- queries: a row each (the last product that read the former ones has been waited for)
-    if (t1 > x.t0) {
-      const uint4* src = (const uint4*)p.q.ptr;
-      if (on) src = (const uint4*)((const uint16_t*)p.q.ptr + prompt_row(p, p.q, w.b, w.s, x.s0 + s) + ll * p.q.sl + head * p.q.sn);
-      if constexpr (T::kQTmem) {
-#pragma unroll
-        for (int c = 0; c < D / 64; ++c) {
-          uint4 v[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = on ? int4_order(__ldg(src + c * 8 + i)) : make_uint4(0u, 0u, 0u, 0u);
-          tmem_st32(tQ + c * 32, (const uint32_t*)v);
-        }
-        tmem_wait_st();
-        fence_before();
-      } else {
-        const uint32_t dst = q0 + half * kHalf * D * 2;
-#pragma unroll
-        for (int ck = 0; ck < D / 8; ++ck) cp_async16(dst + swz(kHalf, row, ck), src + (on ? ck : 0), on ? 16 : 0);
-        cp_async_wait_all();
-        fence_proxy_async();
-      }
-      __syncwarp();
-      if (lane == 0) bar_arrive(q_full);
-    }
-    const int limit = on ? min(x.n, w.s.pos + x.s0 + s + 1) : 0;      // tokens that the row sees
-    float m = -INFINITY, l = 0.f, lc = 0.f;                           // lc: what the additions to l have lost
+    const int limit = row < rows ? min(x.n, w.s.pos + x.s0 + s + 1) : 0;      // tokens that the row sees
+    float m = -INFINITY, l = 0.f, lc = 0.f;            // lc: what the additions to l have lost
     bool seen = false;
-    const int tile0 = tile_no;
+#pragma unroll 1
     for (int t = x.t0; t < t1; ++t) {
       if (!warp_wait(s_full, s_phase)) return false;
       s_phase ^= 1;
       fence_after();
-      uint32_t sr[KT];
-#pragma unroll
-      for (int c = 0; c < KT; c += 32) tmem_ld32(tS + c, sr + c);
       const int tok0 = t * KT;
-      const uint32_t there = sh.pages[(tile0 + t - x.t0) & 7];
-      tmem_wait_ld();
-      seen |= ((there & 1) && limit > tok0) || ((there & 2) && limit > tok0 + 64);
-      if (tok0 + KT > see || there != (1u << (KT / 64)) - 1) {        // some tokens are not seen
-        const int last = limit - tok0;
+      const uint32_t there = sh.pages[(tile_no + t - x.t0) & 7];
+      const bool edge = tok0 + KT > see || there != (1u << (KT / 64)) - 1;    // some tokens are not seen
+      uint32_t sr[C];
+      auto load = [&](int c) {
 #pragma unroll
-        for (int j = 0; j < KT; ++j)
-          if (j >= last || !(there >> (j >> 6) & 1)) sr[j] = 0xff800000u;
-      }
+        for (int j = 0; j < C; j += 32) tmem_ld32(tS + c + j, sr + j);
+        tmem_wait_ld();
+        if (edge) {
+          const int last = there >> (c >> 6) & 1 ? limit - tok0 - c : 0;
+          seen |= last > 0;
+#pragma unroll
+          for (int j = 0; j < C; ++j)
+            if (j >= last) sr[j] = 0xff800000u;
+        }
+      };
+      // the first columns come last and stay: P takes their place
       float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+      for (int c = KT - C; c >= 0; c -= C) {
+        load(c);
 #pragma unroll
-      for (int j = 0; j < KT; j += 8)
+        for (int j = 0; j < C; j += 8)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) mx[i] = max3(mx[i], __uint_as_float(sr[j + 2 * i]), __uint_as_float(sr[j + 2 * i + 1]));
+          for (int i = 0; i < 4; ++i) mx[i] = max3(mx[i], __uint_as_float(sr[j + 2 * i]), __uint_as_float(sr[j + 2 * i + 1]));
+      }
+      if (!edge) seen = true;
       const float m_new = fmaxf(m, max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * p.scale_log2);
       if (__any_sync(0xffffffffu, m_new > m + 8.f)) {
         const float f = m == m_new ? 1.f : ex2(m - m_new);
         if (t > x.t0) {
-          if (!warp_wait(o_full, o_phase ^ 1)) return false;           // the product before this tile's
+          if (!warp_wait(o_full, o_phase ^ 1)) return false;          // the product before this tile's
           fence_after();
 #pragma unroll 1
           for (int c = 0; c < D; c += 32) {
@@ -746,14 +754,19 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, PromptW
         m = m_new;
       }
       const float ref = m == -INFINITY ? 0.f : -m;
-      float ls[4] = {0.f, 0.f, 0.f, 0.f};
+      const f32x2 ref2 = two(ref, ref);
+      f32x2 ls[2] = {0ull, 0ull};
+#pragma unroll 1
+      for (int c = 0; c < KT; c += C) {
+        if (c > 0) load(c);
+        uint32_t pk[C / 2];
 #pragma unroll
-      for (int c = 0; c < KT; c += 64) {
-        uint32_t pk[32];
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          const float a = ex2(fmaf(__uint_as_float(sr[c + 2 * j]), p.scale_log2, ref)), b = ex2(fmaf(__uint_as_float(sr[c + 2 * j + 1]), p.scale_log2, ref));
-          ls[j & 3] += a + b;
+        for (int j = 0; j < C / 2; ++j) {
+          float a, b;
+          split(fma2(two(__uint_as_float(sr[2 * j]), __uint_as_float(sr[2 * j + 1])), scale2, ref2), a, b);
+          a = ex2(a);
+          b = ex2(b);
+          ls[j & 1] = add2(ls[j & 1], two(a, b));
           pk[j] = pack_bf16(a, b);
         }
         tmem_st32(tS + c / 2, pk);
@@ -763,97 +776,200 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, PromptW
       __syncwarp();
       if (lane == 0) bar_arrive(p_full);
       o_phase ^= 1;
-      const float add = ((ls[0] + ls[1]) + (ls[2] + ls[3])) - lc, sum = l + add;
+      float a0, a1;
+      split(add2(ls[0], ls[1]), a0, a1);
+      const float add = (a0 + a1) - lc, sum = l + add;
       lc = (sum - l) - add;
       l = sum;
     }
     tile_no += x.t1 - x.t0;
-
-    // ---- outputs
-    const bool some = t1 > x.t0;
-    if (some) {
-      if (!warp_wait(o_full, o_phase ^ 1)) return false;
-      fence_after();
-    }
-    const bool whole = x.t0 == 0 && x.t1 == x.tiles;
-    const bool mend = sh.bad[item_no & 15] != 0;
-    const bool none = m == -INFINITY && !seen;
-    const float f = whole ? (none ? 0.f : 1.f / l) : 1.f;
-    float* const rec = (float*)p.records + (2 * blockIdx.x + (x.t0 == 0)) * prompt_record_floats(kItemRows, D);
-    uint16_t* dst = nullptr;
-    if (on && whole) dst = (uint16_t*)p.out.ptr + prompt_row(p, p.out, w.b, w.s, x.s0 + s) + ll * p.out.sl + head * p.out.sn;
-#pragma unroll 1
-    for (int c = 0; c < D; c += 32) {
-      uint32_t o[32];
-      if (some) {
-        tmem_ld32(tO + c, o);
-        tmem_wait_ld();
-      }
-      if (!some || none) {
-#pragma unroll
-        for (int j = 0; j < 32; ++j) o[j] = 0u;
-      }
-      if (mend && on) {                          // values that were left out because some rows do not see them
-        for (int tok = max(w.s.pos + x.s0 + 1, x.t0 * KT); tok < min(limit, t1 * KT); ++tok) {
-          const int page = tok >= 0 ? page_of(p.table, p.g, w.b, tok, p.error) : -1;
-          if (page < 0) continue;
-          const uint8_t* const block = p.pages + page_block_offset(p.g, p.layer0 + ll, page, h);
-#pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            const float v = value_at<D, FMT>(block, tok & 63, c + (T::kInt4 ? int4_channel(j) : j));
-            if (!(fabsf(v) <= 3.4e38f)) o[j] = __float_as_uint(__uint_as_float(o[j]) + v);
-          }
-        }
-      }
-      if constexpr (T::kInt4) {              // back in the order of channels
-        uint32_t u[32];
-#pragma unroll
-        for (int j = 0; j < 32; ++j) u[int4_channel(j)] = o[j];
-#pragma unroll
-        for (int j = 0; j < 32; ++j) o[j] = u[j];
-      }
-      if (on && whole) {
-#pragma unroll
-        for (int j = 0; j < 32; j += 8) {
-          uint32_t u[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) u[k] = none ? 0u : pack_bf16(__uint_as_float(o[j + 2 * k]) * f, __uint_as_float(o[j + 2 * k + 1]) * f);
-          *(uint4*)(dst + c + j) = make_uint4(u[0], u[1], u[2], u[3]);
-        }
-      } else if (on) {
-#pragma unroll
-        for (int j = 0; j < 32; j += 4) *(uint4*)(rec + (size_t)ri * D + c + j) = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
-      }
+    if (t1 > x.t0) {
+      if (!warp_wait(smem_u32(&sh.o_empty[half]), e_phase)) return false;     // the last item's have been read
+      e_phase ^= 1;
+      sh.stats[half][0][row] = m;
+      sh.stats[half][1][row] = m == -INFINITY && l == 0.f ? (seen ? 1.f : 0.f) : l;
       __syncwarp();
+      if (lane == 0) bar_arrive(smem_u32(&sh.stats_full[half]));
     }
-    if (on) {
-      if (!whole) {
-        rec[kItemRows * D + ri] = m;
-        rec[kItemRows * (D + 1) + ri] = m == -INFINITY && l == 0.f ? (seen ? 1.f : 0.f) : l;
-      } else if (p.lse) {
-        p.lse[(prompt_lse_row(p, w.b, w.s, x.s0 + s) * p.nlayers + ll) * p.N_q + head] = prompt_log_sum(m, l);
-      }
-    }
-    fence_before();
-    if (!whole && x.t0 == 0 && threadIdx.x == 0) p.desc[blockIdx.x] = prompt_desc(cut, w, x);
-    ++item_no;
   } while (prompt_walk_next(p, cut, w, x.cost));
   return true;
+}
+
+// ---- four warps: the next item's queries, the last item's outputs
+template <int D, int FMT>
+__device__ __forceinline__ bool rows_role(const PagedPromptParams& p, PromptWalk w, Shared& sh, uint32_t q0, uint32_t tmem) {
+  using T = Shape<D, FMT>;
+  constexpr PromptCut cut = T::cut();
+  constexpr int KT = T::KT;
+  const int row = threadIdx.x & 127, lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 3;
+  const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
+  uint32_t phases = 0;                  // bit h: q_empty, 2 + h: stats_full; 4 + h: of o_full behind the item's last product
+  int item_no = 0;
+  auto skip = [&](PromptWalk& a, PromptPiece& x) {     // to the next item that has tiles here
+    do {
+      x = prompt_piece(p, cut, a);
+      if (x.t0 != x.t1) return true;
+    } while (prompt_walk_next(p, cut, a, x.cost));
+    return false;
+  };
+  auto queries = [&](const PromptWalk& a, const PromptPiece& x) {
+    const Halves hv = halves_of<T>(p, a, x);
+    const int ll = p.by_heads.div(a.lh), h = a.lh - ll * p.g.N_kv;
+#pragma unroll 1
+    for (int half = 0; half < 2; ++half) {
+      if (x.t0 == (half ? hv.t1[1] : hv.t1[0])) continue;
+      if (!warp_wait(smem_u32(&sh.q_empty[half]), (phases >> half & 1) ^ 1)) return false;
+      phases ^= 1u << half;
+      fence_after();
+      const int rows = half ? hv.rows[1] : hv.rows[0], ri = half * kHalf;
+      if constexpr (T::kQTmem) {
+        const bool on = row < rows;
+        const int s = p.by_group.div(ri + row);
+        const uint4* src = (const uint4*)p.q.ptr;
+        if (on) src = (const uint4*)((const uint16_t*)p.q.ptr + prompt_row(p, p.q, a.b, a.s, x.s0 + s) + ll * p.q.sl + (h * p.G + ri + row - s * p.G) * p.q.sn);
+#pragma unroll 1
+        for (int c = 0; c < D / 64; ++c) {
+          uint4 v[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] = on ? int4_order(__ldg(src + c * 8 + i)) : make_uint4(0u, 0u, 0u, 0u);
+          tmem_st32(lanes + T::kColQ + half * (D / 2) + c * 32, (const uint32_t*)v);
+        }
+        tmem_wait_st();
+        fence_before();
+      } else {
+        // 16-byte pieces of a row in neighbouring lanes
+        constexpr int P = D / 8;
+        const uint32_t dst = q0 + half * kHalf * D * 2;
+#pragma unroll 4
+        for (int i = row; i < kHalf * P; i += 128) {
+          const int r = i / P, c = i % P, s = p.by_group.div(ri + r);
+          const bool on = r < rows;
+          const uint16_t* const src = (const uint16_t*)p.q.ptr + (on ? prompt_row(p, p.q, a.b, a.s, x.s0 + s) + ll * p.q.sl + (h * p.G + ri + r - s * p.G) * p.q.sn + c * 8 : 0);
+          cp_async16(dst + swz(kHalf, r, c), src, on ? 16 : 0);
+        }
+        cp_async_wait_all();
+        fence_proxy_async();
+      }
+      __syncwarp();
+      if (lane == 0) bar_arrive(smem_u32(&sh.q_full[half]));
+    }
+    return true;
+  };
+  PromptPiece x;
+  if (!skip(w, x)) return true;
+  if (!queries(w, x)) return false;
+  while (true) {
+    PromptWalk next = w;
+    PromptPiece nx;
+    const bool more = prompt_walk_next(p, cut, next, x.cost) && skip(next, nx);
+    if (more && !queries(next, nx)) return false;
+    const Halves hv = halves_of<T>(p, w, x);
+    const int ll = p.by_heads.div(w.lh), h = w.lh - ll * p.g.N_kv;
+    const bool whole = x.t0 == 0 && x.t1 == x.tiles;
+    float* const rec = (float*)p.records + (2 * blockIdx.x + (x.t0 == 0)) * prompt_record_floats(kItemRows, D);
+#pragma unroll 1
+    for (int half = 0; half < 2; ++half) {
+      const int t1 = half ? hv.t1[1] : hv.t1[0], rows = half ? hv.rows[1] : hv.rows[0];
+      const bool some = t1 > x.t0, on = row < rows;
+      float m = -INFINITY, l = 0.f;
+      if (some) {
+        phases ^= (uint32_t)((t1 - x.t0) & 1) << (4 + half);
+        if (!warp_wait(smem_u32(&sh.stats_full[half]), phases >> (2 + half) & 1)) return false;
+        phases ^= 4u << half;
+        m = sh.stats[half][0][row];
+        l = sh.stats[half][1][row];
+        if (!warp_wait(smem_u32(&sh.o_full[half]), (phases >> (4 + half) & 1) ^ 1)) return false;
+        fence_after();
+      }
+      const bool mend = sh.bad[item_no & 31] != 0;
+      const int ri = half * kHalf + row, s = p.by_group.div(ri), head = h * p.G + ri - s * p.G;
+      const bool none = m == -INFINITY && l == 0.f;
+      const float f = none ? 0.f : m == -INFINITY ? __int_as_float(0x7fffffff) : 1.f / l;
+      uint16_t* dst = nullptr;
+      if (on && whole) dst = (uint16_t*)p.out.ptr + prompt_row(p, p.out, w.b, w.s, x.s0 + s) + ll * p.out.sl + head * p.out.sn;
+#pragma unroll 1
+      for (int c = 0; c < D; c += 32) {
+        uint32_t o[32];
+        if (some) {
+          tmem_ld32(lanes + T::kColO + half * D + c, o);
+          tmem_wait_ld();
+          if (c + 32 == D) {            // the half's next product may overwrite it
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_u32(&sh.o_empty[half]));
+          }
+        }
+        if (!some || none) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) o[j] = 0u;
+        }
+        if (mend && on) {               // values that were left out because some rows do not see them
+          const int limit = min(x.n, w.s.pos + x.s0 + s + 1);
+          for (int tok = max(w.s.pos + x.s0 + 1, x.t0 * KT); tok < min(limit, t1 * KT); ++tok) {
+            const int page = tok >= 0 ? page_of(p.table, p.g, w.b, tok, p.error) : -1;
+            if (page < 0) continue;
+            const uint8_t* const block = p.pages + page_block_offset(p.g, p.layer0 + ll, page, h);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+              const float v = value_at<D, FMT>(block, tok & 63, c + (T::kInt4 ? int4_channel(j) : j));
+              if (!(fabsf(v) <= 3.4e38f)) o[j] = __float_as_uint(__uint_as_float(o[j]) + v);
+            }
+          }
+        }
+        if constexpr (T::kInt4) {       // back in the order of channels
+          uint32_t u[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) u[int4_channel(j)] = o[j];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) o[j] = u[j];
+        }
+        if (on && whole) {
+#pragma unroll
+          for (int j = 0; j < 32; j += 8) {
+            uint32_t u[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) u[k] = none ? 0u : pack_bf16(__uint_as_float(o[j + 2 * k]) * f, __uint_as_float(o[j + 2 * k + 1]) * f);
+            *(uint4*)(dst + c + j) = make_uint4(u[0], u[1], u[2], u[3]);
+          }
+        } else if (on) {
+#pragma unroll
+          for (int j = 0; j < 32; j += 4) *(uint4*)(rec + (size_t)ri * D + c + j) = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+        }
+        __syncwarp();
+      }
+      if (on) {
+        if (!whole) {
+          rec[kItemRows * D + ri] = m;
+          rec[kItemRows * (D + 1) + ri] = l;
+        } else if (p.lse) {
+          p.lse[(prompt_lse_row(p, w.b, w.s, x.s0 + s) * p.nlayers + ll) * p.N_q + head] = prompt_log_sum(m, l);
+        }
+      }
+    }
+    if (!whole && x.t0 == 0 && row == 0) p.desc[blockIdx.x] = prompt_desc(cut, w, x);
+    if (!more) return true;
+    w = next;
+    x = nx;
+    ++item_no;
+  }
 }
 
 template <int D, int FMT>
 __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(const __grid_constant__ PagedPromptParams p, const __grid_constant__ CUtensorMap map) {
   using T = Shape<D, FMT>;
   constexpr PromptCut cut = T::cut();
-  extern __shared__ unsigned char smem_raw[];
-  __shared__ __align__(16) Shared sh;
+  extern __shared__ __align__(1024) unsigned char smem[];       // nothing else is in shared memory: it starts on such a border
+  Shared& sh = *(Shared*)(smem + T::kSharedAt);
   begin_dependent();
   const int tid = threadIdx.x, warp = tid >> 5;
   if (tid == 0) p.desc[blockIdx.x].pieces = 0;
+  const uint32_t q0 = smem_u32(smem), ring0 = q0 + T::kQBytes, stage0 = q0 + T::kStageAt;
+  if (q0 & 1023) {
+    if (tid == 0) atomicOr(p.error, kErrSmemAlign);
+    return;
+  }
   PromptWalk w;
   if (!prompt_walk_begin<T::kThreads>(p, cut, w, sh.scratch)) return;
-  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t q0 = base, ring0 = base + T::kQBytes, stage0 = ring0 + T::kSlots * T::kSlot;
   if (warp == T::kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_u32(&sh.tmem)), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -867,7 +983,10 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
       bar_init(smem_u32(&sh.s_full[i]), 1);
       bar_init(smem_u32(&sh.p_full[i]), 4);
       bar_init(smem_u32(&sh.o_full[i]), 1);
+      bar_init(smem_u32(&sh.o_empty[i]), 4);
       bar_init(smem_u32(&sh.q_full[i]), 4);
+      bar_init(smem_u32(&sh.q_empty[i]), 1);
+      bar_init(smem_u32(&sh.stats_full[i]), 4);
     }
     bar_init(smem_u32(&sh.raw), 1);
     for (int i = 0; i < T::kStages; ++i) {
@@ -876,7 +995,7 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     sh.failed = 0;
-    for (int i = 0; i < 16; ++i) sh.bad[i] = 0;
+    for (int i = 0; i < 32; ++i) sh.bad[i] = 0;
   }
   fence_before();
   __syncthreads();
@@ -885,7 +1004,10 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
   bool ok = true;
   if (warp < 8) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(T::kSoftmaxRegs));
-    ok = softmax_role<D, FMT>(p, w, sh, q0, tmem);
+    ok = softmax_role<D, FMT>(p, w, sh, tmem);
+  } else if (warp >= T::kRowsWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(T::kRowsRegs));
+    ok = rows_role<D, FMT>(p, w, sh, q0, tmem);
   } else {
     if (T::kPlain || warp < 12) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(T::kLoadRegs));
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(T::kMmaRegs));
