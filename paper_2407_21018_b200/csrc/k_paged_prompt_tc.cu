@@ -50,33 +50,53 @@ constexpr uint32_t kDescHi = (1024u >> 4) | 1u << 14 | 2u << 29;
 __host__ __device__ constexpr uint32_t idesc(int n, bool b_mn) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24);
 }
-// a, b: low words of descriptors
-__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t id, uint32_t accumulate) {
+// The products' warp runs as one, so that operands stay in uniform registers; its leading lane issues.
+__device__ __forceinline__ uint32_t elect_lane() {
+  uint32_t x;
   asm volatile(
       "{\n\t"
       ".reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t"
+      "}\n"
+      : "=r"(x));
+  return x;
+}
+// a, b: low words of descriptors
+__device__ __forceinline__ void mma_ss(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t id, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t"
+      ".reg .pred p, l;\n\t"
       ".reg .b64 da, db;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
+      "setp.ne.b32 l, %7, 0;\n\t"
       "mov.b64 da, {%1, %6};\n\t"
       "mov.b64 db, {%2, %6};\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, {%5, %5, %5, %5}, p;\n\t"
+      "@l tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, {%5, %5, %5, %5}, p;\n\t"
       "}\n"
-      :: "r"(d), "r"(a), "r"(b), "r"(id), "r"(accumulate), "r"(0u), "r"(kDescHi) : "memory");
+      :: "r"(d), "r"(a), "r"(b), "r"(id), "r"(accumulate), "r"(0u), "r"(kDescHi), "r"(lead) : "memory");
 }
 // a: in tensor memory
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t id, uint32_t accumulate) {
+__device__ __forceinline__ void mma_ts(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t id, uint32_t accumulate) {
   asm volatile(
       "{\n\t"
-      ".reg .pred p;\n\t"
+      ".reg .pred p, l;\n\t"
       ".reg .b64 db;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
+      "setp.ne.b32 l, %7, 0;\n\t"
       "mov.b64 db, {%2, %6};\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, {%5, %5, %5, %5}, p;\n\t"
+      "@l tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, {%5, %5, %5, %5}, p;\n\t"
       "}\n"
-      :: "r"(d), "r"(a), "r"(b), "r"(id), "r"(accumulate), "r"(0u), "r"(kDescHi) : "memory");
+      :: "r"(d), "r"(a), "r"(b), "r"(id), "r"(accumulate), "r"(0u), "r"(kDescHi), "r"(lead) : "memory");
 }
-__device__ __forceinline__ void mma_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+__device__ __forceinline__ void mma_commit(uint32_t lead, uint32_t bar) {
+  asm volatile(
+      "{\n\t"
+      ".reg .pred l;\n\t"
+      "setp.ne.b32 l, %1, 0;\n\t"
+      "@l tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t"
+      "}\n"
+      :: "r"(bar), "r"(lead) : "memory");
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -96,6 +116,18 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
       "{\n\t"
       ".reg .pred p;\n\t"
       "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t"
+      "}\n"
+      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+// the same without giving up the processor for a while
+__device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t"
+      ".reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
       "selp.u32 %0, 1, 0, p;\n\t"
       "}\n"
       : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
@@ -153,9 +185,9 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 constexpr int kMaxSlots = 12, kMaxStages = 8, kMaxSmem = 227 * 1024;
 
 struct Shared {
-  // full, empty: a slot holds operands, may be overwritten.  s_full, p_full: S of a half is there, P is.  o_full: the product
-  // with P has been added to O; o_empty: O has been read.  q_full, q_empty: the same of the queries.  stats_full: m and l.
-  uint64_t full[kMaxSlots], empty[kMaxSlots], s_full[2], p_full[2], o_full[2], o_empty[2], q_full[2], q_empty[2], stats_full[2], raw;
+  // full, empty: a slot holds operands, may be overwritten.  s_full, p_full: S of a half is there, a part of P is.  o_full: a part's
+  // product has been added to O; o_done: the item's last; o_empty: O has been read.  q_full, q_empty: the same of the queries.  stats_full: m and l.
+  uint64_t full[kMaxSlots], empty[kMaxSlots], s_full[2], p_full[2][2], o_full[2], o_done[2], o_empty[2], q_full[2], q_empty[2], stats_full[2], raw;
   uint64_t st_full[kMaxStages], st_empty[kMaxStages];
   uint32_t tmem, failed;
   // The loads are at most kMaxSlots / 2 tiles, so as many items, and one ahead of what is still in use.
@@ -582,97 +614,115 @@ __device__ __forceinline__ bool unpack_role(const PagedPromptParams& p, PromptWa
   return true;
 }
 
-// ---- one thread: products
+// ---- one warp: products
+// A half's weights arrive 64 tokens at a time (a part), and whichever half has some is served.
 template <int D, int FMT>
 __device__ __forceinline__ bool mma_role(const PagedPromptParams& p, PromptWalk w, Shared& sh, uint32_t q0, uint32_t ring0, uint32_t tmem) {
   using T = Shape<D, FMT>;
   constexpr PromptCut cut = T::cut();
   constexpr uint32_t kIdQK = idesc(T::KT, false), kIdPV = idesc(D, true);
-  Ring kr{0, 0};                        // of the next key tile
-  uint32_t phases = 0;                  // bit h: p_full, 2 + h: q_full, 4 + h: o_empty
-  auto wait_full = [&](Ring r) {
-#pragma unroll
-    for (int i = 0; i < T::PARTS; ++i, r.template next<T>())
-      if (!bar_wait(smem_u32(&sh.full[r.slot]), r.phase)) return false;
-    return true;
-  };
-  auto release = [&](const Ring& r) {
-#pragma unroll
-    for (int i = 0; i < T::PARTS; ++i) mma_commit(smem_u32(&sh.empty[r.slot + i]));
-  };
+  constexpr int SUB = T::KT / 64;
+  const uint32_t lead = elect_lane();
+  auto uniform = [](int v) { return __shfl_sync(0xffffffffu, v, 0); };
+  q0 = uniform(q0);
+  ring0 = uniform(ring0);
+  tmem = uniform(tmem);
+  uint32_t phases = 0;                  // bit h: q_full, 2 + h: o_empty, 4 + 2 h + s: p_full
+  uint32_t tile_no = 0;                 // tiles in front of the item: the keys of its tile i are operand 2 (tile_no + i) of the ring
   auto flip = [&](int bit) {            // the phase to wait for
     const uint32_t x = phases >> bit & 1;
     phases ^= 1u << bit;
     return x;
   };
-  auto qk = [&](int half, const Ring& r) {
-    const uint32_t d = tmem + half * T::kColS;
+  auto ring = [&](uint32_t operand) {
+    const uint32_t i = operand * T::PARTS;
+    return Ring{(int)(i % T::kSlots), i / T::kSlots & 1};
+  };
+  auto wait_full = [&](uint32_t operand) {
+    const Ring r = ring(operand);       // (the parts of an operand never wrap)
+#pragma unroll
+    for (int i = 0; i < T::PARTS; ++i)
+      if (!warp_wait(smem_u32(&sh.full[r.slot + i]), r.phase)) return false;
+    return true;
+  };
+  auto release = [&](uint32_t operand) {
+    const Ring r = ring(operand);
+#pragma unroll
+    for (int i = 0; i < T::PARTS; ++i) mma_commit(lead, smem_u32(&sh.empty[r.slot + i]));
+  };
+  auto qk = [&](int half, uint32_t operand, bool last) {
+    const uint32_t d = tmem + half * T::kColS, slot = ring0 + ring(operand).slot * T::kSlot;
 #pragma unroll
     for (int part = 0; part < T::PARTS; ++part) {
-      const uint32_t k = desc_lo(ring0 + (r.slot + part) * T::kSlot, 16), q = desc_lo(q0 + half * (kHalf * D * 2), 16);
+      const uint32_t k = desc_lo(slot + part * T::kSlot, 16), q = desc_lo(q0 + half * (kHalf * D * 2), 16);
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks) {
         const uint32_t b = k + (ks >> 2) * (T::KT * 8) + (ks & 3) * 2;
-        if constexpr (T::kQTmem) mma_ts(d, tmem + T::kColQ + half * (D / 2) + ks * 8, b, kIdQK, part > 0 || ks > 0);
-        else mma_ss(d, q + (ks >> 2) * (kHalf * 8) + (ks & 3) * 2, b, kIdQK, ks > 0);
+        if constexpr (T::kQTmem) mma_ts(lead, d, tmem + T::kColQ + half * (D / 2) + ks * 8, b, kIdQK, part > 0 || ks > 0);
+        else mma_ss(lead, d, q + (ks >> 2) * (kHalf * 8) + (ks & 3) * 2, b, kIdQK, ks > 0);
       }
     }
-    mma_commit(smem_u32(&sh.s_full[half]));
+    mma_commit(lead, smem_u32(&sh.s_full[half]));
+    if (last) mma_commit(lead, smem_u32(&sh.q_empty[half]));
   };
-  auto pv = [&](int half, const Ring& r, bool first) {
-    const uint32_t a = tmem + half * T::kColS, d = tmem + T::kColO + half * D;
+  auto pv = [&](int half, uint32_t operand, int sub, bool first) {
+    const uint32_t a = tmem + half * T::kColS + sub * 64, d = tmem + T::kColO + half * D, slot = ring0 + ring(operand).slot * T::kSlot;
 #pragma unroll
     for (int part = 0; part < T::PARTS; ++part) {
-      const uint32_t v = desc_lo(ring0 + (r.slot + part) * T::kSlot, T::KT * 128);
+      const uint32_t v = desc_lo(slot + part * T::kSlot, T::KT * 128) + sub * 512;
 #pragma unroll
-      for (int ks = 0; ks < T::KT / 16; ++ks) mma_ts(d, a + ks * 8, v + ks * 128, kIdPV, !first || part > 0 || ks > 0);
+      for (int ks = 0; ks < 4; ++ks) mma_ts(lead, d, a + ks * 8, v + ks * 128, kIdPV, !first || part > 0 || ks > 0);
     }
-    mma_commit(smem_u32(&sh.o_full[half]));
+    mma_commit(lead, smem_u32(&sh.o_full[half]));
   };
   PromptPiece x;
   do {
     x = prompt_piece(p, cut, w);
     if (x.t0 == x.t1) continue;
     const Halves hv = halves_of<T>(p, w, x);
-    if (!wait_full(kr)) return false;
-#pragma unroll 1
+    const int t0 = uniform(x.t0), tiles = uniform(x.t1) - t0;
+    const int end[2] = {(uniform(hv.t1[0]) - t0) * SUB, (uniform(hv.t1[1]) - t0) * SUB};      // parts of each half
+    if (!wait_full(2 * tile_no)) return false;
+#pragma unroll
     for (int half = 0; half < 2; ++half) {
-      const int t1 = half ? hv.t1[1] : hv.t1[0];
-      if (x.t0 == t1) continue;
-      if (!bar_wait(smem_u32(&sh.q_full[half]), flip(2 + half))) return false;
+      if (end[half] == 0) continue;
+      if (!warp_wait(smem_u32(&sh.q_full[half]), flip(half))) return false;
       fence_after();
-      qk(half, kr);
-      if (x.t0 + 1 == t1) mma_commit(smem_u32(&sh.q_empty[half]));
+      qk(half, 2 * tile_no, end[half] == SUB);
     }
-    release(kr);
-#pragma unroll 1
-    for (int t = x.t0; t < x.t1; ++t) {
-      Ring vr = kr;
+    release(2 * tile_no);
+    int at[2] = {0, 0};                                 // the next part of each half
+    int polls = 0;
+    while (at[0] < end[0] || at[1] < end[1]) {
 #pragma unroll
-      for (int i = 0; i < T::PARTS; ++i) vr.template next<T>();
-      kr = vr;
-#pragma unroll
-      for (int i = 0; i < T::PARTS; ++i) kr.template next<T>();
-      const bool more = t + 1 < x.t1;
-      if (!wait_full(vr)) return false;
-      bool keys = false;
-#pragma unroll 1
       for (int half = 0; half < 2; ++half) {
-        const int t1 = half ? hv.t1[1] : hv.t1[0];
-        if (t >= t1) continue;
-        if (t == x.t0 && !bar_wait(smem_u32(&sh.o_empty[half]), flip(4 + half) ^ 1)) return false;
-        if (!bar_wait(smem_u32(&sh.p_full[half]), flip(half))) return false;
+        if (at[half] >= end[half]) continue;
+        const int i = at[half] / SUB, sub = at[half] % SUB;
+        // no half is more than a tile ahead: the operands that it would wait for come when the other one has used its own
+        if (sub == 0 && at[half ^ 1] < end[half ^ 1] && at[half] > at[half ^ 1] + SUB) continue;
+        if (!__all_sync(0xffffffffu, bar_test(smem_u32(&sh.p_full[half][sub]), phases >> (4 + 2 * half + sub) & 1))) continue;
+        phases ^= 16u << (2 * half + sub);
+        const bool first = at[half] == 0;
+        if (first && !warp_wait(smem_u32(&sh.o_empty[half]), flip(2 + half) ^ 1)) return false;
+        if (sub == 0 && !wait_full(2 * (tile_no + i) + 1)) return false;
         fence_after();
-        pv(half, vr, t == x.t0);
-        if (t + 1 == t1) continue;
-        if (!keys && !wait_full(kr)) return false;
-        keys = true;
-        qk(half, kr);
-        if (t + 2 == t1) mma_commit(smem_u32(&sh.q_empty[half]));
+        pv(half, 2 * (tile_no + i) + 1, sub, first);
+        ++at[half];
+        if (at[half] == end[half]) mma_commit(lead, smem_u32(&sh.o_done[half]));
+        if (sub == SUB - 1) {
+          // the other half is through with the values, or does not need them
+          if (at[half ^ 1] >= at[half] || at[half] > end[half ^ 1]) release(2 * (tile_no + i) + 1);
+          if (at[half] < end[half]) {
+            if (!wait_full(2 * (tile_no + i + 1))) return false;
+            qk(half, 2 * (tile_no + i + 1), at[half] + SUB >= end[half]);
+            if (at[half ^ 1] >= at[half] || at[half] >= end[half ^ 1]) release(2 * (tile_no + i + 1));
+          }
+        }
+        polls = 0;
       }
-      release(vr);
-      if (more) release(kr);
+      if (++polls > 1 << 25) return false;              // a second at least
     }
+    tile_no += tiles;
   } while (prompt_walk_next(p, cut, w, x.cost));
   return true;
 }
@@ -686,7 +736,7 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, PromptW
   const int half = threadIdx.x >> 7, row = threadIdx.x & 127, lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 3;
   const uint32_t lanes = (uint32_t)(warp * 32) << 16;
   const uint32_t tS = tmem + lanes + half * T::kColS, tO = tmem + lanes + T::kColO + half * D;
-  const uint32_t s_full = smem_u32(&sh.s_full[half]), p_full = smem_u32(&sh.p_full[half]), o_full = smem_u32(&sh.o_full[half]);
+  const uint32_t s_full = smem_u32(&sh.s_full[half]), p_full = smem_u32(&sh.p_full[half][0]), o_full = smem_u32(&sh.o_full[half]);
   const int s = p.by_group.div(half * kHalf + row);    // token of the row in its item
   const f32x2 scale2 = two(p.scale_log2, p.scale_log2);
   uint32_t s_phase = 0, o_phase = 0, e_phase = 1;
@@ -701,53 +751,47 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, PromptW
     float m = -INFINITY, l = 0.f, lc = 0.f;            // lc: what the additions to l have lost
     bool seen = false;
 #pragma unroll 1
-    for (int t = x.t0; t < t1; ++t) {
-      if (!warp_wait(s_full, s_phase)) return false;
-      s_phase ^= 1;
-      fence_after();
-      const int tok0 = t * KT;
-      const uint32_t there = sh.pages[(tile_no + t - x.t0) & 7];
-      const bool edge = tok0 + KT > see || there != (1u << (KT / 64)) - 1;    // some tokens are not seen
-      uint32_t sr[C];
-      auto load = [&](int c) {
-#pragma unroll
-        for (int j = 0; j < C; j += 32) tmem_ld32(tS + c + j, sr + j);
-        tmem_wait_ld();
-        if (edge) {
-          const int last = there >> (c >> 6) & 1 ? limit - tok0 - c : 0;
-          seen |= last > 0;
-#pragma unroll
-          for (int j = 0; j < C; ++j)
-            if (j >= last) sr[j] = 0xff800000u;
-        }
-      };
-      // the first columns come last and stay: P takes their place
-      float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll 1
-      for (int c = KT - C; c >= 0; c -= C) {
-        load(c);
-#pragma unroll
-        for (int j = 0; j < C; j += 8)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) mx[i] = max3(mx[i], __uint_as_float(sr[j + 2 * i]), __uint_as_float(sr[j + 2 * i + 1]));
+    for (int c = x.t0 * KT; c < t1 * KT; c += C) {      // parts of 64 tokens
+      if (KT == C || c % KT == 0) {
+        if (!warp_wait(s_full, s_phase)) return false;
+        s_phase ^= 1;
+        fence_after();
       }
-      if (!edge) seen = true;
+      const uint32_t tP = tS + (KT == C ? 0 : c % KT);
+      uint32_t sr[C];
+#pragma unroll
+      for (int j = 0; j < C; j += 32) tmem_ld32(tP + j, sr + j);
+      const bool here = sh.pages[(tile_no + c / KT - x.t0) & 7] >> (c % KT / 64) & 1;
+      tmem_wait_ld();
+      if (c + C > see || !here) {                       // some tokens are not seen
+        const int last = here ? limit - c : 0;
+        seen |= last > 0;
+#pragma unroll
+        for (int j = 0; j < C; ++j)
+          if (j >= last) sr[j] = 0xff800000u;
+      } else {
+        seen = true;
+      }
+      float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+      for (int j = 0; j < C; j += 8)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mx[i] = max3(mx[i], __uint_as_float(sr[j + 2 * i]), __uint_as_float(sr[j + 2 * i + 1]));
       const float m_new = fmaxf(m, max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * p.scale_log2);
       if (__any_sync(0xffffffffu, m_new > m + 8.f)) {
         const float f = m == m_new ? 1.f : ex2(m - m_new);
-        if (t > x.t0) {
-          if (!warp_wait(o_full, o_phase ^ 1)) return false;          // the product before this tile's
+        if (c > x.t0 * KT) {
+          if (!warp_wait(o_full, o_phase ^ 1)) return false;          // the product before this part's
           fence_after();
 #pragma unroll 1
-          for (int c = 0; c < D; c += 32) {
+          for (int k = 0; k < D; k += 32) {
             uint32_t o[32];
-            tmem_ld32(tO + c, o);
+            tmem_ld32(tO + k, o);
             tmem_wait_ld();
 #pragma unroll
             for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-            tmem_st32(tO + c, o);
+            tmem_st32(tO + k, o);
           }
-          tmem_wait_st();
         }
         l *= f;
         lc *= f;
@@ -756,25 +800,21 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, PromptW
       const float ref = m == -INFINITY ? 0.f : -m;
       const f32x2 ref2 = two(ref, ref);
       f32x2 ls[2] = {0ull, 0ull};
-#pragma unroll 1
-      for (int c = 0; c < KT; c += C) {
-        if (c > 0) load(c);
-        uint32_t pk[C / 2];
+      uint32_t pk[C / 2];
 #pragma unroll
-        for (int j = 0; j < C / 2; ++j) {
-          float a, b;
-          split(fma2(two(__uint_as_float(sr[2 * j]), __uint_as_float(sr[2 * j + 1])), scale2, ref2), a, b);
-          a = ex2(a);
-          b = ex2(b);
-          ls[j & 1] = add2(ls[j & 1], two(a, b));
-          pk[j] = pack_bf16(a, b);
-        }
-        tmem_st32(tS + c / 2, pk);
+      for (int j = 0; j < C / 2; ++j) {
+        float a, b;
+        split(fma2(two(__uint_as_float(sr[2 * j]), __uint_as_float(sr[2 * j + 1])), scale2, ref2), a, b);
+        a = ex2(a);
+        b = ex2(b);
+        ls[j & 1] = add2(ls[j & 1], two(a, b));
+        pk[j] = pack_bf16(a, b);
       }
+      tmem_st32(tP, pk);
       tmem_wait_st();
       fence_before();
       __syncwarp();
-      if (lane == 0) bar_arrive(p_full);
+      if (lane == 0) bar_arrive(p_full + (KT == C ? 0 : c % KT / 64 * 8));
       o_phase ^= 1;
       float a0, a1;
       split(add2(ls[0], ls[1]), a0, a1);
@@ -803,7 +843,7 @@ __device__ __forceinline__ bool rows_role(const PagedPromptParams& p, PromptWalk
   constexpr int KT = T::KT;
   const int row = threadIdx.x & 127, lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 3;
   const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
-  uint32_t phases = 0;                  // bit h: q_empty, 2 + h: stats_full; 4 + h: of o_full behind the item's last product
+  uint32_t phases = 0;                  // bit h: q_empty, 2 + h: stats_full, 4 + h: o_done
   int item_no = 0;
   auto skip = [&](PromptWalk& a, PromptPiece& x) {     // to the next item that has tiles here
     do {
@@ -873,12 +913,12 @@ __device__ __forceinline__ bool rows_role(const PagedPromptParams& p, PromptWalk
       const bool some = t1 > x.t0, on = row < rows;
       float m = -INFINITY, l = 0.f;
       if (some) {
-        phases ^= (uint32_t)((t1 - x.t0) & 1) << (4 + half);
         if (!warp_wait(smem_u32(&sh.stats_full[half]), phases >> (2 + half) & 1)) return false;
         phases ^= 4u << half;
         m = sh.stats[half][0][row];
         l = sh.stats[half][1][row];
-        if (!warp_wait(smem_u32(&sh.o_full[half]), (phases >> (4 + half) & 1) ^ 1)) return false;
+        if (!warp_wait(smem_u32(&sh.o_done[half]), phases >> (4 + half) & 1)) return false;
+        phases ^= 16u << half;
         fence_after();
       }
       const bool mend = sh.bad[item_no & 31] != 0;
@@ -981,8 +1021,10 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
     }
     for (int i = 0; i < 2; ++i) {
       bar_init(smem_u32(&sh.s_full[i]), 1);
-      bar_init(smem_u32(&sh.p_full[i]), 4);
+      bar_init(smem_u32(&sh.p_full[i][0]), 4);
+      bar_init(smem_u32(&sh.p_full[i][1]), 4);
       bar_init(smem_u32(&sh.o_full[i]), 1);
+      bar_init(smem_u32(&sh.o_done[i]), 1);
       bar_init(smem_u32(&sh.o_empty[i]), 4);
       bar_init(smem_u32(&sh.q_full[i]), 4);
       bar_init(smem_u32(&sh.q_empty[i]), 1);
@@ -1017,8 +1059,7 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
     } else if (!T::kPlain && warp == T::kFetchWarp) {
       ok = fetch_role<D, FMT>(p, w, sh, stage0);
     } else {
-      if (tid == T::kMmaWarp * 32) ok = mma_role<D, FMT>(p, w, sh, q0, ring0, tmem);
-      __syncwarp();
+      if (warp == T::kMmaWarp) ok = mma_role<D, FMT>(p, w, sh, q0, ring0, tmem);
     }
   }
   if (!ok) {
