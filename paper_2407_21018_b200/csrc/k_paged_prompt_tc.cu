@@ -107,8 +107,14 @@ __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
 __device__ __forceinline__ void bar_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory");
 }
-__device__ __forceinline__ void bar_arrive_tx(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
+__device__ __forceinline__ void bar_arrive_tx(uint32_t lead, uint32_t bar, uint32_t bytes) {
+  asm volatile(
+      "{\n\t"
+      ".reg .pred l;\n\t"
+      "setp.ne.b32 l, %2, 0;\n\t"
+      "@l mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t"
+      "}\n"
+      :: "r"(bar), "r"(bytes), "r"(lead) : "memory");
 }
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
   uint32_t ok;
@@ -143,14 +149,24 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
 }
 // the same for a whole warp, whose lanes agree on the answer
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, bar_wait(bar, parity)); }
-__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
-  asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-               :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+__device__ __forceinline__ void tma_load(uint32_t lead, uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile(
+      "{\n\t"
+      ".reg .pred l;\n\t"
+      "setp.ne.b32 l, %5, 0;\n\t"
+      "@l cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t"
+      "}\n"
+      :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar), "r"(lead) : "memory");
 }
 // contiguous bytes (a multiple of 16, both addresses too)
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-               :: "r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+__device__ __forceinline__ void bulk_load(uint32_t lead, uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile(
+      "{\n\t"
+      ".reg .pred l;\n\t"
+      "setp.ne.b32 l, %4, 0;\n\t"
+      "@l cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n\t"
+      "}\n"
+      :: "r"(dst), "l"(src), "r"(bytes), "r"(bar), "r"(lead) : "memory");
 }
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
   asm volatile(
@@ -187,11 +203,11 @@ constexpr int kMaxSlots = 12, kMaxStages = 8, kMaxSmem = 227 * 1024;
 struct Shared {
   // full, empty: a slot holds operands, may be overwritten.  s_full, p_full: S of a half is there, a part of P is.  o_full: a part's
   // product has been added to O; o_done: the item's last; o_empty: O has been read.  q_full, q_empty: the same of the queries.  stats_full: m and l.
-  uint64_t full[kMaxSlots], empty[kMaxSlots], s_full[2], p_full[2][2], o_full[2], o_done[2], o_empty[2], q_full[2], q_empty[2], stats_full[2], raw;
+  uint64_t full[kMaxSlots], empty[kMaxSlots], s_full[2], p_full[2][2], o_full[2], o_done[2], o_empty[2], q_full[2], q_empty[2], stats_full[2], raw[2];
   uint64_t st_full[kMaxStages], st_empty[kMaxStages];
   uint32_t tmem, failed;
   // The loads are at most kMaxSlots / 2 tiles, so as many items, and one ahead of what is still in use.
-  uint32_t pages[8];                     // of the tiles under way: bit i: the tile's i-th page is there
+  uint8_t pages[8][2];                   // of the tiles under way: the tile's pages are there
   uint32_t bad[32];                      // of the items under way: a value that some rows do not see is a NaN or an infinity
   uint32_t stage_there[kMaxStages];      // the stage holds a page's rows
   union {
@@ -212,7 +228,7 @@ struct Shape {
   static constexpr int RB = kPlain ? D * 2 : kInt4 ? D / 2 : D;       // bytes of a stored row
   static constexpr int SB = kPlain ? 0 : kInt4 ? D / 16 : 1;          // bytes of its scales
   // quantised pages: 64 stored rows and their scales a stage; two tiles' worth, or what there is room for
-  static constexpr int kStage = kPlain ? 0 : kPageTokens * (RB + SB);
+  static constexpr int kBlock = 2 * kPageTokens * (RB + SB), kStage = kPlain ? 0 : kBlock / 2;
   static constexpr int kStages = kPlain ? 0 : kInt4 || D == 64 ? 8 : 4;
   static constexpr int kFit = (kMaxSmem - (int)sizeof(Shared) - kQBytes - kStages * kStage) / kSlot;
   static constexpr int kSlots = kFit / PARTS * PARTS < kMaxSlots ? kFit / PARTS * PARTS : kMaxSlots;
@@ -222,7 +238,7 @@ struct Shape {
   // fetching; rows
   static constexpr int kGroups = kPlain ? 4 : 5, kThreads = 128 * kGroups;
   static constexpr int kMmaWarp = kPlain ? 11 : 12, kFetchWarp = 13, kRowsWarp = kPlain ? 12 : 16;
-  static constexpr int kLoadWarps = kPlain ? 3 : 4;
+  static constexpr int kLoadWarps = kPlain ? 2 : 4;
   static constexpr int kRegs = kPlain ? 128 : 96;             // a thread at launch
   static constexpr int kSoftmaxRegs = kPlain ? 160 : 128, kLoadRegs = kPlain ? 88 : 80, kMmaRegs = 64, kRowsRegs = kPlain ? 104 : 80;
   static_assert(2 * kSoftmaxRegs + kLoadRegs + (kPlain ? 0 : kMmaRegs) + kRowsRegs <= kRegs * kGroups, "more registers than the block has: a wait without end");
@@ -344,42 +360,44 @@ struct Ring {                 // position in the ring of slots
   }
 };
 
-// Pages of a sequence's tiles, 32 at a time in the lanes of a warp, the next ones on their way.
+// The pool's blocks (of a layer and key head) that hold a sequence's pages, 32 at a time in the lanes of a warp, the next ones
+// on their way.
 struct PageWindow {
-  int32_t now, next;
+  int32_t now, next;          // block; -1: no page of the pool
   int first;                  // page of the sequence that lane 0 holds
-  __device__ __forceinline__ int32_t fetch(const PageTableView& t, int b, int first_page, int pages) const {
-    const int i = first_page + (threadIdx.x & 31);
-    return i < pages ? load_now(t.table + b * t.stride + i) : -1;
+  __device__ __forceinline__ int32_t fetch(const PagedPromptParams& p, const PromptWalk& w, int layer, int h, int at, int pages) const {
+    const int i = at + (threadIdx.x & 31);
+    if (i >= pages) return -1;
+    const int32_t page = load_now(p.table.table + w.b * p.table.stride + i);
+    if ((uint32_t)page >= (uint32_t)p.g.num_pages) {
+      atomicOr(p.error, kErrPage);
+      return -1;
+    }
+    return (layer * p.g.num_pages + page) * p.g.N_kv + h;          // fits 32 bits: a block has 4608 bytes at least
   }
-  __device__ __forceinline__ void begin(const PageTableView& t, int b, int page, int pages) {
+  __device__ __forceinline__ void begin(const PagedPromptParams& p, const PromptWalk& w, int layer, int h, int page, int pages) {
     first = page;
-    now = fetch(t, b, first, pages);
-    next = fetch(t, b, first + 32, pages);
+    now = fetch(p, w, layer, h, first, pages);
+    next = fetch(p, w, layer, h, first + 32, pages);
   }
-  // page i of the sequence (i grows); -1 if there is none, error bit if the table holds no page of the pool
-  __device__ __forceinline__ int at(const PageTableView& t, const PageGeom& g, int b, int i, int pages, uint32_t* error) {
+  // of page i of the sequence (i grows)
+  __device__ __forceinline__ int at(const PagedPromptParams& p, const PromptWalk& w, int layer, int h, int i, int pages) {
     if (i - first >= 32) {
       first += 32;
       now = next;
-      next = fetch(t, b, first + 32, pages);
+      next = fetch(p, w, layer, h, first + 32, pages);
     }
-    const int page = __shfl_sync(0xffffffffu, now, i - first);
-    if (i >= pages) return -1;
-    if ((uint32_t)page >= (uint32_t)g.num_pages) {
-      if ((threadIdx.x & 31) == 0) atomicOr(error, kErrPage);
-      return -1;
-    }
-    return page;
+    return __shfl_sync(0xffffffffu, now, i - first);
   }
 };
 
-// ---- loads of bf16 pages: keys and values by TMA
+// ---- bf16 pages: two warps bring the first and the second page of every tile, keys and values, by TMA
 template <int D, int FMT>
-__device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUtensorMap* map, PromptWalk w, Shared& sh, uint32_t ring0) {
+__device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUtensorMap* map, PromptWalk w, Shared& sh, uint32_t ring0, int mine) {
   using T = Shape<D, FMT>;
   constexpr PromptCut cut = T::cut();
-  const int tid = threadIdx.x & 127, lane = threadIdx.x & 31;     // (of kLoadWarps warps)
+  const int lane = threadIdx.x & 31;
+  const uint32_t lead = elect_lane(), raw = smem_u32(&sh.raw[mine]);
   Ring r{0, 0};
   PageWindow win;
   uint32_t raw_phase = 0;
@@ -388,62 +406,51 @@ __device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUte
   do {
     x = prompt_piece(p, cut, w);
     if (x.t0 == x.t1) continue;
-    const int ll = p.by_heads.div(w.lh), h = w.lh - ll * p.g.N_kv;
+    const int ll = p.by_heads.div(w.lh), h = w.lh - ll * p.g.N_kv, layer = p.layer0 + ll;
     const int see = w.s.pos + x.s0 + 1;            // tokens that every row sees
     const int pages = (x.n + 63) >> 6;
-    win.begin(p.table, w.b, x.t0 * 2, pages);
+    win.begin(p, w, layer, h, x.t0 * 2, pages);
+#pragma unroll 1
     for (int t = x.t0; t < x.t1; ++t, ++tile_no) {
-      const int tok0 = t * T::KT;
-      int page[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) page[i] = win.at(p.table, p.g, w.b, t * 2 + i, pages, p.error);
-      const uint32_t there = (page[0] >= 0 ? 1u : 0u) | (page[1] >= 0 ? 2u : 0u);
+      const int block = win.at(p, w, layer, h, 2 * t + mine, pages), tok0 = (2 * t + mine) * 64;
+      const uint32_t bytes = block >= 0 ? 64 * D * 2 : 0;
 #pragma unroll
       for (int part = 0; part < 2; ++part) {
-        const bool edge = part == 1 && (tok0 + T::KT > see || there != 3u);     // some values must not be met
-        const uint32_t slot = ring0 + r.slot * T::kSlot, full = smem_u32(&sh.full[r.slot]), raw = smem_u32(&sh.raw);
+        const bool edge = part == 1 && (tok0 + 64 > see || block < 0);          // some values must not be met
+        const uint32_t to = ring0 + r.slot * T::kSlot + mine * 8192, full = smem_u32(&sh.full[r.slot]), bar = edge ? raw : full;
         if (!warp_wait(smem_u32(&sh.empty[r.slot]), r.phase ^ 1)) return false;
-        if (tid == 0) {
-          if (part == 0) {
-            sh.pages[tile_no & 7] = there;
-            if (t == x.t0) sh.bad[(item_no + 16) & 31] = 0;
-          }
-          const uint32_t bar = edge ? raw : full;
-          bar_arrive_tx(bar, __popc(there) * 64 * D * 2);
+        if (part == 0 && lane == 0) {
+          sh.pages[tile_no & 7][mine] = block >= 0;
+          if (t == x.t0 && mine == 0) sh.bad[(item_no + 16) & 31] = 0;
+        }
+        __syncwarp();
+        bar_arrive_tx(lead, bar, bytes);
+        if (block >= 0) {
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
-            if (page[i] >= 0) {
-              const int row = (int)((((int64_t)(p.layer0 + ll) * p.g.num_pages + page[i]) * p.g.N_kv + h) * 128) + part * 64;
-#pragma unroll
-              for (int c = 0; c < D / 64; ++c) tma_load(slot + c * T::KT * 128 + i * 8192, map, c * 64, row, bar);
-            }
+          for (int c = 0; c < D / 64; ++c) tma_load(lead, to + c * T::KT * 128, map, c * 64, block * 128 + part * 64, bar);
         }
         if (edge) {
-          __syncwarp();
           if (!warp_wait(raw, raw_phase)) return false;
           raw_phase ^= 1;
-          // thread = token: what is behind the last one or on no page becomes 0, what only some rows see finite
-          for (int i = tid; i < T::KT; i += 32 * T::kLoadWarps) {
-            const int tok = tok0 + i;
-            const bool off = tok >= x.n || !(there >> (i >> 6) & 1);
-            if (!off && tok < see) continue;
+          // what is behind the last token or on no page becomes 0, what only some rows see finite
+          for (int i = lane; i < 64; i += 32) {
+            const bool off = tok0 + i >= x.n || block < 0;
+            if (!off && tok0 + i < see) continue;
             bool any = false;
-#pragma unroll
+#pragma unroll 4
             for (int ck = 0; ck < D / 8; ++ck) {
               uint4 v = make_uint4(0u, 0u, 0u, 0u);
               if (!off) {
-                v = ld_shared(slot + swz(T::KT, i, ck));
+                v = ld_shared(to + swz(T::KT, i, ck));
                 any |= drop_non_finite(v);
               }
-              st_shared(slot + swz(T::KT, i, ck), v);
+              st_shared(to + swz(T::KT, i, ck), v);
             }
             if (any) sh.bad[item_no & 31] = 1;
           }
           fence_proxy_async();
           __syncwarp();
           if (lane == 0) bar_arrive(full);
-        } else if (tid != 0 && lane == 0) {
-          bar_arrive(full);
         }
         r.template next<T>();
       }
@@ -453,47 +460,46 @@ __device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUte
   return true;
 }
 
-// ---- quantised pages: one warp has their bytes copied to the stages, 64 rows and their scales each
+// ---- quantised pages: two warps, in turn, have their bytes copied to the stages, 64 rows and their scales each
 template <int D, int FMT>
-__device__ __forceinline__ bool fetch_role(const PagedPromptParams& p, PromptWalk w, Shared& sh, uint32_t stage0) {
+__device__ __forceinline__ bool fetch_role(const PagedPromptParams& p, PromptWalk w, Shared& sh, uint32_t stage0, int mine) {
   using T = Shape<D, FMT>;
   constexpr PromptCut cut = T::cut();
+  constexpr int PAGES = T::KT / 64;                // of a tile: the two warps share its pages, or else keys and values
   const int lane = threadIdx.x & 31;
-  int stage = 0;
+  const uint32_t lead = elect_lane();
+  int stage = mine;
   uint32_t phase = 0;
   PageWindow win;
   PromptPiece x;
   do {
     x = prompt_piece(p, cut, w);
     if (x.t0 == x.t1) continue;
-    const int ll = p.by_heads.div(w.lh), h = w.lh - ll * p.g.N_kv;
+    const int ll = p.by_heads.div(w.lh), h = w.lh - ll * p.g.N_kv, layer = p.layer0 + ll;
     const int pages = (x.n + 63) >> 6;
-    win.begin(p.table, w.b, x.t0 * (T::KT / 64), pages);
+    win.begin(p, w, layer, h, x.t0 * PAGES, pages);
+#pragma unroll 1
     for (int t = x.t0; t < x.t1; ++t) {
-      int page[T::KT / 64];
+      const int block = win.at(p, w, layer, h, t * PAGES + (PAGES > 1 ? mine : 0), pages);
+      const uint8_t* const src = p.pages + (int64_t)max(block, 0) * T::kBlock;
 #pragma unroll
-      for (int i = 0; i < T::KT / 64; ++i) page[i] = win.at(p.table, p.g, w.b, t * (T::KT / 64) + i, pages, p.error);
-#pragma unroll
-      for (int part = 0; part < 2; ++part)
-#pragma unroll
-        for (int i = 0; i < T::KT / 64; ++i) {
-          if (!warp_wait(smem_u32(&sh.st_empty[stage]), phase ^ 1)) return false;
-          if (lane == 0) {
-            const uint32_t bar = smem_u32(&sh.st_full[stage]), dst = stage0 + stage * T::kStage;
-            sh.stage_there[stage] = page[i] >= 0;
-            bar_arrive_tx(bar, page[i] >= 0 ? kPageTokens * (T::RB + T::SB) : 0);
-            if (page[i] >= 0) {
-              const uint8_t* const block = p.pages + page_block_offset(p.g, p.layer0 + ll, page[i], h);
-              bulk_load(dst, block + part * kPageTokens * T::RB, kPageTokens * T::RB, bar);
-              bulk_load(dst + kPageTokens * T::RB, block + kPageTokens * (2 * T::RB + part * T::SB), kPageTokens * T::SB, bar);
-            }
-          }
-          __syncwarp();
-          if (++stage == T::kStages) {
-            stage = 0;
-            phase ^= 1;
-          }
+      for (int i = 0; i < PAGES; ++i) {
+        const int part = PAGES > 1 ? i : mine;
+        if (!warp_wait(smem_u32(&sh.st_empty[stage]), phase ^ 1)) return false;
+        const uint32_t bar = smem_u32(&sh.st_full[stage]), dst = stage0 + stage * T::kStage;
+        if (lane == 0) sh.stage_there[stage] = block >= 0;
+        __syncwarp();
+        bar_arrive_tx(lead, bar, block >= 0 ? T::kStage : 0);
+        if (block >= 0) {
+          bulk_load(lead, dst, src + part * kPageTokens * T::RB, kPageTokens * T::RB, bar);
+          bulk_load(lead, dst + kPageTokens * T::RB, src + kPageTokens * (2 * T::RB + part * T::SB), kPageTokens * T::SB, bar);
         }
+        stage += 2;
+        if (stage >= T::kStages) {
+          stage -= T::kStages;
+          phase ^= 1;
+        }
+      }
     }
   } while (prompt_walk_next(p, cut, w, x.cost));
   return true;
@@ -587,7 +593,7 @@ __device__ __forceinline__ bool unpack_role(const PagedPromptParams& p, PromptWa
           const int tok0 = t * T::KT + 64 * i;
           if (!warp_wait(smem_u32(&sh.st_full[stage]), phase)) return false;
           const uint32_t here = sh.stage_there[stage], from = stage0 + stage * T::kStage, to = ring0 + slot0 * T::kSlot + i * 64 * 128;
-          there |= here << i;
+          there |= here << 8 * i;
           // rows that no row of queries sees become 0, values that only some see finite
           if (!here || tok0 + 64 > (part ? see : x.n)) any |= unpack_rows<D, FMT, true>(from, to, here ? x.n - tok0 : 0, part ? see - tok0 : 64);
           else unpack_rows<D, FMT, false>(from, to, 64, 64);
@@ -599,7 +605,7 @@ __device__ __forceinline__ bool unpack_role(const PagedPromptParams& p, PromptWa
           }
         }
         if (part == 0 && tid == 0) {
-          sh.pages[tile_no & 7] = there;
+          *(uint16_t*)sh.pages[tile_no & 7] = (uint16_t)there;
           if (t == x.t0) sh.bad[(item_no + 16) & 31] = 0;
         }
         if (any) sh.bad[item_no & 31] = 1;
@@ -761,7 +767,7 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, PromptW
       uint32_t sr[C];
 #pragma unroll
       for (int j = 0; j < C; j += 32) tmem_ld32(tP + j, sr + j);
-      const bool here = sh.pages[(tile_no + c / KT - x.t0) & 7] >> (c % KT / 64) & 1;
+      const bool here = sh.pages[(tile_no + c / KT - x.t0) & 7][c % KT / 64];
       tmem_wait_ld();
       if (c + C > see || !here) {                       // some tokens are not seen
         const int last = here ? limit - c : 0;
@@ -1030,7 +1036,8 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
       bar_init(smem_u32(&sh.q_empty[i]), 1);
       bar_init(smem_u32(&sh.stats_full[i]), 4);
     }
-    bar_init(smem_u32(&sh.raw), 1);
+    bar_init(smem_u32(&sh.raw[0]), 1);
+    bar_init(smem_u32(&sh.raw[1]), 1);
     for (int i = 0; i < T::kStages; ++i) {
       bar_init(smem_u32(&sh.st_full[i]), 1);
       bar_init(smem_u32(&sh.st_empty[i]), T::kLoadWarps);
@@ -1054,10 +1061,10 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
     if (T::kPlain || warp < 12) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(T::kLoadRegs));
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(T::kMmaRegs));
     if (warp < 8 + T::kLoadWarps) {
-      if constexpr (T::kPlain) ok = load_role<D, FMT>(p, &map, w, sh, ring0);
+      if constexpr (T::kPlain) ok = load_role<D, FMT>(p, &map, w, sh, ring0, warp - 8);
       else ok = unpack_role<D, FMT>(p, w, sh, ring0, stage0);
-    } else if (!T::kPlain && warp == T::kFetchWarp) {
-      ok = fetch_role<D, FMT>(p, w, sh, stage0);
+    } else if (!T::kPlain && warp >= T::kFetchWarp && warp < T::kFetchWarp + 2) {
+      ok = fetch_role<D, FMT>(p, w, sh, stage0, warp - T::kFetchWarp);
     } else {
       if (warp == T::kMmaWarp) ok = mma_role<D, FMT>(p, w, sh, q0, ring0, tmem);
     }
