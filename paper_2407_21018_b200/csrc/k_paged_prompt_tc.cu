@@ -127,18 +127,6 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
       : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
-// the same without giving up the processor for a while
-__device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t"
-      ".reg .pred p;\n\t"
-      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t"
-      "}\n"
-      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-  return ok != 0;
-}
 // bounded wait (about a second): false on time-out
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
   if (bar_try(bar, parity)) return true;
@@ -621,46 +609,50 @@ __device__ __forceinline__ bool unpack_role(const PagedPromptParams& p, PromptWa
 }
 
 // ---- one warp: products
-// A half's weights arrive 64 tokens at a time (a part), and whichever half has some is served.
+// The tensor cores' queue is short, so every cycle between two products of a half that is ready counts: positions in the ring
+// move by addition, and the halves come in a fixed order, which they soon keep by themselves.
 template <int D, int FMT>
 __device__ __forceinline__ bool mma_role(const PagedPromptParams& p, PromptWalk w, Shared& sh, uint32_t q0, uint32_t ring0, uint32_t tmem) {
   using T = Shape<D, FMT>;
   constexpr PromptCut cut = T::cut();
   constexpr uint32_t kIdQK = idesc(T::KT, false), kIdPV = idesc(D, true);
-  constexpr int SUB = T::KT / 64;
+  constexpr int SUB = T::KT / 64;       // parts in which the weights of a tile arrive
   const uint32_t lead = elect_lane();
   auto uniform = [](int v) { return __shfl_sync(0xffffffffu, v, 0); };
   q0 = uniform(q0);
   ring0 = uniform(ring0);
   tmem = uniform(tmem);
-  uint32_t phases = 0;                  // bit h: q_full, 2 + h: o_empty, 4 + 2 h + s: p_full
-  uint32_t tile_no = 0;                 // tiles in front of the item: the keys of its tile i are operand 2 (tile_no + i) of the ring
+  const uint32_t full = uniform(smem_u32(sh.full)), empty = uniform(smem_u32(sh.empty));
+  uint32_t phases = 0;                  // bit h: q_full, 2 + h: o_empty, 4 + h: p_full
+  Ring kr{0, 0};                        // of the next keys
   auto flip = [&](int bit) {            // the phase to wait for
     const uint32_t x = phases >> bit & 1;
     phases ^= 1u << bit;
     return x;
   };
-  auto ring = [&](uint32_t operand) {
-    const uint32_t i = operand * T::PARTS;
-    return Ring{(int)(i % T::kSlots), i / T::kSlots & 1};
+  auto advance = [&](Ring r) {
+    r.slot += T::PARTS;                 // (the parts of an operand never wrap)
+    if (r.slot >= T::kSlots) {
+      r.slot -= T::kSlots;
+      r.phase ^= 1;
+    }
+    return r;
   };
-  auto wait_full = [&](uint32_t operand) {
-    const Ring r = ring(operand);       // (the parts of an operand never wrap)
+  auto wait_full = [&](const Ring& r) {
 #pragma unroll
     for (int i = 0; i < T::PARTS; ++i)
-      if (!warp_wait(smem_u32(&sh.full[r.slot + i]), r.phase)) return false;
+      if (!warp_wait(full + (r.slot + i) * 8, r.phase)) return false;
     return true;
   };
-  auto release = [&](uint32_t operand) {
-    const Ring r = ring(operand);
+  auto release = [&](const Ring& r) {
 #pragma unroll
-    for (int i = 0; i < T::PARTS; ++i) mma_commit(lead, smem_u32(&sh.empty[r.slot + i]));
+    for (int i = 0; i < T::PARTS; ++i) mma_commit(lead, empty + (r.slot + i) * 8);
   };
-  auto qk = [&](int half, uint32_t operand, bool last) {
-    const uint32_t d = tmem + half * T::kColS, slot = ring0 + ring(operand).slot * T::kSlot;
+  auto qk = [&](int half, int slot, bool last) {
+    const uint32_t d = tmem + half * T::kColS, at = ring0 + slot * T::kSlot;
 #pragma unroll
     for (int part = 0; part < T::PARTS; ++part) {
-      const uint32_t k = desc_lo(slot + part * T::kSlot, 16), q = desc_lo(q0 + half * (kHalf * D * 2), 16);
+      const uint32_t k = desc_lo(at + part * T::kSlot, 16), q = desc_lo(q0 + half * (kHalf * D * 2), 16);
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks) {
         const uint32_t b = k + (ks >> 2) * (T::KT * 8) + (ks & 3) * 2;
@@ -671,13 +663,13 @@ __device__ __forceinline__ bool mma_role(const PagedPromptParams& p, PromptWalk 
     mma_commit(lead, smem_u32(&sh.s_full[half]));
     if (last) mma_commit(lead, smem_u32(&sh.q_empty[half]));
   };
-  auto pv = [&](int half, uint32_t operand, int sub, bool first) {
-    const uint32_t a = tmem + half * T::kColS + sub * 64, d = tmem + T::kColO + half * D, slot = ring0 + ring(operand).slot * T::kSlot;
+  auto pv = [&](int half, int slot, int sub, bool first) {
+    const uint32_t a = tmem + half * T::kColS + sub * 64, d = tmem + T::kColO + half * D, at = ring0 + slot * T::kSlot;
 #pragma unroll
     for (int part = 0; part < T::PARTS; ++part) {
-      const uint32_t v = desc_lo(slot + part * T::kSlot, T::KT * 128) + sub * 512;
+      const uint32_t v = desc_lo(at + part * T::kSlot, T::KT * 128) + sub * 512;
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) mma_ts(lead, d, a + ks * 8, v + ks * 128, kIdPV, !first || part > 0 || ks > 0);
+      for (int ks = 0; ks < 4; ++ks) mma_ts(lead, d, a + ks * 8, v + ks * 128, kIdPV, part > 0 || ks > 0 ? 1u : first ? 0u : 1u);
     }
     mma_commit(lead, smem_u32(&sh.o_full[half]));
   };
@@ -687,48 +679,47 @@ __device__ __forceinline__ bool mma_role(const PagedPromptParams& p, PromptWalk 
     if (x.t0 == x.t1) continue;
     const Halves hv = halves_of<T>(p, w, x);
     const int t0 = uniform(x.t0), tiles = uniform(x.t1) - t0;
-    const int end[2] = {(uniform(hv.t1[0]) - t0) * SUB, (uniform(hv.t1[1]) - t0) * SUB};      // parts of each half
-    if (!wait_full(2 * tile_no)) return false;
+    const int end[2] = {uniform(hv.t1[0]) - t0, uniform(hv.t1[1]) - t0};          // tiles of each half
+    if (!wait_full(kr)) return false;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       if (end[half] == 0) continue;
       if (!warp_wait(smem_u32(&sh.q_full[half]), flip(half))) return false;
       fence_after();
-      qk(half, 2 * tile_no, end[half] == SUB);
+      qk(half, kr.slot, end[half] == 1);
     }
-    release(2 * tile_no);
-    int at[2] = {0, 0};                                 // the next part of each half
-    int polls = 0;
-    while (at[0] < end[0] || at[1] < end[1]) {
+    release(kr);
+#pragma unroll 1
+    for (int i = 0; i < tiles; ++i) {
+      const Ring vr = advance(kr);
+      kr = advance(vr);
+      bool values = false, keys = false;
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        if (at[half] >= end[half]) continue;
-        const int i = at[half] / SUB, sub = at[half] % SUB;
-        // no half is more than a tile ahead: the operands that it would wait for come when the other one has used its own
-        if (sub == 0 && at[half ^ 1] < end[half ^ 1] && at[half] > at[half ^ 1] + SUB) continue;
-        if (!__all_sync(0xffffffffu, bar_test(smem_u32(&sh.p_full[half][sub]), phases >> (4 + 2 * half + sub) & 1))) continue;
-        phases ^= 16u << (2 * half + sub);
-        const bool first = at[half] == 0;
-        if (first && !warp_wait(smem_u32(&sh.o_empty[half]), flip(2 + half) ^ 1)) return false;
-        if (sub == 0 && !wait_full(2 * (tile_no + i) + 1)) return false;
-        fence_after();
-        pv(half, 2 * (tile_no + i) + 1, sub, first);
-        ++at[half];
-        if (at[half] == end[half]) mma_commit(lead, smem_u32(&sh.o_done[half]));
-        if (sub == SUB - 1) {
-          // the other half is through with the values, or does not need them
-          if (at[half ^ 1] >= at[half] || at[half] > end[half ^ 1]) release(2 * (tile_no + i) + 1);
-          if (at[half] < end[half]) {
-            if (!wait_full(2 * (tile_no + i + 1))) return false;
-            qk(half, 2 * (tile_no + i + 1), at[half] + SUB >= end[half]);
-            if (at[half ^ 1] >= at[half] || at[half] >= end[half ^ 1]) release(2 * (tile_no + i + 1));
+        if (i >= end[half]) continue;
+        const uint32_t phase = flip(4 + half);
+#pragma unroll
+        for (int sub = 0; sub < SUB; ++sub) {
+          if (!warp_wait(smem_u32(&sh.p_full[half][sub]), phase)) return false;
+          if (sub == 0) {
+            if (i == 0 && !warp_wait(smem_u32(&sh.o_empty[half]), flip(2 + half) ^ 1)) return false;
+            if (!values && !wait_full(vr)) return false;
+            values = true;
           }
+          fence_after();
+          pv(half, vr.slot, sub, i == 0 && sub == 0);
         }
-        polls = 0;
+        if (i + 1 == end[half]) {
+          mma_commit(lead, smem_u32(&sh.o_done[half]));
+          continue;
+        }
+        if (!keys && !wait_full(kr)) return false;
+        keys = true;
+        qk(half, kr.slot, i + 2 == end[half]);
       }
-      if (++polls > 1 << 25) return false;              // a second at least
+      release(vr);
+      if (i + 1 < tiles) release(kr);
     }
-    tile_no += tiles;
   } while (prompt_walk_next(p, cut, w, x.cost));
   return true;
 }
