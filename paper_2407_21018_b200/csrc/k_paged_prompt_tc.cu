@@ -222,10 +222,9 @@ struct Shape {
   static constexpr int kSlots = kFit / PARTS * PARTS < kMaxSlots ? kFit / PARTS * PARTS : kMaxSlots;
   static constexpr int kStageAt = kQBytes + kSlots * kSlot, kSharedAt = kStageAt + kStages * kStage, kSmem = kSharedAt + (int)sizeof(Shared);
   static_assert(kSharedAt % 16 == 0 && kSmem <= kMaxSmem && kSlots >= 4 * PARTS, "shared memory");
-  // warpgroups: two halves' softmax; loads (with bf16 pages their fourth warp issues the products); else products and
-  // fetching; rows
+  // warpgroups: two halves' softmax; bf16 pages: loads and products, else unpacking, then products and fetching; rows
   static constexpr int kGroups = kPlain ? 4 : 5, kThreads = 128 * kGroups;
-  static constexpr int kMmaWarp = kPlain ? 11 : 12, kFetchWarp = 13, kRowsWarp = kPlain ? 12 : 16;
+  static constexpr int kMmaWarp = kPlain ? 10 : 12, kFetchWarp = 14, kRowsWarp = kPlain ? 12 : 16;
   static constexpr int kLoadWarps = kPlain ? 2 : 4;
   static constexpr int kRegs = kPlain ? 128 : 96;             // a thread at launch
   static constexpr int kSoftmaxRegs = kPlain ? 160 : 128, kLoadRegs = kPlain ? 88 : 80, kMmaRegs = 64, kRowsRegs = kPlain ? 104 : 80;
@@ -608,117 +607,109 @@ __device__ __forceinline__ bool unpack_role(const PagedPromptParams& p, PromptWa
   return true;
 }
 
-// ---- one warp: products
-// The tensor cores' queue is short, so every cycle between two products of a half that is ready counts: positions in the ring
-// move by addition, and the halves come in a fixed order, which they soon keep by themselves.
+// ---- two warps: the products of a half each
+// The tensor cores' queue is short and a wait costs 140 cycles even where there is nothing to wait for: two warps fill each
+// other's gaps.
 template <int D, int FMT>
-__device__ __forceinline__ bool mma_role(const PagedPromptParams& p, PromptWalk w, Shared& sh, uint32_t q0, uint32_t ring0, uint32_t tmem) {
+__device__ __forceinline__ bool mma_role(const PagedPromptParams& p, PromptWalk w, Shared& sh, uint32_t q0, uint32_t ring0, uint32_t tmem, int half) {
   using T = Shape<D, FMT>;
   constexpr PromptCut cut = T::cut();
   constexpr uint32_t kIdQK = idesc(T::KT, false), kIdPV = idesc(D, true);
   constexpr int SUB = T::KT / 64;       // parts in which the weights of a tile arrive
   const uint32_t lead = elect_lane();
   auto uniform = [](int v) { return __shfl_sync(0xffffffffu, v, 0); };
-  q0 = uniform(q0);
+  half = uniform(half);
   ring0 = uniform(ring0);
   tmem = uniform(tmem);
+  q0 = uniform(q0) + half * (kHalf * D * 2);
   const uint32_t full = uniform(smem_u32(sh.full)), empty = uniform(smem_u32(sh.empty));
-  uint32_t phases = 0;                  // bit h: q_full, 2 + h: o_empty, 4 + h: p_full
-  Ring kr{0, 0};                        // of the next keys
-  auto flip = [&](int bit) {            // the phase to wait for
-    const uint32_t x = phases >> bit & 1;
-    phases ^= 1u << bit;
-    return x;
-  };
-  auto advance = [&](Ring r) {
-    r.slot += T::PARTS;                 // (the parts of an operand never wrap)
+  const uint32_t s_full = uniform(smem_u32(&sh.s_full[half])), p_full = uniform(smem_u32(&sh.p_full[half][0]));
+  const uint32_t o_full = uniform(smem_u32(&sh.o_full[half])), o_done = uniform(smem_u32(&sh.o_done[half]));
+  const uint32_t o_empty = uniform(smem_u32(&sh.o_empty[half])), q_full = uniform(smem_u32(&sh.q_full[half])), q_empty = uniform(smem_u32(&sh.q_empty[half]));
+  const uint32_t tS = tmem + half * T::kColS, tO = tmem + T::kColO + half * D, tQ = tmem + T::kColQ + half * (D / 2);
+  uint32_t p_phase = 0, q_phase = 0, e_phase = 1;
+  Ring r{0, 0};                         // of the next operand
+  auto advance = [&]() {                // (the parts of an operand never wrap)
+    r.slot += T::PARTS;
     if (r.slot >= T::kSlots) {
       r.slot -= T::kSlots;
       r.phase ^= 1;
     }
-    return r;
   };
-  auto wait_full = [&](const Ring& r) {
+  auto wait_full = [&]() {
 #pragma unroll
     for (int i = 0; i < T::PARTS; ++i)
       if (!warp_wait(full + (r.slot + i) * 8, r.phase)) return false;
     return true;
   };
-  auto release = [&](const Ring& r) {
+  // this half is through with the operand: behind its products, or where it has none, now
+  auto release = [&](bool used) {
 #pragma unroll
-    for (int i = 0; i < T::PARTS; ++i) mma_commit(lead, empty + (r.slot + i) * 8);
+    for (int i = 0; i < T::PARTS; ++i) {
+      if (used) mma_commit(lead, empty + (r.slot + i) * 8);
+      else if (lead) bar_arrive(empty + (r.slot + i) * 8);
+    }
+    advance();
   };
-  auto qk = [&](int half, int slot, bool last) {
-    const uint32_t d = tmem + half * T::kColS, at = ring0 + slot * T::kSlot;
+  auto qk = [&](bool last) {
 #pragma unroll
     for (int part = 0; part < T::PARTS; ++part) {
-      const uint32_t k = desc_lo(at + part * T::kSlot, 16), q = desc_lo(q0 + half * (kHalf * D * 2), 16);
+      const uint32_t k = desc_lo(ring0 + (r.slot + part) * T::kSlot, 16), q = desc_lo(q0, 16);
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks) {
         const uint32_t b = k + (ks >> 2) * (T::KT * 8) + (ks & 3) * 2;
-        if constexpr (T::kQTmem) mma_ts(lead, d, tmem + T::kColQ + half * (D / 2) + ks * 8, b, kIdQK, part > 0 || ks > 0);
-        else mma_ss(lead, d, q + (ks >> 2) * (kHalf * 8) + (ks & 3) * 2, b, kIdQK, ks > 0);
+        if constexpr (T::kQTmem) mma_ts(lead, tS, tQ + ks * 8, b, kIdQK, part > 0 || ks > 0);
+        else mma_ss(lead, tS, q + (ks >> 2) * (kHalf * 8) + (ks & 3) * 2, b, kIdQK, ks > 0);
       }
     }
-    mma_commit(lead, smem_u32(&sh.s_full[half]));
-    if (last) mma_commit(lead, smem_u32(&sh.q_empty[half]));
+    mma_commit(lead, s_full);
+    if (last) mma_commit(lead, q_empty);
   };
-  auto pv = [&](int half, int slot, int sub, bool first) {
-    const uint32_t a = tmem + half * T::kColS + sub * 64, d = tmem + T::kColO + half * D, at = ring0 + slot * T::kSlot;
+  auto pv = [&](int sub, uint32_t accumulate) {
 #pragma unroll
     for (int part = 0; part < T::PARTS; ++part) {
-      const uint32_t v = desc_lo(at + part * T::kSlot, T::KT * 128) + sub * 512;
+      const uint32_t v = desc_lo(ring0 + (r.slot + part) * T::kSlot, T::KT * 128) + sub * 512;
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) mma_ts(lead, d, a + ks * 8, v + ks * 128, kIdPV, part > 0 || ks > 0 ? 1u : first ? 0u : 1u);
+      for (int ks = 0; ks < 4; ++ks) mma_ts(lead, tO, tS + sub * 64 + ks * 8, v + ks * 128, kIdPV, part > 0 || ks > 0 ? 1u : accumulate);
     }
-    mma_commit(lead, smem_u32(&sh.o_full[half]));
+    mma_commit(lead, o_full);
   };
   PromptPiece x;
   do {
     x = prompt_piece(p, cut, w);
     if (x.t0 == x.t1) continue;
     const Halves hv = halves_of<T>(p, w, x);
-    const int t0 = uniform(x.t0), tiles = uniform(x.t1) - t0;
-    const int end[2] = {uniform(hv.t1[0]) - t0, uniform(hv.t1[1]) - t0};          // tiles of each half
-    if (!wait_full(kr)) return false;
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      if (end[half] == 0) continue;
-      if (!warp_wait(smem_u32(&sh.q_full[half]), flip(half))) return false;
+    const int t0 = uniform(x.t0), tiles = uniform(x.t1) - t0, n = uniform(half ? hv.t1[1] : hv.t1[0]) - t0;     // n: tiles of this half
+    if (!wait_full()) return false;
+    if (n > 0) {
+      if (!warp_wait(q_full, q_phase)) return false;
+      q_phase ^= 1;
       fence_after();
-      qk(half, kr.slot, end[half] == 1);
+      qk(n == 1);
     }
-    release(kr);
+    release(n > 0);
 #pragma unroll 1
     for (int i = 0; i < tiles; ++i) {
-      const Ring vr = advance(kr);
-      kr = advance(vr);
-      bool values = false, keys = false;
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        if (i >= end[half]) continue;
-        const uint32_t phase = flip(4 + half);
+      if (i == 0 && n > 0) {
+        if (!warp_wait(o_empty, e_phase)) return false;
+        e_phase ^= 1;
+      }
+      if (!wait_full()) return false;
+      if (i < n) {
 #pragma unroll
         for (int sub = 0; sub < SUB; ++sub) {
-          if (!warp_wait(smem_u32(&sh.p_full[half][sub]), phase)) return false;
-          if (sub == 0) {
-            if (i == 0 && !warp_wait(smem_u32(&sh.o_empty[half]), flip(2 + half) ^ 1)) return false;
-            if (!values && !wait_full(vr)) return false;
-            values = true;
-          }
+          if (!warp_wait(p_full + sub * 8, p_phase)) return false;
           fence_after();
-          pv(half, vr.slot, sub, i == 0 && sub == 0);
+          pv(sub, i | sub);
         }
-        if (i + 1 == end[half]) {
-          mma_commit(lead, smem_u32(&sh.o_done[half]));
-          continue;
-        }
-        if (!keys && !wait_full(kr)) return false;
-        keys = true;
-        qk(half, kr.slot, i + 2 == end[half]);
+        p_phase ^= 1;
+        if (i + 1 == n) mma_commit(lead, o_done);
       }
-      release(vr);
-      if (i + 1 < tiles) release(kr);
+      release(i < n);
+      if (i + 1 == tiles) break;
+      if (!wait_full()) return false;
+      if (i + 1 < n) qk(i + 2 == n);
+      release(i + 1 < n);
     }
   } while (prompt_walk_next(p, cut, w, x.cost));
   return true;
@@ -1014,7 +1005,7 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
   if (tid == 0) {
     for (int i = 0; i < T::kSlots; ++i) {
       bar_init(smem_u32(&sh.full[i]), T::kLoadWarps);
-      bar_init(smem_u32(&sh.empty[i]), 1);
+      bar_init(smem_u32(&sh.empty[i]), 2);
     }
     for (int i = 0; i < 2; ++i) {
       bar_init(smem_u32(&sh.s_full[i]), 1);
@@ -1057,7 +1048,7 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
     } else if (!T::kPlain && warp >= T::kFetchWarp && warp < T::kFetchWarp + 2) {
       ok = fetch_role<D, FMT>(p, w, sh, stage0, warp - T::kFetchWarp);
     } else {
-      if (warp == T::kMmaWarp) ok = mma_role<D, FMT>(p, w, sh, q0, ring0, tmem);
+      ok = mma_role<D, FMT>(p, w, sh, q0, ring0, tmem, warp - T::kMmaWarp);
     }
   }
   if (!ok) {
