@@ -186,18 +186,34 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return *(const uint32_t*)&v;
 }
 
-constexpr int kMaxSlots = 12, kMaxStages = 8, kMaxSmem = 227 * 1024;
+constexpr int kMaxSmem = 227 * 1024;
 
+// What of an item belongs to this CTA, worked out once, by the warp that is ahead of all others (the roles' own arithmetic
+// would be most of the kernel's instructions, and all of it is fetched for a single item).
+struct Item {
+  int last;                              // there is none: the roles leave
+  int layer, h, b;
+  int pos0;                              // position of the item's first new token
+  int n, see[2];                         // tokens that the last row sees, and the first row of each half
+  int t0, tiles, end[2];                 // first tile, tiles, and how many of them each half has
+  int rows[2];                           // of queries, of each half
+  int whole, first;                      // all of the item's tiles; its first tile
+  int64_t q_at, out_at, lse_at;          // of the first token and query head, in elements
+};
+constexpr int kItems = 4;                // handed out and not yet taken by all
+
+template <int SLOTS, int STAGES>
 struct Shared {
   // full, empty: a slot holds operands, may be overwritten.  s_full, p_full: S of a half is there, a part of P is.  o_full: a part's
   // product has been added to O; o_done: the item's last; o_empty: O has been read.  q_full, q_empty: the same of the queries.  stats_full: m and l.
-  uint64_t full[kMaxSlots], empty[kMaxSlots], s_full[2], p_full[2][2], o_full[2], o_done[2], o_empty[2], q_full[2], q_empty[2], stats_full[2], raw[2];
-  uint64_t st_full[kMaxStages], st_empty[kMaxStages];
+  uint64_t full[SLOTS], empty[SLOTS], s_full[2], p_full[2][2], o_full[2], o_done[2], o_empty[2], q_full[2], q_empty[2], stats_full[2], raw[2];
+  uint64_t st_full[STAGES], st_empty[STAGES], item_full[kItems], item_empty[kItems];
   uint32_t tmem, failed;
-  // The loads are at most kMaxSlots / 2 tiles, so as many items, and one ahead of what is still in use.
+  // The loads are at most 6 tiles ahead of what is in use, and kItems + 1 items ahead of the outputs.
   uint8_t pages[8][2];                   // of the tiles under way: the tile's pages are there
-  uint32_t bad[32];                      // of the items under way: a value that some rows do not see is a NaN or an infinity
-  uint32_t stage_there[kMaxStages];      // the stage holds a page's rows
+  uint8_t bad[4 * kItems];               // of the items under way: a value that some rows do not see is a NaN or an infinity
+  Item items[kItems];
+  uint8_t stage_there[STAGES];           // the stage holds a page's rows
   union {
     float stats[2][2][kHalf];            // of a half's rows: m, l as in a record
     long long scratch[40];               // at the kernel's start
@@ -217,11 +233,11 @@ struct Shape {
   static constexpr int SB = kPlain ? 0 : kInt4 ? D / 16 : 1;          // bytes of its scales
   // quantised pages: 64 stored rows and their scales a stage; two tiles' worth, or what there is room for
   static constexpr int kBlock = 2 * kPageTokens * (RB + SB), kStage = kPlain ? 0 : kBlock / 2;
-  static constexpr int kStages = kPlain ? 0 : kInt4 || D == 64 ? 8 : 4;
-  static constexpr int kFit = (kMaxSmem - (int)sizeof(Shared) - kQBytes - kStages * kStage) / kSlot;
-  static constexpr int kSlots = kFit / PARTS * PARTS < kMaxSlots ? kFit / PARTS * PARTS : kMaxSlots;
-  static constexpr int kStageAt = kQBytes + kSlots * kSlot, kSharedAt = kStageAt + kStages * kStage, kSmem = kSharedAt + (int)sizeof(Shared);
-  static_assert(kSharedAt % 16 == 0 && kSmem <= kMaxSmem && kSlots >= 4 * PARTS, "shared memory");
+  static constexpr int kStages = kPlain ? 2 : kInt4 || D == 64 ? 8 : 4;      // (of no bytes with bf16 pages)
+  static constexpr int kSlots = kPlain ? (D == 128 ? 5 : 12) : kInt4 ? (D == 128 ? 10 : 12) : (D == 128 ? 4 : 8);
+  using Sh = Shared<kSlots, kStages>;
+  static constexpr int kStageAt = kQBytes + kSlots * kSlot, kSharedAt = kStageAt + kStages * kStage, kSmem = kSharedAt + (int)sizeof(Sh);
+  static_assert(kSharedAt % 16 == 0 && kSmem <= kMaxSmem && kSlots % PARTS == 0 && kSlots >= 4 * PARTS, "shared memory");
   // warpgroups: two halves' softmax; bf16 pages: loads and products, else unpacking, then products and fetching; rows
   static constexpr int kGroups = kPlain ? 4 : 5, kThreads = 128 * kGroups;
   static constexpr int kMmaWarp = kPlain ? 10 : 12, kFetchWarp = 14, kRowsWarp = kPlain ? 12 : 16;
@@ -313,26 +329,73 @@ __device__ float value_at(const uint8_t* block, int slot, int c) {
   }
 }
 
-// Tiles of a half of a piece: those its rows see.
-struct Halves {
-  int rows[2];                // query rows
-  int see[2];                 // tokens that the half's first row sees
-  int t1[2];                  // end of its tiles
-};
 template <typename T>
-__device__ __forceinline__ Halves halves_of(const PagedPromptParams& p, const PromptWalk& w, const PromptPiece& x) {
-  Halves h;
-  const int rows = x.tokens * p.G;
+__device__ __forceinline__ void describe(const PagedPromptParams& p, const PromptWalk& w, const PromptPiece& x, Item& o) {
+  const int ll = p.by_heads.div(w.lh), h = w.lh - ll * p.g.N_kv, rows = x.tokens * p.G;
+  o.last = 0;
+  o.layer = p.layer0 + ll;
+  o.h = h;
+  o.b = w.b;
+  o.pos0 = w.s.pos + x.s0;
+  o.n = x.n;
+  o.t0 = x.t0;
+  o.tiles = x.t1 - x.t0;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    h.rows[i] = max(0, min(kHalf, rows - i * kHalf));
-    const int first = w.s.pos + x.s0 + (int)p.by_group.div(i * kHalf);
-    const int last = w.s.pos + x.s0 + (int)p.by_group.div(i * kHalf + max(h.rows[i], 1) - 1);
-    h.see[i] = first + 1;
-    const int n = max(0, min(x.n, last + 1));
-    h.t1[i] = h.rows[i] == 0 ? x.t0 : max(x.t0, min(x.t1, max(1, (n + T::KT - 1) / T::KT)));
+    const int r = max(0, min(kHalf, rows - i * kHalf));
+    const int first = o.pos0 + (int)p.by_group.div(i * kHalf), last = o.pos0 + (int)p.by_group.div(i * kHalf + max(r, 1) - 1);
+    const int n = max(0, min(x.n, last + 1));          // tokens that the half sees
+    o.rows[i] = r;
+    o.see[i] = first + 1;
+    o.end[i] = r == 0 ? 0 : max(0, min(x.t1, max(1, (n + T::KT - 1) / T::KT)) - x.t0);
   }
-  return h;
+  o.whole = x.t0 == 0 && x.t1 == x.tiles;
+  o.first = x.t0 == 0;
+  o.q_at = prompt_row(p, p.q, w.b, w.s, x.s0) + ll * p.q.sl + h * p.G * p.q.sn;
+  o.out_at = prompt_row(p, p.out, w.b, w.s, x.s0) + ll * p.out.sl + h * p.G * p.out.sn;
+  o.lse_at = (prompt_lse_row(p, w.b, w.s, x.s0) * p.nlayers + ll) * p.N_q + h * p.G;
+}
+
+// Items as the warp that walks along them hands them out, and as the others take them.
+struct Items {
+  int no;
+  __device__ __forceinline__ uint32_t phase() const { return no / kItems & 1; }
+  // The next item; false on a time-out.  Every lane has its own copy of what it uses before the place is given back.
+  template <typename Sh, typename F>
+  __device__ __forceinline__ bool take(Sh& sh, F copy) {
+    const int slot = no & (kItems - 1);
+    if (!warp_wait(smem_u32(&sh.item_full[slot]), phase())) return false;
+    copy(*(const Item*)&sh.items[slot]);
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) bar_arrive(smem_u32(&sh.item_empty[slot]));
+    return true;
+  }
+};
+// the walking warp: on to the next item that has tiles here, which is handed out; `more` is false behind the last
+template <typename T>
+__device__ __forceinline__ bool hand_out(const PagedPromptParams& p, PromptWalk& w, typename T::Sh& sh, int no, bool& more, int64_t& cost) {
+  constexpr PromptCut cut = T::cut();
+  PromptPiece x;
+  if (no > 0) more = prompt_walk_next(p, cut, w, cost);
+  while (more) {
+    x = prompt_piece(p, cut, w);
+    if (x.t0 != x.t1) break;
+    more = prompt_walk_next(p, cut, w, x.cost);
+  }
+  const int slot = no & (kItems - 1);
+  if (!warp_wait(smem_u32(&sh.item_empty[slot]), (no / kItems & 1) ^ 1)) return false;
+  if ((threadIdx.x & 31) == 0) {
+    if (more) {
+      describe<T>(p, w, x, sh.items[slot]);
+      if (x.t0 == 0 && x.t1 != x.tiles) p.desc[blockIdx.x] = prompt_desc(cut, w, x);
+    } else {
+      sh.items[slot].last = 1;
+    }
+    bar_arrive(smem_u32(&sh.item_full[slot]));
+  }
+  __syncwarp();
+  cost = x.cost;
+  return true;
 }
 
 struct Ring {                 // position in the ring of slots
@@ -352,27 +415,27 @@ struct Ring {                 // position in the ring of slots
 struct PageWindow {
   int32_t now, next;          // block; -1: no page of the pool
   int first;                  // page of the sequence that lane 0 holds
-  __device__ __forceinline__ int32_t fetch(const PagedPromptParams& p, const PromptWalk& w, int layer, int h, int at, int pages) const {
+  __device__ __forceinline__ int32_t fetch(const PagedPromptParams& p, int b, int layer, int h, int at, int pages) const {
     const int i = at + (threadIdx.x & 31);
     if (i >= pages) return -1;
-    const int32_t page = load_now(p.table.table + w.b * p.table.stride + i);
+    const int32_t page = load_now(p.table.table + b * p.table.stride + i);
     if ((uint32_t)page >= (uint32_t)p.g.num_pages) {
       atomicOr(p.error, kErrPage);
       return -1;
     }
     return (layer * p.g.num_pages + page) * p.g.N_kv + h;          // fits 32 bits: a block has 4608 bytes at least
   }
-  __device__ __forceinline__ void begin(const PagedPromptParams& p, const PromptWalk& w, int layer, int h, int page, int pages) {
+  __device__ __forceinline__ void begin(const PagedPromptParams& p, int b, int layer, int h, int page, int pages) {
     first = page;
-    now = fetch(p, w, layer, h, first, pages);
-    next = fetch(p, w, layer, h, first + 32, pages);
+    now = fetch(p, b, layer, h, first, pages);
+    next = fetch(p, b, layer, h, first + 32, pages);
   }
   // of page i of the sequence (i grows)
-  __device__ __forceinline__ int at(const PagedPromptParams& p, const PromptWalk& w, int layer, int h, int i, int pages) {
+  __device__ __forceinline__ int at(const PagedPromptParams& p, int b, int layer, int h, int i, int pages) {
     if (i - first >= 32) {
       first += 32;
       now = next;
-      next = fetch(p, w, layer, h, first + 32, pages);
+      next = fetch(p, b, layer, h, first + 32, pages);
     }
     return __shfl_sync(0xffffffffu, now, i - first);
   }
@@ -380,26 +443,27 @@ struct PageWindow {
 
 // ---- bf16 pages: two warps bring the first and the second page of every tile, keys and values, by TMA
 template <int D, int FMT>
-__device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUtensorMap* map, PromptWalk w, Shared& sh, uint32_t ring0, int mine) {
+__device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUtensorMap* map, PromptWalk w, typename Shape<D, FMT>::Sh& sh, uint32_t ring0, int mine) {
   using T = Shape<D, FMT>;
-  constexpr PromptCut cut = T::cut();
   const int lane = threadIdx.x & 31;
   const uint32_t lead = elect_lane(), raw = smem_u32(&sh.raw[mine]);
   Ring r{0, 0};
   PageWindow win;
   uint32_t raw_phase = 0;
-  int tile_no = 0, item_no = 0;
-  PromptPiece x;
-  do {
-    x = prompt_piece(p, cut, w);
-    if (x.t0 == x.t1) continue;
-    const int ll = p.by_heads.div(w.lh), h = w.lh - ll * p.g.N_kv, layer = p.layer0 + ll;
-    const int see = w.s.pos + x.s0 + 1;            // tokens that every row sees
-    const int pages = (x.n + 63) >> 6;
-    win.begin(p, w, layer, h, x.t0 * 2, pages);
+  int tile_no = 0;
+  Items items{0};
+  bool more = true;
+  int64_t cost = 0;
+  for (;; ++items.no) {
+    if (mine == 0 && !hand_out<T>(p, w, sh, items.no, more, cost)) return false;
+    int last, layer, h, b, n, see, t0, tiles;
+    if (!items.take(sh, [&](const Item& i) { last = i.last; layer = i.layer; h = i.h; b = i.b; n = i.n; see = i.see[0]; t0 = i.t0; tiles = i.tiles; })) return false;
+    if (last) return true;
+    const int pages = (n + 63) >> 6;
+    win.begin(p, b, layer, h, t0 * 2, pages);
 #pragma unroll 1
-    for (int t = x.t0; t < x.t1; ++t, ++tile_no) {
-      const int block = win.at(p, w, layer, h, 2 * t + mine, pages), tok0 = (2 * t + mine) * 64;
+    for (int t = t0; t < t0 + tiles; ++t, ++tile_no) {
+      const int block = win.at(p, b, layer, h, 2 * t + mine, pages), tok0 = (2 * t + mine) * 64;
       const uint32_t bytes = block >= 0 ? 64 * D * 2 : 0;
 #pragma unroll
       for (int part = 0; part < 2; ++part) {
@@ -408,7 +472,7 @@ __device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUte
         if (!warp_wait(smem_u32(&sh.empty[r.slot]), r.phase ^ 1)) return false;
         if (part == 0 && lane == 0) {
           sh.pages[tile_no & 7][mine] = block >= 0;
-          if (t == x.t0 && mine == 0) sh.bad[(item_no + 16) & 31] = 0;
+          if (t == t0 && mine == 0) sh.bad[(items.no + 2 * kItems) & (4 * kItems - 1)] = 0;
         }
         __syncwarp();
         bar_arrive_tx(lead, bar, bytes);
@@ -421,7 +485,7 @@ __device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUte
           raw_phase ^= 1;
           // what is behind the last token or on no page becomes 0, what only some rows see finite
           for (int i = lane; i < 64; i += 32) {
-            const bool off = tok0 + i >= x.n || block < 0;
+            const bool off = tok0 + i >= n || block < 0;
             if (!off && tok0 + i < see) continue;
             bool any = false;
 #pragma unroll 4
@@ -433,7 +497,7 @@ __device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUte
               }
               st_shared(to + swz(T::KT, i, ck), v);
             }
-            if (any) sh.bad[item_no & 31] = 1;
+            if (any) sh.bad[items.no & (4 * kItems - 1)] = 1;
           }
           fence_proxy_async();
           __syncwarp();
@@ -442,32 +506,32 @@ __device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUte
         r.template next<T>();
       }
     }
-    ++item_no;
-  } while (prompt_walk_next(p, cut, w, x.cost));
-  return true;
+  }
 }
 
 // ---- quantised pages: two warps, in turn, have their bytes copied to the stages, 64 rows and their scales each
 template <int D, int FMT>
-__device__ __forceinline__ bool fetch_role(const PagedPromptParams& p, PromptWalk w, Shared& sh, uint32_t stage0, int mine) {
+__device__ __forceinline__ bool fetch_role(const PagedPromptParams& p, PromptWalk w, typename Shape<D, FMT>::Sh& sh, uint32_t stage0, int mine) {
   using T = Shape<D, FMT>;
-  constexpr PromptCut cut = T::cut();
   constexpr int PAGES = T::KT / 64;                // of a tile: the two warps share its pages, or else keys and values
   const int lane = threadIdx.x & 31;
   const uint32_t lead = elect_lane();
   int stage = mine;
   uint32_t phase = 0;
   PageWindow win;
-  PromptPiece x;
-  do {
-    x = prompt_piece(p, cut, w);
-    if (x.t0 == x.t1) continue;
-    const int ll = p.by_heads.div(w.lh), h = w.lh - ll * p.g.N_kv, layer = p.layer0 + ll;
-    const int pages = (x.n + 63) >> 6;
-    win.begin(p, w, layer, h, x.t0 * PAGES, pages);
+  Items items{0};
+  bool more = true;
+  int64_t cost = 0;
+  for (;; ++items.no) {
+    if (mine == 0 && !hand_out<T>(p, w, sh, items.no, more, cost)) return false;
+    int last, layer, h, b, n, t0, tiles;
+    if (!items.take(sh, [&](const Item& i) { last = i.last; layer = i.layer; h = i.h; b = i.b; n = i.n; t0 = i.t0; tiles = i.tiles; })) return false;
+    if (last) return true;
+    const int pages = (n + 63) >> 6;
+    win.begin(p, b, layer, h, t0 * PAGES, pages);
 #pragma unroll 1
-    for (int t = x.t0; t < x.t1; ++t) {
-      const int block = win.at(p, w, layer, h, t * PAGES + (PAGES > 1 ? mine : 0), pages);
+    for (int t = t0; t < t0 + tiles; ++t) {
+      const int block = win.at(p, b, layer, h, t * PAGES + (PAGES > 1 ? mine : 0), pages);
       const uint8_t* const src = p.pages + (int64_t)max(block, 0) * T::kBlock;
 #pragma unroll
       for (int i = 0; i < PAGES; ++i) {
@@ -488,8 +552,7 @@ __device__ __forceinline__ bool fetch_role(const PagedPromptParams& p, PromptWal
         }
       }
     }
-  } while (prompt_walk_next(p, cut, w, x.cost));
-  return true;
+  }
 }
 
 // ---- four warps unpack the stages into the ring
@@ -552,19 +615,18 @@ __device__ __forceinline__ bool unpack_rows(uint32_t from, uint32_t to, int n, i
 }
 
 template <int D, int FMT>
-__device__ __forceinline__ bool unpack_role(const PagedPromptParams& p, PromptWalk w, Shared& sh, uint32_t ring0, uint32_t stage0) {
+__device__ __forceinline__ bool unpack_role(typename Shape<D, FMT>::Sh& sh, uint32_t ring0, uint32_t stage0) {
   using T = Shape<D, FMT>;
-  constexpr PromptCut cut = T::cut();
   const int tid = threadIdx.x & 127, lane = threadIdx.x & 31;
   Ring r{0, 0};
-  int stage = 0, tile_no = 0, item_no = 0;
+  int stage = 0, tile_no = 0;
   uint32_t phase = 0;
-  PromptPiece x;
-  do {
-    x = prompt_piece(p, cut, w);
-    if (x.t0 == x.t1) continue;
-    const int see = w.s.pos + x.s0 + 1;            // tokens that every row sees
-    for (int t = x.t0; t < x.t1; ++t, ++tile_no) {
+  Items items{0};
+  for (;; ++items.no) {
+    int last, n, see, t0, tiles;
+    if (!items.take(sh, [&](const Item& i) { last = i.last; n = i.n; see = i.see[0]; t0 = i.t0; tiles = i.tiles; })) return false;
+    if (last) return true;
+    for (int t = t0; t < t0 + tiles; ++t, ++tile_no) {
 #pragma unroll 1
       for (int part = 0; part < 2; ++part) {
         const int slot0 = r.slot;
@@ -582,7 +644,7 @@ __device__ __forceinline__ bool unpack_role(const PagedPromptParams& p, PromptWa
           const uint32_t here = sh.stage_there[stage], from = stage0 + stage * T::kStage, to = ring0 + slot0 * T::kSlot + i * 64 * 128;
           there |= here << 8 * i;
           // rows that no row of queries sees become 0, values that only some see finite
-          if (!here || tok0 + 64 > (part ? see : x.n)) any |= unpack_rows<D, FMT, true>(from, to, here ? x.n - tok0 : 0, part ? see - tok0 : 64);
+          if (!here || tok0 + 64 > (part ? see : n)) any |= unpack_rows<D, FMT, true>(from, to, here ? n - tok0 : 0, part ? see - tok0 : 64);
           else unpack_rows<D, FMT, false>(from, to, 64, 64);
           __syncwarp();
           if (lane == 0) bar_arrive(smem_u32(&sh.st_empty[stage]));
@@ -593,27 +655,24 @@ __device__ __forceinline__ bool unpack_role(const PagedPromptParams& p, PromptWa
         }
         if (part == 0 && tid == 0) {
           *(uint16_t*)sh.pages[tile_no & 7] = (uint16_t)there;
-          if (t == x.t0) sh.bad[(item_no + 16) & 31] = 0;
+          if (t == t0) sh.bad[(items.no + 2 * kItems) & (4 * kItems - 1)] = 0;
         }
-        if (any) sh.bad[item_no & 31] = 1;
+        if (any) sh.bad[items.no & (4 * kItems - 1)] = 1;
         fence_proxy_async();
         __syncwarp();
         if (lane == 0)
           for (int i = 0; i < T::PARTS; ++i) bar_arrive(smem_u32(&sh.full[slot0 + i]));
       }
     }
-    ++item_no;
-  } while (prompt_walk_next(p, cut, w, x.cost));
-  return true;
+  }
 }
 
 // ---- two warps: the products of a half each
 // The tensor cores' queue is short and a wait costs 140 cycles even where there is nothing to wait for: two warps fill each
 // other's gaps.
 template <int D, int FMT>
-__device__ __forceinline__ bool mma_role(const PagedPromptParams& p, PromptWalk w, Shared& sh, uint32_t q0, uint32_t ring0, uint32_t tmem, int half) {
+__device__ __forceinline__ bool mma_role(typename Shape<D, FMT>::Sh& sh, uint32_t q0, uint32_t ring0, uint32_t tmem, int half) {
   using T = Shape<D, FMT>;
-  constexpr PromptCut cut = T::cut();
   constexpr uint32_t kIdQK = idesc(T::KT, false), kIdPV = idesc(D, true);
   constexpr int SUB = T::KT / 64;       // parts in which the weights of a tile arrive
   const uint32_t lead = elect_lane();
@@ -674,12 +733,13 @@ __device__ __forceinline__ bool mma_role(const PagedPromptParams& p, PromptWalk 
     }
     mma_commit(lead, o_full);
   };
-  PromptPiece x;
-  do {
-    x = prompt_piece(p, cut, w);
-    if (x.t0 == x.t1) continue;
-    const Halves hv = halves_of<T>(p, w, x);
-    const int t0 = uniform(x.t0), tiles = uniform(x.t1) - t0, n = uniform(half ? hv.t1[1] : hv.t1[0]) - t0;     // n: tiles of this half
+  Items items{0};
+  for (;; ++items.no) {
+    int last, tiles, n;                 // n: tiles of this half
+    if (!items.take(sh, [&](const Item& i) { last = i.last; tiles = i.tiles; n = i.end[half]; })) return false;
+    if (uniform(last)) return true;
+    tiles = uniform(tiles);
+    n = uniform(n);
     if (!wait_full()) return false;
     if (n > 0) {
       if (!warp_wait(q_full, q_phase)) return false;
@@ -711,15 +771,13 @@ __device__ __forceinline__ bool mma_role(const PagedPromptParams& p, PromptWalk 
       if (i + 1 < n) qk(i + 2 == n);
       release(i + 1 < n);
     }
-  } while (prompt_walk_next(p, cut, w, x.cost));
-  return true;
+  }
 }
 
 // ---- warps 0-3, 4-7: the softmax of a half
 template <int D, int FMT>
-__device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, PromptWalk w, Shared& sh, uint32_t tmem) {
+__device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, typename Shape<D, FMT>::Sh& sh, uint32_t tmem) {
   using T = Shape<D, FMT>;
-  constexpr PromptCut cut = T::cut();
   constexpr int KT = T::KT, C = 64;                    // columns at a time
   const int half = threadIdx.x >> 7, row = threadIdx.x & 127, lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 3;
   const uint32_t lanes = (uint32_t)(warp * 32) << 16;
@@ -729,17 +787,18 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, PromptW
   const f32x2 scale2 = two(p.scale_log2, p.scale_log2);
   uint32_t s_phase = 0, o_phase = 0, e_phase = 1;
   int tile_no = 0;
-  PromptPiece x;
-  do {
-    x = prompt_piece(p, cut, w);
-    if (x.t0 == x.t1) continue;
-    const Halves hv = halves_of<T>(p, w, x);
-    const int rows = half ? hv.rows[1] : hv.rows[0], see = half ? hv.see[1] : hv.see[0], t1 = half ? hv.t1[1] : hv.t1[0];
-    const int limit = row < rows ? min(x.n, w.s.pos + x.s0 + s + 1) : 0;      // tokens that the row sees
+  Items items{0};
+  for (;; ++items.no) {
+    int last, rows, see, n, pos0, t0, tiles, end;
+    if (!items.take(sh, [&](const Item& i) {
+          last = i.last; rows = i.rows[half]; see = i.see[half]; n = i.n; pos0 = i.pos0; t0 = i.t0; tiles = i.tiles; end = i.end[half];
+        })) return false;
+    if (last) return true;
+    const int limit = row < rows ? min(n, pos0 + s + 1) : 0;       // tokens that the row sees
     float m = -INFINITY, l = 0.f, lc = 0.f;            // lc: what the additions to l have lost
     bool seen = false;
 #pragma unroll 1
-    for (int c = x.t0 * KT; c < t1 * KT; c += C) {      // parts of 64 tokens
+    for (int c = t0 * KT; c < (t0 + end) * KT; c += C) {      // parts of 64 tokens
       if (KT == C || c % KT == 0) {
         if (!warp_wait(s_full, s_phase)) return false;
         s_phase ^= 1;
@@ -749,7 +808,7 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, PromptW
       uint32_t sr[C];
 #pragma unroll
       for (int j = 0; j < C; j += 32) tmem_ld32(tP + j, sr + j);
-      const bool here = sh.pages[(tile_no + c / KT - x.t0) & 7][c % KT / 64];
+      const bool here = sh.pages[(tile_no + c / KT - t0) & 7][c % KT / 64];
       tmem_wait_ld();
       if (c + C > see || !here) {                       // some tokens are not seen
         const int last = here ? limit - c : 0;
@@ -768,7 +827,7 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, PromptW
       const float m_new = fmaxf(m, max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * p.scale_log2);
       if (__any_sync(0xffffffffu, m_new > m + 8.f)) {
         const float f = m == m_new ? 1.f : ex2(m - m_new);
-        if (c > x.t0 * KT) {
+        if (c > t0 * KT) {
           if (!warp_wait(o_full, o_phase ^ 1)) return false;          // the product before this part's
           fence_after();
 #pragma unroll 1
@@ -810,8 +869,8 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, PromptW
       lc = (sum - l) - add;
       l = sum;
     }
-    tile_no += x.t1 - x.t0;
-    if (t1 > x.t0) {
+    tile_no += tiles;
+    if (end > 0) {
       if (!warp_wait(smem_u32(&sh.o_empty[half]), e_phase)) return false;     // the last item's have been read
       e_phase ^= 1;
       sh.stats[half][0][row] = m;
@@ -819,166 +878,145 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, PromptW
       __syncwarp();
       if (lane == 0) bar_arrive(smem_u32(&sh.stats_full[half]));
     }
-  } while (prompt_walk_next(p, cut, w, x.cost));
-  return true;
+  }
 }
 
 // ---- four warps: the next item's queries, the last item's outputs
 template <int D, int FMT>
-__device__ __forceinline__ bool rows_role(const PagedPromptParams& p, PromptWalk w, Shared& sh, uint32_t q0, uint32_t tmem) {
+__device__ __forceinline__ bool rows_role(const PagedPromptParams& p, typename Shape<D, FMT>::Sh& sh, uint32_t q0, uint32_t tmem) {
   using T = Shape<D, FMT>;
-  constexpr PromptCut cut = T::cut();
   constexpr int KT = T::KT;
   const int row = threadIdx.x & 127, lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 3;
   const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
   uint32_t phases = 0;                  // bit h: q_empty, 2 + h: stats_full, 4 + h: o_done
-  int item_no = 0;
-  auto skip = [&](PromptWalk& a, PromptPiece& x) {     // to the next item that has tiles here
-    do {
-      x = prompt_piece(p, cut, a);
-      if (x.t0 != x.t1) return true;
-    } while (prompt_walk_next(p, cut, a, x.cost));
-    return false;
-  };
-  auto queries = [&](const PromptWalk& a, const PromptPiece& x) {
-    const Halves hv = halves_of<T>(p, a, x);
-    const int ll = p.by_heads.div(a.lh), h = a.lh - ll * p.g.N_kv;
+  Items items{0};
+  Item it;
+  it.last = 1;
+  for (;; ++items.no) {
+    Item next;
+    if (!items.take(sh, [&](const Item& i) { next = i; })) return false;
+    if (!next.last) {
 #pragma unroll 1
-    for (int half = 0; half < 2; ++half) {
-      if (x.t0 == (half ? hv.t1[1] : hv.t1[0])) continue;
-      if (!warp_wait(smem_u32(&sh.q_empty[half]), (phases >> half & 1) ^ 1)) return false;
-      phases ^= 1u << half;
-      fence_after();
-      const int rows = half ? hv.rows[1] : hv.rows[0], ri = half * kHalf;
-      if constexpr (T::kQTmem) {
-        const bool on = row < rows;
-        const int s = p.by_group.div(ri + row);
-        const uint4* src = (const uint4*)p.q.ptr;
-        if (on) src = (const uint4*)((const uint16_t*)p.q.ptr + prompt_row(p, p.q, a.b, a.s, x.s0 + s) + ll * p.q.sl + (h * p.G + ri + row - s * p.G) * p.q.sn);
-#pragma unroll 1
-        for (int c = 0; c < D / 64; ++c) {
-          uint4 v[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = on ? int4_order(__ldg(src + c * 8 + i)) : make_uint4(0u, 0u, 0u, 0u);
-          tmem_st32(lanes + T::kColQ + half * (D / 2) + c * 32, (const uint32_t*)v);
-        }
-        tmem_wait_st();
-        fence_before();
-      } else {
-        // 16-byte pieces of a row in neighbouring lanes
-        constexpr int P = D / 8;
-        const uint32_t dst = q0 + half * kHalf * D * 2;
-#pragma unroll 4
-        for (int i = row; i < kHalf * P; i += 128) {
-          const int r = i / P, c = i % P, s = p.by_group.div(ri + r);
-          const bool on = r < rows;
-          const uint16_t* const src = (const uint16_t*)p.q.ptr + (on ? prompt_row(p, p.q, a.b, a.s, x.s0 + s) + ll * p.q.sl + (h * p.G + ri + r - s * p.G) * p.q.sn + c * 8 : 0);
-          cp_async16(dst + swz(kHalf, r, c), src, on ? 16 : 0);
-        }
-        cp_async_wait_all();
-        fence_proxy_async();
-      }
-      __syncwarp();
-      if (lane == 0) bar_arrive(smem_u32(&sh.q_full[half]));
-    }
-    return true;
-  };
-  PromptPiece x;
-  if (!skip(w, x)) return true;
-  if (!queries(w, x)) return false;
-  while (true) {
-    PromptWalk next = w;
-    PromptPiece nx;
-    const bool more = prompt_walk_next(p, cut, next, x.cost) && skip(next, nx);
-    if (more && !queries(next, nx)) return false;
-    const Halves hv = halves_of<T>(p, w, x);
-    const int ll = p.by_heads.div(w.lh), h = w.lh - ll * p.g.N_kv;
-    const bool whole = x.t0 == 0 && x.t1 == x.tiles;
-    float* const rec = (float*)p.records + (2 * blockIdx.x + (x.t0 == 0)) * prompt_record_floats(kItemRows, D);
-#pragma unroll 1
-    for (int half = 0; half < 2; ++half) {
-      const int t1 = half ? hv.t1[1] : hv.t1[0], rows = half ? hv.rows[1] : hv.rows[0];
-      const bool some = t1 > x.t0, on = row < rows;
-      float m = -INFINITY, l = 0.f;
-      if (some) {
-        if (!warp_wait(smem_u32(&sh.stats_full[half]), phases >> (2 + half) & 1)) return false;
-        phases ^= 4u << half;
-        m = sh.stats[half][0][row];
-        l = sh.stats[half][1][row];
-        if (!warp_wait(smem_u32(&sh.o_done[half]), phases >> (4 + half) & 1)) return false;
-        phases ^= 16u << half;
+      for (int half = 0; half < 2; ++half) {
+        if ((half ? next.end[1] : next.end[0]) == 0) continue;
+        if (!warp_wait(smem_u32(&sh.q_empty[half]), (phases >> half & 1) ^ 1)) return false;
+        phases ^= 1u << half;
         fence_after();
-      }
-      const bool mend = sh.bad[item_no & 31] != 0;
-      const int ri = half * kHalf + row, s = p.by_group.div(ri), head = h * p.G + ri - s * p.G;
-      const bool none = m == -INFINITY && l == 0.f;
-      const float f = none ? 0.f : m == -INFINITY ? __int_as_float(0x7fffffff) : 1.f / l;
-      uint16_t* dst = nullptr;
-      if (on && whole) dst = (uint16_t*)p.out.ptr + prompt_row(p, p.out, w.b, w.s, x.s0 + s) + ll * p.out.sl + head * p.out.sn;
+        const int rows = half ? next.rows[1] : next.rows[0], ri = half * kHalf;
+        const uint16_t* const q = (const uint16_t*)p.q.ptr + next.q_at;
+        if constexpr (T::kQTmem) {
+          const int s = p.by_group.div(ri + row);
+          const bool on = row < rows;
+          const uint4* const src = (const uint4*)(on ? q + s * p.q.ss + (ri + row - s * p.G) * p.q.sn : (const uint16_t*)p.q.ptr);
 #pragma unroll 1
-      for (int c = 0; c < D; c += 32) {
-        uint32_t o[32];
-        if (some) {
-          tmem_ld32(lanes + T::kColO + half * D + c, o);
-          tmem_wait_ld();
-          if (c + 32 == D) {            // the half's next product may overwrite it
-            fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(smem_u32(&sh.o_empty[half]));
+          for (int c = 0; c < D / 64; ++c) {
+            uint4 v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = on ? int4_order(__ldg(src + c * 8 + i)) : make_uint4(0u, 0u, 0u, 0u);
+            tmem_st32(lanes + T::kColQ + half * (D / 2) + c * 32, (const uint32_t*)v);
           }
-        }
-        if (!some || none) {
-#pragma unroll
-          for (int j = 0; j < 32; ++j) o[j] = 0u;
-        }
-        if (mend && on) {               // values that were left out because some rows do not see them
-          const int limit = min(x.n, w.s.pos + x.s0 + s + 1);
-          for (int tok = max(w.s.pos + x.s0 + 1, x.t0 * KT); tok < min(limit, t1 * KT); ++tok) {
-            const int page = tok >= 0 ? page_of(p.table, p.g, w.b, tok, p.error) : -1;
-            if (page < 0) continue;
-            const uint8_t* const block = p.pages + page_block_offset(p.g, p.layer0 + ll, page, h);
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              const float v = value_at<D, FMT>(block, tok & 63, c + (T::kInt4 ? int4_channel(j) : j));
-              if (!(fabsf(v) <= 3.4e38f)) o[j] = __float_as_uint(__uint_as_float(o[j]) + v);
-            }
+          tmem_wait_st();
+          fence_before();
+        } else {
+          // 16-byte pieces of a row in neighbouring lanes
+          constexpr int P = D / 8;
+          const uint32_t dst = q0 + half * kHalf * D * 2;
+          const int c = row % P;
+#pragma unroll 4
+          for (int r = row / P; r < kHalf; r += 128 / P) {
+            const int s = p.by_group.div(ri + r);
+            const bool on = r < rows;
+            cp_async16(dst + swz(kHalf, r, c), on ? q + s * p.q.ss + (ri + r - s * p.G) * p.q.sn + c * 8 : (const uint16_t*)p.q.ptr, on ? 16 : 0);
           }
-        }
-        if constexpr (T::kInt4) {       // back in the order of channels
-          uint32_t u[32];
-#pragma unroll
-          for (int j = 0; j < 32; ++j) u[int4_channel(j)] = o[j];
-#pragma unroll
-          for (int j = 0; j < 32; ++j) o[j] = u[j];
-        }
-        if (on && whole) {
-#pragma unroll
-          for (int j = 0; j < 32; j += 8) {
-            uint32_t u[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) u[k] = none ? 0u : pack_bf16(__uint_as_float(o[j + 2 * k]) * f, __uint_as_float(o[j + 2 * k + 1]) * f);
-            *(uint4*)(dst + c + j) = make_uint4(u[0], u[1], u[2], u[3]);
-          }
-        } else if (on) {
-#pragma unroll
-          for (int j = 0; j < 32; j += 4) *(uint4*)(rec + (size_t)ri * D + c + j) = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+          cp_async_wait_all();
+          fence_proxy_async();
         }
         __syncwarp();
+        if (lane == 0) bar_arrive(smem_u32(&sh.q_full[half]));
       }
-      if (on) {
-        if (!whole) {
-          rec[kItemRows * D + ri] = m;
-          rec[kItemRows * (D + 1) + ri] = l;
-        } else if (p.lse) {
-          p.lse[(prompt_lse_row(p, w.b, w.s, x.s0 + s) * p.nlayers + ll) * p.N_q + head] = prompt_log_sum(m, l);
+    }
+    if (!it.last) {
+      const bool mend = sh.bad[(items.no - 1) & (4 * kItems - 1)] != 0;
+      float* const rec = (float*)p.records + (2 * blockIdx.x + it.first) * prompt_record_floats(kItemRows, D);
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half) {
+        const int end = half ? it.end[1] : it.end[0];
+        const bool some = end > 0, on = row < (half ? it.rows[1] : it.rows[0]);
+        float m = -INFINITY, l = 0.f;
+        if (some) {
+          if (!warp_wait(smem_u32(&sh.stats_full[half]), phases >> (2 + half) & 1)) return false;
+          m = sh.stats[half][0][row];
+          l = sh.stats[half][1][row];
+          if (!warp_wait(smem_u32(&sh.o_done[half]), phases >> (4 + half) & 1)) return false;
+          phases ^= 20u << half;
+          fence_after();
+        }
+        const int ri = half * kHalf + row, s = p.by_group.div(ri), g = ri - s * p.G;
+        const bool none = m == -INFINITY && l == 0.f;
+        const float f = none ? 0.f : m == -INFINITY ? __int_as_float(0x7fffffff) : 1.f / l;
+        uint16_t* const dst = (uint16_t*)p.out.ptr + it.out_at + s * p.out.ss + g * p.out.sn;
+#pragma unroll 1
+        for (int c = 0; c < D; c += 32) {
+          uint32_t o[32];
+          if (some) {
+            tmem_ld32(lanes + T::kColO + half * D + c, o);
+            tmem_wait_ld();
+            if (c + 32 == D) {          // the half's next product may overwrite it
+              fence_before();
+              __syncwarp();
+              if (lane == 0) bar_arrive(smem_u32(&sh.o_empty[half]));
+            }
+          }
+          if (!some || none) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] = 0u;
+          }
+          if (mend && on) {             // values that were left out because some rows do not see them
+            const int stop = min(min(it.n, it.pos0 + s + 1), (it.t0 + end) * KT);
+            for (int tok = max(it.pos0 + 1, it.t0 * KT); tok < stop; ++tok) {
+              const int page = tok >= 0 ? page_of(p.table, p.g, it.b, tok, p.error) : -1;
+              if (page < 0) continue;
+              const uint8_t* const block = p.pages + page_block_offset(p.g, it.layer, page, it.h);
+#pragma unroll
+              for (int j = 0; j < 32; ++j) {
+                const float v = value_at<D, FMT>(block, tok & 63, c + (T::kInt4 ? int4_channel(j) : j));
+                if (!(fabsf(v) <= 3.4e38f)) o[j] = __float_as_uint(__uint_as_float(o[j]) + v);
+              }
+            }
+          }
+          if constexpr (T::kInt4) {     // back in the order of channels
+            uint32_t u[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) u[int4_channel(j)] = o[j];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] = u[j];
+          }
+          if (on && it.whole) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 8) {
+              uint32_t u[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) u[k] = none ? 0u : pack_bf16(__uint_as_float(o[j + 2 * k]) * f, __uint_as_float(o[j + 2 * k + 1]) * f);
+              *(uint4*)(dst + c + j) = make_uint4(u[0], u[1], u[2], u[3]);
+            }
+          } else if (on) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) *(uint4*)(rec + (size_t)ri * D + c + j) = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+          }
+          __syncwarp();
+        }
+        if (on) {
+          if (!it.whole) {
+            rec[kItemRows * D + ri] = m;
+            rec[kItemRows * (D + 1) + ri] = l;
+          } else if (p.lse) {
+            p.lse[it.lse_at + (int64_t)s * p.nlayers * p.N_q + g] = prompt_log_sum(m, l);
+          }
         }
       }
     }
-    if (!whole && x.t0 == 0 && row == 0) p.desc[blockIdx.x] = prompt_desc(cut, w, x);
-    if (!more) return true;
-    w = next;
-    x = nx;
-    ++item_no;
+    if (next.last) return true;
+    it = next;
   }
 }
 
@@ -987,7 +1025,7 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
   using T = Shape<D, FMT>;
   constexpr PromptCut cut = T::cut();
   extern __shared__ __align__(1024) unsigned char smem[];       // nothing else is in shared memory: it starts on such a border
-  Shared& sh = *(Shared*)(smem + T::kSharedAt);
+  typename T::Sh& sh = *(typename T::Sh*)(smem + T::kSharedAt);
   begin_dependent();
   const int tid = threadIdx.x, warp = tid >> 5;
   if (tid == 0) p.desc[blockIdx.x].pieces = 0;
@@ -1018,6 +1056,10 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
       bar_init(smem_u32(&sh.q_empty[i]), 1);
       bar_init(smem_u32(&sh.stats_full[i]), 4);
     }
+    for (int i = 0; i < kItems; ++i) {
+      bar_init(smem_u32(&sh.item_full[i]), 1);
+      bar_init(smem_u32(&sh.item_empty[i]), 8 + 2 + 2 + 4 + (T::kPlain ? 0 : 4));       // softmax, products, loads, rows, unpacking
+    }
     bar_init(smem_u32(&sh.raw[0]), 1);
     bar_init(smem_u32(&sh.raw[1]), 1);
     for (int i = 0; i < T::kStages; ++i) {
@@ -1026,7 +1068,7 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     sh.failed = 0;
-    for (int i = 0; i < 32; ++i) sh.bad[i] = 0;
+    for (int i = 0; i < 4 * kItems; ++i) sh.bad[i] = 0;
   }
   fence_before();
   __syncthreads();
@@ -1035,20 +1077,20 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
   bool ok = true;
   if (warp < 8) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(T::kSoftmaxRegs));
-    ok = softmax_role<D, FMT>(p, w, sh, tmem);
+    ok = softmax_role<D, FMT>(p, sh, tmem);
   } else if (warp >= T::kRowsWarp) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(T::kRowsRegs));
-    ok = rows_role<D, FMT>(p, w, sh, q0, tmem);
+    ok = rows_role<D, FMT>(p, sh, q0, tmem);
   } else {
     if (T::kPlain || warp < 12) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(T::kLoadRegs));
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(T::kMmaRegs));
     if (warp < 8 + T::kLoadWarps) {
       if constexpr (T::kPlain) ok = load_role<D, FMT>(p, &map, w, sh, ring0, warp - 8);
-      else ok = unpack_role<D, FMT>(p, w, sh, ring0, stage0);
+      else ok = unpack_role<D, FMT>(sh, ring0, stage0);
     } else if (!T::kPlain && warp >= T::kFetchWarp && warp < T::kFetchWarp + 2) {
       ok = fetch_role<D, FMT>(p, w, sh, stage0, warp - T::kFetchWarp);
     } else {
-      ok = mma_role<D, FMT>(p, w, sh, q0, ring0, tmem, warp - T::kMmaWarp);
+      ok = mma_role<D, FMT>(sh, q0, ring0, tmem, warp - T::kMmaWarp);
     }
   }
   if (!ok) {

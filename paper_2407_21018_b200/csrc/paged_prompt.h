@@ -12,12 +12,13 @@
 namespace think {
 
 struct PromptCut {
-  int tile, extra;            // tokens of a tile, places of an item besides its tokens
+  int tile, extra;            // tokens of a tile (64 or 128), places of an item besides its tokens
   // tile j stands at slot(j) of its item: `extra` + tile neighbouring places always hold one
   THINK_HD int64_t slot(int64_t j) const { return j == 0 ? 0 : extra + tile * j; }
   THINK_HD int64_t first_tile(int64_t x) const {        // that stands at x or behind
     if (x <= 0) return 0;
-    const int64_t j = div_wide(x - extra + tile - 1 > 0 ? x - extra + tile - 1 : 0, tile);
+    const uint64_t y = (uint64_t)(x - extra + tile - 1 > 0 ? x - extra + tile - 1 : 0);
+    const int64_t j = (int64_t)(y >> (tile == 64 ? 6 : 7));
     return j < 1 ? 1 : j;
   }
   // parts of a line so that every part holds a tile
