@@ -66,12 +66,14 @@ __global__ void __launch_bounds__(kThreads) k_paged_prompt_simple(const PagedPro
   float* const sk = sq + kRows * RS;
   float* const sv = sk + kTile * RS;
   float* const sp = sv + kTile * RS;
-  __shared__ long long s_scratch[40];
   begin_dependent();
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
-  if (tid == 0) p.desc[blockIdx.x].pieces = 0;
+  PromptDesc desc = {0, 0, 0, 0, 0};
   PromptWalk w;
-  if (!prompt_walk_begin<kThreads>(p, cut, w, s_scratch)) return;
+  if (!prompt_walk_begin(p, cut, w)) {              // (every warp for itself)
+    if (tid == 0) p.desc[blockIdx.x] = desc;
+    return;
+  }
   PromptPiece x;
   do {
     x = prompt_piece(p, cut, w);
@@ -211,9 +213,11 @@ __global__ void __launch_bounds__(kThreads) k_paged_prompt_simple(const PagedPro
         }
       }
     }
-    if (!whole && x.t0 == 0 && tid == 0) p.desc[blockIdx.x] = prompt_desc(cut, w, x);
+    if (x.t0 > 0) desc.carries = x.t1 == x.tiles ? 1 : 2;
+    else if (!whole) desc = PromptDesc{w.lh, w.b, w.i, 1, desc.carries};
     __syncthreads();                                // the next item's queries take this one's place
   } while (prompt_walk_next(p, cut, w, x.cost));
+  if (tid == 0) p.desc[blockIdx.x] = desc;
 }
 
 // Joins the pieces of the items that were cut, in their order: a warp per row, the states' statistics over its lanes.
@@ -223,17 +227,26 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_paged_prompt_join(const Pag
   constexpr int W = D / 32;                         // channels of a lane
   begin_dependent();
   const PromptDesc d = p.desc[blockIdx.x];
-  if (d.pieces == 0) return;
+  if (!d.begins) return;
   bool bad = false;
   const PromptSeq seq = prompt_seq(p, d.b, bad);
-  const int lane = threadIdx.x & 31, r = blockIdx.y * kJoinWarps + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  int pieces = 2;                                   // up to the CTA that ends it
+  for (int c = blockIdx.x + 1;; c += 32) {
+    const uint32_t ends = __ballot_sync(0xffffffffu, c + lane < p.grid && p.desc[min(c + lane, p.grid - 1)].carries == 1);
+    if (ends || c + 32 >= p.grid) {
+      pieces = c - (int)blockIdx.x + __ffs(ends);
+      break;
+    }
+  }
+  const int r = blockIdx.y * kJoinWarps + (threadIdx.x >> 5);
   const int s0 = d.item * p.per, rows = min(p.per, seq.rows - s0) * p.G;
   if (r >= rows) return;
   constexpr size_t kRec = (size_t)ROWS * (D + 2);
   auto rec = [&](int i) { return (const float*)p.records + (i == 0 ? 2 * blockIdx.x + 1 : 2 * (blockIdx.x + i)) * kRec; };
   float m = -INFINITY;
   bool any = false;
-  for (int i = lane; i < d.pieces; i += 32) {
+  for (int i = lane; i < pieces; i += 32) {
     const float x = rec(i)[ROWS * D + r], y = rec(i)[ROWS * (D + 1) + r];
     any |= !(y == 0.f);
     m = fmaxf(m, x);
@@ -242,16 +255,16 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_paged_prompt_join(const Pag
   for (int s = 1; s < 32; s <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
   any = __any_sync(0xffffffffu, any);
   float o[W] = {}, l = 0.f;
-  for (int i0 = 0; i0 < d.pieces; i0 += 32) {
+  for (int i0 = 0; i0 < pieces; i0 += 32) {
     const int i = i0 + lane;
     float f = 0.f, fl = 0.f;
-    if (i < d.pieces) {
+    if (i < pieces) {
       const float x = rec(i)[ROWS * D + r], y = rec(i)[ROWS * (D + 1) + r];
       f = x == -INFINITY ? (y == y ? 0.f : y) : exp2f(x - m);      // (a sum may be NaN under a maximum of -infinity)
       fl = f * y;
     }
 #pragma unroll 4
-    for (int k = 0; k < min(32, d.pieces - i0); ++k) {
+    for (int k = 0; k < min(32, pieces - i0); ++k) {
       const float g = __shfl_sync(0xffffffffu, f, k);
       l += __shfl_sync(0xffffffffu, fl, k);
       if (g == 0.f) continue;

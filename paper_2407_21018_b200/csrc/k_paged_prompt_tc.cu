@@ -214,10 +214,7 @@ struct Shared {
   uint8_t bad[4 * kItems];               // of the items under way: a value that some rows do not see is a NaN or an infinity
   Item items[kItems];
   uint8_t stage_there[STAGES];           // the stage holds a page's rows
-  union {
-    float stats[2][2][kHalf];            // of a half's rows: m, l as in a record
-    long long scratch[40];               // at the kernel's start
-  };
+  float stats[2][2][kHalf];              // of a half's rows: m, l as in a record
 };
 
 // ---- what depends on the format and the head dimension
@@ -371,32 +368,49 @@ struct Items {
     return true;
   }
 };
-// the walking warp: on to the next item that has tiles here, which is handed out; `more` is false behind the last
-template <typename T>
-__device__ __forceinline__ bool hand_out(const PagedPromptParams& p, PromptWalk& w, typename T::Sh& sh, int no, bool& more, int64_t& cost) {
-  constexpr PromptCut cut = T::cut();
-  PromptPiece x;
-  if (no > 0) more = prompt_walk_next(p, cut, w, cost);
-  while (more) {
-    x = prompt_piece(p, cut, w);
-    if (x.t0 != x.t1) break;
-    more = prompt_walk_next(p, cut, w, x.cost);
+// The warp that walks.
+struct Walker {
+  PromptWalk w;
+  PromptDesc desc;
+  int64_t cost;
+  int state;                  // 0: at a new item, 1: on to the next one, 2: at the end
+  __device__ __forceinline__ void begin(const PagedPromptParams& p, const PromptCut& cut) {
+    desc = PromptDesc{0, 0, 0, 0, 0};
+    state = prompt_walk_begin(p, cut, w) ? 0 : 2;
   }
-  const int slot = no & (kItems - 1);
-  if (!warp_wait(smem_u32(&sh.item_empty[slot]), (no / kItems & 1) ^ 1)) return false;
-  if ((threadIdx.x & 31) == 0) {
-    if (more) {
-      describe<T>(p, w, x, sh.items[slot]);
-      if (x.t0 == 0 && x.t1 != x.tiles) p.desc[blockIdx.x] = prompt_desc(cut, w, x);
-    } else {
-      sh.items[slot].last = 1;
+  // hands out the next item that has tiles here, or says that there is none
+  template <typename T>
+  __device__ __forceinline__ bool hand_out(const PagedPromptParams& p, typename T::Sh& sh, int no) {
+    constexpr PromptCut cut = T::cut();
+    PromptPiece x;
+#pragma unroll 1
+    while (state < 2) {
+      if (state == 1 && !prompt_walk_next(p, cut, w, cost)) {
+        state = 2;
+        break;
+      }
+      state = 1;
+      x = prompt_piece(p, cut, w);
+      cost = x.cost;
+      if (x.t0 != x.t1) break;
     }
-    bar_arrive(smem_u32(&sh.item_full[slot]));
+    const int slot = no & (kItems - 1);
+    if (!warp_wait(smem_u32(&sh.item_empty[slot]), (no / kItems & 1) ^ 1)) return false;
+    if ((threadIdx.x & 31) == 0) {
+      if (state < 2) {
+        describe<T>(p, w, x, sh.items[slot]);
+        if (x.t0 > 0) desc.carries = x.t1 == x.tiles ? 1 : 2;
+        else if (x.t1 != x.tiles) desc = PromptDesc{w.lh, w.b, w.i, 1, desc.carries};
+      } else {
+        sh.items[slot].last = 1;
+        p.desc[blockIdx.x] = desc;
+      }
+      bar_arrive(smem_u32(&sh.item_full[slot]));
+    }
+    __syncwarp();
+    return true;
   }
-  __syncwarp();
-  cost = x.cost;
-  return true;
-}
+};
 
 struct Ring {                 // position in the ring of slots
   int slot;
@@ -443,7 +457,7 @@ struct PageWindow {
 
 // ---- bf16 pages: two warps bring the first and the second page of every tile, keys and values, by TMA
 template <int D, int FMT>
-__device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUtensorMap* map, PromptWalk w, typename Shape<D, FMT>::Sh& sh, uint32_t ring0, int mine) {
+__device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUtensorMap* map, typename Shape<D, FMT>::Sh& sh, uint32_t ring0, int mine) {
   using T = Shape<D, FMT>;
   const int lane = threadIdx.x & 31;
   const uint32_t lead = elect_lane(), raw = smem_u32(&sh.raw[mine]);
@@ -452,10 +466,10 @@ __device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUte
   uint32_t raw_phase = 0;
   int tile_no = 0;
   Items items{0};
-  bool more = true;
-  int64_t cost = 0;
+  Walker walk;
+  if (mine == 0) walk.begin(p, T::cut());
   for (;; ++items.no) {
-    if (mine == 0 && !hand_out<T>(p, w, sh, items.no, more, cost)) return false;
+    if (mine == 0 && !walk.template hand_out<T>(p, sh, items.no)) return false;
     int last, layer, h, b, n, see, t0, tiles;
     if (!items.take(sh, [&](const Item& i) { last = i.last; layer = i.layer; h = i.h; b = i.b; n = i.n; see = i.see[0]; t0 = i.t0; tiles = i.tiles; })) return false;
     if (last) return true;
@@ -511,7 +525,7 @@ __device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUte
 
 // ---- quantised pages: two warps, in turn, have their bytes copied to the stages, 64 rows and their scales each
 template <int D, int FMT>
-__device__ __forceinline__ bool fetch_role(const PagedPromptParams& p, PromptWalk w, typename Shape<D, FMT>::Sh& sh, uint32_t stage0, int mine) {
+__device__ __forceinline__ bool fetch_role(const PagedPromptParams& p, typename Shape<D, FMT>::Sh& sh, uint32_t stage0, int mine) {
   using T = Shape<D, FMT>;
   constexpr int PAGES = T::KT / 64;                // of a tile: the two warps share its pages, or else keys and values
   const int lane = threadIdx.x & 31;
@@ -520,10 +534,10 @@ __device__ __forceinline__ bool fetch_role(const PagedPromptParams& p, PromptWal
   uint32_t phase = 0;
   PageWindow win;
   Items items{0};
-  bool more = true;
-  int64_t cost = 0;
+  Walker walk;
+  if (mine == 0) walk.begin(p, T::cut());
   for (;; ++items.no) {
-    if (mine == 0 && !hand_out<T>(p, w, sh, items.no, more, cost)) return false;
+    if (mine == 0 && !walk.template hand_out<T>(p, sh, items.no)) return false;
     int last, layer, h, b, n, t0, tiles;
     if (!items.take(sh, [&](const Item& i) { last = i.last; layer = i.layer; h = i.h; b = i.b; n = i.n; t0 = i.t0; tiles = i.tiles; })) return false;
     if (last) return true;
@@ -971,19 +985,6 @@ __device__ __forceinline__ bool rows_role(const PagedPromptParams& p, typename S
 #pragma unroll
             for (int j = 0; j < 32; ++j) o[j] = 0u;
           }
-          if (mend && on) {             // values that were left out because some rows do not see them
-            const int stop = min(min(it.n, it.pos0 + s + 1), (it.t0 + end) * KT);
-            for (int tok = max(it.pos0 + 1, it.t0 * KT); tok < stop; ++tok) {
-              const int page = tok >= 0 ? page_of(p.table, p.g, it.b, tok, p.error) : -1;
-              if (page < 0) continue;
-              const uint8_t* const block = p.pages + page_block_offset(p.g, it.layer, page, it.h);
-#pragma unroll
-              for (int j = 0; j < 32; ++j) {
-                const float v = value_at<D, FMT>(block, tok & 63, c + (T::kInt4 ? int4_channel(j) : j));
-                if (!(fabsf(v) <= 3.4e38f)) o[j] = __float_as_uint(__uint_as_float(o[j]) + v);
-              }
-            }
-          }
           if constexpr (T::kInt4) {     // back in the order of channels
             uint32_t u[32];
 #pragma unroll
@@ -1005,6 +1006,23 @@ __device__ __forceinline__ bool rows_role(const PagedPromptParams& p, typename S
           }
           __syncwarp();
         }
+        if (mend && on) {               // values that were left out because some rows do not see them
+          const int stop = min(min(it.n, it.pos0 + s + 1), (it.t0 + end) * KT);
+#pragma unroll 1
+          for (int tok = max(max(it.pos0 + 1, it.t0 * KT), 0); tok < stop; ++tok) {
+            const int page = page_of(p.table, p.g, it.b, tok, p.error);
+            if (page < 0) continue;
+            const uint8_t* const block = p.pages + page_block_offset(p.g, it.layer, page, it.h);
+#pragma unroll 1
+            for (int c = 0; c < D; ++c) {
+              const float v = value_at<D, FMT>(block, tok & 63, c);
+              if (fabsf(v) <= 3.4e38f) continue;
+              if (it.whole) dst[c] = (uint16_t)(pack_bf16(__uint_as_float((uint32_t)dst[c] << 16) + v, 0.f) & 0xffffu);
+              else rec[(size_t)ri * D + c] += v;
+            }
+          }
+        }
+        __syncwarp();
         if (on) {
           if (!it.whole) {
             rec[kItemRows * D + ri] = m;
@@ -1023,19 +1041,15 @@ __device__ __forceinline__ bool rows_role(const PagedPromptParams& p, typename S
 template <int D, int FMT>
 __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(const __grid_constant__ PagedPromptParams p, const __grid_constant__ CUtensorMap map) {
   using T = Shape<D, FMT>;
-  constexpr PromptCut cut = T::cut();
   extern __shared__ __align__(1024) unsigned char smem[];       // nothing else is in shared memory: it starts on such a border
   typename T::Sh& sh = *(typename T::Sh*)(smem + T::kSharedAt);
   begin_dependent();
   const int tid = threadIdx.x, warp = tid >> 5;
-  if (tid == 0) p.desc[blockIdx.x].pieces = 0;
   const uint32_t q0 = smem_u32(smem), ring0 = q0 + T::kQBytes, stage0 = q0 + T::kStageAt;
   if (q0 & 1023) {
     if (tid == 0) atomicOr(p.error, kErrSmemAlign);
     return;
   }
-  PromptWalk w;
-  if (!prompt_walk_begin<T::kThreads>(p, cut, w, sh.scratch)) return;
   if (warp == T::kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_u32(&sh.tmem)), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -1085,10 +1099,10 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
     if (T::kPlain || warp < 12) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(T::kLoadRegs));
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(T::kMmaRegs));
     if (warp < 8 + T::kLoadWarps) {
-      if constexpr (T::kPlain) ok = load_role<D, FMT>(p, &map, w, sh, ring0, warp - 8);
+      if constexpr (T::kPlain) ok = load_role<D, FMT>(p, &map, sh, ring0, warp - 8);
       else ok = unpack_role<D, FMT>(sh, ring0, stage0);
     } else if (!T::kPlain && warp >= T::kFetchWarp && warp < T::kFetchWarp + 2) {
-      ok = fetch_role<D, FMT>(p, w, sh, stage0, warp - T::kFetchWarp);
+      ok = fetch_role<D, FMT>(p, sh, stage0, warp - T::kFetchWarp);
     } else {
       ok = mma_role<D, FMT>(sh, q0, ring0, tmem, warp - T::kMmaWarp);
     }

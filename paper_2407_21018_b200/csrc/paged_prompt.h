@@ -11,6 +11,31 @@
 
 namespace think {
 
+// n / parts and n % parts for parts <= 2^15, 16 bits at a time (a 64-bit division is a routine of a hundred instructions, which
+// a kernel fetches to run it once)
+struct PromptShare {
+  int64_t each;
+  int rest, parts;
+  THINK_HD PromptShare(int64_t n, int parts_) : each(0), rest(0), parts(parts_) {
+#ifdef __CUDACC__
+#pragma unroll 1
+#endif
+    for (int i = 48; i >= 0; i -= 16) {
+      const uint32_t x = (uint32_t)rest << 16 | (uint32_t)(n >> i & 0xffff), q = x / (uint32_t)parts;
+      each = each << 16 | q;
+      rest = (int)(x - q * (uint32_t)parts);
+    }
+  }
+  THINK_HD int64_t begin(int i) const { return i * each + (uint32_t)(i * rest) / (uint32_t)parts; }      // floor(i n / parts), i <= parts
+};
+// place / length for 0 <= place, where the quotient fits 31 bits
+THINK_HD int prompt_quotient(int64_t place, int64_t length) {
+  int64_t q = (int64_t)((float)place / (float)length);
+  while (q * length > place) --q;
+  while ((q + 1) * length <= place) ++q;
+  return (int)q;
+}
+
 struct PromptCut {
   int tile, extra;            // tokens of a tile (64 or 128), places of an item besides its tokens
   // tile j stands at slot(j) of its item: `extra` + tile neighbouring places always hold one
@@ -23,8 +48,9 @@ struct PromptCut {
   }
   // parts of a line so that every part holds a tile
   THINK_HD int parts(int64_t total, int most) const {
-    const int64_t n = div_wide(total, extra + tile);
-    return n < 1 ? 1 : n < most ? (int)n : most;
+    if (total >= (int64_t)most * (extra + tile)) return most;
+    const int n = (int)((uint32_t)total / (uint32_t)(extra + tile));
+    return n < 1 ? 1 : n;
   }
 };
 

@@ -5,8 +5,11 @@
 
 namespace think {
 
-struct PromptDesc {           // an item that a CTA begins and others end: pieces of CTAs cta .. cta + pieces - 1
-  int lh, b, item, pieces;    // pieces 0: none
+// Of a CTA: the item that it begins and another ends, if there is one; and what it does with the one that it is in the middle
+// of when it begins.
+struct PromptDesc {
+  int lh, b, item;
+  int16_t begins, carries;    // carries: 0 none, 1 ends it, 2 hands it on
 };
 
 struct PagedPromptParams {
@@ -77,65 +80,61 @@ __device__ __forceinline__ int64_t prompt_lse_row(const PagedPromptParams& p, in
 
 struct PromptWalk {
   int64_t at, begin, end;     // where the item begins; the CTA's part of the line
-  int64_t total;
-  int parts;
   int lh, b, i;
   PromptSeq s;
 };
 
-// All threads of a CTA; `scratch`: 40 64-bit words of shared memory, free again afterwards.  False: the CTA has no part.
-template <int THREADS>
-__device__ __forceinline__ bool prompt_walk_begin(const PagedPromptParams& p, const PromptCut& cut, PromptWalk& w, long long* scratch) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int B = p.table.B, per = (B + THREADS - 1) / THREADS, b0 = min(B, tid * per), b1 = min(B, b0 + per);
+// A warp; its lanes share the sequences.  False: the CTA has no part.
+__device__ __forceinline__ bool prompt_walk_begin(const PagedPromptParams& p, const PromptCut& cut, PromptWalk& w) {
+  const int lane = threadIdx.x & 31, B = p.table.B, per = (B + 31) >> 5, b0 = min(B, lane * per), b1 = min(B, b0 + per);
   bool bad = false;
-  long long mine = 0;
-  for (int b = b0; b < b1; ++b) mine += prompt_line(p, prompt_seq(p, b, bad), cut.extra).total();
-  if (bad && blockIdx.x == 0) atomicOr(p.error, kErrPage);
-  long long upto = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, upto, o);
-    if (lane >= o) upto += y;
-  }
-  if (lane == 31) scratch[warp] = upto;
-  __syncthreads();
-  long long sum = lane < THREADS / 32 ? scratch[lane] : 0;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, sum, o);
-    if (lane >= o) sum += y;
-  }
-  const long long W = __shfl_sync(0xffffffffu, sum, 31), before = __shfl_sync(0xffffffffu, sum, warp > 0 ? warp - 1 : 0);
-  upto += warp > 0 ? before : 0;
-  const int LH = p.nlayers * p.g.N_kv;
-  w.total = W * LH;
-  w.parts = cut.parts(w.total, p.grid);
-  if (W == 0 || (int)blockIdx.x >= w.parts) return false;
-  w.begin = split_begin(w.total, w.parts, blockIdx.x);
-  w.end = split_begin(w.total, w.parts, blockIdx.x + 1);
-  w.lh = (int)div_wide(w.begin, W);
-  const int64_t place = w.begin - w.lh * W;
-  if (mine > 0 && place < upto && place >= upto - mine) {      // one thread
-    long long x = upto - mine;
-    for (int b = b0; b < b1; ++b) {
-      const PromptLine line = prompt_line(p, prompt_seq(p, b, bad), cut.extra);
+  long long upto = 0, before = 0, place = 0;
+  int owner = -1;
+  // first the sums, then the lane with the CTA's place looks for it
+#pragma unroll 1
+  for (int pass = 0; pass < 2; ++pass) {
+    long long sum = before;
+#pragma unroll 1
+    for (int b = b0; b < b1 && (pass == 0 || lane == owner); ++b) {
+      const PromptSeq s = prompt_seq(p, b, bad);
+      const PromptLine line = prompt_line(p, s, cut.extra);
       const long long n = line.total();
-      if (place < x + n) {
-        scratch[32] = b;
-        scratch[33] = line.find(place - x);
-        scratch[34] = w.lh * W + x + line.begin(scratch[33]);
+      if (pass == 1 && place < sum + n) {
+        w.b = b;
+        w.i = line.find(place - sum);
+        w.s = s;
+        w.at = sum + line.begin(w.i);
         break;
       }
-      x += n;
+      sum += n;
     }
+    if (pass == 1) break;
+    upto = sum;
+#pragma unroll 1
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += y;
+    }
+    before = upto - sum;
+    const long long W = __shfl_sync(0xffffffffu, upto, 31), total = W * p.nlayers * p.g.N_kv;
+    const int parts = cut.parts(total, p.grid);
+    if (bad && blockIdx.x == 0) atomicOr(p.error, kErrPage);
+    if (W == 0 || (int)blockIdx.x >= parts) return false;
+    const PromptShare share(total, parts);
+    w.begin = share.begin(blockIdx.x);
+    w.end = share.begin(blockIdx.x + 1);
+    w.lh = prompt_quotient(w.begin, W);
+    place = w.begin - w.lh * W;
+    owner = __ffs(__ballot_sync(0xffffffffu, place < upto)) - 1;      // the first lane whose sequences reach behind it
+    w.at = W;
   }
-  __syncthreads();
-  w.b = (int)scratch[32];
-  w.i = (int)scratch[33];
-  w.at = scratch[34];
-  w.s = prompt_seq(p, w.b, bad);
-  __syncthreads();
+  const long long W = __shfl_sync(0xffffffffu, upto, 31);
+  w.b = __shfl_sync(0xffffffffu, w.b, owner);
+  w.i = __shfl_sync(0xffffffffu, w.i, owner);
+  w.s.pos = __shfl_sync(0xffffffffu, w.s.pos, owner);
+  w.s.rows = __shfl_sync(0xffffffffu, w.s.rows, owner);
+  w.s.start = __shfl_sync(0xffffffffu, w.s.start, owner);
+  w.at = w.lh * W + __shfl_sync(0xffffffffu, w.at, owner);
   return true;
 }
 
@@ -175,12 +174,6 @@ __device__ __forceinline__ bool prompt_walk_next(const PagedPromptParams& p, con
     w.s = prompt_seq(p, w.b, bad);
   } while (w.s.rows == 0);                  // some sequence has rows: the line is not at its end
   return true;
-}
-
-// The description of an item that this CTA begins and does not end.
-__device__ __forceinline__ PromptDesc prompt_desc(const PromptCut& cut, const PromptWalk& w, const PromptPiece& x) {
-  const int last = split_owner(w.total, w.parts, w.at + cut.slot(x.tiles - 1));
-  return PromptDesc{w.lh, w.b, w.i, last - (int)blockIdx.x + 1};
 }
 
 // (m + log2 l) in natural logarithms; l's exponent meets m first, so that small sums keep their bits
