@@ -246,7 +246,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_paged_prompt_join(const Pag
   auto rec = [&](int i) { return (const float*)p.records + (i == 0 ? 2 * blockIdx.x + 1 : 2 * (blockIdx.x + i)) * kRec; };
   float m = -INFINITY;
   bool any = false;
+  auto there = [&](int i) { return i < pieces && (i == 0 || p.desc[blockIdx.x + i].carries != 0); };      // (a CTA may have no tile)
   for (int i = lane; i < pieces; i += 32) {
+    if (!there(i)) continue;
     const float x = rec(i)[ROWS * D + r], y = rec(i)[ROWS * (D + 1) + r];
     any |= !(y == 0.f);
     m = fmaxf(m, x);
@@ -258,7 +260,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_paged_prompt_join(const Pag
   for (int i0 = 0; i0 < pieces; i0 += 32) {
     const int i = i0 + lane;
     float f = 0.f, fl = 0.f;
-    if (i < pieces) {
+    if (there(i)) {
       const float x = rec(i)[ROWS * D + r], y = rec(i)[ROWS * (D + 1) + r];
       f = x == -INFINITY ? (y == y ? 0.f : y) : exp2f(x - m);      // (a sum may be NaN under a maximum of -infinity)
       fl = f * y;

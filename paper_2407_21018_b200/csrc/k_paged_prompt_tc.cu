@@ -1054,6 +1054,7 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_u32(&sh.tmem)), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  if (T::kPlain && tid == 32) asm volatile("prefetch.tensormap [%0];" :: "l"(&map) : "memory");
   if (tid == 0) {
     for (int i = 0; i < T::kSlots; ++i) {
       bar_init(smem_u32(&sh.full[i]), T::kLoadWarps);

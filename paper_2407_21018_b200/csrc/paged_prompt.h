@@ -38,7 +38,7 @@ THINK_HD int prompt_quotient(int64_t place, int64_t length) {
 
 struct PromptCut {
   int tile, extra;            // tokens of a tile (64 or 128), places of an item besides its tokens
-  // tile j stands at slot(j) of its item: `extra` + tile neighbouring places always hold one
+  // tile j stands at slot(j) of its item
   THINK_HD int64_t slot(int64_t j) const { return j == 0 ? 0 : extra + tile * j; }
   THINK_HD int64_t first_tile(int64_t x) const {        // that stands at x or behind
     if (x <= 0) return 0;
@@ -46,11 +46,11 @@ struct PromptCut {
     const int64_t j = (int64_t)(y >> (tile == 64 ? 6 : 7));
     return j < 1 ? 1 : j;
   }
-  // parts of a line so that every part holds a tile
-  THINK_HD int parts(int64_t total, int most) const {
-    if (total >= (int64_t)most * (extra + tile)) return most;
-    const int n = (int)((uint32_t)total / (uint32_t)(extra + tile));
-    return n < 1 ? 1 : n;
+  // Parts of a line: all there are for long ones; for short ones as many as items (what a small item costs is latency) and
+  // one more for every four tiles (joining pieces costs, too).  A part may be without a tile.
+  THINK_HD int parts(int64_t total, int64_t items, int most) const {
+    const int64_t n = items + (total >> (tile == 64 ? 8 : 9));
+    return n < most ? (int)n : most;
   }
 };
 

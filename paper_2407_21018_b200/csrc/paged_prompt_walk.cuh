@@ -88,7 +88,7 @@ struct PromptWalk {
 __device__ __forceinline__ bool prompt_walk_begin(const PagedPromptParams& p, const PromptCut& cut, PromptWalk& w) {
   const int lane = threadIdx.x & 31, B = p.table.B, per = (B + 31) >> 5, b0 = min(B, lane * per), b1 = min(B, b0 + per);
   bool bad = false;
-  long long upto = 0, before = 0, place = 0;
+  long long upto = 0, before = 0, place = 0, items = 0;
   int owner = -1;
   // first the sums, then the lane with the CTA's place looks for it
 #pragma unroll 1
@@ -107,6 +107,7 @@ __device__ __forceinline__ bool prompt_walk_begin(const PagedPromptParams& p, co
         break;
       }
       sum += n;
+      items += line.items();
     }
     if (pass == 1) break;
     upto = sum;
@@ -114,10 +115,11 @@ __device__ __forceinline__ bool prompt_walk_begin(const PagedPromptParams& p, co
     for (int o = 1; o < 32; o <<= 1) {
       const long long y = __shfl_up_sync(0xffffffffu, upto, o);
       if (lane >= o) upto += y;
+      items += __shfl_xor_sync(0xffffffffu, items, o);
     }
     before = upto - sum;
     const long long W = __shfl_sync(0xffffffffu, upto, 31), total = W * p.nlayers * p.g.N_kv;
-    const int parts = cut.parts(total, p.grid);
+    const int parts = cut.parts(total, items * p.nlayers * p.g.N_kv, p.grid);
     if (bad && blockIdx.x == 0) atomicOr(p.error, kErrPage);
     if (W == 0 || (int)blockIdx.x >= parts) return false;
     const PromptShare share(total, parts);
