@@ -324,7 +324,7 @@ cudaError_t paged_prompt_setup(int dtype, int format, int D) {
   return D == 128 ? setup_simple<128>() : setup_simple<64>();
 }
 int paged_prompt_rows(int dtype) { return dtype == THINK_BF16 ? paged_prompt_tc_rows() : kRows; }
-PromptCut paged_prompt_cut(int dtype, int format) { return dtype == THINK_BF16 ? paged_prompt_tc_cut(format) : PromptCut{kTile, kExtra}; }
+PromptCut paged_prompt_cut(int dtype) { return dtype == THINK_BF16 ? paged_prompt_tc_cut() : PromptCut{kTile, kExtra}; }
 
 cudaError_t launch_paged_prompt(const PagedPromptParams& p, int dtype, int format, const void* map, cudaStream_t s) {
   if (dtype == THINK_BF16) return p.g.D == 128 ? launch_tc<128>(p, format, map, s) : launch_tc<64>(p, format, map, s);

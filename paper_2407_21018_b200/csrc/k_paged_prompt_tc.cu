@@ -200,17 +200,18 @@ struct Item {
   int whole, first;                      // all of the item's tiles; its first tile
   int64_t q_at, out_at, lse_at;          // of the first token and query head, in elements
 };
-constexpr int kItems = 4;                // handed out and not yet taken by all
+constexpr int kItems = 2;                // handed out and not yet taken by all
 
 template <int SLOTS, int STAGES>
 struct Shared {
-  // full, empty: a slot holds operands, may be overwritten.  s_full, p_full: S of a half is there, a part of P is.  o_full: a part's
-  // product has been added to O; o_done: the item's last; o_empty: O has been read.  q_full, q_empty: the same of the queries.  stats_full: m and l.
-  uint64_t full[SLOTS], empty[SLOTS], s_full[2], p_full[2][2], o_full[2], o_done[2], o_empty[2], q_full[2], q_empty[2], stats_full[2], raw[2];
+  // full, empty: a slot holds an operand, may be overwritten.  s_full, p_full: S of a half is there, P is (two tiles each).
+  // o_full: a tile's product has been added to O; o_done: the item's last; o_empty: O has been read.  q_full, q_empty: the
+  // same of the queries.  stats_full: m and l.
+  uint64_t full[SLOTS], empty[SLOTS], s_full[2][2], p_full[2][2], o_full[2], o_done[2], o_empty[2], q_full[2], q_empty[2], stats_full[2], raw;
   uint64_t st_full[STAGES], st_empty[STAGES], item_full[kItems], item_empty[kItems];
   uint32_t tmem, failed;
-  // The loads are at most 6 tiles ahead of what is in use, and kItems + 1 items ahead of the outputs.
-  uint8_t pages[8][2];                   // of the tiles under way: the tile's pages are there
+  // The loads are at most 8 tiles ahead of what is in use, and kItems + 1 items ahead of the outputs.
+  uint8_t pages[16];                     // of the tiles under way: the tile's page is there
   uint8_t bad[4 * kItems];               // of the items under way: a value that some rows do not see is a NaN or an infinity
   Item items[kItems];
   uint8_t stage_there[STAGES];           // the stage holds a page's rows
@@ -218,32 +219,30 @@ struct Shared {
 };
 
 // ---- what depends on the format and the head dimension
+constexpr int KT = kPageTokens;          // tokens of a tile
+
 template <int D, int FMT>
 struct Shape {
   static constexpr bool kInt4 = FMT == THINK_PAGE_INT4, kPlain = FMT == THINK_PAGE_PLAIN;
-  static constexpr int KT = kInt4 ? 64 : 128;                 // tokens of a tile
   static constexpr int PARTS = kInt4 ? 2 : 1;                 // bf16 operands that a key or value is the sum of
-  static constexpr bool kQTmem = kInt4;
-  static constexpr int kSlot = KT * D * 2;
-  static constexpr int kQBytes = kQTmem ? 0 : 2 * kHalf * D * 2;
+  static constexpr int kSlot = KT * D * 2, kQBytes = 2 * kHalf * D * 2;
   static constexpr int RB = kPlain ? D * 2 : kInt4 ? D / 2 : D;       // bytes of a stored row
   static constexpr int SB = kPlain ? 0 : kInt4 ? D / 16 : 1;          // bytes of its scales
-  // quantised pages: 64 stored rows and their scales a stage; two tiles' worth, or what there is room for
+  // quantised pages: 64 stored rows and their scales a stage
   static constexpr int kBlock = 2 * kPageTokens * (RB + SB), kStage = kPlain ? 0 : kBlock / 2;
-  static constexpr int kStages = kPlain ? 2 : kInt4 || D == 64 ? 8 : 4;      // (of no bytes with bf16 pages)
-  static constexpr int kSlots = kPlain ? (D == 128 ? 5 : 12) : kInt4 ? (D == 128 ? 10 : 12) : (D == 128 ? 4 : 8);
+  static constexpr int kStages = kPlain ? 2 : 4;              // (of no bytes with bf16 pages)
+  static constexpr int kSlots = D == 64 ? 16 : kPlain ? 10 : 8;
   using Sh = Shared<kSlots, kStages>;
   static constexpr int kStageAt = kQBytes + kSlots * kSlot, kSharedAt = kStageAt + kStages * kStage, kSmem = kSharedAt + (int)sizeof(Sh);
-  static_assert(kSharedAt % 16 == 0 && kSmem <= kMaxSmem && kSlots % PARTS == 0 && kSlots >= 4 * PARTS, "shared memory");
+  static_assert(kSharedAt % 16 == 0 && kSmem <= kMaxSmem && kSlots % PARTS == 0, "shared memory");
   // warpgroups: two halves' softmax; bf16 pages: loads and products, else unpacking, then products and fetching; rows
   static constexpr int kGroups = kPlain ? 4 : 5, kThreads = 128 * kGroups;
   static constexpr int kMmaWarp = kPlain ? 10 : 12, kFetchWarp = 14, kRowsWarp = kPlain ? 12 : 16;
-  static constexpr int kLoadWarps = kPlain ? 2 : 4;
   static constexpr int kRegs = kPlain ? 128 : 96;             // a thread at launch
-  static constexpr int kSoftmaxRegs = kPlain ? 160 : 128, kLoadRegs = kPlain ? 88 : 80, kMmaRegs = 64, kRowsRegs = kPlain ? 104 : 80;
+  static constexpr int kSoftmaxRegs = kPlain ? 152 : 128, kLoadRegs = kPlain ? 96 : 80, kMmaRegs = 64, kRowsRegs = kPlain ? 112 : 80;
   static_assert(2 * kSoftmaxRegs + kLoadRegs + (kPlain ? 0 : kMmaRegs) + kRowsRegs <= kRegs * kGroups, "more registers than the block has: a wait without end");
-  // tensor memory: S of each half, Q, O of each half
-  static constexpr int kColS = KT, kColQ = 2 * KT, kColO = 256;
+  // tensor memory: S of each half, twice, O of each half
+  static constexpr int kColO = 4 * KT;
   static __host__ __device__ constexpr PromptCut cut() { return PromptCut{KT, kExtra}; }
 };
 
@@ -344,7 +343,7 @@ __device__ __forceinline__ void describe(const PagedPromptParams& p, const Promp
     const int n = max(0, min(x.n, last + 1));          // tokens that the half sees
     o.rows[i] = r;
     o.see[i] = first + 1;
-    o.end[i] = r == 0 ? 0 : max(0, min(x.t1, max(1, (n + T::KT - 1) / T::KT)) - x.t0);
+    o.end[i] = r == 0 ? 0 : max(0, min(x.t1, max(1, (n + KT - 1) / KT)) - x.t0);
   }
   o.whole = x.t0 == 0 && x.t1 == x.tiles;
   o.first = x.t0 == 0;
@@ -455,61 +454,66 @@ struct PageWindow {
   }
 };
 
-// ---- bf16 pages: two warps bring the first and the second page of every tile, keys and values, by TMA
+// The order of an item's operands, in which they are loaded, unpacked and used: keys two tiles ahead of values.
+//   for j = 0 .. tiles + 1:   values of tile j - 2 if there is one, keys of tile j if there is one
+
+// ---- bf16 pages: a warp brings keys, one values, by TMA
 template <int D, int FMT>
-__device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUtensorMap* map, typename Shape<D, FMT>::Sh& sh, uint32_t ring0, int mine) {
+__device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUtensorMap* map, typename Shape<D, FMT>::Sh& sh, uint32_t ring0, int part) {
   using T = Shape<D, FMT>;
   const int lane = threadIdx.x & 31;
-  const uint32_t lead = elect_lane(), raw = smem_u32(&sh.raw[mine]);
+  const uint32_t lead = elect_lane(), raw = smem_u32(&sh.raw);
   Ring r{0, 0};
   PageWindow win;
   uint32_t raw_phase = 0;
   int tile_no = 0;
   Items items{0};
   Walker walk;
-  if (mine == 0) walk.begin(p, T::cut());
+  if (part == 0) walk.begin(p, T::cut());
   for (;; ++items.no) {
-    if (mine == 0 && !walk.template hand_out<T>(p, sh, items.no)) return false;
+    if (part == 0 && !walk.template hand_out<T>(p, sh, items.no)) return false;
     int last, layer, h, b, n, see, t0, tiles;
     if (!items.take(sh, [&](const Item& i) { last = i.last; layer = i.layer; h = i.h; b = i.b; n = i.n; see = i.see[0]; t0 = i.t0; tiles = i.tiles; })) return false;
     if (last) return true;
     const int pages = (n + 63) >> 6;
-    win.begin(p, b, layer, h, t0 * 2, pages);
+    win.begin(p, b, layer, h, t0, pages);
 #pragma unroll 1
-    for (int t = t0; t < t0 + tiles; ++t, ++tile_no) {
-      const int block = win.at(p, b, layer, h, 2 * t + mine, pages), tok0 = (2 * t + mine) * 64;
-      const uint32_t bytes = block >= 0 ? 64 * D * 2 : 0;
-#pragma unroll
-      for (int part = 0; part < 2; ++part) {
-        const bool edge = part == 1 && (tok0 + 64 > see || block < 0);          // some values must not be met
-        const uint32_t to = ring0 + r.slot * T::kSlot + mine * 8192, full = smem_u32(&sh.full[r.slot]), bar = edge ? raw : full;
+    for (int j = 0; j < tiles + 2; ++j) {
+      if (part == 0 && j >= 2) r.template next<T>();
+      const int i = part ? j - 2 : j;
+      if (i >= 0 && i < tiles) {
+        const int block = win.at(p, b, layer, h, t0 + i, pages), tok0 = (t0 + i) * KT;
+        const bool edge = part == 1 && (tok0 + KT > see || block < 0);          // some values must not be met
+        const uint32_t to = ring0 + r.slot * T::kSlot, full = smem_u32(&sh.full[r.slot]), bar = edge ? raw : full;
         if (!warp_wait(smem_u32(&sh.empty[r.slot]), r.phase ^ 1)) return false;
         if (part == 0 && lane == 0) {
-          sh.pages[tile_no & 7][mine] = block >= 0;
-          if (t == t0 && mine == 0) sh.bad[(items.no + 2 * kItems) & (4 * kItems - 1)] = 0;
+          sh.pages[tile_no & 15] = block >= 0;
+          if (i == 0) sh.bad[(items.no + 2 * kItems) & (4 * kItems - 1)] = 0;
         }
+        ++tile_no;
         __syncwarp();
-        bar_arrive_tx(lead, bar, bytes);
+        bar_arrive_tx(lead, bar, block >= 0 ? T::kSlot : 0);
         if (block >= 0) {
 #pragma unroll
-          for (int c = 0; c < D / 64; ++c) tma_load(lead, to + c * T::KT * 128, map, c * 64, block * 128 + part * 64, bar);
+          for (int c = 0; c < D / 64; ++c) tma_load(lead, to + c * KT * 128, map, c * 64, block * 128 + part * 64, bar);
         }
         if (edge) {
           if (!warp_wait(raw, raw_phase)) return false;
           raw_phase ^= 1;
           // what is behind the last token or on no page becomes 0, what only some rows see finite
-          for (int i = lane; i < 64; i += 32) {
-            const bool off = tok0 + i >= n || block < 0;
-            if (!off && tok0 + i < see) continue;
+#pragma unroll 1
+          for (int k = lane; k < KT; k += 32) {
+            const bool off = tok0 + k >= n || block < 0;
+            if (!off && tok0 + k < see) continue;
             bool any = false;
 #pragma unroll 4
             for (int ck = 0; ck < D / 8; ++ck) {
               uint4 v = make_uint4(0u, 0u, 0u, 0u);
               if (!off) {
-                v = ld_shared(to + swz(T::KT, i, ck));
+                v = ld_shared(to + swz(KT, k, ck));
                 any |= drop_non_finite(v);
               }
-              st_shared(to + swz(T::KT, i, ck), v);
+              st_shared(to + swz(KT, k, ck), v);
             }
             if (any) sh.bad[items.no & (4 * kItems - 1)] = 1;
           }
@@ -519,37 +523,43 @@ __device__ __forceinline__ bool load_role(const PagedPromptParams& p, const CUte
         }
         r.template next<T>();
       }
+      if (part == 1 && j < tiles) r.template next<T>();
     }
   }
 }
 
-// ---- quantised pages: two warps, in turn, have their bytes copied to the stages, 64 rows and their scales each
+// ---- quantised pages: a warp has the bytes of keys copied to the stages, one those of values: 64 rows and their scales each
 template <int D, int FMT>
-__device__ __forceinline__ bool fetch_role(const PagedPromptParams& p, typename Shape<D, FMT>::Sh& sh, uint32_t stage0, int mine) {
+__device__ __forceinline__ bool fetch_role(const PagedPromptParams& p, typename Shape<D, FMT>::Sh& sh, uint32_t stage0, int part) {
   using T = Shape<D, FMT>;
-  constexpr int PAGES = T::KT / 64;                // of a tile: the two warps share its pages, or else keys and values
   const int lane = threadIdx.x & 31;
   const uint32_t lead = elect_lane();
-  int stage = mine;
+  int stage = 0;
   uint32_t phase = 0;
+  auto next = [&]() {
+    if (++stage == T::kStages) {
+      stage = 0;
+      phase ^= 1;
+    }
+  };
   PageWindow win;
   Items items{0};
   Walker walk;
-  if (mine == 0) walk.begin(p, T::cut());
+  if (part == 0) walk.begin(p, T::cut());
   for (;; ++items.no) {
-    if (mine == 0 && !walk.template hand_out<T>(p, sh, items.no)) return false;
+    if (part == 0 && !walk.template hand_out<T>(p, sh, items.no)) return false;
     int last, layer, h, b, n, t0, tiles;
     if (!items.take(sh, [&](const Item& i) { last = i.last; layer = i.layer; h = i.h; b = i.b; n = i.n; t0 = i.t0; tiles = i.tiles; })) return false;
     if (last) return true;
     const int pages = (n + 63) >> 6;
-    win.begin(p, b, layer, h, t0 * PAGES, pages);
+    win.begin(p, b, layer, h, t0, pages);
 #pragma unroll 1
-    for (int t = t0; t < t0 + tiles; ++t) {
-      const int block = win.at(p, b, layer, h, t * PAGES + (PAGES > 1 ? mine : 0), pages);
-      const uint8_t* const src = p.pages + (int64_t)max(block, 0) * T::kBlock;
-#pragma unroll
-      for (int i = 0; i < PAGES; ++i) {
-        const int part = PAGES > 1 ? i : mine;
+    for (int j = 0; j < tiles + 2; ++j) {
+      if (part == 0 && j >= 2) next();
+      const int i = part ? j - 2 : j;
+      if (i >= 0 && i < tiles) {
+        const int block = win.at(p, b, layer, h, t0 + i, pages);
+        const uint8_t* const src = p.pages + (int64_t)max(block, 0) * T::kBlock;
         if (!warp_wait(smem_u32(&sh.st_empty[stage]), phase ^ 1)) return false;
         const uint32_t bar = smem_u32(&sh.st_full[stage]), dst = stage0 + stage * T::kStage;
         if (lane == 0) sh.stage_there[stage] = block >= 0;
@@ -559,12 +569,9 @@ __device__ __forceinline__ bool fetch_role(const PagedPromptParams& p, typename 
           bulk_load(lead, dst, src + part * kPageTokens * T::RB, kPageTokens * T::RB, bar);
           bulk_load(lead, dst + kPageTokens * T::RB, src + kPageTokens * (2 * T::RB + part * T::SB), kPageTokens * T::SB, bar);
         }
-        stage += 2;
-        if (stage >= T::kStages) {
-          stage -= T::kStages;
-          phase ^= 1;
-        }
+        next();
       }
+      if (part == 1 && j < tiles) next();
     }
   }
 }
@@ -607,7 +614,7 @@ __device__ __forceinline__ bool unpack_rows(uint32_t from, uint32_t to, int n, i
         uint4 hi, lo;
         int4_to_bf16(word, s2, hi, lo);
         if (drop) hi = lo = make_uint4(0u, 0u, 0u, 0u);
-        const uint32_t at = to + swz(T::KT, r0, 4 * c + kk) + u * PASS * 128;
+        const uint32_t at = to + swz(KT, r0, 4 * c + kk) + u * PASS * 128;
         st_shared(at, hi);
         st_shared(at + T::kSlot, lo);
       }
@@ -621,8 +628,8 @@ __device__ __forceinline__ bool unpack_rows(uint32_t from, uint32_t to, int n, i
         if (EDGE && row >= see) any |= drop_non_finite(v[k]);
       }
       const bool turn = c >> 2 & 1;
-      st_shared(to + swz(T::KT, r0, 2 * c + turn) + u * PASS * 128, turn ? v[1] : v[0]);
-      st_shared(to + swz(T::KT, r0, 2 * c + !turn) + u * PASS * 128, turn ? v[0] : v[1]);
+      st_shared(to + swz(KT, r0, 2 * c + turn) + u * PASS * 128, turn ? v[1] : v[0]);
+      st_shared(to + swz(KT, r0, 2 * c + !turn) + u * PASS * 128, turn ? v[0] : v[1]);
     }
   }
   return any;
@@ -640,42 +647,41 @@ __device__ __forceinline__ bool unpack_role(typename Shape<D, FMT>::Sh& sh, uint
     int last, n, see, t0, tiles;
     if (!items.take(sh, [&](const Item& i) { last = i.last; n = i.n; see = i.see[0]; t0 = i.t0; tiles = i.tiles; })) return false;
     if (last) return true;
-    for (int t = t0; t < t0 + tiles; ++t, ++tile_no) {
 #pragma unroll 1
-      for (int part = 0; part < 2; ++part) {
-        const int slot0 = r.slot;
+    for (int k = 0; k < 2 * tiles + 4; ++k) {
+      const int part = ~k & 1, i = part ? (k >> 1) - 2 : k >> 1;
+      if (i < 0 || i >= tiles) continue;
+      const int slot0 = r.slot, tok0 = (t0 + i) * KT;
 #pragma unroll
-        for (int i = 0; i < T::PARTS; ++i) {                          // (parts of a tile never wrap)
-          if (!warp_wait(smem_u32(&sh.empty[r.slot]), r.phase ^ 1)) return false;
-          r.template next<T>();
+      for (int u = 0; u < T::PARTS; ++u) {                            // (the parts of an operand never wrap)
+        if (!warp_wait(smem_u32(&sh.empty[r.slot]), r.phase ^ 1)) return false;
+        r.template next<T>();
+      }
+      if (!warp_wait(smem_u32(&sh.st_full[stage]), phase)) return false;
+      const bool here = sh.stage_there[stage] != 0;
+      const uint32_t from = stage0 + stage * T::kStage, to = ring0 + slot0 * T::kSlot;
+      bool any = false;
+      // rows that no row of queries sees become 0, values that only some see finite
+      if (!here || tok0 + KT > (part ? see : n)) any = unpack_rows<D, FMT, true>(from, to, here ? n - tok0 : 0, part ? see - tok0 : KT);
+      else unpack_rows<D, FMT, false>(from, to, KT, KT);
+      if (part == 0) {
+        if (tid == 0) {
+          sh.pages[tile_no & 15] = here;
+          if (i == 0) sh.bad[(items.no + 2 * kItems) & (4 * kItems - 1)] = 0;
         }
-        uint32_t there = 0;
-        bool any = false;
-#pragma unroll 1
-        for (int i = 0; i < T::KT / 64; ++i) {
-          const int tok0 = t * T::KT + 64 * i;
-          if (!warp_wait(smem_u32(&sh.st_full[stage]), phase)) return false;
-          const uint32_t here = sh.stage_there[stage], from = stage0 + stage * T::kStage, to = ring0 + slot0 * T::kSlot + i * 64 * 128;
-          there |= here << 8 * i;
-          // rows that no row of queries sees become 0, values that only some see finite
-          if (!here || tok0 + 64 > (part ? see : n)) any |= unpack_rows<D, FMT, true>(from, to, here ? n - tok0 : 0, part ? see - tok0 : 64);
-          else unpack_rows<D, FMT, false>(from, to, 64, 64);
-          __syncwarp();
-          if (lane == 0) bar_arrive(smem_u32(&sh.st_empty[stage]));
-          if (++stage == T::kStages) {
-            stage = 0;
-            phase ^= 1;
-          }
-        }
-        if (part == 0 && tid == 0) {
-          *(uint16_t*)sh.pages[tile_no & 7] = (uint16_t)there;
-          if (t == t0) sh.bad[(items.no + 2 * kItems) & (4 * kItems - 1)] = 0;
-        }
-        if (any) sh.bad[items.no & (4 * kItems - 1)] = 1;
-        fence_proxy_async();
-        __syncwarp();
-        if (lane == 0)
-          for (int i = 0; i < T::PARTS; ++i) bar_arrive(smem_u32(&sh.full[slot0 + i]));
+        ++tile_no;
+      }
+      if (any) sh.bad[items.no & (4 * kItems - 1)] = 1;
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) {
+        bar_arrive(smem_u32(&sh.st_empty[stage]));
+#pragma unroll
+        for (int u = 0; u < T::PARTS; ++u) bar_arrive(smem_u32(&sh.full[slot0 + u]));
+      }
+      if (++stage == T::kStages) {
+        stage = 0;
+        phase ^= 1;
       }
     }
   }
@@ -687,8 +693,7 @@ __device__ __forceinline__ bool unpack_role(typename Shape<D, FMT>::Sh& sh, uint
 template <int D, int FMT>
 __device__ __forceinline__ bool mma_role(typename Shape<D, FMT>::Sh& sh, uint32_t q0, uint32_t ring0, uint32_t tmem, int half) {
   using T = Shape<D, FMT>;
-  constexpr uint32_t kIdQK = idesc(T::KT, false), kIdPV = idesc(D, true);
-  constexpr int SUB = T::KT / 64;       // parts in which the weights of a tile arrive
+  constexpr uint32_t kIdQK = idesc(KT, false), kIdPV = idesc(D, true);
   const uint32_t lead = elect_lane();
   auto uniform = [](int v) { return __shfl_sync(0xffffffffu, v, 0); };
   half = uniform(half);
@@ -696,11 +701,11 @@ __device__ __forceinline__ bool mma_role(typename Shape<D, FMT>::Sh& sh, uint32_
   tmem = uniform(tmem);
   q0 = uniform(q0) + half * (kHalf * D * 2);
   const uint32_t full = uniform(smem_u32(sh.full)), empty = uniform(smem_u32(sh.empty));
-  const uint32_t s_full = uniform(smem_u32(&sh.s_full[half])), p_full = uniform(smem_u32(&sh.p_full[half][0]));
+  const uint32_t s_full = uniform(smem_u32(&sh.s_full[half][0])), p_full = uniform(smem_u32(&sh.p_full[half][0]));
   const uint32_t o_full = uniform(smem_u32(&sh.o_full[half])), o_done = uniform(smem_u32(&sh.o_done[half]));
   const uint32_t o_empty = uniform(smem_u32(&sh.o_empty[half])), q_full = uniform(smem_u32(&sh.q_full[half])), q_empty = uniform(smem_u32(&sh.q_empty[half]));
-  const uint32_t tS = tmem + half * T::kColS, tO = tmem + T::kColO + half * D, tQ = tmem + T::kColQ + half * (D / 2);
-  uint32_t p_phase = 0, q_phase = 0, e_phase = 1;
+  const uint32_t tS = tmem + half * 2 * KT, tO = tmem + T::kColO + half * D;
+  uint32_t p_phase = 0, q_phase = 0, e_phase = 1;      // p_phase: a bit for each of the two tiles
   Ring r{0, 0};                         // of the next operand
   auto advance = [&]() {                // (the parts of an operand never wrap)
     r.slot += T::PARTS;
@@ -724,26 +729,22 @@ __device__ __forceinline__ bool mma_role(typename Shape<D, FMT>::Sh& sh, uint32_
     }
     advance();
   };
-  auto qk = [&](bool last) {
+  auto qk = [&](int buf) {
 #pragma unroll
     for (int part = 0; part < T::PARTS; ++part) {
       const uint32_t k = desc_lo(ring0 + (r.slot + part) * T::kSlot, 16), q = desc_lo(q0, 16);
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) {
-        const uint32_t b = k + (ks >> 2) * (T::KT * 8) + (ks & 3) * 2;
-        if constexpr (T::kQTmem) mma_ts(lead, tS, tQ + ks * 8, b, kIdQK, part > 0 || ks > 0);
-        else mma_ss(lead, tS, q + (ks >> 2) * (kHalf * 8) + (ks & 3) * 2, b, kIdQK, ks > 0);
-      }
+      for (int ks = 0; ks < D / 16; ++ks)
+        mma_ss(lead, tS + buf * KT, q + (ks >> 2) * (kHalf * 8) + (ks & 3) * 2, k + (ks >> 2) * (KT * 8) + (ks & 3) * 2, kIdQK, part > 0 || ks > 0);
     }
-    mma_commit(lead, s_full);
-    if (last) mma_commit(lead, q_empty);
+    mma_commit(lead, s_full + buf * 8);
   };
-  auto pv = [&](int sub, uint32_t accumulate) {
+  auto pv = [&](int buf, uint32_t accumulate) {
 #pragma unroll
     for (int part = 0; part < T::PARTS; ++part) {
-      const uint32_t v = desc_lo(ring0 + (r.slot + part) * T::kSlot, T::KT * 128) + sub * 512;
+      const uint32_t v = desc_lo(ring0 + (r.slot + part) * T::kSlot, KT * 128);
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) mma_ts(lead, tO, tS + sub * 64 + ks * 8, v + ks * 128, kIdPV, part > 0 || ks > 0 ? 1u : accumulate);
+      for (int ks = 0; ks < 4; ++ks) mma_ts(lead, tO, tS + buf * KT + ks * 8, v + ks * 128, kIdPV, part > 0 || ks > 0 ? 1u : accumulate);
     }
     mma_commit(lead, o_full);
   };
@@ -754,36 +755,37 @@ __device__ __forceinline__ bool mma_role(typename Shape<D, FMT>::Sh& sh, uint32_
     if (uniform(last)) return true;
     tiles = uniform(tiles);
     n = uniform(n);
-    if (!wait_full()) return false;
-    if (n > 0) {
-      if (!warp_wait(q_full, q_phase)) return false;
-      q_phase ^= 1;
-      fence_after();
-      qk(n == 1);
-    }
-    release(n > 0);
 #pragma unroll 1
-    for (int i = 0; i < tiles; ++i) {
-      if (i == 0 && n > 0) {
-        if (!warp_wait(o_empty, e_phase)) return false;
-        e_phase ^= 1;
-      }
-      if (!wait_full()) return false;
-      if (i < n) {
-#pragma unroll
-        for (int sub = 0; sub < SUB; ++sub) {
-          if (!warp_wait(p_full + sub * 8, p_phase)) return false;
+    for (int j = 0; j < tiles + 2; ++j) {
+      const int buf = j & 1;
+      if (j >= 2) {                     // values of tile j - 2
+        if (!wait_full()) return false;
+        if (j - 2 < n) {
+          if (j == 2) {
+            if (!warp_wait(o_empty, e_phase)) return false;
+            e_phase ^= 1;
+          }
+          if (!warp_wait(p_full + buf * 8, p_phase >> buf & 1)) return false;
+          p_phase ^= 1u << buf;
           fence_after();
-          pv(sub, i | sub);
+          pv(buf, j - 2);
+          if (j - 1 == n) mma_commit(lead, o_done);
         }
-        p_phase ^= 1;
-        if (i + 1 == n) mma_commit(lead, o_done);
+        release(j - 2 < n);
       }
-      release(i < n);
-      if (i + 1 == tiles) break;
-      if (!wait_full()) return false;
-      if (i + 1 < n) qk(i + 2 == n);
-      release(i + 1 < n);
+      if (j < tiles) {                  // keys of tile j: S takes the place of P of tile j - 2
+        if (!wait_full()) return false;
+        if (j < n) {
+          if (j == 0) {
+            if (!warp_wait(q_full, q_phase)) return false;
+            q_phase ^= 1;
+            fence_after();
+          }
+          qk(buf);
+          if (j + 1 == n) mma_commit(lead, q_empty);
+        }
+        release(j < n);
+      }
     }
   }
 }
@@ -792,11 +794,10 @@ __device__ __forceinline__ bool mma_role(typename Shape<D, FMT>::Sh& sh, uint32_
 template <int D, int FMT>
 __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, typename Shape<D, FMT>::Sh& sh, uint32_t tmem) {
   using T = Shape<D, FMT>;
-  constexpr int KT = T::KT, C = 64;                    // columns at a time
   const int half = threadIdx.x >> 7, row = threadIdx.x & 127, lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 3;
   const uint32_t lanes = (uint32_t)(warp * 32) << 16;
-  const uint32_t tS = tmem + lanes + half * T::kColS, tO = tmem + lanes + T::kColO + half * D;
-  const uint32_t s_full = smem_u32(&sh.s_full[half]), p_full = smem_u32(&sh.p_full[half][0]), o_full = smem_u32(&sh.o_full[half]);
+  const uint32_t tS = tmem + lanes + half * 2 * KT, tO = tmem + lanes + T::kColO + half * D;
+  const uint32_t s_full = smem_u32(&sh.s_full[half][0]), p_full = smem_u32(&sh.p_full[half][0]), o_full = smem_u32(&sh.o_full[half]);
   const int s = p.by_group.div(half * kHalf + row);    // token of the row in its item
   const f32x2 scale2 = two(p.scale_log2, p.scale_log2);
   uint32_t s_phase = 0, o_phase = 0, e_phase = 1;
@@ -812,37 +813,36 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, typenam
     float m = -INFINITY, l = 0.f, lc = 0.f;            // lc: what the additions to l have lost
     bool seen = false;
 #pragma unroll 1
-    for (int c = t0 * KT; c < (t0 + end) * KT; c += C) {      // parts of 64 tokens
-      if (KT == C || c % KT == 0) {
-        if (!warp_wait(s_full, s_phase)) return false;
-        s_phase ^= 1;
-        fence_after();
-      }
-      const uint32_t tP = tS + (KT == C ? 0 : c % KT);
-      uint32_t sr[C];
+    for (int i = 0; i < end; ++i) {
+      const int buf = i & 1, tok0 = (t0 + i) * KT;
+      if (!warp_wait(s_full + buf * 8, s_phase >> buf & 1)) return false;
+      s_phase ^= 1u << buf;
+      fence_after();
+      const uint32_t tP = tS + buf * KT;
+      uint32_t sr[KT];
 #pragma unroll
-      for (int j = 0; j < C; j += 32) tmem_ld32(tP + j, sr + j);
-      const bool here = sh.pages[(tile_no + c / KT - t0) & 7][c % KT / 64];
+      for (int j = 0; j < KT; j += 32) tmem_ld32(tP + j, sr + j);
+      const bool here = sh.pages[(tile_no + i) & 15];
       tmem_wait_ld();
-      if (c + C > see || !here) {                       // some tokens are not seen
-        const int last = here ? limit - c : 0;
-        seen |= last > 0;
+      if (tok0 + KT > see || !here) {                   // some tokens are not seen
+        const int stop = here ? limit - tok0 : 0;
+        seen |= stop > 0;
 #pragma unroll
-        for (int j = 0; j < C; ++j)
-          if (j >= last) sr[j] = 0xff800000u;
+        for (int j = 0; j < KT; ++j)
+          if (j >= stop) sr[j] = 0xff800000u;
       } else {
         seen = true;
       }
       float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-      for (int j = 0; j < C; j += 8)
+      for (int j = 0; j < KT; j += 8)
 #pragma unroll
         for (int i = 0; i < 4; ++i) mx[i] = max3(mx[i], __uint_as_float(sr[j + 2 * i]), __uint_as_float(sr[j + 2 * i + 1]));
       const float m_new = fmaxf(m, max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * p.scale_log2);
       if (__any_sync(0xffffffffu, m_new > m + 8.f)) {
         const float f = m == m_new ? 1.f : ex2(m - m_new);
-        if (c > t0 * KT) {
-          if (!warp_wait(o_full, o_phase ^ 1)) return false;          // the product before this part's
+        if (i > 0) {
+          if (!warp_wait(o_full, o_phase ^ 1)) return false;          // the product before this tile's
           fence_after();
 #pragma unroll 1
           for (int k = 0; k < D; k += 32) {
@@ -861,9 +861,9 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, typenam
       const float ref = m == -INFINITY ? 0.f : -m;
       const f32x2 ref2 = two(ref, ref);
       f32x2 ls[2] = {0ull, 0ull};
-      uint32_t pk[C / 2];
+      uint32_t pk[KT / 2];
 #pragma unroll
-      for (int j = 0; j < C / 2; ++j) {
+      for (int j = 0; j < KT / 2; ++j) {
         float a, b;
         split(fma2(two(__uint_as_float(sr[2 * j]), __uint_as_float(sr[2 * j + 1])), scale2, ref2), a, b);
         a = ex2(a);
@@ -875,7 +875,7 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, typenam
       tmem_wait_st();
       fence_before();
       __syncwarp();
-      if (lane == 0) bar_arrive(p_full + (KT == C ? 0 : c % KT / 64 * 8));
+      if (lane == 0) bar_arrive(p_full + buf * 8);
       o_phase ^= 1;
       float a0, a1;
       split(add2(ls[0], ls[1]), a0, a1);
@@ -899,7 +899,6 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, typenam
 template <int D, int FMT>
 __device__ __forceinline__ bool rows_role(const PagedPromptParams& p, typename Shape<D, FMT>::Sh& sh, uint32_t q0, uint32_t tmem) {
   using T = Shape<D, FMT>;
-  constexpr int KT = T::KT;
   const int row = threadIdx.x & 127, lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 3;
   const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
   uint32_t phases = 0;                  // bit h: q_empty, 2 + h: stats_full, 4 + h: o_done
@@ -918,20 +917,7 @@ __device__ __forceinline__ bool rows_role(const PagedPromptParams& p, typename S
         fence_after();
         const int rows = half ? next.rows[1] : next.rows[0], ri = half * kHalf;
         const uint16_t* const q = (const uint16_t*)p.q.ptr + next.q_at;
-        if constexpr (T::kQTmem) {
-          const int s = p.by_group.div(ri + row);
-          const bool on = row < rows;
-          const uint4* const src = (const uint4*)(on ? q + s * p.q.ss + (ri + row - s * p.G) * p.q.sn : (const uint16_t*)p.q.ptr);
-#pragma unroll 1
-          for (int c = 0; c < D / 64; ++c) {
-            uint4 v[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = on ? int4_order(__ldg(src + c * 8 + i)) : make_uint4(0u, 0u, 0u, 0u);
-            tmem_st32(lanes + T::kColQ + half * (D / 2) + c * 32, (const uint32_t*)v);
-          }
-          tmem_wait_st();
-          fence_before();
-        } else {
+        {
           // 16-byte pieces of a row in neighbouring lanes
           constexpr int P = D / 8;
           const uint32_t dst = q0 + half * kHalf * D * 2;
@@ -940,9 +926,11 @@ __device__ __forceinline__ bool rows_role(const PagedPromptParams& p, typename S
           for (int r = row / P; r < kHalf; r += 128 / P) {
             const int s = p.by_group.div(ri + r);
             const bool on = r < rows;
-            cp_async16(dst + swz(kHalf, r, c), on ? q + s * p.q.ss + (ri + r - s * p.G) * p.q.sn + c * 8 : (const uint16_t*)p.q.ptr, on ? 16 : 0);
+            const uint16_t* const src = on ? q + s * p.q.ss + (ri + r - s * p.G) * p.q.sn + c * 8 : (const uint16_t*)p.q.ptr;
+            if constexpr (T::kInt4) st_shared(dst + swz(kHalf, r, c), on ? int4_order(__ldg((const uint4*)src)) : make_uint4(0u, 0u, 0u, 0u));
+            else cp_async16(dst + swz(kHalf, r, c), src, on ? 16 : 0);
           }
-          cp_async_wait_all();
+          if (!T::kInt4) cp_async_wait_all();
           fence_proxy_async();
         }
         __syncwarp();
@@ -950,7 +938,6 @@ __device__ __forceinline__ bool rows_role(const PagedPromptParams& p, typename S
       }
     }
     if (!it.last) {
-      const bool mend = sh.bad[(items.no - 1) & (4 * kItems - 1)] != 0;
       float* const rec = (float*)p.records + (2 * blockIdx.x + it.first) * prompt_record_floats(kItemRows, D);
 #pragma unroll 1
       for (int half = 0; half < 2; ++half) {
@@ -965,6 +952,7 @@ __device__ __forceinline__ bool rows_role(const PagedPromptParams& p, typename S
           phases ^= 20u << half;
           fence_after();
         }
+        const bool mend = *(volatile uint8_t*)&sh.bad[(items.no - 1) & (4 * kItems - 1)] != 0;      // (behind the waits)
         const int ri = half * kHalf + row, s = p.by_group.div(ri), g = ri - s * p.G;
         const bool none = m == -INFINITY && l == 0.f;
         const float f = none ? 0.f : m == -INFINITY ? __int_as_float(0x7fffffff) : 1.f / l;
@@ -1057,13 +1045,14 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
   if (T::kPlain && tid == 32) asm volatile("prefetch.tensormap [%0];" :: "l"(&map) : "memory");
   if (tid == 0) {
     for (int i = 0; i < T::kSlots; ++i) {
-      bar_init(smem_u32(&sh.full[i]), T::kLoadWarps);
+      bar_init(smem_u32(&sh.full[i]), T::kPlain ? 1 : 4);
       bar_init(smem_u32(&sh.empty[i]), 2);
     }
     for (int i = 0; i < 2; ++i) {
-      bar_init(smem_u32(&sh.s_full[i]), 1);
-      bar_init(smem_u32(&sh.p_full[i][0]), 4);
-      bar_init(smem_u32(&sh.p_full[i][1]), 4);
+      for (int k = 0; k < 2; ++k) {
+        bar_init(smem_u32(&sh.s_full[i][k]), 1);
+        bar_init(smem_u32(&sh.p_full[i][k]), 4);
+      }
       bar_init(smem_u32(&sh.o_full[i]), 1);
       bar_init(smem_u32(&sh.o_done[i]), 1);
       bar_init(smem_u32(&sh.o_empty[i]), 4);
@@ -1075,11 +1064,10 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
       bar_init(smem_u32(&sh.item_full[i]), 1);
       bar_init(smem_u32(&sh.item_empty[i]), 8 + 2 + 2 + 4 + (T::kPlain ? 0 : 4));       // softmax, products, loads, rows, unpacking
     }
-    bar_init(smem_u32(&sh.raw[0]), 1);
-    bar_init(smem_u32(&sh.raw[1]), 1);
+    bar_init(smem_u32(&sh.raw), 1);
     for (int i = 0; i < T::kStages; ++i) {
       bar_init(smem_u32(&sh.st_full[i]), 1);
-      bar_init(smem_u32(&sh.st_empty[i]), T::kLoadWarps);
+      bar_init(smem_u32(&sh.st_empty[i]), 4);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     sh.failed = 0;
@@ -1099,7 +1087,7 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
   } else {
     if (T::kPlain || warp < 12) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(T::kLoadRegs));
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(T::kMmaRegs));
-    if (warp < 8 + T::kLoadWarps) {
+    if (warp < (T::kPlain ? 10 : 12)) {
       if constexpr (T::kPlain) ok = load_role<D, FMT>(p, &map, sh, ring0, warp - 8);
       else ok = unpack_role<D, FMT>(sh, ring0, stage0);
     } else if (!T::kPlain && warp >= T::kFetchWarp && warp < T::kFetchWarp + 2) {
@@ -1149,7 +1137,7 @@ cudaError_t launch(const PagedPromptParams& p, const CUtensorMap& map, cudaStrea
 
 }  // namespace
 
-PromptCut paged_prompt_tc_cut(int format) { return PromptCut{format == THINK_PAGE_INT4 ? 64 : 128, kExtra}; }
+PromptCut paged_prompt_tc_cut() { return PromptCut{KT, kExtra}; }
 int paged_prompt_tc_rows() { return kItemRows; }
 
 cudaError_t paged_prompt_tc_setup(int format, int D) {

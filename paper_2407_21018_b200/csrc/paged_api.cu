@@ -361,7 +361,7 @@ thinK_status thinK_paged_prompt_attn(thinK_paged* p, thinK_tensor5 q, thinK_tens
   d.per = paged_prompt_rows(p->g.dtype) / p->g.G;
   // positions fit 32 bits; so do the items of a sequence, and all places of the line 62
   const int64_t tokens = (int64_t)table.max_pages * kPageTokens;
-  const PromptCut cut = paged_prompt_cut(p->g.dtype, p->g.format);
+  const PromptCut cut = paged_prompt_cut(p->g.dtype);
   const double items = (double)max_rows / d.per + 1;
   if (tokens + max_rows > INT32_MAX || (int64_t)nlayers * p->g.g.N_kv > INT32_MAX ||
       items * ((double)tokens + max_rows + cut.extra) * table.B * nlayers * p->g.g.N_kv > 4.0e15) return THINK_ERR_UNSUPPORTED;

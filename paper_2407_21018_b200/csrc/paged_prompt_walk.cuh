@@ -38,12 +38,12 @@ __host__ __device__ inline size_t prompt_record_floats(int rows, int D) { return
 cudaError_t launch_paged_prompt(const PagedPromptParams& p, int dtype, int format, const void* map, cudaStream_t s);
 cudaError_t paged_prompt_setup(int dtype, int format, int D);       // kernel attributes on the current device
 int paged_prompt_rows(int dtype);                                   // query rows of an item
-PromptCut paged_prompt_cut(int dtype, int format);
+PromptCut paged_prompt_cut(int dtype);
 
 cudaError_t launch_paged_prompt_tc(const PagedPromptParams& p, int format, const void* map, cudaStream_t s);
 cudaError_t paged_prompt_tc_setup(int format, int D);
 int paged_prompt_tc_rows();
-PromptCut paged_prompt_tc_cut(int format);
+PromptCut paged_prompt_tc_cut();
 
 #ifdef __CUDACC__
 struct PromptSeq {
