@@ -205,7 +205,7 @@ constexpr int kItems = 2;                // handed out and not yet taken by all
 template <int SLOTS, int STAGES>
 struct Shared {
   // full, empty: a slot holds an operand, may be overwritten.  s_full, p_full: S of a half is there, P is (two tiles each).
-  // o_full: a tile's product has been added to O; o_done: the item's last; o_empty: O has been read.  q_full, q_empty: the
+  // o_done: the item's last product has been added to O; o_full: the last but one; o_empty: O has been read.  q_full, q_empty: the
   // same of the queries.  stats_full: m and l.
   uint64_t full[SLOTS], empty[SLOTS], s_full[2][2], p_full[2][2], o_full[2], o_done[2], o_empty[2], q_full[2], q_empty[2], stats_full[2], raw;
   uint64_t st_full[STAGES], st_empty[STAGES], item_full[kItems], item_empty[kItems];
@@ -225,16 +225,16 @@ template <int D, int FMT>
 struct Shape {
   static constexpr bool kInt4 = FMT == THINK_PAGE_INT4, kPlain = FMT == THINK_PAGE_PLAIN;
   static constexpr int PARTS = kInt4 ? 2 : 1;                 // bf16 operands that a key or value is the sum of
-  static constexpr int kSlot = KT * D * 2, kQBytes = 2 * kHalf * D * 2;
+  static constexpr int kPart = KT * D * 2, kSlot = PARTS * kPart, kQBytes = 2 * kHalf * D * 2;
   static constexpr int RB = kPlain ? D * 2 : kInt4 ? D / 2 : D;       // bytes of a stored row
   static constexpr int SB = kPlain ? 0 : kInt4 ? D / 16 : 1;          // bytes of its scales
   // quantised pages: 64 stored rows and their scales a stage
   static constexpr int kBlock = 2 * kPageTokens * (RB + SB), kStage = kPlain ? 0 : kBlock / 2;
   static constexpr int kStages = kPlain ? 2 : 4;              // (of no bytes with bf16 pages)
-  static constexpr int kSlots = D == 64 ? 16 : kPlain ? 10 : 8;
+  static constexpr int kSlots = (D == 64 ? 16 : kPlain ? 10 : 8) / PARTS;
   using Sh = Shared<kSlots, kStages>;
   static constexpr int kStageAt = kQBytes + kSlots * kSlot, kSharedAt = kStageAt + kStages * kStage, kSmem = kSharedAt + (int)sizeof(Sh);
-  static_assert(kSharedAt % 16 == 0 && kSmem <= kMaxSmem && kSlots % PARTS == 0, "shared memory");
+  static_assert(kSharedAt % 16 == 0 && kSmem <= kMaxSmem, "shared memory");
   // warpgroups: two halves' softmax; bf16 pages: loads and products, else unpacking, then products and fetching; rows
   static constexpr int kGroups = kPlain ? 4 : 5, kThreads = 128 * kGroups;
   static constexpr int kMmaWarp = kPlain ? 10 : 12, kFetchWarp = 14, kRowsWarp = kPlain ? 12 : 16;
@@ -616,7 +616,7 @@ __device__ __forceinline__ bool unpack_rows(uint32_t from, uint32_t to, int n, i
         if (drop) hi = lo = make_uint4(0u, 0u, 0u, 0u);
         const uint32_t at = to + swz(KT, r0, 4 * c + kk) + u * PASS * 128;
         st_shared(at, hi);
-        st_shared(at + T::kSlot, lo);
+        st_shared(at + T::kPart, lo);
       }
     } else {
       const float sc = e8m0(sb[u]);
@@ -652,11 +652,8 @@ __device__ __forceinline__ bool unpack_role(typename Shape<D, FMT>::Sh& sh, uint
       const int part = ~k & 1, i = part ? (k >> 1) - 2 : k >> 1;
       if (i < 0 || i >= tiles) continue;
       const int slot0 = r.slot, tok0 = (t0 + i) * KT;
-#pragma unroll
-      for (int u = 0; u < T::PARTS; ++u) {                            // (the parts of an operand never wrap)
-        if (!warp_wait(smem_u32(&sh.empty[r.slot]), r.phase ^ 1)) return false;
-        r.template next<T>();
-      }
+      if (!warp_wait(smem_u32(&sh.empty[slot0]), r.phase ^ 1)) return false;
+      r.template next<T>();
       if (!warp_wait(smem_u32(&sh.st_full[stage]), phase)) return false;
       const bool here = sh.stage_there[stage] != 0;
       const uint32_t from = stage0 + stage * T::kStage, to = ring0 + slot0 * T::kSlot;
@@ -676,8 +673,7 @@ __device__ __forceinline__ bool unpack_role(typename Shape<D, FMT>::Sh& sh, uint
       __syncwarp();
       if (lane == 0) {
         bar_arrive(smem_u32(&sh.st_empty[stage]));
-#pragma unroll
-        for (int u = 0; u < T::PARTS; ++u) bar_arrive(smem_u32(&sh.full[slot0 + u]));
+        bar_arrive(smem_u32(&sh.full[slot0]));
       }
       if (++stage == T::kStages) {
         stage = 0;
@@ -707,32 +703,16 @@ __device__ __forceinline__ bool mma_role(typename Shape<D, FMT>::Sh& sh, uint32_
   const uint32_t tS = tmem + half * 2 * KT, tO = tmem + T::kColO + half * D;
   uint32_t p_phase = 0, q_phase = 0, e_phase = 1;      // p_phase: a bit for each of the two tiles
   Ring r{0, 0};                         // of the next operand
-  auto advance = [&]() {                // (the parts of an operand never wrap)
-    r.slot += T::PARTS;
-    if (r.slot >= T::kSlots) {
-      r.slot -= T::kSlots;
-      r.phase ^= 1;
-    }
-  };
-  auto wait_full = [&]() {
-#pragma unroll
-    for (int i = 0; i < T::PARTS; ++i)
-      if (!warp_wait(full + (r.slot + i) * 8, r.phase)) return false;
-    return true;
-  };
   // this half is through with the operand: behind its products, or where it has none, now
   auto release = [&](bool used) {
-#pragma unroll
-    for (int i = 0; i < T::PARTS; ++i) {
-      if (used) mma_commit(lead, empty + (r.slot + i) * 8);
-      else if (lead) bar_arrive(empty + (r.slot + i) * 8);
-    }
-    advance();
+    if (used) mma_commit(lead, empty + r.slot * 8);
+    else if (lead) bar_arrive(empty + r.slot * 8);
+    r.template next<T>();
   };
   auto qk = [&](int buf) {
 #pragma unroll
     for (int part = 0; part < T::PARTS; ++part) {
-      const uint32_t k = desc_lo(ring0 + (r.slot + part) * T::kSlot, 16), q = desc_lo(q0, 16);
+      const uint32_t k = desc_lo(ring0 + r.slot * T::kSlot + part * T::kPart, 16), q = desc_lo(q0, 16);
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks)
         mma_ss(lead, tS + buf * KT, q + (ks >> 2) * (kHalf * 8) + (ks & 3) * 2, k + (ks >> 2) * (KT * 8) + (ks & 3) * 2, kIdQK, part > 0 || ks > 0);
@@ -742,11 +722,10 @@ __device__ __forceinline__ bool mma_role(typename Shape<D, FMT>::Sh& sh, uint32_
   auto pv = [&](int buf, uint32_t accumulate) {
 #pragma unroll
     for (int part = 0; part < T::PARTS; ++part) {
-      const uint32_t v = desc_lo(ring0 + (r.slot + part) * T::kSlot, KT * 128);
+      const uint32_t v = desc_lo(ring0 + r.slot * T::kSlot + part * T::kPart, KT * 128);
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks) mma_ts(lead, tO, tS + buf * KT + ks * 8, v + ks * 128, kIdPV, part > 0 || ks > 0 ? 1u : accumulate);
     }
-    mma_commit(lead, o_full);
   };
   Items items{0};
   for (;; ++items.no) {
@@ -759,7 +738,7 @@ __device__ __forceinline__ bool mma_role(typename Shape<D, FMT>::Sh& sh, uint32_
     for (int j = 0; j < tiles + 2; ++j) {
       const int buf = j & 1;
       if (j >= 2) {                     // values of tile j - 2
-        if (!wait_full()) return false;
+        if (!warp_wait(full + r.slot * 8, r.phase)) return false;
         if (j - 2 < n) {
           if (j == 2) {
             if (!warp_wait(o_empty, e_phase)) return false;
@@ -769,12 +748,13 @@ __device__ __forceinline__ bool mma_role(typename Shape<D, FMT>::Sh& sh, uint32_
           p_phase ^= 1u << buf;
           fence_after();
           pv(buf, j - 2);
+          if (j == n) mma_commit(lead, o_full);         // of the last tile but one: see the softmax
           if (j - 1 == n) mma_commit(lead, o_done);
         }
         release(j - 2 < n);
       }
       if (j < tiles) {                  // keys of tile j: S takes the place of P of tile j - 2
-        if (!wait_full()) return false;
+        if (!warp_wait(full + r.slot * 8, r.phase)) return false;
         if (j < n) {
           if (j == 0) {
             if (!warp_wait(q_full, q_phase)) return false;
@@ -842,7 +822,9 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, typenam
       if (__any_sync(0xffffffffu, m_new > m + 8.f)) {
         const float f = m == m_new ? 1.f : ex2(m - m_new);
         if (i > 0) {
-          if (!warp_wait(o_full, o_phase ^ 1)) return false;          // the product before this tile's
+          // the product before this tile's is done when the logits of the next tile are, which are computed behind it; in the
+          // last tile it has a barrier of its own
+          if (!(i + 1 < end ? warp_wait(s_full + (buf ^ 1) * 8, s_phase >> (buf ^ 1) & 1) : warp_wait(o_full, o_phase))) return false;
           fence_after();
 #pragma unroll 1
           for (int k = 0; k < D; k += 32) {
@@ -876,7 +858,6 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, typenam
       fence_before();
       __syncwarp();
       if (lane == 0) bar_arrive(p_full + buf * 8);
-      o_phase ^= 1;
       float a0, a1;
       split(add2(ls[0], ls[1]), a0, a1);
       const float add = (a0 + a1) - lc, sum = l + add;
@@ -884,6 +865,7 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, typenam
       l = sum;
     }
     tile_no += tiles;
+    if (end > 1) o_phase ^= 1;
     if (end > 0) {
       if (!warp_wait(smem_u32(&sh.o_empty[half]), e_phase)) return false;     // the last item's have been read
       e_phase ^= 1;

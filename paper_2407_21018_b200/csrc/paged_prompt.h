@@ -47,9 +47,9 @@ struct PromptCut {
     return j < 1 ? 1 : j;
   }
   // Parts of a line: all there are for long ones; for short ones as many as items (what a small item costs is latency) and
-  // one more for every four tiles (joining pieces costs, too).  A part may be without a tile.
+  // one more for every 512 tokens (joining pieces costs, too).  A part may be without a tile.
   THINK_HD int parts(int64_t total, int64_t items, int most) const {
-    const int64_t n = items + (total >> (tile == 64 ? 8 : 9));
+    const int64_t n = items + ((total - items * extra) >> 9);
     return n < most ? (int)n : most;
   }
 };
