@@ -695,6 +695,9 @@ class PagedKVCache:
 # ---------------------------------------------------------------------------
 # Rotary positions
 # ---------------------------------------------------------------------------
+_NO_VIEW = Tensor5(None, 0, 0, 0, 0)
+
+
 class Rope:
     """Rotary positions of queries and keys (see thinK_rope_apply): layout ROPE_HALVES or ROPE_PAIRS, scaling ROPE_PLAIN,
     ROPE_LINEAR, ROPE_NTK, ROPE_YARN or ROPE_BANDS."""
@@ -714,13 +717,21 @@ class Rope:
         """Radians per token of a pair, -1 if there is no such pair."""
         return float(lib.thinK_rope_frequency(self.handle, pair))
 
-    def _view(self, x: torch.Tensor, like: torch.Tensor, what: str):
-        """[b, s, l, n, d] view of a padded or packed ([s, l, n, d]) tensor."""
-        if (x.dtype is not self.torch_dtype or x.dim() not in (4, 5) or x.dim() != like.dim() or x.shape[-1] != self._D
-                or x.stride(-1) != 1 or x.get_device() != like.get_device() or x.get_device() < 0 or x.shape[:-2] != like.shape[:-2]):
+    def _side(self, x: torch.Tensor, y: Optional[torch.Tensor], lead, index: int, what: str):
+        """Heads and [b, s, l, n, d] views of queries or keys and of where they go; packed tensors ([s, l, n, d]) have one entry."""
+        shape, st = x.shape, x.stride()
+        if (x.dtype is not self.torch_dtype or shape[-1] != self._D or st[-1] != 1 or x.get_device() != index
+                or shape[:-2] != lead):
             raise ThinKError(ERR_INVALID_ARG, "thinK_rope_apply: " + what)
-        s = x.stride()
-        return Tensor5(x.data_ptr(), *s[:4]) if len(s) == 5 else Tensor5(x.data_ptr(), 0, *s[:3])
+        packed = len(st) == 4
+        a = Tensor5(x.data_ptr(), 0, st[0], st[1], st[2]) if packed else Tensor5(x.data_ptr(), st[0], st[1], st[2], st[3])
+        if y is None or y is x:
+            return shape[-2], x, a, a
+        st = y.stride()
+        if y.dtype is not self.torch_dtype or y.shape != shape or st[-1] != 1 or y.get_device() != index:
+            raise ThinKError(ERR_INVALID_ARG, "thinK_rope_apply: " + what + "_out")
+        return shape[-2], y, a, (Tensor5(y.data_ptr(), 0, st[0], st[1], st[2]) if packed else
+                                 Tensor5(y.data_ptr(), st[0], st[1], st[2], st[3]))
 
     def apply(self, q: Optional[torch.Tensor], k: Optional[torch.Tensor], pos: torch.Tensor, rows: Optional[torch.Tensor] = None,
               q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, transpose=False, stream=None):
@@ -729,52 +740,42 @@ class Rope:
         [tokens, L, N, D] go with pos [tokens]."""
         where = "thinK_rope_apply"
         like = q if q is not None else k
-        if like is None:
+        if like is None or (q is None and q_out is not None) or (k is None and k_out is not None):
             raise ThinKError(ERR_INVALID_ARG, where)
-        index = like.get_device()
-        views, heads, outs = [], [], []
-        for x, y, what in ((q, q_out, "q"), (k, k_out, "k")):
-            if x is None:
-                if y is not None:
-                    raise ThinKError(ERR_INVALID_ARG, where + ": " + what)
-                views.append((Tensor5(), Tensor5()))
-                heads.append(0)
-                outs.append(None)
-                continue
-            a = self._view(x, like, what)
-            if y is None:
-                y, b = x, a
-            else:
-                b = self._view(y, like, what + "_out")
-                if y.shape != x.shape:
-                    raise ThinKError(ERR_INVALID_ARG, where + ": " + what + "_out")
-            views.append((a, b))
-            heads.append(x.shape[-2])
-            outs.append(y)
-        shape = like.shape
-        B, S, L = shape[:3] if len(shape) == 5 else (1,) + tuple(shape[:2])
-        if pos.dtype is not _INT32 or pos.get_device() != index or max(B, S, L, *heads) >> 31:
+        lead, index = like.shape[:-2], like.get_device()
+        dims = len(lead)
+        if index < 0 or dims not in (2, 3):
+            raise ThinKError(ERR_INVALID_ARG, where)
+        N_q = N_kv = 0
+        qa = qb = ka = kb = _NO_VIEW
+        if q is not None:
+            N_q, q_out, qa, qb = self._side(q, q_out, lead, index, "q")
+        if k is not None:
+            N_kv, k_out, ka, kb = self._side(k, k_out, lead, index, "k")
+        B, S, L = lead if dims == 3 else (1, lead[0], lead[1])
+        st, own = pos.stride(), pos.shape                  # positions: of every row, or of row 0
+        if pos.dtype is not _INT32 or pos.get_device() != index or (B | S | L | N_q | N_kv) >> 31:
             raise ThinKError(ERR_INVALID_ARG, where + ": pos")
-        if len(shape) == 4:
-            if pos.dim() != 1 or pos.shape[0] < S or (S > 1 and pos.stride(0) != 1):
-                raise ThinKError(ERR_INVALID_ARG, where + ": pos")
-            stride = max(S, 1)
-        elif pos.dim() == 2:
-            if pos.shape[0] < B or pos.shape[1] < S or (S > 1 and pos.stride(1) != 1) or (B > 1 and pos.stride(0) < max(S, 1)):
-                raise ThinKError(ERR_INVALID_ARG, where + ": pos")
-            stride = pos.stride(0) if B > 1 else max(S, 1)
+        if dims == 2 or len(own) == 2:
+            stride = S if S > 0 else 1
+            if dims == 2:
+                ok = len(own) == 1 and own[0] >= S and (S < 2 or st[0] == 1)
+            else:
+                ok = own[0] >= B and own[1] >= S and (S < 2 or st[1] == 1) and (B < 2 or st[0] >= stride)
+                if B > 1:
+                    stride = st[0]
         else:
-            if pos.dim() != 1 or pos.shape[0] < B or (B > 1 and pos.stride(0) != 1):
-                raise ThinKError(ERR_INVALID_ARG, where + ": pos")
             stride = 0
+            ok = len(own) == 1 and own[0] >= B and (B < 2 or st[0] == 1)
+        if not ok:
+            raise ThinKError(ERR_INVALID_ARG, where + ": pos")
         count = None
         if rows is not None:
             if rows.dtype is not _INT32 or rows.dim() != 1 or rows.shape[0] < B or rows.get_device() != index or (B > 1 and rows.stride(0) != 1):
                 raise ThinKError(ERR_INVALID_ARG, where + ": rows")
             count = rows.data_ptr()
         raw = _raw_stream(index) if stream is None else stream.cuda_stream
-        args = (self.handle, views[0][0], views[1][0], views[0][1], views[1][1], B, S, L, heads[0], heads[1], pos.data_ptr(), stride,
-                count, int(bool(transpose)), raw)
+        args = (self.handle, qa, ka, qb, kb, B, S, L, N_q, N_kv, pos.data_ptr(), stride, count, 1 if transpose else 0, raw)
         if _current_device() == index:
             status = lib.thinK_rope_apply(*args)
         else:
@@ -782,7 +783,7 @@ class Rope:
                 status = lib.thinK_rope_apply(*args)
         if status != THINK_OK:
             raise ThinKError(status, where)
-        return outs[0], outs[1]
+        return q_out, k_out
 
     def __del__(self):
         try:

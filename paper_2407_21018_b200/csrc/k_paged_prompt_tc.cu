@@ -24,7 +24,7 @@ namespace think {
 namespace {
 
 constexpr int kHalf = 128, kItemRows = 2 * kHalf;
-constexpr int kExtra = 256;             // places of an item besides its tokens: what starting and ending one costs
+constexpr int kExtra = 256, kShare = 9; // see PromptCut: starting and ending an item costs as much as four tiles
 
 // ---- PTX
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -243,7 +243,7 @@ struct Shape {
   static_assert(2 * kSoftmaxRegs + kLoadRegs + (kPlain ? 0 : kMmaRegs) + kRowsRegs <= kRegs * kGroups, "more registers than the block has: a wait without end");
   // tensor memory: S of each half, twice, O of each half
   static constexpr int kColO = 4 * KT;
-  static __host__ __device__ constexpr PromptCut cut() { return PromptCut{KT, kExtra}; }
+  static __host__ __device__ constexpr PromptCut cut() { return PromptCut{kExtra, kShare}; }
 };
 
 // byte offset of 16-byte chunk ck of row r in an operand of `rows` rows: 64-channel blocks of 128-byte rows, swizzled
@@ -1119,7 +1119,7 @@ cudaError_t launch(const PagedPromptParams& p, const CUtensorMap& map, cudaStrea
 
 }  // namespace
 
-PromptCut paged_prompt_tc_cut() { return PromptCut{KT, kExtra}; }
+PromptCut paged_prompt_tc_cut() { return PromptCut{kExtra, kShare}; }
 int paged_prompt_tc_rows() { return kItemRows; }
 
 cudaError_t paged_prompt_tc_setup(int format, int D) {

@@ -37,19 +37,19 @@ THINK_HD int prompt_quotient(int64_t place, int64_t length) {
 }
 
 struct PromptCut {
-  int tile, extra;            // tokens of a tile (64 or 128), places of an item besides its tokens
-  // tile j stands at slot(j) of its item
+  int extra, share;           // places of an item besides its tokens; tokens that are worth a part of their own in short calls, log 2
+  static constexpr int tile = 64;       // tokens; tile j stands at slot(j) of its item
   THINK_HD int64_t slot(int64_t j) const { return j == 0 ? 0 : extra + tile * j; }
   THINK_HD int64_t first_tile(int64_t x) const {        // that stands at x or behind
     if (x <= 0) return 0;
     const uint64_t y = (uint64_t)(x - extra + tile - 1 > 0 ? x - extra + tile - 1 : 0);
-    const int64_t j = (int64_t)(y >> (tile == 64 ? 6 : 7));
+    const int64_t j = (int64_t)(y >> 6);
     return j < 1 ? 1 : j;
   }
   // Parts of a line: all there are for long ones; for short ones as many as items (what a small item costs is latency) and
-  // one more for every 512 tokens (joining pieces costs, too).  A part may be without a tile.
+  // some more for long items (joining pieces costs, too).  A part may be without a tile.
   THINK_HD int parts(int64_t total, int64_t items, int most) const {
-    const int64_t n = items + ((total - items * extra) >> 9);
+    const int64_t n = items + ((total - items * extra) >> share);
     return n < most ? (int)n : most;
   }
 };
