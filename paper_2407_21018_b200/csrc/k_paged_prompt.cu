@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(kThreads) k_paged_prompt_simple(const PagedPro
 }
 
 // Joins the pieces of the items that were cut, in their order: a warp per row, the states' statistics over its lanes.
-constexpr int kJoinWarps = 8;
+constexpr int kJoinWarps = 32;
 template <int D, int E, int ROWS>
 __global__ void __launch_bounds__(32 * kJoinWarps) k_paged_prompt_join(const PagedPromptParams p) {
   constexpr int W = D / 32;                         // channels of a lane
