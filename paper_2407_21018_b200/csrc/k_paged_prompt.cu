@@ -13,51 +13,9 @@ namespace {
 constexpr int kRows = 64, kTile = 64, kThreads = 256;
 constexpr int kExtra = 64, kShare = 7;  // see PromptCut
 
-// four channels of a stored row
-template <int D, int E, int FMT>
-__device__ __forceinline__ float4 load_stored(const uint8_t* block, int part, int slot, int c) {
-  constexpr int RB = FMT == THINK_PAGE_PLAIN ? D * E : FMT == THINK_PAGE_E4M3 ? D : D / 2;
-  constexpr int SB = FMT == THINK_PAGE_PLAIN ? 0 : FMT == THINK_PAGE_E4M3 ? 1 : D / 16;
-  const uint8_t* const row = block + (part * kPageTokens + slot) * RB;
-  const uint8_t* const sc = block + 2 * kPageTokens * RB + (part * kPageTokens + slot) * SB;
-  if constexpr (FMT == THINK_PAGE_PLAIN && E == 4) {
-    return *(const float4*)(row + c * 4);
-  } else if constexpr (FMT == THINK_PAGE_PLAIN) {
-    const uint2 w = *(const uint2*)(row + c * 2);
-    return make_float4(bf16lo(w.x), bf16hi(w.x), bf16lo(w.y), bf16hi(w.y));
-  } else if constexpr (FMT == THINK_PAGE_E4M3) {
-    const uint32_t w = *(const uint32_t*)(row + c);
-    const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xffffu), __NV_E4M3);
-    const __half2_raw b = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3);
-    const float2 x = __half22float2(*(const __half2*)&a), y = __half22float2(*(const __half2*)&b);
-    const float s = e8m0(*sc);
-    return make_float4(x.x * s, x.y * s, y.x * s, y.y * s);
-  } else {
-    const uint32_t w = *(const uint16_t*)(row + c / 2);
-    const float s = __uint_as_float((uint32_t)((const uint16_t*)sc)[c / kGroupChannels] << 16);
-    return make_float4(((int)(w & 15) - 8) * s, ((int)((w >> 4) & 15) - 8) * s, ((int)((w >> 8) & 15) - 8) * s, ((int)(w >> 12) - 8) * s);
-  }
-}
-
-template <int E>
-__device__ __forceinline__ float4 load4(const void* base, int64_t e) {
-  if constexpr (E == 4) return *(const float4*)((const float*)base + e);
-  const uint2 w = *(const uint2*)((const uint16_t*)base + e);
-  return make_float4(bf16lo(w.x), bf16hi(w.x), bf16lo(w.y), bf16hi(w.y));
-}
-template <int E>
-__device__ __forceinline__ void store4(void* base, int64_t e, const float4& x) {
-  if constexpr (E == 4) {
-    *(float4*)((float*)base + e) = x;
-  } else {
-    const __nv_bfloat162 a = __floats2bfloat162_rn(x.x, x.y), b = __floats2bfloat162_rn(x.z, x.w);
-    *(uint2*)((uint16_t*)base + e) = make_uint2(*(const uint32_t*)&a, *(const uint32_t*)&b);
-  }
-}
-
 // A thread owns 4 rows (4 ty ..) and, of the logits, the tokens tx + 16 j, of the outputs the channels 4 tx + 64 j.
-template <int D, int E, int FMT>
-__global__ void __launch_bounds__(kThreads) k_paged_prompt_simple(const PagedPromptParams p) {
+template <int D>
+__global__ void __launch_bounds__(kThreads) k_paged_prompt_fp32(const PagedPromptParams p) {
   constexpr int RS = D + 4, PS = kTile + 4;         // row strides that keep 16-byte reads of neighbouring rows apart
   constexpr int J = D / 64;
   const PromptCut cut{kExtra, kShare};
@@ -83,7 +41,7 @@ __global__ void __launch_bounds__(kThreads) k_paged_prompt_simple(const PagedPro
     for (int i = tid; i < kRows * (D / 4); i += kThreads) {
       const int r = i / (D / 4), c = 4 * (i % (D / 4)), s = p.by_group.div(r), g = r - s * p.G;
       float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (r < rows) f = load4<E>(p.q.ptr, prompt_row(p, p.q, w.b, w.s, x.s0 + s) + ll * p.q.sl + (h * p.G + g) * p.q.sn + c);
+      if (r < rows) f = *(const float4*)((const float*)p.q.ptr + prompt_row(p, p.q, w.b, w.s, x.s0 + s) + ll * p.q.sl + (h * p.G + g) * p.q.sn + c);
       *(float4*)(sq + r * RS + c) = make_float4(f.x * p.scale_log2, f.y * p.scale_log2, f.z * p.scale_log2, f.w * p.scale_log2);
     }
     int limit[4];                                   // tokens that a row sees
@@ -109,13 +67,13 @@ __global__ void __launch_bounds__(kThreads) k_paged_prompt_simple(const PagedPro
       const int page = tok0 < x.n ? page_of(p.table, p.g, w.b, tok0, p.error) : -1;
       if (page < 0) continue;                       // (the same in every thread)
       __syncthreads();                              // the last tile, and the queries' place, are no longer read
-      const uint8_t* const block = p.pages + page_block_offset(p.g, p.layer0 + ll, page, h);
+      const float* const block = (const float*)(p.pages + page_block_offset(p.g, p.layer0 + ll, page, h));
       for (int i = tid; i < kTile * (D / 4); i += kThreads) {
         const int r = i / (D / 4), c = 4 * (i % (D / 4));
         float4 k = make_float4(0.f, 0.f, 0.f, 0.f), v = k;
         if (tok0 + r < x.n) {
-          k = load_stored<D, E, FMT>(block, 0, r, c);
-          v = load_stored<D, E, FMT>(block, 1, r, c);
+          k = *(const float4*)(block + r * D + c);
+          v = *(const float4*)(block + (kPageTokens + r) * D + c);
         }
         *(float4*)(sk + r * RS + c) = k;
         *(float4*)(sv + r * RS + c) = v;
@@ -201,8 +159,8 @@ __global__ void __launch_bounds__(kThreads) k_paged_prompt_simple(const PagedPro
         const int64_t at = prompt_row(p, p.out, w.b, w.s, x.s0 + s) + ll * p.out.sl + head * p.out.sn + 4 * tx;
 #pragma unroll
         for (int j = 0; j < J; ++j)
-          store4<E>((void*)p.out.ptr, at + 64 * j,
-                    none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o[a][j].x * f, o[a][j].y * f, o[a][j].z * f, o[a][j].w * f));
+          *(float4*)((float*)p.out.ptr + at + 64 * j) =
+              none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o[a][j].x * f, o[a][j].y * f, o[a][j].z * f, o[a][j].w * f);
         if (p.lse && tx == 0) p.lse[(prompt_lse_row(p, w.b, w.s, x.s0 + s) * p.nlayers + ll) * p.N_q + head] = prompt_log_sum(m[a], l[a]);
       } else {
 #pragma unroll
@@ -300,11 +258,11 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_paged_prompt_join(const Pag
 }
 
 template <int D>
-constexpr size_t simple_smem() { return sizeof(float) * (size_t)((kRows + 2 * kTile) * (D + 4) + kRows * (kTile + 4)); }
+constexpr size_t fp32_smem() { return sizeof(float) * (size_t)((kRows + 2 * kTile) * (D + 4) + kRows * (kTile + 4)); }
 
 template <int D>
-cudaError_t launch_simple(const PagedPromptParams& p, cudaStream_t s) {
-  const cudaError_t e = launch_dependent(k_paged_prompt_simple<D, 4, THINK_PAGE_PLAIN>, dim3(p.grid), kThreads, simple_smem<D>(), s, p);
+cudaError_t launch_fp32(const PagedPromptParams& p, cudaStream_t s) {
+  const cudaError_t e = launch_dependent(k_paged_prompt_fp32<D>, dim3(p.grid), kThreads, fp32_smem<D>(), s, p);
   return e != cudaSuccess ? e : launch_dependent(k_paged_prompt_join<D, 4, kRows>, dim3(p.grid, kRows / kJoinWarps), 32 * kJoinWarps, 0, s, p);
 }
 template <int D>
@@ -313,22 +271,22 @@ cudaError_t launch_tc(const PagedPromptParams& p, int format, const void* map, c
   return e != cudaSuccess ? e : launch_dependent(k_paged_prompt_join<D, 2, 256>, dim3(p.grid, 256 / kJoinWarps), 32 * kJoinWarps, 0, s, p);
 }
 template <int D>
-cudaError_t setup_simple() {
-  return cudaFuncSetAttribute(k_paged_prompt_simple<D, 4, THINK_PAGE_PLAIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)simple_smem<D>());
+cudaError_t setup_fp32() {
+  return cudaFuncSetAttribute(k_paged_prompt_fp32<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)fp32_smem<D>());
 }
 
 }  // namespace
 
 cudaError_t paged_prompt_setup(int dtype, int format, int D) {
   if (dtype == THINK_BF16) return paged_prompt_tc_setup(format, D);
-  return D == 128 ? setup_simple<128>() : setup_simple<64>();
+  return D == 128 ? setup_fp32<128>() : setup_fp32<64>();
 }
 int paged_prompt_rows(int dtype) { return dtype == THINK_BF16 ? paged_prompt_tc_rows() : kRows; }
 PromptCut paged_prompt_cut(int dtype) { return dtype == THINK_BF16 ? paged_prompt_tc_cut() : PromptCut{kExtra, kShare}; }
 
 cudaError_t launch_paged_prompt(const PagedPromptParams& p, int dtype, int format, const void* map, cudaStream_t s) {
   if (dtype == THINK_BF16) return p.g.D == 128 ? launch_tc<128>(p, format, map, s) : launch_tc<64>(p, format, map, s);
-  return p.g.D == 128 ? launch_simple<128>(p, s) : launch_simple<64>(p, s);
+  return p.g.D == 128 ? launch_fp32<128>(p, s) : launch_fp32<64>(p, s);
 }
 
 }  // namespace think

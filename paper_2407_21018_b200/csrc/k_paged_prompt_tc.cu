@@ -206,8 +206,8 @@ template <int SLOTS, int STAGES>
 struct Shared {
   // full, empty: a slot holds an operand, may be overwritten.  s_full, p_full: S of a half is there, P is (two tiles each).
   // o_done: the item's last product has been added to O; o_full: the last but one; o_empty: O has been read.  q_full, q_empty: the
-  // same of the queries.  stats_full: m and l.
-  uint64_t full[SLOTS], empty[SLOTS], s_full[2][2], p_full[2][2], o_full[2], o_done[2], o_empty[2], q_full[2], q_empty[2], stats_full[2], raw;
+  // same of the queries.  stats_full: m and l.  left: all products are done.
+  uint64_t full[SLOTS], empty[SLOTS], s_full[2][2], p_full[2][2], o_full[2], o_done[2], o_empty[2], q_full[2], q_empty[2], stats_full[2], raw, left[2];
   uint64_t st_full[STAGES], st_empty[STAGES], item_full[kItems], item_empty[kItems];
   uint32_t tmem, failed;
   // The loads are at most 8 tiles ahead of what is in use, and kItems + 1 items ahead of the outputs.
@@ -731,7 +731,7 @@ __device__ __forceinline__ bool mma_role(typename Shape<D, FMT>::Sh& sh, uint32_
   for (;; ++items.no) {
     int last, tiles, n;                 // n: tiles of this half
     if (!items.take(sh, [&](const Item& i) { last = i.last; tiles = i.tiles; n = i.end[half]; })) return false;
-    if (uniform(last)) return true;
+    if (uniform(last)) break;
     tiles = uniform(tiles);
     n = uniform(n);
 #pragma unroll 1
@@ -768,6 +768,10 @@ __device__ __forceinline__ bool mma_role(typename Shape<D, FMT>::Sh& sh, uint32_
       }
     }
   }
+  // all that was committed has arrived before the block leaves, and its barriers with it
+  const uint32_t left = uniform(smem_u32(&sh.left[half]));
+  mma_commit(lead, left);
+  return warp_wait(left, 0);
 }
 
 // ---- warps 0-3, 4-7: the softmax of a half
@@ -1041,6 +1045,7 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
       bar_init(smem_u32(&sh.q_full[i]), 4);
       bar_init(smem_u32(&sh.q_empty[i]), 1);
       bar_init(smem_u32(&sh.stats_full[i]), 4);
+      bar_init(smem_u32(&sh.left[i]), 1);
     }
     for (int i = 0; i < kItems; ++i) {
       bar_init(smem_u32(&sh.item_full[i]), 1);

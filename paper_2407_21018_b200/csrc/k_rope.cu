@@ -46,10 +46,10 @@ struct RopeParams {
   uint64_t turns[kRopeMaxD / 2];
 };
 
-template <typename T>
-__device__ __forceinline__ void turn(float a, float b, const float2& cs, float& u, float& v) {
-  u = fmaf(a, cs.x, -(b * cs.y));
-  v = fmaf(b, cs.x, a * cs.y);
+__device__ __forceinline__ void turn(float a, float b, float c, float s, float& u, float& v) {
+  const float x = fmaf(a, c, -(b * s));
+  v = fmaf(b, c, a * s);
+  u = x;
 }
 
 // 16 bytes of bf16 or fp32 as floats and back
@@ -87,13 +87,14 @@ template <int E, bool VEC>
 __global__ void __launch_bounds__(kRopeThreads) k_rope(const __grid_constant__ RopeParams p) {
   using T = typename std::conditional<E == 2, __nv_bfloat16, float>::type;
   constexpr int V = 16 / E;
-  __shared__ float2 s_cs[kRopeTable];
+  __shared__ __align__(16) float2 s_cs[kRopeTable];
   __shared__ int s_on[64];
   begin_dependent();
   const int b = p.by_blocks.div(blockIdx.x), s0 = (blockIdx.x - b * p.blocks_s) * p.tokens;
   const int rows = p.rows ? min(load_now(p.rows + b), p.S) : p.S;
   const int n = min(p.tokens, rows - s0);
   if (n <= 0) return;                   // whole block
+  const int shift = !VEC ? 0 : (E == 2 ? 3 : 2) - p.interleaved, w = 1 << shift, across = p.pairs >> shift;      // w: pairs of a piece
   for (int i = threadIdx.x; i < n * p.pairs; i += kRopeThreads) {
     const int t = p.by_pairs.div(i), j = i - t * p.pairs;
     const int32_t pos = p.pos_stride ? load_now(p.pos + b * p.pos_stride + s0 + t)
@@ -106,7 +107,9 @@ __global__ void __launch_bounds__(kRopeThreads) k_rope(const __grid_constant__ R
     float sn, cn;
     sincospif(r, &sn, &cn);
     const float c = quarter & 1 ? sn : cn, s = quarter & 1 ? cn : sn;     // signs: cos - + by quarters 1, 2; sin by 2, 3
-    s_cs[i] = make_float2((quarter + 1) & 2 ? -c * p.m : c * p.m, (quarter & 2 ? -s : s) * p.m * p.sign);
+    // two pairs of a piece, then the same two of the next: lanes with neighbouring pieces read neighbouring 16 bytes
+    const int at = t * p.pairs + (VEC ? (j & (w - 2)) * across + 2 * (j >> shift) + (j & 1) : j);
+    s_cs[at] = make_float2((quarter + 1) & 2 ? -c * p.m : c * p.m, (quarter & 2 ? -s : s) * p.m * p.sign);
   }
   __syncthreads();
   for (int i = threadIdx.x; i < n * p.items; i += kRopeThreads) {
@@ -127,7 +130,11 @@ __global__ void __launch_bounds__(kRopeThreads) k_rope(const __grid_constant__ R
           float f[V];
           open16<E>(w, f);
 #pragma unroll
-          for (int k = 0; k < V; k += 2) turn<T>(f[k], f[k + 1], cs[unit * (V / 2) + k / 2], f[k], f[k + 1]);
+          for (int k = 0; k < V; k += 4) {
+            const float4 c = *(const float4*)(cs + k / 2 * across + 2 * unit);
+            turn(f[k], f[k + 1], c.x, c.y, f[k], f[k + 1]);
+            turn(f[k + 2], f[k + 3], c.z, c.w, f[k + 2], f[k + 3]);
+          }
           w = close16<E>(f);
         }
         __stcs((uint4*)y + unit, w);
@@ -138,7 +145,11 @@ __global__ void __launch_bounds__(kRopeThreads) k_rope(const __grid_constant__ R
         open16<E>(wa, a);
         open16<E>(wb, c);
 #pragma unroll
-        for (int k = 0; k < V; ++k) turn<T>(a[k], c[k], cs[unit * V + k], a[k], c[k]);
+        for (int k = 0; k < V; k += 2) {
+          const float4 f = *(const float4*)(cs + k * across + 2 * unit);
+          turn(a[k], c[k], f.x, f.y, a[k], c[k]);
+          turn(a[k + 1], c[k + 1], f.z, f.w, a[k + 1], c[k + 1]);
+        }
         __stcs((uint4*)y + unit, close16<E>(a));
         __stcs((uint4*)y + unit + half, close16<E>(c));
       } else {
@@ -151,7 +162,7 @@ __global__ void __launch_bounds__(kRopeThreads) k_rope(const __grid_constant__ R
       if (unit < p.pairs) {
         const int i0 = p.interleaved ? 2 * unit : unit, i1 = p.interleaved ? i0 + 1 : i0 + p.pairs;
         float u, v;
-        turn<T>((float)xe[i0], (float)xe[i1], cs[unit], u, v);
+        turn((float)xe[i0], (float)xe[i1], cs[unit].x, cs[unit].y, u, v);
         ye[i0] = (T)u;
         ye[i1] = (T)v;
       } else {
