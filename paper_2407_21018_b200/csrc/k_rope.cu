@@ -38,6 +38,7 @@ struct RopeParams {
   int tokens, blocks_s;                 // tokens of a block, blocks of an entry
   int units, items;                     // units of a row, of a token (all layers and heads)
   int interleaved;
+  int second;                           // 0, or pieces of a row that a unit's second is behind its first
   float m, sign;
   const int32_t* pos;
   int64_t pos_stride;                   // 0: position pos[b] + s
@@ -125,19 +126,25 @@ __global__ void __launch_bounds__(kRopeThreads) k_rope(const __grid_constant__ R
     const float2* const cs = s_cs + t * p.pairs;
     if constexpr (VEC) {
       if (p.interleaved) {
-        uint4 w = __ldcs((const uint4*)x + unit);
-        if (unit * V < p.R) {
+        // a piece and, where their number is even, the one half the pieces on
+        auto turned = [&](const uint4& w, int piece) {
+          if (piece * V >= p.R) return w;
           float f[V];
           open16<E>(w, f);
 #pragma unroll
           for (int k = 0; k < V; k += 4) {
-            const float4 c = *(const float4*)(cs + k / 2 * across + 2 * unit);
+            const float4 c = *(const float4*)(cs + k / 2 * across + 2 * piece);
             turn(f[k], f[k + 1], c.x, c.y, f[k], f[k + 1]);
             turn(f[k + 2], f[k + 3], c.z, c.w, f[k + 2], f[k + 3]);
           }
-          w = close16<E>(f);
+          return close16<E>(f);
+        };
+        const uint4 wa = __ldcs((const uint4*)x + unit);
+        if (p.second) {
+          const uint4 wb = __ldcs((const uint4*)x + unit + p.second);
+          __stcs((uint4*)y + unit + p.second, turned(wb, unit + p.second));
         }
-        __stcs((uint4*)y + unit, w);
+        __stcs((uint4*)y + unit, turned(wa, unit));
       } else if (unit * V < p.pairs) {
         const int half = p.pairs / V;
         const uint4 wa = __ldcs((const uint4*)x + unit), wb = __ldcs((const uint4*)x + unit + half);
@@ -316,7 +323,8 @@ thinK_status thinK_rope_apply(const thinK_rope* r, thinK_tensor5 q, thinK_tensor
   p.R = r->R; p.D = r->D; p.pairs = r->R / 2;
   p.interleaved = !halves;
   if (vec) p.units = (halves ? p.pairs : p.R) / V + (in_place ? 0 : (p.D - p.R) / V);
-  else p.units = p.pairs + (in_place ? 0 : p.D - p.R);
+  if (vec && !halves && p.units % 2 == 0) p.second = p.units /= 2;
+  if (!vec) p.units = p.pairs + (in_place ? 0 : p.D - p.R);
   const int64_t heads_all = (int64_t)N_q + N_kv, items = heads_all * nlayers * p.units;
   if (items > (1 << 24)) return THINK_ERR_UNSUPPORTED;                 // item numbers of a block fit 31 bits
   p.heads_q = N_q; p.heads = (int)heads_all;
