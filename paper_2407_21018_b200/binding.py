@@ -390,6 +390,7 @@ class PagePlan:
         at = 2 * room
         self.pos, self.rows, self.seq_lens = x[at:at + B], x[at + B:at + 2 * B], x[at + 2 * B:at + 3 * B]
         self.start, self.free_count = x[at + 3 * B:at + 4 * B + 1], x[at + 4 * B + 1:]
+        self._own = self.seq_lens, self.free_count
         self._index = x.get_device()
         self._ptrs = [t.data_ptr() for t in (self.pos, self.rows, self.start, self.token_pos, self.slots, self.seq_lens,
                                              self.free_count)]
@@ -563,8 +564,7 @@ class PagedKVCache:
                          self._vector(free_pages, 1, where, ": free_pages"),
                          have, pos, rows, start, token_pos, slots, new, left, out.max_tokens)
         self._call(lib.thinK_paged_plan, where, C.byref(step), self._stream(stream))
-        if in_place:
-            out.seq_lens, out.free_count = seq_lens, free_count
+        out.seq_lens, out.free_count = (seq_lens, free_count) if in_place else out._own
         return out
 
     def decode_attn(self, q: torch.Tensor, table: torch.Tensor, seq_lens: torch.Tensor,

@@ -273,7 +273,7 @@ thinK_status thinK_paged_plan(thinK_paged* p, const thinK_paged_step* step, void
     if (!m[i].ptr || !aligned(m[i].ptr, m[i].ptr == a.token_pos || m[i].ptr == a.slots ? 16 : 4)) return THINK_ERR_INVALID_ARG;
     for (int j = 0; j < i; ++j) {
       if (!m[i].out && !m[j].out) continue;
-      if ((m[i].ptr == a.seq_len_out && m[j].ptr == a.seq_len && j == 0) || (m[i].ptr == a.free_left && m[j].ptr == a.free_count && j == 2)) continue;
+      if (m[i].ptr == m[j].ptr && ((i == 10 && j == 0) || (i == 11 && j == 2))) continue;      // in place: seq_len, free_count
       if (overlap(m[i].ptr, m[i].bytes, m[j].ptr, m[j].bytes)) return THINK_ERR_INVALID_ARG;
     }
   }
@@ -337,11 +337,11 @@ thinK_status thinK_paged_prompt_attn(thinK_paged* p, thinK_tensor5 q, thinK_tens
   if (!aligned(pos, 4) || !aligned(rows, 4) || !aligned(start, 4) || !aligned(lse, 4)) return THINK_ERR_INVALID_ARG;
   if (start && !rows) return THINK_ERR_INVALID_ARG;
   if (max_rows == 0) return THINK_OK;                  // views without rows may have no memory
+  if (start) q.stride_b = out.stride_b = 0;
   if (!view_ok(q, p->g.elem) || !view_ok(out, p->g.elem) || !scratch || !aligned(scratch, 256)) return THINK_ERR_INVALID_ARG;
   if (scratch_bytes < thinK_paged_prompt_scratch(p)) return THINK_ERR_CAPACITY;
   if (p->g.dtype == THINK_BF16 && p->g.format == THINK_PAGE_PLAIN && !p->mapped) return THINK_ERR_UNSUPPORTED;
   const int B = start ? 1 : table.B, unit = 16 / p->g.elem;
-  if (start) q.stride_b = out.stride_b = 0;
   auto view = [&](const thinK_tensor5& t) {
     return RowView{{t.stride_b / unit, t.stride_s / unit, t.stride_l / unit, t.stride_n / unit}, {B, max_rows, nlayers, p->g.N_q}, p->g.g.D / unit};
   };

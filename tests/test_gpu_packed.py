@@ -369,3 +369,62 @@ def test_rope_captured_and_on_another_stream():
     pos.copy_(ints([5] * 200))
     graph.replay()
     assert not torch.equal(out, again) and torch.equal(out[5], again[5])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("layout", ["halves", "pairs"])
+@pytest.mark.parametrize("D,R", [(24, 24), (56, 16), (40, 8), (88, 64)])
+def test_rope_rows_of_an_odd_number_of_pieces(dtype, layout, D, R):
+    """5 and 7 pieces of 16 bytes a row, in place (only those that turn) and not."""
+    r, freq, m = make_rope(D, dtype, R, layout, "plain")
+    x = torch.randn(2, 40, 1, 3, D, generator=gen(D), device="cuda").to(dtype)
+    y, z = torch.zeros_like(x), x.clone()
+    r.apply(x, None, ints([3, 70000]), q_out=y)
+    check_rope(x, y, [[3 + s for s in range(40)], [70000 + s for s in range(40)]], [[True] * 40] * 2, dtype, R, layout, freq, m, False)
+    r.apply(z, None, ints([3, 70000]))
+    assert torch.equal(y, z)
+
+
+def test_a_plan_serves_calls_in_place_and_not():
+    cache, tk = small_cache(9, 2), binding()
+    step = Step([10, 64], [5, 3], 3, 4, 20, num_pages=9)
+    change, lens, table, free_pages, count = step.upload()
+    plan = tk.PagePlan(2, 20)
+    cache.plan(change, lens, table, free_pages, count, in_place=True, out=plan)
+    assert plan.seq_lens is lens and lens.tolist() == [15, 67] and plan.free_count is count
+    before = lens.clone()
+    cache.plan(change, lens, table, free_pages, count, out=plan)
+    assert torch.equal(lens, before) and plan.seq_lens.tolist() == [20, 70] and plan.free_count is not count
+
+
+def test_calls_that_the_binding_refuses():
+    tk = binding()
+    cache = small_cache(9, 2, L=2, N_kv=2, N_q=4, D=64)
+    bf = torch.bfloat16
+    table, two = torch.zeros(2, 3, dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    x, slots = torch.zeros(5, 2, 2, 64, dtype=bf, device="cuda"), torch.full((5,), -1, dtype=torch.int32, device="cuda")
+    q = torch.zeros(2, 5, 2, 4, 64, dtype=bf, device="cuda")
+    free_pages = torch.zeros(9, dtype=torch.int32, device="cuda")
+    one = free_pages[:1].clone()
+    rope = tk.Rope(64, bf)
+    calls = [lambda: cache.write_slots(x.float(), x, slots), lambda: cache.write_slots(x, x[:4], slots), lambda: cache.write_slots(x, x, slots[:4]),
+             lambda: cache.write_slots(x, x, slots.long()), lambda: cache.write_slots(x, x, slots.cpu()), lambda: cache.write_slots(x, x, slots, layer0=1),
+             lambda: cache.write_slots(x[:, :1], x[:, :1], slots), lambda: cache.write_slots(x[..., ::2], x[..., ::2], slots),
+             lambda: cache.prompt_attn(q.float(), table), lambda: cache.prompt_attn(q[:, :, :1], table), lambda: cache.prompt_attn(q, table[:1]),
+             lambda: cache.prompt_attn(q, table.long()), lambda: cache.prompt_attn(q, table, pos=two[:1]), lambda: cache.prompt_attn(q, table, rows=two.long()),
+             lambda: cache.prompt_attn(q, table, out=q), lambda: cache.prompt_attn(q, table, out=q[:, :4]), lambda: cache.prompt_attn(q[0], table, start=two),
+             lambda: cache.prompt_attn(q, table, lse=torch.zeros(2, 5, 2, 4, device="cuda", dtype=bf)), lambda: cache.prompt_attn(q, table, scratch=free_pages),
+             lambda: cache.prompt_attn(q, table, scratch=torch.zeros(256, dtype=torch.uint8, device="cuda")), lambda: cache.prompt_attn(q, table, layer0=2),
+             lambda: cache.plan(two, two, table, free_pages, one), lambda: cache.plan(two, two, table[:1], free_pages, one, 9),
+             lambda: cache.plan(two.long(), two.clone(), table, free_pages, one, 9), lambda: cache.plan(two, two.clone(), table, free_pages[:8], one, 9),
+             lambda: cache.plan(two, two.clone(), table, free_pages, one, out=tk.PagePlan(3, 9)), lambda: cache.plan(two, two, table, free_pages, one, 9, in_place=True),
+             lambda: cache.plan(two, two.clone(), table, free_pages, one, 8, out=tk.PagePlan(2, 9)),
+             lambda: cache.plan(two, two.clone(), table, free_pages, free_pages[:1], 9),
+             lambda: rope.apply(q.float(), None, two), lambda: rope.apply(q, x, two), lambda: rope.apply(q, None, two.long()), lambda: rope.apply(q, None, two[:1]),
+             lambda: rope.apply(q, None, two.cpu()), lambda: rope.apply(q, None, two, rows=two[:1]), lambda: rope.apply(q, None, two, q_out=q[:, :4]),
+             lambda: rope.apply(q, None, two, q_out=q.transpose(0, 1).contiguous().transpose(0, 1)[:, :, :1].expand(q.shape))]
+    for i, call in enumerate(calls):
+        with pytest.raises(tk.ThinKError) as e:
+            call()
+        assert e.value.status in (tk.ERR_INVALID_ARG, tk.ERR_CAPACITY), i
+    assert cache.device_error() == 0
