@@ -34,10 +34,9 @@ struct RopeSide {                       // queries or keys
 struct RopeParams {
   RopeSide side[2];
   int heads_q, heads;                   // heads of queries, of both, a layer
-  int nlayers, S, R, D, pairs;          // pairs: R / 2
+  int nlayers, S, R, D, pairs, table;   // pairs: R / 2; table: room for a token's, those of whole pieces
   int tokens, blocks_s;                 // tokens of a block, blocks of an entry
   int units, items;                     // units of a row, of a token (all layers and heads)
-  int interleaved;
   int second;                           // 0, or pieces of a row that a unit's second is behind its first
   float m, sign;
   const int32_t* pos;
@@ -82,12 +81,13 @@ __device__ __forceinline__ uint4 close16(const float (&f)[16 / E]) {
   }
 }
 
-// VEC: units are 16-byte pieces (half layout: a piece and its partner; interleaved: a piece), then pieces to copy.
-// Otherwise, where pairs do not come in such pieces (R / 2 or R no multiple of one), units are single pairs, then channels.
-template <int E, bool VEC>
+// What a unit is: a piece of 16 bytes and its partner half a rotation on; a piece and, where their number is even, the one half
+// the pieces on (interleaved pairs lie within pieces); two or one channels and their partners, where half a rotation is no
+// multiple of a piece (two channels where it is even).  Behind the units that turn are those that copy, by pieces.
+enum RopeForm { kHalves, kPairs, kTwo, kOne };
+template <int E, int FORM>
 __global__ void __launch_bounds__(kRopeThreads) k_rope(const __grid_constant__ RopeParams p) {
-  using T = typename std::conditional<E == 2, __nv_bfloat16, float>::type;
-  constexpr int V = 16 / E;
+  constexpr int V = 16 / E, kShift = FORM == kHalves ? (E == 2 ? 3 : 2) : FORM == kPairs ? (E == 2 ? 2 : 1) : 0, W = 1 << kShift;      // W: pairs of a piece
   __shared__ __align__(16) float2 s_cs[kRopeTable];
   __shared__ int s_on[64];
   begin_dependent();
@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(kRopeThreads) k_rope(const __grid_constant__ R
   const int rows = p.rows ? min(load_now(p.rows + b), p.S) : p.S;
   const int n = min(p.tokens, rows - s0);
   if (n <= 0) return;                   // whole block
-  const int shift = !VEC ? 0 : (E == 2 ? 3 : 2) - p.interleaved, w = 1 << shift, across = p.pairs >> shift;      // w: pairs of a piece
+  const int across = p.table >> kShift;
   for (int i = threadIdx.x; i < n * p.pairs; i += kRopeThreads) {
     const int t = p.by_pairs.div(i), j = i - t * p.pairs;
     const int32_t pos = p.pos_stride ? load_now(p.pos + b * p.pos_stride + s0 + t)
@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(kRopeThreads) k_rope(const __grid_constant__ R
     sincospif(r, &sn, &cn);
     const float c = quarter & 1 ? sn : cn, s = quarter & 1 ? cn : sn;     // signs: cos - + by quarters 1, 2; sin by 2, 3
     // two pairs of a piece, then the same two of the next: lanes with neighbouring pieces read neighbouring 16 bytes
-    const int at = t * p.pairs + (VEC ? (j & (w - 2)) * across + 2 * (j >> shift) + (j & 1) : j);
+    const int at = t * p.table + (W > 1 ? (j & (W - 2)) * across + 2 * (j >> kShift) + (j & 1) : j);
     s_cs[at] = make_float2((quarter + 1) & 2 ? -c * p.m : c * p.m, (quarter & 2 ? -s : s) * p.m * p.sign);
   }
   __syncthreads();
@@ -123,30 +123,29 @@ __global__ void __launch_bounds__(kRopeThreads) k_rope(const __grid_constant__ R
     const int h = key ? h0 - p.heads_q : h0;
     const uint8_t* const x = side.x + b * side.xb + (s0 + t) * side.xs + l * side.xl + h * side.xn;
     uint8_t* const y = side.y + b * side.yb + (s0 + t) * side.ys + l * side.yl + h * side.yn;
-    const float2* const cs = s_cs + t * p.pairs;
-    if constexpr (VEC) {
-      if (p.interleaved) {
-        // a piece and, where their number is even, the one half the pieces on
-        auto turned = [&](const uint4& w, int piece) {
-          if (piece * V >= p.R) return w;
-          float f[V];
-          open16<E>(w, f);
+    const float2* const cs = s_cs + t * p.table;
+    if constexpr (FORM == kPairs) {
+      auto turned = [&](const uint4& w, int piece) {
+        if (piece * V >= p.R) return w;
+        float f[V];
+        open16<E>(w, f);
 #pragma unroll
-          for (int k = 0; k < V; k += 4) {
-            const float4 c = *(const float4*)(cs + k / 2 * across + 2 * piece);
-            turn(f[k], f[k + 1], c.x, c.y, f[k], f[k + 1]);
-            turn(f[k + 2], f[k + 3], c.z, c.w, f[k + 2], f[k + 3]);
-          }
-          return close16<E>(f);
-        };
-        const uint4 wa = __ldcs((const uint4*)x + unit);
-        if (p.second) {
-          const uint4 wb = __ldcs((const uint4*)x + unit + p.second);
-          __stcs((uint4*)y + unit + p.second, turned(wb, unit + p.second));
+        for (int k = 0; k < V; k += 4) {
+          const float4 c = *(const float4*)(cs + k / 2 * across + 2 * piece);
+          if (piece * V + k < p.R) turn(f[k], f[k + 1], c.x, c.y, f[k], f[k + 1]);
+          if (piece * V + k + 2 < p.R) turn(f[k + 2], f[k + 3], c.z, c.w, f[k + 2], f[k + 3]);
         }
-        __stcs((uint4*)y + unit, turned(wa, unit));
-      } else if (unit * V < p.pairs) {
-        const int half = p.pairs / V;
+        return close16<E>(f);
+      };
+      const uint4 wa = __ldcs((const uint4*)x + unit);
+      if (p.second) {
+        const uint4 wb = __ldcs((const uint4*)x + unit + p.second);
+        __stcs((uint4*)y + unit + p.second, turned(wb, unit + p.second));
+      }
+      __stcs((uint4*)y + unit, turned(wa, unit));
+    } else if constexpr (FORM == kHalves) {
+      const int half = p.pairs / V;
+      if (unit < half) {
         const uint4 wa = __ldcs((const uint4*)x + unit), wb = __ldcs((const uint4*)x + unit + half);
         float a[V], c[V];
         open16<E>(wa, a);
@@ -160,21 +159,30 @@ __global__ void __launch_bounds__(kRopeThreads) k_rope(const __grid_constant__ R
         __stcs((uint4*)y + unit, close16<E>(a));
         __stcs((uint4*)y + unit + half, close16<E>(c));
       } else {
-        const int piece = unit + p.pairs / V;
-        __stcs((uint4*)y + piece, __ldcs((const uint4*)x + piece));
+        __stcs((uint4*)y + unit + half, __ldcs((const uint4*)x + unit + half));
       }
     } else {
-      const T* const xe = (const T*)x;
-      T* const ye = (T*)y;
-      if (unit < p.pairs) {
-        const int i0 = p.interleaved ? 2 * unit : unit, i1 = p.interleaved ? i0 + 1 : i0 + p.pairs;
-        float u, v;
-        turn((float)xe[i0], (float)xe[i1], cs[unit].x, cs[unit].y, u, v);
-        ye[i0] = (T)u;
-        ye[i1] = (T)v;
+      using T = typename std::conditional<E == 2, __nv_bfloat16, float>::type;
+      struct alignas(sizeof(T) * (FORM == kTwo ? 2 : 1)) Some { T v[FORM == kTwo ? 2 : 1]; };
+      constexpr int N = FORM == kTwo ? 2 : 1;
+      const Some* const xe = (const Some*)x;
+      Some* const ye = (Some*)y;
+      const int turning = p.pairs / N, border = (p.R + V - 1) / V * V;
+      if (unit < turning) {
+        Some a = xe[unit], c = xe[unit + turning];
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          float u, v;
+          turn((float)a.v[k], (float)c.v[k], cs[N * unit + k].x, cs[N * unit + k].y, u, v);
+          a.v[k] = (T)u;
+          c.v[k] = (T)v;
+        }
+        ye[unit] = a;
+        ye[unit + turning] = c;
       } else {
-        const int c = unit + p.pairs;
-        ye[c] = xe[c];
+        const int c = unit + turning, piece = border / V + c - border / N;
+        if (c < border / N) ye[c] = xe[c];
+        else __stcs((uint4*)y + piece, __ldcs((const uint4*)x + piece));
       }
     }
   }
@@ -310,8 +318,7 @@ thinK_status thinK_rope_apply(const thinK_rope* r, thinK_tensor5 q, thinK_tensor
       if (i < j && ov[i].shares_with(ov[j], (int64_t)((uintptr_t)to[j].ptr / 16) - (int64_t)((uintptr_t)to[i].ptr / 16))) return THINK_ERR_INVALID_ARG;
     }
   const bool in_place = (!N_q || same(q, q_out)) && (!N_kv || same(k, k_out));
-  const bool halves = r->layout == THINK_ROPE_HALVES;
-  const bool vec = halves ? (r->R / 2) % V == 0 : r->R % V == 0;
+  const int form = r->layout == THINK_ROPE_PAIRS ? kPairs : (r->R / 2) % V == 0 ? kHalves : (r->R / 2) % 2 == 0 ? kTwo : kOne;
   RopeParams p;
   memset((void*)&p, 0, sizeof(p));
   for (int i = 0; i < 2; ++i) {
@@ -321,10 +328,12 @@ thinK_status thinK_rope_apply(const thinK_rope* r, thinK_tensor5 q, thinK_tensor
                          to[i].stride_b * r->elem, to[i].stride_s * r->elem, to[i].stride_l * r->elem, to[i].stride_n * r->elem};
   }
   p.R = r->R; p.D = r->D; p.pairs = r->R / 2;
-  p.interleaved = !halves;
-  if (vec) p.units = (halves ? p.pairs : p.R) / V + (in_place ? 0 : (p.D - p.R) / V);
-  if (vec && !halves && p.units % 2 == 0) p.second = p.units /= 2;
-  if (!vec) p.units = p.pairs + (in_place ? 0 : p.D - p.R);
+  const int border = (p.R + V - 1) / V * V, rest = in_place ? 0 : (p.D - border) / V;        // pieces that no pair touches
+  if (form == kPairs) p.units = border / V + rest;
+  else if (form == kHalves) p.units = p.pairs / V + rest;
+  else p.units = (p.pairs + (in_place ? 0 : border - p.R)) / (form == kTwo ? 2 : 1) + rest;
+  if (form == kPairs && p.units % 2 == 0) p.second = p.units /= 2;
+  p.table = form == kPairs ? border / 2 : p.pairs;
   const int64_t heads_all = (int64_t)N_q + N_kv, items = heads_all * nlayers * p.units;
   if (items > (1 << 24)) return THINK_ERR_UNSUPPORTED;                 // item numbers of a block fit 31 bits
   p.heads_q = N_q; p.heads = (int)heads_all;
@@ -336,7 +345,7 @@ thinK_status thinK_rope_apply(const thinK_rope* r, thinK_tensor5 q, thinK_tensor
   int tokens = (int)((4 * kRopeThreads + items - 1) / items);
   const int64_t fill = (int64_t)B * S / (4 * kSMs);
   if (tokens > fill) tokens = (int)fill;
-  if (tokens > kRopeTable / p.pairs) tokens = kRopeTable / p.pairs;
+  if (tokens > kRopeTable / p.table) tokens = kRopeTable / p.table;
   if (tokens > 64) tokens = 64;
   if (tokens < 1) tokens = 1;
   p.tokens = tokens;
@@ -348,7 +357,9 @@ thinK_status thinK_rope_apply(const thinK_rope* r, thinK_tensor5 q, thinK_tensor
   p.by_pairs = FastDiv((uint32_t)p.pairs);
   p.by_blocks = FastDiv((uint32_t)p.blocks_s);
   memcpy(p.turns, r->turns, sizeof(p.turns));
-  void (*const kernel)(const RopeParams) = r->elem == 2 ? (vec ? k_rope<2, true> : k_rope<2, false>) : (vec ? k_rope<4, true> : k_rope<4, false>);
+  static void (*const kernels[2][4])(const RopeParams) = {{k_rope<2, kHalves>, k_rope<2, kPairs>, k_rope<2, kTwo>, k_rope<2, kOne>},
+                                                          {k_rope<4, kHalves>, k_rope<4, kPairs>, k_rope<4, kTwo>, k_rope<4, kOne>}};
+  void (*const kernel)(const RopeParams) = kernels[r->elem == 4][form];
   return launch_dependent(kernel, dim3((unsigned)(p.blocks_s * B)), kRopeThreads, 0, (cudaStream_t)stream, p) == cudaSuccess ? THINK_OK
                                                                                                                              : THINK_ERR_CUDA;
 }
