@@ -10,7 +10,8 @@
 // the CTAs share the pages, meet, and share the tokens.  Lengths and the count of free pages are stored behind that
 // meeting, so inputs and results may be the same arrays; the pages taken are read below the old count and the ones given
 // back are stored at or above it, so that one list serves as both, too.
-// Bound: latency.  A step of 64 tokens is three dependent loads behind the launch; 100,000 tokens write 0.8 MB.
+// Bound: latency.  A step of 64 tokens is three dependent loads behind the launch; 100,000 tokens write 0.8 MB.  A call takes the host
+// 8 us, which hides the kernel (4 us; 76,800 tokens of 256 sequences 10).
 #include <cooperative_groups.h>
 
 #include "paged_internal.h"
@@ -202,7 +203,9 @@ __global__ void __launch_bounds__(1024) k_paged_plan(const PagedPlanParams p) {
 // One CTA for as many sequences and tokens as it serves in the time that a cluster needs to meet; else a cluster of eight,
 // the portable most.
 cudaError_t launch_paged_plan(const PagedPlanParams& p, cudaStream_t s) {
-  const bool small = p.table.B <= 256 && p.max_tokens <= 2048;
+  // One CTA saves the cluster's start and meeting (256 sequences, with the copies around it in a graph: 6 instead of 8.5 us), until
+  // the tokens are too many for it (2048: 6.6 against 8.1 us; 7680: 13.9 against 8.4).
+  const bool small = p.table.B <= 256 * kPer && p.max_tokens <= 2048;
   const int ctas = small ? 1 : 8, threads = small ? 256 : 1024;
   const size_t smem = sizeof(int) * (4 * (size_t)p.table.B + 3);
   if (smem > 48 * 1024) {

@@ -3,6 +3,11 @@
 //
 // out_s = sum_t w_t V_t / sum_t w_t, w_t = 2^(x_t - m), x = scale log2(e) q_s K_t, over the tokens t <= pos + s, in one
 // pass over tiles of 64 tokens with the running maximum m and sum of a softmax.
+//
+// fp32 caches keep fp32 products, which the tensor cores do not have: a block has 64 rows of queries and a tile in shared
+// memory, a thread 4 x 4 logits and 4 rows of outputs in registers.  Bound: shared memory reads (two 16-byte reads feed 16
+// multiply-adds).  Short calls (two sequences of up to 512 tokens, 4 heads of 64: 44 us) are one item a block, 5 tiles in a row, and
+// the join.  The cut into parts (paged_prompt.h) keeps one of those from having a long item all to itself.
 #include <math.h>
 
 #include "paged_prompt_walk.cuh"

@@ -2,16 +2,28 @@
 //
 // An item is 256 rows of queries that share a key head (256 / G new tokens times the G heads), as two halves of 128 rows
 // that take turns on the tensor cores: while one half's logits pass through the softmax, the other's products run.
-//   S = Q K^T       tcgen05.mma into tensor memory, a tile of KT tokens; thread t of a half's four warps owns row t
+//   S = Q K^T       tcgen05.mma from shared memory into tensor memory, a tile of 64 tokens; two tiles' S a half, so that the
+//                   next one is there when a softmax ends; thread t of a half's four warps owns row t
 //   P = 2^(x - m)   read from tensor memory, written back over S as bf16: the A operand of
 //   O += P V        tcgen05.mma, V as stored ([token][channel]) is the MN-major B operand
-// Roles: warps 0-3 and 4-7 the softmax of a half each; three or four warps bring keys and values into a ring of shared-memory
-// slots (bf16 pages by TMA; others as bytes by bulk copies that one more warp issues, unpacked in registers); one thread issues
-// all products; four warps load the next item's queries and store the last item's outputs, so that the others go from item
-// to item without a pause.  m only moves when a row's logits pass it by 2^8 (O is then rescaled in tensor memory), so the
-// softmax seldom waits for the products.  Loops stay rolled: unrolled, the roles' code together missed the instruction cache.
-// 4-bit values n * s have 11 bits: they enter as the sum of two bf16, which is exact, at twice the products; their keys
-// and values need twice the room, so tiles are 64 tokens and Q is held in tensor memory too.
+// Roles: warps 0-3 and 4-7 the softmax of a half each; a warp for the products of each half; a warp for keys and one for values
+// bring them into a ring of shared-memory slots (bf16 pages by TMA; others as bytes by bulk copies, which four warps unpack
+// from stages into the ring); four warps load the next item's queries and store the last item's outputs, so that the others
+// go from item to item without a pause.  One of the loading warps walks along the items and hands out their description.  m only
+// moves when a row's logits pass it by 2^8 (O is then rescaled in tensor memory), so the softmax seldom waits for the products.
+// 4-bit values n * s have 11 bits: they enter as the sum of two bf16, which is exact, at twice the products.
+// P is rounded to bf16 (2^-9 of a weight on average, what the products take); l sums the unrounded weights, with what its
+// additions lose carried along, in fp32.
+//
+// What bounds it (a prompt of 8192 tokens, 32 heads of 128 over 8 key heads, 490 us replayed: 0.55 TFLOP at 1120 TFLOP/s, 0.69 of the
+// measured GEMM rate; 0.59 among other calls, where the clock falls): nothing alone.  Tensor pipe and exponentials are each busy
+// for 47 % of the cycles: products of 64 tokens wait for shared memory (S: 48 instead of 32 cycles each, Q and K are both read), 16
+// exponentials a cycle and SM take 1024 cycles a tile of both halves against 1280 of products, and a scheduler has one warp of each half to
+// overlap the rest of a softmax with.  e4m3 adds the unpacking (8192 tokens 680 us), 4 bits twice the products (1100 us).  Few rows: DRAM
+// (8 rows over 131072 tokens, twice, 1.07 GB in 172 us).  Short calls: code that is fetched for the first time (100 tokens: 21 us and
+// 6 for the join).  Loops stay rolled for that, and because the roles' code together misses the instruction cache.
+// Tiles of 128 tokens, whose S has one place a half, took 563 us for the same prompt; P in places of its own and S read ahead of
+// the weights of the tile before 515; exponentials in part by a polynomial, or of the halves strictly in turn, were slower too.
 // Every wait is bounded (about a second): on a time-out the CTA raises the error word, frees its tensor memory and leaves.
 #include <math.h>
 #include <string.h>

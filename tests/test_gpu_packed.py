@@ -428,3 +428,16 @@ def test_calls_that_the_binding_refuses():
             call()
         assert e.value.status in (tk.ERR_INVALID_ARG, tk.ERR_CAPACITY), i
     assert cache.device_error() == 0
+
+
+@pytest.mark.parametrize("B", [257, 1000, 1024, 1025])
+@pytest.mark.parametrize("share", [1.0, 0.3])
+def test_plan_of_a_decode_step_of_many_sequences(B, share):
+    r = np.random.default_rng(B)
+    lens, change = r.integers(0, 300, B).tolist(), r.choice([1, 1, 1, -70, 0], B).tolist()
+    need = sum(max(0, ko.pages_of(max(n + c, 0)) - ko.pages_of(n)) for n, c in zip(lens, change))
+    step = Step(lens, change, 6, int(need * share), B)
+    cache = small_cache(step.num_pages, B)
+    change_d, lens_d, table, free_pages, count = step.upload()
+    got = cache.plan(change_d, lens_d, table, free_pages, count, B)
+    check_plan(got, table, free_pages, step.want())
