@@ -826,10 +826,19 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, typenam
         })) return false;
     if (last) return true;
     const int limit = row < rows ? min(n, pos0 + s + 1) : 0;       // tokens that the row sees
+    int i = 0;
+    if (warp * 32 >= rows) {            // no row: P stays what it is, and what becomes of it is not looked at
+#pragma unroll 1
+      for (; i < end; ++i) {
+        if (!warp_wait(s_full + (i & 1) * 8, s_phase >> (i & 1) & 1)) return false;
+        s_phase ^= 1u << (i & 1);
+        if (lane == 0) bar_arrive(p_full + (i & 1) * 8);
+      }
+    }
     float m = -INFINITY, l = 0.f, lc = 0.f;            // lc: what the additions to l have lost
     bool seen = false;
 #pragma unroll 1
-    for (int i = 0; i < end; ++i) {
+    for (; i < end; ++i) {
       const int buf = i & 1, tok0 = (t0 + i) * KT;
       if (!warp_wait(s_full + buf * 8, s_phase >> buf & 1)) return false;
       s_phase ^= 1u << buf;
