@@ -7,8 +7,8 @@
 //   P = 2^(x - m)   read from tensor memory, written back over S as bf16: the A operand of
 //   O += P V        tcgen05.mma, V as stored ([token][channel]) is the MN-major B operand
 // Roles: warps 0-3 and 4-7 the softmax of a half each; a warp for the products of each half; a warp for keys and one for values
-// bring them into a ring of shared-memory slots (bf16 pages by TMA; others as bytes by bulk copies, which four warps unpack
-// from stages into the ring); four warps load the next item's queries and store the last item's outputs, so that the others
+// bring them into a ring of shared-memory slots (bf16 pages by TMA; others as bytes by bulk copies, which four or eight warps
+// unpack from stages into the ring); four warps load the next item's queries and store the last item's outputs, so that the others
 // go from item to item without a pause.  One of the loading warps walks along the items and hands out their description.  m only
 // moves when a row's logits pass it by 2^8 (O is then rescaled in tensor memory), so the softmax seldom waits for the products.
 // 4-bit values n * s have 11 bits: they enter as the sum of two bf16, which is exact, at twice the products.
@@ -247,12 +247,16 @@ struct Shape {
   using Sh = Shared<kSlots, kStages>;
   static constexpr int kStageAt = kQBytes + kSlots * kSlot, kSharedAt = kStageAt + kStages * kStage, kSmem = kSharedAt + (int)sizeof(Sh);
   static_assert(kSharedAt % 16 == 0 && kSmem <= kMaxSmem, "shared memory");
-  // warpgroups: two halves' softmax; bf16 pages: loads and products, else unpacking, then products and fetching; rows
-  static constexpr int kGroups = kPlain ? 4 : 5, kThreads = 128 * kGroups;
-  static constexpr int kMmaWarp = kPlain ? 10 : 12, kFetchWarp = 14, kRowsWarp = kPlain ? 12 : 16;
-  static constexpr int kRegs = kPlain ? 128 : 96;             // a thread at launch
-  static constexpr int kSoftmaxRegs = kPlain ? 152 : 128, kLoadRegs = kPlain ? 96 : 80, kMmaRegs = 64, kRowsRegs = kPlain ? 112 : 80;
-  static_assert(2 * kSoftmaxRegs + kLoadRegs + (kPlain ? 0 : kMmaRegs) + kRowsRegs <= kRegs * kGroups, "more registers than the block has: a wait without end");
+  // Warps: two halves' softmax; bf16 pages: loads and products, else unpacking, products and fetching; rows.  Eight warps unpack e4m3
+  // (8 rows over 131072 tokens, twice: 270 us with four, 254 with eight; long and ragged calls the same), four 4 bits (287 and 293 us).
+  static constexpr int kUnpackWarps = kPlain ? 0 : kInt4 ? 4 : 8;
+  static constexpr int kMmaWarp = kPlain ? 10 : 8 + kUnpackWarps, kFetchWarp = kMmaWarp + 2, kRowsWarp = 12 + kUnpackWarps;
+  static constexpr int kThreads = 32 * (kRowsWarp + 4);
+  // registers a thread: at launch, and as the roles have them
+  static constexpr int kRegs = kPlain ? 128 : kInt4 ? 96 : 80;
+  static constexpr int kSoftmaxRegs = kPlain ? 152 : kInt4 ? 128 : 120, kLoadRegs = kPlain ? 96 : kInt4 ? 80 : 56;
+  static constexpr int kMmaRegs = kPlain ? 96 : kInt4 ? 64 : 56, kRowsRegs = kPlain ? 112 : kInt4 ? 80 : 72;
+  static_assert(8 * kSoftmaxRegs + kUnpackWarps * kLoadRegs + 4 * kMmaRegs + 4 * kRowsRegs <= kRegs * kThreads / 32, "more registers than the block has: a wait without end");
   // tensor memory: S of each half, twice, O of each half
   static constexpr int kColO = 4 * KT;
   static __host__ __device__ constexpr PromptCut cut() { return PromptCut{kExtra, kShare}; }
@@ -588,17 +592,17 @@ __device__ __forceinline__ bool fetch_role(const PagedPromptParams& p, typename 
   }
 }
 
-// ---- four warps unpack the stages into the ring
+// ---- four or eight warps unpack the stages into the ring
 // 64 stored rows at `from` to rows of the operand at `to` (of 64-channel blocks of KT rows).  A unit is 16 stored bytes: 16
 // channels of e4m3, 32 of 4 bits.  EDGE: rows from `n` on become 0, those from `see` on finite; whether any was not.  (In a rolled
 // loop: it comes too seldom to stay in the instruction cache, unrolled it took ragged batches 325 instead of 297 us.)
 template <int D, int FMT, bool EDGE>
 __device__ __forceinline__ bool unpack_rows(uint32_t from, uint32_t to, int n, int see) {
   using T = Shape<D, FMT>;
-  constexpr int CH = T::kInt4 ? 32 : 16, PER_ROW = D / CH, UNITS = kPageTokens * PER_ROW / 128, PASS = 128 / PER_ROW;
+  constexpr int CH = T::kInt4 ? 32 : 16, PER_ROW = D / CH, PASS = 32 * T::kUnpackWarps / PER_ROW, UNITS = (kPageTokens + PASS - 1) / PASS;
   constexpr int kUnroll = EDGE ? 1 : UNITS, kLoad = EDGE ? 1 : UNITS;
-  static_assert(PASS % 8 == 0, "the swizzle of a lane's rows is the same");
-  const int tid = threadIdx.x & 127, c = tid % PER_ROW, r0 = tid / PER_ROW;
+  static_assert(PASS % 8 == 0 && PASS <= kPageTokens, "the swizzle of a lane's rows is the same");
+  const int tid = threadIdx.x & (32 * T::kUnpackWarps - 1), c = tid % PER_ROW, r0 = tid / PER_ROW;
   uint32_t src = from + r0 * T::RB + c * 16, ssrc = from + kPageTokens * T::RB + r0 * T::SB + (T::kInt4 ? 2 * c : 0);
   // neighbouring lanes store to different banks
   const int turn = T::kInt4 ? (c >> 1) ^ ((r0 & 1) << 1) : c >> 2 & 1;
@@ -670,7 +674,7 @@ __device__ __forceinline__ bool unpack_rows(uint32_t from, uint32_t to, int n, i
 template <int D, int FMT>
 __device__ __forceinline__ bool unpack_role(typename Shape<D, FMT>::Sh& sh, uint32_t ring0, uint32_t stage0) {
   using T = Shape<D, FMT>;
-  const int tid = threadIdx.x & 127, lane = threadIdx.x & 31;
+  const int tid = threadIdx.x & (32 * T::kUnpackWarps - 1), lane = threadIdx.x & 31;
   Ring r{0, 0};
   int stage = 0, tile_no = 0;
   uint32_t phase = 0;
@@ -1072,7 +1076,7 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
   if (T::kPlain && tid == 32) asm volatile("prefetch.tensormap [%0];" :: "l"(&map) : "memory");
   if (tid == 0) {
     for (int i = 0; i < T::kSlots; ++i) {
-      bar_init(smem_u32(&sh.full[i]), T::kPlain ? 1 : 4);
+      bar_init(smem_u32(&sh.full[i]), T::kPlain ? 1 : T::kUnpackWarps);
       bar_init(smem_u32(&sh.empty[i]), 2);
     }
     for (int i = 0; i < 2; ++i) {
@@ -1090,12 +1094,12 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
     }
     for (int i = 0; i < kItems; ++i) {
       bar_init(smem_u32(&sh.item_full[i]), 1);
-      bar_init(smem_u32(&sh.item_empty[i]), 8 + 2 + 2 + 4 + (T::kPlain ? 0 : 4));       // softmax, products, loads, rows, unpacking
+      bar_init(smem_u32(&sh.item_empty[i]), 8 + 2 + 2 + 4 + T::kUnpackWarps);       // softmax, products, loads, rows, unpacking
     }
     bar_init(smem_u32(&sh.raw), 1);
     for (int i = 0; i < T::kStages; ++i) {
       bar_init(smem_u32(&sh.st_full[i]), 1);
-      bar_init(smem_u32(&sh.st_empty[i]), 4);
+      bar_init(smem_u32(&sh.st_empty[i]), T::kPlain ? 1 : T::kUnpackWarps);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     sh.failed = 0;
@@ -1113,9 +1117,9 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(T::kRowsRegs));
     ok = rows_role<D, FMT>(p, sh, q0, tmem);
   } else {
-    if (T::kPlain || warp < 12) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(T::kLoadRegs));
+    if (warp < 8 + T::kUnpackWarps) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(T::kLoadRegs));
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(T::kMmaRegs));
-    if (warp < (T::kPlain ? 10 : 12)) {
+    if (warp < (T::kPlain ? 10 : T::kMmaWarp)) {
       if constexpr (T::kPlain) ok = load_role<D, FMT>(p, &map, sh, ring0, warp - 8);
       else ok = unpack_role<D, FMT>(sh, ring0, stage0);
     } else if (!T::kPlain && warp >= T::kFetchWarp && warp < T::kFetchWarp + 2) {
