@@ -16,14 +16,14 @@ namespace think {
 namespace {
 
 constexpr int kRows = 64, kTile = 64, kThreads = 256;
-constexpr int kExtra = 64, kShare = 7;  // see PromptCut
+constexpr int kExtra = 64;              // see PromptCut
 
 // A thread owns 4 rows (4 ty ..) and, of the logits, the tokens tx + 16 j, of the outputs the channels 4 tx + 64 j.
 template <int D>
 __global__ void __launch_bounds__(kThreads) k_paged_prompt_fp32(const PagedPromptParams p) {
   constexpr int RS = D + 4, PS = kTile + 4;         // row strides that keep 16-byte reads of neighbouring rows apart
   constexpr int J = D / 64;
-  const PromptCut cut{kExtra, kShare};
+  const PromptCut cut{kExtra};
   extern __shared__ __align__(16) float smem[];
   float* const sq = smem;
   float* const sk = sq + kRows * RS;
@@ -287,7 +287,7 @@ cudaError_t paged_prompt_setup(int dtype, int format, int D) {
   return D == 128 ? setup_fp32<128>() : setup_fp32<64>();
 }
 int paged_prompt_rows(int dtype) { return dtype == THINK_BF16 ? paged_prompt_tc_rows() : kRows; }
-PromptCut paged_prompt_cut(int dtype) { return dtype == THINK_BF16 ? paged_prompt_tc_cut() : PromptCut{kExtra, kShare}; }
+PromptCut paged_prompt_cut(int dtype) { return dtype == THINK_BF16 ? paged_prompt_tc_cut() : PromptCut{kExtra}; }
 
 cudaError_t launch_paged_prompt(const PagedPromptParams& p, int dtype, int format, const void* map, cudaStream_t s) {
   if (dtype == THINK_BF16) return p.g.D == 128 ? launch_tc<128>(p, format, map, s) : launch_tc<64>(p, format, map, s);

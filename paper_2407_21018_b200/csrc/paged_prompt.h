@@ -5,7 +5,7 @@
 // with all query heads of the key head.  Item i of a sequence at position pos sees its first pos + min((i + 1) per, rows)
 // tokens, tile by tile; it takes that many places on a line, and `extra` more for its start and end.  Sums over the
 // items of a sequence have a closed form, so a place is found without a list.  The line runs over layers and key heads,
-// in each over the sequences, and is cut evenly: a part owns the tiles that stand in it.
+// in each over the sequences, and is cut evenly, or every item is: a part owns the tiles that stand in it.
 #pragma once
 #include "paged_split.h"
 
@@ -37,7 +37,7 @@ THINK_HD int prompt_quotient(int64_t place, int64_t length) {
 }
 
 struct PromptCut {
-  int extra, share;           // places of an item besides its tokens; tokens that are worth a part of their own in short calls, log 2
+  int extra;                  // places of an item besides its tokens
   static constexpr int tile = 64;       // tokens; tile j stands at slot(j) of its item
   THINK_HD int64_t slot(int64_t j) const { return j == 0 ? 0 : extra + tile * j; }
   THINK_HD int64_t first_tile(int64_t x) const {        // that stands at x or behind
@@ -46,11 +46,15 @@ struct PromptCut {
     const int64_t j = (int64_t)(y >> 6);
     return j < 1 ? 1 : j;
   }
-  // Parts of a line: all there are for long ones; for short ones as many as items (what a small item costs is latency) and
-  // some more for long items (joining pieces costs, too).  A part may be without a tile.
-  THINK_HD int parts(int64_t total, int64_t items, int most) const {
-    const int64_t n = items + ((total - items * extra) >> share);
-    return n < most ? (int)n : most;
+  // Pieces of each item, or 0: the line is cut evenly, in one part for each CTA.  Where there are fewer items than CTAs and none is
+  // much longer than others, an item has CTAs of its own, so that none starts and ends two (64 rows over 8192 tokens, 8 items: 36
+  // instead of 40 us).  A piece may be without a tile.
+  THINK_HD int pieces(int64_t total, int64_t items, int64_t largest, int most) const {
+    if (items < 1 || items > most) return 0;
+    const int k = most / (int)items;
+    if ((largest - extra) * most > total * k) return 0;
+    const uint32_t places = (uint32_t)((uint64_t)largest >> 6) + 1, each = (places + k - 1) / k;
+    return (int)((places + each - 1) / each);         // no more than shorten the longest piece by a tile
   }
 };
 

@@ -88,46 +88,62 @@ struct PromptWalk {
 __device__ __forceinline__ bool prompt_walk_begin(const PagedPromptParams& p, const PromptCut& cut, PromptWalk& w) {
   const int lane = threadIdx.x & 31, B = p.table.B, per = (B + 31) >> 5, b0 = min(B, lane * per), b1 = min(B, b0 + per);
   bool bad = false;
-  long long upto = 0, before = 0, place = 0, items = 0;
-  int owner = -1;
-  // first the sums, then the lane with the CTA's place looks for it
+  long long upto = 0, before = 0, place = 0, items = 0, items_before = 0, largest = 0, cost = 0;
+  int owner = -1, pieces = 0, number = 0;
+  // first the sums, then the lane with the CTA's place (or item) looks for it
 #pragma unroll 1
   for (int pass = 0; pass < 2; ++pass) {
-    long long sum = before;
+    long long sum = before, num = items_before;
 #pragma unroll 1
     for (int b = b0; b < b1 && (pass == 0 || lane == owner); ++b) {
       const PromptSeq s = prompt_seq(p, b, bad);
       const PromptLine line = prompt_line(p, s, cut.extra);
       const long long n = line.total();
-      if (pass == 1 && place < sum + n) {
+      const int m = line.items();
+      if (pass == 1 && (pieces ? number < num + m : place < sum + n)) {
         w.b = b;
-        w.i = line.find(place - sum);
+        w.i = pieces ? number - (int)num : line.find(place - sum);
         w.s = s;
         w.at = sum + line.begin(w.i);
+        cost = line.cost(w.i);
         break;
       }
       sum += n;
-      items += line.items();
+      num += m;
+      if (m > 0) largest = max(largest, (long long)line.cost(m - 1));
     }
     if (pass == 1) break;
     upto = sum;
+    items = num;
 #pragma unroll 1
     for (int o = 1; o < 32; o <<= 1) {
-      const long long y = __shfl_up_sync(0xffffffffu, upto, o);
-      if (lane >= o) upto += y;
-      items += __shfl_xor_sync(0xffffffffu, items, o);
+      const long long y = __shfl_up_sync(0xffffffffu, upto, o), z = __shfl_up_sync(0xffffffffu, items, o);
+      if (lane >= o) {
+        upto += y;
+        items += z;
+      }
+      largest = max(largest, __shfl_xor_sync(0xffffffffu, largest, o));
     }
     before = upto - sum;
+    items_before = items - num;
     const long long W = __shfl_sync(0xffffffffu, upto, 31), total = W * p.nlayers * p.g.N_kv;
-    const int parts = cut.parts(total, items * p.nlayers * p.g.N_kv, p.grid);
+    const long long each = __shfl_sync(0xffffffffu, items, 31), all = each * p.nlayers * p.g.N_kv;
     if (bad && blockIdx.x == 0) atomicOr(p.error, kErrPage);
-    if (W == 0 || (int)blockIdx.x >= parts) return false;
-    const PromptShare share(total, parts);
-    w.begin = share.begin(blockIdx.x);
-    w.end = share.begin(blockIdx.x + 1);
-    w.lh = prompt_quotient(w.begin, W);
-    place = w.begin - w.lh * W;
-    owner = __ffs(__ballot_sync(0xffffffffu, place < upto)) - 1;      // the first lane whose sequences reach behind it
+    if (W == 0) return false;
+    pieces = cut.pieces(total, all, largest, p.grid);
+    if (pieces) {
+      number = (int)blockIdx.x / pieces;
+      if (number >= all) return false;
+      w.lh = number / (int)each;
+      number -= w.lh * (int)each;
+    } else {
+      const PromptShare share(total, p.grid);
+      w.begin = share.begin(blockIdx.x);
+      w.end = share.begin(blockIdx.x + 1);
+      w.lh = prompt_quotient(w.begin, W);
+      place = w.begin - w.lh * W;
+    }
+    owner = __ffs(__ballot_sync(0xffffffffu, pieces ? number < items : place < upto)) - 1;      // the first lane whose sequences reach behind it
     w.at = W;
   }
   const long long W = __shfl_sync(0xffffffffu, upto, 31);
@@ -137,7 +153,13 @@ __device__ __forceinline__ bool prompt_walk_begin(const PagedPromptParams& p, co
   w.s.rows = __shfl_sync(0xffffffffu, w.s.rows, owner);
   w.s.start = __shfl_sync(0xffffffffu, w.s.start, owner);
   w.at = w.lh * W + __shfl_sync(0xffffffffu, w.at, owner);
-  return true;
+  if (pieces) {
+    const PromptShare share(__shfl_sync(0xffffffffu, cost, owner), pieces);
+    const int j = (int)blockIdx.x % pieces;
+    w.begin = w.at + share.begin(j);
+    w.end = w.at + share.begin(j + 1);
+  }
+  return w.begin < w.end;
 }
 
 // What of the current item belongs to this CTA.
