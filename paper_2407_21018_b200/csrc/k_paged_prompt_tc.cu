@@ -36,7 +36,9 @@ namespace think {
 namespace {
 
 constexpr int kHalf = 128, kItemRows = 2 * kHalf;
-constexpr int kExtra = 256;             // see PromptCut: starting and ending an item costs as much as four tiles (ragged e4m3 batch 295 us; with 0 345)
+// See PromptCut: starting and ending an item costs as much as six tiles (a prompt of 8192 bf16 tokens, a ragged e4m3 batch of 48 in us with
+// 128: 534, 315, 256: 496, 297, 384: 489, 291, 640: 498, 319).
+constexpr int kExtra = 384;
 
 // ---- PTX
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }

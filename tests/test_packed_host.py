@@ -36,7 +36,7 @@ int main() {
       bad += prompt_quotient(len * q, len) != q || prompt_quotient(len * q + len - 1, len) != q || prompt_quotient(len * q + below(len), len) != q;
     }
   }
-  for (PromptCut cut : {PromptCut{256}, PromptCut{64}}) {
+  for (PromptCut cut : {PromptCut{384}, PromptCut{64}}) {
     for (int64_t x = -70; x < 2000; ++x) {
       const int64_t j = cut.first_tile(x);
       bad += cut.slot(j) < x || (j > 0 && cut.slot(j - 1) >= x);
@@ -130,7 +130,7 @@ cudaError_t paged_decode_setup(int, int, int, int) { return cudaSuccess; }
 cudaError_t paged_prompt_setup(int, int, int) { return cudaSuccess; }
 size_t paged_decode_record_bytes(int ctas) { return 4096 * (size_t)ctas; }
 int paged_prompt_rows(int dtype) { return dtype == THINK_BF16 ? 256 : 64; }
-PromptCut paged_prompt_cut(int) { return PromptCut{256}; }
+PromptCut paged_prompt_cut(int) { return PromptCut{384}; }
 }
 """
 
