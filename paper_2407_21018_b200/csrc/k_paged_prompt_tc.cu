@@ -15,13 +15,13 @@
 // P is rounded to bf16 (2^-9 of a weight on average, what the products take); l sums the unrounded weights, with what its
 // additions lose carried along, in fp32.
 //
-// What bounds it (a prompt of 8192 tokens, 32 heads of 128 over 8 key heads, 490 us replayed: 0.55 TFLOP at 1120 TFLOP/s, 0.69 of the
-// measured GEMM rate; 0.59 among other calls, where the clock falls): nothing alone.  Tensor pipe and exponentials are each busy
+// What bounds it (a prompt of 8192 tokens, 32 heads of 128 over 8 key heads, 493 us replayed: 0.55 TFLOP at 1115 TFLOP/s, 0.68 of the
+// measured GEMM rate; 583 among other calls, where the clock falls): nothing alone.  Tensor pipe and exponentials are each busy
 // for 47 % of the cycles: products of 64 tokens wait for shared memory (S: 48 instead of 32 cycles each, Q and K are both read), 16
 // exponentials a cycle and SM take 1024 cycles a tile of both halves against 1280 of products, and a scheduler has one warp of each half to
-// overlap the rest of a softmax with.  e4m3 adds the unpacking (8192 tokens 680 us), 4 bits twice the products (1100 us).  Few rows: DRAM
-// (8 rows over 131072 tokens, twice, 1.07 GB in 172 us).  Short calls: code that is fetched for the first time (100 tokens: 21 us and
-// 6 for the join).  Loops stay rolled for that, and because the roles' code together misses the instruction cache.
+// overlap the rest of a softmax with.  e4m3 adds the unpacking (8192 tokens 620 to 750 us), 4 bits twice the products (800 us).  Few rows: DRAM
+// (8 rows over 131072 tokens, twice, 1.07 GB in 174 us).  Short calls: code that is fetched for the first time (100 tokens: 22 us,
+// the join among them).  Loops stay rolled for that, and because the roles' code together misses the instruction cache.
 // Tiles of 128 tokens, whose S has one place a half, took 563 us for the same prompt; P in places of its own and S read ahead of
 // the weights of the tile before 515; exponentials in part by a polynomial, or of the halves strictly in turn, were slower too.
 // Every wait is bounded (about a second): on a time-out the CTA raises the error word, frees its tensor memory and leaves.
