@@ -432,3 +432,19 @@ def test_a_packed_step_end_to_end():
         if keys[b]:
             want, _, _ = po.attention(last[b, 0, :4].double().cpu().numpy(), np.stack(keys[b])[:, 0], np.stack(vals[b])[:, 0], D ** -0.5)
             assert np.abs(got[b, 0, :4].double().cpu().numpy() - want).max() < 0.02
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS, ids=IDS)
+@pytest.mark.parametrize("rows,held,N_kv,L", [
+    ([5], [9000], 1, 1),                                       # one item over all CTAs
+    ([4, 4, 4], [3000, 3001, 2950], 2, 1),                     # items of CTAs of their own
+    ([1 + 7 * b % 90 for b in range(23)], [(311 * b) % 700 for b in range(23)], 4, 2),         # more items than CTAs
+    ([3, 1] + [2] * 30, [6000, 5] + [10 * b for b in range(30)], 1, 2),                       # fewer, one of them long
+], ids=["one", "alike", "many", "unlike"])
+def test_ways_in_which_work_is_cut(fmt, dtype, rows, held, N_kv, L):
+    p = Prompt(fmt, dtype, rows, held, D=128, N_kv=N_kv, G=4, L=L, seed=9)
+    out, lse = p.call()
+    p.check(out, lse, lambda b, s: s in (0, rows[b] - 1) or (s % 40 == 0 and b % 3 == 0))
+    assert p.cache.device_error() == 0
+    again = p.call()
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
