@@ -507,8 +507,10 @@ thinK_status thinK_paged_prompt_attn(thinK_paged* p, thinK_tensor5 q, thinK_tens
 /* Bytes of the scratch buffer of thinK_paged_prompt_attn (0 if p is NULL). */
 size_t thinK_paged_prompt_scratch(const thinK_paged* p);
 
-/* The handle's error word (bits 8 and 16 above), read with a synchronous copy; wait for the calls that it is to cover
- * first.  The word keeps its bits as long as the handle lives. */
+/* The handle's error word, read with a synchronous copy; wait for the calls that it is to cover first.  Bits: 8 and 16 as
+ * above; of thinK_paged_prompt_attn on bf16 caches also 2, a bounded wait inside the kernel ran out, and 4, a block found its
+ * shared memory misaligned (rows that such a block had to compute are not to be relied on).  The word keeps its bits as long as
+ * the handle lives. */
 thinK_status thinK_paged_device_error(thinK_paged* p, int32_t* out_code);
 
 thinK_status thinK_paged_destroy(thinK_paged* p);

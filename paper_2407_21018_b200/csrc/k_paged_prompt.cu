@@ -190,9 +190,10 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_paged_prompt_join(const Pag
   constexpr int W = D / 32;                         // channels of a lane
   begin_dependent();
   const PromptDesc d = p.desc[blockIdx.x];
-  if (!d.begins) return;
+  if (!d.names_item(p.table.B, p.nlayers * p.g.N_kv)) return;
   bool bad = false;
   const PromptSeq seq = prompt_seq(p, d.b, bad);
+  if (d.item >= prompt_line(p, seq, 0).items()) return;
   const int lane = threadIdx.x & 31;
   int pieces = 2;                                   // up to the CTA that ends it
   for (int c = blockIdx.x + 1;; c += 32) {

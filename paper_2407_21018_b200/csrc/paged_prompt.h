@@ -75,4 +75,14 @@ struct PromptLine {           // a sequence's items
   }
 };
 
+// Of a CTA: the item that it begins and another ends, if there is one; and what it does with the one that it is in the middle
+// of when it begins.
+struct PromptDesc {
+  int lh, b, item;
+  int16_t begins, carries;    // carries: 0 none, 1 ends it, 2 hands it on
+  // Whether the item that it begins is one of a call of B sequences and `heads` layers and key heads; its number is looked at
+  // with the sequence's rows.  (A CTA whose waits ran out leaves an empty one behind; nothing else may become an address.)
+  THINK_HD bool names_item(int B, int heads) const { return begins != 0 && b >= 0 && b < B && lh >= 0 && lh < heads && item >= 0; }
+};
+
 }  // namespace think

@@ -5,13 +5,6 @@
 
 namespace think {
 
-// Of a CTA: the item that it begins and another ends, if there is one; and what it does with the one that it is in the middle
-// of when it begins.
-struct PromptDesc {
-  int lh, b, item;
-  int16_t begins, carries;    // carries: 0 none, 1 ends it, 2 hands it on
-};
-
 struct PagedPromptParams {
   PageGeom g;
   const uint8_t* pages;

@@ -1,0 +1,44 @@
+"""CPU checks of packed batches where a call or a kernel goes wrong: what the host side of an entry point answers, and what a
+kernel may trust."""
+from test_paged_host import compile_and_run
+
+
+def test_descriptors_that_nobody_wrote(tmp_path):
+    """The join of cut items takes a descriptor for an item only if its sequence, its layer and head and its number exist: random
+    bytes and the values next to every limit."""
+    out = compile_and_run(tmp_path, r"""
+#include <stdio.h>
+#include <string.h>
+#include <random>
+#include "paged_prompt.h"
+using namespace think;
+int main() {
+  std::mt19937_64 g(1);
+  long bad = 0, taken = 0;
+  auto check = [&](const PromptDesc& d, int B, int heads) {
+    const bool in = d.begins && 0 <= d.b && d.b < B && 0 <= d.lh && d.lh < heads && 0 <= d.item;
+    bad += d.names_item(B, heads) != in;
+    taken += in;
+  };
+  for (int it = 0; it < 300000; ++it) {
+    PromptDesc d;
+    uint32_t w[sizeof(d) / 4];
+    for (uint32_t& x : w) x = (uint32_t)g();
+    memcpy((void*)&d, w, sizeof(d));
+    const int B = 1 + (int)(g() % 4096), heads = 1 + (int)(g() % 1000);
+    check(d, B, heads);
+    for (int b : {-1, 0, B - 1, B}) for (int lh : {-1, 0, heads - 1, heads}) for (int item : {-2147483647 - 1, -1, 0, 2147483647})
+      for (int16_t begins : {0, 1, -1}) check(PromptDesc{lh, b, item, begins, d.carries}, B, heads);
+    bad += PromptDesc{0, 0, 0, 0, 0}.names_item(B, heads);
+  }
+  // an item's number against the sequence's: none of a sequence without rows, and what numbers stand for stays within rows
+  for (int rows = 0; rows < 600; ++rows)
+    for (int per : {1, 7, 64, 256}) {
+      const int items = PromptLine{0, rows, per}.items();
+      bad += rows == 0 ? items != 0 : (items - 1) * per >= rows || items * per < rows;
+    }
+  bad += PromptLine{0, 2147483647, 1}.items() != 2147483647;
+  printf("%ld %d\n", bad, taken > 1000);
+}
+""")
+    assert out.split() == ["0", "1"]
