@@ -1073,11 +1073,11 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
   begin_dependent();
   const int tid = threadIdx.x, warp = tid >> 5;
   const uint32_t q0 = smem_u32(smem), ring0 = q0 + T::kQBytes, stage0 = q0 + T::kStageAt;
-  // What the join finds if this block gives up: nothing.  The warp that walks along the items stores the true one, behind the
-  // barrier below.
-  if (tid == 0) p.desc[blockIdx.x] = PromptDesc{0, 0, 0, 0, 0};
   if (q0 & 1023) {
-    if (tid == 0) atomicOr(p.error, kErrSmemAlign);
+    if (tid == 0) {
+      atomicOr(p.error, kErrSmemAlign);
+      p.desc[blockIdx.x] = PromptDesc{0, 0, 0, 0, 0};
+    }
     return;
   }
   if (warp == T::kMmaWarp) {
@@ -1146,6 +1146,7 @@ __global__ void __launch_bounds__(Shape<D, FMT>::kThreads, 1) k_paged_prompt_tc(
   fence_before();
   __syncthreads();
   if (sh.failed) {                       // copies and products under way end before their memory is given up
+    if (tid == 0) p.desc[blockIdx.x] = PromptDesc{0, 0, 0, 0, 0};      // (the walk may not have come to its end: nothing to join)
     const long long t0 = clock64();
     while (clock64() - t0 < 4000000LL) {}
   }
