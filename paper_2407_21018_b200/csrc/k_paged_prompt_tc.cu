@@ -24,7 +24,7 @@
 // the join among them).  Loops stay rolled for that, and because the roles' code together misses the instruction cache.
 // Tiles of 128 tokens, whose S has one place a half, took 563 us for the same prompt; P in places of its own and S read ahead of
 // the weights of the tile before 515; exponentials in part by a polynomial, or of the halves strictly in turn, were slower too.
-// Every wait is bounded (about a second): on a time-out the CTA raises the error word, frees its tensor memory and leaves.
+// Every wait is bounded (about a second, those for whole items by the others): on a time-out the CTA raises the error word, frees its tensor memory and leaves.
 #include <math.h>
 #include <string.h>
 
@@ -151,6 +151,18 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
 }
 // the same for a whole warp, whose lanes agree on the answer
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, bar_wait(bar, parity)); }
+// A warp's wait that spans items: the warps that load queries and store outputs wait for all of an item, softmax warps of a half
+// without rows for the next one, and with tables of 2^31 tokens an item is 2^25 tiles (half a minute).  It ends when a wait of
+// another warp, for a tile, ran out, and by itself after minutes.
+__device__ __forceinline__ bool warp_wait_long(const uint32_t& failed, uint32_t bar, uint32_t parity) {
+  bool ok = bar_try(bar, parity);
+  if (!ok) {
+    const long long t0 = clock64();
+    while (!(ok = bar_try(bar, parity)))
+      if (*(const volatile uint32_t*)&failed || clock64() - t0 > (1LL << 39)) break;
+  }
+  return __all_sync(0xffffffffu, ok);
+}
 __device__ __forceinline__ void tma_load(uint32_t lead, uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
   asm volatile(
       "{\n\t"
@@ -375,10 +387,10 @@ struct Items {
   int no;
   __device__ __forceinline__ uint32_t phase() const { return no / kItems & 1; }
   // The next item; false on a time-out.  Every lane has its own copy of what it uses before the place is given back.
-  template <typename Sh, typename F>
+  template <bool LONG = false, typename Sh, typename F>
   __device__ __forceinline__ bool take(Sh& sh, F copy) {
     const int slot = no & (kItems - 1);
-    if (!warp_wait(smem_u32(&sh.item_full[slot]), phase())) return false;
+    if (!(LONG ? warp_wait_long(sh.failed, smem_u32(&sh.item_full[slot]), phase()) : warp_wait(smem_u32(&sh.item_full[slot]), phase()))) return false;
     copy(*(const Item*)&sh.items[slot]);
     __syncwarp();
     if ((threadIdx.x & 31) == 0) bar_arrive(smem_u32(&sh.item_empty[slot]));
@@ -827,7 +839,7 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, typenam
   Items items{0};
   for (;; ++items.no) {
     int last, rows, see, n, pos0, t0, tiles, end;
-    if (!items.take(sh, [&](const Item& i) {
+    if (!items.take<true>(sh, [&](const Item& i) {
           last = i.last; rows = i.rows[half]; see = i.see[half]; n = i.n; pos0 = i.pos0; t0 = i.t0; tiles = i.tiles; end = i.end[half];
         })) return false;
     if (last) return true;
@@ -940,12 +952,12 @@ __device__ __forceinline__ bool rows_role(const PagedPromptParams& p, typename S
   it.last = 1;
   for (;; ++items.no) {
     Item next;
-    if (!items.take(sh, [&](const Item& i) { next = i; })) return false;
+    if (!items.take<true>(sh, [&](const Item& i) { next = i; })) return false;
     if (!next.last) {
 #pragma unroll 1
       for (int half = 0; half < 2; ++half) {
         if ((half ? next.end[1] : next.end[0]) == 0) continue;
-        if (!warp_wait(smem_u32(&sh.q_empty[half]), (phases >> half & 1) ^ 1)) return false;
+        if (!warp_wait_long(sh.failed, smem_u32(&sh.q_empty[half]), (phases >> half & 1) ^ 1)) return false;
         phases ^= 1u << half;
         fence_after();
         const int rows = half ? next.rows[1] : next.rows[0], ri = half * kHalf;
@@ -984,10 +996,10 @@ __device__ __forceinline__ bool rows_role(const PagedPromptParams& p, typename S
         const bool some = end > 0, on = row < (half ? it.rows[1] : it.rows[0]);
         float m = -INFINITY, l = 0.f;
         if (some) {
-          if (!warp_wait(smem_u32(&sh.stats_full[half]), phases >> (2 + half) & 1)) return false;
+          if (!warp_wait_long(sh.failed, smem_u32(&sh.stats_full[half]), phases >> (2 + half) & 1)) return false;
           m = sh.stats[half][0][row];
           l = sh.stats[half][1][row];
-          if (!warp_wait(smem_u32(&sh.o_done[half]), phases >> (4 + half) & 1)) return false;
+          if (!warp_wait_long(sh.failed, smem_u32(&sh.o_done[half]), phases >> (4 + half) & 1)) return false;
           phases ^= 20u << half;
           fence_after();
         }

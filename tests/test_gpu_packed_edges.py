@@ -1,0 +1,35 @@
+"""GPU tests of packed batches at the ends of their ranges: the longest sequences, the largest and smallest values and scales, the
+batch sizes at which a launch changes its form.  Bounds as in test_gpu_prompt."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged_oracle as po
+from test_gpu_prompt import FMT, IDS, KINDS, PAGE, Prompt, binding, bounds, gen, ints
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("fmt", ["plain", "int4"])
+def test_items_that_take_seconds(fmt):
+    """148 items of 268 million tokens, one a block (the table names one page again and again): warps wait for longer than any wait
+    without a tile may last.  Only the sum of the softmax is looked at; outputs of so many equal addends carry (n + 16) u."""
+    tk = binding()
+    N, D, pages = 148, 64, 1 << 22
+    cache = tk.PagedKVCache(tk.make_paged_config(1, N, N, D, 1, 1, torch.bfloat16, FMT[fmt]))
+    g = gen(1)
+    k, v = (torch.randn(1, PAGE, 1, N, D, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    one = ints([[0]])
+    cache.write(k, v, one)
+    q = torch.randn(1, 1, 1, N, D, generator=g, device="cuda").to(torch.bfloat16)
+    _, short = cache.prompt_attn(q, one, ints([PAGE - 1]), return_lse=True)
+    table = torch.zeros(1, pages, dtype=torch.int32, device="cuda")
+    a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    a.record()
+    _, lse = cache.prompt_attn(q, table, ints([pages * PAGE - 1]), return_lse=True)
+    b.record()
+    b.synchronize()
+    assert cache.device_error() == 0
+    assert a.elapsed_time(b) > 1200                      # (2e9 cycles are 1.02 s at 1965 MHz)
+    # the sum keeps what its additions lose, so only its own few roundings count: exp2 2^-21, log and its product 4 u |lse|
+    assert (lse - short - 22 * np.log(2.0)).abs().max() <= 2 * (2.0 ** -20 + 4 * 2.0 ** -23 * float(lse.abs().max()))
