@@ -22,6 +22,8 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kPer = 4;              // sequences of a thread: kMaxPagedBatch / 1024
+constexpr int kParts = 32;           // warps, at most
+__host__ __device__ constexpr size_t plan_smem(int B) { return sizeof(long long) * kParts + sizeof(int) * (4 * (size_t)B + 3); }
 
 __host__ __device__ constexpr int pages_of(int n) { return (int)(((int64_t)n + kPageTokens - 1) / kPageTokens); }
 
@@ -58,11 +60,11 @@ __device__ __forceinline__ int last_at_or_below(const int* at, int n, int x) {
 }
 
 __global__ void __launch_bounds__(1024) k_paged_plan(const PagedPlanParams p) {
-  extern __shared__ int smem[];
-  __shared__ long long s_part[32];
+  extern __shared__ long long smem[];
+  long long* const s_part = smem;
   begin_dependent();
   const int tid = threadIdx.x, nt = blockDim.x, B = p.table.B;
-  int* const s_start = smem;                         // [B + 1] granted tokens in front of a sequence
+  int* const s_start = (int*)(s_part + kParts);      // [B + 1] granted tokens in front of a sequence
   int* const s_held = s_start + B + 1;               // [B]     tokens held before, less what it loses
   int* const s_take = s_held + B;                    // [B + 1] pages taken in front of a sequence
   int* const s_give = s_take + B + 1;                // [B + 1] pages given back in front of a sequence
@@ -207,10 +209,14 @@ cudaError_t launch_paged_plan(const PagedPlanParams& p, cudaStream_t s) {
   // the tokens are too many for it (2048: 6.6 against 8.1 us; 7680: 13.9 against 8.4).
   const bool small = p.table.B <= 256 * kPer && p.max_tokens <= 2048;
   const int ctas = small ? 1 : 8, threads = small ? 256 : 1024;
-  const size_t smem = sizeof(int) * (4 * (size_t)p.table.B + 3);
+  const size_t smem = plan_smem(p.table.B);          // all that the kernel has
   if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(k_paged_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
+    // (the same value in every call: calls of different sizes on several threads do not take it away from one another)
+    const cudaError_t e = cudaFuncSetAttribute(k_paged_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan_smem(kMaxPagedBatch));
+    if (e != cudaSuccess) {
+      (void)cudaGetLastError();                      // reported here, not by the caller's next check
+      return e;
+    }
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ctas);

@@ -1,5 +1,9 @@
 """GPU tests of packed batches at the ends of their ranges: the longest sequences, the largest and smallest values and scales, the
 batch sizes at which a launch changes its form.  Bounds as in test_gpu_prompt."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -33,3 +37,24 @@ def test_items_that_take_seconds(fmt):
     assert a.elapsed_time(b) > 1200                      # (2e9 cycles are 1.02 s at 1965 MHz)
     # the sum keeps what its additions lose, so only its own few roundings count: exp2 2^-21, log and its product 4 u |lse|
     assert (lse - short - 22 * np.log(2.0)).abs().max() <= 2 * (2.0 ** -20 + 4 * 2.0 ** -23 * float(lse.abs().max()))
+
+
+PLAN_SIZES = r"""
+import sys
+sys.path[:0] = sys.argv[1:]
+import torch
+from test_gpu_packed import check_plan, small_cache, Step
+for B in (3040, 3055, 3056, 3071, 3072, 3056, 4096):
+    step = Step([b % 130 for b in range(B)], [(b * 7) % 5 - 1 for b in range(B)], 3, 900, 2 * B)
+    cache = small_cache(step.num_pages, B)
+    change, lens, table, free_pages, count = step.upload()
+    check_plan(cache.plan(change, lens, table, free_pages, count, step.max_tokens), table, free_pages, step.want())
+print("fine")
+"""
+
+
+def test_plan_around_48_kb_of_shared_memory():
+    """In a process of its own: a larger call before may not be what makes one work."""
+    tests = os.path.dirname(os.path.abspath(__file__))
+    r = subprocess.run([sys.executable, "-c", PLAN_SIZES, tests, os.path.dirname(tests)], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.split() == ["fine"], r.stdout + r.stderr
