@@ -183,17 +183,17 @@ __global__ void __launch_bounds__(kThreads) k_paged_prompt_fp32(const PagedPromp
   if (tid == 0) p.desc[blockIdx.x] = desc;
 }
 
-// Joins the pieces of the items that were cut, in their order: a warp per row, the states' statistics over its lanes.
+// Joins the pieces of the items that were cut, in their order: a warp per row, the states' statistics over its lanes.  Two blocks
+// an SM: with more than 32 registers there is one, and a prompt of 8192 tokens takes 8 us longer.
 constexpr int kJoinWarps = 32;
 template <int D, int E, int ROWS>
-__global__ void __launch_bounds__(32 * kJoinWarps) k_paged_prompt_join(const PagedPromptParams p) {
+__global__ void __launch_bounds__(32 * kJoinWarps, 2) k_paged_prompt_join(const PagedPromptParams p) {
   constexpr int W = D / 32;                         // channels of a lane
   begin_dependent();
   const PromptDesc d = p.desc[blockIdx.x];
   if (!d.names_item(p.table.B, p.nlayers * p.g.N_kv)) return;
   bool bad = false;
   const PromptSeq seq = prompt_seq(p, d.b, bad);
-  if (d.item >= prompt_line(p, seq, 0).items()) return;
   const int lane = threadIdx.x & 31;
   int pieces = 2;                                   // up to the CTA that ends it
   for (int c = blockIdx.x + 1;; c += 32) {
@@ -204,8 +204,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_paged_prompt_join(const Pag
     }
   }
   const int r = blockIdx.y * kJoinWarps + (threadIdx.x >> 5);
-  const int s0 = d.item * p.per, rows = min(p.per, seq.rows - s0) * p.G;
-  if (r >= rows) return;
+  const int64_t s0 = (int64_t)d.item * p.per;
+  const int rows = (int)max((int64_t)0, min((int64_t)p.per, seq.rows - s0)) * p.G;
+  if (r >= rows) return;                            // (nor is there an item behind the sequence's last row)
   constexpr size_t kRec = (size_t)ROWS * (D + 2);
   auto rec = [&](int i) { return (const float*)p.records + (i == 0 ? 2 * blockIdx.x + 1 : 2 * (blockIdx.x + i)) * kRec; };
   float m = -INFINITY;

@@ -82,7 +82,9 @@ struct PromptDesc {
   int16_t begins, carries;    // carries: 0 none, 1 ends it, 2 hands it on
   // Whether the item that it begins is one of a call of B sequences and `heads` layers and key heads; its number is looked at
   // with the sequence's rows.  (A CTA whose waits ran out leaves an empty one behind; nothing else may become an address.)
-  THINK_HD bool names_item(int B, int heads) const { return begins != 0 && b >= 0 && b < B && lh >= 0 && lh < heads && item >= 0; }
+  THINK_HD bool names_item(int B, int heads) const {
+    return (begins != 0) & ((uint32_t)b < (uint32_t)B) & ((uint32_t)lh < (uint32_t)heads) & (item >= 0);
+  }
 };
 
 }  // namespace think
