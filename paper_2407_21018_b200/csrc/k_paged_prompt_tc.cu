@@ -9,8 +9,9 @@
 // Roles: warps 0-3 and 4-7 the softmax of a half each; a warp for the products of each half; a warp for keys and one for values
 // bring them into a ring of shared-memory slots (bf16 pages by TMA; others as bytes by bulk copies, which four or eight warps
 // unpack from stages into the ring); four warps load the next item's queries and store the last item's outputs, so that the others
-// go from item to item without a pause.  One of the loading warps walks along the items and hands out their description.  m only
-// moves when a row's logits pass it by 2^8 (O is then rescaled in tensor memory), so the softmax seldom waits for the products.
+// go from item to item without a pause.  One of the loading warps walks along the items and hands out their description.  m stands
+// 2^8 above the largest logit and only moves when one passes it (O is then rescaled in tensor memory), so the softmax seldom waits
+// for the products.
 // 4-bit values n * s have 11 bits: they enter as the sum of two bf16, which is exact, at twice the products.
 // P is rounded to bf16 (2^-9 of a weight on average, what the products take); l sums the unrounded weights, with what its
 // additions lose carried along, in fp32.
@@ -39,6 +40,9 @@ constexpr int kHalf = 128, kItemRows = 2 * kHalf;
 // See PromptCut: starting and ending an item costs as much as six tiles (a prompt of 8192 bf16 tokens, a ragged e4m3 batch of 48 in us with
 // 128: 534, 315, 256: 496, 297, 384: 489, 291, 640: 498, 319).
 constexpr int kExtra = 384;
+// A row's reference m stands so far (in base 2) above the largest logit there was when it last moved, and moves when a logit passes
+// it: seldom, and no weight is above 1, so that a weight times a value passes fp32 only where the value does.
+constexpr float kAbove = 8.f;
 
 // ---- PTX
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -881,8 +885,9 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, typenam
       for (int j = 0; j < KT; j += 8)
 #pragma unroll
         for (int i = 0; i < 4; ++i) mx[i] = max3(mx[i], __uint_as_float(sr[j + 2 * i]), __uint_as_float(sr[j + 2 * i + 1]));
-      const float m_new = fmaxf(m, max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * p.scale_log2);
-      if (__any_sync(0xffffffffu, m_new > m + 8.f)) {
+      const float top = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * p.scale_log2;
+      if (__any_sync(0xffffffffu, top > m)) {           // see kAbove
+        const float m_new = fmaxf(m, top + kAbove);
         const float f = m == m_new ? 1.f : ex2(m - m_new);
         if (i > 0) {
           // the product before this tile's is done when the logits of the next tile are, which are computed behind it; in the

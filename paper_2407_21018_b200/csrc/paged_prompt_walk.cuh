@@ -23,8 +23,8 @@ struct PagedPromptParams {
   FastDiv by_group, by_heads;
 };
 
-// A piece's state, row by row: O [rows][D] (not divided by l), m, l [rows].  m: the largest logit in base 2 that the weights
-// are relative to.  l = 0 and m = -infinity: no token; l = 1 with that m: tokens, but all their logits are -infinity.
+// A piece's state, row by row: O [rows][D] (not divided by l), m, l [rows].  m: the logit in base 2 that the weights are relative
+// to, the largest one or up to 2^8 above it.  l = 0 and m = -infinity: no token; l = 1 with that m: tokens, but all their logits are -infinity.
 __host__ __device__ inline size_t prompt_record_floats(int rows, int D) { return (size_t)rows * (D + 2); }
 
 // `map`: of a bf16 cache of plain pages, the pool as rows of D elements in boxes of 64 x 64 (a CUtensorMap)

@@ -58,3 +58,25 @@ def test_plan_around_48_kb_of_shared_memory():
     tests = os.path.dirname(os.path.abspath(__file__))
     r = subprocess.run([sys.executable, "-c", PLAN_SIZES, tests, os.path.dirname(tests)], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and r.stdout.split() == ["fine"], r.stdout + r.stderr
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS, ids=IDS)
+@pytest.mark.parametrize("value", [2.0 ** 127, -1.75 * 2.0 ** 126])
+def test_large_values_at_logits_above_those_before(fmt, dtype, value):
+    """A token in the second tile has a weight of e^4 relative to all tokens of the first, and a value next to the type's largest: its
+    share is 0.3 of that value, whatever the weights are relative to on the way."""
+    t, n = 90, 120
+
+    def keys(k):
+        k[:] = 0
+        k[0, t] = 2.0
+
+    def values(v):
+        v[0, t, 0, 0, 5] = value
+
+    p = Prompt(fmt, dtype, [n], [0], N_kv=1, G=4, D=64, k_edit=keys, v_edit=values)
+    p.q.fill_(0.25)
+    out, lse = p.call()
+    p.check(out, lse, lambda b, s: s < 4 or s >= t - 2)
+    share = out[t:, 0, :, 5].double() / value
+    assert (share > 0.25).all() and (share < 0.45).all()
