@@ -497,7 +497,8 @@ thinK_status thinK_paged_decode_attn(thinK_paged* p, const void* q, void* out, f
  * tokens gets out = 0 and lse = -infinity; one with tokens whose logits are all -infinity out = NaN and lse = -infinity.
  * What a row does not see does not reach it, whatever it holds (NaN, infinities).
  * Logits, softmax sums and outputs are accumulated in fp32 from the stored values, which enter exactly (4-bit ones, of 11
- * bits, as the sum of two bf16).  On bf16 caches a weight meets the values rounded to bf16 (2^-8 of itself at most; weights
+ * bits, as the sum of two bf16; values past bf16's largest, which a row that holds that number may be stored as in E4M3, count as
+ * infinite as they do when read back, 4-bit ones from 2^129 - 2^121 on, which no written row holds).  On bf16 caches a weight meets the values rounded to bf16 (2^-8 of itself at most; weights
  * below 2^-118 of the largest may count as none); the softmax sum takes it unrounded.  fp32 caches compute in fp32.  Results do not
  * depend on timing. */
 thinK_status thinK_paged_prompt_attn(thinK_paged* p, thinK_tensor5 q, thinK_tensor5 out, float* lse, thinK_page_table table,

@@ -326,7 +326,11 @@ __device__ __forceinline__ uint2 e4m3_to_bf16(uint32_t w, float s) {
 }
 // 8 4-bit codes times their scale (bf16, twice) as the sum of two bf16: the product rounded, and what the rounding took away
 // (n s has 11 bits, so the rest fits).  Channels come out in the order 0 4 1 5 2 6 3 7, which saves sorting them: queries are
-// permuted alike, and outputs back.
+// permuted alike, and outputs back.  7 s may round past the largest bf16 number (a group whose largest magnitude is that number):
+// the first part ends there, and the second has what is missing, exactly as long as it fits (|n s| < 2^129 - 2^121).  BOUND:
+// what does not fit, which no written row holds, ends at that number too, for a value that some rows must not meet as infinite.
+constexpr uint32_t kMostBf16 = 0x7f7f7f7fu;
+template <bool BOUND>
 __device__ __forceinline__ void int4_to_bf16(uint32_t w, uint32_t s2, uint4& hi, uint4& lo) {
   uint32_t h[4], l[4];
 #pragma unroll
@@ -334,7 +338,9 @@ __device__ __forceinline__ void int4_to_bf16(uint32_t w, uint32_t s2, uint4& hi,
     uint32_t n;
     asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(n) : "r"(((w >> (4 * i)) & 0x000f000fu) | 0x43004300u), "r"(0xc308c308u));      // (128 + c) - 136
     asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(h[i]) : "r"(n), "r"(s2));
+    asm("min.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(h[i]) : "r"(kMostBf16));      // (a NaN scale: the second part is NaN)
     asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(l[i]) : "r"(n), "r"(s2), "r"(h[i] ^ 0x80008000u));
+    if (BOUND) asm("min.NaN.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(l[i]) : "r"(kMostBf16));
   }
   hi = make_uint4(h[0], h[1], h[2], h[3]);
   lo = make_uint4(l[0], l[1], l[2], l[3]);
@@ -344,19 +350,24 @@ __device__ __forceinline__ uint4 int4_order(const uint4& v) {          // 8 chan
   return make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
 }
 
-// A value of the pool as fp32, for the few that are looked at one by one.
+// A value of the pool that is a NaN or an infinity, as fp32, or 0: for the few that are looked at one by one.  (A 4-bit one of a
+// finite scale is finite.)
 template <int D, int FMT>
-__device__ float value_at(const uint8_t* block, int slot, int c) {
+__device__ float non_finite_value(const uint8_t* block, int slot, int c) {
   using T = Shape<D, FMT>;
   const uint8_t* const row = block + (kPageTokens + slot) * T::RB;
   const uint8_t* const sc = block + 2 * kPageTokens * T::RB + (kPageTokens + slot) * T::SB;
-  if constexpr (T::kPlain) return __uint_as_float((uint32_t)((const uint16_t*)row)[c] << 16);
-  else if constexpr (FMT == THINK_PAGE_E4M3) {
+  float v, by = 1.f;
+  if constexpr (T::kPlain) {
+    v = __uint_as_float((uint32_t)((const uint16_t*)row)[c] << 16);
+  } else if constexpr (FMT == THINK_PAGE_E4M3) {
     const __half_raw h = __nv_cvt_fp8_to_halfraw(row[c], __NV_E4M3);
-    return __half2float(*(const __half*)&h) * e8m0(*sc);
+    v = __half2float(*(const __half*)&h) * e8m0(*sc);
   } else {
-    return ((row[c / 2] >> (4 * (c & 1)) & 15) - 8) * __uint_as_float((uint32_t)((const uint16_t*)sc)[c / kGroupChannels] << 16);
+    v = __uint_as_float((uint32_t)((const uint16_t*)sc)[c / kGroupChannels] << 16);
+    by = (float)((row[c / 2] >> (4 * (c & 1)) & 15) - 8);
   }
+  return fabsf(v) <= 3.402823466e38f ? 0.f : v * by;
 }
 
 template <typename T>
@@ -658,7 +669,7 @@ __device__ __forceinline__ bool unpack_rows(uint32_t from, uint32_t to, int n, i
         const int kk = k ^ turn;
         const uint32_t word = kk & 2 ? (kk & 1 ? q[3] : q[2]) : (kk & 1 ? q[1] : q[0]);
         uint4 hi, lo;
-        int4_to_bf16(word, s2, hi, lo);
+        int4_to_bf16<EDGE>(word, s2, hi, lo);
         if (drop) hi = lo = make_uint4(0u, 0u, 0u, 0u);
         const uint32_t at = to + swz(KT, 0, (4 * c + kk) ^ (r0 & 7));
         st_shared(at, hi);
@@ -1059,8 +1070,8 @@ __device__ __forceinline__ bool rows_role(const PagedPromptParams& p, typename S
             const uint8_t* const block = p.pages + page_block_offset(p.g, it.layer, page, it.h);
 #pragma unroll 1
             for (int c = 0; c < D; ++c) {
-              const float v = value_at<D, FMT>(block, tok & 63, c);
-              if (fabsf(v) <= 3.4e38f) continue;
+              const float v = non_finite_value<D, FMT>(block, tok & 63, c);
+              if (v == 0.f) continue;
               if (it.whole) dst[c] = (uint16_t)(pack_bf16(__uint_as_float((uint32_t)dst[c] << 16) + v, 0.f) & 0xffffu);
               else rec[(size_t)ri * D + c] += v;
             }

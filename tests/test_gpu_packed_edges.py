@@ -80,3 +80,52 @@ def test_large_values_at_logits_above_those_before(fmt, dtype, value):
     p.check(out, lse, lambda b, s: s < 4 or s >= t - 2)
     share = out[t:, 0, :, 5].double() / value
     assert (share > 0.25).all() and (share < 0.45).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_largest_values_in_4_bits(D, sign):
+    """A group whose largest magnitude is bf16's largest number: 7 s lies above it by 2^-9 of itself.  Rows in front of the token
+    are as without it, in keys and in values; rows that see the value are what the formula gives."""
+    t, most = 40, sign * torch.finfo(torch.bfloat16).max
+
+    def edit(x):
+        x[0, t, 0, 0, 5] = most
+
+    clean = Prompt("int4", torch.bfloat16, [100], [0], N_kv=1, G=4, D=D)
+    want, wl = clean.call()
+    for which in ("k_edit", "v_edit"):
+        p = Prompt("int4", torch.bfloat16, [100], [0], N_kv=1, G=4, D=D, **{which: edit})
+        out, lse = p.call()
+        assert torch.equal(out[:t], want[:t]) and torch.equal(lse[:t], wl[:t]), which
+        if which == "v_edit":
+            assert torch.equal(lse, wl)
+            p.check(out, lse, lambda b, s: s >= t - 1)
+
+
+def test_4_bit_values_past_32_bits_that_a_program_stored():
+    """Code 0 stands for -8, which no written row has: -8 times a scale of 1.75 * 2^125 is -1.75 * 2^128.  Rows in front of the token are
+    as without it; of the others those are compared whose outputs fit their type."""
+    tk = binding()
+    t, G, D = 40, 4, 64
+    p = Prompt("int4", torch.bfloat16, [100], [0], N_kv=1, G=G, D=D)
+    want, wl = p.call()
+    page = int(p.table[0, 0])
+    code, scale = (tk.paged_offset(p.cfg, 0, page, 0, t, part) for part in (tk.PART_V, tk.PART_V_SCALE))
+    p.pool[code + 2] = 0
+    p.pool[scale:scale + 2] = torch.tensor([0x60, 0x7e], dtype=torch.uint8, device="cuda")
+    p.k, p.v = p.exact_int4()
+    assert float(p.v[0, t].abs().max()) == 1.75 * 2.0 ** 128
+    out, lse = p.call()
+    assert torch.equal(out[:t], want[:t]) and torch.equal(lse, wl)
+    assert out[t:].isnan().sum() == 0
+    seen = 0
+    for s in range(t, 100):
+        exact, el, sizes = po.attention(*(x.double().cpu().numpy() for x in (p.q[s, 0], p.k[0, :s + 1, 0, 0], p.v[0, :s + 1, 0, 0])), p.scale)
+        sizes["vmax"] = float(p.v.abs().max())
+        tol, half, _ = bounds(sizes, s + 1, D, torch.bfloat16, el)
+        fits = (np.abs(exact) < 2.0 ** 127).all(1) & (sizes["absv"] < 2.0 ** 127).all(1)
+        err = np.abs(out[s, 0].double().cpu().numpy() - exact)
+        assert (err <= tol + half * (np.abs(exact) + tol))[fits].all()
+        seen += int(fits.sum())
+    assert seen > 100
