@@ -848,7 +848,6 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, typenam
   const uint32_t tS = tmem + lanes + half * 2 * KT, tO = tmem + lanes + T::kColO + half * D;
   const uint32_t s_full = smem_u32(&sh.s_full[half][0]), p_full = smem_u32(&sh.p_full[half][0]), o_full = smem_u32(&sh.o_full[half]);
   const int s = p.by_group.div(half * kHalf + row);    // token of the row in its item
-  const f32x2 scale2 = two(p.scale_log2, p.scale_log2);
   uint32_t s_phase = 0, o_phase = 0, e_phase = 1;
   int tile_no = 0;
   Items items{0};
@@ -869,6 +868,7 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, typenam
       }
     }
     float m = -INFINITY, l = 0.f, lc = 0.f;            // lc: what the additions to l have lost
+    float ref = 0.f, scale = p.scale_log2;             // weights: 2^(scale S + ref)
     bool seen = false;
 #pragma unroll 1
     for (; i < end; ++i) {
@@ -918,9 +918,13 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, typenam
         l *= f;
         lc *= f;
         m = m_new;
+        // A logit minus m is exact up to one rounding, but m itself is rounded: from 2^27 on (where logits that differ are 16 and
+        // more apart) both are taken so many times smaller that the rounding stays below 2^4.
+        const float less = __uint_as_float((uint32_t)(127 - max(0, (int)(__float_as_uint(m) >> 23 & 255) - (127 + 27))) << 23);
+        scale = p.scale_log2 * less;
+        ref = m == -INFINITY ? 0.f : -m * less;
       }
-      const float ref = m == -INFINITY ? 0.f : -m;
-      const f32x2 ref2 = two(ref, ref);
+      const f32x2 ref2 = two(ref, ref), scale2 = two(scale, scale);
       f32x2 ls[2] = {0ull, 0ull};
       uint32_t pk[KT / 2];
 #pragma unroll

@@ -129,3 +129,39 @@ def test_4_bit_values_past_32_bits_that_a_program_stored():
         assert (err <= tol + half * (np.abs(exact) + tol))[fits].all()
         seen += int(fits.sum())
     assert seen > 100
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS, ids=IDS)
+@pytest.mark.parametrize("scale", [1e4, 1e6, 1e8, 1e9, 1e10, 1e15, 1e25, 1e34])
+def test_large_logits(fmt, dtype, scale):
+    """Keys and queries of whole numbers, so that products are exact and equal ones equal: with such scales all the weight is on the
+    tokens with a row's largest product, in equal shares.  Only roundings of the weights' quotient and of the output are left.
+    fp32 caches scale the queries first, which rounds them: equal products of 64 channels come to differ by up to 64 * 2^-24 of
+    sums of some 10^2 * scale * 1.44, above 1 for every scale here.  There the general bounds hold, which allow that."""
+    g = gen(3)
+
+    def keys(k):
+        k.copy_(torch.randint(-7, 8, k.shape, generator=g, device="cuda"))
+        k[..., ::32] = 7                       # (4-bit groups then have a scale of 1)
+
+    p = Prompt(fmt, dtype, [150, 4], [30, 4000], N_kv=1, G=4, D=64, k_edit=keys, scale=scale)
+    p.q.copy_(torch.randint(-3, 4, p.q.shape, generator=g, device="cuda"))
+    out, lse = p.call()
+    assert out.isfinite().all() and lse.isfinite().all()
+    if dtype == torch.float32:
+        with np.errstate(over="ignore"):
+            p.check(out, lse, lambda b, s: s % 7 == 0)
+        return
+    w, half = 2.0 ** -8, torch.finfo(dtype).eps / 2
+    for b in range(2):
+        for s in range(p.rows[b]):
+            n = p.held[b] + s + 1
+            q, k, v = p.at(p.q, b)[s, 0].double(), p.k[b, :n, 0, 0].double(), p.v[b, :n, 0, 0].double()
+            x = q @ k.T
+            share = (x == x.max(1, keepdim=True).values).double()
+            share /= share.sum(1, keepdim=True)
+            want, size = share @ v, share @ v.abs()
+            tol = w * size
+            assert ((p.at(out, b)[s, 0].double() - want).abs() <= tol + half * (want.abs() + tol)).all(), (b, s)
+            top = x.max(1).values * scale      # the logarithm of the number of such tokens, 9 at most, aside
+            assert ((p.at(lse, b)[s, 0].double() - top).abs() <= 9 + 2.0 ** -20 * top.abs()).all(), (b, s)
