@@ -920,7 +920,8 @@ __device__ __forceinline__ bool softmax_role(const PagedPromptParams& p, typenam
         m = m_new;
         // A logit minus m is exact up to one rounding, but m itself is rounded: from 2^27 on (where logits that differ are 16 and
         // more apart) both are taken so many times smaller that the rounding stays below 2^4.
-        const float less = __uint_as_float((uint32_t)(127 - max(0, (int)(__float_as_uint(m) >> 23 & 255) - (127 + 27))) << 23);
+        const int e = (int)(__float_as_uint(m) >> 23 & 255);
+        const float less = __uint_as_float((uint32_t)(127 - (e < 255 ? max(0, e - (127 + 27)) : 0)) << 23);
         scale = p.scale_log2 * less;
         ref = m == -INFINITY ? 0.f : -m * less;
       }

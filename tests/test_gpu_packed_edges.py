@@ -165,3 +165,12 @@ def test_large_logits(fmt, dtype, scale):
             assert ((p.at(out, b)[s, 0].double() - want).abs() <= tol + half * (want.abs() + tol)).all(), (b, s)
             top = x.max(1).values * scale      # the logarithm of the number of such tokens, 9 at most, aside
             assert ((p.at(lse, b)[s, 0].double() - top).abs() <= 9 + 2.0 ** -20 * top.abs()).all(), (b, s)
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS, ids=IDS)
+@pytest.mark.parametrize("scale", [1e-5, 1e-30, 1e-42])
+def test_small_scales(fmt, dtype, scale):
+    """Some rows see nothing in pieces of their item in which others do."""
+    p = Prompt(fmt, dtype, [70, 3], [30, 200], N_kv=1, G=4, D=64, scale=scale)
+    out, lse = p.call()
+    p.check(out, lse)
