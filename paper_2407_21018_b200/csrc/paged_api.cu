@@ -33,6 +33,7 @@ struct Geometry {
   PageGeom g;
   int N_q, G, dtype, format, max_batch, elem;
   float scale_log2;
+  double scale_log2_wide;
 };
 
 // Offsets in the workspace (and in a scratch buffer, whose error word is not used).  Partial states lie at the same
@@ -70,7 +71,8 @@ thinK_status make_geometry(const thinK_paged_config* c, Geometry* o) {
   // the pool's size in bytes has to fit a signed 64-bit offset
   if ((double)c->L * c->num_pages * c->N_kv * r.g.block_bytes > 4.0e18) return THINK_ERR_UNSUPPORTED;
   const double scale = c->softmax_scale == 0.0 ? 1.0 / sqrt((double)c->D) : c->softmax_scale;
-  r.scale_log2 = (float)(scale * kLog2e);
+  r.scale_log2_wide = scale * kLog2e;
+  r.scale_log2 = (float)r.scale_log2_wide;
   *o = r;
   return THINK_OK;
 }
@@ -375,6 +377,11 @@ thinK_status thinK_paged_prompt_attn(thinK_paged* p, thinK_tensor5 q, thinK_tens
   d.N_q = p->g.N_q; d.G = p->g.G;
   d.layer0 = layer0; d.nlayers = nlayers;
   d.scale_log2 = p->g.scale_log2;
+  if (p->g.dtype == THINK_BF16) {
+    const PromptScale scale(p->g.scale_log2_wide);
+    d.scale_log2 = scale.logits;
+    d.q_scale2 = (uint32_t)(127 + scale.queries) << 7 | (uint32_t)(127 + scale.queries) << 23;
+  }
   d.error = (uint32_t*)p->ws;
   d.desc = (PromptDesc*)scratch;
   d.records = (uint8_t*)scratch + align_up(sizeof(PromptDesc) * kSMs, 256);

@@ -7,6 +7,8 @@
 // items of a sequence have a closed form, so a place is found without a list.  The line runs over layers and key heads,
 // in each over the sequences, and is cut evenly, or every item is: a part owns the tiles that stand in it.
 #pragma once
+#include <math.h>
+
 #include "paged_split.h"
 
 namespace think {
@@ -35,6 +37,21 @@ THINK_HD int prompt_quotient(int64_t place, int64_t length) {
   while ((q + 1) * length <= place) ++q;
   return (int)q;
 }
+
+// The softmax scale in base 2 as a power of two on the queries, which bf16 ones above 2^-126 / scale take exactly (2^-126 at the least:
+// a scale below that leaves all weights alike anyway), and what is left of it on the logits, 1 to 2 for scales up to 1.  A logit then passes fp32 only where
+// the formula's does, not the product of a query and a key.  Never 0, so that a masked logit, -infinity, stays what it is.
+struct PromptScale {
+  int queries;                // exponent
+  float logits;
+  explicit PromptScale(double scale_log2) {
+    int e;
+    frexp(scale_log2, &e);
+    queries = e - 1 < -126 ? -126 : e - 1 > 0 ? 0 : e - 1;
+    logits = (float)ldexp(scale_log2, -queries);
+    if (!(logits >= 1.17549435e-38f)) logits = 1.17549435e-38f;
+  }
+};
 
 struct PromptCut {
   int extra;                  // places of an item besides its tokens

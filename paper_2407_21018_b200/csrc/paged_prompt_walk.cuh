@@ -15,7 +15,8 @@ struct PagedPromptParams {
   int max_rows;
   int N_q, G, per;            // per: new tokens of an item
   int layer0, nlayers;
-  float scale_log2;
+  float scale_log2;           // on logits
+  uint32_t q_scale2;          // on bf16 queries or on e4m3 keys, two bf16: see PromptScale
   uint32_t* error;
   PromptDesc* desc;           // one per CTA
   uint8_t* records;           // two per CTA

@@ -174,3 +174,48 @@ def test_small_scales(fmt, dtype, scale):
     p = Prompt(fmt, dtype, [70, 3], [30, 200], N_kv=1, G=4, D=64, scale=scale)
     out, lse = p.call()
     p.check(out, lse)
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS, ids=IDS)
+@pytest.mark.parametrize("scale", [0.0, 1.0, 2.0 ** -60])
+def test_products_past_32_bits(fmt, dtype, scale):
+    """A key next to the largest bf16 number: its products with queries pass fp32, its logits do not (those that do, with a scale of 1,
+    are infinite in the formula in fp32 as well and not looked at)."""
+    t, most = 40, 1.75 * 2.0 ** 127
+
+    def edit(x):
+        x[0, t, 0, 0, 5] = most
+
+    p = Prompt(fmt, dtype, [100], [0], N_kv=1, G=4, D=64, k_edit=edit, scale=scale)
+    p.q.clamp_(-1.75, 1.75)
+    if scale == 1.0:
+        p.q[..., 5] *= 0.25
+    out, lse = p.call()
+    assert out.isfinite().all() and lse.isfinite().all()
+    p.check(out, lse, lambda b, s: s < t)
+    # Behind it the bounds, relative to such a logit, are infinite.  But it is above or below all others by 2^50 and more, so a row
+    # holds that token's value, or what it would hold without that token.
+    q, k, v = (x.double().cpu().numpy() for x in (p.q[:, 0], p.k[0, :, 0, 0], p.v[0, :, 0, 0]))
+    half = torch.finfo(dtype).eps / 2
+    for s in range(t, 100):
+        for g in range(4):
+            x = float(q[s, g] @ k[t]) * p.scale
+            assert abs(x) > 2.0 ** 50
+            others = [i for i in range(s + 1) if i != t]
+            if x > 0:
+                want, wl, tol, ltol = v[t], x, 2.0 ** -8 * np.abs(v[t]), 2.0 ** -20 * abs(x)
+            else:
+                want, wl, sizes = po.attention(q[s, g:g + 1], k[others], v[others], p.scale)
+                sizes["vmax"] = np.abs(v).max()
+                tol, _, ltol = bounds(sizes, s + 1, 64, dtype, wl)
+                want, wl, tol, ltol = want[0], wl[0], tol[0], ltol[0]
+            assert (np.abs(out[s, 0, g].double().cpu().numpy() - want) <= tol + half * (np.abs(want) + tol)).all(), (s, g)
+            assert abs(float(lse[s, 0, g]) - wl) <= ltol, (s, g)
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS, ids=IDS)
+@pytest.mark.parametrize("scale", [1e-46, 1e-60, 1e-300])
+def test_scales_next_to_nothing(fmt, dtype, scale):
+    p = Prompt(fmt, dtype, [70, 3], [30, 200], N_kv=1, G=4, D=64, scale=scale)
+    out, lse = p.call()
+    p.check(out, lse)

@@ -42,3 +42,28 @@ int main() {
 }
 """)
     assert out.split() == ["0", "1"]
+
+
+def test_scale_of_the_logits(tmp_path):
+    """The power of two on the queries times what is left on the logits is the scale, at every exponent; what is left is never 0 and
+    is 1 to 2 wherever the scale is below 1 and has an exponent of fp32."""
+    out = compile_and_run(tmp_path, r"""
+#include <stdio.h>
+#include "paged_prompt.h"
+using namespace think;
+int main() {
+  long bad = 0;
+  for (int e = -1074; e <= 127; ++e)
+    for (double f : {1.0, 1.25, 1.9999}) {
+      const double x = ldexp(f, e);
+      if (x == 0 || x > 3.4e38) continue;
+      const PromptScale s(x);
+      bad += s.queries > 0 || s.queries < -126 || !(s.logits >= 1.17549435e-38f) || s.logits > 3.4028235e38f;
+      if (e >= -126) bad += fabs(ldexp((double)s.logits, s.queries) / x - 1) > ldexp(1, -24);
+      if (e >= -126 && e < 0) bad += s.logits < 1 || s.logits >= 2.0001f || s.queries != e;
+      if (e >= 0) bad += s.queries != 0;
+    }
+  printf("%ld\n", bad);
+}
+""")
+    assert out.split() == ["0"]
