@@ -495,7 +495,8 @@ thinK_status thinK_paged_decode_attn(thinK_paged* p, const void* q, void* out, f
  * A count of rows above max_rows, a start outside the packed rows, a negative position and tokens behind the table's end
  * set bit 16 of the error word: rows are cut to what there is, tokens that have no page are left out.  A row without
  * tokens gets out = 0 and lse = -infinity; one with tokens whose logits are all -infinity out = NaN and lse = -infinity.
- * What a row does not see does not reach it, whatever it holds (NaN, infinities).
+ * What a row does not see does not reach it, whatever it holds (NaN, infinities); what it sees does: an infinite value gives an
+ * infinity or a NaN, however small its weight.
  * Logits, softmax sums and outputs are accumulated in fp32 from the stored values, which enter exactly (4-bit ones, of 11
  * bits, as the sum of two bf16; values past bf16's largest, which a row that holds that number may be stored as in E4M3, count as
  * infinite as they do when read back, 4-bit ones from 2^129 - 2^121 on, which no written row holds).  On bf16 caches a weight meets the values rounded to bf16 (2^-8 of itself at most; weights

@@ -225,16 +225,19 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 2) k_paged_prompt_join(const 
   for (int i0 = 0; i0 < pieces; i0 += 32) {
     const int i = i0 + lane;
     float f = 0.f, fl = 0.f;
+    bool some = false;                              // tokens: their values count however small their weights (0 times infinity is a NaN)
     if (there(i)) {
       const float x = rec(i)[ROWS * D + r], y = rec(i)[ROWS * (D + 1) + r];
+      some = !(y == 0.f);
       f = x == -INFINITY ? (y == y ? 0.f : y) : exp2f(x - m);      // (a sum may be NaN under a maximum of -infinity)
       fl = f * y;
     }
+    const uint32_t with = __ballot_sync(0xffffffffu, some);
 #pragma unroll 4
     for (int k = 0; k < min(32, pieces - i0); ++k) {
       const float g = __shfl_sync(0xffffffffu, f, k);
       l += __shfl_sync(0xffffffffu, fl, k);
-      if (g == 0.f) continue;
+      if (!(with >> k & 1)) continue;
       const float* const src = rec(i0 + k) + (size_t)r * D + lane * W;
       float v[W];
       if constexpr (W == 4) *(float4*)v = *(const float4*)src; else *(float2*)v = *(const float2*)src;

@@ -219,3 +219,27 @@ def test_scales_next_to_nothing(fmt, dtype, scale):
     p = Prompt(fmt, dtype, [70, 3], [30, 200], N_kv=1, G=4, D=64, scale=scale)
     out, lse = p.call()
     p.check(out, lse)
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS, ids=IDS)
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+@pytest.mark.parametrize("held", [20, 300, 9000])
+def test_values_that_are_not_finite_at_weights_of_next_to_nothing(fmt, dtype, value, held):
+    """The first tokens, up to 200 of them, have logits hundreds of powers of two below the others: a NaN or an infinity among them is
+    in the output of all rows, whether their item is one piece or cut, and whether it shares a piece with heavier ones or not."""
+    def keys(k):
+        k[:] = 1.0
+        k[0, :min(200, held - 8)] = -8.0
+
+    def values(v):
+        v[0, 10, 0, 0, 7] = value
+
+    clean = Prompt(fmt, dtype, [5], [held], N_kv=1, G=4, D=64, k_edit=keys)
+    p = Prompt(fmt, dtype, [5], [held], N_kv=1, G=4, D=64, k_edit=keys, v_edit=values)
+    for x in (clean, p):
+        x.q.abs_().add_(1.0)
+    (want, wl), (out, lse) = clean.call(), p.call()
+    bad = slice(0, 64) if fmt == "e4m3" else slice(0, 32) if fmt == "int4" else slice(7, 8)       # (a quantised row or group is all NaN)
+    assert not out[..., bad].isfinite().any()
+    keep = [c for c in range(64) if not bad.start <= c < bad.stop]
+    assert torch.equal(out[..., keep], want[..., keep]) and torch.equal(lse, wl)
