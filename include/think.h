@@ -501,7 +501,10 @@ thinK_status thinK_paged_decode_attn(thinK_paged* p, const void* q, void* out, f
  * bits, as the sum of two bf16; values past bf16's largest, which a row that holds that number may be stored as in E4M3, count as
  * infinite as they do when read back, 4-bit ones from 2^129 - 2^121 on, which no written row holds).  On bf16 caches a weight meets the values rounded to bf16 (2^-8 of itself at most; weights
  * below 2^-118 of the largest may count as none); the softmax sum takes it unrounded.  fp32 caches compute in fp32.  Results do not
- * depend on timing. */
+ * depend on timing.
+ * THINK_ERR_UNSUPPORTED where 64 * max_pages + max_rows passes 2^31 - 1, where (max_rows * N_q / N_kv / 256 + 1) * (64 * max_pages +
+ * max_rows + 384) * B * nlayers * N_kv passes 4e15 (fp32: 64 in place of 256 and 384; packed rows count for every entry), and where
+ * the kernel could not be set up when the handle was created (its other calls work all the same). */
 thinK_status thinK_paged_prompt_attn(thinK_paged* p, thinK_tensor5 q, thinK_tensor5 out, float* lse, thinK_page_table table,
                                      const int32_t* pos, const int32_t* rows, const int32_t* start, int32_t max_rows,
                                      void* scratch, size_t scratch_bytes, int32_t layer0, int32_t nlayers, void* stream);

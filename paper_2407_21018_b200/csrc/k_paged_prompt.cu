@@ -288,8 +288,9 @@ cudaError_t setup_fp32() {
 }  // namespace
 
 cudaError_t paged_prompt_setup(int dtype, int format, int D) {
-  if (dtype == THINK_BF16) return paged_prompt_tc_setup(format, D);
-  return D == 128 ? setup_fp32<128>() : setup_fp32<64>();
+  const cudaError_t e = dtype == THINK_BF16 ? paged_prompt_tc_setup(format, D) : D == 128 ? setup_fp32<128>() : setup_fp32<64>();
+  if (e != cudaSuccess) (void)cudaGetLastError();    // reported by the call that needs the kernel
+  return e;
 }
 int paged_prompt_rows(int dtype) { return dtype == THINK_BF16 ? paged_prompt_tc_rows() : kRows; }
 PromptCut paged_prompt_cut(int dtype) { return dtype == THINK_BF16 ? paged_prompt_tc_cut() : PromptCut{kExtra}; }

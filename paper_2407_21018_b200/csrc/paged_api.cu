@@ -116,7 +116,7 @@ struct thinK_paged {
   uint8_t* ws;
   int grid;
   CUtensorMap map;           // bf16 caches of plain pages: see launch_paged_prompt
-  bool mapped;
+  bool attends;              // thinK_paged_prompt_attn can run: its kernel and, where it needs one, the map are in order
 };
 
 namespace {
@@ -204,7 +204,6 @@ thinK_status thinK_paged_create(const thinK_paged_config* cfg, const thinK_paged
   int dev = 0, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
       paged_decode_setup(p->g.dtype, p->g.format, p->g.g.D, p->g.G) != cudaSuccess ||
-      paged_prompt_setup(p->g.dtype, p->g.format, p->g.g.D) != cudaSuccess ||
       cudaMemset(p->ws, 0, p->w.records) != cudaSuccess ||
       cudaMemset(p->ws + p->w.counters, 0, p->w.total - p->w.counters) != cudaSuccess || cudaStreamSynchronize(cudaStreamLegacy) != cudaSuccess) {
     delete p;
@@ -212,7 +211,8 @@ thinK_status thinK_paged_create(const thinK_paged_config* cfg, const thinK_paged
   }
   p->grid = sms < kSMs ? sms : kSMs;                 // one wave, one CTA an SM
   memset(&p->map, 0, sizeof(p->map));
-  p->mapped = p->g.dtype == THINK_BF16 && p->g.format == THINK_PAGE_PLAIN && map_pool(p);
+  p->attends = paged_prompt_setup(p->g.dtype, p->g.format, p->g.g.D) == cudaSuccess &&
+               (p->g.dtype != THINK_BF16 || p->g.format != THINK_PAGE_PLAIN || map_pool(p));
   *out = p;
   return THINK_OK;
 }
@@ -342,7 +342,7 @@ thinK_status thinK_paged_prompt_attn(thinK_paged* p, thinK_tensor5 q, thinK_tens
   if (start) q.stride_b = out.stride_b = 0;
   if (!view_ok(q, p->g.elem) || !view_ok(out, p->g.elem) || !scratch || !aligned(scratch, 256)) return THINK_ERR_INVALID_ARG;
   if (scratch_bytes < thinK_paged_prompt_scratch(p)) return THINK_ERR_CAPACITY;
-  if (p->g.dtype == THINK_BF16 && p->g.format == THINK_PAGE_PLAIN && !p->mapped) return THINK_ERR_UNSUPPORTED;
+  if (!p->attends) return THINK_ERR_UNSUPPORTED;
   const int B = start ? 1 : table.B, unit = 16 / p->g.elem;
   auto view = [&](const thinK_tensor5& t) {
     return RowView{{t.stride_b / unit, t.stride_s / unit, t.stride_l / unit, t.stride_n / unit}, {B, max_rows, nlayers, p->g.N_q}, p->g.g.D / unit};

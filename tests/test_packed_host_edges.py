@@ -1,6 +1,13 @@
 """CPU checks of packed batches where a call or a kernel goes wrong: what the host side of an entry point answers, and what a
 kernel may trust."""
-from test_paged_host import compile_and_run
+import ctypes as C
+import os
+import subprocess
+
+import pytest
+
+from test_packed_host import FAKE
+from test_paged_host import ROOT, compile_and_run, tk  # noqa: F401
 
 
 def test_descriptors_that_nobody_wrote(tmp_path):
@@ -67,3 +74,32 @@ int main() {
 }
 """)
     assert out.split() == ["0"]
+
+
+@pytest.mark.parametrize("broken", ["setup", "map"])
+@pytest.mark.parametrize("dtype,fmt", [(0, 0), (0, 1), (0, 2), (1, 0)])
+def test_a_cache_without_prompt_attention(tk, tmp_path, broken, dtype, fmt):  # noqa: F811
+    """Where the attention's kernel or the map of the pool cannot be set up, that call alone is refused."""
+    fake = FAKE.replace("paged_prompt_setup(int, int, int) { return cudaSuccess; }", "paged_prompt_setup(int, int, int) { return cudaErrorLaunchOutOfResources; }"
+                        ) if broken == "setup" else FAKE.replace("return CUDA_SUCCESS; }", "return CUDA_ERROR_INVALID_VALUE; }")
+    assert fake != FAKE
+    (tmp_path / "fake.cpp").write_text("#include <cuda.h>\n" + fake)
+    csrc, so = os.path.join(ROOT, "paper_2407_21018_b200", "csrc"), str(tmp_path / "fake.so")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-Wl,-Bsymbolic", "-I", os.path.join(ROOT, "include"), "-I", csrc,
+                    "-I", "/usr/local/cuda/include", "-x", "c++", os.path.join(csrc, "paged_api.cu"), str(tmp_path / "fake.cpp"), "-o", so],
+                   check=True, capture_output=True)
+    lib = C.CDLL(so)
+    for name in ("thinK_paged_bytes", "thinK_paged_create", "thinK_paged_write", "thinK_paged_decode_attn", "thinK_paged_prompt_attn",
+                 "thinK_paged_prompt_scratch"):
+        real = getattr(tk.lib, name)
+        getattr(lib, name).argtypes, getattr(lib, name).restype = real.argtypes, real.restype
+    cfg, need, h = tk.make_paged_config(2, 8, 4, 128, 10, 8, dtype, fmt), tk.PagedSizes(), C.c_void_p()
+    assert lib.thinK_paged_bytes(C.byref(cfg), C.byref(need)) == 0
+    assert lib.thinK_paged_create(C.byref(cfg), C.byref(need), 1 << 40, 1 << 41, C.byref(h)) == 0
+    rows, table = tk.Tensor5(1 << 30, 4096, 1024, 512, 128), tk.PageTable(4096, 4, 4, 3)
+    assert lib.thinK_paged_write(h, rows, tk.Tensor5(1 << 31, 4096, 1024, 512, 128), table, None, None, 4, 0, 2, None) == 0
+    assert lib.thinK_paged_decode_attn(h, 1 << 30, 1 << 31, None, table, 4096, None, 0, 0, 2, None) == 0
+    q, out = tk.Tensor5(1 << 30, 4 * 2048, 2048, 1024, 128), tk.Tensor5(1 << 31, 4 * 2048, 2048, 1024, 128)
+    refused = broken == "setup" or (dtype, fmt) == (0, 0)         # (only bf16 pages of plain rows have a map)
+    assert lib.thinK_paged_prompt_attn(h, q, out, None, table, None, None, None, 4, 1 << 34, lib.thinK_paged_prompt_scratch(h), 0, 2, None) == (
+        tk.ERR_UNSUPPORTED if refused else 0)
