@@ -353,7 +353,7 @@ thinK_status thinK_rope_apply(const thinK_rope* r, thinK_tensor5 q, thinK_tensor
   if (tokens > 64) tokens = 64;
   if (tokens < 1) tokens = 1;
   p.tokens = tokens;
-  p.blocks_s = (S + tokens - 1) / tokens;
+  p.blocks_s = (int)(((int64_t)S + tokens - 1) / tokens);
   if ((int64_t)p.blocks_s * B > INT32_MAX) return THINK_ERR_UNSUPPORTED;
   p.by_items = FastDiv((uint32_t)p.items);
   p.by_units = FastDiv((uint32_t)p.units);

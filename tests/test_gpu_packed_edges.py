@@ -9,6 +9,7 @@ import pytest
 import torch
 
 from oracle import paged_oracle as po
+from test_gpu_packed import check_rope, make_rope
 from test_gpu_prompt import FMT, IDS, KINDS, PAGE, Prompt, binding, bounds, gen, ints
 
 pytestmark = pytest.mark.gpu
@@ -243,3 +244,17 @@ def test_values_that_are_not_finite_at_weights_of_next_to_nothing(fmt, dtype, va
     assert not out[..., bad].isfinite().any()
     keep = [c for c in range(64) if not bad.start <= c < bad.stop]
     assert torch.equal(out[..., keep], want[..., keep]) and torch.equal(lse, wl)
+
+
+@pytest.mark.parametrize("S", [2 ** 31 - 64, 2 ** 31 - 1])
+def test_rope_of_the_longest_axis(S):
+    """34 GB of rows of 16 bytes; a block has 64 of them, so the last numbers of rows round up past 2^31."""
+    r, freq, m = make_rope(8, torch.bfloat16, 8, "halves", "plain")
+    x = torch.empty(1, S, 1, 1, 8, dtype=torch.bfloat16, device="cuda")
+    at = [0, 1, 63, 64, 2 ** 30 - 1, 2 ** 30, S - 65, S - 64, S - 2, S - 1]
+    rows = torch.randn(len(at), 1, 1, 8, generator=gen(1), device="cuda").to(torch.bfloat16)
+    for i, s in enumerate(at):
+        x[0, s] = rows[i]
+    r.apply(x, None, ints([0]))
+    got = torch.stack([x[0, s] for s in at])
+    check_rope(rows[None], got[None], [at], [[True] * len(at)], torch.bfloat16, 8, "halves", freq, m, False)
