@@ -258,3 +258,44 @@ def test_rope_of_the_longest_axis(S):
     r.apply(x, None, ints([0]))
     got = torch.stack([x[0, s] for s in at])
     check_rope(rows[None], got[None], [at], [[True] * len(at)], torch.bfloat16, 8, "halves", freq, m, False)
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS, ids=IDS)
+@pytest.mark.parametrize("B,most,held", [(33, 40, 300), (64, 3, 90), (65, 90, 40), (129, 20, 200), (1000, 2, 70)])
+def test_batches_of_more_sequences_than_lanes(fmt, dtype, B, most, held):
+    """A lane of the warp that looks for a block's place has several sequences, some without rows; first and last rows of all."""
+    r = np.random.default_rng(B)
+    rows = r.integers(0, most + 1, B)
+    rows[r.random(B) < 0.3] = 0
+    rows[[0, B - 1]] = 0, most
+    rows, before = rows.tolist(), r.integers(0, held + 1, B).tolist()
+    p = Prompt(fmt, dtype, rows, before, N_kv=1, G=2, D=64, packed=B % 2 == 1, seed=B)
+    out, lse = p.call()
+    p.check(out, lse, lambda b, s: s in (0, rows[b] - 1))
+    assert p.cache.device_error() == 0
+    again = p.call()
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS[:3], ids=IDS[:3])
+def test_a_token_of_each_of_4096_sequences(fmt, dtype):
+    B = 4096
+    r = np.random.default_rng(2)
+    before = r.integers(0, 130, B).tolist()
+    p = Prompt(fmt, dtype, [1] * B, before, N_kv=1, G=1, D=64)
+    out, lse = p.call()
+    p.check(out, lse, lambda b, s: b % 5 == 0 or b > B - 40)
+    want, wl = p.cache.decode_attn(p.q, p.table, p.pos + 1, return_lse=True)
+    vmax = float(p.v.abs().max())
+    assert (out.double() - want.double()).abs().max() <= vmax * (2.0 ** -7 if dtype == torch.bfloat16 else 2.0 ** -13)
+    assert (lse - wl).abs().max() <= 2.0 ** -13
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS, ids=IDS)
+@pytest.mark.parametrize("G", [3, 4, 8])
+def test_last_rows_of_every_sequence(fmt, dtype, G):
+    """The last item of a sequence is not full, and the next sequence's rows follow it at once."""
+    rows, held = [33, 1, 70, 2, 86, 64, 5, 257], [100, 0, 64, 500, 1, 0, 63, 10]
+    p = Prompt(fmt, dtype, rows, held, N_kv=1, G=G, D=128, seed=G)
+    out, lse = p.call()
+    p.check(out, lse, lambda b, s: s >= rows[b] - 3)
