@@ -63,7 +63,8 @@ def test_plan_around_48_kb_of_shared_memory():
 
 @pytest.mark.parametrize("fmt,dtype", KINDS, ids=IDS)
 @pytest.mark.parametrize("value", [2.0 ** 127, -1.75 * 2.0 ** 126])
-def test_large_values_at_logits_above_those_before(fmt, dtype, value):
+@pytest.mark.parametrize("N_kv,G", [(1, 4), (160, 1)], ids=["a tile a block", "an item a block"])
+def test_large_values_at_logits_above_those_before(fmt, dtype, value, N_kv, G):
     """A token in the second tile has a weight of e^4 relative to all tokens of the first, and a value next to the type's largest: its
     share is 0.3 of that value, whatever the weights are relative to on the way."""
     t, n = 90, 120
@@ -73,9 +74,9 @@ def test_large_values_at_logits_above_those_before(fmt, dtype, value):
         k[0, t] = 2.0
 
     def values(v):
-        v[0, t, 0, 0, 5] = value
+        v[0, t, 0, :, 5] = value
 
-    p = Prompt(fmt, dtype, [n], [0], N_kv=1, G=4, D=64, k_edit=keys, v_edit=values)
+    p = Prompt(fmt, dtype, [n], [0], N_kv=N_kv, G=G, D=64, k_edit=keys, v_edit=values)
     p.q.fill_(0.25)
     out, lse = p.call()
     p.check(out, lse, lambda b, s: s < 4 or s >= t - 2)
