@@ -300,3 +300,37 @@ def test_last_rows_of_every_sequence(fmt, dtype, G):
     p = Prompt(fmt, dtype, rows, held, N_kv=1, G=G, D=128, seed=G)
     out, lse = p.call()
     p.check(out, lse, lambda b, s: s >= rows[b] - 3)
+
+
+@pytest.mark.parametrize("fmt,dtype", [KINDS[0], KINDS[2], KINDS[3]], ids=[IDS[0], IDS[2], IDS[3]])
+@pytest.mark.parametrize("scale,grow", [(1e-3, 0), (1e6, 0), (1e9, 0), (1e25, 0), (1.0, 10), (100.0, 14), (1e-4, 14)])
+def test_large_logits_in_pieces_of_many_tiles(fmt, dtype, scale, grow):
+    """More items than blocks, six tiles each; with `grow` the keys of a tile are 2^grow times those of the tile before, so that a row's
+    largest logit passes through all sizes.  Whole numbers times powers of two: products are exact, and from some size on all of the
+    weight is on the largest."""
+    N, n, g = 150, 384, gen(5)
+
+    def keys(k):
+        k.copy_(torch.randint(-7, 8, k.shape, generator=g, device="cuda"))
+        k[..., ::32] = 7                       # (4-bit groups then have a power of two as scale)
+        k *= 2.0 ** (grow * (torch.arange(k.shape[1], device="cuda") // PAGE)[None, :, None, None, None])
+
+    p = Prompt(fmt, dtype, [8], [n - 8], N_kv=N, G=1, D=64, k_edit=keys, scale=scale)
+    p.q.copy_(torch.randint(-3, 4, p.q.shape, generator=g, device="cuda"))
+    out, lse = p.call()
+    half = torch.finfo(dtype).eps / 2
+    for s in range(8):
+        m = n - 8 + s + 1
+        q, k, v = p.q[s, 0].double(), p.k[0, :m, 0].double(), p.v[0, :m, 0].double()
+        x = torch.einsum("hd,nhd->hn", q, k) * scale
+        w = torch.softmax(x, 1)
+        want, size = torch.einsum("hn,nhd->hd", w, v), torch.einsum("hn,nhd->hd", w, v.abs())
+        # A logit x = scale * product carries the scale's rounding, its own and the reference's, 2^-22 |x| with room: that counts where
+        # tokens other than the largest have weight.  Equal products stay equal.
+        top = x.max(1, keepdim=True).values
+        near = ((x > top - 40) & (x < top)).any(1)                   # others that carry weight
+        err = torch.where(near, 2.0 ** -22 * (top.squeeze(1).abs() + 40), torch.zeros_like(top.squeeze(1)))
+        tol = (2.0 ** -8 + 2.0 ** -13 + torch.expm1(2 * err))[:, None] * size
+        assert ((out[s, 0].double() - want).abs() <= tol + half * (want.abs() + tol)).all(), s
+        wl = torch.logsumexp(x, 1)
+        assert ((lse[s, 0].double() - wl).abs() <= err + 2.0 ** -10 + 2.0 ** -20 * wl.abs() + (top.squeeze(1).abs() > 2.0 ** 26) * 9).all(), s
