@@ -570,7 +570,8 @@ double thinK_rope_frequency(const thinK_rope* r, int32_t pair);
  *   transpose: 1 turns by -t f_j (with the same m): the gradient of a loss with respect to q and k from those with
  *           respect to q_out and k_out.
  * q_out may be q itself (same pointer and strides), k_out k; apart from that no row of q_out and k_out may share memory with
- * another row of the two, nor with one of q or k (THINK_ERR_INVALID_ARG).  q and k may repeat rows (strides of 0). */
+ * another row of the two, nor with one of q or k (THINK_ERR_INVALID_ARG).  q and k may repeat rows (strides of 0).
+ * THINK_ERR_UNSUPPORTED for more than 2^24 pieces of 16 bytes in all rows of a token, and for more than 2^31 - 1 blocks of tokens. */
 thinK_status thinK_rope_apply(const thinK_rope* r, thinK_tensor5 q, thinK_tensor5 k, thinK_tensor5 q_out, thinK_tensor5 k_out,
                               int32_t B, int32_t S, int32_t nlayers, int32_t N_q, int32_t N_kv, const int32_t* pos,
                               int64_t pos_stride, const int32_t* rows, int32_t transpose, void* stream);

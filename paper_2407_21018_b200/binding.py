@@ -610,7 +610,8 @@ class PagedKVCache:
         return out if lse is None else (out, lse)
 
     def new_prompt_scratch(self) -> torch.Tensor:
-        """A scratch buffer for prompt_attn calls that may run at the same time as others of this cache."""
+        """A scratch buffer for prompt_attn calls that may run at the same time as others of this cache: on another stream, or
+        from a captured graph of their own."""
         return torch.empty(int(lib.thinK_paged_prompt_scratch(self.handle)), dtype=torch.uint8, device=self.device)
 
     def prompt_attn(self, q: torch.Tensor, table: torch.Tensor, pos: Optional[torch.Tensor] = None,
@@ -737,7 +738,8 @@ class Rope:
               q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, transpose=False, stream=None):
         """Turns q [B, S, L, N_q, D] and k [B, S, L, N_kv, D] (or either one alone), in place unless q_out and k_out are given;
         returns (q_out, k_out).  pos (int32): [B], of row 0 of each entry, or [B, S], of every row.  Packed tensors
-        [tokens, L, N, D] go with pos [tokens]."""
+        [tokens, L, N, D] go with pos [tokens].  The call works on the tensors' memory: autograd does not see it, no graph is
+        built and no version counted.  The gradient is a call with transpose=True, the caller's to make."""
         where = "thinK_rope_apply"
         like = q if q is not None else k
         if like is None or (q is None and q_out is not None) or (k is None and k_out is not None):

@@ -12,16 +12,18 @@
 // go from item to item without a pause.  One of the loading warps walks along the items and hands out their description.  m stands
 // 2^8 above the largest logit and only moves when one passes it (O is then rescaled in tensor memory), so the softmax seldom waits
 // for the products.
-// 4-bit values n * s have 11 bits: they enter as the sum of two bf16, which is exact, at twice the products.
+// 4-bit values n * s have 11 bits: they enter as the sum of two bf16, which is exact, at twice the products.  Queries (on e4m3 pages keys)
+// are taken times the power of two in the softmax scale, so that S passes fp32 no sooner than the logits.
 // P is rounded to bf16 (2^-9 of a weight on average, what the products take); l sums the unrounded weights, with what its
 // additions lose carried along, in fp32.
 //
-// What bounds it (a prompt of 8192 tokens, 32 heads of 128 over 8 key heads, 493 us replayed: 0.55 TFLOP at 1115 TFLOP/s, 0.68 of the
-// measured GEMM rate; 583 among other calls, where the clock falls): nothing alone.  Tensor pipe and exponentials are each busy
-// for 47 % of the cycles: products of 64 tokens wait for shared memory (S: 48 instead of 32 cycles each, Q and K are both read), 16
-// exponentials a cycle and SM take 1024 cycles a tile of both halves against 1280 of products, and a scheduler has one warp of each half to
-// overlap the rest of a softmax with.  e4m3 adds the unpacking (8192 tokens 620 to 750 us), 4 bits twice the products (800 us).  Few rows: DRAM
-// (8 rows over 131072 tokens, twice, 1.07 GB in 174 us).  Short calls: code that is fetched for the first time (100 tokens: 22 us,
+// What bounds it (a prompt of 8192 tokens, 32 heads of 128 over 8 key heads, 482 us replayed: 0.55 TFLOP at 1140 TFLOP/s, 0.70 of the
+// measured GEMM rate; 564 among other calls, where the clock falls): no unit.  Tensor pipe and exponentials are each busy for 47 % of
+// the cycles (a tile of both halves: 1280 cycles of products, S at 48 a product because Q and K both come from shared memory, and
+// 1024 of exponentials, against 2160).  It waits for the chain of a softmax warp: tensor memory read, maximum, vote, exponentials, packing,
+// write, arrival, with one warp of each half a scheduler.  Heads of 64 have half the products and take no fewer cycles a tile (2 x 4096
+// tokens, 12 heads: 122 to 135 us).  e4m3 adds the unpacking (8192 tokens 610 to 740 us), 4 bits twice the products (780 to 830 us).  Few rows:
+// DRAM (8 rows over 131072 tokens, twice, 1.07 GB in 173 us).  Short calls: code that is fetched for the first time (100 tokens: 22 us,
 // the join among them).  Loops stay rolled for that, and because the roles' code together misses the instruction cache.
 // Tiles of 128 tokens, whose S has one place a half, took 563 us for the same prompt; P in places of its own and S read ahead of
 // the weights of the tile before 515; exponentials in part by a polynomial, or of the halves strictly in turn, were slower too.
