@@ -45,7 +45,7 @@ import sys
 sys.path[:0] = sys.argv[1:]
 import torch
 from test_gpu_packed import check_plan, small_cache, Step
-for B in (3040, 3055, 3056, 3071, 3072, 3056, 4096):
+for B in (3040, 3055, 3056, 3071, 3073, 3056, 4096):
     step = Step([b % 130 for b in range(B)], [(b * 7) % 5 - 1 for b in range(B)], 3, 900, 2 * B)
     cache = small_cache(step.num_pages, B)
     change, lens, table, free_pages, count = step.upload()
